@@ -60,9 +60,12 @@ extern "C" {
 #define SPEC_DEV_TOKEN 2          /* token outside [0,V)                                         */
 #define SPEC_DEV_NONFINITE 3      /* a logit row holds NaN / +inf, or only -inf                  */
 #define SPEC_DEV_TIMEOUT 4        /* a bounded on-device wait ran out                            */
+#define SPEC_DEV_PAGE 5           /* a block id outside the cache, or a key beyond the block table */
+#define SPEC_DEV_BLOCKS 6         /* no free block left, or no room for one in the block table   */
 
 #define SPEC_F32 0
 #define SPEC_BF16 1
+#define SPEC_F16 2                /* the operators on projections and caches only                */
 
 typedef struct {
     int32_t B, N, V;              /* sequences, nodes per sequence (root included), vocabulary   */
@@ -257,6 +260,171 @@ int32_t spec_sample_bonus(const float *weights, int32_t R, int32_t V, const floa
 int32_t spec_host_staging_bytes(const SpecIn *in, int64_t *bytes);
 int32_t spec_verify_host(const SpecIn *in, const SpecOut *out, int32_t algorithm, void *dev_buf,
                          int64_t dev_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * The operators around a verification in a decoding loop (the target model's pass over the draft tree of
+ * Section 2, step 2, and what a paged cache of keys and values needs before and after it).
+ *
+ * A cache is num_blocks blocks of block_size slots; slot s is entry s % block_size of block s / block_size.  A request's token at
+ * position j lies at entry j % block_size of the block that its row of the block table names in column j / block_size.
+ * lengths[b] is the number of committed tokens.  The N nodes of a request's tree lie behind them: node i at entry lengths[b] + i
+ * (node 0 is the root: the token emitted last, whose keys and values are not in the cache yet), at POSITION
+ * lengths[b] + depth(i).  A request with lengths[b] < 0 takes no part: nothing of it is read but the length.  n_nodes (optional,
+ * [B]): the request's tree has n_nodes[b] <= N nodes; what belongs to the others is not read.  Status codes per request as
+ * above; a request with n_nodes[b] outside [0,N] counts as one without nodes, with SPEC_DEV_TOPOLOGY.  N is at most
+ * SPEC_MAX_NODES here too; a node may have any number of children.
+ * ------------------------------------------------------------------------------------------------ */
+
+/*
+ * Blocks, slots and positions of a step, from the requests' lengths.  Request b needs ceil((lengths[b] + nodes) / block_size) blocks
+ * and has the first owned[b] columns of its row of block_table.  What it lacks is taken, request by request, from a
+ * ring of free blocks: the free_range[1] entries of free_blocks from index free_range[0] on (mod free_size).
+ * The first request that the ring has too few blocks for, and every later one that lacks any, gets none
+ * (SPEC_DEV_BLOCKS, slots and positions -1); so does one whose row is too short, which takes none from the ring either.
+ * block_table is written in columns owned[b] .. only; owned and free_range are inputs and stay as they are, the new
+ * values are owned_out and free_range_out (other arrays): the call can be repeated.
+ * A bad tree leaves positions of -1 and SPEC_DEV_TOPOLOGY, a negative or too large block id slots of -1 and
+ * SPEC_DEV_PAGE.  Idle requests and nodes beyond n_nodes[b]: slots and positions -1.
+ */
+typedef struct {
+    int32_t B, N;
+    int32_t block_size, table_width;  /* slots of a block; columns of block_table                     */
+    const int32_t *lengths;           /* [B]                                                          */
+    const int32_t *n_nodes;           /* optional [B]                                                 */
+    const int32_t *parent;            /* [N], or [B,N] with topo_seq_stride = N                       */
+    int64_t topo_seq_stride;
+    int32_t *block_table;             /* row b at b * table_stride                                    */
+    int64_t table_stride;
+    const int32_t *owned;             /* [B]                                                          */
+    const int32_t *free_blocks;       /* [free_size]                                                  */
+    int32_t free_size;
+    const int32_t *free_range;        /* [2]: index of the first free block, number of free blocks    */
+    int32_t *slots, *positions;       /* [B,N]                                                        */
+    int32_t *owned_out;               /* [B]                                                          */
+    int32_t *free_range_out;          /* [2]                                                          */
+    int32_t *status;                  /* [B]                                                          */
+} SpecSlots;
+int32_t spec_cache_slots(const SpecSlots *a, void *stream);
+
+/*
+ * Norm and rotation of queries and keys per head, and keys and values into the cache, in one pass: for a head's row x of a query or key,
+ *   y = x / sqrt(mean(x^2) + eps) * weight   (no norm where the weight is NULL),
+ *   (a, b) -> (a cos t - b sin t, b cos t + a sin t), t = positions[token] * inv_freq[i], for the i-th of the rot/2 pairs of the first
+ *   rot entries: (y_i, y_{i + rot/2}) with pairs = 0 (halves), (y_{2i}, y_{2i+1}) with pairs = 1 (neighbours).
+ * Queries go to q_out (may be q itself), keys and values (values as they are) to slot slots[token] of the caches.
+ * Arithmetic in fp32, angles reduced in fp64, one rounding at the end.  A token whose slot is outside
+ * [0, num_blocks * block_size) is padding: nothing of it is read or written.  No two tokens may share a slot.
+ * D: a multiple of 8 up to 256; rot: a multiple of 16 up to D.  Strides in elements; the D entries of a head are contiguous.
+ */
+typedef struct {
+    int32_t T, Hq, Hkv, D, rot, pairs, dtype;   /* tokens; heads; SPEC_F32, SPEC_BF16 or SPEC_F16     */
+    int32_t num_blocks, block_size;
+    const void *q, *k, *v;
+    int64_t q_stride[2], k_stride[2], v_stride[2];              /* token, head                        */
+    const void *q_weight, *k_weight;            /* optional [D], of the same type                     */
+    float eps;
+    const float *inv_freq;                      /* [rot/2]; may be NULL for rot = 0                     */
+    const int32_t *positions, *slots;           /* [T]                                                */
+    void *q_out;
+    int64_t q_out_stride[2];
+    void *k_cache, *v_cache;
+    int64_t k_cache_stride[3], v_cache_stride[3];               /* block, slot, head                  */
+} SpecNormRope;
+int32_t spec_norm_rope_cache(const SpecNormRope *a, void *stream);
+
+/*
+ * Attention of the nodes of every request's tree over its committed tokens and the tree (Section 2, step 2: the target pass with
+ * a tree mask).  Node i of request b, at position t = lengths[b] + depth(i), sees
+ *   the committed tokens at positions j < lengths[b], and itself and its ancestors in the tree,
+ *   with window > 0 of these only the ones at positions > t - window or < sinks;
+ *   out[b,i,h] = sum_j softmax_j(scale q[b,i,h] . k_j) v_j over what it sees, k and v of head h / (Hq / Hkv).
+ * N = 1, parent = {-1}: plain decoding; parent[i] = i - 1: a stretch of a prompt.
+ * Scores, maxima and sums in fp32; probabilities are rounded to the type of the values for the product with them.
+ * A row that sees nothing (a block id outside [0, num_blocks) hides its keys and gives SPEC_DEV_PAGE) is 0, its lse -inf; so are all
+ * rows of a request with a bad tree (SPEC_DEV_TOPOLOGY).  What no node sees is not read; what a node does not see does not
+ * reach its row, whatever it holds (NaN and infinities too).  Rows of idle requests and of nodes beyond n_nodes[b] stay as they were.
+ * D: 64, 128 or 256.  q, caches and out of one type, SPEC_BF16 or SPEC_F16.  Strides in elements, multiples of 8, and bases on 16 bytes;
+ * the D entries of a head are contiguous.  lse: optional, log of sum_j exp(scale q.k_j) (natural).
+ * `ws`: spec_tree_attention_workspace_bytes() bytes (a function of the sizes; contents do not matter).
+ */
+typedef struct {
+    int32_t B, N, Hq, Hkv, D, dtype;
+    int32_t num_blocks, block_size, table_width;
+    int32_t window, sinks;            /* window 0: none                                               */
+    float scale;
+    const void *q;
+    int64_t q_stride[3];              /* request, node, head                                          */
+    const void *k_cache, *v_cache;
+    int64_t k_cache_stride[3], v_cache_stride[3];               /* block, slot, head                  */
+    const int32_t *block_table;
+    int64_t table_stride;
+    const int32_t *lengths;           /* [B]                                                          */
+    const int32_t *n_nodes;           /* optional [B]                                                 */
+    const int32_t *parent;            /* [N], or [B,N] with topo_seq_stride = N                       */
+    int64_t topo_seq_stride;
+    void *out;
+    int64_t out_stride[3];            /* request, node, head                                          */
+    float *lse;                       /* optional [B,N,Hq]                                            */
+    int32_t *status;                  /* [B]                                                          */
+} SpecAttention;
+int32_t spec_tree_attention_workspace_bytes(const SpecAttention *a, int64_t *bytes);
+int32_t spec_tree_attention(const SpecAttention *a, void *ws, int64_t ws_bytes, void *stream);
+
+/*
+ * After a verification: the accepted path's entries move behind the committed tokens, in every cache of a stack (keys and values of all
+ * layers).  The path's node at depth d = 1, 2, ... goes from entry lengths[b] + node to entry lengths[b] + d; other entries
+ * stay as they are.  lengths_out[b] = lengths[b] + depth(accepted) + 1 (the root is committed too; the correction token is the next
+ * tree's root).  accepted_node[b] = -1 (a failed verification) or an idle request: nothing moves, the length stays.
+ * accepted_node outside the tree: SPEC_DEV_TOPOLOGY, as with a bad tree; a bad block id on the path: SPEC_DEV_PAGE; then nothing of the
+ * request moves and its length stays.  The blocks that hold a request's tree must be its own.
+ */
+typedef struct {
+    int32_t B, N, caches;
+    int32_t num_blocks, block_size, table_width;
+    void *cache;                      /* row of slot e of block k of cache c: c * stride[0] + k * stride[1] + e * stride[2] bytes */
+    int64_t stride[3];
+    int64_t row_bytes;
+    const int32_t *block_table;
+    int64_t table_stride;
+    const int32_t *lengths;           /* [B]                                                          */
+    const int32_t *n_nodes;           /* optional [B]                                                 */
+    const int32_t *parent;            /* [N], or [B,N] with topo_seq_stride = N                       */
+    int64_t topo_seq_stride;
+    const int32_t *accepted_node;     /* [B]                                                          */
+    int32_t *lengths_out;             /* [B], not `lengths`                                           */
+    int32_t *status;                  /* [B]                                                          */
+} SpecCommit;
+int32_t spec_cache_commit(const SpecCommit *a, void *stream);
+
+/*
+ * Verification of drafted chains from probabilities (the single-path case of Section 3.1, for callers that have the laws
+ * already: own logit processors, grammar masks).  Request b drafted the tokens token[cu_drafts[b] .. cu_drafts[b+1]); its i-th draft (0-based) is
+ * judged by row cu_drafts[b] + b + i of target_probs and row cu_drafts[b] + i of draft_probs; the request's last
+ * target row (index cu_drafts[b+1] + b) is the law behind all drafts.  Draft i is accepted when u_accept[its index] < min(1, p(x) / q(x)) (0 where
+ * p(x) <= 0, 1 where q(x) <= 0 < p(x)); the first one rejected ends the chain, and a token is drawn by inverse CDF from
+ * norm((p - q)+) of its rows, or from the last row where all were accepted, with u_bonus of that target row.
+ * draft_probs NULL: the drafts were looked up, q is 1 at the drafted token and 0 elsewhere.
+ * Rows need not be normalised for the draw; decisions and sums in fp64.  (p - q)+ without mass: the draw is from p.
+ * A gathered probability that is negative or not finite, or a row without finite positive mass: SPEC_DEV_NONFINITE; a token outside [0,V):
+ * SPEC_DEV_TOKEN; cu_drafts that decrease, leave [0, n_drafts], or give a request more than max_drafts:
+ * SPEC_DEV_TOPOLOGY; then accept_len and tokens are -1.
+ */
+typedef struct {
+    int32_t B, V, max_drafts, dtype;  /* SPEC_F32 or SPEC_BF16                                        */
+    int64_t n_drafts;                 /* drafts of all requests                                       */
+    const void *target_probs;         /* [n_drafts + B, V], rows target_stride elements apart         */
+    const void *draft_probs;          /* [n_drafts, V], rows draft_stride elements apart, or NULL     */
+    int64_t target_stride, draft_stride;
+    const int32_t *token;             /* [n_drafts]                                                   */
+    const int32_t *cu_drafts;         /* [B + 1]                                                      */
+    const float *u_accept;            /* [n_drafts]                                                   */
+    const float *u_bonus;             /* [n_drafts + B]                                               */
+    int32_t *accept_len;              /* [B]                                                          */
+    int32_t *out_tokens;              /* [B, max_drafts + 1]: accepted drafts, the drawn token, then -1 */
+    int32_t *bonus_token;             /* [B]                                                          */
+    int32_t *status;                  /* [B]                                                          */
+} SpecChains;
+int32_t spec_verify_probs(const SpecChains *a, void *stream);
 
 /* Launch plan of SpecInfer's walk for a vocabulary size and dtype, of a batch under top-k that fills the
  * device several times over (host-only query, for benchmarks and tests; smaller batches and batches

@@ -7,7 +7,9 @@ prepared calls, the host-buffer call, the plan queries and the entry point witho
 There is no CPU fallback: a missing library or a missing CUDA device raises ``RuntimeError``.
 
 Device-resident API (inputs already in HBM, nothing is synchronised):
-    verify_specinfer / verify_traversal / tree_probs / sample_bonus
+    verify_specinfer / verify_traversal / verify_otlp / tree_probs / sample_bonus / tree_analysis
+Around a verification in a decoding loop with a paged cache (likewise):
+    cache_slots / norm_rope_cache / tree_attention / verify_probs / cache_commit
 Host API (pinned host buffers in, host results out; copies and one stream sync inside):
     HostVerifier
 """
@@ -29,7 +31,8 @@ EXPORTS = ("spec_workspace_bytes", "spec_tree_probs", "spec_verify_specinfer", "
            "spec_sample_bonus", "spec_query_plan", "spec_host_staging_bytes", "spec_verify_host",
            "spec_verify_specinfer_static", "spec_kernel_launches", "spec_analysis_workspace_bytes",
            "spec_tree_analysis", "spec_latency_model", "spec_test_hooks", "spec_row_statistics",
-           "spec_verify_otlp")
+           "spec_verify_otlp", "spec_cache_slots", "spec_norm_rope_cache", "spec_tree_attention_workspace_bytes",
+           "spec_tree_attention", "spec_cache_commit", "spec_verify_probs")
 
 
 class SpecIn(C.Structure):
@@ -124,6 +127,7 @@ def _calls():
         except ImportError as e:
             raise RuntimeError(f"the native host path is missing: build it with `python -m paper_2602_16994_b200.build` ({e})")
         _torch_calls.init(LIB_PATH, VerifyOutputs, AnalysisOutputs)
+        _torch_calls.init_step(LIB_PATH, SlotOutputs, AttentionOutputs, CommitOutputs, ChainOutputs)
         _native = _torch_calls
     return _native
 
@@ -388,6 +392,97 @@ def tree_probs(logits, which=0, temperature=1.0, top_k=0, top_p=1.0, temperature
 def sample_bonus(weights, u, want_margin=False, stream=None):
     """Inverse-CDF draw from each row of ``weights`` [R,V] float32 with uniforms ``u`` [R]."""
     return _calls().sample_bonus(weights, u, want_margin, stream)
+
+
+@dataclass
+class SlotOutputs:
+    slots: torch.Tensor          # [B,N] int32 slot of each node in the cache, -1: none
+    positions: torch.Tensor      # [B,N] int32 lengths[b] + depth, -1: none
+    block_table: torch.Tensor    # the argument, with the new blocks
+    owned: torch.Tensor          # [B] int32 columns of the table in use after the step
+    free_range: torch.Tensor     # [2] int32 what is left of the ring
+    status: torch.Tensor         # [B] int32
+
+
+def cache_slots(lengths, parent, block_table, owned, free_blocks, free_range, block_size, n_nodes=None,
+                stream=None) -> SlotOutputs:
+    """Blocks for what requests of these lengths and their trees need beyond the ones they own, and the trees' slots and positions.
+
+    All int32 on the device: ``lengths`` [B] committed tokens (negative: an idle row), ``parent`` [N] or [B,N],
+    ``block_table`` [B,W] (written in place, in columns from ``owned[b]`` on), ``owned`` [B], ``free_blocks`` a ring of
+    which the ``free_range[1]`` entries from ``free_range[0]`` on are free.  ``owned`` and ``free_range`` stay as they are: the
+    new ones are returned, and the call can be repeated.  ``n_nodes`` [B]: trees of fewer than N nodes.
+    """
+    return _calls().cache_slots(lengths, parent, block_table, owned, free_blocks, free_range, block_size, n_nodes, stream)
+
+
+PAIRS = {"halves": 0, "neighbours": 1}
+
+
+def norm_rope_cache(q, k, v, inv_freq, positions, slots, k_cache, v_cache, q_weight=None, k_weight=None, eps=1e-6,
+                    pairs="halves", q_out=None, stream=None):
+    """RMS norm of each head's query and key (where a weight is given), their rotation at ``positions``, and keys and
+    values into ``slots`` of the caches, in one pass.  Returns the queries.
+
+    ``q`` [T,Hq,D], ``k`` and ``v`` [T,Hkv,D] (any strides, e.g. views of a fused projection), caches
+    [num_blocks, block_size, Hkv, D], all float32, bfloat16 or float16; ``inv_freq`` float32 with an entry per pair, so that the
+    first 2 * len(inv_freq) entries of a head are rotated; ``positions`` and ``slots`` int32 with T entries.  ``pairs``: "halves"
+    turns (y[i], y[i + rot/2]), "neighbours" (y[2i], y[2i+1]).  A token with a slot outside the cache is padding.
+    ``q_out`` may be ``q``.
+    """
+    return _calls().norm_rope_cache(q, k, v, inv_freq, positions, slots, k_cache, v_cache, q_weight, k_weight, eps, PAIRS[pairs],
+                                    q_out, stream)
+
+
+@dataclass
+class AttentionOutputs:
+    out: torch.Tensor            # [B,N,Hq,D]
+    status: torch.Tensor         # [B] int32
+    lse: torch.Tensor | None = None      # [B,N,Hq] float32
+
+
+def tree_attention(q, k_cache, v_cache, block_table, lengths, parent, n_nodes=None, scale=None, window=0, sinks=0, out=None,
+                   want_lse=False, stream=None) -> AttentionOutputs:
+    """Attention of every node of the draft trees over its request's committed tokens, its ancestors and itself.
+
+    ``q`` [B,N,Hq,D] and caches [num_blocks, block_size, Hkv, D], bfloat16 or float16, D 64, 128 or 256; the trees' keys and
+    values lie at entries ``lengths[b] + node`` already (``norm_rope_cache`` at the slots of ``cache_slots``).
+    ``window`` > 0: only positions above the node's own less ``window``, and the first ``sinks``.  ``scale``:
+    1 / sqrt(D) where None.  A tree of one node is plain decoding.
+    """
+    return _calls().tree_attention(q, k_cache, v_cache, block_table, lengths, parent, n_nodes, scale, window, sinks, out, want_lse,
+                                   stream)
+
+
+@dataclass
+class CommitOutputs:
+    lengths: torch.Tensor        # [B] int32 committed tokens after the step
+    status: torch.Tensor         # [B] int32
+
+
+def cache_commit(cache, accepted_node, parent, lengths, block_table, n_nodes=None, stream=None) -> CommitOutputs:
+    """Move the accepted paths' entries behind the committed tokens, in every cache of the stack ``cache``
+    [caches, num_blocks, block_size, ...] (keys and values of all layers), in place.  ``accepted_node`` [B] is a
+    verifier's output (-1: nothing moves)."""
+    return _calls().cache_commit(cache, accepted_node, parent, lengths, block_table, n_nodes, stream)
+
+
+@dataclass
+class ChainOutputs:
+    accept_len: torch.Tensor     # [B] int32 accepted drafts, -1: see status
+    out_tokens: torch.Tensor     # [B, max_drafts + 1] int32 accepted drafts, the drawn token, then -1
+    bonus_token: torch.Tensor    # [B] int32
+    status: torch.Tensor         # [B] int32
+
+
+def verify_probs(target_probs, draft_probs, token, cu_drafts, u_accept, u_bonus, max_drafts, stream=None) -> ChainOutputs:
+    """Verification of drafted chains from probabilities (ragged: request b drafted ``token[cu_drafts[b]:cu_drafts[b+1]]``).
+
+    ``target_probs`` [T + B, V]: for each request a row per draft, then the row behind all of them; ``draft_probs`` [T, V], or None
+    for drafts that were looked up (q = 1 at the token); float32 or bfloat16.  ``u_accept`` [T] and ``u_bonus`` [T + B] float32
+    in [0, 1); ``max_drafts``: no request has more.
+    """
+    return _calls().verify_probs(target_probs, draft_probs, token, cu_drafts, u_accept, u_bonus, max_drafts, stream)
 
 
 class HostVerifier:

@@ -7,8 +7,10 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SRC = [os.path.join(HERE, "csrc", "specverify.cu")]
-DEPS = [os.path.join(HERE, "csrc", f) for f in ("common.cuh", "verify.cuh", "rowops.cuh", "cut.cuh", "stream.cuh", "walk.cuh", "nodes.cuh", "trunc.cuh", "analysis.cuh")]
+SRC = [os.path.join(HERE, "csrc", f) for f in ("specverify.cu", "step.cu")]
+DEPS = {"specverify.cu": ("common.cuh", "host.h", "verify.cuh", "rowops.cuh", "cut.cuh", "stream.cuh", "walk.cuh", "nodes.cuh", "trunc.cuh",
+                          "analysis.cuh"),
+        "step.cu": ("common.cuh", "host.h", "tree.cuh", "slots.cuh", "rope.cuh", "attend.cuh", "chain.cuh", "commit.cuh")}
 LIB = os.path.join(HERE, "libspecverify.so")
 HEADERS = [os.path.join(ROOT, "include", "specverify.h")]
 
@@ -17,11 +19,15 @@ CALLS_SRC = os.path.join(HERE, "csrc", "torch_calls.cpp")
 CALLS = os.path.join(HERE, "_torch_calls.so")
 
 
-def stale(out: str = LIB, sources=tuple(SRC + DEPS + HEADERS)) -> bool:
+def sources_of(src: str) -> list:
+    return [src] + [os.path.join(HERE, "csrc", f) for f in DEPS[os.path.basename(src)]] + HEADERS
+
+
+def stale(out: str = LIB, sources=None) -> bool:
     if not os.path.exists(out):
         return True
     t = os.path.getmtime(out)
-    return any(os.path.getmtime(f) > t for f in sources)
+    return any(os.path.getmtime(f) > t for f in (sources or sorted({f for s in SRC for f in sources_of(s)})))
 
 
 def build_calls(force: bool = False) -> str:
@@ -47,12 +53,18 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
-           "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"),
-           "-o", LIB] + SRC
+           "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include")]
     if verbose:
-        cmd.insert(1, "-Xptxas")
-        cmd.insert(2, "-v")
-    subprocess.check_call(cmd)
+        cmd[1:1] = ["-Xptxas", "-v"]
+    objects, running = [], []
+    for src in SRC:                      # (the sources side by side, each object only when its own files changed)
+        objects.append(src[:-3] + ".o")
+        if force or stale(objects[-1], sources_of(src)):
+            running.append((src, subprocess.Popen(cmd + ["-c", "-o", objects[-1], src])))
+    failed = [src for src, p in running if p.wait() != 0]
+    if failed:
+        raise RuntimeError(f"nvcc failed: {', '.join(failed)}")
+    subprocess.check_call([nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-Xcompiler", "-fPIC", "-o", LIB] + objects)
     return LIB
 
 

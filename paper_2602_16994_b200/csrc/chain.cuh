@@ -1,0 +1,230 @@
+// Verification of drafted chains from probabilities (spec_verify_probs).
+#pragma once
+#include <cooperative_groups.h>
+
+#include "common.cuh"
+
+namespace specv {
+namespace chain {
+namespace cg = cooperative_groups;
+
+// A cluster per request, a slice of the vocabulary per CTA.  Every CTA finds the accepted drafts by itself (a lane per draft: the
+// chain is one round of dependent loads, whatever its length), then the cluster draws from the one row, or pair of rows, that the
+// chain stopped at: the sums of tiles of 128 weights stay in shared memory, the slices' sums are exchanged, and the CTA that the
+// target falls into finds the tile and reads it once more.  Weights, sums and comparisons are fp64: fp32 sums over 1e5 weights would move the
+// borders between tokens by more than the tokens' own masses.  The bytes of one row of p and of q per request bound the call.
+constexpr int NT = 256, WARPS = NT / 32, TILE = 128, TILES = 1024, CMAX = 16;
+
+struct Params {
+    int B, V, SL, most;                 // SL: weights of a slice, a multiple of TILE
+    long long n_drafts;
+    const void *p, *q;
+    long long p_stride, q_stride;
+    const int *token, *cu;
+    const float *u_accept, *u_bonus;
+    int *accept_len, *out_tokens, *bonus, *status;
+};
+
+template <typename T> __device__ __forceinline__ float value(const T *p);
+template <> __device__ __forceinline__ float value<float>(const float *p) { return __ldg(p); }
+template <> __device__ __forceinline__ float value<unsigned short>(const unsigned short *p) { return __uint_as_float((uint32_t)__ldg(p) << 16); }
+
+// four consecutive entries of a row; beyond the slice: 0
+template <typename T> __device__ __forceinline__ float4 entries(const T *row, int t, int end, bool vec)
+{
+    if (vec && t + 3 < end) {
+        if constexpr (sizeof(T) == 4) return __ldg(reinterpret_cast<const float4 *>(row + t));
+        const uint2 w = __ldg(reinterpret_cast<const uint2 *>(row + t));
+        return make_float4(bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y));
+    }
+    return make_float4(t < end ? value(row + t) : 0.f, t + 1 < end ? value(row + t + 1) : 0.f, t + 2 < end ? value(row + t + 2) : 0.f,
+                       t + 3 < end ? value(row + t + 3) : 0.f);
+}
+// max(v, 0), but NaN where v is NaN
+__device__ __forceinline__ double positive(double v) { return v <= 0.0 ? 0.0 : v; }
+
+// The rows that a draw reads: (p - q)+ where q is given, p without entry `hole` otherwise.
+template <typename T> struct Rows {
+    const T *p, *q;
+    int hole;
+    bool vec;
+    __device__ __forceinline__ void raw(int t, int end, float4 &a, float4 &b) const
+    {
+        a = entries(p, t, end, vec);
+        b = q ? entries(q, t, end, vec) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    __device__ __forceinline__ void weights(int t, const float4 &a, const float4 &b, double w[4]) const
+    {
+        w[0] = positive((double)a.x - (double)b.x);
+        w[1] = positive((double)a.y - (double)b.y);
+        w[2] = positive((double)a.z - (double)b.z);
+        w[3] = positive((double)a.w - (double)b.w);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) if (t + k == hole) w[k] = 0.0;
+    }
+};
+
+// first lane with running sum > tau (and weight); else the last with weight and rest = inf; -1 where there is none
+__device__ __forceinline__ int first_above(double v, double tau, double &rest)
+{
+    const int lane = threadIdx.x & 31;
+    double incl = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const double t = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += t;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, v > 0.0 && incl > tau), pos = __ballot_sync(0xffffffffu, v > 0.0);
+    const int at = hit ? __ffs(hit) - 1 : 31 - __clz(pos);
+    const double before = __shfl_sync(0xffffffffu, incl - v, at < 0 ? 0 : at);
+    rest = hit ? fmax(tau - before, 0.0) : CUDART_INF;
+    return pos ? at : -1;
+}
+
+template <typename T> __global__ void __launch_bounds__(NT) spec_chain_kernel(const Params P)
+{
+    cg::cluster_group cluster = cg::this_cluster();
+    const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int b = blockIdx.x / C, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    __shared__ double tile[TILES], total[2][CMAX];
+    grid_dependency_wait();
+    int *out = P.out_tokens + (long long)b * (P.most + 1);
+    // the accepted drafts (every warp alike)
+    const long long first = __ldg(P.cu + b), end_draft = __ldg(P.cu + b + 1);
+    const long long n = end_draft - first;
+    int status = first < 0 || n < 0 || end_draft > P.n_drafts || n > P.most ? SPEC_DEV_TOPOLOGY : SPEC_DEV_OK;
+    int len = 0;
+    const T *p0 = (const T *)P.p + (first + b) * P.p_stride, *q0 = P.q ? (const T *)P.q + first * P.q_stride : nullptr;
+    for (int i0 = 0; status == SPEC_DEV_OK && i0 < n; i0 += 32) {
+        const int i = i0 + lane;
+        bool stop = false;
+        int wrong = SPEC_DEV_OK;
+        if (i < n) {
+            const int x = __ldg(P.token + first + i);
+            if (x < 0 || x >= P.V) {
+                wrong = SPEC_DEV_TOKEN;
+            } else {
+                const double px = (double)value(p0 + (long long)i * P.p_stride + x);
+                const double qx = q0 ? (double)value(q0 + (long long)i * P.q_stride + x) : 1.0;
+                if (!(px >= 0.0 && px < CUDART_INF && qx >= 0.0 && qx < CUDART_INF)) wrong = SPEC_DEV_NONFINITE;
+                const double ratio = px > 0.0 ? (qx > 0.0 ? px / qx : 1.0) : 0.0;
+                stop = !((double)__ldg(P.u_accept + first + i) < fmin(ratio, 1.0));
+            }
+        }
+        const unsigned bad = __ballot_sync(0xffffffffu, wrong != SPEC_DEV_OK), rejected = __ballot_sync(0xffffffffu, stop);
+        const int at = rejected ? __ffs(rejected) - 1 : 32;
+        const unsigned upto = at >= 31 ? 0xffffffffu : (2u << at) - 1u;      // what lies behind the first rejected draft does not matter
+        if (bad & upto) status = __shfl_sync(0xffffffffu, wrong, __ffs(bad & upto) - 1);
+        if (rejected) { len = i0 + at; break; }
+        len = (int)min((long long)i0 + 32, n);
+    }
+    const bool whole = len == n;                                             // all drafts accepted
+    Rows<T> rows;
+    rows.p = p0 + (long long)len * P.p_stride;
+    rows.q = whole || !q0 ? nullptr : q0 + (long long)len * P.q_stride;
+    rows.hole = -1;
+    if (status == SPEC_DEV_OK && !whole && !q0) rows.hole = __ldg(P.token + first + len);
+    const int t0 = rank * P.SL, end = min(P.V, t0 + P.SL), tiles = max(0, (end - t0 + TILE - 1) / TILE);
+    double all = 0.0, mine = 0.0;
+    const int per = ((tiles + 31) / 32) | 1, r0 = lane * per, r1 = min(tiles, r0 + per);
+    if (status == SPEC_DEV_OK) {
+        // (the second round: what was left of p is 0 everywhere, the draw is from p)
+        for (int round = 0; round < 2; ++round) {
+            rows.vec = (((uintptr_t)rows.p | (uintptr_t)rows.q) & (4 * sizeof(T) - 1)) == 0;
+            constexpr int AHEAD = 4;
+            for (int i0 = warp; i0 < tiles; i0 += WARPS * AHEAD) {
+                float4 x[AHEAD], y[AHEAD];
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) rows.raw(t0 + (i0 + k * WARPS) * TILE + lane * 4, end, x[k], y[k]);
+                double s[AHEAD];
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) {
+                    double w[4];
+                    rows.weights(t0 + (i0 + k * WARPS) * TILE + lane * 4, x[k], y[k], w);
+                    s[k] = (w[0] + w[1]) + (w[2] + w[3]);
+                }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) {
+#pragma unroll
+                    for (int k = 0; k < AHEAD; ++k) s[k] += __shfl_xor_sync(0xffffffffu, s[k], o);
+                }
+                if (lane < AHEAD) {
+                    const int i = i0 + lane * WARPS;
+                    const double sum = lane == 0 ? s[0] : lane == 1 ? s[1] : lane == 2 ? s[2] : s[3];
+                    if (i < tiles) tile[i] = sum;
+                }
+            }
+            __syncthreads();
+            // a run of tiles per lane (of every warp alike: the slice's sum is needed by all)
+            mine = 0.0;
+            for (int i = r0; i < r1; ++i) mine += tile[i];
+            const double slice = warp_sum(mine);
+            if (C > 1) {
+                cluster.sync();              // peers must be running, and through with the round before, when their shared memory is written
+                if (tid < C) *cluster.map_shared_rank(&total[round][rank], tid) = slice;
+                cluster.sync();
+            } else {
+                if (tid == 0) total[round][0] = slice;
+                __syncthreads();
+            }
+            all = 0.0;
+            for (int r = 0; r < C; ++r) all += total[round][r];
+            if (!(all == 0.0) || whole) {
+                if (!(all > 0.0 && all < CUDART_INF)) status = SPEC_DEV_NONFINITE;
+                const double share = lane < C ? total[round][lane] : 0.0;
+                mine = status == SPEC_DEV_OK ? mine : 0.0;
+                double tau, tau2, tau3;
+                const long long row = first + b + len;
+                const int owner = status == SPEC_DEV_OK ? first_above(share, (double)__ldg(P.u_bonus + row) * all, tau) : 0;
+                if (status == SPEC_DEV_OK && owner == rank && warp == 0) {
+                    const int l = first_above(mine, tau, tau2);
+                    int ti = -1;                             // the tile inside the lane's run, by that lane
+                    double rest = tau2;
+                    if (lane == l) {
+                        int last = -1;
+                        double run = 0.0, upto = 0.0;
+                        for (int i = r0; i < r1; ++i) {
+                            const double x = tile[i];
+                            if (x > 0.0) last = i;
+                            if (x > 0.0 && run + x > tau2) { ti = i; upto = run; break; }
+                            run += x;
+                        }
+                        if (ti >= 0) rest = tau2 - upto;
+                        else { ti = last; rest = CUDART_INF; }
+                    }
+                    ti = __shfl_sync(0xffffffffu, ti, l < 0 ? 0 : l);
+                    rest = __shfl_sync(0xffffffffu, rest, l < 0 ? 0 : l);
+                    const int at = t0 + ti * TILE + lane * 4;
+                    float4 x, y;
+                    double w[4];
+                    rows.raw(at, end, x, y);
+                    rows.weights(at, x, y, w);
+                    const int who = first_above((w[0] + w[1]) + (w[2] + w[3]), rest, tau3);
+                    int found = -1, last = -1;
+                    double run = 0.0;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        run += w[k];
+                        if (w[k] > 0.0) last = k;
+                        if (found < 0 && w[k] > 0.0 && run > tau3) found = k;
+                    }
+                    const int token = __shfl_sync(0xffffffffu, at + (found >= 0 ? found : last), who < 0 ? 0 : who);
+                    for (int i = lane; i <= P.most; i += 32)
+                        out[i] = i < len ? __ldg(P.token + first + i) : i == len ? token : -1;
+                    if (lane == 0) { P.accept_len[b] = len; P.bonus[b] = token; P.status[b] = SPEC_DEV_OK; }
+                }
+                break;
+            }
+            rows.q = nullptr;
+            rows.hole = -1;
+        }
+        if (status == SPEC_DEV_OK && !(all > 0.0)) status = SPEC_DEV_NONFINITE;
+    }
+    if (status != SPEC_DEV_OK && rank == 0 && warp == 0) {
+        for (int i = lane; i <= P.most; i += 32) out[i] = -1;
+        if (lane == 0) { P.accept_len[b] = -1; P.bonus[b] = -1; P.status[b] = status; }
+    }
+}
+
+}  // namespace chain
+}  // namespace specv

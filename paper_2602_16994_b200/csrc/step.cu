@@ -1,0 +1,253 @@
+// libspecverify: the operators around a verification in a decoding loop -- host side of their C ABI.
+//
+// Kernels: slots.cuh (blocks, slots and positions of a step), rope.cuh (norm and rotation per head, keys and values into the
+// cache), attend.cuh (attention of a tree's nodes over the paged cache), chain.cuh (verification from
+// probabilities), commit.cuh (the accepted path moves in the cache).  As in specverify.cu, this file validates arguments,
+// chooses the launch shape and enqueues; it never allocates and never synchronises.
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <mutex>
+
+#include "attend.cuh"
+#include "chain.cuh"
+#include "commit.cuh"
+#include "common.cuh"
+#include "host.h"
+#include "rope.cuh"
+#include "slots.cuh"
+#include "specverify.h"
+
+namespace specv {
+namespace {
+
+// A kernel that waits by itself for the one before it in the stream (so its CTAs may be placed while that one's last CTAs
+// work), in clusters of C CTAs where C > 0.
+template <typename P>
+int launch(void (*kernel)(P), dim3 grid, int threads, int smem, int C, cudaStream_t st, const P &params)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads, 1, 1);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.numAttrs = 1;
+    if (C > 0) {
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = (unsigned)C;
+        attr[1].val.clusterDim.y = 1;
+        attr[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
+    }
+    cfg.attrs = attr;
+    void *args[1] = {const_cast<P *>(&params)};
+    if (cudaLaunchKernelExC(&cfg, (const void *)kernel, args) != cudaSuccess) { cudaGetLastError(); return SPEC_ERR_CUDA; }
+    count_launch();
+    return SPEC_OK;
+}
+
+// Attributes of a kernel that its launch needs, set once per device: dynamic shared memory, clusters above 8 CTAs.
+std::mutex g_mutex;
+template <typename K> int prepare(K kernel, int smem, bool big_clusters)
+{
+    struct Entry { const void *k; int dev; };
+    static Entry cache[256];
+    static int used = 0;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return SPEC_ERR_CUDA; }
+    std::lock_guard<std::mutex> lock(g_mutex);
+    for (int i = 0; i < used; ++i)
+        if (cache[i].k == (const void *)kernel && cache[i].dev == dev) return SPEC_OK;
+    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
+        cudaGetLastError();
+        return SPEC_ERR_CUDA;
+    }
+    if (big_clusters && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+        cudaGetLastError();
+        return SPEC_ERR_CUDA;
+    }
+    if (used < 256) cache[used++] = Entry{(const void *)kernel, dev};
+    return SPEC_OK;
+}
+
+TreeArgs tree_args(int N, const int32_t *lengths, const int32_t *n_nodes, const int32_t *parent, int64_t stride)
+{
+    return TreeArgs{N, lengths, n_nodes, parent, stride};
+}
+bool bad_tree_shape(int B, int N, int64_t topo_seq_stride)
+{
+    return B < 1 || B > 65535 || N < 1 || N > SPEC_MAX_NODES || (topo_seq_stride != 0 && topo_seq_stride < N);
+}
+bool bad_pages(int num_blocks, int block, int width)
+{
+    return num_blocks < 1 || block < 1 || width < 1 || (int64_t)num_blocks * block > 0x7FFFFFFF;
+}
+bool aligned(const void *p, int64_t n) { return ((uintptr_t)p & (uintptr_t)(n - 1)) == 0; }
+
+}  // namespace
+}  // namespace specv
+
+using namespace specv;
+
+extern "C" {
+
+int32_t spec_cache_slots(const SpecSlots *a, void *stream)
+{
+    if (!a || !a->lengths || !a->parent || !a->block_table || !a->owned || !a->free_range || !a->slots || !a->positions || !a->owned_out ||
+        !a->free_range_out || !a->status || (a->free_size > 0 && !a->free_blocks))
+        return SPEC_ERR_NULL;
+    if (bad_tree_shape(a->B, a->N, a->topo_seq_stride) || a->block_size < 1 || a->table_width < 1 || a->table_stride < a->table_width ||
+        a->free_size < 0)
+        return SPEC_ERR_SHAPE;
+    if (a->owned_out == a->owned || a->owned_out == a->lengths || a->free_range_out == a->free_range) return SPEC_ERR_PARAM;
+    slots::Params p = {};
+    p.tree = tree_args(a->N, a->lengths, a->n_nodes, a->parent, a->topo_seq_stride);
+    p.B = a->B; p.block = a->block_size; p.width = a->table_width; p.free_size = a->free_size;
+    p.table = a->block_table; p.table_stride = a->table_stride;
+    p.owned = a->owned; p.ring = a->free_blocks; p.range = a->free_range;
+    p.slots = a->slots; p.positions = a->positions; p.owned_out = a->owned_out; p.range_out = a->free_range_out; p.status = a->status;
+    return launch(slots::spec_slots_kernel, dim3((a->B + slots::WARPS - 1) / slots::WARPS), slots::NT, slots::WARPS * a->N * 4, 0,
+                  (cudaStream_t)stream, p);
+}
+
+int32_t spec_norm_rope_cache(const SpecNormRope *a, void *stream)
+{
+    if (!a || !a->q || !a->k || !a->v || (a->rot > 0 && !a->inv_freq) || !a->positions || !a->slots || !a->q_out || !a->k_cache || !a->v_cache)
+        return SPEC_ERR_NULL;
+    if (a->T < 1 || a->Hq < 1 || a->Hkv < 1 || a->Hq > 65535 || a->Hkv > 65535 || a->num_blocks < 1 || a->block_size < 1 ||
+        (int64_t)a->num_blocks * a->block_size > 0x7FFFFFFF)
+        return SPEC_ERR_SHAPE;
+    if (a->dtype != SPEC_F32 && a->dtype != SPEC_BF16 && a->dtype != SPEC_F16) return SPEC_ERR_DTYPE;
+    if ((a->pairs != 0 && a->pairs != 1) || !(a->eps >= 0.f) || a->rot < 0) return SPEC_ERR_PARAM;
+    if (a->D < 8 || a->D > 256 || a->D % 8 || a->rot > a->D || a->rot % 16) return SPEC_ERR_UNSUPPORTED;
+    rope::Params p = {};
+    p.T = a->T; p.Hq = a->Hq; p.Hkv = a->Hkv; p.D = a->D; p.rot = a->rot; p.pairs = a->pairs;
+    p.lanes = 1;
+    while (p.lanes * 8 < a->D) p.lanes *= 2;
+    p.block = a->block_size; p.n_slots = (long long)a->num_blocks * a->block_size;
+    p.x[0] = a->q; p.x[1] = a->k; p.x[2] = a->v;
+    const int64_t *in[3] = {a->q_stride, a->k_stride, a->v_stride};
+    const int64_t esz = a->dtype == SPEC_F32 ? 4 : 2;
+    int64_t all = (int64_t)(uintptr_t)a->q | (int64_t)(uintptr_t)a->k | (int64_t)(uintptr_t)a->v | (int64_t)(uintptr_t)a->q_out |
+                  (int64_t)(uintptr_t)a->k_cache | (int64_t)(uintptr_t)a->v_cache;
+    for (int i = 0; i < 3; ++i)
+        for (int j = 0; j < 2; ++j) { p.x_stride[i][j] = in[i][j]; all |= in[i][j] * esz; }
+    p.weight[0] = a->q_weight; p.weight[1] = a->k_weight; p.eps = a->eps;
+    p.inv_freq = a->inv_freq; p.positions = a->positions; p.slots = a->slots;
+    p.q_out = a->q_out; p.cache[0] = a->k_cache; p.cache[1] = a->v_cache;
+    for (int j = 0; j < 2; ++j) { p.q_out_stride[j] = a->q_out_stride[j]; all |= a->q_out_stride[j] * esz; }
+    for (int j = 0; j < 3; ++j) {
+        p.cache_stride[0][j] = a->k_cache_stride[j]; p.cache_stride[1][j] = a->v_cache_stride[j];
+        all |= (a->k_cache_stride[j] | a->v_cache_stride[j]) * esz;
+    }
+    const bool vec = (all & 15) == 0;
+    const auto go = [&](auto kernel) { return launch(kernel, dim3(a->T), rope::NT, 0, 0, (cudaStream_t)stream, p); };
+    if (a->dtype == SPEC_F32) return vec ? go(rope::spec_rope_kernel<float, true>) : go(rope::spec_rope_kernel<float, false>);
+    if (a->dtype == SPEC_F16) return vec ? go(rope::spec_rope_kernel<__half, true>) : go(rope::spec_rope_kernel<__half, false>);
+    return vec ? go(rope::spec_rope_kernel<__nv_bfloat16, true>) : go(rope::spec_rope_kernel<__nv_bfloat16, false>);
+}
+
+static int attention_check(const SpecAttention *a)
+{
+    if (!a || !a->q || !a->k_cache || !a->v_cache || !a->block_table || !a->lengths || !a->parent || !a->out || !a->status)
+        return SPEC_ERR_NULL;
+    if (bad_tree_shape(a->B, a->N, a->topo_seq_stride) || bad_pages(a->num_blocks, a->block_size, a->table_width) ||
+        a->table_stride < a->table_width || a->Hkv < 1 || a->Hq < a->Hkv || a->Hq % a->Hkv || a->Hq > 65535)
+        return SPEC_ERR_SHAPE;
+    if (a->dtype != SPEC_BF16 && a->dtype != SPEC_F16) return SPEC_ERR_DTYPE;
+    if (!(a->scale > -3.4e38f && a->scale < 3.4e38f) || a->window < 0 || a->sinks < 0) return SPEC_ERR_PARAM;
+    if (a->D != 64 && a->D != 128 && a->D != 256) return SPEC_ERR_UNSUPPORTED;
+    int64_t all = 0;
+    for (int j = 0; j < 3; ++j) all |= a->q_stride[j] | a->k_cache_stride[j] | a->v_cache_stride[j] | a->out_stride[j];
+    if (all % 8 || !aligned(a->q, 16) || !aligned(a->k_cache, 16) || !aligned(a->v_cache, 16) || !aligned(a->out, 16))
+        return SPEC_ERR_UNSUPPORTED;
+    return SPEC_OK;
+}
+
+int32_t spec_tree_attention_workspace_bytes(const SpecAttention *a, int64_t *bytes)
+{
+    if (!bytes) return SPEC_ERR_NULL;
+    const int rc = attention_check(a);
+    if (rc) return rc;
+    *bytes = 256;
+    return SPEC_OK;
+}
+
+int32_t spec_tree_attention(const SpecAttention *a, void *ws, int64_t ws_bytes, void *stream)
+{
+    const int rc = attention_check(a);
+    if (rc) return rc;
+    if (!ws || !aligned(ws, 256) || ws_bytes < 256) return SPEC_ERR_WORKSPACE;
+    attend::Params p = {};
+    p.tree = tree_args(a->N, a->lengths, a->n_nodes, a->parent, a->topo_seq_stride);
+    p.B = a->B; p.Hq = a->Hq; p.Hkv = a->Hkv; p.D = a->D; p.num_blocks = a->num_blocks; p.block = a->block_size; p.width = a->table_width;
+    p.window = a->window; p.sinks = a->sinks; p.scale = a->scale;
+    p.q = a->q; p.k = a->k_cache; p.v = a->v_cache; p.table = a->block_table; p.table_stride = a->table_stride;
+    p.out = a->out; p.lse = a->lse; p.status = a->status;
+    for (int j = 0; j < 3; ++j) {
+        p.q_stride[j] = a->q_stride[j]; p.k_stride[j] = a->k_cache_stride[j]; p.v_stride[j] = a->v_cache_stride[j];
+        p.out_stride[j] = a->out_stride[j];
+    }
+    const dim3 grid(a->Hkv, a->N, a->B);
+    return a->dtype == SPEC_F16 ? launch(attend::spec_attend_kernel<__half>, grid, attend::NT, 0, 0, (cudaStream_t)stream, p)
+                                : launch(attend::spec_attend_kernel<__nv_bfloat16>, grid, attend::NT, 0, 0, (cudaStream_t)stream, p);
+}
+
+int32_t spec_cache_commit(const SpecCommit *a, void *stream)
+{
+    if (!a || !a->cache || !a->block_table || !a->lengths || !a->parent || !a->accepted_node || !a->lengths_out || !a->status)
+        return SPEC_ERR_NULL;
+    if (bad_tree_shape(a->B, a->N, a->topo_seq_stride) || bad_pages(a->num_blocks, a->block_size, a->table_width) ||
+        a->table_stride < a->table_width || a->caches < 1 || a->row_bytes < 1)
+        return SPEC_ERR_SHAPE;
+    if (a->lengths_out == a->lengths || a->lengths_out == a->accepted_node) return SPEC_ERR_PARAM;
+    commit::Params p = {};
+    p.tree = tree_args(a->N, a->lengths, a->n_nodes, a->parent, a->topo_seq_stride);
+    p.B = a->B; p.caches = a->caches; p.num_blocks = a->num_blocks; p.block = a->block_size; p.width = a->table_width;
+    p.cache = (unsigned char *)a->cache;
+    int64_t all = (int64_t)(uintptr_t)a->cache | a->row_bytes;
+    for (int j = 0; j < 3; ++j) { p.stride[j] = a->stride[j]; all |= a->stride[j]; }
+    p.table = a->block_table; p.table_stride = a->table_stride; p.accepted = a->accepted_node;
+    p.lengths_out = a->lengths_out; p.status = a->status;
+    const int unit = all % 16 == 0 ? 16 : all % 4 == 0 ? 4 : 1;
+    p.words = a->row_bytes / unit;
+    p.per = (int)std::max<int64_t>(1, commit::NT / p.words);
+    const dim3 grid((a->caches + p.per - 1) / p.per, a->B);
+    const cudaStream_t st = (cudaStream_t)stream;
+    return unit == 16  ? launch(commit::spec_commit_kernel<uint4>, grid, commit::NT, 0, 0, st, p)
+           : unit == 4 ? launch(commit::spec_commit_kernel<uint32_t>, grid, commit::NT, 0, 0, st, p)
+                       : launch(commit::spec_commit_kernel<unsigned char>, grid, commit::NT, 0, 0, st, p);
+}
+
+int32_t spec_verify_probs(const SpecChains *a, void *stream)
+{
+    if (!a || !a->target_probs || !a->cu_drafts || !a->u_bonus || !a->accept_len || !a->out_tokens || !a->bonus_token || !a->status ||
+        (a->n_drafts > 0 && (!a->token || !a->u_accept)))
+        return SPEC_ERR_NULL;
+    if (a->B < 1 || a->B > (1 << 26) || a->V < 1 || a->max_drafts < 0 || a->max_drafts > (1 << 20) || a->n_drafts < 0 || a->target_stride < a->V ||
+        (a->draft_probs && a->draft_stride < a->V))
+        return SPEC_ERR_SHAPE;
+    if (a->dtype != SPEC_F32 && a->dtype != SPEC_BF16) return SPEC_ERR_DTYPE;
+    // the largest cluster whose slices are worth a CTA and that leaves one wave of eight CTAs per SM
+    int C = 1;
+    while (C < chain::CMAX && a->V / (2 * C) >= 4096 && (int64_t)a->B * 2 * C <= 148 * 8) C *= 2;
+    while (C < chain::CMAX && (int64_t)a->V > (int64_t)C * chain::TILES * chain::TILE) C *= 2;
+    if ((int64_t)a->V > (int64_t)C * chain::TILES * chain::TILE) return SPEC_ERR_UNSUPPORTED;
+    chain::Params p = {};
+    p.B = a->B; p.V = a->V; p.most = a->max_drafts; p.n_drafts = a->n_drafts;
+    p.SL = ((a->V + C - 1) / C + chain::TILE - 1) / chain::TILE * chain::TILE;
+    p.p = a->target_probs; p.q = a->n_drafts ? a->draft_probs : nullptr; p.p_stride = a->target_stride; p.q_stride = a->draft_stride;
+    p.token = a->token; p.cu = a->cu_drafts; p.u_accept = a->u_accept; p.u_bonus = a->u_bonus;
+    p.accept_len = a->accept_len; p.out_tokens = a->out_tokens; p.bonus = a->bonus_token; p.status = a->status;
+    const auto go = [&](auto kernel) {
+        const int rc = prepare(kernel, 0, true);
+        return rc ? rc : launch(kernel, dim3((unsigned)(a->B * C)), chain::NT, 0, C, (cudaStream_t)stream, p);
+    };
+    return a->dtype == SPEC_F32 ? go(chain::spec_chain_kernel<float>) : go(chain::spec_chain_kernel<unsigned short>);
+}
+
+}  // extern "C"

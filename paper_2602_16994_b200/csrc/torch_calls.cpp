@@ -9,8 +9,14 @@
 #include <Python.h>
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <dlfcn.h>
+
+#include <cmath>
+#include <optional>
+
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "specverify.h"
@@ -391,6 +397,343 @@ PyObject *py_init(PyObject *, PyObject *args)
     Py_RETURN_NONE;
 }
 
+// ---- the operators around a verification ---------------------------------------------------------------------------------------
+struct StepLibrary {
+    decltype(&spec_cache_slots) slots;
+    decltype(&spec_norm_rope_cache) norm_rope;
+    decltype(&spec_tree_attention_workspace_bytes) attention_bytes;
+    decltype(&spec_tree_attention) attention;
+    decltype(&spec_cache_commit) commit;
+    decltype(&spec_verify_probs) probs;
+} step_lib;
+PyObject *slot_outputs_class, *attention_outputs_class, *commit_outputs_class, *chain_outputs_class;
+
+// Where a call runs: the device of its tensors, made current for the call, and its stream.  A stream that the caller names may be another than the
+// current one: outputs and scratch then come from that stream's memory, and the allocator is told of both streams, so that memory
+// freed on one is not handed out again while the other still uses it.
+class Place {
+public:
+    Place(const at::Tensor &first, PyObject *stream) : device_(first.device()), guard_(device_), named_(stream != Py_None)
+    {
+        stream_ = stream_of(stream);
+        if (!named_) return;
+        caller_ = c10::cuda::getCurrentCUDAStream(device_.index());
+        switch_.emplace(c10::cuda::getStreamFromExternal((cudaStream_t)stream_, device_.index()));
+    }
+    const at::Device &device() const { return device_; }
+    void *stream() const { return stream_; }
+    // an input: on the same device, and in use by the call's stream
+    void uses(const at::Tensor &t, const char *name) const
+    {
+        if (t.device() != device_) raise("%s must live on the device of the other tensors", name);
+        if (named_ && t.numel()) t.record_stream(switch_->current_stream().unwrap());
+    }
+    at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType t) const
+    {
+        at::Tensor r = empty(sizes, t, device_);
+        if (named_ && r.numel()) r.record_stream(caller_->unwrap());
+        return r;
+    }
+
+private:
+    c10::Device device_;
+    c10::cuda::CUDAGuard guard_;
+    bool named_;
+    void *stream_;
+    std::optional<c10::cuda::CUDAStream> caller_;
+    std::optional<c10::cuda::CUDAStreamGuard> switch_;
+};
+
+void need(const void *f) { if (!f) raise("the library lacks an entry point"); }
+const at::Tensor &ints(PyObject *o, const char *name, const Place &place, int64_t count = -1)
+{
+    const at::Tensor &t = cuda_tensor(o, name);
+    check_vector(t, name, at::kInt, "torch.int32");
+    if (count >= 0 && t.numel() != count) raise("%s must have %lld entries", name, (long long)count);
+    place.uses(t, name);
+    return t;
+}
+const at::Tensor &floats(PyObject *o, const char *name, const Place &place, int64_t count = -1)
+{
+    const at::Tensor &t = cuda_tensor(o, name);
+    check_vector(t, name, at::kFloat, "torch.float32");
+    if (count >= 0 && t.numel() != count) raise("%s must have %lld entries", name, (long long)count);
+    place.uses(t, name);
+    return t;
+}
+int32_t *int_ptr(const at::Tensor &t) { return (int32_t *)t.data_ptr(); }
+int32_t small(int64_t v, const char *what)
+{
+    if (v > 0x7FFFFFFF || v < 0) raise("%s is out of range", what);
+    return (int32_t)v;
+}
+// the parents of one tree for all, or of one per request: row length, and the stride between requests
+int64_t tree_of(PyObject *o, const Place &place, int64_t B, int64_t *N, const int32_t **parent)
+{
+    const at::Tensor &t = ints(o, "parent", place);
+    if (t.dim() == 2 ? t.size(0) != B : t.dim() != 1) raise("parent must be [N] or [B,N]");
+    *N = t.size(-1);
+    *parent = int_ptr(t);
+    return t.dim() == 1 ? 0 : *N;
+}
+struct Table { int32_t *ptr; int64_t stride; int32_t width; };
+Table table_of(PyObject *o, const Place &place, int64_t B)
+{
+    const at::Tensor &t = cuda_tensor(o, "block_table");
+    if (t.scalar_type() != at::kInt || t.dim() != 2 || t.size(0) != B || (t.size(1) > 1 && t.stride(1) != 1))
+        raise("block_table must be a [B,W] torch.int32 tensor with contiguous rows");
+    place.uses(t, "block_table");
+    const int64_t W = t.size(1);
+    return {int_ptr(t), B > 1 ? t.stride(0) : (W > t.stride(0) ? W : t.stride(0)), small(W, "the table's width")};
+}
+int element_type(at::ScalarType t)
+{
+    return t == at::kFloat ? SPEC_F32 : t == at::kBFloat16 ? SPEC_BF16 : t == at::kHalf ? SPEC_F16 : -1;
+}
+void rows_of(const at::Tensor &t, const char *name, int dims, at::ScalarType type, const Place &place)
+{
+    if (t.dim() != dims || t.scalar_type() != type || (t.size(dims - 1) > 1 && t.stride(dims - 1) != 1))
+        raise("%s must have %d dimensions, the last contiguous, and the type of the other tensors", name, dims);
+    place.uses(t, name);
+}
+void no_gradient(const at::Tensor &t, const char *name)
+{
+    if (t.requires_grad() && c10::GradMode::is_enabled()) raise("%s requires a gradient: the call has no backward pass", name);
+}
+// strides of all but the last dimension; of a dimension of one entry, which nothing steps along: 0
+void strides_of(const at::Tensor &t, int64_t *to)
+{
+    for (int64_t i = 0; i + 1 < t.dim(); ++i) to[i] = t.size(i) > 1 ? t.stride(i) : 0;
+}
+
+// cache_slots(lengths, parent, block_table, owned, free_blocks, free_range, block_size, n_nodes, stream)
+PyObject *py_slots(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!arity(n, 9)) return nullptr;
+    return guarded([&]() -> PyObject * {
+        need((void *)step_lib.slots);
+        const at::Tensor &lengths = cuda_tensor(a[0], "lengths");
+        const Place place(lengths, a[8]);
+        const int64_t B = ints(a[0], "lengths", place).numel();
+        int64_t N;
+        SpecSlots s = {};
+        s.topo_seq_stride = tree_of(a[1], place, B, &N, &s.parent);
+        const Table table = table_of(a[2], place, B);
+        const at::Tensor &ring = ints(a[4], "free_blocks", place);
+        s.B = small(B, "B"); s.N = small(N, "N"); s.block_size = truncated(a[6]); s.table_width = table.width;
+        s.lengths = int_ptr(lengths); s.block_table = table.ptr; s.table_stride = table.stride;
+        s.n_nodes = a[7] == Py_None ? nullptr : int_ptr(ints(a[7], "n_nodes", place, B));
+        s.owned = int_ptr(ints(a[3], "owned", place, B));
+        s.free_blocks = int_ptr(ring); s.free_size = small(ring.numel(), "free_blocks");
+        s.free_range = int_ptr(ints(a[5], "free_range", place, 2));
+        const at::Tensor t[6] = {place.fresh({B, N}, at::kInt), place.fresh({B, N}, at::kInt), THPVariable_Unpack(a[2]),
+                                 place.fresh({B}, at::kInt), place.fresh({2}, at::kInt), place.fresh({B}, at::kInt)};
+        s.slots = int_ptr(t[0]); s.positions = int_ptr(t[1]); s.owned_out = int_ptr(t[3]); s.free_range_out = int_ptr(t[4]);
+        s.status = int_ptr(t[5]);
+        check(unlocked([&] { return step_lib.slots(&s, place.stream()); }), "spec_cache_slots");
+        return result(slot_outputs_class, t, 6);
+    });
+}
+
+// norm_rope_cache(q, k, v, inv_freq, positions, slots, k_cache, v_cache, q_weight, k_weight, eps, pairs, q_out, stream)
+PyObject *py_norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!arity(n, 14)) return nullptr;
+    return guarded([&]() -> PyObject * {
+        need((void *)step_lib.norm_rope);
+        const at::Tensor &q = cuda_tensor(a[0], "q"), &k = cuda_tensor(a[1], "k"), &v = cuda_tensor(a[2], "v");
+        const at::Tensor &kc = cuda_tensor(a[6], "k_cache"), &vc = cuda_tensor(a[7], "v_cache");
+        const Place place(q, a[13]);
+        const auto type = q.scalar_type();
+        if (element_type(type) < 0) raise("q must be float32, bfloat16 or float16");
+        rows_of(q, "q", 3, type, place);
+        rows_of(k, "k", 3, type, place);
+        rows_of(v, "v", 3, type, place);
+        rows_of(kc, "k_cache", 4, type, place);
+        rows_of(vc, "v_cache", 4, type, place);
+        no_gradient(q, "q"); no_gradient(k, "k"); no_gradient(v, "v");
+        const int64_t T = q.size(0), D = q.size(2), Hkv = k.size(1);
+        if (k.size(0) != T || k.size(2) != D || v.sizes() != k.sizes()) raise("q, k and v must be [T,Hq,D], [T,Hkv,D] and [T,Hkv,D]");
+        if (kc.size(2) != Hkv || kc.size(3) != D || vc.sizes() != kc.sizes()) raise("the caches must be [num_blocks, block_size, Hkv, D]");
+        SpecNormRope s = {};
+        const void **weight[2] = {&s.q_weight, &s.k_weight};
+        for (int i = 0; i < 2; ++i) {
+            if (a[8 + i] == Py_None) continue;
+            const at::Tensor &w = cuda_tensor(a[8 + i], i ? "k_weight" : "q_weight");
+            if (w.scalar_type() != type || !w.is_contiguous() || w.numel() != D) raise("the weights must be contiguous [D] tensors of the type of q");
+            no_gradient(w, i ? "k_weight" : "q_weight");
+            place.uses(w, "weight");
+            *weight[i] = w.data_ptr();
+        }
+        const at::Tensor &freq = floats(a[3], "inv_freq", place);
+        s.positions = int_ptr(ints(a[4], "positions", place, T));
+        s.slots = int_ptr(ints(a[5], "slots", place, T));
+        s.T = small(T, "T"); s.Hq = small(q.size(1), "Hq"); s.Hkv = small(Hkv, "Hkv"); s.D = small(D, "D");
+        s.rot = small(2 * freq.numel(), "inv_freq"); s.pairs = truncated(a[11]); s.dtype = element_type(type); s.eps = (float)number(a[10]);
+        s.num_blocks = small(kc.size(0), "num_blocks"); s.block_size = small(kc.size(1), "block_size");
+        at::Tensor out;
+        if (a[12] == Py_None) {
+            out = place.fresh(q.sizes(), type);
+        } else {
+            out = cuda_tensor(a[12], "q_out");
+            rows_of(out, "q_out", 3, type, place);
+            if (out.sizes() != q.sizes()) raise("q_out must have the shape of q");
+        }
+        s.q = q.data_ptr(); s.k = k.data_ptr(); s.v = v.data_ptr(); s.inv_freq = (const float *)freq.data_ptr();
+        s.q_out = out.data_ptr(); s.k_cache = kc.data_ptr(); s.v_cache = vc.data_ptr();
+        strides_of(q, s.q_stride); strides_of(k, s.k_stride); strides_of(v, s.v_stride); strides_of(out, s.q_out_stride);
+        strides_of(kc, s.k_cache_stride); strides_of(vc, s.v_cache_stride);
+        if (T) check(unlocked([&] { return step_lib.norm_rope(&s, place.stream()); }), "spec_norm_rope_cache");
+        return THPVariable_Wrap(out);
+    });
+}
+
+// tree_attention(q, k_cache, v_cache, block_table, lengths, parent, n_nodes, scale, window, sinks, out, want_lse, stream)
+PyObject *py_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!arity(n, 13)) return nullptr;
+    return guarded([&]() -> PyObject * {
+        need((void *)step_lib.attention);
+        const at::Tensor &q = cuda_tensor(a[0], "q"), &kc = cuda_tensor(a[1], "k_cache"), &vc = cuda_tensor(a[2], "v_cache");
+        const Place place(q, a[12]);
+        const auto type = q.scalar_type();
+        if (type != at::kBFloat16 && type != at::kHalf) raise("q must be bfloat16 or float16");
+        rows_of(q, "q", 4, type, place);
+        rows_of(kc, "k_cache", 4, type, place);
+        rows_of(vc, "v_cache", 4, type, place);
+        no_gradient(q, "q"); no_gradient(kc, "k_cache"); no_gradient(vc, "v_cache");
+        const int64_t B = q.size(0), Hq = q.size(2), D = q.size(3);
+        if (kc.size(3) != D || vc.sizes() != kc.sizes()) raise("the caches must be [num_blocks, block_size, Hkv, D]");
+        SpecAttention s = {};
+        int64_t N;
+        s.topo_seq_stride = tree_of(a[5], place, B, &N, &s.parent);
+        if (N != q.size(1)) raise("q must be [B,N,Hq,D] with the N of parent");
+        const Table table = table_of(a[3], place, B);
+        s.B = small(B, "B"); s.N = small(N, "N"); s.Hq = small(Hq, "Hq"); s.Hkv = small(kc.size(2), "Hkv"); s.D = small(D, "D");
+        s.dtype = element_type(type);
+        s.num_blocks = small(kc.size(0), "num_blocks"); s.block_size = small(kc.size(1), "block_size"); s.table_width = table.width;
+        s.window = truncated(a[8]); s.sinks = truncated(a[9]);
+        s.scale = a[7] == Py_None ? (float)(1.0 / std::sqrt((double)(D > 0 ? D : 1))) : (float)number(a[7]);
+        s.block_table = table.ptr; s.table_stride = table.stride;
+        s.lengths = int_ptr(ints(a[4], "lengths", place, B));
+        s.n_nodes = a[6] == Py_None ? nullptr : int_ptr(ints(a[6], "n_nodes", place, B));
+        at::Tensor t[3];
+        if (a[10] == Py_None) {
+            t[0] = place.fresh(q.sizes(), type);
+        } else {
+            t[0] = cuda_tensor(a[10], "out");
+            rows_of(t[0], "out", 4, type, place);
+            if (t[0].sizes() != q.sizes()) raise("out must have the shape of q");
+        }
+        t[1] = place.fresh({B}, at::kInt);
+        if (PyObject_IsTrue(a[11])) t[2] = place.fresh({B, N, Hq}, at::kFloat);
+        s.q = q.data_ptr(); s.k_cache = kc.data_ptr(); s.v_cache = vc.data_ptr(); s.out = t[0].data_ptr(); s.status = int_ptr(t[1]);
+        s.lse = t[2].defined() ? (float *)t[2].data_ptr() : nullptr;
+        strides_of(q, s.q_stride); strides_of(kc, s.k_cache_stride); strides_of(vc, s.v_cache_stride); strides_of(t[0], s.out_stride);
+        int64_t bytes = 0;
+        check(step_lib.attention_bytes(&s, &bytes), "spec_tree_attention_workspace_bytes");
+        // scratch of this call alone (the allocator's blocks lie on 512 bytes): calls on several streams, or captured into several
+        // graphs, never share it
+        const at::Tensor ws = empty({bytes}, at::kByte, place.device());
+        check(unlocked([&] { return step_lib.attention(&s, ws.data_ptr(), bytes, place.stream()); }), "spec_tree_attention");
+        return result(attention_outputs_class, t, 3);
+    });
+}
+
+// cache_commit(cache, accepted_node, parent, lengths, block_table, n_nodes, stream)
+PyObject *py_commit(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!arity(n, 7)) return nullptr;
+    return guarded([&]() -> PyObject * {
+        need((void *)step_lib.commit);
+        const at::Tensor &cache = cuda_tensor(a[0], "cache");
+        const Place place(cache, a[6]);
+        place.uses(cache, "cache");
+        if (cache.dim() < 4) raise("cache must be [caches, num_blocks, block_size, ...]");
+        int64_t row = 1;
+        for (int64_t i = cache.dim() - 1; i >= 3; --i) {
+            if (cache.size(i) > 1 && cache.stride(i) != row) raise("the entries of a slot of cache must be contiguous");
+            row *= cache.size(i);
+        }
+        const at::Tensor &lengths = cuda_tensor(a[3], "lengths");
+        const int64_t B = ints(a[3], "lengths", place).numel(), esz = cache.element_size();
+        SpecCommit s = {};
+        int64_t N;
+        s.topo_seq_stride = tree_of(a[2], place, B, &N, &s.parent);
+        const Table table = table_of(a[4], place, B);
+        s.B = small(B, "B"); s.N = small(N, "N"); s.caches = small(cache.size(0), "caches");
+        s.num_blocks = small(cache.size(1), "num_blocks"); s.block_size = small(cache.size(2), "block_size"); s.table_width = table.width;
+        s.cache = cache.data_ptr(); s.row_bytes = row * esz;
+        for (int i = 0; i < 3; ++i) s.stride[i] = cache.size(i) > 1 ? cache.stride(i) * esz : 0;
+        s.block_table = table.ptr; s.table_stride = table.stride;
+        s.lengths = int_ptr(lengths); s.accepted_node = int_ptr(ints(a[1], "accepted_node", place, B));
+        s.n_nodes = a[5] == Py_None ? nullptr : int_ptr(ints(a[5], "n_nodes", place, B));
+        const at::Tensor t[2] = {place.fresh({B}, at::kInt), place.fresh({B}, at::kInt)};
+        s.lengths_out = int_ptr(t[0]); s.status = int_ptr(t[1]);
+        check(unlocked([&] { return step_lib.commit(&s, place.stream()); }), "spec_cache_commit");
+        return result(commit_outputs_class, t, 2);
+    });
+}
+
+// verify_probs(target_probs, draft_probs, token, cu_drafts, u_accept, u_bonus, max_drafts, stream)
+PyObject *py_chains(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!arity(n, 8)) return nullptr;
+    return guarded([&]() -> PyObject * {
+        need((void *)step_lib.probs);
+        const at::Tensor &p = cuda_tensor(a[0], "target_probs");
+        const Place place(p, a[7]);
+        const auto type = p.scalar_type();
+        if (type != at::kFloat && type != at::kBFloat16) raise("target_probs must be float32 or bfloat16");
+        rows_of(p, "target_probs", 2, type, place);
+        const at::Tensor &token = ints(a[2], "token", place), &cu = ints(a[3], "cu_drafts", place);
+        const int64_t T = token.numel(), B = cu.numel() - 1, V = p.size(1);
+        if (p.size(0) != T + B) raise("target_probs must have a row per draft and one more per request");
+        SpecChains s = {};
+        s.target_stride = p.size(0) > 1 ? p.stride(0) : V;
+        s.draft_stride = V;
+        if (a[1] != Py_None) {
+            const at::Tensor &q = cuda_tensor(a[1], "draft_probs");
+            rows_of(q, "draft_probs", 2, type, place);
+            if (q.size(0) != T || q.size(1) != V) raise("draft_probs must have a row of target_probs' length per draft");
+            s.draft_probs = q.data_ptr();
+            if (T > 1) s.draft_stride = q.stride(0);
+        }
+        s.B = small(B, "B"); s.V = small(V, "V"); s.max_drafts = truncated(a[6]); s.dtype = element_type(type); s.n_drafts = T;
+        s.target_probs = p.data_ptr();
+        s.token = int_ptr(token); s.cu_drafts = int_ptr(cu);
+        s.u_accept = (const float *)floats(a[4], "u_accept", place, T).data_ptr();
+        s.u_bonus = (const float *)floats(a[5], "u_bonus", place, T + B).data_ptr();
+        const at::Tensor t[4] = {place.fresh({B}, at::kInt), place.fresh({B, (int64_t)(s.max_drafts < 0 ? 0 : s.max_drafts) + 1}, at::kInt),
+                                 place.fresh({B}, at::kInt), place.fresh({B}, at::kInt)};
+        s.accept_len = int_ptr(t[0]); s.out_tokens = int_ptr(t[1]); s.bonus_token = int_ptr(t[2]); s.status = int_ptr(t[3]);
+        check(unlocked([&] { return step_lib.probs(&s, place.stream()); }), "spec_verify_probs");
+        return result(chain_outputs_class, t, 4);
+    });
+}
+
+// init_step(path of libspecverify.so, SlotOutputs, AttentionOutputs, CommitOutputs, ChainOutputs): the entry points above
+PyObject *py_init_step(PyObject *, PyObject *args)
+{
+    const char *path;
+    PyObject *c[4];
+    if (!PyArg_ParseTuple(args, "sOOOO", &path, &c[0], &c[1], &c[2], &c[3])) return nullptr;
+    void *h = dlopen(path, RTLD_NOW | RTLD_LOCAL);
+    if (!h) return PyErr_Format(PyExc_RuntimeError, "%s", dlerror());
+    const auto find = [&](auto &f, const char *name) { f = reinterpret_cast<std::remove_reference_t<decltype(f)>>(dlsym(h, name)); };
+    find(step_lib.slots, "spec_cache_slots");
+    find(step_lib.norm_rope, "spec_norm_rope_cache");
+    find(step_lib.attention_bytes, "spec_tree_attention_workspace_bytes");
+    find(step_lib.attention, "spec_tree_attention");
+    find(step_lib.commit, "spec_cache_commit");
+    find(step_lib.probs, "spec_verify_probs");
+    slot_outputs_class = Py_NewRef(c[0]);
+    attention_outputs_class = Py_NewRef(c[1]);
+    commit_outputs_class = Py_NewRef(c[2]);
+    chain_outputs_class = Py_NewRef(c[3]);
+    Py_RETURN_NONE;
+}
+
 PyMethodDef methods[] = {
     {"init", py_init, METH_VARARGS, nullptr},
     {"verify", (PyCFunction)(void *)py_verify, METH_FASTCALL, nullptr},
@@ -398,6 +741,12 @@ PyMethodDef methods[] = {
     {"tree_probs", (PyCFunction)(void *)py_probs, METH_FASTCALL, nullptr},
     {"sample_bonus", (PyCFunction)(void *)py_bonus, METH_FASTCALL, nullptr},
     {"launch", (PyCFunction)(void *)py_launch, METH_FASTCALL, nullptr},
+    {"init_step", py_init_step, METH_VARARGS, nullptr},
+    {"cache_slots", (PyCFunction)(void *)py_slots, METH_FASTCALL, nullptr},
+    {"norm_rope_cache", (PyCFunction)(void *)py_norm_rope, METH_FASTCALL, nullptr},
+    {"tree_attention", (PyCFunction)(void *)py_attention, METH_FASTCALL, nullptr},
+    {"cache_commit", (PyCFunction)(void *)py_commit, METH_FASTCALL, nullptr},
+    {"verify_probs", (PyCFunction)(void *)py_chains, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_torch_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
