@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 SRC = [os.path.join(HERE, "csrc", f) for f in ("specverify.cu", "step.cu")]
 DEPS = {"specverify.cu": ("common.cuh", "host.h", "verify.cuh", "rowops.cuh", "cut.cuh", "stream.cuh", "walk.cuh", "nodes.cuh", "trunc.cuh",
                           "analysis.cuh"),
-        "step.cu": ("common.cuh", "host.h", "tree.cuh", "slots.cuh", "rope.cuh", "attend.cuh", "chain.cuh", "commit.cuh")}
+        "step.cu": ("common.cuh", "host.h", "tree.cuh", "tmem.cuh", "slots.cuh", "rope.cuh", "attend.cuh", "chain.cuh", "commit.cuh")}
 LIB = os.path.join(HERE, "libspecverify.so")
 HEADERS = [os.path.join(ROOT, "include", "specverify.h")]
 

@@ -8,6 +8,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <atomic>
 #include <mutex>
 
 #include "attend.cuh"
@@ -72,6 +73,20 @@ template <typename K> int prepare(K kernel, int smem, bool big_clusters)
     }
     if (used < 256) cache[used++] = Entry{(const void *)kernel, dev};
     return SPEC_OK;
+}
+
+// CTAs of the attention kernel: one per SM
+int attention_ctas()
+{
+    static std::atomic<int> cached[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) { cudaGetLastError(); return 148; }
+    int n = cached[dev].load(std::memory_order_relaxed);
+    if (n) return n;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) { cudaGetLastError(); n = 148; }
+    n = std::min(n, attend::CTAS_MAX);
+    cached[dev].store(n, std::memory_order_relaxed);
+    return n;
 }
 
 TreeArgs tree_args(int N, const int32_t *lengths, const int32_t *n_nodes, const int32_t *parent, int64_t stride)
@@ -168,12 +183,26 @@ static int attention_check(const SpecAttention *a)
     return SPEC_OK;
 }
 
+// Two blocks of 128 rows share the loads of a tile where a request has more rows than one block.
+static bool two_blocks(const SpecAttention *a) { return a->D <= 128 && (int64_t)a->N * (a->Hq / a->Hkv) > 128; }
+
+struct AttentionLayout { int64_t part, ml, late, total; };
+static AttentionLayout attention_layout(const SpecAttention *a, int ctas)
+{
+    const int64_t rows = two_blocks(a) ? 256 : 128;
+    AttentionLayout L = {};
+    L.ml = (int64_t)ctas * 2 * rows * a->D * 4;
+    L.late = L.ml + (int64_t)ctas * 2 * rows * 8;
+    L.total = L.late + ((int64_t)ctas * 4 + 255) / 256 * 256;
+    return L;
+}
+
 int32_t spec_tree_attention_workspace_bytes(const SpecAttention *a, int64_t *bytes)
 {
     if (!bytes) return SPEC_ERR_NULL;
     const int rc = attention_check(a);
     if (rc) return rc;
-    *bytes = 256;
+    *bytes = attention_layout(a, attention_ctas()).total;
     return SPEC_OK;
 }
 
@@ -181,10 +210,13 @@ int32_t spec_tree_attention(const SpecAttention *a, void *ws, int64_t ws_bytes, 
 {
     const int rc = attention_check(a);
     if (rc) return rc;
-    if (!ws || !aligned(ws, 256) || ws_bytes < 256) return SPEC_ERR_WORKSPACE;
+    const int ctas = attention_ctas();
+    const AttentionLayout L = attention_layout(a, ctas);
+    if (!ws || !aligned(ws, 256) || ws_bytes < L.total) return SPEC_ERR_WORKSPACE;
     attend::Params p = {};
     p.tree = tree_args(a->N, a->lengths, a->n_nodes, a->parent, a->topo_seq_stride);
-    p.B = a->B; p.Hq = a->Hq; p.Hkv = a->Hkv; p.D = a->D; p.num_blocks = a->num_blocks; p.block = a->block_size; p.width = a->table_width;
+    p.B = a->B; p.Hq = a->Hq; p.Hkv = a->Hkv; p.G = a->Hq / a->Hkv;
+    p.num_blocks = a->num_blocks; p.block = a->block_size; p.width = a->table_width;
     p.window = a->window; p.sinks = a->sinks; p.scale = a->scale;
     p.q = a->q; p.k = a->k_cache; p.v = a->v_cache; p.table = a->block_table; p.table_stride = a->table_stride;
     p.out = a->out; p.lse = a->lse; p.status = a->status;
@@ -192,9 +224,27 @@ int32_t spec_tree_attention(const SpecAttention *a, void *ws, int64_t ws_bytes, 
         p.q_stride[j] = a->q_stride[j]; p.k_stride[j] = a->k_cache_stride[j]; p.v_stride[j] = a->v_cache_stride[j];
         p.out_stride[j] = a->out_stride[j];
     }
-    const dim3 grid(a->Hkv, a->N, a->B);
-    return a->dtype == SPEC_F16 ? launch(attend::spec_attend_kernel<__half>, grid, attend::NT, 0, 0, (cudaStream_t)stream, p)
-                                : launch(attend::spec_attend_kernel<__nv_bfloat16>, grid, attend::NT, 0, 0, (cudaStream_t)stream, p);
+    p.ctas = ctas;
+    p.part = (float *)((unsigned char *)ws + L.part);
+    p.ml = (float2 *)((unsigned char *)ws + L.ml);
+    p.late = (int *)((unsigned char *)ws + L.late);
+    const bool half = a->dtype == SPEC_F16;
+    const cudaStream_t st = (cudaStream_t)stream;
+    const auto go = [&](auto shape, auto attend_kernel, auto join_kernel) -> int {
+        using S = decltype(shape);
+        const int smem = S::total + 1024;
+        int e = prepare(attend_kernel, smem, false);
+        if (e) return e;
+        e = launch(attend_kernel, dim3(ctas), S::NT, smem, 0, st, p);
+        return e ? e : launch(join_kernel, dim3((unsigned)(ctas * (S::ROWS / 32) + a->B)), attend::JOIN_NT, 0, 0, st, p);
+    };
+#define GO(D, MT)                                                                                                                          \
+    (half ? go(attend::Shape<D, MT>(), attend::spec_attend_kernel<__half, D, MT>, attend::spec_join_kernel<__half, D, MT>)                \
+          : go(attend::Shape<D, MT>(), attend::spec_attend_kernel<__nv_bfloat16, D, MT>, attend::spec_join_kernel<__nv_bfloat16, D, MT>))
+    if (a->D == 256) return GO(256, 1);
+    if (a->D == 128) return two_blocks(a) ? GO(128, 2) : GO(128, 1);
+    return two_blocks(a) ? GO(64, 2) : GO(64, 1);
+#undef GO
 }
 
 int32_t spec_cache_commit(const SpecCommit *a, void *stream)
