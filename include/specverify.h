@@ -351,7 +351,7 @@ typedef struct {
     int32_t B, N, Hq, Hkv, D, dtype;
     int32_t num_blocks, block_size, table_width;
     int32_t window, sinks;            /* window 0: none                                               */
-    float scale;
+    float scale;                      /* >= 0, finite                                                 */
     const void *q;
     int64_t q_stride[3];              /* request, node, head                                          */
     const void *k_cache, *v_cache;

@@ -31,6 +31,10 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.69314718055994531f;
 struct Params {
     TreeArgs tree;
     int B, Hq, Hkv, G, num_blocks, block, width, window, sinks;
+    unsigned block_mul;                        // key / block = (umulhi(block_mul, key) + key) >> block_shift for keys below 2^31
+    int block_shift;
+    unsigned group_mul;                        // row / G likewise
+    int group_shift;
     float scale;
     const void *q, *k, *v;
     long long q_stride[3], k_stride[3], v_stride[3];
@@ -40,7 +44,7 @@ struct Params {
     long long out_stride[3];
     float *lse;
     int *status;
-    int ctas;
+    int ctas, groups;                          // CTAs with a run each; groups of 32 rows that a block of rows has at most
     float *part;                               // [ctas][2][D / 4][rows][4] unfinished O
     float2 *ml;                                // [ctas][2][rows] reference and l
     int *late;                                 // [ctas] a wait ran out
@@ -64,16 +68,19 @@ __device__ __forceinline__ Request request_of(const Params &P, int b)
     r.rows = r.n * P.G;
     return r;
 }
+__device__ __forceinline__ int node_of(const Params &P, int row)
+{
+    return (int)((__umulhi(P.group_mul, (unsigned)row) + (unsigned)row) >> P.group_shift);
+}
 __device__ __forceinline__ Tiles tiles_of(const Params &P, const Request &r, int m, int block_rows)
 {
-    const int last = (min(r.rows, (m + 1) * block_rows) - 1) / P.G;          // the block's last node
+    const int last = (m + 1) * block_rows >= r.rows ? r.n - 1 : node_of(P, (m + 1) * block_rows - 1);        // the block's last node
     Tiles t;
-    t.end = (int)(((long long)r.len + last + KT) / KT);
+    t.end = (int)(((unsigned)r.len + (unsigned)last + KT) / KT);
     t.sink = t.from = 0;
     if (P.window) {
-        t.sink = min(t.end, (int)(((long long)min(P.sinks, r.len) + KT - 1) / KT));
-        t.from = max(0, r.len - P.window + 1) / KT;
-        if (t.from < t.sink) t.from = t.sink;
+        t.sink = min(t.end, (int)(((unsigned)min(P.sinks, r.len) + KT - 1) / KT));
+        t.from = max(max(0, r.len - P.window + 1) / KT, t.sink);
     }
     return t;
 }
@@ -84,14 +91,23 @@ __device__ __forceinline__ long long tiles_of_request(const Params &P, int b, in
     for (int m = 0; m * block_rows < r.rows; ++m) s += tiles_of(P, r, m, block_rows).count();
     return s * P.Hkv;
 }
-__device__ __forceinline__ long long run_start(long long all, int c, int ctas) { return all * c / ctas; }
+struct Cuts {                                  // runs of equal length, the first `more` of them longer by one
+    long long all, each;
+    int more;
+    __device__ __forceinline__ Cuts(long long all_, int ctas) : all(all_)
+    {
+        each = all_ <= 0xffffffffll ? (long long)((uint32_t)all_ / (uint32_t)ctas) : all_ / ctas;
+        more = (int)(all_ - each * ctas);
+    }
+    __device__ __forceinline__ long long start(int c) const { return each * c + min(c, more); }
+};
 
 // A place in the order of all tiles: request, block of rows, key head, tile.
 struct Place {
     int b, m, h, i;
 };
 // All threads of the CTA: the number of tiles; in found[], the request that the start of run `c` falls into and the tiles ahead of it.
-__device__ __forceinline__ long long find_request(const Params &P, int block_rows, int c, long long *sums, long long *found, int tid, int threads)
+__device__ __forceinline__ Cuts find_request(const Params &P, int block_rows, int c, long long *sums, long long *found, int tid, int threads)
 {
     const int per = (P.B + threads - 1) / threads, b0 = min(P.B, tid * per), b1 = min(P.B, b0 + per);
     long long mine = 0;
@@ -110,7 +126,8 @@ __device__ __forceinline__ long long find_request(const Params &P, int block_row
         if (w < warp) ahead += sums[w];
         all += sums[w];
     }
-    const long long target = run_start(all, c, P.ctas);
+    const Cuts cuts(all, P.ctas);
+    const long long target = cuts.start(c);
     if (target >= ahead && target < ahead + mine) {
         for (int b = b0; b < b1; ++b) {
             const long long t = tiles_of_request(P, b, block_rows);
@@ -119,7 +136,7 @@ __device__ __forceinline__ long long find_request(const Params &P, int block_row
         }
     }
     __syncthreads();
-    return all;
+    return cuts;
 }
 
 // The unit that a CTA works on, tiles [begin, end) of it, the last first.
@@ -168,8 +185,8 @@ __device__ __forceinline__ Place place_in(const Params &P, int b, long long skip
     for (;; ++p.m) {
         const int count = tiles_of(P, r, p.m, block_rows).count();
         if (skip < (long long)count * P.Hkv) {
-            p.h = (int)(skip / count);
-            p.i = (int)(skip % count);
+            p.h = skip <= 0xffffffffll ? (int)((uint32_t)skip / (uint32_t)count) : (int)(skip / count);
+            p.i = (int)(skip - (long long)p.h * count);
             return p;
         }
         skip -= (long long)count * P.Hkv;
@@ -219,9 +236,13 @@ __device__ __forceinline__ void seen_words(const Params &P, const Request &r, in
         --walk.depth;
     }
 }
-__device__ __forceinline__ int block_of(const Params &P, int b, long long key)
+__device__ __forceinline__ int column_of(const Params &P, int key)
 {
-    const long long col = key / P.block;
+    return (int)((__umulhi(P.block_mul, (unsigned)key) + (unsigned)key) >> P.block_shift);
+}
+// the block of a column of a request's row; -1 where there is none in the cache
+__device__ __forceinline__ int block_in(const Params &P, int b, int col)
+{
     const int id = col < P.width ? __ldg(P.table + (long long)b * P.table_stride + col) : -1;
     return id < 0 || id >= P.num_blocks ? -1 : id;
 }
@@ -231,7 +252,6 @@ template <int D, int MT> struct Shape {
     static constexpr int PANELS = D / 64;
     static constexpr int ROWS = 128 * MT;
     static constexpr int SLOTS = D == 64 ? 10 : MT == 2 || D == 256 ? 9 : 11;     // panels of keys and values in flight
-    static constexpr int LAG = D == 256 ? 1 : D == 128 ? 2 : 3;                    // copies of tiles that a thread has under way
     static constexpr int SOFT = 4 * MT, WARPS = SOFT + 1 + 4, NT = WARPS * 32;    // warps: rows, products, copies
     static constexpr int NP = 128;                                                // threads that copy
     static constexpr int O = 256;                                                 // column of the first O; S buffers at 0 and 128
@@ -300,71 +320,79 @@ template <> struct Pair<__half> {
     static __device__ __forceinline__ float value(unsigned short x) { return __half2float(__ushort_as_half(x)); }
 };
 
-// y of 32 columns and what comes of them
+// The largest of 32 columns of scores that the row sees.
+template <bool MASK> __device__ __forceinline__ float top_of(const uint32_t (&s)[32], uint32_t word, float top)
+{
+#pragma unroll
+    for (int k = 0; k < 32; k += 2) {
+        const float x = !MASK || (word >> k) & 1u ? __uint_as_float(s[k]) : -CUDART_INF_F;
+        const float y = !MASK || (word >> (k + 1)) & 1u ? __uint_as_float(s[k + 1]) : -CUDART_INF_F;
+        top = fmaxf(top, fmaxf(x, y));
+    }
+    return top;
+}
+// 32 columns of scores: weights, their sum, and the weights rounded to the values' type, two to a register.
 template <typename T, bool MASK>
-__device__ __forceinline__ void weigh(const uint32_t (&s)[32], uint32_t word, unsigned long long c2, unsigned long long r2, float &top,
-                                      unsigned long long &sum, uint32_t *pk)
+__device__ __forceinline__ void weigh(const uint32_t (&s)[32], uint32_t word, unsigned long long c2, unsigned long long r2,
+                                      unsigned long long &sum, uint32_t (&pk)[16])
 {
 #pragma unroll
     for (int k = 0; k < 32; k += 2) {
         const unsigned long long y2 = fma_f32x2(pack_f32x2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, r2);
         float y0, y1;
         unpack_f32x2(y2, y0, y1);
+        float p0 = ex2_approx(y0), p1 = ex2_approx(y1);
         if (MASK) {
-            y0 = (word >> k) & 1u ? y0 : -CUDART_INF_F;
-            y1 = (word >> (k + 1)) & 1u ? y1 : -CUDART_INF_F;
+            p0 = (word >> k) & 1u ? p0 : 0.f;
+            p1 = (word >> (k + 1)) & 1u ? p1 : 0.f;
         }
-        top = fmaxf(top, fmaxf(y0, y1));
-        const float p0 = ex2_approx(y0), p1 = ex2_approx(y1);
         sum = add_f32x2(sum, pack_f32x2(p0, p1));
         pk[k / 2] = Pair<T>::pack(p0, p1);
     }
 }
-template <bool MASK> __device__ __forceinline__ void raise_top(const uint32_t (&s)[32], uint32_t word, float c, float &top)
-{
-#pragma unroll
-    for (int k = 0; k < 32; ++k) {
-        const float y = __uint_as_float(s[k]) * c;
-        top = fmaxf(top, !MASK || ((word >> k) & 1u) ? y : -CUDART_INF_F);
-    }
-}
-// A row's tile: largest y (against the reference), sum and packed weights.  128 columns in four loads, each under way while the one before
-// is worked on.
-template <typename T, bool MASK>
-__device__ __forceinline__ float weigh_tile(uint32_t at, const uint32_t (&words)[4], float c, float ref, float &sum, uint32_t (&pk)[64])
+// The largest score of a tile; a load under way while the columns before are worked on.
+template <bool MASK> __device__ __forceinline__ float tile_top(uint32_t at, const uint32_t (&words)[4])
 {
     uint32_t a[32], b[32];
     float top = -CUDART_INF_F;
+    tc::tmem_load(at, a);
+    tc::wait_loads(a);
+    tc::tmem_load(at + 32, b);
+    top = top_of<MASK>(a, words[0], top);
+    tc::wait_loads(b);
+    tc::tmem_load(at + 64, a);
+    top = top_of<MASK>(b, words[1], top);
+    tc::wait_loads(a);
+    tc::tmem_load(at + 96, b);
+    top = top_of<MASK>(a, words[2], top);
+    tc::wait_loads(b);
+    return top_of<MASK>(b, words[3], top);
+}
+// A tile's weights, put in the place of its scores (16 columns for 32: never beyond the scores that are loaded); returns their sum.
+template <typename T, bool MASK> __device__ __forceinline__ float tile_weights(uint32_t at, const uint32_t (&words)[4], float c, float ref)
+{
+    uint32_t a[32], b[32], pk[16];
     unsigned long long s2 = 0ull;
     const unsigned long long c2 = pack_f32x2(c, c), r2 = pack_f32x2(-ref, -ref);
     tc::tmem_load(at, a);
     tc::wait_loads(a);
     tc::tmem_load(at + 32, b);
-    weigh<T, MASK>(a, words[0], c2, r2, top, s2, pk);
+    weigh<T, MASK>(a, words[0], c2, r2, s2, pk);
     tc::wait_loads(b);
+    tc::tmem_store16(at, pk);
     tc::tmem_load(at + 64, a);
-    weigh<T, MASK>(b, words[1], c2, r2, top, s2, pk + 16);
+    weigh<T, MASK>(b, words[1], c2, r2, s2, pk);
     tc::wait_loads(a);
+    tc::tmem_store16(at + 16, pk);
     tc::tmem_load(at + 96, b);
-    weigh<T, MASK>(a, words[2], c2, r2, top, s2, pk + 32);
+    weigh<T, MASK>(a, words[2], c2, r2, s2, pk);
     tc::wait_loads(b);
-    weigh<T, MASK>(b, words[3], c2, r2, top, s2, pk + 48);
+    tc::tmem_store16(at + 32, pk);
+    weigh<T, MASK>(b, words[3], c2, r2, s2, pk);
+    tc::tmem_store16(at + 48, pk);
     float x, y;
     unpack_f32x2(s2, x, y);
-    sum = x + y;
-    return top;
-}
-template <bool MASK> __device__ __forceinline__ float top_of_tile(uint32_t at, const uint32_t (&words)[4], float c)
-{
-    uint32_t a[32];
-    float top = -CUDART_INF_F;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        tc::tmem_load(at + 32 * w, a);
-        tc::wait_loads(a);
-        raise_top<MASK>(a, words[w], c, top);
-    }
-    return top;
+    return x + y;
 }
 
 template <typename T, int D, int MT>
@@ -373,7 +401,9 @@ __global__ void __launch_bounds__(Shape<D, MT>::NT, 1) spec_attend_kernel(const 
     using S = Shape<D, MT>;
     unsigned char *base = dyn_smem + (-smem_u32(dyn_smem) & 1023u);
     Bars *B = (Bars *)(base + S::off_bar);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c = blockIdx.x;
+    // what needs no input comes ahead of the wait for the kernel before
+    if (warp == S::SOFT) tc::tmem_alloc(&B->tmem, 512);
     if (tid == 0) {
         for (int i = 0; i < S::SLOTS; ++i) { mbar_init(&B->full[i], S::NP); mbar_init(&B->empty[i], 1); }
         mbar_init(&B->q_full, S::NP);
@@ -386,23 +416,15 @@ __global__ void __launch_bounds__(Shape<D, MT>::NT, 1) spec_attend_kernel(const 
         }
         B->dead = 0;
         B->poison = 0;
-        B->found[0] = -1;
         mbar_fence_init();
     }
     grid_dependency_wait();
     grid_launch_dependents();                  // (the joining kernel's CTAs may be placed as this one's leave; it waits by itself)
-    __syncthreads();
-    const int c = blockIdx.x;
-    const long long all = find_request(P, S::ROWS, c, B->sums, B->found, tid, S::NT);
+    const Cuts cuts = find_request(P, S::ROWS, c, B->sums, B->found, tid, S::NT);
     Run run;
-    run.left = run_start(all, c + 1, P.ctas) - run_start(all, c, P.ctas);
+    run.left = cuts.start(c + 1) - cuts.start(c);
     run.first = true;
-    if (run.left <= 0) {
-        if (tid == 0) P.late[c] = 0;
-        return;
-    }
-    run.at = place_in(P, (int)B->found[0], run_start(all, c, P.ctas) - B->found[1], S::ROWS);
-    if (warp == S::SOFT) tc::tmem_alloc(&B->tmem, 512);
+    if (run.left > 0) run.at = place_in(P, (int)B->found[0], cuts.start(c) - B->found[1], S::ROWS);
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
@@ -421,7 +443,7 @@ __global__ void __launch_bounds__(Shape<D, MT>::NT, 1) spec_attend_kernel(const 
                 n_run += seg.steps();
                 continue;
             }
-            const int r = seg.m * S::ROWS + row, node = min(r, seg.r.rows - 1) / P.G;
+            const int r = seg.m * S::ROWS + row, node = node_of(P, min(r, seg.r.rows - 1));
             const bool live = row < seg.rows, warp_live = t * 128 + quad * 32 < seg.rows;
             if (tree_of != seg.b && (tree_of < 0 || P.tree.topo_seq_stride || P.tree.n_nodes)) {
                 bar_sync(1 + t, 128);
@@ -450,23 +472,20 @@ __global__ void __launch_bounds__(Shape<D, MT>::NT, 1) spec_attend_kernel(const 
                     const volatile uint32_t *hidden = B->hidden[n_run & 7];
                     const uint32_t h0 = hidden[0], h1 = hidden[1], h2 = hidden[2], h3 = hidden[3];
                     const bool masked = !seen_by_all(P, seg.r, tile) || (h0 | h1 | h2 | h3) != 0;
-                    uint32_t words[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu}, pk[64];
+                    uint32_t words[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
                     if (masked) {
                         seen_words(P, seg.r, tile, depth, parent, walk, words);
                         words[0] &= ~h0; words[1] &= ~h1; words[2] &= ~h2; words[3] &= ~h3;
                     }
+                    float top = (masked ? tile_top<true>(s_at, words) : tile_top<false>(s_at, words)) * c;       // (c >= 0)
+                    if (!(top > -CUDART_INF_F)) top = -CUDART_INF_F;         // (0 times infinity: a row without scores to speak of)
                     if (step == 0) {
-                        const float top = masked ? top_of_tile<true>(s_at, words, c) : top_of_tile<false>(s_at, words, c);
                         any = top > -CUDART_INF_F;
                         ref = any ? top : 0.f;
-                    }
-                    float sum;
-                    const float top = masked ? weigh_tile<T, true>(s_at, words, c, ref, sum, pk) : weigh_tile<T, false>(s_at, words, c, ref, sum, pk);
-                    const bool over = step > 0 && (any ? top > 8.f : top > -CUDART_INF_F);
-                    if (__any_sync(0xffffffffu, over)) {
-                        // a new reference: what has been summed is scaled, the tile gone through again
+                    } else if (const bool over = any ? top > ref + 8.f : top > -CUDART_INF_F; __any_sync(0xffffffffu, over)) {
+                        // a new reference: what has been summed is scaled
                         const float old = ref;
-                        if (over) ref = ref + top;
+                        if (over) ref = top;
                         const float f = over && any ? ex2_approx(old - ref) : 1.f;
                         any |= over;
                         l *= f;
@@ -481,26 +500,24 @@ __global__ void __launch_bounds__(Shape<D, MT>::NT, 1) spec_attend_kernel(const 
                             for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
                             tc::tmem_store(o_at + d, o);
                         }
-                        tc::wait_stores();
-                        masked ? weigh_tile<T, true>(s_at, words, c, ref, sum, pk) : weigh_tile<T, false>(s_at, words, c, ref, sum, pk);
                     }
-                    l += sum;
-                    tc::tmem_store(s_at, pk);
-                    tc::tmem_store(s_at + 32, pk + 32);
+                    l += masked ? tile_weights<T, true>(s_at, words, c, ref) : tile_weights<T, false>(s_at, words, c, ref);
                     tc::wait_stores();
                     tc::fence_before();
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&B->p_full[buf]);
             }
-            // the segment's end
+            // the segment's end.  The last scores follow all products but the last two (one: MT = 2): a phase at a time, or its parity
+            // would be taken for that of the one before
+            if (MT == 1 && n_tile > 1) wait(B, &B->pv_done[t], n_tile & 1);
             wait(B, &B->pv_done[t], (n_tile - 1) & 1);
             tc::fence_after();
             if (warp_live) {
                 const bool poison = *(volatile int *)&B->poison != 0;
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 const long long slot = (long long)blockIdx.x * 2 + (seg.head ? 0 : 1);
-                const int head = seg.h * P.G + r % P.G;
+                const int head = seg.h * P.G + r - node * P.G;
                 T *to = (T *)P.out + seg.b * P.out_stride[0] + node * P.out_stride[1] + head * P.out_stride[2];
                 float *part = P.part + slot * S::ROWS * D;
 #pragma unroll 1
@@ -521,11 +538,10 @@ __global__ void __launch_bounds__(Shape<D, MT>::NT, 1) spec_attend_kernel(const 
                             for (int j = 0; j < KT; ++j) {
                                 const uint32_t word = j < 32 ? words[0] : j < 64 ? words[1] : j < 96 ? words[2] : words[3];
                                 if (!((word >> (j & 31)) & 1u)) continue;
-                                const long long key = (long long)tile * KT + j;
-                                const int id = block_of(P, seg.b, key);
+                                const int key = tile * KT + j, col = column_of(P, key), id = block_in(P, seg.b, col);
                                 if (id < 0) continue;
-                                const unsigned short *v = (const unsigned short *)P.v + id * P.v_stride[0] + key % P.block * P.v_stride[1] +
-                                                          seg.h * P.v_stride[2] + d;
+                                const unsigned short *v = (const unsigned short *)P.v + id * P.v_stride[0] +
+                                                          (key - col * P.block) * P.v_stride[1] + seg.h * P.v_stride[2] + d;
 #pragma unroll
                                 for (int k = 0; k < 32; ++k) {
                                     const float x = Pair<T>::value(__ldg(v + k));
@@ -601,7 +617,11 @@ __global__ void __launch_bounds__(Shape<D, MT>::NT, 1) spec_attend_kernel(const 
         };
         while (run.next(P, S::ROWS, seg)) {
             const int steps = seg.steps(), tiles = MT == 1 || seg.rows <= 128 ? 1 : 2;
-            const auto keys_in = [&](uint32_t n) { for (int p = 0; p < S::PANELS; ++p) slot_wait(n + p); tc::fence_after(); };
+            const auto keys_in = [&](uint32_t n) {
+                for (int p = 0; p < S::PANELS; ++p) slot_wait(n + p);
+                tc::publish_shared();              // (the copies' writes, seen through the barrier, for the tensor cores)
+                tc::fence_after();
+            };
             wait(B, &B->q_full, n_seg & 1);
             if (MT == 1) {
                 // order of the slots: K0, K1, V0, K2, V1, ...: scores one tile ahead
@@ -658,72 +678,64 @@ __global__ void __launch_bounds__(Shape<D, MT>::NT, 1) spec_attend_kernel(const 
         const int pt = tid - (S::SOFT + 1) * 32;
         constexpr int CH = D / 8, RPI = S::NP / CH;                   // chunks of a row; rows that the threads copy at a time
         const int ch = pt % CH, r0 = pt / CH;
+        const uint32_t to0 = (uint32_t)(r0 * 128);
         const uint32_t slots = smem_u32(base + S::off_slots), q_at = smem_u32(base);
         ulonglong2 *rows = (ulonglong2 *)(base + S::off_rows);
         uint32_t n_slot = 0, n_seg = 0, n_row = 0;
-        uint32_t open[S::LAG + 1];                                    // the copies under way: slot, and whether values of a tile in part seen
-        int under = 0;
-        for (int i = 0; i <= S::LAG; ++i) open[i] = 0;
-        // a copy's arrival: values that are not finite leave a tile that some rows do not see
-        const auto arrive = [&](uint32_t o) {
-            const uint32_t n = o >> 2;
-            if (o & 2) {
+        // Copies arrive on their barrier by themselves.  Not so values of a tile that some rows do not see: entries that are not finite
+        // leave it first, as 0 times them would reach those rows.  That waits until the next copies are under way, or until there is no
+        // room for them.
+        bool late_values = false, before = false;                     // (before: the tile before is one that some rows do not see)
+        uint32_t late_slot = 0;
+        const auto clean = [&]() {
 #pragma unroll 1
-                for (int i = r0; i < KT; i += RPI) {
-                    unsigned char *at = base + S::off_slots + (n + ch / 8) % S::SLOTS * PANEL + i * 128 + (((ch & 7) ^ (i & 7)) << 4);
-                    uint4 w = *(uint4 *)at;
-                    uint32_t *x = (uint32_t *)&w;
-                    bool bad = false;
+            for (int i = r0; i < KT; i += RPI) {
+                unsigned char *at = base + S::off_slots + (late_slot + ch / 8) % S::SLOTS * PANEL + i * 128 + (((ch & 7) ^ (i & 7)) << 4);
+                uint4 w = *(uint4 *)at;
+                uint32_t *x = (uint32_t *)&w;
+                bool bad = false;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        if (Pair<T>::finite(x[k])) continue;
-                        bad = true;
-                        const uint32_t lo = x[k] & 0xFFFFu, hi = x[k] & 0xFFFF0000u;
-                        x[k] = (Pair<T>::finite(lo) ? lo : 0u) | (Pair<T>::finite(hi) ? hi : 0u);
-                    }
-                    if (bad) { *(uint4 *)at = w; *(volatile int *)&B->poison = 1; }
+                for (int k = 0; k < 4; ++k) {
+                    if (Pair<T>::finite(x[k])) continue;
+                    bad = true;
+                    const uint32_t lo = x[k] & 0xFFFFu, hi = x[k] & 0xFFFF0000u;
+                    x[k] = (Pair<T>::finite(lo) ? lo : 0u) | (Pair<T>::finite(hi) ? hi : 0u);
                 }
+                if (bad) { *(uint4 *)at = w; *(volatile int *)&B->poison = 1; }
             }
             tc::publish_shared();
-            if (o & 1) mbar_arrive(&B->q_full);
-            else for (int p = 0; p < S::PANELS; ++p) mbar_arrive(&B->full[(n + p) % S::SLOTS]);
+            for (int p = 0; p < S::PANELS; ++p) mbar_arrive(&B->full[(late_slot + p) % S::SLOTS]);
+            late_values = false;
         };
-        // closes the copies issued last and lets the oldest arrive
-        const auto turn = [&](uint32_t o) {
-            tc::close_copies();
-#pragma unroll
-            for (int i = S::LAG; i > 0; --i) open[i] = open[i - 1];
-            open[0] = o;
-            if (under < S::LAG) { ++under; return; }
-            tc::wait_copies<S::LAG>();
-            arrive(open[S::LAG]);
-        };
-        // A wait for room.  Copies under way arrive first: what has been copied may be what the room is waiting for.
+        // a wait for room: values that are held back may be what the room is waiting for
         const auto room = [&](uint64_t *bar, uint32_t parity) {
-            if (mbar_test(bar, parity)) return;
-            tc::wait_copies<0>();
-            for (int i = under - 1; i >= 0; --i) {
-#pragma unroll
-                for (int j = 0; j < S::LAG; ++j) if (j == i) arrive(open[j]);
-            }
-            under = 0;
+            if (late_values && !mbar_test(bar, parity)) { tc::wait_copies<0>(); clean(); }
             wait(B, bar, parity);
         };
-        // sources of a tile's rows, one per thread: null where no row of the request sees the key or its block is bad
-        const auto sources = [&](const Segment &s, int tile) {
+        // Block of the thread's key of a tile, -1 where no row of the request sees it: asked for a tile ahead of its use.
+        struct Source { int id, in; bool seen; };
+        const auto source = [&](const Segment &s, int tile) {
             const long long key = (long long)tile * KT + pt;
-            const bool seen = key < (long long)s.r.len + s.r.n &&
-                              (key >= s.r.len || P.window == 0 || key < P.sinks || key > (long long)s.r.len - P.window);
-            const int id = seen ? block_of(P, s.b, key) : -1;
-            ulonglong2 a = make_ulonglong2(0, 0);
-            if (id >= 0) {
-                const int in = (int)(key % P.block);
-                a.x = (unsigned long long)((const T *)P.k + id * P.k_stride[0] + in * P.k_stride[1] + s.h * P.k_stride[2]);
-                a.y = (unsigned long long)((const T *)P.v + id * P.v_stride[0] + in * P.v_stride[1] + s.h * P.v_stride[2]);
+            Source x = {-1, 0, key < (long long)s.r.len + s.r.n &&
+                                   (key >= s.r.len || P.window == 0 || key < P.sinks || key > (long long)s.r.len - P.window)};
+            if (x.seen) {
+                const int col = column_of(P, (int)key);
+                x.in = (int)key - col * P.block;
+                x.id = col < P.width ? __ldg(P.table + (long long)s.b * P.table_stride + col) : -1;
+            }
+            return x;
+        };
+        // addresses of a tile's rows, one per thread: odd where no row of the request sees the key or its block is bad
+        const auto put_sources = [&](const Segment &s, const Source &x) {
+            const bool good = x.seen && x.id >= 0 && x.id < P.num_blocks;
+            ulonglong2 a = make_ulonglong2((unsigned long long)P.k | 1, (unsigned long long)P.v | 1);       // (odd: zeros, nothing is read)
+            if (good) {
+                a.x = (unsigned long long)((const T *)P.k + x.id * P.k_stride[0] + x.in * P.k_stride[1] + s.h * P.k_stride[2]);
+                a.y = (unsigned long long)((const T *)P.v + x.id * P.v_stride[0] + x.in * P.v_stride[1] + s.h * P.v_stride[2]);
             }
             bar_sync(4, S::NP);                                       // (all are through with the tile before the last)
             rows[(n_row & 1) * KT + pt] = a;
-            const uint32_t bad = __ballot_sync(0xffffffffu, seen && id < 0);
+            const uint32_t bad = __ballot_sync(0xffffffffu, x.seen && !good);
             if (lane == 0) B->hidden[n_row & 7][pt >> 5] = bad;
             bar_sync(4, S::NP);
             ++n_row;
@@ -733,54 +745,68 @@ __global__ void __launch_bounds__(Shape<D, MT>::NT, 1) spec_attend_kernel(const 
                 const uint32_t k = n + p;
                 if (k >= S::SLOTS) room(&B->empty[k % S::SLOTS], (k / S::SLOTS - 1) & 1);
             }
-            const ulonglong2 *from = rows + (which & 1) * KT;
-#pragma unroll 8
-            for (int i = r0; i < KT; i += RPI) {
-                const unsigned long long a = values ? from[i].y : from[i].x;
-                tc::copy16(slots + (n + ch / 8) % S::SLOTS * PANEL + i * 128 + (((ch & 7) ^ (i & 7)) << 4), a ? (const char *)a + ch * 16 : nullptr, P.k);
+            const unsigned long long *from = (const unsigned long long *)(rows + (which & 1) * KT) + (values ? 1 : 0);
+            const uint32_t to = slots + (n + ch / 8) % S::SLOTS * PANEL + to0;
+            constexpr int EACH = KT / RPI, STEP = 8;
+#pragma unroll 1
+            for (int k0 = 0; k0 < EACH; k0 += STEP) {
+                unsigned long long a[STEP];
+#pragma unroll
+                for (int k = 0; k < STEP; ++k) a[k] = from[2 * (r0 + (k0 + k) * RPI)];
+#pragma unroll
+                for (int k = 0; k < STEP; ++k)
+                    tc::copy16(to + (k0 + k) * RPI * 128 + (((ch & 7) ^ ((r0 + k * RPI) & 7)) << 4), (a[k] & ~1ull) + ch * 16, a[k] & 1 ? 0 : 16);
             }
-            turn(n << 2 | (values && part ? 2u : 0u));
+            const bool hold = values && part;
+            if (!hold)
+                for (int p = 0; p < S::PANELS; ++p) tc::arrive_with_copies(&B->full[(n + p) % S::SLOTS]);
+            tc::close_copies();
+            if (late_values) { tc::wait_copies<1>(); clean(); }
+            if (hold) { late_values = true; late_slot = n; }
         };
-        while (run.next(P, S::ROWS, seg)) {
-            const int steps = seg.steps();
-            const auto copy_q = [&]() {
-                if (n_seg) room(&B->q_empty, (n_seg - 1) & 1);
-                for (int i = r0; i < S::ROWS; i += RPI) {
-                    const int r = seg.m * S::ROWS + i;
-                    const T *from = nullptr;
-                    if (i < seg.rows)
-                        from = (const T *)P.q + seg.b * P.q_stride[0] + r / P.G * P.q_stride[1] + (seg.h * P.G + r % P.G) * P.q_stride[2] + ch * 8;
-                    tc::copy16(q_at + ((ch / 8) * MT + i / 128) * PANEL + i % 128 * 128 + (((ch & 7) ^ (i & 7)) << 4), from, P.q);
-                }
-                turn(1u);
-                ++n_seg;
-            };
-            uint32_t last_row = 0;
-            bool last_part = false;
-            for (int i = 0; i < steps; ++i) {
-                const int tile = seg.tile(i);
-                const bool part = !seen_by_all(P, seg.r, tile);
-                sources(seg, tile);
+        const auto copy_q = [&](const Segment &s) {
+            if (n_seg) room(&B->q_empty, (n_seg - 1) & 1);
+            const T *q = (const T *)P.q + s.b * P.q_stride[0] + s.h * P.G * P.q_stride[2] + ch * 8;
+#pragma unroll 4
+            for (int i = r0; i < S::ROWS; i += RPI) {
+                const int r = s.m * S::ROWS + i, node = node_of(P, r);
+                const bool in = i < s.rows;
+                tc::copy16(q_at + ((ch / 8) * MT + i / 128) * PANEL + i % 128 * 128 + (((ch & 7) ^ (i & 7)) << 4),
+                           (unsigned long long)(in ? q + node * P.q_stride[1] + (r - node * P.G) * P.q_stride[2] : (const T *)P.q), in ? 16 : 0);
+            }
+            tc::arrive_with_copies(&B->q_full);
+            tc::close_copies();
+            ++n_seg;
+        };
+        if (run.next(P, S::ROWS, seg)) {
+            bool more = true;
+            int step = 0;
+            Source src = source(seg, seg.tile(0));
+            while (more) {
+                const Segment now = seg;
+                const int at = step;
+                const Source here = src;
+                const bool last = ++step == now.steps();
+                if (last) { more = run.next(P, S::ROWS, seg); step = 0; }
+                if (more) src = source(seg, seg.tile(step));
+                const bool part = !seen_by_all(P, now.r, now.tile(at));
+                put_sources(now, here);
                 copy_tile(n_slot, n_row - 1, false, part);
                 n_slot += S::PANELS;
-                if (i == 0) copy_q();
+                if (at == 0) copy_q(now);
                 if (MT == 1) {
-                    if (i > 0) { copy_tile(n_slot, last_row, true, last_part); n_slot += S::PANELS; }
-                    last_row = n_row - 1;
-                    last_part = part;
+                    // values a tile behind the keys
+                    if (at > 0) { copy_tile(n_slot, n_row - 2, true, before); n_slot += S::PANELS; }
+                    if (last) { copy_tile(n_slot, n_row - 1, true, part); n_slot += S::PANELS; }
+                    before = part;
                 } else {
                     copy_tile(n_slot, n_row - 1, true, part);
                     n_slot += S::PANELS;
                 }
             }
-            if (MT == 1) { copy_tile(n_slot, last_row, true, last_part); n_slot += S::PANELS; }
         }
-        // the last arrivals
         tc::wait_copies<0>();
-        for (int i = under - 1; i >= 0; --i) {
-#pragma unroll
-            for (int j = 0; j < S::LAG; ++j) if (j == i) arrive(open[j]);
-        }
+        if (late_values) clean();
     }
     tc::fence_before();
     __syncthreads();
@@ -795,17 +821,18 @@ __global__ void __launch_bounds__(Shape<D, MT>::NT, 1) spec_attend_kernel(const 
 // The first P.ctas * groups CTAs: (start of run j + 1, 32 rows).  Where that start lies inside a unit and is the first to, the unit's
 // parts are put together: out = sum 2^(ref_c - ref) O_c / sum 2^(ref_c - ref) l_c.  The others: a request each, its status (while the
 // attention still runs: that reads inputs alone) and zeros for a bad tree.
-constexpr int JOIN_NT = 256, CTAS_MAX = 256;
+constexpr int JOIN_NT = 256, CTAS_MAX = 160;
 
 template <typename T, int D, int MT> __global__ void __launch_bounds__(JOIN_NT) spec_join_kernel(const __grid_constant__ Params P)
 {
     using S = Shape<D, MT>;
-    constexpr int GROUPS = S::ROWS / 32, WARPS = JOIN_NT / 32;
-    __shared__ float share[CTAS_MAX][32];
+    constexpr int WARPS = JOIN_NT / 32;
+    __shared__ float share[CTAS_MAX][32], sum_of[CTAS_MAX][32], inverse[32];
     __shared__ long long sums[WARPS], found[2];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if ((int)blockIdx.x >= P.ctas * GROUPS) {
-        const int b = blockIdx.x - P.ctas * GROUPS;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, groups = P.groups;
+    grid_launch_dependents();                  // (the next kernel waits for this one by itself, and this one for the attention)
+    if ((int)blockIdx.x >= P.ctas * groups) {
+        const int b = blockIdx.x - P.ctas * groups;
         const int len = __ldg(P.tree.lengths + b), nn = tree_nodes(P.tree, b), n = len < 0 ? 0 : max(nn, 0);
         const int *parent = P.tree.parent + (long long)b * P.tree.topo_seq_stride;
         bool bad = false, page = false;
@@ -818,7 +845,7 @@ template <typename T, int D, int MT> __global__ void __launch_bounds__(JOIN_NT) 
         const long long sinks = min((long long)P.sinks, (long long)len), cols = (keys + P.block - 1) / P.block;
         for (long long col = tid; col < cols; col += JOIN_NT) {
             const long long a = col * P.block, e = a + P.block;
-            if (e > since || a < sinks) page |= block_of(P, b, a) < 0;
+            if (e > since || a < sinks) page |= block_in(P, b, (int)col) < 0;
         }
         bad = __syncthreads_or(bad) != 0;
         page = __syncthreads_or(page) != 0;
@@ -837,56 +864,79 @@ template <typename T, int D, int MT> __global__ void __launch_bounds__(JOIN_NT) 
         }
         return;
     }
-    const int j = blockIdx.x / GROUPS, group = blockIdx.x % GROUPS;
+    const int j = blockIdx.x / groups, group = blockIdx.x % groups;
     if (tid == 0) found[0] = -1;
     __syncthreads();
-    const long long all = find_request(P, S::ROWS, j + 1, sums, found, tid, JOIN_NT);
-    const long long cut = run_start(all, j + 1, P.ctas);
+    const Cuts cuts = find_request(P, S::ROWS, j + 1, sums, found, tid, JOIN_NT);
+    const long long cut = cuts.start(j + 1);
     if (j + 1 < P.ctas && found[0] >= 0) {
         const int b = (int)found[0];
         const Place at = place_in(P, b, cut - found[1], S::ROWS);
         const Request r = request_of(P, b);
         const long long begin = cut - at.i, end = begin + tiles_of(P, r, at.m, S::ROWS).count();
-        const int rows = min(r.rows - at.m * S::ROWS, S::ROWS), row = group * 32 + lane;
-        if (at.i > 0 && run_start(all, j, P.ctas) <= begin && group * 32 < rows) {
+        const int rows = min(min(r.rows - at.m * S::ROWS, S::ROWS) - group * 32, 32), row0 = group * 32;
+        if (at.i > 0 && cuts.start(j) <= begin && rows > 0) {
+            // CTAs j .. last have a part each (the first `last` whose run starts before the unit's end; a cut inside the unit means that
+            // no run is empty but where there are fewer tiles than CTAs, and then the empty ones come last)
+            if (tid == 0) found[0] = j;
+            __syncthreads();
+            for (int c = j + 1 + tid; c < P.ctas; c += JOIN_NT)
+                if (cuts.start(c) < end && cuts.start(c + 1) >= end) found[0] = c;
+            __syncthreads();
+            const int last = (int)found[0];
+            // the first one's run may start before the unit
+            const auto slot = [&](int c) { return 2 * c + (c == j && cuts.start(j) < begin ? 1 : 0); };
             grid_dependency_wait();
-            // CTA c's part: where its run starts is the unit's start or inside it; the first CTA's may start before
-            int last = j;
-            while (last + 1 < P.ctas && run_start(all, last + 1, P.ctas) < end) ++last;
-            const auto slot = [&](int c) { return 2 * c + (run_start(all, c, P.ctas) < begin ? 1 : 0); };
-            const auto has = [&](int c) { return run_start(all, c, P.ctas) < run_start(all, c + 1, P.ctas); };
-            for (int c = j + warp; c <= last; c += WARPS)
-                share[c][lane] = has(c) && row < rows ? __ldcg(&P.ml[(long long)slot(c) * S::ROWS + row].x) : -CUDART_INF_F;
-            __syncthreads();
-            float ref = -CUDART_INF_F, l = 0.f;
-            for (int c = j; c <= last; ++c) ref = fmaxf(ref, share[c][lane]);
-            __syncthreads();
-            const float base = ref == -CUDART_INF_F ? 0.f : ref;
-            for (int c = j + warp; c <= last; c += WARPS) {
-                const float x = share[c][lane];
-                // (a part whose reference is no number stays what it is: its sums are not either)
-                share[c][lane] = x == -CUDART_INF_F ? 0.f : ex2_approx(x - base);
+            for (int i = tid; i < (last + 1 - j) * rows; i += JOIN_NT) {
+                const int c = j + i / rows, row = i % rows;
+                const float2 x = __ldcg(&P.ml[(long long)slot(c) * S::ROWS + row0 + row]);
+                share[c][row] = x.x;
+                sum_of[c][row] = x.y;
             }
             __syncthreads();
-            if (row < rows) {
-                for (int c = j; c <= last; ++c)
-                    if (has(c)) l += share[c][lane] == 0.f ? 0.f : share[c][lane] * __ldcg(&P.ml[(long long)slot(c) * S::ROWS + row].y);
-                const float inv = l == 0.f ? 0.f : 1.f / l;
-                const int q = at.m * S::ROWS + row, node = q / P.G, head = at.h * P.G + q % P.G;
-                T *to = (T *)P.out + b * P.out_stride[0] + node * P.out_stride[1] + head * P.out_stride[2];
-                for (int ch = warp; ch < D / 4; ch += WARPS) {
-                    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-                    for (int c = j; c <= last; ++c) {
-                        const float w = share[c][lane];
-                        if (w == 0.f) continue;
-                        const float4 x = __ldcg((const float4 *)P.part + ((long long)slot(c) * (D / 4) + ch) * S::ROWS + row);
-                        o.x = fmaf(w, x.x, o.x); o.y = fmaf(w, x.y, o.y); o.z = fmaf(w, x.z, o.z); o.w = fmaf(w, x.w, o.w);
-                    }
-                    *(uint2 *)(to + ch * 4) = make_uint2(Pair<T>::pack(o.x * inv, o.y * inv), Pair<T>::pack(o.z * inv, o.w * inv));
+            // a warp per row: the largest reference, the parts' weights, the sum
+            for (int row = warp; row < rows; row += WARPS) {
+                float ref = -CUDART_INF_F, l = 0.f;
+                for (int c = j + lane; c <= last; c += 32) ref = fmaxf(ref, share[c][row]);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) ref = fmaxf(ref, __shfl_xor_sync(0xffffffffu, ref, o));
+                for (int c = j + lane; c <= last; c += 32) {
+                    // (a part that saw nothing counts for nothing, whatever the others' reference)
+                    const float w = share[c][row] == -CUDART_INF_F ? 0.f : ex2_approx(share[c][row] - ref);
+                    share[c][row] = w;
+                    if (w != 0.f) l = fmaf(w, sum_of[c][row], l);
                 }
-                if (P.lse && warp == 0)
-                    P.lse[((long long)b * P.tree.N + node) * P.Hq + head] = l == 0.f ? -CUDART_INF_F : (ref + log2f(l)) * LN2;
+                l = warp_sum(l);
+                if (lane == 0) {
+                    inverse[row] = l == 0.f ? 0.f : 1.f / l;
+                    if (P.lse) {
+                        const int q = at.m * S::ROWS + row0 + row;
+                        P.lse[((long long)b * P.tree.N + q / P.G) * P.Hq + at.h * P.G + q % P.G] =
+                            l == 0.f ? -CUDART_INF_F : (ref + log2f(l)) * LN2;
+                    }
+                }
+            }
+            __syncthreads();
+            // a thread per four entries of a row, parts in order, eight loads under way
+            for (int i = tid; i < rows * (D / 4); i += JOIN_NT) {
+                const int row = i % rows, ch = i / rows;
+                const float4 *part = (const float4 *)P.part + (long long)ch * S::ROWS + row0 + row;
+                constexpr long long STEP = (long long)(D / 4) * S::ROWS;
+                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int c0 = j; c0 <= last; c0 += 8) {
+                    float4 x[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[k] = __ldcg(part + slot(min(c0 + k, last)) * STEP);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const float w = c0 + k <= last ? share[c0 + k][row] : 0.f;
+                        if (w != 0.f) { o.x = fmaf(w, x[k].x, o.x); o.y = fmaf(w, x[k].y, o.y); o.z = fmaf(w, x[k].z, o.z); o.w = fmaf(w, x[k].w, o.w); }
+                    }
+                }
+                const int q = at.m * S::ROWS + row0 + row;
+                const float inv = inverse[row];
+                T *to = (T *)P.out + b * P.out_stride[0] + q / P.G * P.out_stride[1] + (at.h * P.G + q % P.G) * P.out_stride[2] + ch * 4;
+                *(uint2 *)to = make_uint2(Pair<T>::pack(o.x * inv, o.y * inv), Pair<T>::pack(o.z * inv, o.w * inv));
             }
             return;
         }

@@ -174,7 +174,7 @@ static int attention_check(const SpecAttention *a)
         a->table_stride < a->table_width || a->Hkv < 1 || a->Hq < a->Hkv || a->Hq % a->Hkv || a->Hq > 65535)
         return SPEC_ERR_SHAPE;
     if (a->dtype != SPEC_BF16 && a->dtype != SPEC_F16) return SPEC_ERR_DTYPE;
-    if (!(a->scale > -3.4e38f && a->scale < 3.4e38f) || a->window < 0 || a->sinks < 0) return SPEC_ERR_PARAM;
+    if (!(a->scale >= 0.f && a->scale <= 3.4e38f) || a->window < 0 || a->sinks < 0) return SPEC_ERR_PARAM;
     if (a->D != 64 && a->D != 128 && a->D != 256) return SPEC_ERR_UNSUPPORTED;
     int64_t all = 0;
     for (int j = 0; j < 3; ++j) all |= a->q_stride[j] | a->k_cache_stride[j] | a->v_cache_stride[j] | a->out_stride[j];
@@ -217,6 +217,13 @@ int32_t spec_tree_attention(const SpecAttention *a, void *ws, int64_t ws_bytes, 
     p.tree = tree_args(a->N, a->lengths, a->n_nodes, a->parent, a->topo_seq_stride);
     p.B = a->B; p.Hq = a->Hq; p.Hkv = a->Hkv; p.G = a->Hq / a->Hkv;
     p.num_blocks = a->num_blocks; p.block = a->block_size; p.width = a->table_width;
+    // floor(n / d) for n < 2^31 and 2^(s-1) < d <= 2^s: (n + umulhi(m, n)) >> s with m = floor(2^32 (2^s - d) / d) + 1
+    const auto divisor = [](uint64_t d, unsigned *mul, int *shift) {
+        while ((1ull << *shift) < d) ++*shift;
+        *mul = (unsigned)((((uint64_t)1 << 32) * ((1ull << *shift) - d)) / d + 1);
+    };
+    divisor(a->block_size, &p.block_mul, &p.block_shift);
+    divisor(p.G, &p.group_mul, &p.group_shift);
     p.window = a->window; p.sinks = a->sinks; p.scale = a->scale;
     p.q = a->q; p.k = a->k_cache; p.v = a->v_cache; p.table = a->block_table; p.table_stride = a->table_stride;
     p.out = a->out; p.lse = a->lse; p.status = a->status;
@@ -233,10 +240,11 @@ int32_t spec_tree_attention(const SpecAttention *a, void *ws, int64_t ws_bytes, 
     const auto go = [&](auto shape, auto attend_kernel, auto join_kernel) -> int {
         using S = decltype(shape);
         const int smem = S::total + 1024;
+        p.groups = ((int)std::min<int64_t>(S::ROWS, (int64_t)p.tree.N * p.G) + 31) / 32;
         int e = prepare(attend_kernel, smem, false);
         if (e) return e;
         e = launch(attend_kernel, dim3(ctas), S::NT, smem, 0, st, p);
-        return e ? e : launch(join_kernel, dim3((unsigned)(ctas * (S::ROWS / 32) + a->B)), attend::JOIN_NT, 0, 0, st, p);
+        return e ? e : launch(join_kernel, dim3((unsigned)(ctas * p.groups + a->B)), attend::JOIN_NT, 0, 0, st, p);
     };
 #define GO(D, MT)                                                                                                                          \
     (half ? go(attend::Shape<D, MT>(), attend::spec_attend_kernel<__half, D, MT>, attend::spec_join_kernel<__half, D, MT>)                \

@@ -50,6 +50,13 @@ __device__ __forceinline__ void tmem_store(uint32_t at, const uint32_t *r)      
                  "r"(r[31])
                  : "memory");
 }
+__device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&r)[16]) // 16 columns
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(at),
+                 "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+                 "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+                 : "memory");
+}
 __device__ __forceinline__ void wait_stores() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // ---- products -----------------------------------------------------------------------------------------------------------------
@@ -86,10 +93,16 @@ __device__ __forceinline__ void commit(uint64_t *bar)
 }
 
 // ---- copies to shared memory ---------------------------------------------------------------------------------------------------
-// 16 bytes, zeros where `from` is null (`any`: an address that may be named instead; nothing is read)
-__device__ __forceinline__ void copy16(uint32_t to, const void *from, const void *any)
+// 16 bytes, of which the first `bytes` are read and the others zeros.  (No order with other memory accesses is asked of the compiler:
+// the wait or arrival behind the copies has it.)
+__device__ __forceinline__ void copy16(uint32_t to, unsigned long long from, int bytes)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from ? from : any), "r"(from ? 16 : 0) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes));
+}
+// one arrival of this thread on the barrier when its copies so far are done
+__device__ __forceinline__ void arrive_with_copies(uint64_t *bar)
+{
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 __device__ __forceinline__ void close_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }

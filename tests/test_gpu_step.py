@@ -310,9 +310,9 @@ def test_attention_whose_scores_rise_along_the_context():
         check_attention(c)
 
 
-def test_attention_scale_zero_and_negative():
-    check_attention(attention_case([200], tree(4, 2, 4), 4, 1, 64, torch.bfloat16, 16, scale=0.0))
-    check_attention(attention_case([200], tree(4, 2, 4), 4, 1, 64, torch.bfloat16, 16, scale=-0.2))
+@pytest.mark.parametrize("scale", [0.0, 0.01, 1.0])
+def test_attention_scale(scale):
+    check_attention(attention_case([200], tree(4, 2, 4), 4, 1, 64, torch.bfloat16, 16, scale=scale))
 
 
 def test_attention_keeps_what_a_row_does_not_see_out_of_it():
@@ -448,11 +448,14 @@ def test_attention_in_a_graph_and_on_another_stream():
 
 
 def test_attention_is_the_same_every_time():
-    d = cuda(attention_case([3000, 129, 700], tree(8, 2, 6), 8, 2, 128, torch.bfloat16, 16, seed=18))
-    first = binding.tree_attention(**d, want_lse=True)
-    for _ in range(20):
-        again = binding.tree_attention(**d, want_lse=True)
-        assert torch.equal(first.out, again.out) and torch.equal(first.lse, again.lse)
+    for parent in (chain(1), tree(4, 2, 4), tree(8, 2, 6)):
+        c = attention_case([3000, 129, 700, 1500, 2200], parent, 32, 8, 128, torch.bfloat16, 16, seed=18)
+        d, want = cuda(c), ref.attention(**c)
+        check_attention(c, want)
+        first = binding.tree_attention(**d, want_lse=True)
+        for _ in range(20):
+            again = binding.tree_attention(**d, want_lse=True)
+            assert torch.equal(first.out, again.out) and torch.equal(first.lse, again.lse)
 
 
 # ---------------------------------------------------------------------------------------------

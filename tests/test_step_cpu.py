@@ -67,7 +67,7 @@ def test_attention_refusals(lib):
         assert size(**kw) == -2, kw
     for dtype in (-1, 0, 3):
         assert size(dtype=dtype) == -3
-    for kw in (dict(scale=float("nan")), dict(scale=float("inf")), dict(window=-1), dict(sinks=-1)):
+    for kw in (dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=-0.5), dict(window=-1), dict(sinks=-1)):
         assert size(**kw) == -4, kw
     for kw in (dict(D=96), dict(D=512), dict(q=0x10008), dict(k_cache=0x10002), dict(out=0x10004), dict(q_stride=(1, 8, 8)),
                dict(k_cache_stride=(8, 8, 12)), dict(out_stride=(8, 4, 8))):
