@@ -153,28 +153,46 @@ struct Run {
     Place at;
     long long left;
     bool first;
-    // the next segment of the run; false at its end
-    __device__ __forceinline__ bool next(const Params &P, int block_rows, Segment &s)
+};
+// The next segment of a run; false at its end.  (Once in the code: every role of the kernel takes its segments here, and what runs once
+// per segment costs its instructions' fetching.)
+__device__ __noinline__ bool next_segment(const Params &P, int block_rows, Run *run, Segment *s)
+{
+    if (run->left <= 0) return false;
+    Place at = run->at;
+    Request r;
+    for (;;) {
+        r = request_of(P, at.b);
+        if (at.m * block_rows < r.rows) break;
+        ++at.b; at.m = 0;
+    }
+    const Tiles t = tiles_of(P, r, at.m, block_rows);
+    const int count = t.count(), end = (int)min((long long)count, at.i + run->left);
+    s->b = at.b; s->m = at.m; s->h = at.h; s->begin = at.i; s->end = end;
+    s->whole = at.i == 0 && end == count;
+    s->head = run->first;
+    s->r = r;
+    s->t = t;
+    s->rows = min(r.rows - at.m * block_rows, block_rows);
+    run->left -= end - at.i;
+    run->first = false;
+    at.i = 0;
+    if (++at.h == P.Hkv) { at.h = 0; ++at.m; }
+    run->at = at;
+    return true;
+}
+// a warp's run and the segments it has in hand
+struct __align__(16) Hand {
+    Run run;
+    Segment seg[2];
+    int more;
+    // all lanes of the warp; seg[i] is the next segment
+    __device__ __forceinline__ bool next(const Params &P, int block_rows, int i)
     {
-        if (left <= 0) return false;
-        for (;;) {
-            s.r = request_of(P, at.b);
-            if (at.m * block_rows < s.r.rows) break;
-            ++at.b; at.m = 0;
-        }
-        s.b = at.b; s.m = at.m; s.h = at.h;
-        s.t = tiles_of(P, s.r, at.m, block_rows);
-        const int count = s.t.count();
-        s.begin = at.i;
-        s.end = (int)min((long long)count, at.i + left);
-        s.whole = s.begin == 0 && s.end == count;
-        s.head = first;
-        s.rows = min(s.r.rows - at.m * block_rows, block_rows);
-        left -= s.end - s.begin;
-        first = false;
-        at.i = 0;
-        if (++at.h == P.Hkv) { at.h = 0; ++at.m; }
-        return true;
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) more = next_segment(P, block_rows, &run, &seg[i]);
+        __syncwarp();
+        return more != 0;
     }
 };
 // the place `skip` tiles into request b
@@ -248,19 +266,26 @@ __device__ __forceinline__ int block_in(const Params &P, int b, int col)
 }
 
 // ---- the kernel ---------------------------------------------------------------------------------------------------------------
-template <int D, int MT> struct Shape {
+// MT = 2: 256 rows, a warpgroup per 128.  MT = 1, WG = 2: 128 rows, the warpgroups take tiles in turn, each with its own O, reference and l,
+// put together at the segment's end: one warpgroup's tile takes 1400 cycles of arithmetic and 1040 of products one after the other,
+// and the cache delivers one every 2740.  WG = 1: one warpgroup (D = 256: tensor memory has room for one O).
+template <int D_, int MT_, int WG_> struct Shape {
+    static constexpr int D = D_, MT = MT_, WG = WG_;
+    static constexpr bool TURNS = MT == 1 && WG == 2;
     static constexpr int PANELS = D / 64;
     static constexpr int ROWS = 128 * MT;
-    static constexpr int SLOTS = D == 64 ? 10 : MT == 2 || D == 256 ? 9 : 11;     // panels of keys and values in flight
-    static constexpr int SOFT = 4 * MT, WARPS = SOFT + 1 + 4, NT = WARPS * 32;    // warps: rows, products, copies
+    static constexpr int SLOTS = D == 64 ? 10 : MT == 2 || D == 256 ? 9 : 10;     // panels of keys and values in flight
+    static constexpr int SOFT = 4 * WG, WARPS = SOFT + 1 + 4, NT = WARPS * 32;    // warps: rows, products, copies
     static constexpr int NP = 128;                                                // threads that copy
     static constexpr int O = 256;                                                 // column of the first O; S buffers at 0 and 128
     static constexpr int off_slots = ROWS * D * 2;
     static constexpr int off_parent = off_slots + SLOTS * PANEL;                  // one array of parents per row warpgroup
-    static constexpr int off_rows = off_parent + MT * SPEC_MAX_NODES * 2;         // [2][128] sources of a tile's rows: keys, values
-    static constexpr int off_bar = off_rows + 2 * KT * 16;
+    static constexpr int off_rows = off_parent + WG * SPEC_MAX_NODES * 2;         // [2][128] addresses of a tile's rows: keys, values
+    static constexpr int off_halves = off_rows + 2 * KT * 16;                     // [2][2][128] references and sums of the two turns
+    static constexpr int off_hand = off_halves + (TURNS ? 4096 : 0);
+    static constexpr int off_bar = off_hand + WARPS * (int)sizeof(Hand);
     static constexpr int total = off_bar + 1024;
-    static_assert(total + 1024 <= 227 * 1024, "shared memory");
+    static_assert(off_bar % 16 == 0 && total + 1024 <= 227 * 1024, "shared memory");
 };
 struct Bars {
     uint64_t full[16], empty[16];
@@ -320,56 +345,100 @@ template <> struct Pair<__half> {
     static __device__ __forceinline__ float value(unsigned short x) { return __half2float(__ushort_as_half(x)); }
 };
 
-// The largest of 32 columns of scores that the row sees.
-template <bool MASK> __device__ __forceinline__ float top_of(const uint32_t (&s)[32], uint32_t word, float top)
+// the largest of three, NaN where one of them is
+__device__ __forceinline__ float max3(float a, float b, float c)
 {
-#pragma unroll
-    for (int k = 0; k < 32; k += 2) {
-        const float x = !MASK || (word >> k) & 1u ? __uint_as_float(s[k]) : -CUDART_INF_F;
-        const float y = !MASK || (word >> (k + 1)) & 1u ? __uint_as_float(s[k + 1]) : -CUDART_INF_F;
-        top = fmaxf(top, fmaxf(x, y));
-    }
-    return top;
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
 }
-// 32 columns of scores: weights, their sum, and the weights rounded to the values' type, two to a register.
-template <typename T, bool MASK>
-__device__ __forceinline__ void weigh(const uint32_t (&s)[32], uint32_t word, unsigned long long c2, unsigned long long r2,
-                                      unsigned long long &sum, uint32_t (&pk)[16])
+__device__ __forceinline__ float top_of(const uint32_t (&s)[32], float top)
+{
+    float other = top;                                              // (two chains)
+#pragma unroll
+    for (int k = 0; k < 32; k += 4) {
+        top = max3(top, __uint_as_float(s[k]), __uint_as_float(s[k + 1]));
+        other = max3(other, __uint_as_float(s[k + 2]), __uint_as_float(s[k + 3]));
+    }
+    return max3(top, other, other);
+}
+// 2^y of a pair without the special function unit, which does 16 a cycle on an SM and is what the arithmetic of a tile waits for: y = n + f,
+// n the nearest integer (adding 1.5 2^23 leaves it in the low bits), 2^f by the polynomial of degree 5 that fits it to 2e-7 on
+// [-1/2, 1/2], n added to the exponent.  Exactly 0 for y <= -127.
+__device__ __forceinline__ unsigned long long exp2_pair(unsigned long long y2)
+{
+    const auto both = [](float v) { return pack_f32x2(v, v); };
+    float y0, y1;
+    unpack_f32x2(y2, y0, y1);
+    y2 = pack_f32x2(fmaxf(y0, -127.f), fmaxf(y1, -127.f));
+    const unsigned long long t = add_f32x2(y2, both(12582912.f)), n = add_f32x2(t, both(-12582912.f)), f = fma_f32x2(n, both(-1.f), y2);
+    unsigned long long p = fma_f32x2(f, both(1.33389e-3f), both(9.61852e-3f));
+    p = fma_f32x2(p, f, both(5.550341e-2f));
+    p = fma_f32x2(p, f, both(2.4022651e-1f));
+    p = fma_f32x2(p, f, both(6.9314718e-1f));
+    p = fma_f32x2(p, f, both(1.f));
+    float t0, t1, p0, p1;
+    unpack_f32x2(t, t0, t1);
+    unpack_f32x2(p, p0, p1);
+    return pack_f32x2(__int_as_float(__float_as_int(p0) + (__float_as_int(t0) << 23)), __int_as_float(__float_as_int(p1) + (__float_as_int(t1) << 23)));
+}
+// 32 columns of scores: weights, their sum, and the weights rounded to the values' type, two to a register.  Three pairs of eight go without
+// the special function unit: 128 columns take a warp 1021 cycles, two warps of a scheduler 1826 (none: 1551 and 2381, every second: 1158
+// and 2023).
+template <typename T>
+__device__ __forceinline__ void weigh(const uint32_t (&s)[32], unsigned long long c2, unsigned long long r2, unsigned long long &sum, uint32_t (&pk)[16])
 {
 #pragma unroll
     for (int k = 0; k < 32; k += 2) {
         const unsigned long long y2 = fma_f32x2(pack_f32x2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, r2);
-        float y0, y1;
-        unpack_f32x2(y2, y0, y1);
-        float p0 = ex2_approx(y0), p1 = ex2_approx(y1);
-        if (MASK) {
-            p0 = (word >> k) & 1u ? p0 : 0.f;
-            p1 = (word >> (k + 1)) & 1u ? p1 : 0.f;
+        unsigned long long p2;
+        float x, y;
+        if (k % 16 == 6 || k % 16 == 10 || k % 16 == 14) {
+            p2 = exp2_pair(y2);
+        } else {
+            unpack_f32x2(y2, x, y);
+            p2 = pack_f32x2(ex2_approx(x), ex2_approx(y));
         }
-        sum = add_f32x2(sum, pack_f32x2(p0, p1));
-        pk[k / 2] = Pair<T>::pack(p0, p1);
+        sum = add_f32x2(sum, p2);
+        unpack_f32x2(p2, x, y);
+        pk[k / 2] = Pair<T>::pack(x, y);
     }
 }
+// Scores that the row does not see become -inf.
+__device__ __forceinline__ void hide(uint32_t at, const uint32_t (&words)[4])
+{
+#pragma unroll 1
+    for (int w = 0; w < 4; ++w) {
+        uint32_t a[32];
+        tc::tmem_load(at + 32 * w, a);
+        tc::wait_loads(a);
+        const uint32_t word = w == 0 ? words[0] : w == 1 ? words[1] : w == 2 ? words[2] : words[3];
+#pragma unroll
+        for (int k = 0; k < 32; ++k) a[k] = (word >> k) & 1u ? a[k] : 0xFF800000u;
+        tc::tmem_store(at + 32 * w, a);
+    }
+    tc::wait_stores();
+}
 // The largest score of a tile; a load under way while the columns before are worked on.
-template <bool MASK> __device__ __forceinline__ float tile_top(uint32_t at, const uint32_t (&words)[4])
+__device__ __forceinline__ float tile_top(uint32_t at)
 {
     uint32_t a[32], b[32];
     float top = -CUDART_INF_F;
     tc::tmem_load(at, a);
     tc::wait_loads(a);
     tc::tmem_load(at + 32, b);
-    top = top_of<MASK>(a, words[0], top);
+    top = top_of(a, top);
     tc::wait_loads(b);
     tc::tmem_load(at + 64, a);
-    top = top_of<MASK>(b, words[1], top);
+    top = top_of(b, top);
     tc::wait_loads(a);
     tc::tmem_load(at + 96, b);
-    top = top_of<MASK>(a, words[2], top);
+    top = top_of(a, top);
     tc::wait_loads(b);
-    return top_of<MASK>(b, words[3], top);
+    return top_of(b, top);
 }
 // A tile's weights, put in the place of its scores (16 columns for 32: never beyond the scores that are loaded); returns their sum.
-template <typename T, bool MASK> __device__ __forceinline__ float tile_weights(uint32_t at, const uint32_t (&words)[4], float c, float ref)
+template <typename T> __device__ __forceinline__ float tile_weights(uint32_t at, float c, float ref)
 {
     uint32_t a[32], b[32], pk[16];
     unsigned long long s2 = 0ull;
@@ -377,31 +446,54 @@ template <typename T, bool MASK> __device__ __forceinline__ float tile_weights(u
     tc::tmem_load(at, a);
     tc::wait_loads(a);
     tc::tmem_load(at + 32, b);
-    weigh<T, MASK>(a, words[0], c2, r2, s2, pk);
+    weigh<T>(a, c2, r2, s2, pk);
     tc::wait_loads(b);
     tc::tmem_store16(at, pk);
     tc::tmem_load(at + 64, a);
-    weigh<T, MASK>(b, words[1], c2, r2, s2, pk);
+    weigh<T>(b, c2, r2, s2, pk);
     tc::wait_loads(a);
     tc::tmem_store16(at + 16, pk);
     tc::tmem_load(at + 96, b);
-    weigh<T, MASK>(a, words[2], c2, r2, s2, pk);
+    weigh<T>(a, c2, r2, s2, pk);
     tc::wait_loads(b);
     tc::tmem_store16(at + 32, pk);
-    weigh<T, MASK>(b, words[3], c2, r2, s2, pk);
+    weigh<T>(b, c2, r2, s2, pk);
     tc::tmem_store16(at + 48, pk);
     float x, y;
     unpack_f32x2(s2, x, y);
     return x + y;
 }
-
-template <typename T, int D, int MT>
-__global__ void __launch_bounds__(Shape<D, MT>::NT, 1) spec_attend_kernel(const __grid_constant__ Params P)
+// Values that are not finite were taken out of tiles that not all rows see; those that this row sees come back, into columns d .. d + 31.
+template <typename T>
+__device__ __noinline__ void put_back(const Params &P, const Segment &seg, int node, int depth, const unsigned short *parent, int d, float *o)
 {
-    using S = Shape<D, MT>;
+    Walk walk = {node, 0};
+    for (int step = 0; step < seg.steps(); ++step) {
+        const int tile = seg.tile(step);
+        if (seen_by_all(P, seg.r, tile)) continue;
+        uint32_t words[4];
+        seen_words(P, seg.r, tile, depth, parent, walk, words);
+        for (int j = 0; j < KT; ++j) {
+            const uint32_t word = j < 32 ? words[0] : j < 64 ? words[1] : j < 96 ? words[2] : words[3];
+            if (!((word >> (j & 31)) & 1u)) continue;
+            const int key = tile * KT + j, col = column_of(P, key), id = block_in(P, seg.b, col);
+            if (id < 0) continue;
+            const unsigned short *v = (const unsigned short *)P.v + id * P.v_stride[0] + (key - col * P.block) * P.v_stride[1] + seg.h * P.v_stride[2] + d;
+            for (int k = 0; k < 32; ++k) {
+                const float x = Pair<T>::value(__ldg(v + k));
+                if (!(fabsf(x) < CUDART_INF_F)) o[k] += x;
+            }
+        }
+    }
+}
+
+template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) spec_attend_kernel(const __grid_constant__ Params P)
+{
+    constexpr int D = S::D, MT = S::MT;
     unsigned char *base = dyn_smem + (-smem_u32(dyn_smem) & 1023u);
     Bars *B = (Bars *)(base + S::off_bar);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c = blockIdx.x;
+    Hand *hand = (Hand *)(base + S::off_hand) + warp;
     // what needs no input comes ahead of the wait for the kernel before
     if (warp == S::SOFT) tc::tmem_alloc(&B->tmem, 512);
     if (tid == 0) {
@@ -412,7 +504,7 @@ __global__ void __launch_bounds__(Shape<D, MT>::NT, 1) spec_attend_kernel(const 
             mbar_init(&B->s_full[t], 1);
             mbar_init(&B->p_full[t], 4);
             mbar_init(&B->pv_done[t], 1);
-            mbar_init(&B->o_empty[t], 4);
+            mbar_init(&B->o_empty[t], S::TURNS ? 8 : 4);
         }
         B->dead = 0;
         B->poison = 0;
@@ -421,75 +513,79 @@ __global__ void __launch_bounds__(Shape<D, MT>::NT, 1) spec_attend_kernel(const 
     grid_dependency_wait();
     grid_launch_dependents();                  // (the joining kernel's CTAs may be placed as this one's leave; it waits by itself)
     const Cuts cuts = find_request(P, S::ROWS, c, B->sums, B->found, tid, S::NT);
-    Run run;
-    run.left = cuts.start(c + 1) - cuts.start(c);
-    run.first = true;
-    if (run.left > 0) run.at = place_in(P, (int)B->found[0], cuts.start(c) - B->found[1], S::ROWS);
+    if (lane == 0) {
+        hand->run.left = cuts.start(c + 1) - cuts.start(c);
+        hand->run.first = true;
+        if (hand->run.left > 0) hand->run.at = place_in(P, (int)B->found[0], cuts.start(c) - B->found[1], S::ROWS);
+    }
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
     const uint32_t tmem = B->tmem;
-    Segment seg;
     if (warp < S::SOFT) {
         // ---------------------------------------------------------------- rows: a thread owns one
-        const int t = warp >> 2, quad = warp & 3, row = t * 128 + quad * 32 + lane, gt = tid & 127;
-        const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16), o_at = lanes + S::O + t * D;
-        unsigned short *parent = (unsigned short *)(base + S::off_parent) + t * SPEC_MAX_NODES;
+        const int w = warp >> 2, quad = warp & 3, t = MT == 2 ? w : 0, row = t * 128 + quad * 32 + lane, gt = tid & 127;
+        const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16), o_at = lanes + S::O + w * D;
+        unsigned short *parent = (unsigned short *)(base + S::off_parent) + w * SPEC_MAX_NODES;
+        float2 *halves = (float2 *)(base + S::off_halves);
         const float c = P.scale * LOG2E;
-        uint32_t n_tile = 0, n_run = 0;        // tiles that this warpgroup has been through, tiles of the run that went by
+        uint32_t n_tile = 0, n_run = 0, n_seg = 0;     // tiles that this warpgroup has been through, tiles of the run that went by, segments
         int tree_of = -1;
-        while (run.next(P, S::ROWS, seg)) {
+        Segment &seg = hand->seg[0];
+        for (; hand->next(P, S::ROWS, 0); ++n_seg) {
+            const int steps = seg.steps();
             if (t * 128 >= seg.rows) {
-                n_run += seg.steps();
+                n_run += steps;
                 continue;
             }
             const int r = seg.m * S::ROWS + row, node = node_of(P, min(r, seg.r.rows - 1));
             const bool live = row < seg.rows, warp_live = t * 128 + quad * 32 < seg.rows;
             if (tree_of != seg.b && (tree_of < 0 || P.tree.topo_seq_stride || P.tree.n_nodes)) {
-                bar_sync(1 + t, 128);
+                bar_sync(1 + w, 128);
                 const int *from = P.tree.parent + (long long)seg.b * P.tree.topo_seq_stride;
                 for (int i = gt; i < seg.r.n; i += 128) {
                     const int p = __ldg(from + i);
                     parent[i] = p >= 0 && p < i ? (unsigned short)p : (unsigned short)0xFFFF;
                 }
                 tree_of = seg.b;
-                bar_sync(1 + t, 128);
+                bar_sync(1 + w, 128);
             }
             int depth = 0;
             if (P.window)
                 for (unsigned short x = parent[node]; x != 0xFFFF; x = parent[x]) ++depth;
             Walk walk = {node, 0};
             float ref = 0.f, l = 0.f;
-            bool any = false;                  // whether the row has a reference
-            for (int step = 0; step < seg.steps(); ++step, ++n_tile, ++n_run) {
-                const int buf = MT == 1 ? n_tile & 1 : t;
-                const uint32_t parity = MT == 1 ? (n_tile >> 1) & 1 : n_tile & 1;
+            bool any = false, begun = false;           // whether the row has a reference; whether there has been a tile
+            for (int step = 0; step < steps; ++step, ++n_run) {
+                if (S::TURNS && (int)(n_run & 1) != w) continue;
+                const int buf = MT == 2 ? t : n_run & 1;
                 const uint32_t s_at = lanes + buf * 128;
-                wait(B, &B->s_full[buf], parity);
+                wait(B, &B->s_full[buf], (MT == 2 ? n_tile : n_run >> 1) & 1);
                 tc::fence_after();
                 if (warp_live) {
                     const int tile = seg.tile(step);
                     const volatile uint32_t *hidden = B->hidden[n_run & 7];
                     const uint32_t h0 = hidden[0], h1 = hidden[1], h2 = hidden[2], h3 = hidden[3];
-                    const bool masked = !seen_by_all(P, seg.r, tile) || (h0 | h1 | h2 | h3) != 0;
-                    uint32_t words[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
-                    if (masked) {
+                    if (!seen_by_all(P, seg.r, tile) || (h0 | h1 | h2 | h3) != 0) {
+                        uint32_t words[4];
                         seen_words(P, seg.r, tile, depth, parent, walk, words);
                         words[0] &= ~h0; words[1] &= ~h1; words[2] &= ~h2; words[3] &= ~h3;
+                        hide(s_at, words);
                     }
-                    float top = (masked ? tile_top<true>(s_at, words) : tile_top<false>(s_at, words)) * c;       // (c >= 0)
-                    if (!(top > -CUDART_INF_F)) top = -CUDART_INF_F;         // (0 times infinity: a row without scores to speak of)
-                    if (step == 0) {
-                        any = top > -CUDART_INF_F;
-                        ref = any ? top : 0.f;
-                    } else if (const bool over = any ? top > ref + 8.f : top > -CUDART_INF_F; __any_sync(0xffffffffu, over)) {
+                    const float top = tile_top(s_at) * c;                      // (c > 0)
+                    // a score that is no number, or infinite, leaves the row none either
+                    const float next = top < CUDART_INF_F ? top : CUDART_NAN_F;
+                    if (!begun) {
+                        any = !(top <= -CUDART_INF_F);
+                        ref = any ? next : 0.f;
+                    } else if (const bool over = any ? !(top <= ref + 8.f) : !(top <= -CUDART_INF_F); __any_sync(0xffffffffu, over)) {
                         // a new reference: what has been summed is scaled
                         const float old = ref;
-                        if (over) ref = top;
+                        if (over) ref = next;
                         const float f = over && any ? ex2_approx(old - ref) : 1.f;
                         any |= over;
                         l *= f;
-                        wait(B, &B->pv_done[t], (n_tile - 1) & 1);
+                        wait(B, &B->pv_done[w], (n_tile - 1) & 1);
                         tc::fence_after();
 #pragma unroll 1
                         for (int d = 0; d < D; d += 32) {
@@ -501,18 +597,37 @@ __global__ void __launch_bounds__(Shape<D, MT>::NT, 1) spec_attend_kernel(const 
                             tc::tmem_store(o_at + d, o);
                         }
                     }
-                    l += masked ? tile_weights<T, true>(s_at, words, c, ref) : tile_weights<T, false>(s_at, words, c, ref);
+                    l += tile_weights<T>(s_at, c, ref);
                     tc::wait_stores();
                     tc::fence_before();
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&B->p_full[buf]);
+                begun = true;
+                ++n_tile;
             }
-            // the segment's end.  The last scores follow all products but the last two (one: MT = 2): a phase at a time, or its parity
-            // would be taken for that of the one before
-            if (MT == 1 && n_tile > 1) wait(B, &B->pv_done[t], n_tile & 1);
-            wait(B, &B->pv_done[t], (n_tile - 1) & 1);
+            // the segment's end.  One warpgroup for all tiles: the last scores follow all products but the last two, which are waited for one
+            // after the other (the parity of a phase is that of the one two before)
+            if (begun) {
+                if (S::WG == 1 && n_tile > 1) wait(B, &B->pv_done[w], n_tile & 1);
+                wait(B, &B->pv_done[w], (n_tile - 1) & 1);
+            }
             tc::fence_after();
+            float f0 = 1.f, f1 = 0.f;
+            if (S::TURNS) {
+                // both turns' references and sums, then both O: this warpgroup gives out half of the columns
+                float2 *mine = halves + (n_seg & 1) * 256;
+                mine[w * 128 + gt] = make_float2(any ? ref : -CUDART_INF_F, l);
+                tc::fence_before();
+                bar_sync(3, 256);
+                tc::fence_after();
+                const float2 x = mine[gt], y = mine[128 + gt];
+                ref = x.x >= y.x || x.x != x.x ? x.x : y.x;                  // (NaN if one is)
+                f0 = x.x == -CUDART_INF_F ? 0.f : ex2_approx(x.x - ref);
+                f1 = y.x == -CUDART_INF_F ? 0.f : ex2_approx(y.x - ref);
+                any = f0 != 0.f || f1 != 0.f;
+                l = (f0 == 0.f ? 0.f : f0 * x.y) + (f1 == 0.f ? 0.f : f1 * y.y);
+            }
             if (warp_live) {
                 const bool poison = *(volatile int *)&B->poison != 0;
                 const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -520,46 +635,38 @@ __global__ void __launch_bounds__(Shape<D, MT>::NT, 1) spec_attend_kernel(const 
                 const int head = seg.h * P.G + r - node * P.G;
                 T *to = (T *)P.out + seg.b * P.out_stride[0] + node * P.out_stride[1] + head * P.out_stride[2];
                 float *part = P.part + slot * S::ROWS * D;
+                const int d0 = S::TURNS ? w * (D / 2) : 0, d1 = S::TURNS ? d0 + D / 2 : D;
 #pragma unroll 1
-                for (int d = 0; d < D; d += 32) {
+                for (int d = d0; d < d1; d += 32) {
                     uint32_t o[32];
-                    tc::tmem_load(o_at + d, o);
+                    tc::tmem_load((S::TURNS ? lanes + S::O : o_at) + d, o);
                     tc::wait_loads(o);
-                    if (poison && live) {
-                        // values that are not finite were taken out of tiles that not all rows see; those that this row sees come back
-                        Walk w = {node, 0};
-#pragma unroll 1
-                        for (int step = 0; step < seg.steps(); ++step) {
-                            const int tile = seg.tile(step);
-                            if (seen_by_all(P, seg.r, tile)) continue;
-                            uint32_t words[4];
-                            seen_words(P, seg.r, tile, depth, parent, w, words);
-#pragma unroll 1
-                            for (int j = 0; j < KT; ++j) {
-                                const uint32_t word = j < 32 ? words[0] : j < 64 ? words[1] : j < 96 ? words[2] : words[3];
-                                if (!((word >> (j & 31)) & 1u)) continue;
-                                const int key = tile * KT + j, col = column_of(P, key), id = block_in(P, seg.b, col);
-                                if (id < 0) continue;
-                                const unsigned short *v = (const unsigned short *)P.v + id * P.v_stride[0] +
-                                                          (key - col * P.block) * P.v_stride[1] + seg.h * P.v_stride[2] + d;
+                    if (S::TURNS) {
+                        uint32_t o1[32];
+                        tc::tmem_load(lanes + S::O + D + d, o1);
+                        tc::wait_loads(o1);
 #pragma unroll
-                                for (int k = 0; k < 32; ++k) {
-                                    const float x = Pair<T>::value(__ldg(v + k));
-                                    if (!(fabsf(x) < CUDART_INF_F)) o[k] = __float_as_uint(__uint_as_float(o[k]) + x);
-                                }
-                            }
-                        }
+                        for (int k = 0; k < 32; ++k)                          // (a turn without a tile has no O)
+                            o[k] = __float_as_uint((f0 == 0.f ? 0.f : f0 * __uint_as_float(o[k])) + (f1 == 0.f ? 0.f : f1 * __uint_as_float(o1[k])));
+                    }
+                    if (poison && live) {
+                        float x[32];
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) x[k] = __uint_as_float(o[k]);
+                        put_back<T>(P, seg, node, depth, parent, d, x);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(x[k]);
                     }
                     if (!live) continue;
                     if (seg.whole) {
 #pragma unroll
                         for (int k = 0; k < 32; k += 8) {
-                            uint4 w;
-                            w.x = Pair<T>::pack(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv);
-                            w.y = Pair<T>::pack(__uint_as_float(o[k + 2]) * inv, __uint_as_float(o[k + 3]) * inv);
-                            w.z = Pair<T>::pack(__uint_as_float(o[k + 4]) * inv, __uint_as_float(o[k + 5]) * inv);
-                            w.w = Pair<T>::pack(__uint_as_float(o[k + 6]) * inv, __uint_as_float(o[k + 7]) * inv);
-                            *(uint4 *)(to + d + k) = w;
+                            uint4 x;
+                            x.x = Pair<T>::pack(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv);
+                            x.y = Pair<T>::pack(__uint_as_float(o[k + 2]) * inv, __uint_as_float(o[k + 3]) * inv);
+                            x.z = Pair<T>::pack(__uint_as_float(o[k + 4]) * inv, __uint_as_float(o[k + 5]) * inv);
+                            x.w = Pair<T>::pack(__uint_as_float(o[k + 6]) * inv, __uint_as_float(o[k + 7]) * inv);
+                            *(uint4 *)(to + d + k) = x;
                         }
                     } else {
 #pragma unroll
@@ -567,7 +674,7 @@ __global__ void __launch_bounds__(Shape<D, MT>::NT, 1) spec_attend_kernel(const 
                             *(uint4 *)(part + ((long long)((d + k) / 4) * S::ROWS + row) * 4) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
                     }
                 }
-                if (live) {
+                if (live && d0 == 0) {
                     if (seg.whole) {
                         if (P.lse)
                             P.lse[((long long)seg.b * P.tree.N + node) * P.Hq + head] = l == 0.f ? -CUDART_INF_F : (ref + log2f(l)) * LN2;
@@ -584,94 +691,97 @@ __global__ void __launch_bounds__(Shape<D, MT>::NT, 1) spec_attend_kernel(const 
         // ---------------------------------------------------------------- products: one thread issues, the warp waits
         constexpr uint32_t DS = tc::product_desc(Pair<T>::TYPE, KT, false), DO = tc::product_desc(Pair<T>::TYPE, 64, true);
         const uint32_t q_at = smem_u32(base), slots = smem_u32(base + S::off_slots);
-        uint32_t n_slot = 0, n_seg = 0, n_tile = 0, n_p[2] = {0, 0}, n_o[2] = {0, 0};
-        const auto slot_wait = [&](uint32_t n) { wait(B, &B->full[n % S::SLOTS], (n / S::SLOTS) & 1); };
-        // S of row block t into buffer buf, from the keys in slots n ..
-        const auto scores = [&](int t, int buf, uint32_t n, bool release) {
-            if (lane == 0) {
+        uint32_t n = 0, n_seg = 0, n_tile = 0, n_p[2] = {0, 0}, n_o[2] = {0, 0};         // n: the next slot to read
+        const auto copied = [&](uint32_t k) {
+            for (int p = 0; p < S::PANELS; ++p) wait(B, &B->full[(k + p) % S::SLOTS], ((k + p) / S::SLOTS) & 1);
+            tc::publish_shared();                      // (the copies' writes, seen through the barrier, for the tensor cores)
+            tc::fence_after();
+        };
+        const auto is_copied = [&](uint32_t k) {
+            bool all = true;
+            for (int p = 0; p < S::PANELS; ++p) all &= mbar_test(&B->full[(k + p) % S::SLOTS], ((k + p) / S::SLOTS) & 1);
+            if (!__all_sync(0xffffffffu, all)) return false;
+            tc::publish_shared();
+            tc::fence_after();
+            return true;
+        };
+        // S of row block t into buffer buf, from the keys in slots k ..
+        const auto scores = [&](int t, int buf, uint32_t k, bool release) {
+            if (tc::elected()) {
 #pragma unroll
                 for (int p = 0; p < S::PANELS; ++p) {
                     const uint64_t qd = tc::panel_desc(q_at + (p * MT + t) * PANEL);
-                    const uint64_t kd = tc::panel_desc(slots + (n + p) % S::SLOTS * PANEL);
+                    const uint64_t kd = tc::panel_desc(slots + (k + p) % S::SLOTS * PANEL);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) tc::mma_ss(tmem + buf * 128, qd + 2 * k, kd + 2 * k, DS, p > 0 || k > 0);
-                    if (release) tc::commit(&B->empty[(n + p) % S::SLOTS]);
+                    for (int i = 0; i < 4; ++i) tc::mma_ss(tmem + buf * 128, qd + 2 * i, kd + 2 * i, DS, p > 0 || i > 0);
+                    if (release) tc::commit(&B->empty[(k + p) % S::SLOTS]);
                 }
                 tc::commit(&B->s_full[buf]);
             }
             __syncwarp();
         };
-        const auto sums = [&](int t, int buf, uint32_t n, bool add, bool release) {
-            if (lane == 0) {
+        // O number o (+)= P (in buffer buf) V, from the values in slots k ..
+        const auto sums = [&](int o, int buf, uint32_t k, bool add, bool release) {
+            if (tc::elected()) {
 #pragma unroll
                 for (int p = 0; p < S::PANELS; ++p) {
-                    const uint64_t vd = tc::panel_desc(slots + (n + p) % S::SLOTS * PANEL);
+                    const uint64_t vd = tc::panel_desc(slots + (k + p) % S::SLOTS * PANEL);
 #pragma unroll
-                    for (int k = 0; k < KT / 16; ++k)
-                        tc::mma_ts(tmem + S::O + t * D + p * 64, tmem + buf * 128 + k * 8, vd + k * (2048 >> 4), DO, add || k > 0);
-                    if (release) tc::commit(&B->empty[(n + p) % S::SLOTS]);
+                    for (int i = 0; i < KT / 16; ++i)
+                        tc::mma_ts(tmem + S::O + o * D + p * 64, tmem + buf * 128 + i * 8, vd + i * (2048 >> 4), DO, add || i > 0);
+                    if (release) tc::commit(&B->empty[(k + p) % S::SLOTS]);
                 }
-                tc::commit(&B->pv_done[t]);
+                tc::commit(&B->pv_done[o]);
             }
             __syncwarp();
         };
-        while (run.next(P, S::ROWS, seg)) {
-            const int steps = seg.steps(), tiles = MT == 1 || seg.rows <= 128 ? 1 : 2;
-            const auto keys_in = [&](uint32_t n) {
-                for (int p = 0; p < S::PANELS; ++p) slot_wait(n + p);
-                tc::publish_shared();              // (the copies' writes, seen through the barrier, for the tensor cores)
-                tc::fence_after();
-            };
+        for (; hand->next(P, S::ROWS, 0); ++n_seg) {
+            const int steps = hand->seg[0].steps(), blocks = MT == 1 || hand->seg[0].rows <= 128 ? 1 : 2;
             wait(B, &B->q_full, n_seg & 1);
+            copied(n);
             if (MT == 1) {
                 // order of the slots: K0, K1, V0, K2, V1, ...: scores one tile ahead
-                uint32_t n = n_slot;
-                keys_in(n);
                 scores(0, n_tile & 1, n, true);
                 n += S::PANELS;
-                for (int i = 0; i < steps; ++i) {
+                for (int i = 0; i < steps; ++i, ++n_tile) {
                     if (i + 1 < steps) {
-                        keys_in(n);
-                        scores(0, (n_tile + i + 1) & 1, n, true);
+                        copied(n);
+                        scores(0, (n_tile + 1) & 1, n, true);
                         n += S::PANELS;
                     }
-                    if (i + 1 == max(1, steps - 1) && lane == 0) tc::commit(&B->q_empty);
-                    keys_in(n);
-                    const int buf = (n_tile + i) & 1;
-                    wait(B, &B->p_full[buf], ((n_tile + i) >> 1) & 1);
-                    if (i == 0) { if (n_o[0]) wait(B, &B->o_empty[0], (n_o[0] - 1) & 1); ++n_o[0]; }
+                    if (i + 1 == max(1, steps - 1) && tc::elected()) tc::commit(&B->q_empty);
+                    copied(n);
+                    const int buf = n_tile & 1;
+                    wait(B, &B->p_full[buf], (n_tile >> 1) & 1);
+                    if (i == 0 && n_seg) wait(B, &B->o_empty[0], (n_seg - 1) & 1);
                     tc::fence_after();
-                    sums(0, buf, n, i > 0, true);
+                    sums(S::TURNS ? buf : 0, buf, n, i >= S::WG, true);
                     n += S::PANELS;
                 }
-                n_slot = n;
-                n_tile += steps;
             } else {
                 // order of the slots: K0, V0, K1, V1, ...: a row block's next scores right behind its sums
-                uint32_t n = n_slot;
-                keys_in(n);
-                for (int t = 0; t < tiles; ++t) scores(t, t, n, t == tiles - 1);
+                for (int t = 0; t < blocks; ++t) scores(t, t, n, t == blocks - 1);
                 n += S::PANELS;
-                if (steps == 1 && lane == 0) tc::commit(&B->q_empty);
+                if (steps == 1 && tc::elected()) tc::commit(&B->q_empty);
                 for (int i = 0; i < steps; ++i) {
-                    keys_in(n);
-                    for (int t = 0; t < tiles; ++t) {
+                    copied(n);
+                    // the next keys' arrival is seen to before the weights are waited for, if it has come
+                    const bool more = i + 1 < steps;
+                    bool keys = more && is_copied(n + S::PANELS);
+                    for (int t = 0; t < blocks; ++t) {
                         wait(B, &B->p_full[t], n_p[t] & 1);
                         ++n_p[t];
                         if (i == 0) { if (n_o[t]) wait(B, &B->o_empty[t], (n_o[t] - 1) & 1); ++n_o[t]; }
                         tc::fence_after();
-                        sums(t, t, n, i > 0, t == tiles - 1);
-                        if (i + 1 < steps) {
-                            if (t == 0) keys_in(n + S::PANELS);
-                            scores(t, t, n + S::PANELS, t == tiles - 1);
-                        }
+                        sums(t, t, n, i > 0, t == blocks - 1);
+                        if (!more) continue;
+                        if (!keys) { copied(n + S::PANELS); keys = true; }
+                        scores(t, t, n + S::PANELS, t == blocks - 1);
                     }
-                    if (i + 2 == steps && lane == 0) tc::commit(&B->q_empty);
-                    n += 2 * S::PANELS;
+                    if (i + 2 == steps && tc::elected()) tc::commit(&B->q_empty);
+                    n += more ? 2 * S::PANELS : S::PANELS;
                 }
-                n_slot = n - S::PANELS;
             }
-            ++n_seg;
         }
     } else {
         // ---------------------------------------------------------------- copies: 128 threads, a row's 16-byte chunks over its lanes
@@ -778,17 +888,17 @@ __global__ void __launch_bounds__(Shape<D, MT>::NT, 1) spec_attend_kernel(const 
             tc::close_copies();
             ++n_seg;
         };
-        if (run.next(P, S::ROWS, seg)) {
+        if (hand->next(P, S::ROWS, 0)) {
             bool more = true;
-            int step = 0;
-            Source src = source(seg, seg.tile(0));
+            int step = 0, in = 0;                                     // in: which of the segments in hand is gone through
+            Source src = source(hand->seg[0], hand->seg[0].tile(0));
             while (more) {
-                const Segment now = seg;
+                const Segment &now = hand->seg[in];
                 const int at = step;
                 const Source here = src;
                 const bool last = ++step == now.steps();
-                if (last) { more = run.next(P, S::ROWS, seg); step = 0; }
-                if (more) src = source(seg, seg.tile(step));
+                if (last) { more = hand->next(P, S::ROWS, in ^= 1); step = 0; }
+                if (more) src = source(hand->seg[in], hand->seg[in].tile(step));
                 const bool part = !seen_by_all(P, now.r, now.tile(at));
                 put_sources(now, here);
                 copy_tile(n_slot, n_row - 1, false, part);
@@ -823,9 +933,9 @@ __global__ void __launch_bounds__(Shape<D, MT>::NT, 1) spec_attend_kernel(const 
 // attention still runs: that reads inputs alone) and zeros for a bad tree.
 constexpr int JOIN_NT = 256, CTAS_MAX = 160;
 
-template <typename T, int D, int MT> __global__ void __launch_bounds__(JOIN_NT) spec_join_kernel(const __grid_constant__ Params P)
+template <typename T, typename S> __global__ void __launch_bounds__(JOIN_NT) spec_join_kernel(const __grid_constant__ Params P)
 {
-    using S = Shape<D, MT>;
+    constexpr int D = S::D;
     constexpr int WARPS = JOIN_NT / 32;
     __shared__ float share[CTAS_MAX][32], sum_of[CTAS_MAX][32], inverse[32];
     __shared__ long long sums[WARPS], found[2];

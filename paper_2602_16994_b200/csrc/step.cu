@@ -224,7 +224,8 @@ int32_t spec_tree_attention(const SpecAttention *a, void *ws, int64_t ws_bytes, 
     };
     divisor(a->block_size, &p.block_mul, &p.block_shift);
     divisor(p.G, &p.group_mul, &p.group_shift);
-    p.window = a->window; p.sinks = a->sinks; p.scale = a->scale;
+    p.window = a->window; p.sinks = a->sinks;
+    p.scale = std::max(a->scale, 1.17549435e-38f);      // (so that what is not seen, -inf, stays that under a scale of 0)
     p.q = a->q; p.k = a->k_cache; p.v = a->v_cache; p.table = a->block_table; p.table_stride = a->table_stride;
     p.out = a->out; p.lse = a->lse; p.status = a->status;
     for (int j = 0; j < 3; ++j) {
@@ -246,12 +247,14 @@ int32_t spec_tree_attention(const SpecAttention *a, void *ws, int64_t ws_bytes, 
         e = launch(attend_kernel, dim3(ctas), S::NT, smem, 0, st, p);
         return e ? e : launch(join_kernel, dim3((unsigned)(ctas * p.groups + a->B)), attend::JOIN_NT, 0, 0, st, p);
     };
-#define GO(D, MT)                                                                                                                          \
-    (half ? go(attend::Shape<D, MT>(), attend::spec_attend_kernel<__half, D, MT>, attend::spec_join_kernel<__half, D, MT>)                \
-          : go(attend::Shape<D, MT>(), attend::spec_attend_kernel<__nv_bfloat16, D, MT>, attend::spec_join_kernel<__nv_bfloat16, D, MT>))
-    if (a->D == 256) return GO(256, 1);
-    if (a->D == 128) return two_blocks(a) ? GO(128, 2) : GO(128, 1);
-    return two_blocks(a) ? GO(64, 2) : GO(64, 1);
+#define GO(D, MT, WG)                                                                                                                      \
+    (half ? go(attend::Shape<D, MT, WG>(), attend::spec_attend_kernel<__half, attend::Shape<D, MT, WG>>,                                  \
+               attend::spec_join_kernel<__half, attend::Shape<D, MT, WG>>)                                                                \
+          : go(attend::Shape<D, MT, WG>(), attend::spec_attend_kernel<__nv_bfloat16, attend::Shape<D, MT, WG>>,                           \
+               attend::spec_join_kernel<__nv_bfloat16, attend::Shape<D, MT, WG>>))
+    if (a->D == 256) return GO(256, 1, 1);
+    if (a->D == 128) return two_blocks(a) ? GO(128, 2, 2) : GO(128, 1, 2);
+    return two_blocks(a) ? GO(64, 2, 2) : GO(64, 1, 2);
 #undef GO
 }
 
