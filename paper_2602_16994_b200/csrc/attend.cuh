@@ -15,6 +15,7 @@
 // run ends in leaves its O, l and reference in the workspace, and spec_join_kernel puts such parts together.  Every CTA finds its run from
 // the lengths by itself; the host never sees them.
 #pragma once
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -29,6 +30,8 @@ constexpr int PANEL = KT * 128;                // bytes of a panel: 128 rows of 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.69314718055994531f;
 
 struct Params {
+    CUtensorMap k_map, v_map;                  // the caches as [block][slot][head][entry], boxes of `box` slots by 64 entries
+    int box;                                   // a power of two up to 32 that divides the block; 0: blocks of no multiple of 8 slots
     TreeArgs tree;
     int B, Hq, Hkv, G, num_blocks, block, width, window, sinks;
     unsigned block_mul;                        // key / block = (umulhi(block_mul, key) + key) >> block_shift for keys below 2^31
@@ -219,12 +222,13 @@ __device__ __forceinline__ uint32_t bits_of(long long a, long long lo, long long
     if (x >= y) return 0;
     return (y == 32 ? 0xffffffffu : (1u << y) - 1u) & ~((1u << x) - 1u);
 }
-// Whether every row of any block sees all keys of a tile (a node's depth is at most its index).
-__device__ __forceinline__ bool seen_by_all(const Params &P, const Request &r, int tile)
+// Whether every row of any block sees keys a .. a + count - 1 (a node's depth is at most its index).
+__device__ __forceinline__ bool seen_by_all(const Params &P, const Request &r, long long a, int count)
 {
-    const long long a = (long long)tile * KT, e = a + KT;
+    const long long e = a + count;
     return e <= r.len && (P.window == 0 || e <= P.sinks || a > (long long)r.len + r.n - 1 - P.window);
 }
+__device__ __forceinline__ bool seen_by_all(const Params &P, const Request &r, int tile) { return seen_by_all(P, r, (long long)tile * KT, KT); }
 // A row's walk up the tree, as tiles are taken from the last to the first.
 struct Walk {
     int node, depth;                           // next node to take, its depth less the row's (0, -1, ...)
@@ -274,14 +278,15 @@ template <int D_, int MT_, int WG_> struct Shape {
     static constexpr bool TURNS = MT == 1 && WG == 2;
     static constexpr int PANELS = D / 64;
     static constexpr int ROWS = 128 * MT;
-    static constexpr int SLOTS = D == 64 ? 10 : MT == 2 || D == 256 ? 9 : 10;     // panels of keys and values in flight
+    static constexpr int WIDE = PANELS < 2 ? 1 : 2;                               // panels of a slot: up to 128 entries of a tile's rows
+    static constexpr int SLOT = WIDE * PANEL, STEP = PANELS / WIDE;               // bytes of a slot; slots of a tile's keys or values
+    static constexpr int SLOTS = D == 64 ? 10 : MT == 2 || D == 256 ? 4 : 5;      // slots in flight
     static constexpr int SOFT = 4 * WG, WARPS = SOFT + 1 + 4, NT = WARPS * 32;    // warps: rows, products, copies
     static constexpr int NP = 128;                                                // threads that copy
     static constexpr int O = 256;                                                 // column of the first O; S buffers at 0 and 128
     static constexpr int off_slots = ROWS * D * 2;
-    static constexpr int off_parent = off_slots + SLOTS * PANEL;                  // one array of parents per row warpgroup
-    static constexpr int off_rows = off_parent + WG * SPEC_MAX_NODES * 2;         // [2][128] addresses of a tile's rows: keys, values
-    static constexpr int off_halves = off_rows + 2 * KT * 16;                     // [2][2][128] references and sums of the two turns
+    static constexpr int off_parent = off_slots + SLOTS * SLOT;                  // one array of parents per row warpgroup
+    static constexpr int off_halves = off_parent + WG * SPEC_MAX_NODES * 2;       // [2][2][128] references and sums of the two turns
     static constexpr int off_hand = off_halves + (TURNS ? 4096 : 0);
     static constexpr int off_bar = off_hand + WARPS * (int)sizeof(Hand);
     static constexpr int total = off_bar + 1024;
@@ -293,6 +298,7 @@ struct Bars {
     uint32_t tmem;
     int dead, poison;
     uint32_t hidden[8][4];                     // keys of a tile on bad blocks, by the tile's number in the CTA's run % 8
+    uint32_t plain[8];                         // a byte per warp that copies: whether it stored (part of) the tile by itself
     long long found[2], sums[16];
 };
 static_assert(sizeof(Bars) <= 1024, "the area behind the buffers");
@@ -419,46 +425,36 @@ __device__ __forceinline__ void hide(uint32_t at, const uint32_t (&words)[4])
     }
     tc::wait_stores();
 }
-// The largest score of a tile; a load under way while the columns before are worked on.
+// The largest score of a tile.
 __device__ __forceinline__ float tile_top(uint32_t at)
 {
-    uint32_t a[32], b[32];
     float top = -CUDART_INF_F;
-    tc::tmem_load(at, a);
-    tc::wait_loads(a);
-    tc::tmem_load(at + 32, b);
-    top = top_of(a, top);
-    tc::wait_loads(b);
-    tc::tmem_load(at + 64, a);
-    top = top_of(b, top);
-    tc::wait_loads(a);
-    tc::tmem_load(at + 96, b);
-    top = top_of(a, top);
-    tc::wait_loads(b);
-    return top_of(b, top);
+#pragma unroll 1
+    for (int w = 0; w < KT; w += 64) {
+        uint32_t a[32], b[32];
+        tc::tmem_load(at + w, a);
+        tc::tmem_load(at + w + 32, b);
+        tc::wait_loads(a);
+        tc::wait_loads(b);
+        top = top_of(a, top);
+        top = top_of(b, top);
+    }
+    return top;
 }
-// A tile's weights, put in the place of its scores (16 columns for 32: never beyond the scores that are loaded); returns their sum.
+// A tile's weights, put in the place of its scores (16 columns for 32: never beyond the scores that are loaded); returns their sum.  A loop, not
+// four copies: the schedulers' instruction caches hold the loops of all roles, and fetching what does not fit took longer than the arithmetic.
 template <typename T> __device__ __forceinline__ float tile_weights(uint32_t at, float c, float ref)
 {
-    uint32_t a[32], b[32], pk[16];
     unsigned long long s2 = 0ull;
     const unsigned long long c2 = pack_f32x2(c, c), r2 = pack_f32x2(-ref, -ref);
-    tc::tmem_load(at, a);
-    tc::wait_loads(a);
-    tc::tmem_load(at + 32, b);
-    weigh<T>(a, c2, r2, s2, pk);
-    tc::wait_loads(b);
-    tc::tmem_store16(at, pk);
-    tc::tmem_load(at + 64, a);
-    weigh<T>(b, c2, r2, s2, pk);
-    tc::wait_loads(a);
-    tc::tmem_store16(at + 16, pk);
-    tc::tmem_load(at + 96, b);
-    weigh<T>(a, c2, r2, s2, pk);
-    tc::wait_loads(b);
-    tc::tmem_store16(at + 32, pk);
-    weigh<T>(b, c2, r2, s2, pk);
-    tc::tmem_store16(at + 48, pk);
+#pragma unroll 1
+    for (int w = 0; w < 4; ++w) {
+        uint32_t a[32], pk[16];
+        tc::tmem_load(at + 32 * w, a);
+        tc::wait_loads(a);
+        weigh<T>(a, c2, r2, s2, pk);
+        tc::tmem_store16(at + 16 * w, pk);
+    }
     float x, y;
     unpack_f32x2(s2, x, y);
     return x + y;
@@ -496,6 +492,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
     Hand *hand = (Hand *)(base + S::off_hand) + warp;
     // what needs no input comes ahead of the wait for the kernel before
     if (warp == S::SOFT) tc::tmem_alloc(&B->tmem, 512);
+    if (tid == S::NT - 1 && P.box) { tc::prefetch_map(&P.k_map); tc::prefetch_map(&P.v_map); }
     if (tid == 0) {
         for (int i = 0; i < S::SLOTS; ++i) { mbar_init(&B->full[i], S::NP); mbar_init(&B->empty[i], 1); }
         mbar_init(&B->q_full, S::NP);
@@ -689,19 +686,20 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         }
     } else if (warp == S::SOFT) {
         // ---------------------------------------------------------------- products: one thread issues, the warp waits
-        constexpr uint32_t DS = tc::product_desc(Pair<T>::TYPE, KT, false), DO = tc::product_desc(Pair<T>::TYPE, 64, true);
+        constexpr uint32_t DS = tc::product_desc(Pair<T>::TYPE, KT, false), DO = tc::product_desc(Pair<T>::TYPE, 64 * S::WIDE, true);
         const uint32_t q_at = smem_u32(base), slots = smem_u32(base + S::off_slots);
         uint32_t n = 0, n_seg = 0, n_tile = 0, n_p[2] = {0, 0}, n_o[2] = {0, 0};         // n: the next slot to read
-        const auto copied = [&](uint32_t k) {
-            for (int p = 0; p < S::PANELS; ++p) wait(B, &B->full[(k + p) % S::SLOTS], ((k + p) / S::SLOTS) & 1);
-            tc::publish_shared();                      // (the copies' writes, seen through the barrier, for the tensor cores)
+        // the copies to slots k .., of the run's tile i, are there; what threads stored, seen through the barrier, is put before the tensor cores
+        const auto copied = [&](uint32_t k, uint32_t i) {
+            for (int p = 0; p < S::STEP; ++p) wait(B, &B->full[(k + p) % S::SLOTS], ((k + p) / S::SLOTS) & 1);
+            if (*(volatile uint32_t *)&B->plain[i & 7]) tc::publish_shared();
             tc::fence_after();
         };
-        const auto is_copied = [&](uint32_t k) {
+        const auto is_copied = [&](uint32_t k, uint32_t i) {
             bool all = true;
-            for (int p = 0; p < S::PANELS; ++p) all &= mbar_test(&B->full[(k + p) % S::SLOTS], ((k + p) / S::SLOTS) & 1);
+            for (int p = 0; p < S::STEP; ++p) all &= mbar_test(&B->full[(k + p) % S::SLOTS], ((k + p) / S::SLOTS) & 1);
             if (!__all_sync(0xffffffffu, all)) return false;
-            tc::publish_shared();
+            if (*(volatile uint32_t *)&B->plain[i & 7]) tc::publish_shared();
             tc::fence_after();
             return true;
         };
@@ -709,12 +707,15 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         const auto scores = [&](int t, int buf, uint32_t k, bool release) {
             if (tc::elected()) {
 #pragma unroll
-                for (int p = 0; p < S::PANELS; ++p) {
-                    const uint64_t qd = tc::panel_desc(q_at + (p * MT + t) * PANEL);
-                    const uint64_t kd = tc::panel_desc(slots + (k + p) % S::SLOTS * PANEL);
+                for (int p = 0; p < S::STEP; ++p) {
+                    const uint32_t slot = (k + p) % S::SLOTS;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) tc::mma_ss(tmem + buf * 128, qd + 2 * i, kd + 2 * i, DS, p > 0 || i > 0);
-                    if (release) tc::commit(&B->empty[(k + p) % S::SLOTS]);
+                    for (int x = 0; x < S::WIDE; ++x) {
+                        const uint64_t qd = tc::panel_desc(q_at + ((p * S::WIDE + x) * MT + t) * PANEL), kd = tc::panel_desc(slots + slot * S::SLOT + x * PANEL);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) tc::mma_ss(tmem + buf * 128, qd + 2 * i, kd + 2 * i, DS, p > 0 || x > 0 || i > 0);
+                    }
+                    if (release) tc::commit(&B->empty[slot]);
                 }
                 tc::commit(&B->s_full[buf]);
             }
@@ -724,12 +725,13 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         const auto sums = [&](int o, int buf, uint32_t k, bool add, bool release) {
             if (tc::elected()) {
 #pragma unroll
-                for (int p = 0; p < S::PANELS; ++p) {
-                    const uint64_t vd = tc::panel_desc(slots + (k + p) % S::SLOTS * PANEL);
+                for (int p = 0; p < S::STEP; ++p) {
+                    const uint32_t slot = (k + p) % S::SLOTS;
+                    const uint64_t vd = tc::panel_desc(slots + slot * S::SLOT);
 #pragma unroll
                     for (int i = 0; i < KT / 16; ++i)
-                        tc::mma_ts(tmem + S::O + o * D + p * 64, tmem + buf * 128 + i * 8, vd + i * (2048 >> 4), DO, add || i > 0);
-                    if (release) tc::commit(&B->empty[(k + p) % S::SLOTS]);
+                        tc::mma_ts(tmem + S::O + o * D + p * 128, tmem + buf * 128 + i * 8, vd + i * (2048 >> 4), DO, add || i > 0);
+                    if (release) tc::commit(&B->empty[slot]);
                 }
                 tc::commit(&B->pv_done[o]);
             }
@@ -738,36 +740,37 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         for (; hand->next(P, S::ROWS, 0); ++n_seg) {
             const int steps = hand->seg[0].steps(), blocks = MT == 1 || hand->seg[0].rows <= 128 ? 1 : 2;
             wait(B, &B->q_full, n_seg & 1);
-            copied(n);
+            tc::publish_shared();
+            copied(n, n_tile);
             if (MT == 1) {
                 // order of the slots: K0, K1, V0, K2, V1, ...: scores one tile ahead
                 scores(0, n_tile & 1, n, true);
-                n += S::PANELS;
+                n += S::STEP;
                 for (int i = 0; i < steps; ++i, ++n_tile) {
                     if (i + 1 < steps) {
-                        copied(n);
+                        copied(n, n_tile + 1);
                         scores(0, (n_tile + 1) & 1, n, true);
-                        n += S::PANELS;
+                        n += S::STEP;
                     }
                     if (i + 1 == max(1, steps - 1) && tc::elected()) tc::commit(&B->q_empty);
-                    copied(n);
+                    copied(n, n_tile);
                     const int buf = n_tile & 1;
                     wait(B, &B->p_full[buf], (n_tile >> 1) & 1);
                     if (i == 0 && n_seg) wait(B, &B->o_empty[0], (n_seg - 1) & 1);
                     tc::fence_after();
                     sums(S::TURNS ? buf : 0, buf, n, i >= S::WG, true);
-                    n += S::PANELS;
+                    n += S::STEP;
                 }
             } else {
                 // order of the slots: K0, V0, K1, V1, ...: a row block's next scores right behind its sums
                 for (int t = 0; t < blocks; ++t) scores(t, t, n, t == blocks - 1);
-                n += S::PANELS;
+                n += S::STEP;
                 if (steps == 1 && tc::elected()) tc::commit(&B->q_empty);
-                for (int i = 0; i < steps; ++i) {
-                    copied(n);
+                for (int i = 0; i < steps; ++i, ++n_tile) {
+                    copied(n, n_tile);
                     // the next keys' arrival is seen to before the weights are waited for, if it has come
                     const bool more = i + 1 < steps;
-                    bool keys = more && is_copied(n + S::PANELS);
+                    bool keys = more && is_copied(n + S::STEP, n_tile + 1);
                     for (int t = 0; t < blocks; ++t) {
                         wait(B, &B->p_full[t], n_p[t] & 1);
                         ++n_p[t];
@@ -775,59 +778,64 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                         tc::fence_after();
                         sums(t, t, n, i > 0, t == blocks - 1);
                         if (!more) continue;
-                        if (!keys) { copied(n + S::PANELS); keys = true; }
-                        scores(t, t, n + S::PANELS, t == blocks - 1);
+                        if (!keys) { copied(n + S::STEP, n_tile + 1); keys = true; }
+                        scores(t, t, n + S::STEP, t == blocks - 1);
                     }
                     if (i + 2 == steps && tc::elected()) tc::commit(&B->q_empty);
-                    n += more ? 2 * S::PANELS : S::PANELS;
+                    n += more ? 2 * S::STEP : S::STEP;
                 }
             }
         }
     } else {
-        // ---------------------------------------------------------------- copies: 128 threads, a row's 16-byte chunks over its lanes
-        const int pt = tid - (S::SOFT + 1) * 32;
-        constexpr int CH = D / 8, RPI = S::NP / CH;                   // chunks of a row; rows that the threads copy at a time
-        const int ch = pt % CH, r0 = pt / CH;
-        const uint32_t to0 = (uint32_t)(r0 * 128);
+        // ---------------------------------------------------------------- copies: a warp for 32 rows of every tile, each for itself
+        const int part = warp - S::SOFT - 1;
+        constexpr int CH = D / 8;                                     // 16-byte chunks of a row
         const uint32_t slots = smem_u32(base + S::off_slots), q_at = smem_u32(base);
-        ulonglong2 *rows = (ulonglong2 *)(base + S::off_rows);
-        uint32_t n_slot = 0, n_seg = 0, n_row = 0;
-        // Copies arrive on their barrier by themselves.  Not so values of a tile that some rows do not see: entries that are not finite
-        // leave it first, as 0 times them would reach those rows.  That waits until the next copies are under way, or until there is no
-        // room for them.
-        bool late_values = false, before = false;                     // (before: the tile before is one that some rows do not see)
+        uint32_t n = 0, n_seg = 0, n_tile = 0;                        // n: the next slot to fill
+        // Blocks of boxes of at least 8 slots go by the tensor map, a box per thread and panel.  Where not all rows see all of the warp's keys, or a
+        // block is bad, the warp's threads copy: keys that no row sees, or on bad blocks, as zeros, nothing of them is read.  Such copies arrive
+        // on their barrier by themselves, but for values: entries that are not finite leave those first, as 0 times them would reach rows that do
+        // not see them.  That waits until the next copies are under way, or until there is no room for them.
+        bool late_values = false;
         uint32_t late_slot = 0;
+        const auto place = [&](uint32_t slot, int row, int chunk) {
+            return (slot + chunk / (8 * S::WIDE)) % S::SLOTS * S::SLOT + chunk / 8 % S::WIDE * PANEL + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
+        };
         const auto clean = [&]() {
 #pragma unroll 1
-            for (int i = r0; i < KT; i += RPI) {
-                unsigned char *at = base + S::off_slots + (late_slot + ch / 8) % S::SLOTS * PANEL + i * 128 + (((ch & 7) ^ (i & 7)) << 4);
-                uint4 w = *(uint4 *)at;
-                uint32_t *x = (uint32_t *)&w;
+            for (int i = 0; i < CH; ++i) {
+                const int x = i * 32 + lane;
+                unsigned char *at = base + S::off_slots + place(late_slot, part * 32 + x / CH, x % CH);
+                uint4 v = *(uint4 *)at;
+                uint32_t *e = (uint32_t *)&v;
                 bool bad = false;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    if (Pair<T>::finite(x[k])) continue;
+                    if (Pair<T>::finite(e[k])) continue;
                     bad = true;
-                    const uint32_t lo = x[k] & 0xFFFFu, hi = x[k] & 0xFFFF0000u;
-                    x[k] = (Pair<T>::finite(lo) ? lo : 0u) | (Pair<T>::finite(hi) ? hi : 0u);
+                    const uint32_t lo = e[k] & 0xFFFFu, hi = e[k] & 0xFFFF0000u;
+                    e[k] = (Pair<T>::finite(lo) ? lo : 0u) | (Pair<T>::finite(hi) ? hi : 0u);
                 }
-                if (bad) { *(uint4 *)at = w; *(volatile int *)&B->poison = 1; }
+                if (bad) { *(uint4 *)at = v; *(volatile int *)&B->poison = 1; }
             }
             tc::publish_shared();
-            for (int p = 0; p < S::PANELS; ++p) mbar_arrive(&B->full[(late_slot + p) % S::SLOTS]);
+            for (int p = 0; p < S::STEP; ++p) mbar_arrive(&B->full[(late_slot + p) % S::SLOTS]);
             late_values = false;
         };
         // a wait for room: values that are held back may be what the room is waiting for
         const auto room = [&](uint64_t *bar, uint32_t parity) {
-            if (late_values && !mbar_test(bar, parity)) { tc::wait_copies<0>(); clean(); }
+            if (late_values && !__all_sync(0xffffffffu, mbar_test(bar, parity))) { tc::wait_copies<0>(); clean(); }
             wait(B, bar, parity);
+            __syncwarp();
         };
-        // Block of the thread's key of a tile, -1 where no row of the request sees it: asked for a tile ahead of its use.
-        struct Source { int id, in; bool seen; };
+        // Block and slot of the lane's key of a tile, asked for a tile ahead of its use.  whole: all rows see all of the warp's keys.
+        struct Source { int id, in, h, b; bool seen, whole; };
         const auto source = [&](const Segment &s, int tile) {
-            const long long key = (long long)tile * KT + pt;
-            Source x = {-1, 0, key < (long long)s.r.len + s.r.n &&
-                                   (key >= s.r.len || P.window == 0 || key < P.sinks || key > (long long)s.r.len - P.window)};
+            const long long first = (long long)tile * KT + part * 32, key = first + lane;
+            Source x = {-1, 0, s.h, s.b,
+                        key < (long long)s.r.len + s.r.n &&
+                            (key >= s.r.len || P.window == 0 || key < P.sinks || key > (long long)s.r.len - P.window),
+                        seen_by_all(P, s.r, first, 32)};
             if (x.seen) {
                 const int col = column_of(P, (int)key);
                 x.in = (int)key - col * P.block;
@@ -835,83 +843,88 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             }
             return x;
         };
-        // addresses of a tile's rows, one per thread: odd where no row of the request sees the key or its block is bad
-        const auto put_sources = [&](const Segment &s, const Source &x) {
-            const bool good = x.seen && x.id >= 0 && x.id < P.num_blocks;
-            ulonglong2 a = make_ulonglong2((unsigned long long)P.k | 1, (unsigned long long)P.v | 1);       // (odd: zeros, nothing is read)
-            if (good) {
-                a.x = (unsigned long long)((const T *)P.k + x.id * P.k_stride[0] + x.in * P.k_stride[1] + s.h * P.k_stride[2]);
-                a.y = (unsigned long long)((const T *)P.v + x.id * P.v_stride[0] + x.in * P.v_stride[1] + s.h * P.v_stride[2]);
-            }
-            bar_sync(4, S::NP);                                       // (all are through with the tile before the last)
-            rows[(n_row & 1) * KT + pt] = a;
-            const uint32_t bad = __ballot_sync(0xffffffffu, x.seen && !good);
-            if (lane == 0) B->hidden[n_row & 7][pt >> 5] = bad;
-            bar_sync(4, S::NP);
-            ++n_row;
-        };
-        const auto copy_tile = [&](uint32_t n, uint32_t which, bool values, bool part) {
-            for (int p = 0; p < S::PANELS; ++p) {
+        const auto copy_rows = [&](const Source &x, bool by_map, bool values) {
+            for (int p = 0; p < S::STEP; ++p) {
                 const uint32_t k = n + p;
                 if (k >= S::SLOTS) room(&B->empty[k % S::SLOTS], (k / S::SLOTS - 1) & 1);
             }
-            const unsigned long long *from = (const unsigned long long *)(rows + (which & 1) * KT) + (values ? 1 : 0);
-            const uint32_t to = slots + (n + ch / 8) % S::SLOTS * PANEL + to0;
-            constexpr int EACH = KT / RPI, STEP = 8;
-#pragma unroll 1
-            for (int k0 = 0; k0 < EACH; k0 += STEP) {
-                unsigned long long a[STEP];
-#pragma unroll
-                for (int k = 0; k < STEP; ++k) a[k] = from[2 * (r0 + (k0 + k) * RPI)];
-#pragma unroll
-                for (int k = 0; k < STEP; ++k)
-                    tc::copy16(to + (k0 + k) * RPI * 128 + (((ch & 7) ^ ((r0 + k * RPI) & 7)) << 4), (a[k] & ~1ull) + ch * 16, a[k] & 1 ? 0 : 16);
+            bool hold = false;
+            if (by_map) {
+                if (lane == 0) {
+                    for (int p = 0; p < S::STEP; ++p) {
+                        uint64_t *bar = &B->full[(n + p) % S::SLOTS];
+                        tc::expect_bytes(bar, 32 * 128 * S::WIDE);
+                        tc::arrive_many(bar, 32);
+                    }
+                }
+                const int boxes = 32 / P.box, g = lane % boxes, p = lane / boxes;
+                const int id = __shfl_sync(0xffffffffu, x.id, g * P.box), in = __shfl_sync(0xffffffffu, x.in, g * P.box);
+                for (int k = p; k < S::PANELS; k += P.box)
+                    tc::box_load(slots + place(n, part * 32 + g * P.box, k * 8), values ? &P.v_map : &P.k_map, k * 64, x.h, in, id,
+                                 &B->full[(n + k / S::WIDE) % S::SLOTS]);
+            } else {
+                const long long *st = values ? P.v_stride : P.k_stride;
+                const T *from = (const T *)(values ? P.v : P.k);
+                const bool good = x.seen && x.id >= 0 && x.id < P.num_blocks;
+                // (odd: zeros)
+                const unsigned long long a = good ? (unsigned long long)(from + x.id * st[0] + x.in * st[1] + x.h * st[2]) : (unsigned long long)from | 1;
+#pragma unroll 4
+                for (int i = 0; i < CH; ++i) {
+                    const int y = i * 32 + lane, row = y / CH;
+                    const unsigned long long f = __shfl_sync(0xffffffffu, a, row);
+                    tc::copy16(slots + place(n, part * 32 + row, y % CH), (f & ~1ull) + (y % CH) * 16, f & 1 ? 0 : 16);
+                }
+                hold = values && !x.whole;
+                if (!hold)
+                    for (int p = 0; p < S::STEP; ++p) tc::arrive_with_copies(&B->full[(n + p) % S::SLOTS]);
             }
-            const bool hold = values && part;
-            if (!hold)
-                for (int p = 0; p < S::PANELS; ++p) tc::arrive_with_copies(&B->full[(n + p) % S::SLOTS]);
             tc::close_copies();
             if (late_values) { tc::wait_copies<1>(); clean(); }
             if (hold) { late_values = true; late_slot = n; }
+            n += S::STEP;
         };
         const auto copy_q = [&](const Segment &s) {
             if (n_seg) room(&B->q_empty, (n_seg - 1) & 1);
-            const T *q = (const T *)P.q + s.b * P.q_stride[0] + s.h * P.G * P.q_stride[2] + ch * 8;
+            const T *q = (const T *)P.q + s.b * P.q_stride[0] + s.h * P.G * P.q_stride[2];
 #pragma unroll 4
-            for (int i = r0; i < S::ROWS; i += RPI) {
-                const int r = s.m * S::ROWS + i, node = node_of(P, r);
-                const bool in = i < s.rows;
-                tc::copy16(q_at + ((ch / 8) * MT + i / 128) * PANEL + i % 128 * 128 + (((ch & 7) ^ (i & 7)) << 4),
-                           (unsigned long long)(in ? q + node * P.q_stride[1] + (r - node * P.G) * P.q_stride[2] : (const T *)P.q), in ? 16 : 0);
+            for (int i = 0; i < MT * CH; ++i) {
+                const int y = i * 32 + lane, row = part * (32 * MT) + y / CH, c = y % CH, r = s.m * S::ROWS + row, node = node_of(P, r);
+                const bool in = row < s.rows;
+                tc::copy16(q_at + ((c / 8) * MT + row / 128) * PANEL + row % 128 * 128 + (((c & 7) ^ (row & 7)) << 4),
+                           (unsigned long long)(in ? q + node * P.q_stride[1] + (r - node * P.G) * P.q_stride[2] + c * 8 : (const T *)P.q), in ? 16 : 0);
             }
             tc::arrive_with_copies(&B->q_full);
             tc::close_copies();
             ++n_seg;
         };
         if (hand->next(P, S::ROWS, 0)) {
-            bool more = true;
+            bool more = true, before_map = false;
             int step = 0, in = 0;                                     // in: which of the segments in hand is gone through
-            Source src = source(hand->seg[0], hand->seg[0].tile(0));
+            Source ahead = source(hand->seg[0], hand->seg[0].tile(0)), before = ahead;
             while (more) {
                 const Segment &now = hand->seg[in];
                 const int at = step;
-                const Source here = src;
+                const Source here = ahead;
                 const bool last = ++step == now.steps();
                 if (last) { more = hand->next(P, S::ROWS, in ^= 1); step = 0; }
-                if (more) src = source(hand->seg[in], hand->seg[in].tile(step));
-                const bool part = !seen_by_all(P, now.r, now.tile(at));
-                put_sources(now, here);
-                copy_tile(n_slot, n_row - 1, false, part);
-                n_slot += S::PANELS;
+                if (more) ahead = source(hand->seg[in], hand->seg[in].tile(step));
+                const uint32_t bad = __ballot_sync(0xffffffffu, here.seen && (here.id < 0 || here.id >= P.num_blocks));
+                const bool by_map = P.box && here.whole && bad == 0;
+                if (lane == 0) {
+                    B->hidden[n_tile & 7][part] = bad;
+                    ((volatile unsigned char *)&B->plain[n_tile & 7])[part] = !by_map;
+                }
+                ++n_tile;
+                copy_rows(here, by_map, false);
                 if (at == 0) copy_q(now);
                 if (MT == 1) {
                     // values a tile behind the keys
-                    if (at > 0) { copy_tile(n_slot, n_row - 2, true, before); n_slot += S::PANELS; }
-                    if (last) { copy_tile(n_slot, n_row - 1, true, part); n_slot += S::PANELS; }
-                    before = part;
+                    if (at > 0) copy_rows(before, before_map, true);
+                    if (last) copy_rows(here, by_map, true);
+                    before = here;
+                    before_map = by_map;
                 } else {
-                    copy_tile(n_slot, n_row - 1, true, part);
-                    n_slot += S::PANELS;
+                    copy_rows(here, by_map, true);
                 }
             }
         }

@@ -75,6 +75,32 @@ template <typename K> int prepare(K kernel, int smem, bool big_clusters)
     return SPEC_OK;
 }
 
+// Tensor map of a cache of 16-bit entries as [block][slot][head][entry]; boxes of `box` slots by 64 entries, 128-byte swizzle.  The driver's
+// function is asked for once.
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+bool cache_map(CUtensorMap *map, const void *cache, const int64_t stride[3], int D, int Hkv, int block, int num_blocks, int box, bool half)
+{
+    static const EncodeTiled encode = [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess) { cudaGetLastError(); return (EncodeTiled) nullptr; }
+        return found == cudaDriverEntryPointSuccess ? (EncodeTiled)f : nullptr;
+    }();
+    if (!encode) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)Hkv, (cuuint64_t)block, (cuuint64_t)num_blocks};
+    cuuint64_t strides[3];
+    for (int i = 0; i < 3; ++i) {
+        const int64_t s = stride[2 - i] * 2;                    // (nothing steps along a dimension of one entry)
+        if (s < 0 || (s == 0 && dims[i + 1] > 1) || s >= (1ll << 40)) return false;
+        strides[i] = s ? (cuuint64_t)s : 16;
+    }
+    const cuuint32_t shape[4] = {64, 1, (cuuint32_t)box, 1}, each[4] = {1, 1, 1, 1};
+    return encode(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(cache), dims, strides, shape,
+                  each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // CTAs of the attention kernel: one per SM
 int attention_ctas()
 {
@@ -237,6 +263,10 @@ int32_t spec_tree_attention(const SpecAttention *a, void *ws, int64_t ws_bytes, 
     p.ml = (float2 *)((unsigned char *)ws + L.ml);
     p.late = (int *)((unsigned char *)ws + L.late);
     const bool half = a->dtype == SPEC_F16;
+    p.box = a->block_size % 8 ? 0 : a->block_size % 16 ? 8 : a->block_size % 32 ? 16 : 32;
+    if (p.box && !(cache_map(&p.k_map, a->k_cache, a->k_cache_stride, a->D, a->Hkv, a->block_size, a->num_blocks, p.box, half) &&
+                   cache_map(&p.v_map, a->v_cache, a->v_cache_stride, a->D, a->Hkv, a->block_size, a->num_blocks, p.box, half)))
+        p.box = 0;
     const cudaStream_t st = (cudaStream_t)stream;
     const auto go = [&](auto shape, auto attend_kernel, auto join_kernel) -> int {
         using S = decltype(shape);

@@ -61,10 +61,10 @@ __device__ __forceinline__ void wait_stores() { asm volatile("tcgen05.wait::st.s
 
 // ---- products -----------------------------------------------------------------------------------------------------------------
 // Shared-memory operand in panels of 64 16-bit entries: rows of 128 bytes, 16-byte chunk c of row r at chunk c ^ (r % 8); eight rows
-// (1024 bytes) from group to group.
+// (1024 bytes) from group to group; where the operand's rows run along the contraction, the next 64 of its entries lie a panel of 128 rows on.
 __device__ __forceinline__ uint64_t panel_desc(uint32_t addr)
 {
-    return (uint64_t)((addr >> 4) & 0x3FFF) | ((uint64_t)(1024 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+    return (uint64_t)((addr >> 4) & 0x3FFF) | ((uint64_t)(16384 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 // M = 128, fp32 sums; type 0: f16, 1: bf16; b_rows: the second operand's rows run along the contraction (its entries of a
 // row along N)
@@ -111,6 +111,22 @@ __device__ __forceinline__ void copy16(uint32_t to, unsigned long long from, int
 __device__ __forceinline__ void arrive_with_copies(uint64_t *bar)
 {
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// A box by a tensor map of four dimensions; its bytes count on the barrier.
+__device__ __forceinline__ void box_load(uint32_t to, const void *map, int x, int y, int z, int w, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(to), "l"(map),
+                 "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
+                 : "memory");
+}
+__device__ __forceinline__ void prefetch_map(const void *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+__device__ __forceinline__ void expect_bytes(uint64_t *bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void arrive_many(uint64_t *bar, uint32_t count)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(count) : "memory");
 }
 __device__ __forceinline__ void close_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
