@@ -31,6 +31,8 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.69314718055994531f;
 
 struct Params {
     CUtensorMap k_map, v_map;                  // the caches as [block][slot][head][entry], boxes of `box` slots by 64 entries
+    CUtensorMap q_map;                         // the queries as [request][node][head][entry], boxes of 128 rows by 64 entries
+    bool q_boxes;                              // (where 128 rows are whole nodes)
     int box;                                   // a power of two up to 32 that divides the block; 0: blocks of no multiple of 8 slots
     TreeArgs tree;
     int B, Hq, Hkv, G, num_blocks, block, width, window, sinks;
@@ -276,6 +278,7 @@ __device__ __forceinline__ int block_in(const Params &P, int b, int col)
 template <int D_, int MT_, int WG_> struct Shape {
     static constexpr int D = D_, MT = MT_, WG = WG_;
     static constexpr bool TURNS = MT == 1 && WG == 2;
+    static constexpr int PARTS = MT == 2 ? 2 : 1, W = KT / PARTS;                 // a tile's columns in parts: see the products
     static constexpr int PANELS = D / 64;
     static constexpr int ROWS = 128 * MT;
     static constexpr int WIDE = PANELS < 2 ? 1 : 2;                               // panels of a slot: up to 128 entries of a tile's rows
@@ -294,7 +297,7 @@ template <int D_, int MT_, int WG_> struct Shape {
 };
 struct Bars {
     uint64_t full[16], empty[16];
-    uint64_t q_full, q_empty, s_full[2], p_full[2], pv_done[2], o_empty[2];
+    uint64_t q_full, q_empty, s_full[4], p_full[4], pv_done[2], o_empty[2];
     uint32_t tmem;
     int dead, poison;
     uint32_t hidden[8][4];                     // keys of a tile on bad blocks, by the tile's number in the CTA's run % 8
@@ -358,16 +361,6 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-__device__ __forceinline__ float top_of(const uint32_t (&s)[32], float top)
-{
-    float other = top;                                              // (two chains)
-#pragma unroll
-    for (int k = 0; k < 32; k += 4) {
-        top = max3(top, __uint_as_float(s[k]), __uint_as_float(s[k + 1]));
-        other = max3(other, __uint_as_float(s[k + 2]), __uint_as_float(s[k + 3]));
-    }
-    return max3(top, other, other);
-}
 // 2^y of a pair without the special function unit, which does 16 a cycle on an SM and is what the arithmetic of a tile waits for: y = n + f,
 // n the nearest integer (adding 1.5 2^23 leaves it in the low bits), 2^f by the polynomial of degree 5 that fits it to 2e-7 on
 // [-1/2, 1/2], n added to the exponent.  Exactly 0 for y <= -127.
@@ -410,45 +403,74 @@ __device__ __forceinline__ void weigh(const uint32_t (&s)[32], unsigned long lon
         pk[k / 2] = Pair<T>::pack(x, y);
     }
 }
+// the largest of 32 scores, NaN where one of them is
+__device__ __forceinline__ float top_of(const uint32_t (&s)[32])
+{
+    float top = __uint_as_float(s[0]), other = __uint_as_float(s[1]);         // (two chains)
+#pragma unroll
+    for (int k = 2; k < 30; k += 4) {
+        top = max3(top, __uint_as_float(s[k]), __uint_as_float(s[k + 1]));
+        other = max3(other, __uint_as_float(s[k + 2]), __uint_as_float(s[k + 3]));
+    }
+    return max3(max3(top, other, other), __uint_as_float(s[30]), __uint_as_float(s[31]));
+}
 // Scores that the row does not see become -inf.
-__device__ __forceinline__ void hide(uint32_t at, const uint32_t (&words)[4])
+template <int W> __device__ __forceinline__ void hide(uint32_t at, const uint32_t (&words)[4], int first)
 {
 #pragma unroll 1
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < W / 32; ++w) {
         uint32_t a[32];
         tc::tmem_load(at + 32 * w, a);
         tc::wait_loads(a);
-        const uint32_t word = w == 0 ? words[0] : w == 1 ? words[1] : w == 2 ? words[2] : words[3];
+        const int x = first + w;
+        const uint32_t word = x == 0 ? words[0] : x == 1 ? words[1] : x == 2 ? words[2] : words[3];
 #pragma unroll
         for (int k = 0; k < 32; ++k) a[k] = (word >> k) & 1u ? a[k] : 0xFF800000u;
         tc::tmem_store(at + 32 * w, a);
     }
     tc::wait_stores();
 }
-// The largest score of a tile.
-__device__ __forceinline__ float tile_top(uint32_t at)
+// A row's state: reference (any: there is one) and the sum of its weights.
+struct Row {
+    float ref, l;
+    bool any;
+};
+__device__ __noinline__ void scale_sums(uint32_t at, int columns, float f)
+{
+    for (int d = 0; d < columns; d += 32) {
+        uint32_t o[32];
+        tc::tmem_load(at + d, o);
+        tc::wait_loads(o);
+#pragma unroll
+        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+        tc::tmem_store(at + d, o);
+    }
+    tc::wait_stores();
+}
+// The largest of W scores.
+template <int W> __device__ __forceinline__ float tile_top(uint32_t at)
 {
     float top = -CUDART_INF_F;
 #pragma unroll 1
-    for (int w = 0; w < KT; w += 64) {
+    for (int w = 0; w < W; w += 64) {
         uint32_t a[32], b[32];
         tc::tmem_load(at + w, a);
         tc::tmem_load(at + w + 32, b);
         tc::wait_loads(a);
         tc::wait_loads(b);
-        top = top_of(a, top);
-        top = top_of(b, top);
+        top = max3(top, top_of(a), top_of(b));
     }
     return top;
 }
-// A tile's weights, put in the place of its scores (16 columns for 32: never beyond the scores that are loaded); returns their sum.  A loop, not
-// four copies: the schedulers' instruction caches hold the loops of all roles, and fetching what does not fit took longer than the arithmetic.
-template <typename T> __device__ __forceinline__ float tile_weights(uint32_t at, float c, float ref)
+// W weights, put in the place of the scores (16 columns for 32: never beyond the scores that are loaded).  A loop, not copies: the schedulers'
+// instruction caches hold the loops of all roles, and fetching what does not fit took longer than the arithmetic (unrolled: 3700
+// cycles for a tile of 256 rows, rolled: 1700).
+template <typename T, int W> __device__ __forceinline__ float tile_weights(uint32_t at, float c, float ref)
 {
     unsigned long long s2 = 0ull;
     const unsigned long long c2 = pack_f32x2(c, c), r2 = pack_f32x2(-ref, -ref);
 #pragma unroll 1
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < W / 32; ++w) {
         uint32_t a[32], pk[16];
         tc::tmem_load(at + 32 * w, a);
         tc::wait_loads(a);
@@ -497,9 +519,8 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         for (int i = 0; i < S::SLOTS; ++i) { mbar_init(&B->full[i], S::NP); mbar_init(&B->empty[i], 1); }
         mbar_init(&B->q_full, S::NP);
         mbar_init(&B->q_empty, 1);
+        for (int t = 0; t < 4; ++t) { mbar_init(&B->s_full[t], 1); mbar_init(&B->p_full[t], 4); }
         for (int t = 0; t < 2; ++t) {
-            mbar_init(&B->s_full[t], 1);
-            mbar_init(&B->p_full[t], 4);
             mbar_init(&B->pv_done[t], 1);
             mbar_init(&B->o_empty[t], S::TURNS ? 8 : 4);
         }
@@ -526,7 +547,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         unsigned short *parent = (unsigned short *)(base + S::off_parent) + w * SPEC_MAX_NODES;
         float2 *halves = (float2 *)(base + S::off_halves);
         const float c = P.scale * LOG2E;
-        uint32_t n_tile = 0, n_run = 0, n_seg = 0;     // tiles that this warpgroup has been through, tiles of the run that went by, segments
+        uint32_t n_part = 0, n_run = 0, n_seg = 0;     // parts of tiles that this warpgroup has been through, tiles of the run, segments
         int tree_of = -1;
         Segment &seg = hand->seg[0];
         for (; hand->next(P, S::ROWS, 0); ++n_seg) {
@@ -551,66 +572,67 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             if (P.window)
                 for (unsigned short x = parent[node]; x != 0xFFFF; x = parent[x]) ++depth;
             Walk walk = {node, 0};
-            float ref = 0.f, l = 0.f;
-            bool any = false, begun = false;           // whether the row has a reference; whether there has been a tile
+            Row of = {0.f, 0.f, false};
+            bool begun = false;                        // whether there has been a tile
             for (int step = 0; step < steps; ++step, ++n_run) {
                 if (S::TURNS && (int)(n_run & 1) != w) continue;
-                const int buf = MT == 2 ? t : n_run & 1;
-                const uint32_t s_at = lanes + buf * 128;
-                wait(B, &B->s_full[buf], (MT == 2 ? n_tile : n_run >> 1) & 1);
-                tc::fence_after();
-                if (warp_live) {
-                    const int tile = seg.tile(step);
-                    const volatile uint32_t *hidden = B->hidden[n_run & 7];
-                    const uint32_t h0 = hidden[0], h1 = hidden[1], h2 = hidden[2], h3 = hidden[3];
-                    if (!seen_by_all(P, seg.r, tile) || (h0 | h1 | h2 | h3) != 0) {
-                        uint32_t words[4];
-                        seen_words(P, seg.r, tile, depth, parent, walk, words);
-                        words[0] &= ~h0; words[1] &= ~h1; words[2] &= ~h2; words[3] &= ~h3;
-                        hide(s_at, words);
-                    }
-                    const float top = tile_top(s_at) * c;                      // (c > 0)
-                    // a score that is no number, or infinite, leaves the row none either
-                    const float next = top < CUDART_INF_F ? top : CUDART_NAN_F;
-                    if (!begun) {
-                        any = !(top <= -CUDART_INF_F);
-                        ref = any ? next : 0.f;
-                    } else if (const bool over = any ? !(top <= ref + 8.f) : !(top <= -CUDART_INF_F); __any_sync(0xffffffffu, over)) {
-                        // a new reference: what has been summed is scaled
-                        const float old = ref;
-                        if (over) ref = next;
-                        const float f = over && any ? ex2_approx(old - ref) : 1.f;
-                        any |= over;
-                        l *= f;
-                        wait(B, &B->pv_done[w], (n_tile - 1) & 1);
-                        tc::fence_after();
+                uint32_t words[4] = {0u, 0u, 0u, 0u};
+                bool masked = false;
 #pragma unroll 1
-                        for (int d = 0; d < D; d += 32) {
-                            uint32_t o[32];
-                            tc::tmem_load(o_at + d, o);
-                            tc::wait_loads(o);
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-                            tc::tmem_store(o_at + d, o);
+                for (int h = 0; h < S::PARTS; ++h, ++n_part) {
+                    const int buf = MT == 2 ? t * 2 + h : n_run & 1;
+                    const uint32_t s_at = lanes + (MT == 2 ? buf * 64 : buf * 128);
+                    wait(B, &B->s_full[buf], (MT == 2 ? n_part >> 1 : n_run >> 1) & 1);
+                    tc::fence_after();
+                    if (warp_live) {
+                        if (h == 0) {
+                            const int tile = seg.tile(step);
+                            const volatile uint32_t *hidden = B->hidden[n_run & 7];
+                            const uint32_t h0 = hidden[0], h1 = hidden[1], h2 = hidden[2], h3 = hidden[3];
+                            masked = !seen_by_all(P, seg.r, tile) || (h0 | h1 | h2 | h3) != 0;
+                            if (masked) {
+                                seen_words(P, seg.r, tile, depth, parent, walk, words);
+                                words[0] &= ~h0; words[1] &= ~h1; words[2] &= ~h2; words[3] &= ~h3;
+                            }
                         }
+                        if (masked) hide<S::W>(s_at, words, h * (S::W / 32));
+                        const float top = tile_top<S::W>(s_at) * c;                // (c > 0)
+                        const bool over = of.any ? !(top <= of.ref + 8.f) : !(top <= -CUDART_INF_F);
+                        if (__any_sync(0xffffffffu, over)) {
+                            // a new reference: what has been summed is scaled
+                            float f = 1.f;
+                            if (over) {
+                                // (whole numbers: O keeps its digits; a score that is no number, or infinite, leaves the row none either, for good)
+                                const float ref = top < CUDART_INF_F && of.ref == of.ref ? ceilf(top) : CUDART_NAN_F;
+                                if (of.any) f = ex2_approx(of.ref - ref);
+                                of.ref = ref;
+                                of.any = true;
+                            }
+                            of.l *= f;
+                            if (begun && __any_sync(0xffffffffu, f != 1.f)) {
+                                wait(B, &B->pv_done[w], (n_part - 1) & 1);
+                                tc::fence_after();
+                                scale_sums(o_at, D, f);
+                            }
+                        }
+                        of.l += tile_weights<T, S::W>(s_at, c, of.ref);
+                        tc::wait_stores();
+                        tc::fence_before();
                     }
-                    l += tile_weights<T>(s_at, c, ref);
-                    tc::wait_stores();
-                    tc::fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&B->p_full[buf]);
+                    begun = true;
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&B->p_full[buf]);
-                begun = true;
-                ++n_tile;
             }
-            // the segment's end.  One warpgroup for all tiles: the last scores follow all products but the last two, which are waited for one
-            // after the other (the parity of a phase is that of the one two before)
+            // the segment's end.  Where scores run ahead of the weights, the last follow all products but the last two, which are waited for one after
+            // the other (the parity of a phase is that of the one two before)
             if (begun) {
-                if (S::WG == 1 && n_tile > 1) wait(B, &B->pv_done[w], n_tile & 1);
-                wait(B, &B->pv_done[w], (n_tile - 1) & 1);
+                if (!S::TURNS && n_part > 1) wait(B, &B->pv_done[w], n_part & 1);
+                wait(B, &B->pv_done[w], (n_part - 1) & 1);
             }
             tc::fence_after();
-            float f0 = 1.f, f1 = 0.f;
+            float ref = of.ref, l = of.l, f0 = 1.f, f1 = 0.f;
+            bool any = of.any;
             if (S::TURNS) {
                 // both turns' references and sums, then both O: this warpgroup gives out half of the columns
                 float2 *mine = halves + (n_seg & 1) * 256;
@@ -686,7 +708,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         }
     } else if (warp == S::SOFT) {
         // ---------------------------------------------------------------- products: one thread issues, the warp waits
-        constexpr uint32_t DS = tc::product_desc(Pair<T>::TYPE, KT, false), DO = tc::product_desc(Pair<T>::TYPE, 64 * S::WIDE, true);
+        constexpr uint32_t DS = tc::product_desc(Pair<T>::TYPE, S::W, false), DO = tc::product_desc(Pair<T>::TYPE, 64 * S::WIDE, true);
         const uint32_t q_at = smem_u32(base), slots = smem_u32(base + S::off_slots);
         uint32_t n = 0, n_seg = 0, n_tile = 0, n_p[2] = {0, 0}, n_o[2] = {0, 0};         // n: the next slot to read
         // the copies to slots k .., of the run's tile i, are there; what threads stored, seen through the barrier, is put before the tensor cores
@@ -703,34 +725,35 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             tc::fence_after();
             return true;
         };
-        // S of row block t into buffer buf, from the keys in slots k ..
-        const auto scores = [&](int t, int buf, uint32_t k, bool release) {
+        // S of row block t for part h of a tile into columns `to`, from the keys in slots k ..; `bar`: where that is told
+        const auto scores = [&](int t, int h, int to, uint32_t k, uint64_t *bar, bool release) {
             if (tc::elected()) {
 #pragma unroll
                 for (int p = 0; p < S::STEP; ++p) {
                     const uint32_t slot = (k + p) % S::SLOTS;
 #pragma unroll
                     for (int x = 0; x < S::WIDE; ++x) {
-                        const uint64_t qd = tc::panel_desc(q_at + ((p * S::WIDE + x) * MT + t) * PANEL), kd = tc::panel_desc(slots + slot * S::SLOT + x * PANEL);
+                        const uint64_t qd = tc::panel_desc(q_at + ((p * S::WIDE + x) * MT + t) * PANEL);
+                        const uint64_t kd = tc::panel_desc(slots + slot * S::SLOT + x * PANEL + h * S::W * 128);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) tc::mma_ss(tmem + buf * 128, qd + 2 * i, kd + 2 * i, DS, p > 0 || x > 0 || i > 0);
+                        for (int i = 0; i < 4; ++i) tc::mma_ss(tmem + to, qd + 2 * i, kd + 2 * i, DS, p > 0 || x > 0 || i > 0);
                     }
                     if (release) tc::commit(&B->empty[slot]);
                 }
-                tc::commit(&B->s_full[buf]);
+                tc::commit(bar);
             }
             __syncwarp();
         };
-        // O number o (+)= P (in buffer buf) V, from the values in slots k ..
-        const auto sums = [&](int o, int buf, uint32_t k, bool add, bool release) {
+        // O number o (+)= P (in columns `from`) V for part h of a tile, from the values in slots k ..
+        const auto sums = [&](int o, int h, int from, uint32_t k, bool add, bool release) {
             if (tc::elected()) {
 #pragma unroll
                 for (int p = 0; p < S::STEP; ++p) {
                     const uint32_t slot = (k + p) % S::SLOTS;
-                    const uint64_t vd = tc::panel_desc(slots + slot * S::SLOT);
+                    const uint64_t vd = tc::panel_desc(slots + slot * S::SLOT + h * S::W * 128);
 #pragma unroll
-                    for (int i = 0; i < KT / 16; ++i)
-                        tc::mma_ts(tmem + S::O + o * D + p * 128, tmem + buf * 128 + i * 8, vd + i * (2048 >> 4), DO, add || i > 0);
+                    for (int i = 0; i < S::W / 16; ++i)
+                        tc::mma_ts(tmem + S::O + o * D + p * 128, tmem + from + i * 8, vd + i * (2048 >> 4), DO, add || i > 0);
                     if (release) tc::commit(&B->empty[slot]);
                 }
                 tc::commit(&B->pv_done[o]);
@@ -740,16 +763,16 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         for (; hand->next(P, S::ROWS, 0); ++n_seg) {
             const int steps = hand->seg[0].steps(), blocks = MT == 1 || hand->seg[0].rows <= 128 ? 1 : 2;
             wait(B, &B->q_full, n_seg & 1);
-            tc::publish_shared();
+            if (!P.q_boxes) tc::publish_shared();
             copied(n, n_tile);
             if (MT == 1) {
                 // order of the slots: K0, K1, V0, K2, V1, ...: scores one tile ahead
-                scores(0, n_tile & 1, n, true);
+                scores(0, 0, (n_tile & 1) * 128, n, &B->s_full[n_tile & 1], true);
                 n += S::STEP;
                 for (int i = 0; i < steps; ++i, ++n_tile) {
                     if (i + 1 < steps) {
                         copied(n, n_tile + 1);
-                        scores(0, (n_tile + 1) & 1, n, true);
+                        scores(0, 0, (n_tile + 1 & 1) * 128, n, &B->s_full[n_tile + 1 & 1], true);
                         n += S::STEP;
                     }
                     if (i + 1 == max(1, steps - 1) && tc::elected()) tc::commit(&B->q_empty);
@@ -758,28 +781,34 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                     wait(B, &B->p_full[buf], (n_tile >> 1) & 1);
                     if (i == 0 && n_seg) wait(B, &B->o_empty[0], (n_seg - 1) & 1);
                     tc::fence_after();
-                    sums(S::TURNS ? buf : 0, buf, n, i >= S::WG, true);
+                    sums(S::TURNS ? buf : 0, 0, buf * 128, n, i >= S::WG, true);
                     n += S::STEP;
                 }
             } else {
-                // order of the slots: K0, V0, K1, V1, ...: a row block's next scores right behind its sums
-                for (int t = 0; t < blocks; ++t) scores(t, t, n, t == blocks - 1);
+                // order of the slots: K0, V0, K1, V1, ....  A tile in two parts of 64 keys: while a row block's weights of one part are at work, its other part
+                // has its products, and its next scores right behind them.  (Products of one part: 8 with N = 64 for S, 4 with N = 128 for O.)
+                for (int h = 0; h < 2; ++h)
+                    for (int t = 0; t < blocks; ++t) scores(t, h, (t * 2 + h) * 64, n, &B->s_full[t * 2 + h], h == 1 && t == blocks - 1);
                 n += S::STEP;
                 if (steps == 1 && tc::elected()) tc::commit(&B->q_empty);
+#pragma unroll 1
                 for (int i = 0; i < steps; ++i, ++n_tile) {
                     copied(n, n_tile);
                     // the next keys' arrival is seen to before the weights are waited for, if it has come
                     const bool more = i + 1 < steps;
                     bool keys = more && is_copied(n + S::STEP, n_tile + 1);
-                    for (int t = 0; t < blocks; ++t) {
-                        wait(B, &B->p_full[t], n_p[t] & 1);
-                        ++n_p[t];
-                        if (i == 0) { if (n_o[t]) wait(B, &B->o_empty[t], (n_o[t] - 1) & 1); ++n_o[t]; }
+#pragma unroll 1
+                    for (int u = 0; u < 2 * blocks; ++u) {
+                        const int h = u / blocks, t = u % blocks, buf = t * 2 + h;
+                        const bool last = u == 2 * blocks - 1;
+                        wait(B, &B->p_full[buf], n_p[t] & 1);
+                        if (h == 1) ++n_p[t];
+                        if (i == 0 && h == 0) { if (n_o[t]) wait(B, &B->o_empty[t], (n_o[t] - 1) & 1); ++n_o[t]; }
                         tc::fence_after();
-                        sums(t, t, n, i > 0, t == blocks - 1);
+                        sums(t, h, buf * 64, n, i > 0 || h > 0, last);
                         if (!more) continue;
                         if (!keys) { copied(n + S::STEP, n_tile + 1); keys = true; }
-                        scores(t, t, n + S::STEP, t == blocks - 1);
+                        scores(t, h, buf * 64, n + S::STEP, &B->s_full[buf], last);
                     }
                     if (i + 2 == steps && tc::elected()) tc::commit(&B->q_empty);
                     n += more ? 2 * S::STEP : S::STEP;
@@ -885,6 +914,18 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         };
         const auto copy_q = [&](const Segment &s) {
             if (n_seg) room(&B->q_empty, (n_seg - 1) & 1);
+            ++n_seg;
+            if (P.q_boxes) {
+                // (nodes beyond N come as zeros)
+                if (part == 0 && lane == 0) {
+                    tc::expect_bytes(&B->q_full, S::ROWS * D * 2);
+                    tc::arrive_many(&B->q_full, S::NP);
+                }
+                __syncwarp();
+                if (part == 0 && lane < S::PANELS * MT)
+                    tc::box_load(q_at + lane * PANEL, &P.q_map, lane / MT * 64, s.h * P.G, node_of(P, s.m * S::ROWS + lane % MT * 128), s.b, &B->q_full);
+                return;
+            }
             const T *q = (const T *)P.q + s.b * P.q_stride[0] + s.h * P.G * P.q_stride[2];
 #pragma unroll 4
             for (int i = 0; i < MT * CH; ++i) {
@@ -895,7 +936,6 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             }
             tc::arrive_with_copies(&B->q_full);
             tc::close_copies();
-            ++n_seg;
         };
         if (hand->next(P, S::ROWS, 0)) {
             bool more = true, before_map = false;

@@ -75,11 +75,11 @@ template <typename K> int prepare(K kernel, int smem, bool big_clusters)
     return SPEC_OK;
 }
 
-// Tensor map of a cache of 16-bit entries as [block][slot][head][entry]; boxes of `box` slots by 64 entries, 128-byte swizzle.  The driver's
-// function is asked for once.
+// Tensor map of 16-bit entries in four dimensions (sizes and strides in entries from the innermost, whose entries are contiguous), boxes 64 entries
+// wide, 128-byte swizzle; false where it has no map.  The driver's function is asked for once.
 typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                                 const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-bool cache_map(CUtensorMap *map, const void *cache, const int64_t stride[3], int D, int Hkv, int block, int num_blocks, int box, bool half)
+bool tensor_map(CUtensorMap *map, const void *base, bool half, const int64_t (&size)[4], const int64_t (&stride)[3], const int (&box)[3])
 {
     static const EncodeTiled encode = [] {
         void *f = nullptr;
@@ -88,15 +88,15 @@ bool cache_map(CUtensorMap *map, const void *cache, const int64_t stride[3], int
         return found == cudaDriverEntryPointSuccess ? (EncodeTiled)f : nullptr;
     }();
     if (!encode) return false;
-    const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)Hkv, (cuuint64_t)block, (cuuint64_t)num_blocks};
-    cuuint64_t strides[3];
+    cuuint64_t dims[4], strides[3];
+    for (int i = 0; i < 4; ++i) dims[i] = (cuuint64_t)size[i];
     for (int i = 0; i < 3; ++i) {
-        const int64_t s = stride[2 - i] * 2;                    // (nothing steps along a dimension of one entry)
-        if (s < 0 || (s == 0 && dims[i + 1] > 1) || s >= (1ll << 40)) return false;
+        const int64_t s = stride[i] * 2;                        // (nothing steps along a dimension of one entry)
+        if (s < 0 || (s == 0 && size[i + 1] > 1) || s >= (1ll << 40)) return false;
         strides[i] = s ? (cuuint64_t)s : 16;
     }
-    const cuuint32_t shape[4] = {64, 1, (cuuint32_t)box, 1}, each[4] = {1, 1, 1, 1};
-    return encode(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(cache), dims, strides, shape,
+    const cuuint32_t shape[4] = {64, (cuuint32_t)box[0], (cuuint32_t)box[1], (cuuint32_t)box[2]}, each[4] = {1, 1, 1, 1};
+    return encode(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides, shape,
                   each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -264,9 +264,12 @@ int32_t spec_tree_attention(const SpecAttention *a, void *ws, int64_t ws_bytes, 
     p.late = (int *)((unsigned char *)ws + L.late);
     const bool half = a->dtype == SPEC_F16;
     p.box = a->block_size % 8 ? 0 : a->block_size % 16 ? 8 : a->block_size % 32 ? 16 : 32;
-    if (p.box && !(cache_map(&p.k_map, a->k_cache, a->k_cache_stride, a->D, a->Hkv, a->block_size, a->num_blocks, p.box, half) &&
-                   cache_map(&p.v_map, a->v_cache, a->v_cache_stride, a->D, a->Hkv, a->block_size, a->num_blocks, p.box, half)))
-        p.box = 0;
+    const int64_t sizes[4] = {a->D, a->Hkv, a->block_size, a->num_blocks}, q_sizes[4] = {a->D, a->Hq, a->N, a->B};
+    const auto cache_map = [&](CUtensorMap *map, const void *cache, const int64_t *s) {
+        return tensor_map(map, cache, half, sizes, {s[2], s[1], s[0]}, {1, p.box, 1});
+    };
+    if (p.box && !(cache_map(&p.k_map, a->k_cache, a->k_cache_stride) && cache_map(&p.v_map, a->v_cache, a->v_cache_stride))) p.box = 0;
+    p.q_boxes = 128 % p.G == 0 && tensor_map(&p.q_map, a->q, half, q_sizes, {a->q_stride[2], a->q_stride[1], a->q_stride[0]}, {p.G, 128 / p.G, 1});
     const cudaStream_t st = (cudaStream_t)stream;
     const auto go = [&](auto shape, auto attend_kernel, auto join_kernel) -> int {
         using S = decltype(shape);

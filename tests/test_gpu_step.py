@@ -367,6 +367,24 @@ def test_attention_passes_on_what_a_row_sees():
     assert bool((got[1:, :, 9] == float("inf")).all())
 
 
+@pytest.mark.parametrize("length", [40, 301, 700])
+@pytest.mark.parametrize("fill", [float("nan"), float("inf")])
+def test_attention_of_keys_that_are_no_numbers(length, fill):
+    """Rows that see such a key are NaN in every entry, wherever in the sequence it lies; the others are as without it."""
+    parent = tree(4, 2, 4)
+    c = attention_case([length], parent, 4, 2, 128, torch.bfloat16, 16, seed=13)
+    clean = binding.tree_attention(**cuda(c))
+    tree_paths = ref.paths(parent.tolist())
+    for j in (0, 31, 33, 100, 130, length - 1, length + 7):
+        if j >= length and j != length + 7 or j < 0:
+            continue
+        d = cuda(c)
+        d["k_cache"][c["block_table"][0, j // 16].item(), j % 16] = fill
+        got = binding.tree_attention(**d).out[0].cpu()
+        hit = torch.tensor([j < length or j - length in p for p in tree_paths])
+        assert bool(got[hit].isnan().all()) and torch.equal(got[~hit], clean.out[0].cpu()[~hit])
+
+
 def test_attention_with_bad_blocks_and_bad_trees():
     parent = tree(4, 2, 4).repeat(5, 1)
     c = attention_case([100, 100, 100, 10, 33], parent, 4, 2, 128, torch.bfloat16, 16, seed=13)
