@@ -284,7 +284,7 @@ template <int D_, int MT_, int WG_> struct Shape {
     static constexpr int WIDE = PANELS < 2 ? 1 : 2;                               // panels of a slot: up to 128 entries of a tile's rows
     static constexpr int SLOT = WIDE * PANEL, STEP = PANELS / WIDE;               // bytes of a slot; slots of a tile's keys or values
     static constexpr int SLOTS = D == 64 ? 10 : MT == 2 || D == 256 ? 4 : 5;      // slots in flight
-    static constexpr int SOFT = 4 * WG, WARPS = SOFT + 1 + 4, NT = WARPS * 32;    // warps: rows, products, copies
+    static constexpr int SOFT = 4 * WG, WARPS = SOFT + WG + 4, NT = WARPS * 32;   // warps: rows, products (one per row warpgroup), copies
     static constexpr int NP = 128;                                                // threads that copy
     static constexpr int O = 256;                                                 // column of the first O; S buffers at 0 and 128
     static constexpr int off_slots = ROWS * D * 2;
@@ -516,9 +516,9 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
     if (warp == S::SOFT) tc::tmem_alloc(&B->tmem, 512);
     if (tid == S::NT - 1 && P.box) { tc::prefetch_map(&P.k_map); tc::prefetch_map(&P.v_map); }
     if (tid == 0) {
-        for (int i = 0; i < S::SLOTS; ++i) { mbar_init(&B->full[i], S::NP); mbar_init(&B->empty[i], 1); }
+        for (int i = 0; i < S::SLOTS; ++i) { mbar_init(&B->full[i], S::NP); mbar_init(&B->empty[i], MT); }
         mbar_init(&B->q_full, S::NP);
-        mbar_init(&B->q_empty, 1);
+        mbar_init(&B->q_empty, S::WG);
         for (int t = 0; t < 4; ++t) { mbar_init(&B->s_full[t], 1); mbar_init(&B->p_full[t], 4); }
         for (int t = 0; t < 2; ++t) {
             mbar_init(&B->pv_done[t], 1);
@@ -706,24 +706,18 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             __syncwarp();
             if (lane == 0) mbar_arrive(&B->o_empty[t]);
         }
-    } else if (warp == S::SOFT) {
-        // ---------------------------------------------------------------- products: one thread issues, the warp waits
+    } else if (warp < S::SOFT + S::WG) {
+        // ---------------------------------------------------------------- products: one thread issues, the warp waits.  A warp per row warpgroup: what
+        // one spends on barriers (some 800 cycles a tile) passes while the tensor cores work for the other.
+        const int m = warp - S::SOFT;
         constexpr uint32_t DS = tc::product_desc(Pair<T>::TYPE, S::W, false), DO = tc::product_desc(Pair<T>::TYPE, 64 * S::WIDE, true);
         const uint32_t q_at = smem_u32(base), slots = smem_u32(base + S::off_slots);
-        uint32_t n = 0, n_seg = 0, n_tile = 0, n_p[2] = {0, 0}, n_o[2] = {0, 0};         // n: the next slot to read
+        uint32_t n = 0, n_seg = 0, n_tile = 0, n_mine = 0, n_o = 0;    // next slot; segments and tiles of the run; own tiles, own segments
         // the copies to slots k .., of the run's tile i, are there; what threads stored, seen through the barrier, is put before the tensor cores
         const auto copied = [&](uint32_t k, uint32_t i) {
             for (int p = 0; p < S::STEP; ++p) wait(B, &B->full[(k + p) % S::SLOTS], ((k + p) / S::SLOTS) & 1);
             if (*(volatile uint32_t *)&B->plain[i & 7]) tc::publish_shared();
             tc::fence_after();
-        };
-        const auto is_copied = [&](uint32_t k, uint32_t i) {
-            bool all = true;
-            for (int p = 0; p < S::STEP; ++p) all &= mbar_test(&B->full[(k + p) % S::SLOTS], ((k + p) / S::SLOTS) & 1);
-            if (!__all_sync(0xffffffffu, all)) return false;
-            if (*(volatile uint32_t *)&B->plain[i & 7]) tc::publish_shared();
-            tc::fence_after();
-            return true;
         };
         // S of row block t for part h of a tile into columns `to`, from the keys in slots k ..; `bar`: where that is told
         const auto scores = [&](int t, int h, int to, uint32_t k, uint64_t *bar, bool release) {
@@ -760,64 +754,90 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             }
             __syncwarp();
         };
+        const auto let_go = [&](uint64_t *bar) {
+            if (tc::elected()) tc::commit(bar);
+            __syncwarp();
+        };
+        // (the slots' order: K0, V0, K1, V1, ...)
+        const auto keys_of = [&](int i) { return n + 2 * S::STEP * i; };
+        const auto values_of = [&](int i) { return n + 2 * S::STEP * i + S::STEP; };
         for (; hand->next(P, S::ROWS, 0); ++n_seg) {
-            const int steps = hand->seg[0].steps(), blocks = MT == 1 || hand->seg[0].rows <= 128 ? 1 : 2;
+            const int steps = hand->seg[0].steps();
+            const bool mine = MT == 1 || m * 128 < hand->seg[0].rows;
             wait(B, &B->q_full, n_seg & 1);
             if (!P.q_boxes) tc::publish_shared();
-            copied(n, n_tile);
-            if (MT == 1) {
-                // order of the slots: K0, K1, V0, K2, V1, ...: scores one tile ahead
-                scores(0, 0, (n_tile & 1) * 128, n, &B->s_full[n_tile & 1], true);
-                n += S::STEP;
-                for (int i = 0; i < steps; ++i, ++n_tile) {
-                    if (i + 1 < steps) {
-                        copied(n, n_tile + 1);
-                        scores(0, 0, (n_tile + 1 & 1) * 128, n, &B->s_full[n_tile + 1 & 1], true);
-                        n += S::STEP;
+            if (MT == 2 && !mine) {
+                for (int i = 0; i < steps; ++i) {
+                    copied(keys_of(i), n_tile + i);
+                    for (int p = 0; p < S::STEP; ++p) let_go(&B->empty[(keys_of(i) + p) % S::SLOTS]);
+                    copied(values_of(i), n_tile + i);
+                    for (int p = 0; p < S::STEP; ++p) let_go(&B->empty[(values_of(i) + p) % S::SLOTS]);
+                }
+                let_go(&B->q_empty);
+            } else if (MT == 2) {
+                // A tile in two parts of 64 keys: while the weights of one part are at work the other has its products, and its next scores right behind
+                // them.  (Products of a part: 8 with N = 64 for S, 4 with N = 128 for O.)
+                copied(n, n_tile);
+                for (int h = 0; h < 2; ++h) scores(m, h, (m * 2 + h) * 64, n, &B->s_full[m * 2 + h], h == 1);
+                if (steps == 1) let_go(&B->q_empty);
+#pragma unroll 1
+                for (int i = 0; i < steps; ++i, ++n_mine) {
+                    const bool more = i + 1 < steps;
+                    copied(values_of(i), n_tile + i);
+#pragma unroll 1
+                    for (int h = 0; h < 2; ++h) {
+                        const int buf = m * 2 + h;
+                        wait(B, &B->p_full[buf], n_mine & 1);
+                        if (i == 0 && h == 0 && n_o) wait(B, &B->o_empty[m], (n_o - 1) & 1);
+                        tc::fence_after();
+                        sums(m, h, buf * 64, values_of(i), i > 0 || h > 0, h == 1);
+                        if (!more) continue;
+                        if (h == 0) copied(keys_of(i + 1), n_tile + i + 1);
+                        scores(m, h, buf * 64, keys_of(i + 1), &B->s_full[buf], h == 1);
                     }
-                    if (i + 1 == max(1, steps - 1) && tc::elected()) tc::commit(&B->q_empty);
-                    copied(n, n_tile);
-                    const int buf = n_tile & 1;
-                    wait(B, &B->p_full[buf], (n_tile >> 1) & 1);
-                    if (i == 0 && n_seg) wait(B, &B->o_empty[0], (n_seg - 1) & 1);
+                    if (i + 2 == steps) let_go(&B->q_empty);
+                }
+                ++n_o;
+            } else if (S::TURNS) {
+                const int first = (int)((m - n_tile) & 1);
+                if (first >= steps) let_go(&B->q_empty);
+#pragma unroll 1
+                for (int i = first; i < steps; i += 2, ++n_mine) {
+                    copied(keys_of(i), n_tile + i);
+                    scores(0, 0, m * 128, keys_of(i), &B->s_full[m], true);
+                    if (i + 2 >= steps) let_go(&B->q_empty);
+                    copied(values_of(i), n_tile + i);
+                    wait(B, &B->p_full[m], n_mine & 1);
+                    if (i == first && n_seg) wait(B, &B->o_empty[0], (n_seg - 1) & 1);
                     tc::fence_after();
-                    sums(S::TURNS ? buf : 0, 0, buf * 128, n, i >= S::WG, true);
-                    n += S::STEP;
+                    sums(m, 0, m * 128, values_of(i), i > first, true);
                 }
             } else {
-                // order of the slots: K0, V0, K1, V1, ....  A tile in two parts of 64 keys: while a row block's weights of one part are at work, its other part
-                // has its products, and its next scores right behind them.  (Products of one part: 8 with N = 64 for S, 4 with N = 128 for O.)
-                for (int h = 0; h < 2; ++h)
-                    for (int t = 0; t < blocks; ++t) scores(t, h, (t * 2 + h) * 64, n, &B->s_full[t * 2 + h], h == 1 && t == blocks - 1);
-                n += S::STEP;
-                if (steps == 1 && tc::elected()) tc::commit(&B->q_empty);
+                // scores a tile ahead
+                copied(n, n_tile);
+                scores(0, 0, (n_tile & 1) * 128, n, &B->s_full[n_tile & 1], true);
+                if (steps == 1) let_go(&B->q_empty);
 #pragma unroll 1
-                for (int i = 0; i < steps; ++i, ++n_tile) {
-                    copied(n, n_tile);
-                    // the next keys' arrival is seen to before the weights are waited for, if it has come
-                    const bool more = i + 1 < steps;
-                    bool keys = more && is_copied(n + S::STEP, n_tile + 1);
-#pragma unroll 1
-                    for (int u = 0; u < 2 * blocks; ++u) {
-                        const int h = u / blocks, t = u % blocks, buf = t * 2 + h;
-                        const bool last = u == 2 * blocks - 1;
-                        wait(B, &B->p_full[buf], n_p[t] & 1);
-                        if (h == 1) ++n_p[t];
-                        if (i == 0 && h == 0) { if (n_o[t]) wait(B, &B->o_empty[t], (n_o[t] - 1) & 1); ++n_o[t]; }
-                        tc::fence_after();
-                        sums(t, h, buf * 64, n, i > 0 || h > 0, last);
-                        if (!more) continue;
-                        if (!keys) { copied(n + S::STEP, n_tile + 1); keys = true; }
-                        scores(t, h, buf * 64, n + S::STEP, &B->s_full[buf], last);
+                for (int i = 0; i < steps; ++i) {
+                    const uint32_t at = n_tile + i;
+                    if (i + 1 < steps) {
+                        copied(keys_of(i + 1), at + 1);
+                        scores(0, 0, (at + 1 & 1) * 128, keys_of(i + 1), &B->s_full[at + 1 & 1], true);
+                        if (i + 2 == steps) let_go(&B->q_empty);
                     }
-                    if (i + 2 == steps && tc::elected()) tc::commit(&B->q_empty);
-                    n += more ? 2 * S::STEP : S::STEP;
+                    copied(values_of(i), at);
+                    wait(B, &B->p_full[at & 1], (at >> 1) & 1);
+                    if (i == 0 && n_seg) wait(B, &B->o_empty[0], (n_seg - 1) & 1);
+                    tc::fence_after();
+                    sums(0, 0, (at & 1) * 128, values_of(i), i > 0, true);
                 }
             }
+            n_tile += steps;
+            n += 2 * S::STEP * steps;
         }
     } else {
         // ---------------------------------------------------------------- copies: a warp for 32 rows of every tile, each for itself
-        const int part = warp - S::SOFT - 1;
+        const int part = warp - S::SOFT - S::WG;
         constexpr int CH = D / 8;                                     // 16-byte chunks of a row
         const uint32_t slots = smem_u32(base + S::off_slots), q_at = smem_u32(base);
         uint32_t n = 0, n_seg = 0, n_tile = 0;                        // n: the next slot to fill
@@ -938,9 +958,9 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             tc::close_copies();
         };
         if (hand->next(P, S::ROWS, 0)) {
-            bool more = true, before_map = false;
+            bool more = true;
             int step = 0, in = 0;                                     // in: which of the segments in hand is gone through
-            Source ahead = source(hand->seg[0], hand->seg[0].tile(0)), before = ahead;
+            Source ahead = source(hand->seg[0], hand->seg[0].tile(0));
             while (more) {
                 const Segment &now = hand->seg[in];
                 const int at = step;
@@ -957,15 +977,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                 ++n_tile;
                 copy_rows(here, by_map, false);
                 if (at == 0) copy_q(now);
-                if (MT == 1) {
-                    // values a tile behind the keys
-                    if (at > 0) copy_rows(before, before_map, true);
-                    if (last) copy_rows(here, by_map, true);
-                    before = here;
-                    before_map = by_map;
-                } else {
-                    copy_rows(here, by_map, true);
-                }
+                copy_rows(here, by_map, true);
             }
         }
         tc::wait_copies<0>();
