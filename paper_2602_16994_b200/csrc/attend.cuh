@@ -89,22 +89,17 @@ __device__ __forceinline__ Tiles tiles_of(const Params &P, const Request &r, int
     }
     return t;
 }
-__device__ __forceinline__ long long tiles_of_request(const Params &P, int b, int block_rows)
+__device__ __forceinline__ int tiles_of_request(const Params &P, int b, int block_rows)
 {
     const Request r = request_of(P, b);
-    long long s = 0;
+    int s = 0;
     for (int m = 0; m * block_rows < r.rows; ++m) s += tiles_of(P, r, m, block_rows).count();
     return s * P.Hkv;
 }
 struct Cuts {                                  // runs of equal length, the first `more` of them longer by one
-    long long all, each;
-    int more;
-    __device__ __forceinline__ Cuts(long long all_, int ctas) : all(all_)
-    {
-        each = all_ <= 0xffffffffll ? (long long)((uint32_t)all_ / (uint32_t)ctas) : all_ / ctas;
-        more = (int)(all_ - each * ctas);
-    }
-    __device__ __forceinline__ long long start(int c) const { return each * c + min(c, more); }
+    int all, each, more;
+    __device__ __forceinline__ Cuts(int all_, int ctas) : all(all_), each((int)((unsigned)all_ / (unsigned)ctas)) { more = all - each * ctas; }
+    __device__ __forceinline__ int start(int c) const { return each * c + min(c, more); }
 };
 
 // A place in the order of all tiles: request, block of rows, key head, tile.
@@ -112,30 +107,30 @@ struct Place {
     int b, m, h, i;
 };
 // All threads of the CTA: the number of tiles; in found[], the request that the start of run `c` falls into and the tiles ahead of it.
-__device__ __forceinline__ Cuts find_request(const Params &P, int block_rows, int c, long long *sums, long long *found, int tid, int threads)
+__device__ __forceinline__ Cuts find_request(const Params &P, int block_rows, int c, int *sums, int *found, int tid, int threads)
 {
     const int per = (P.B + threads - 1) / threads, b0 = min(P.B, tid * per), b1 = min(P.B, b0 + per);
-    long long mine = 0;
+    int mine = 0;
     for (int b = b0; b < b1; ++b) mine += tiles_of_request(P, b, block_rows);
     const int lane = tid & 31, warp = tid >> 5, warps = threads >> 5;
-    long long incl = mine;
+    int incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const long long t = __shfl_up_sync(0xffffffffu, incl, o);
+        const int t = __shfl_up_sync(0xffffffffu, incl, o);
         if (lane >= o) incl += t;
     }
     if (lane == 31) sums[warp] = incl;
     __syncthreads();
-    long long ahead = incl - mine, all = 0;
+    int ahead = incl - mine, all = 0;
     for (int w = 0; w < warps; ++w) {
         if (w < warp) ahead += sums[w];
         all += sums[w];
     }
     const Cuts cuts(all, P.ctas);
-    const long long target = cuts.start(c);
+    const int target = cuts.start(c);
     if (target >= ahead && target < ahead + mine) {
         for (int b = b0; b < b1; ++b) {
-            const long long t = tiles_of_request(P, b, block_rows);
+            const int t = per == 1 ? mine : tiles_of_request(P, b, block_rows);
             if (target < ahead + t) { found[0] = b; found[1] = ahead; break; }
             ahead += t;
         }
@@ -156,7 +151,7 @@ struct Segment {
 };
 struct Run {
     Place at;
-    long long left;
+    int left;
     bool first;
 };
 // The next segment of a run; false at its end.  (Once in the code: every role of the kernel takes its segments here, and what runs once
@@ -172,7 +167,7 @@ __device__ __noinline__ bool next_segment(const Params &P, int block_rows, Run *
         ++at.b; at.m = 0;
     }
     const Tiles t = tiles_of(P, r, at.m, block_rows);
-    const int count = t.count(), end = (int)min((long long)count, at.i + run->left);
+    const int count = t.count(), end = min(count, at.i + run->left);
     s->b = at.b; s->m = at.m; s->h = at.h; s->begin = at.i; s->end = end;
     s->whole = at.i == 0 && end == count;
     s->head = run->first;
@@ -201,18 +196,18 @@ struct __align__(16) Hand {
     }
 };
 // the place `skip` tiles into request b
-__device__ __forceinline__ Place place_in(const Params &P, int b, long long skip, int block_rows)
+__device__ __forceinline__ Place place_in(const Params &P, int b, int skip, int block_rows)
 {
     const Request r = request_of(P, b);
     Place p = {b, 0, 0, 0};
     for (;; ++p.m) {
         const int count = tiles_of(P, r, p.m, block_rows).count();
-        if (skip < (long long)count * P.Hkv) {
-            p.h = skip <= 0xffffffffll ? (int)((uint32_t)skip / (uint32_t)count) : (int)(skip / count);
-            p.i = (int)(skip - (long long)p.h * count);
+        if (skip < count * P.Hkv) {
+            p.h = (int)((unsigned)skip / (unsigned)count);
+            p.i = skip - p.h * count;
             return p;
         }
-        skip -= (long long)count * P.Hkv;
+        skip -= count * P.Hkv;
     }
 }
 
@@ -302,7 +297,7 @@ struct Bars {
     int dead, poison;
     uint32_t hidden[8][4];                     // keys of a tile on bad blocks, by the tile's number in the CTA's run % 8
     uint32_t plain[8];                         // a byte per warp that copies: whether it stored (part of) the tile by itself
-    long long found[2], sums[16];
+    int found[2], sums[16];
 };
 static_assert(sizeof(Bars) <= 1024, "the area behind the buffers");
 
@@ -534,7 +529,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
     if (lane == 0) {
         hand->run.left = cuts.start(c + 1) - cuts.start(c);
         hand->run.first = true;
-        if (hand->run.left > 0) hand->run.at = place_in(P, (int)B->found[0], cuts.start(c) - B->found[1], S::ROWS);
+        if (hand->run.left > 0) hand->run.at = place_in(P, B->found[0], cuts.start(c) - B->found[1], S::ROWS);
     }
     tc::fence_before();
     __syncthreads();
@@ -993,18 +988,17 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
 }
 
 // ---- joining ------------------------------------------------------------------------------------------------------------------
-// The first P.ctas * groups CTAs: (start of run j + 1, 32 rows).  Where that start lies inside a unit and is the first to, the unit's
-// parts are put together: out = sum 2^(ref_c - ref) O_c / sum 2^(ref_c - ref) l_c.  The others: a request each, its status (while the
-// attention still runs: that reads inputs alone) and zeros for a bad tree.
-constexpr int JOIN_NT = 256, CTAS_MAX = 160;
+// The first P.ctas * groups CTAs: (start of run j + 1, JOIN_ROWS rows).  Where that start lies inside a unit and is the first to, the unit's
+// parts are put together, in order: out = sum 2^(ref_c - ref) O_c / sum 2^(ref_c - ref) l_c.  The others: a request each, its status and
+// zeros for a bad tree.  Few threads, registers and next to no shared memory, so that a CTA finds room beside one of the attention's and
+// has found its unit, or checked its request (from inputs alone), when the attention ends.
+constexpr int JOIN_NT = 128, JOIN_ROWS = 8, CTAS_MAX = 160;
 
 template <typename T, typename S> __global__ void __launch_bounds__(JOIN_NT) spec_join_kernel(const __grid_constant__ Params P)
 {
     constexpr int D = S::D;
-    constexpr int WARPS = JOIN_NT / 32;
-    __shared__ float share[CTAS_MAX][32], sum_of[CTAS_MAX][32], inverse[32];
-    __shared__ long long sums[WARPS], found[2];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, groups = P.groups;
+    __shared__ int sums[JOIN_NT / 32], found[2];
+    const int tid = threadIdx.x, groups = P.groups;
     grid_launch_dependents();                  // (the next kernel waits for this one by itself, and this one for the attention)
     if ((int)blockIdx.x >= P.ctas * groups) {
         const int b = blockIdx.x - P.ctas * groups;
@@ -1017,10 +1011,11 @@ template <typename T, typename S> __global__ void __launch_bounds__(JOIN_NT) spe
         }
         // columns of the table that hold a key that some node sees
         const long long keys = n ? (long long)len + n : 0, since = P.window ? max(0ll, (long long)len - P.window + 1) : 0;
-        const long long sinks = min((long long)P.sinks, (long long)len), cols = (keys + P.block - 1) / P.block;
-        for (long long col = tid; col < cols; col += JOIN_NT) {
-            const long long a = col * P.block, e = a + P.block;
-            if (e > since || a < sinks) page |= block_in(P, b, (int)col) < 0;
+        const long long sinks = min((long long)P.sinks, (long long)len);
+        const int cols = (int)((keys + P.block - 1) / P.block);
+        for (int col = tid; col < cols; col += JOIN_NT) {
+            const long long a = (long long)col * P.block, e = a + P.block;
+            if (e > since || a < sinks) page |= block_in(P, b, col) < 0;
         }
         bad = __syncthreads_or(bad) != 0;
         page = __syncthreads_or(page) != 0;
@@ -1039,84 +1034,65 @@ template <typename T, typename S> __global__ void __launch_bounds__(JOIN_NT) spe
         }
         return;
     }
-    const int j = blockIdx.x / groups, group = blockIdx.x % groups;
+    const int j = blockIdx.x / groups, row0 = blockIdx.x % groups * JOIN_ROWS;
     if (tid == 0) found[0] = -1;
     __syncthreads();
     const Cuts cuts = find_request(P, S::ROWS, j + 1, sums, found, tid, JOIN_NT);
-    const long long cut = cuts.start(j + 1);
-    if (j + 1 < P.ctas && found[0] >= 0) {
-        const int b = (int)found[0];
-        const Place at = place_in(P, b, cut - found[1], S::ROWS);
+    const int cut = cuts.start(j + 1), b = found[0];
+    bool joins = j + 1 < P.ctas && b >= 0;
+    Place at = {0, 0, 0, 0};
+    int rows = 0, last = j;
+    if (joins) {
+        at = place_in(P, b, cut - found[1], S::ROWS);
         const Request r = request_of(P, b);
-        const long long begin = cut - at.i, end = begin + tiles_of(P, r, at.m, S::ROWS).count();
-        const int rows = min(min(r.rows - at.m * S::ROWS, S::ROWS) - group * 32, 32), row0 = group * 32;
-        if (at.i > 0 && cuts.start(j) <= begin && rows > 0) {
-            // CTAs j .. last have a part each (the first `last` whose run starts before the unit's end; a cut inside the unit means that
-            // no run is empty but where there are fewer tiles than CTAs, and then the empty ones come last)
-            if (tid == 0) found[0] = j;
-            __syncthreads();
-            for (int c = j + 1 + tid; c < P.ctas; c += JOIN_NT)
-                if (cuts.start(c) < end && cuts.start(c + 1) >= end) found[0] = c;
-            __syncthreads();
-            const int last = (int)found[0];
-            // the first one's run may start before the unit
-            const auto slot = [&](int c) { return 2 * c + (c == j && cuts.start(j) < begin ? 1 : 0); };
-            grid_dependency_wait();
-            for (int i = tid; i < (last + 1 - j) * rows; i += JOIN_NT) {
-                const int c = j + i / rows, row = i % rows;
-                const float2 x = __ldcg(&P.ml[(long long)slot(c) * S::ROWS + row0 + row]);
-                share[c][row] = x.x;
-                sum_of[c][row] = x.y;
-            }
-            __syncthreads();
-            // a warp per row: the largest reference, the parts' weights, the sum
-            for (int row = warp; row < rows; row += WARPS) {
-                float ref = -CUDART_INF_F, l = 0.f;
-                for (int c = j + lane; c <= last; c += 32) ref = fmaxf(ref, share[c][row]);
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) ref = fmaxf(ref, __shfl_xor_sync(0xffffffffu, ref, o));
-                for (int c = j + lane; c <= last; c += 32) {
-                    // (a part that saw nothing counts for nothing, whatever the others' reference)
-                    const float w = share[c][row] == -CUDART_INF_F ? 0.f : ex2_approx(share[c][row] - ref);
-                    share[c][row] = w;
-                    if (w != 0.f) l = fmaf(w, sum_of[c][row], l);
-                }
-                l = warp_sum(l);
-                if (lane == 0) {
-                    inverse[row] = l == 0.f ? 0.f : 1.f / l;
-                    if (P.lse) {
-                        const int q = at.m * S::ROWS + row0 + row;
-                        P.lse[((long long)b * P.tree.N + q / P.G) * P.Hq + at.h * P.G + q % P.G] =
-                            l == 0.f ? -CUDART_INF_F : (ref + log2f(l)) * LN2;
-                    }
-                }
-            }
-            __syncthreads();
-            // a thread per four entries of a row, parts in order, eight loads under way
-            for (int i = tid; i < rows * (D / 4); i += JOIN_NT) {
-                const int row = i % rows, ch = i / rows;
-                const float4 *part = (const float4 *)P.part + (long long)ch * S::ROWS + row0 + row;
-                constexpr long long STEP = (long long)(D / 4) * S::ROWS;
-                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-                for (int c0 = j; c0 <= last; c0 += 8) {
-                    float4 x[8];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) x[k] = __ldcg(part + slot(min(c0 + k, last)) * STEP);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const float w = c0 + k <= last ? share[c0 + k][row] : 0.f;
-                        if (w != 0.f) { o.x = fmaf(w, x[k].x, o.x); o.y = fmaf(w, x[k].y, o.y); o.z = fmaf(w, x[k].z, o.z); o.w = fmaf(w, x[k].w, o.w); }
-                    }
-                }
-                const int q = at.m * S::ROWS + row0 + row;
-                const float inv = inverse[row];
-                T *to = (T *)P.out + b * P.out_stride[0] + q / P.G * P.out_stride[1] + (at.h * P.G + q % P.G) * P.out_stride[2] + ch * 4;
-                *(uint2 *)to = make_uint2(Pair<T>::pack(o.x * inv, o.y * inv), Pair<T>::pack(o.z * inv, o.w * inv));
-            }
-            return;
-        }
+        const int begin = cut - at.i, end = begin + tiles_of(P, r, at.m, S::ROWS).count();
+        rows = min(min(r.rows - at.m * S::ROWS, S::ROWS) - row0, JOIN_ROWS);
+        joins = at.i > 0 && cuts.start(j) <= begin && rows > 0;
+        // CTAs j .. last have a part each: the first one's run may start before the unit
+        if (joins) while (last + 1 < P.ctas && cuts.start(last + 1) < end && cuts.start(last + 1) < cuts.start(last + 2)) ++last;
+        if (joins && cuts.start(j) < begin) at.i = 1;          // (its part is its second)
+        else at.i = 0;
     }
     grid_dependency_wait();
+    if (!joins) return;
+    // a thread per four entries of a row, eight loads under way
+    for (int i = tid; i < rows * (D / 4); i += JOIN_NT) {
+        const int row = row0 + i % rows, ch = i / rows;
+        const auto slot = [&](int c) { return (long long)(2 * c + (c == j ? at.i : 0)); };
+        float ref = -CUDART_INF_F, l = 0.f;
+        for (int c0 = j; c0 <= last; c0 += 8) {
+            float x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = __ldcg(&P.ml[slot(min(c0 + k, last)) * S::ROWS + row].x);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) ref = fmaxf(ref, x[k]);
+        }
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int c0 = j; c0 <= last; c0 += 4) {
+            float4 x[4];
+            float2 m[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const long long s = slot(min(c0 + k, last));
+                m[k] = __ldcg(&P.ml[s * S::ROWS + row]);
+                x[k] = __ldcg((const float4 *)P.part + (s * (D / 4) + ch) * S::ROWS + row);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                // (a part that saw nothing counts for nothing, whatever the others' reference)
+                const float w = c0 + k > last || m[k].x == -CUDART_INF_F ? 0.f : ex2_approx(m[k].x - ref);
+                if (w != 0.f) {
+                    l = fmaf(w, m[k].y, l);
+                    o.x = fmaf(w, x[k].x, o.x); o.y = fmaf(w, x[k].y, o.y); o.z = fmaf(w, x[k].z, o.z); o.w = fmaf(w, x[k].w, o.w);
+                }
+            }
+        }
+        const int q = at.m * S::ROWS + row, node = node_of(P, q), head = at.h * P.G + q - node * P.G;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        T *to = (T *)P.out + b * P.out_stride[0] + node * P.out_stride[1] + head * P.out_stride[2] + ch * 4;
+        *(uint2 *)to = make_uint2(Pair<T>::pack(o.x * inv, o.y * inv), Pair<T>::pack(o.z * inv, o.w * inv));
+        if (P.lse && ch == 0) P.lse[((long long)b * P.tree.N + node) * P.Hq + head] = l == 0.f ? -CUDART_INF_F : (ref + log2f(l)) * LN2;
+    }
 }
 
 }  // namespace attend

@@ -202,6 +202,9 @@ static int attention_check(const SpecAttention *a)
     if (a->dtype != SPEC_BF16 && a->dtype != SPEC_F16) return SPEC_ERR_DTYPE;
     if (!(a->scale >= 0.f && a->scale <= 3.4e38f) || a->window < 0 || a->sinks < 0) return SPEC_ERR_PARAM;
     if (a->D != 64 && a->D != 128 && a->D != 256) return SPEC_ERR_UNSUPPORTED;
+    // (tiles are counted in 32 bits)
+    const int64_t blocks = ((int64_t)a->N * (a->Hq / a->Hkv) + 127) / 128, keys = std::min<int64_t>((int64_t)a->table_width * a->block_size, 0x7FFFFFFF) + a->N;
+    if ((double)a->B * a->Hkv * (double)blocks * (double)(keys / attend::KT + 2) > 2.0e9) return SPEC_ERR_UNSUPPORTED;
     int64_t all = 0;
     for (int j = 0; j < 3; ++j) all |= a->q_stride[j] | a->k_cache_stride[j] | a->v_cache_stride[j] | a->out_stride[j];
     if (all % 8 || !aligned(a->q, 16) || !aligned(a->k_cache, 16) || !aligned(a->v_cache, 16) || !aligned(a->out, 16))
@@ -274,7 +277,7 @@ int32_t spec_tree_attention(const SpecAttention *a, void *ws, int64_t ws_bytes, 
     const auto go = [&](auto shape, auto attend_kernel, auto join_kernel) -> int {
         using S = decltype(shape);
         const int smem = S::total + 1024;
-        p.groups = ((int)std::min<int64_t>(S::ROWS, (int64_t)p.tree.N * p.G) + 31) / 32;
+        p.groups = ((int)std::min<int64_t>(S::ROWS, (int64_t)p.tree.N * p.G) + attend::JOIN_ROWS - 1) / attend::JOIN_ROWS;
         int e = prepare(attend_kernel, smem, false);
         if (e) return e;
         e = launch(attend_kernel, dim3(ctas), S::NT, smem, 0, st, p);
