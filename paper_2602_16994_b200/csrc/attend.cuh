@@ -56,6 +56,9 @@ struct Params {
 };
 
 // ---- the schedule -------------------------------------------------------------------------------------------------------------
+// A unit's length, in tiles, is its tiles and START: what its first segment costs beside them (queries, the tree's tile, results).  A cut in those first
+// START goes to the unit's beginning: no run ends with the first tile or two of a unit.
+constexpr int START = 2;
 // Tiles of a block of rows: [0, sink) and [from, end) of the tiles of its keys.
 struct Tiles {
     int sink, from, end;
@@ -93,7 +96,7 @@ __device__ __forceinline__ int tiles_of_request(const Params &P, int b, int bloc
 {
     const Request r = request_of(P, b);
     int s = 0;
-    for (int m = 0; m * block_rows < r.rows; ++m) s += tiles_of(P, r, m, block_rows).count();
+    for (int m = 0; m * block_rows < r.rows; ++m) s += tiles_of(P, r, m, block_rows).count() + START;
     return s * P.Hkv;
 }
 struct Cuts {                                  // runs of equal length, the first `more` of them longer by one
@@ -102,11 +105,12 @@ struct Cuts {                                  // runs of equal length, the firs
     __device__ __forceinline__ int start(int c) const { return each * c + min(c, more); }
 };
 
-// A place in the order of all tiles: request, block of rows, key head, tile.
+// A place in the order of all units: request, block of rows, key head, and the way into the unit (START, then its tiles).
 struct Place {
     int b, m, h, i;
+    __device__ __forceinline__ int tile() const { return max(0, i - START); }
 };
-// All threads of the CTA: the number of tiles; in found[], the request that the start of run `c` falls into and the tiles ahead of it.
+// All threads of the CTA: the cuts; in found[], the request that the start of run `c` falls into and the length of all ahead of it.
 __device__ __forceinline__ Cuts find_request(const Params &P, int block_rows, int c, int *sums, int *found, int tid, int threads)
 {
     const int per = (P.B + threads - 1) / threads, b0 = min(P.B, tid * per), b1 = min(P.B, b0 + per);
@@ -162,19 +166,21 @@ __device__ __noinline__ bool next_segment(const Params &P, int block_rows, Run *
     Place at = run->at;
     Request r;
     for (;;) {
+        if (at.b >= P.B) return false;
         r = request_of(P, at.b);
         if (at.m * block_rows < r.rows) break;
         ++at.b; at.m = 0;
     }
     const Tiles t = tiles_of(P, r, at.m, block_rows);
-    const int count = t.count(), end = min(count, at.i + run->left);
-    s->b = at.b; s->m = at.m; s->h = at.h; s->begin = at.i; s->end = end;
-    s->whole = at.i == 0 && end == count;
+    const int count = t.count(), upto = min(count + START, at.i + run->left), end = max(0, upto - START);
+    run->left -= upto - at.i;
+    if (end == 0) return false;                // (the run ends before the unit's first tile)
+    s->b = at.b; s->m = at.m; s->h = at.h; s->begin = at.tile(); s->end = end;
+    s->whole = s->begin == 0 && end == count;
     s->head = run->first;
     s->r = r;
     s->t = t;
     s->rows = min(r.rows - at.m * block_rows, block_rows);
-    run->left -= end - at.i;
     run->first = false;
     at.i = 0;
     if (++at.h == P.Hkv) { at.h = 0; ++at.m; }
@@ -195,20 +201,21 @@ struct __align__(16) Hand {
         return more != 0;
     }
 };
-// the place `skip` tiles into request b
+// the place `skip` into request b
 __device__ __forceinline__ Place place_in(const Params &P, int b, int skip, int block_rows)
 {
     const Request r = request_of(P, b);
     Place p = {b, 0, 0, 0};
-    for (;; ++p.m) {
-        const int count = tiles_of(P, r, p.m, block_rows).count();
-        if (skip < count * P.Hkv) {
-            p.h = (int)((unsigned)skip / (unsigned)count);
-            p.i = skip - p.h * count;
+    for (; p.m * block_rows < r.rows; ++p.m) {
+        const int length = tiles_of(P, r, p.m, block_rows).count() + START;
+        if (skip < length * P.Hkv) {
+            p.h = (int)((unsigned)skip / (unsigned)length);
+            p.i = skip - p.h * length;
             return p;
         }
-        skip -= count * P.Hkv;
+        skip -= length * P.Hkv;
     }
+    return p;                                  // (not reached: the request has that many tiles)
 }
 
 // ---- what a row sees ----------------------------------------------------------------------------------------------------------
@@ -524,7 +531,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         mbar_fence_init();
     }
     grid_dependency_wait();
-    grid_launch_dependents();                  // (the joining kernel's CTAs may be placed as this one's leave; it waits by itself)
+    grid_launch_dependents();                  // (the joining kernel's CTAs may be placed beside this one's; they wait by themselves)
     const Cuts cuts = find_request(P, S::ROWS, c, B->sums, B->found, tid, S::NT);
     if (lane == 0) {
         hand->run.left = cuts.start(c + 1) - cuts.start(c);
@@ -994,7 +1001,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
 // has found its unit, or checked its request (from inputs alone), when the attention ends.
 constexpr int JOIN_NT = 128, JOIN_ROWS = 8, CTAS_MAX = 160;
 
-template <typename T, typename S> __global__ void __launch_bounds__(JOIN_NT) spec_join_kernel(const __grid_constant__ Params P)
+template <typename T, typename S> __global__ void __launch_bounds__(JOIN_NT, 8) spec_join_kernel(const __grid_constant__ Params P)
 {
     constexpr int D = S::D;
     __shared__ int sums[JOIN_NT / 32], found[2];
@@ -1045,9 +1052,9 @@ template <typename T, typename S> __global__ void __launch_bounds__(JOIN_NT) spe
     if (joins) {
         at = place_in(P, b, cut - found[1], S::ROWS);
         const Request r = request_of(P, b);
-        const int begin = cut - at.i, end = begin + tiles_of(P, r, at.m, S::ROWS).count();
+        const int begin = cut - at.i, end = begin + START + tiles_of(P, r, at.m, S::ROWS).count();
         rows = min(min(r.rows - at.m * S::ROWS, S::ROWS) - row0, JOIN_ROWS);
-        joins = at.i > 0 && cuts.start(j) <= begin && rows > 0;
+        joins = at.tile() > 0 && cuts.start(j) <= begin + START && rows > 0;
         // CTAs j .. last have a part each: the first one's run may start before the unit
         if (joins) while (last + 1 < P.ctas && cuts.start(last + 1) < end && cuts.start(last + 1) < cuts.start(last + 2)) ++last;
         if (joins && cuts.start(j) < begin) at.i = 1;          // (its part is its second)
@@ -1055,30 +1062,28 @@ template <typename T, typename S> __global__ void __launch_bounds__(JOIN_NT) spe
     }
     grid_dependency_wait();
     if (!joins) return;
-    // a thread per four entries of a row, eight loads under way
+    // a thread per four entries of a row, eight parts' loads under way
     for (int i = tid; i < rows * (D / 4); i += JOIN_NT) {
         const int row = row0 + i % rows, ch = i / rows;
-        const auto slot = [&](int c) { return (long long)(2 * c + (c == j ? at.i : 0)); };
         float ref = -CUDART_INF_F, l = 0.f;
-        for (int c0 = j; c0 <= last; c0 += 8) {
-            float x[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = __ldcg(&P.ml[slot(min(c0 + k, last)) * S::ROWS + row].x);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) ref = fmaxf(ref, x[k]);
-        }
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int c0 = j; c0 <= last; c0 += 4) {
-            float4 x[4];
-            float2 m[4];
+        for (int c0 = j; c0 <= last; c0 += 8) {
+            float4 x[8];
+            float2 m[8];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const long long s = slot(min(c0 + k, last));
-                m[k] = __ldcg(&P.ml[s * S::ROWS + row]);
-                x[k] = __ldcg((const float4 *)P.part + (s * (D / 4) + ch) * S::ROWS + row);
+            for (int k = 0; k < 8; ++k) {
+                const int c = min(c0 + k, last), slot = 2 * c + (c == j ? at.i : 0);
+                m[k] = __ldcg(&P.ml[slot * S::ROWS + row]);
+                x[k] = __ldcg((const float4 *)P.part + (slot * (D / 4) + ch) * S::ROWS + row);
             }
+            float top = ref;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < 8; ++k) top = fmaxf(top, m[k].x);
+            const float f = ref == -CUDART_INF_F ? 0.f : ex2_approx(ref - top);
+            ref = top;
+            l *= f; o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
                 // (a part that saw nothing counts for nothing, whatever the others' reference)
                 const float w = c0 + k > last || m[k].x == -CUDART_INF_F ? 0.f : ex2_approx(m[k].x - ref);
                 if (w != 0.f) {

@@ -51,7 +51,9 @@ int launch(void (*kernel)(P), dim3 grid, int threads, int smem, int C, cudaStrea
     return SPEC_OK;
 }
 
-// Attributes of a kernel that its launch needs, set once per device: dynamic shared memory, clusters above 8 CTAs.
+// Attributes of a kernel that its launch needs, set once per device: dynamic shared memory, clusters above 8 CTAs, and as much of an SM's L1 as can be as
+// shared memory, for all kernels alike: CTAs of one that starts early find room beside those of the one before, and no SM is emptied
+// to be divided anew between them.
 std::mutex g_mutex;
 template <typename K> int prepare(K kernel, int smem, bool big_clusters)
 {
@@ -71,6 +73,8 @@ template <typename K> int prepare(K kernel, int smem, bool big_clusters)
         cudaGetLastError();
         return SPEC_ERR_CUDA;
     }
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess)
+        cudaGetLastError();
     if (used < 256) cache[used++] = Entry{(const void *)kernel, dev};
     return SPEC_OK;
 }
@@ -151,7 +155,8 @@ int32_t spec_cache_slots(const SpecSlots *a, void *stream)
     p.table = a->block_table; p.table_stride = a->table_stride;
     p.owned = a->owned; p.ring = a->free_blocks; p.range = a->free_range;
     p.slots = a->slots; p.positions = a->positions; p.owned_out = a->owned_out; p.range_out = a->free_range_out; p.status = a->status;
-    return launch(slots::spec_slots_kernel, dim3((a->B + slots::WARPS - 1) / slots::WARPS), slots::NT, slots::WARPS * a->N * 4, 0,
+    const int rc = prepare(slots::spec_slots_kernel, 0, false);
+    return rc ? rc : launch(slots::spec_slots_kernel, dim3((a->B + slots::WARPS - 1) / slots::WARPS), slots::NT, slots::WARPS * a->N * 4, 0,
                   (cudaStream_t)stream, p);
 }
 
@@ -186,7 +191,10 @@ int32_t spec_norm_rope_cache(const SpecNormRope *a, void *stream)
         all |= (a->k_cache_stride[j] | a->v_cache_stride[j]) * esz;
     }
     const bool vec = (all & 15) == 0;
-    const auto go = [&](auto kernel) { return launch(kernel, dim3(a->T), rope::NT, 0, 0, (cudaStream_t)stream, p); };
+    const auto go = [&](auto kernel) {
+        const int rc = prepare(kernel, 0, false);
+        return rc ? rc : launch(kernel, dim3(a->T), rope::NT, 0, 0, (cudaStream_t)stream, p);
+    };
     if (a->dtype == SPEC_F32) return vec ? go(rope::spec_rope_kernel<float, true>) : go(rope::spec_rope_kernel<float, false>);
     if (a->dtype == SPEC_F16) return vec ? go(rope::spec_rope_kernel<__half, true>) : go(rope::spec_rope_kernel<__half, false>);
     return vec ? go(rope::spec_rope_kernel<__nv_bfloat16, true>) : go(rope::spec_rope_kernel<__nv_bfloat16, false>);
@@ -279,6 +287,7 @@ int32_t spec_tree_attention(const SpecAttention *a, void *ws, int64_t ws_bytes, 
         const int smem = S::total + 1024;
         p.groups = ((int)std::min<int64_t>(S::ROWS, (int64_t)p.tree.N * p.G) + attend::JOIN_ROWS - 1) / attend::JOIN_ROWS;
         int e = prepare(attend_kernel, smem, false);
+        if (!e) e = prepare(join_kernel, 0, false);
         if (e) return e;
         e = launch(attend_kernel, dim3(ctas), S::NT, smem, 0, st, p);
         return e ? e : launch(join_kernel, dim3((unsigned)(ctas * p.groups + a->B)), attend::JOIN_NT, 0, 0, st, p);
@@ -314,10 +323,13 @@ int32_t spec_cache_commit(const SpecCommit *a, void *stream)
     p.words = a->row_bytes / unit;
     p.per = (int)std::max<int64_t>(1, commit::NT / p.words);
     const dim3 grid((a->caches + p.per - 1) / p.per, a->B);
-    const cudaStream_t st = (cudaStream_t)stream;
-    return unit == 16  ? launch(commit::spec_commit_kernel<uint4>, grid, commit::NT, 0, 0, st, p)
-           : unit == 4 ? launch(commit::spec_commit_kernel<uint32_t>, grid, commit::NT, 0, 0, st, p)
-                       : launch(commit::spec_commit_kernel<unsigned char>, grid, commit::NT, 0, 0, st, p);
+    const auto go = [&](auto kernel) {
+        const int rc = prepare(kernel, 0, false);
+        return rc ? rc : launch(kernel, grid, commit::NT, 0, 0, (cudaStream_t)stream, p);
+    };
+    return unit == 16  ? go(commit::spec_commit_kernel<uint4>)
+           : unit == 4 ? go(commit::spec_commit_kernel<uint32_t>)
+                       : go(commit::spec_commit_kernel<unsigned char>);
 }
 
 int32_t spec_verify_probs(const SpecChains *a, void *stream)
