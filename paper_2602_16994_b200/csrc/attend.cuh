@@ -53,6 +53,7 @@ struct Params {
     float *part;                               // [ctas][2][D / 4][rows][4] unfinished O
     float2 *ml;                                // [ctas][2][rows] reference and l
     int *late;                                 // [ctas] a wait ran out
+    int4 *joint;                               // [ctas] the unit whose first part this is: request, block, head; parts, slot and rows
 };
 
 // ---- the schedule -------------------------------------------------------------------------------------------------------------
@@ -191,12 +192,15 @@ __device__ __noinline__ bool next_segment(const Params &P, int block_rows, Run *
 struct __align__(16) Hand {
     Run run;
     Segment seg[2];
-    int more;
+    int more, segments;                        // (segments: how many there were)
     // all lanes of the warp; seg[i] is the next segment
     __device__ __forceinline__ bool next(const Params &P, int block_rows, int i)
     {
         __syncwarp();
-        if ((threadIdx.x & 31) == 0) more = next_segment(P, block_rows, &run, &seg[i]);
+        if ((threadIdx.x & 31) == 0) {
+            more = next_segment(P, block_rows, &run, &seg[i]);
+            segments += more;
+        }
         __syncwarp();
         return more != 0;
     }
@@ -536,6 +540,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
     if (lane == 0) {
         hand->run.left = cuts.start(c + 1) - cuts.start(c);
         hand->run.first = true;
+        hand->segments = 0;
         if (hand->run.left > 0) hand->run.at = place_in(P, B->found[0], cuts.start(c) - B->found[1], S::ROWS);
     }
     tc::fence_before();
@@ -990,21 +995,32 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
     if (warp == S::SOFT) {
         tc::fence_after();
         tc::tmem_free(tmem, 512);
-        if (lane == 0) P.late[c] = B->dead;
+        if (lane == 0) {
+            P.late[c] = B->dead;
+            // the first of a unit's parts tells what there is to join
+            const Segment &seg = hand->seg[0];
+            int4 joint = make_int4(0, 0, 0, 0);
+            if (hand->segments && seg.begin == 0 && !seg.whole) {
+                // (the unit's end, from what of it lies in this run)
+                const int end = cuts.start(c + 1) + seg.t.count() - seg.end;
+                int last = c + 1;
+                while (cuts.start(last + 1) < end) ++last;
+                joint = make_int4(seg.b, seg.m, seg.h, last + 1 - c | (seg.head ? 0 : 1 << 15) | seg.rows << 16);
+            }
+            P.joint[c] = joint;
+        }
     }
 }
 
 // ---- joining ------------------------------------------------------------------------------------------------------------------
-// The first P.ctas * groups CTAs: (start of run j + 1, JOIN_ROWS rows).  Where that start lies inside a unit and is the first to, the unit's
-// parts are put together, in order: out = sum 2^(ref_c - ref) O_c / sum 2^(ref_c - ref) l_c.  The others: a request each, its status and
-// zeros for a bad tree.  Few threads, registers and next to no shared memory, so that a CTA finds room beside one of the attention's and
-// has found its unit, or checked its request (from inputs alone), when the attention ends.
+// The first P.ctas * groups CTAs: (CTA of the attention, JOIN_ROWS rows).  Where that one had the first of a unit's parts, they are put together, in
+// order: out = sum 2^(ref_c - ref) O_c / sum 2^(ref_c - ref) l_c.  The others: a request each, its status (from inputs alone, while the
+// attention still runs) and zeros for a bad tree.
 constexpr int JOIN_NT = 128, JOIN_ROWS = 8, CTAS_MAX = 160;
 
 template <typename T, typename S> __global__ void __launch_bounds__(JOIN_NT, 8) spec_join_kernel(const __grid_constant__ Params P)
 {
     constexpr int D = S::D;
-    __shared__ int sums[JOIN_NT / 32], found[2];
     const int tid = threadIdx.x, groups = P.groups;
     grid_launch_dependents();                  // (the next kernel waits for this one by itself, and this one for the attention)
     if ((int)blockIdx.x >= P.ctas * groups) {
@@ -1042,26 +1058,11 @@ template <typename T, typename S> __global__ void __launch_bounds__(JOIN_NT, 8) 
         return;
     }
     const int j = blockIdx.x / groups, row0 = blockIdx.x % groups * JOIN_ROWS;
-    if (tid == 0) found[0] = -1;
-    __syncthreads();
-    const Cuts cuts = find_request(P, S::ROWS, j + 1, sums, found, tid, JOIN_NT);
-    const int cut = cuts.start(j + 1), b = found[0];
-    bool joins = j + 1 < P.ctas && b >= 0;
-    Place at = {0, 0, 0, 0};
-    int rows = 0, last = j;
-    if (joins) {
-        at = place_in(P, b, cut - found[1], S::ROWS);
-        const Request r = request_of(P, b);
-        const int begin = cut - at.i, end = begin + START + tiles_of(P, r, at.m, S::ROWS).count();
-        rows = min(min(r.rows - at.m * S::ROWS, S::ROWS) - row0, JOIN_ROWS);
-        joins = at.tile() > 0 && cuts.start(j) <= begin + START && rows > 0;
-        // CTAs j .. last have a part each: the first one's run may start before the unit
-        if (joins) while (last + 1 < P.ctas && cuts.start(last + 1) < end && cuts.start(last + 1) < cuts.start(last + 2)) ++last;
-        if (joins && cuts.start(j) < begin) at.i = 1;          // (its part is its second)
-        else at.i = 0;
-    }
     grid_dependency_wait();
-    if (!joins) return;
+    const int4 joint = __ldcg(P.joint + j);
+    const int b = joint.x, parts = joint.w & 0x7FFF, first = joint.w >> 15 & 1, rows = min((joint.w >> 16) - row0, JOIN_ROWS);
+    if (parts == 0 || rows <= 0) return;
+    const int last = j + parts - 1;
     // a thread per four entries of a row, eight parts' loads under way
     for (int i = tid; i < rows * (D / 4); i += JOIN_NT) {
         const int row = row0 + i % rows, ch = i / rows;
@@ -1072,7 +1073,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(JOIN_NT, 8) 
             float2 m[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const int c = min(c0 + k, last), slot = 2 * c + (c == j ? at.i : 0);
+                const int c = min(c0 + k, last), slot = 2 * c + (c == j ? first : 0);
                 m[k] = __ldcg(&P.ml[slot * S::ROWS + row]);
                 x[k] = __ldcg((const float4 *)P.part + (slot * (D / 4) + ch) * S::ROWS + row);
             }
@@ -1092,7 +1093,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(JOIN_NT, 8) 
                 }
             }
         }
-        const int q = at.m * S::ROWS + row, node = node_of(P, q), head = at.h * P.G + q - node * P.G;
+        const int q = joint.y * S::ROWS + row, node = node_of(P, q), head = joint.z * P.G + q - node * P.G;
         const float inv = l == 0.f ? 0.f : 1.f / l;
         T *to = (T *)P.out + b * P.out_stride[0] + node * P.out_stride[1] + head * P.out_stride[2] + ch * 4;
         *(uint2 *)to = make_uint2(Pair<T>::pack(o.x * inv, o.y * inv), Pair<T>::pack(o.z * inv, o.w * inv));

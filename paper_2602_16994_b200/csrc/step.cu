@@ -223,13 +223,14 @@ static int attention_check(const SpecAttention *a)
 // Two blocks of 128 rows share the loads of a tile where a request has more rows than one block.
 static bool two_blocks(const SpecAttention *a) { return a->D <= 128 && (int64_t)a->N * (a->Hq / a->Hkv) > 128; }
 
-struct AttentionLayout { int64_t part, ml, late, total; };
+struct AttentionLayout { int64_t part, ml, joint, late, total; };
 static AttentionLayout attention_layout(const SpecAttention *a, int ctas)
 {
     const int64_t rows = two_blocks(a) ? 256 : 128;
     AttentionLayout L = {};
     L.ml = (int64_t)ctas * 2 * rows * a->D * 4;
-    L.late = L.ml + (int64_t)ctas * 2 * rows * 8;
+    L.joint = L.ml + (int64_t)ctas * 2 * rows * 8;
+    L.late = L.joint + (int64_t)ctas * 16;
     L.total = L.late + ((int64_t)ctas * 4 + 255) / 256 * 256;
     return L;
 }
@@ -272,6 +273,7 @@ int32_t spec_tree_attention(const SpecAttention *a, void *ws, int64_t ws_bytes, 
     p.ctas = ctas;
     p.part = (float *)((unsigned char *)ws + L.part);
     p.ml = (float2 *)((unsigned char *)ws + L.ml);
+    p.joint = (int4 *)((unsigned char *)ws + L.joint);
     p.late = (int *)((unsigned char *)ws + L.late);
     const bool half = a->dtype == SPEC_F16;
     p.box = a->block_size % 8 ? 0 : a->block_size % 16 ? 8 : a->block_size % 32 ? 16 : 32;
