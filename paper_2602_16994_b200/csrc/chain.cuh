@@ -10,10 +10,10 @@ namespace cg = cooperative_groups;
 
 // A cluster per request, a slice of the vocabulary per CTA.  Every CTA finds the accepted drafts by itself (a lane per draft: the
 // chain is one round of dependent loads, whatever its length), then the cluster draws from the one row, or pair of rows, that the
-// chain stopped at: the sums of tiles of 128 weights stay in shared memory, the slices' sums are exchanged, and the CTA that the
+// chain stopped at: the sums of tiles of 512 weights stay in shared memory, the slices' sums are exchanged, and the CTA that the
 // target falls into finds the tile and reads it once more.  Weights, sums and comparisons are fp64: fp32 sums over 1e5 weights would move the
 // borders between tokens by more than the tokens' own masses.  The bytes of one row of p and of q per request bound the call.
-constexpr int NT = 256, WARPS = NT / 32, TILE = 128, TILES = 1024, CMAX = 16;
+constexpr int NT = 256, WARPS = NT / 32, TILE = 512, TILES = 1024, CMAX = 16;      // a tile: four loads of 128 entries by a warp
 
 struct Params {
     int B, V, SL, most;                 // SL: weights of a slice, a multiple of TILE
@@ -40,9 +40,6 @@ template <typename T> __device__ __forceinline__ float4 entries(const T *row, in
     return make_float4(t < end ? value(row + t) : 0.f, t + 1 < end ? value(row + t + 1) : 0.f, t + 2 < end ? value(row + t + 2) : 0.f,
                        t + 3 < end ? value(row + t + 3) : 0.f);
 }
-// max(v, 0), but NaN where v is NaN
-__device__ __forceinline__ double positive(double v) { return v <= 0.0 ? 0.0 : v; }
-
 // The rows that a draw reads: (p - q)+ where q is given, p without entry `hole` otherwise.
 template <typename T> struct Rows {
     const T *p, *q;
@@ -52,15 +49,22 @@ template <typename T> struct Rows {
     {
         a = entries(p, t, end, vec);
         b = q ? entries(q, t, end, vec) : make_float4(0.f, 0.f, 0.f, 0.f);
+        if (hole >= t && hole < t + 4) {
+            if (hole == t) a.x = 0.f;
+            if (hole == t + 1) a.y = 0.f;
+            if (hole == t + 2) a.z = 0.f;
+            if (hole == t + 3) a.w = 0.f;
+        }
     }
-    __device__ __forceinline__ void weights(int t, const float4 &a, const float4 &b, double w[4]) const
+    // (compared in fp32, where p > q means the same; NaN stays)
+    static __device__ __forceinline__ double weight(float p, float q)
     {
-        w[0] = positive((double)a.x - (double)b.x);
-        w[1] = positive((double)a.y - (double)b.y);
-        w[2] = positive((double)a.z - (double)b.z);
-        w[3] = positive((double)a.w - (double)b.w);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) if (t + k == hole) w[k] = 0.0;
+        const bool none = p <= q;
+        return (double)(none ? 0.f : p) - (double)(none ? 0.f : q);
+    }
+    static __device__ __forceinline__ double sum(const float4 &a, const float4 &b)
+    {
+        return (weight(a.x, b.x) + weight(a.y, b.y)) + (weight(a.z, b.z) + weight(a.w, b.w));
     }
 };
 
@@ -131,28 +135,15 @@ template <typename T> __global__ void __launch_bounds__(NT) spec_chain_kernel(co
         // (the second round: what was left of p is 0 everywhere, the draw is from p)
         for (int round = 0; round < 2; ++round) {
             rows.vec = (((uintptr_t)rows.p | (uintptr_t)rows.q) & (4 * sizeof(T) - 1)) == 0;
-            constexpr int AHEAD = 4;
-            for (int i0 = warp; i0 < tiles; i0 += WARPS * AHEAD) {
-                float4 x[AHEAD], y[AHEAD];
+            for (int i = warp; i < tiles; i += WARPS) {
+                const int t = t0 + i * TILE + lane * 4;
+                float4 x[4], y[4];
 #pragma unroll
-                for (int k = 0; k < AHEAD; ++k) rows.raw(t0 + (i0 + k * WARPS) * TILE + lane * 4, end, x[k], y[k]);
-                double s[AHEAD];
+                for (int k = 0; k < 4; ++k) rows.raw(t + k * 128, end, x[k], y[k]);
+                double s = (rows.sum(x[0], y[0]) + rows.sum(x[1], y[1])) + (rows.sum(x[2], y[2]) + rows.sum(x[3], y[3]));
 #pragma unroll
-                for (int k = 0; k < AHEAD; ++k) {
-                    double w[4];
-                    rows.weights(t0 + (i0 + k * WARPS) * TILE + lane * 4, x[k], y[k], w);
-                    s[k] = (w[0] + w[1]) + (w[2] + w[3]);
-                }
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) {
-#pragma unroll
-                    for (int k = 0; k < AHEAD; ++k) s[k] += __shfl_xor_sync(0xffffffffu, s[k], o);
-                }
-                if (lane < AHEAD) {
-                    const int i = i0 + lane * WARPS;
-                    const double sum = lane == 0 ? s[0] : lane == 1 ? s[1] : lane == 2 ? s[2] : s[3];
-                    if (i < tiles) tile[i] = sum;
-                }
+                for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                if (lane == 0) tile[i] = s;
             }
             __syncthreads();
             // a run of tiles per lane (of every warp alike: the slice's sum is needed by all)
@@ -194,21 +185,29 @@ template <typename T> __global__ void __launch_bounds__(NT) spec_chain_kernel(co
                     }
                     ti = __shfl_sync(0xffffffffu, ti, l < 0 ? 0 : l);
                     rest = __shfl_sync(0xffffffffu, rest, l < 0 ? 0 : l);
-                    const int at = t0 + ti * TILE + lane * 4;
-                    float4 x, y;
-                    double w[4];
-                    rows.raw(at, end, x, y);
-                    rows.weights(at, x, y, w);
-                    const int who = first_above((w[0] + w[1]) + (w[2] + w[3]), rest, tau3);
-                    int found = -1, last = -1;
-                    double run = 0.0;
+                    // the tile's quarters in order, then the lane's four entries.  Where rounding leaves none above the target, the last with weight
+                    int at = -1;
+                    for (int k = 0; k < TILE; k += 128) {
+                        const int t = t0 + ti * TILE + k + lane * 4;
+                        float4 x, y;
+                        rows.raw(t, end, x, y);
+                        const double w[4] = {rows.weight(x.x, y.x), rows.weight(x.y, y.y), rows.weight(x.z, y.z), rows.weight(x.w, y.w)};
+                        const double mine4 = (w[0] + w[1]) + (w[2] + w[3]), sum4 = warp_sum(mine4);
+                        const int who = first_above(mine4, rest, tau3);
+                        if (who < 0) continue;
+                        int found = -1, last = -1;
+                        double run = 0.0;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        run += w[k];
-                        if (w[k] > 0.0) last = k;
-                        if (found < 0 && w[k] > 0.0 && run > tau3) found = k;
+                        for (int j = 0; j < 4; ++j) {
+                            run += w[j];
+                            if (w[j] > 0.0) last = j;
+                            if (found < 0 && w[j] > 0.0 && run > tau3) found = j;
+                        }
+                        at = __shfl_sync(0xffffffffu, t + (found >= 0 ? found : last), who);
+                        if (__shfl_sync(0xffffffffu, tau3, who) != CUDART_INF) break;
+                        rest -= sum4;
                     }
-                    const int token = __shfl_sync(0xffffffffu, at + (found >= 0 ? found : last), who < 0 ? 0 : who);
+                    const int token = at;
                     for (int i = lane; i <= P.most; i += 32)
                         out[i] = i < len ? __ldg(P.token + first + i) : i == len ? token : -1;
                     if (lane == 0) { P.accept_len[b] = len; P.bonus[b] = token; P.status[b] = SPEC_DEV_OK; }

@@ -3,6 +3,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 
 namespace specv {
@@ -11,13 +13,14 @@ namespace rope {
 constexpr int NT = 256, WARPS = NT / 32, ROT_MAX = 256;
 
 struct Params {
-    int T, Hq, Hkv, D, rot, pairs, lanes;          // lanes: threads of a head's row, a power of two >= D / 8
-    int block;
+    int T, Hq, Hkv, D, rot, pairs, lane_shift;     // 1 << lane_shift threads to a head's row, a power of two >= D / 8
+    int block, block_shift;
+    unsigned block_mul;                            // slot / block = (umulhi(block_mul, slot) + slot) >> block_shift
     long long n_slots;
     const void *x[3];                              // q, k, v
     long long x_stride[3][2];
     const void *weight[2];
-    float eps;
+    float eps, inv_D;
     const float *inv_freq;
     const int *positions, *slots;
     void *q_out, *cache[2];
@@ -58,79 +61,155 @@ template <typename T, bool VEC> __device__ __forceinline__ void store8(T *p, con
     }
 }
 
-// A CTA per token: its angles once for all heads (the position times a frequency, in turns, reduced in fp64: fp32 would lose 1e-2 of
-// an angle at position 1e5), then a row per `lanes` threads, eight entries each.  Loads of the rows go out before the angles are
-// computed.  Bound by the bytes of the projections.
-template <typename T, bool VEC> __global__ void __launch_bounds__(NT) spec_rope_kernel(const Params P)
-{
-    __shared__ float2 turn[ROT_MAX / 2];
-    const int tid = threadIdx.x, t = blockIdx.x;
-    grid_dependency_wait();
-    const int slot = __ldg(P.slots + t);
-    if (slot < 0 || slot >= P.n_slots) return;
-    const int heads = P.Hq + 2 * P.Hkv, group = tid / P.lanes, l = tid % P.lanes, groups = NT / P.lanes;
-    const bool on = l * 8 < P.D;
-    const int pos = __ldg(P.positions + t);
-    for (int i = tid; i < P.rot / 2; i += NT) {
-        const double turns = (double)pos * (double)__ldg(P.inv_freq + i) * 0.15915494309189533577;      // 1 / 2 pi
-        float s, c;
-        sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
-        turn[i] = make_float2(c, s);
-    }
-    __syncthreads();
-    const long long at_block = slot / P.block, at_slot = slot % P.block;
-    for (int h0 = 0; h0 < heads; h0 += groups) {
-        const int h = h0 + group;
-        const int kind = h < P.Hq ? 0 : h < P.Hq + P.Hkv ? 1 : 2, head = kind == 0 ? h : kind == 1 ? h - P.Hq : h - P.Hq - P.Hkv;
-        const bool live = on && h < heads;
-        Eight<T> e;
-        if (live) e = load8<T, VEC>((const T *)P.x[kind] + t * P.x_stride[kind][0] + head * P.x_stride[kind][1] + l * 8);
-        float y[8];
+// What a thread does to eight entries of a row: norm over the row's threads, rotation.
+struct Turner {
+    int l, lanes, half;                            // thread of the row, threads of a row, threads of half a rotated part
+    bool on, halves;
+    const float2 *turn;
+    float inv_D, eps;
+
+    __device__ __forceinline__ void operator()(float (&y)[8], const float (&w)[8], bool norm) const
+    {
+        if (norm) {
+            float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = live ? to_f(e.v[i]) : 0.f;
-        const T *weight = kind < 2 ? (const T *)P.weight[kind] : nullptr;
-        float sum = 0.f;
+            for (int i = 0; i < 8; ++i) sum = fmaf(y[i], y[i], sum);
+            for (int o = lanes >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            const float r = rsqrtf(sum * inv_D + eps);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fmaf(y[i], y[i], sum);
-        for (int o = P.lanes >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (weight && live) {
-            const float r = 1.f / sqrtf(sum / (float)P.D + P.eps);
-            const Eight<T> w = load8<T, false>(weight + l * 8);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = y[i] * r * to_f(w.v[i]);
+            for (int i = 0; i < 8; ++i) y[i] = y[i] * r * w[i];
         }
-        const int half = P.rot / 16;                               // threads of half a rotated part
-        if (P.pairs == 0) {
+        const bool turned = l < 2 * half;
+        if (halves) {
             // the pair's other entry lies rot / 2 further on or back, with the same place in another thread
-            const int lane = tid & 31, other = l < half ? lane + half : lane - half;
-            const bool turned = l < 2 * half;
-            const int i0 = (l < half ? l : l - half) * 8;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float z = __shfl_sync(0xffffffffu, y[i], turned ? other & 31 : lane);
-                if (turned && kind < 2) {
-                    const float2 cs = turn[i0 + i];
-                    y[i] = l < half ? y[i] * cs.x - z * cs.y : y[i] * cs.x + z * cs.y;
-                }
-            }
-        } else if (l < 2 * half && kind < 2) {
+            const int lane = threadIdx.x & 31, other = turned ? (l < half ? lane + half : lane - half) & 31 : lane;
+            const float4 *cs = (const float4 *)(turn + (turned ? (l < half ? l : l - half) * 8 : 0));
+            const float sign = l < half ? -1.f : 1.f;
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
-                const float2 cs = turn[l * 4 + i / 2];
-                const float a = y[i], b = y[i + 1];
-                y[i] = a * cs.x - b * cs.y;
-                y[i + 1] = b * cs.x + a * cs.y;
+                const float z0 = __shfl_sync(0xffffffffu, y[i], other), z1 = __shfl_sync(0xffffffffu, y[i + 1], other);
+                if (!turned) continue;
+                const float4 c = cs[i / 2];
+                y[i] = y[i] * c.x + sign * (z0 * c.y);
+                y[i + 1] = y[i + 1] * c.z + sign * (z1 * c.w);
+            }
+        } else if (turned) {
+            const float4 *cs = (const float4 *)(turn + l * 4);
+#pragma unroll
+            for (int i = 0; i < 8; i += 4) {
+                const float4 c = cs[i / 4];
+                const float a0 = y[i], b0 = y[i + 1], a1 = y[i + 2], b1 = y[i + 3];
+                y[i] = a0 * c.x - b0 * c.y;
+                y[i + 1] = b0 * c.x + a0 * c.y;
+                y[i + 2] = a1 * c.z - b1 * c.w;
+                y[i + 3] = b1 * c.z + a1 * c.w;
             }
         }
-        if (!live) continue;
-        if (kind < 2) {
+    }
+};
+template <typename T> __device__ __forceinline__ void widen(const Eight<T> &e, float (&y)[8])
+{
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e.v[i] = from_f<T>(y[i]);
+    for (int i = 0; i < 8; ++i) y[i] = to_f(e.v[i]);
+}
+template <typename T> __device__ __forceinline__ void narrow(const float (&y)[8], Eight<T> &e)
+{
+    if constexpr (sizeof(T) == 2) {
+        uint32_t *w = reinterpret_cast<uint32_t *>(&e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (std::is_same<T, __half>::value) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(y[2 * i + 1]), "f"(y[2 * i]));
+            else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(y[2 * i + 1]), "f"(y[2 * i]));
         }
-        T *to = kind == 0 ? (T *)P.q_out + t * P.q_out_stride[0] + head * P.q_out_stride[1]
-                          : (T *)P.cache[kind - 1] + at_block * P.cache_stride[kind - 1][0] + at_slot * P.cache_stride[kind - 1][1]
-                                + head * P.cache_stride[kind - 1][2];
-        store8<T, VEC>(to + l * 8, e);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e.v[i] = from_f<T>(y[i]);
+    }
+}
+
+// A CTA per token, and several tokens one after the other in a long batch: the token's angles once for all heads (the position times a frequency, in
+// turns, reduced in fp64: fp32 would lose 1e-2 of an angle at position 1e5), then a row per `lanes` threads, eight entries each: the
+// queries' rows two at a time, then those of keys and values side by side.  The first rows of each are on their way while the angles are computed.
+// Bound by the bytes of the projections, if the instructions are few: 6528 tokens of 48 heads of 128 entries (160 MB) took 55 us (2.9
+// instructions a cycle) with the kinds of rows mixed in one loop, 50 with a CTA per token (two thirds of them for addresses).
+template <typename T, bool VEC> __global__ void __launch_bounds__(NT, 4) spec_rope_kernel(const Params P)
+{
+    __shared__ __align__(16) float2 turns[2][ROT_MAX / 2];
+    const int tid = threadIdx.x, lanes = 1 << P.lane_shift, groups = NT >> P.lane_shift, group = tid >> P.lane_shift, l = tid & (lanes - 1);
+    // (threads behind the row's end, of rows of 8 * lanes entries, hold zeros)
+    const bool on = l * 8 < P.D, on_q0 = on && group < P.Hq, on_q1 = on && group + groups < P.Hq, on_kv = on && group < 2 * P.Hkv;
+    const bool norm_q = P.weight[0] != nullptr, norm_k = P.weight[1] != nullptr, first_key = group < P.Hkv;
+    const T *q_head = (const T *)P.x[0] + group * P.x_stride[0][1] + l * 8;
+    T *out_head = (T *)P.q_out + group * P.q_out_stride[1] + l * 8;
+    const long long q_step = groups * P.x_stride[0][1], out_step = groups * P.q_out_stride[1];
+    const auto kv_head = [&](int h) {
+        return h < P.Hkv ? (const T *)P.x[1] + h * P.x_stride[1][1] + l * 8 : (const T *)P.x[2] + (h - P.Hkv) * P.x_stride[2][1] + l * 8;
+    };
+    const auto cache_head = [&](int h) {
+        return h < P.Hkv ? (T *)P.cache[0] + h * P.cache_stride[0][2] + l * 8 : (T *)P.cache[1] + (h - P.Hkv) * P.cache_stride[1][2] + l * 8;
+    };
+    const T *kv_first = kv_head(group);
+    T *cache_first = cache_head(group);
+    grid_dependency_wait();
+    int t = blockIdx.x, slot = __ldg(P.slots + t), pos = __ldg(P.positions + t);
+    for (int turn_of = 0; t < P.T; turn_of ^= 1) {
+        const int now = t, here = slot, at = pos;
+        t += gridDim.x;
+        if (t < P.T) { slot = __ldg(P.slots + t); pos = __ldg(P.positions + t); }
+        if (here < 0 || here >= P.n_slots) continue;
+        const T *q = q_head + now * P.x_stride[0][0];
+        T *out = out_head + now * P.q_out_stride[0];
+        const long long k_token = now * P.x_stride[1][0], v_token = now * P.x_stride[2][0];
+        Eight<T> a = {}, b = {}, c = {};
+        if (on_q0) a = load8<T, VEC>(q);
+        if (on_q1) b = load8<T, VEC>(q + q_step);
+        if (on_kv) c = load8<T, VEC>(kv_first + (first_key ? k_token : v_token));
+        float2 *turn = turns[turn_of];
+        for (int i = tid; i < P.rot / 2; i += NT) {
+            const double angle = (double)at * (double)__ldg(P.inv_freq + i) * 0.15915494309189533577;      // in turns: / 2 pi
+            float sine, cosine;
+            sincospif(2.f * (float)(angle - rint(angle)), &sine, &cosine);
+            turn[i] = make_float2(cosine, sine);
+        }
+        __syncthreads();
+        const Turner turner = {l, lanes, P.rot / 16, on, P.pairs == 0, turn, P.inv_D, P.eps};
+        float w[8] = {}, y[8];
+        if (on && norm_q) widen(load8<T, VEC>((const T *)P.weight[0] + l * 8), w);
+        for (int h0 = 0; h0 < P.Hq; h0 += 2 * groups) {
+            const int h = h0 + group;
+            widen(a, y);
+            turner(y, w, norm_q);
+            narrow(y, a);
+            if (on && h < P.Hq) store8<T, VEC>(out, a);
+            if (h0 + groups < P.Hq) {
+                widen(b, y);
+                turner(y, w, norm_q);
+                narrow(y, b);
+                if (on && h + groups < P.Hq) store8<T, VEC>(out + out_step, b);
+            }
+            q += 2 * q_step;
+            out += 2 * out_step;
+            if (h0 + 2 * groups < P.Hq) {
+                if (on && h + 2 * groups < P.Hq) a = load8<T, VEC>(q);
+                if (on && h + 3 * groups < P.Hq) b = load8<T, VEC>(q + q_step);
+            }
+        }
+        if (on && norm_k) widen(load8<T, VEC>((const T *)P.weight[1] + l * 8), w);
+        const int block = (int)((__umulhi(P.block_mul, (unsigned)here) + (unsigned)here) >> P.block_shift), in = here - block * P.block;
+        const long long k_slot = block * P.cache_stride[0][0] + in * P.cache_stride[0][1], v_slot = block * P.cache_stride[1][0] + in * P.cache_stride[1][1];
+        for (int h0 = 0; h0 < 2 * P.Hkv; h0 += groups) {
+            const int h = h0 + group;
+            const bool key = h < P.Hkv, live = on && h < 2 * P.Hkv;
+            if (h0 && live) c = load8<T, VEC>(kv_head(h) + (key ? k_token : v_token));
+            if (__any_sync(0xffffffffu, key)) {
+                Eight<T> turned;
+                widen(c, y);
+                turner(y, w, norm_k);
+                narrow(y, turned);
+                if (key) c = turned;
+            }
+            if (live) store8<T, VEC>((h0 ? cache_head(h) : cache_first) + (key ? k_slot : v_slot), c);
+        }
     }
 }
 

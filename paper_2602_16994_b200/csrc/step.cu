@@ -131,6 +131,13 @@ bool bad_pages(int num_blocks, int block, int width)
 {
     return num_blocks < 1 || block < 1 || width < 1 || (int64_t)num_blocks * block > 0x7FFFFFFF;
 }
+// floor(n / d) for n < 2^31 and 2^(s-1) < d <= 2^s: (n + umulhi(m, n)) >> s with m = floor(2^32 (2^s - d) / d) + 1
+void divisor(uint64_t d, unsigned *mul, int *shift)
+{
+    *shift = 0;
+    while ((1ull << *shift) < d) ++*shift;
+    *mul = (unsigned)((((uint64_t)1 << 32) * ((1ull << *shift) - d)) / d + 1);
+}
 bool aligned(const void *p, int64_t n) { return ((uintptr_t)p & (uintptr_t)(n - 1)) == 0; }
 
 }  // namespace
@@ -172,17 +179,18 @@ int32_t spec_norm_rope_cache(const SpecNormRope *a, void *stream)
     if (a->D < 8 || a->D > 256 || a->D % 8 || a->rot > a->D || a->rot % 16) return SPEC_ERR_UNSUPPORTED;
     rope::Params p = {};
     p.T = a->T; p.Hq = a->Hq; p.Hkv = a->Hkv; p.D = a->D; p.rot = a->rot; p.pairs = a->pairs;
-    p.lanes = 1;
-    while (p.lanes * 8 < a->D) p.lanes *= 2;
+    while ((8 << p.lane_shift) < a->D) ++p.lane_shift;
+    divisor(a->block_size, &p.block_mul, &p.block_shift);
     p.block = a->block_size; p.n_slots = (long long)a->num_blocks * a->block_size;
     p.x[0] = a->q; p.x[1] = a->k; p.x[2] = a->v;
     const int64_t *in[3] = {a->q_stride, a->k_stride, a->v_stride};
     const int64_t esz = a->dtype == SPEC_F32 ? 4 : 2;
     int64_t all = (int64_t)(uintptr_t)a->q | (int64_t)(uintptr_t)a->k | (int64_t)(uintptr_t)a->v | (int64_t)(uintptr_t)a->q_out |
-                  (int64_t)(uintptr_t)a->k_cache | (int64_t)(uintptr_t)a->v_cache;
+                  (int64_t)(uintptr_t)a->k_cache | (int64_t)(uintptr_t)a->v_cache | (int64_t)(uintptr_t)a->q_weight |
+                  (int64_t)(uintptr_t)a->k_weight;
     for (int i = 0; i < 3; ++i)
         for (int j = 0; j < 2; ++j) { p.x_stride[i][j] = in[i][j]; all |= in[i][j] * esz; }
-    p.weight[0] = a->q_weight; p.weight[1] = a->k_weight; p.eps = a->eps;
+    p.weight[0] = a->q_weight; p.weight[1] = a->k_weight; p.eps = a->eps; p.inv_D = 1.f / (float)a->D;
     p.inv_freq = a->inv_freq; p.positions = a->positions; p.slots = a->slots;
     p.q_out = a->q_out; p.cache[0] = a->k_cache; p.cache[1] = a->v_cache;
     for (int j = 0; j < 2; ++j) { p.q_out_stride[j] = a->q_out_stride[j]; all |= a->q_out_stride[j] * esz; }
@@ -193,7 +201,9 @@ int32_t spec_norm_rope_cache(const SpecNormRope *a, void *stream)
     const bool vec = (all & 15) == 0;
     const auto go = [&](auto kernel) {
         const int rc = prepare(kernel, 0, false);
-        return rc ? rc : launch(kernel, dim3(a->T), rope::NT, 0, 0, (cudaStream_t)stream, p);
+        // as many CTAs as have room (four to an SM), each with as many tokens as the others
+        const int most = 148 * 4, each = (a->T + most - 1) / most;
+        return rc ? rc : launch(kernel, dim3((a->T + each - 1) / each), rope::NT, 0, 0, (cudaStream_t)stream, p);
     };
     if (a->dtype == SPEC_F32) return vec ? go(rope::spec_rope_kernel<float, true>) : go(rope::spec_rope_kernel<float, false>);
     if (a->dtype == SPEC_F16) return vec ? go(rope::spec_rope_kernel<__half, true>) : go(rope::spec_rope_kernel<__half, false>);
@@ -255,11 +265,6 @@ int32_t spec_tree_attention(const SpecAttention *a, void *ws, int64_t ws_bytes, 
     p.tree = tree_args(a->N, a->lengths, a->n_nodes, a->parent, a->topo_seq_stride);
     p.B = a->B; p.Hq = a->Hq; p.Hkv = a->Hkv; p.G = a->Hq / a->Hkv;
     p.num_blocks = a->num_blocks; p.block = a->block_size; p.width = a->table_width;
-    // floor(n / d) for n < 2^31 and 2^(s-1) < d <= 2^s: (n + umulhi(m, n)) >> s with m = floor(2^32 (2^s - d) / d) + 1
-    const auto divisor = [](uint64_t d, unsigned *mul, int *shift) {
-        while ((1ull << *shift) < d) ++*shift;
-        *mul = (unsigned)((((uint64_t)1 << 32) * ((1ull << *shift) - d)) / d + 1);
-    };
     divisor(a->block_size, &p.block_mul, &p.block_shift);
     divisor(p.G, &p.group_mul, &p.group_shift);
     p.window = a->window; p.sinks = a->sinks;
@@ -343,9 +348,10 @@ int32_t spec_verify_probs(const SpecChains *a, void *stream)
         (a->draft_probs && a->draft_stride < a->V))
         return SPEC_ERR_SHAPE;
     if (a->dtype != SPEC_F32 && a->dtype != SPEC_BF16) return SPEC_ERR_DTYPE;
-    // the largest cluster whose slices are worth a CTA and that leaves one wave of eight CTAs per SM
+    // the largest cluster whose slices are worth a CTA and that leaves one wave of four CTAs per SM (128 requests of 151936 entries: 37 us with
+    // eight CTAs each, in two waves)
     int C = 1;
-    while (C < chain::CMAX && a->V / (2 * C) >= 4096 && (int64_t)a->B * 2 * C <= 148 * 8) C *= 2;
+    while (C < chain::CMAX && a->V / (2 * C) >= 4096 && (int64_t)a->B * 2 * C <= 148 * 4) C *= 2;
     while (C < chain::CMAX && (int64_t)a->V > (int64_t)C * chain::TILES * chain::TILE) C *= 2;
     if ((int64_t)a->V > (int64_t)C * chain::TILES * chain::TILE) return SPEC_ERR_UNSUPPORTED;
     chain::Params p = {};
