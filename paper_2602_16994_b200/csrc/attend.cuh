@@ -312,7 +312,7 @@ struct Bars {
 };
 static_assert(sizeof(Bars) <= 1024, "the area behind the buffers");
 
-// A bounded wait; once one has run out all others return at once, and the kernel comes to its end.
+// A bounded wait; once one has run out all others return at once, no copies or products are issued any more, and the kernel comes to its end.
 __device__ __forceinline__ void wait(Bars *B, uint64_t *bar, uint32_t parity)
 {
     if (mbar_try_wait(bar, parity)) return;
@@ -587,9 +587,9 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                 bool masked = false;
 #pragma unroll 1
                 for (int h = 0; h < S::PARTS; ++h, ++n_part) {
-                    const int buf = MT == 2 ? t * 2 + h : n_run & 1;
-                    const uint32_t s_at = lanes + (MT == 2 ? buf * 64 : buf * 128);
-                    wait(B, &B->s_full[buf], (MT == 2 ? n_part >> 1 : n_run >> 1) & 1);
+                    const int buf = MT == 2 ? t * S::PARTS + h : n_run & 1;
+                    const uint32_t s_at = lanes + buf * S::W;
+                    wait(B, &B->s_full[buf], (MT == 2 ? n_part / S::PARTS : n_run >> 1) & 1);
                     tc::fence_after();
                     if (warp_live) {
                         if (h == 0) {
@@ -609,10 +609,11 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                             // a new reference: what has been summed is scaled
                             float f = 1.f;
                             if (over) {
-                                // (whole numbers: O keeps its digits; a score that is no number, or infinite, leaves the row none either, for good)
-                                const float ref = top < CUDART_INF_F && of.ref == of.ref ? ceilf(top) : CUDART_NAN_F;
-                                if (of.any) f = ex2_approx(of.ref - ref);
-                                of.ref = ref;
+                                // (the first one is the largest score, which gets the weight 1; later ones lie whole numbers above it, so that what is
+                                // scaled keeps its digits; a score that is no number, or infinite, leaves the row no number either, for good)
+                                const float up = of.any ? ceilf(top - of.ref) : 0.f;
+                                if (of.any) f = ex2_approx(-up);
+                                of.ref = top < CUDART_INF_F && of.ref == of.ref ? (of.any ? of.ref + up : top) : CUDART_NAN_F;
                                 of.any = true;
                             }
                             of.l *= f;
@@ -634,7 +635,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             // the segment's end.  Where scores run ahead of the weights, the last follow all products but the last two, which are waited for one after
             // the other (the parity of a phase is that of the one two before)
             if (begun) {
-                if (!S::TURNS && n_part > 1) wait(B, &B->pv_done[w], n_part & 1);
+                if ((S::WG == 1 || S::PARTS == 2) && n_part > 1) wait(B, &B->pv_done[w], n_part & 1);
                 wait(B, &B->pv_done[w], (n_part - 1) & 1);
             }
             tc::fence_after();
@@ -727,8 +728,9 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             tc::fence_after();
         };
         // S of row block t for part h of a tile into columns `to`, from the keys in slots k ..; `bar`: where that is told
+        const auto gone = [&] { return *(volatile int *)&B->dead != 0; };
         const auto scores = [&](int t, int h, int to, uint32_t k, uint64_t *bar, bool release) {
-            if (tc::elected()) {
+            if (!gone() && tc::elected()) {
 #pragma unroll
                 for (int p = 0; p < S::STEP; ++p) {
                     const uint32_t slot = (k + p) % S::SLOTS;
@@ -747,7 +749,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         };
         // O number o (+)= P (in columns `from`) V for part h of a tile, from the values in slots k ..
         const auto sums = [&](int o, int h, int from, uint32_t k, bool add, bool release) {
-            if (tc::elected()) {
+            if (!gone() && tc::elected()) {
 #pragma unroll
                 for (int p = 0; p < S::STEP; ++p) {
                     const uint32_t slot = (k + p) % S::SLOTS;
@@ -762,7 +764,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             __syncwarp();
         };
         const auto let_go = [&](uint64_t *bar) {
-            if (tc::elected()) tc::commit(bar);
+            if (!gone() && tc::elected()) tc::commit(bar);
             __syncwarp();
         };
         // (the slots' order: K0, V0, K1, V1, ...)
@@ -785,22 +787,23 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                 // A tile in two parts of 64 keys: while the weights of one part are at work the other has its products, and its next scores right behind
                 // them.  (Products of a part: 8 with N = 64 for S, 4 with N = 128 for O.)
                 copied(n, n_tile);
-                for (int h = 0; h < 2; ++h) scores(m, h, (m * 2 + h) * 64, n, &B->s_full[m * 2 + h], h == 1);
+                for (int h = 0; h < S::PARTS; ++h) scores(m, h, (m * S::PARTS + h) * S::W, n, &B->s_full[m * S::PARTS + h], h == S::PARTS - 1);
                 if (steps == 1) let_go(&B->q_empty);
 #pragma unroll 1
                 for (int i = 0; i < steps; ++i, ++n_mine) {
                     const bool more = i + 1 < steps;
                     copied(values_of(i), n_tile + i);
 #pragma unroll 1
-                    for (int h = 0; h < 2; ++h) {
-                        const int buf = m * 2 + h;
+                    for (int h = 0; h < S::PARTS; ++h) {
+                        const int buf = m * S::PARTS + h;
+                        const bool last = h == S::PARTS - 1;
                         wait(B, &B->p_full[buf], n_mine & 1);
                         if (i == 0 && h == 0 && n_o) wait(B, &B->o_empty[m], (n_o - 1) & 1);
                         tc::fence_after();
-                        sums(m, h, buf * 64, values_of(i), i > 0 || h > 0, h == 1);
+                        sums(m, h, buf * S::W, values_of(i), i > 0 || h > 0, last);
                         if (!more) continue;
                         if (h == 0) copied(keys_of(i + 1), n_tile + i + 1);
-                        scores(m, h, buf * 64, keys_of(i + 1), &B->s_full[buf], h == 1);
+                        scores(m, h, buf * S::W, keys_of(i + 1), &B->s_full[buf], last);
                     }
                     if (i + 2 == steps) let_go(&B->q_empty);
                 }
@@ -904,6 +907,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                 const uint32_t k = n + p;
                 if (k >= S::SLOTS) room(&B->empty[k % S::SLOTS], (k / S::SLOTS - 1) & 1);
             }
+            if (*(volatile int *)&B->dead) { n += S::STEP; return; }
             bool hold = false;
             if (by_map) {
                 if (lane == 0) {
@@ -942,6 +946,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         const auto copy_q = [&](const Segment &s) {
             if (n_seg) room(&B->q_empty, (n_seg - 1) & 1);
             ++n_seg;
+            if (*(volatile int *)&B->dead) return;
             if (P.q_boxes) {
                 // (nodes beyond N come as zeros)
                 if (part == 0 && lane == 0) {
@@ -989,6 +994,11 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         }
         tc::wait_copies<0>();
         if (late_values) clean();
+    }
+    if (*(volatile int *)&B->dead) {
+        // a wait ran out, and nobody waits any more: copies and products under way, which depend on nothing else, get a millisecond to end
+        const long long t0 = clock64();
+        while (clock64() - t0 < 2000000) __nanosleep(1000);
     }
     tc::fence_before();
     __syncthreads();

@@ -141,6 +141,13 @@ void divisor(uint64_t d, unsigned *mul, int *shift)
 bool aligned(const void *p, int64_t n) { return ((uintptr_t)p & (uintptr_t)(n - 1)) == 0; }
 
 }  // namespace
+
+int set_step_wait(long long cycles)
+{
+    if (cudaMemcpyToSymbol(c_wait_cycles, &cycles, sizeof(cycles)) != cudaSuccess) { cudaGetLastError(); return SPEC_ERR_CUDA; }
+    return SPEC_OK;
+}
+
 }  // namespace specv
 
 using namespace specv;

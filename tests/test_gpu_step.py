@@ -7,6 +7,7 @@ import torch
 
 from . import step_ref as ref
 from paper_2602_16994_b200 import binding, synth
+from paper_2602_16994_b200.tree_cache import TreeCache
 
 pytestmark = pytest.mark.gpu
 
@@ -465,6 +466,17 @@ def test_attention_in_a_graph_and_on_another_stream():
     assert torch.equal(outs[0], fresh) and not torch.equal(fresh, want)
 
 
+def test_attention_to_one_key_is_its_value():
+    for length in (0, 700):
+        c = attention_case([length, 0], tree(4, 2, 4), 4, 2, 128, torch.bfloat16, 16, seed=20, window=1)
+        c["q"][:] = torch.randn_like(c["q"].float()).to(c["q"].dtype)
+        got = binding.tree_attention(**cuda(c)).out.cpu()
+        for b, n in enumerate((length, 0)):
+            at = torch.arange(n, n + 19)
+            v = c["v_cache"][c["block_table"][b, at // 16].long(), at % 16]
+            assert torch.equal(got[b], v.repeat_interleave(2, 1))
+
+
 def test_attention_is_the_same_every_time():
     for parent in (chain(1), tree(4, 2, 4), tree(8, 2, 6)):
         c = attention_case([3000, 129, 700, 1500, 2200], parent, 32, 8, 128, torch.bfloat16, 16, seed=18)
@@ -696,6 +708,38 @@ def test_steps_of_a_decoding_loop():
                     i = int(table[b, j // block])
                     assert torch.equal(cache[2 * layer, i, j % block].cpu(), k) and torch.equal(cache[2 * layer + 1, i, j % block].cpu(), v)
     assert int(lengths.sum()) > 6 * B
+
+
+def test_tree_cache():
+    """The same steps through the class that keeps the state; a request ends and its blocks go to another."""
+    g = torch.Generator().manual_seed(1)
+    B, N, blocks, block = 3, 10, 12, 8
+    cache = TreeCache(B, 1, blocks, block, 2, 64, width=8)
+    parent = tree(3, 0, 3).cuda()
+    lengths, held = [0] * B, {}
+    for step in range(4):
+        if step == 3:
+            cache.release(1)
+            assert int(cache.free_range[1]) + int(cache.owned.sum()) == blocks
+        s = cache.begin(parent)
+        assert s.status.tolist() == [0] * B
+        used = [x for row in cache.block_table.tolist() for x in row if x >= 0]
+        assert len(set(used)) == len(used)
+        qkv = torch.randn(B * N, 8, 64, generator=g).to(torch.bfloat16).cuda()
+        q = cache.write(0, qkv[:, :4], qkv[:, 4:6], qkv[:, 6:], torch.ones(32, device="cuda") * 0.01)
+        out = cache.attend(0, q.view(B, N, 4, 64), window=30, sinks=2)
+        assert out.status.tolist() == [0] * B
+        want = ref.attention(q.view(B, N, 4, 64).cpu(), cache.storage[0].cpu(), cache.storage[1].cpu(), cache.block_table.cpu(),
+                             cache.lengths.cpu(), parent.cpu(), window=30, sinks=2)
+        bound = want["mass"] * (2.0**-8 + 2.0**-10) + want["out"].abs() * 2.0**-8
+        live = want["live"]
+        assert bool(((out.out.cpu().double() - want["out"]).abs() <= bound)[live].all())
+        accepted = torch.tensor([9, 4, 0], dtype=I32, device="cuda")
+        done = cache.commit(accepted)
+        lengths = [n + d if n >= 0 else n for n, d in zip(lengths, (4, 2, 1))]
+        if step == 3:
+            lengths[1] = -1
+        assert done.lengths.tolist() == lengths
 
 
 def attention_lists(old, k, v):
