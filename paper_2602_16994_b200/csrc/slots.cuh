@@ -53,7 +53,42 @@ __global__ void __launch_bounds__(NT) spec_slots_kernel(const Params P)
     int begin = P.free_size ? __ldg(P.range) : 0, count = P.free_size ? __ldg(P.range + 1) : 0;
     if (begin < 0 || begin >= P.free_size || count < 0 || count > P.free_size) begin = count = 0;
     bool fit;
+    if (blockIdx.x == gridDim.x - 1) {
+        // one CTA more: blocks taken by all, the largest running sum that the ring has; a run of requests per thread
+        const int per = (P.B + NT - 1) / NT, i0 = min(P.B, tid * per), i1 = min(P.B, i0 + per);
+        long long run = 0;
+#pragma unroll 4
+        for (int i = i0; i < i1; ++i) run += lacks(P, i, &fit);
+        long long incl = run;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long t = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += t;
+        }
+        __syncthreads();
+        if (lane == 31) part[warp] = incl;
+        __syncthreads();
+        long long at = incl - run, best = 0;
+        for (int w = 0; w < warp; ++w) at += part[w];
+#pragma unroll 4
+        for (int i = i0; i < i1; ++i) {
+            at += lacks(P, i, &fit);
+            if (at <= count) best = at;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
+        __syncthreads();
+        if (lane == 0) part[warp] = best;
+        __syncthreads();
+        if (tid == 0) {
+            for (int w = 0; w < WARPS; ++w) best = max(best, part[w]);
+            P.range_out[0] = P.free_size ? (int)((begin + best) % P.free_size) : 0;
+            P.range_out[1] = (int)(count - best);
+        }
+        return;
+    }
     long long before = 0;
+#pragma unroll 4
     for (int i = tid; i < b0; i += NT) before += lacks(P, i, &fit);
     before = block_sum(before, part);
     const int lack = b < P.B ? lacks(P, b, &fit) : 0;
@@ -92,36 +127,6 @@ __global__ void __launch_bounds__(NT) spec_slots_kernel(const Params P)
                           : n_or_bad < 0 ? SPEC_DEV_TOPOLOGY
                           : !placed ? SPEC_DEV_BLOCKS : page ? SPEC_DEV_PAGE : sound ? SPEC_DEV_OK : SPEC_DEV_TOPOLOGY;
         }
-    }
-    if (blockIdx.x != gridDim.x - 1) return;
-    // the last CTA: blocks taken by all, the largest running sum that the ring has; a run of requests per thread
-    const int per = (P.B + NT - 1) / NT, i0 = min(P.B, tid * per), i1 = min(P.B, i0 + per);
-    long long run = 0;
-    for (int i = i0; i < i1; ++i) run += lacks(P, i, &fit);
-    long long incl = run;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long t = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += t;
-    }
-    __syncthreads();
-    if (lane == 31) part[warp] = incl;
-    __syncthreads();
-    long long at = incl - run, best = 0;
-    for (int w = 0; w < warp; ++w) at += part[w];
-    for (int i = i0; i < i1; ++i) {
-        at += lacks(P, i, &fit);
-        if (at <= count) best = at;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
-    __syncthreads();
-    if (lane == 0) part[warp] = best;
-    __syncthreads();
-    if (tid == 0) {
-        for (int w = 0; w < WARPS; ++w) best = max(best, part[w]);
-        P.range_out[0] = P.free_size ? (int)((begin + best) % P.free_size) : 0;
-        P.range_out[1] = (int)(count - best);
     }
 }
 

@@ -170,7 +170,7 @@ int32_t spec_cache_slots(const SpecSlots *a, void *stream)
     p.owned = a->owned; p.ring = a->free_blocks; p.range = a->free_range;
     p.slots = a->slots; p.positions = a->positions; p.owned_out = a->owned_out; p.range_out = a->free_range_out; p.status = a->status;
     const int rc = prepare(slots::spec_slots_kernel, 0, false);
-    return rc ? rc : launch(slots::spec_slots_kernel, dim3((a->B + slots::WARPS - 1) / slots::WARPS), slots::NT, slots::WARPS * a->N * 4, 0,
+    return rc ? rc : launch(slots::spec_slots_kernel, dim3((a->B + slots::WARPS - 1) / slots::WARPS + 1), slots::NT, slots::WARPS * a->N * 4, 0,
                   (cudaStream_t)stream, p);
 }
 

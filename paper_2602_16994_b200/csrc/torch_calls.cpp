@@ -15,6 +15,7 @@
 #include <dlfcn.h>
 
 #include <cmath>
+#include <initializer_list>
 #include <optional>
 
 #include <torch/csrc/autograd/python_variable.h>
@@ -444,6 +445,32 @@ private:
     std::optional<c10::cuda::CUDAStreamGuard> switch_;
 };
 
+// Several int32 outputs out of one allocation (an output each costs the host about as much as the rest of a small call), on 16 bytes each.
+class Pieces {
+public:
+    Pieces(const Place &place, std::initializer_list<int64_t> counts)
+    {
+        int64_t total = 0;
+        for (const int64_t n : counts) total += up(n);
+        base_ = place.fresh({total}, at::kInt);
+    }
+    at::Tensor take(at::IntArrayRef sizes)
+    {
+        auto piece = c10::make_intrusive<c10::TensorImpl>(c10::Storage(base_.storage()), base_.key_set(), base_.dtype());
+        piece->set_storage_offset(at_);
+        piece->set_sizes_contiguous(sizes);
+        int64_t n = 1;
+        for (const int64_t s : sizes) n *= s;
+        at_ += up(n);
+        return at::Tensor(std::move(piece));
+    }
+
+private:
+    static int64_t up(int64_t n) { return (n + 3) / 4 * 4; }
+    at::Tensor base_;
+    int64_t at_ = 0;
+};
+
 void need(const void *f) { if (!f) raise("the library lacks an entry point"); }
 const at::Tensor &ints(PyObject *o, const char *name, const Place &place, int64_t count = -1)
 {
@@ -526,8 +553,8 @@ PyObject *py_slots(PyObject *, PyObject *const *a, Py_ssize_t n)
         s.owned = int_ptr(ints(a[3], "owned", place, B));
         s.free_blocks = int_ptr(ring); s.free_size = small(ring.numel(), "free_blocks");
         s.free_range = int_ptr(ints(a[5], "free_range", place, 2));
-        const at::Tensor t[6] = {place.fresh({B, N}, at::kInt), place.fresh({B, N}, at::kInt), THPVariable_Unpack(a[2]),
-                                 place.fresh({B}, at::kInt), place.fresh({2}, at::kInt), place.fresh({B}, at::kInt)};
+        Pieces made(place, {B * N, B * N, B, 2, B});
+        const at::Tensor t[6] = {made.take({B, N}), made.take({B, N}), THPVariable_Unpack(a[2]), made.take({B}), made.take({2}), made.take({B})};
         s.slots = int_ptr(t[0]); s.positions = int_ptr(t[1]); s.owned_out = int_ptr(t[3]); s.free_range_out = int_ptr(t[4]);
         s.status = int_ptr(t[5]);
         check(unlocked([&] { return step_lib.slots(&s, place.stream()); }), "spec_cache_slots");
@@ -668,7 +695,8 @@ PyObject *py_commit(PyObject *, PyObject *const *a, Py_ssize_t n)
         s.block_table = table.ptr; s.table_stride = table.stride;
         s.lengths = int_ptr(lengths); s.accepted_node = int_ptr(ints(a[1], "accepted_node", place, B));
         s.n_nodes = a[5] == Py_None ? nullptr : int_ptr(ints(a[5], "n_nodes", place, B));
-        const at::Tensor t[2] = {place.fresh({B}, at::kInt), place.fresh({B}, at::kInt)};
+        Pieces made(place, {B, B});
+        const at::Tensor t[2] = {made.take({B}), made.take({B})};
         s.lengths_out = int_ptr(t[0]); s.status = int_ptr(t[1]);
         check(unlocked([&] { return step_lib.commit(&s, place.stream()); }), "spec_cache_commit");
         return result(commit_outputs_class, t, 2);
@@ -704,8 +732,9 @@ PyObject *py_chains(PyObject *, PyObject *const *a, Py_ssize_t n)
         s.token = int_ptr(token); s.cu_drafts = int_ptr(cu);
         s.u_accept = (const float *)floats(a[4], "u_accept", place, T).data_ptr();
         s.u_bonus = (const float *)floats(a[5], "u_bonus", place, T + B).data_ptr();
-        const at::Tensor t[4] = {place.fresh({B}, at::kInt), place.fresh({B, (int64_t)(s.max_drafts < 0 ? 0 : s.max_drafts) + 1}, at::kInt),
-                                 place.fresh({B}, at::kInt), place.fresh({B}, at::kInt)};
+        const int64_t out = (int64_t)(s.max_drafts < 0 ? 0 : s.max_drafts) + 1;
+        Pieces made(place, {B, B * out, B, B});
+        const at::Tensor t[4] = {made.take({B}), made.take({B, out}), made.take({B}), made.take({B})};
         s.accept_len = int_ptr(t[0]); s.out_tokens = int_ptr(t[1]); s.bonus_token = int_ptr(t[2]); s.status = int_ptr(t[3]);
         check(unlocked([&] { return step_lib.probs(&s, place.stream()); }), "spec_verify_probs");
         return result(chain_outputs_class, t, 4);
