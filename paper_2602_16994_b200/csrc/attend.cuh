@@ -2,14 +2,16 @@
 //
 // Mathematics.  A unit is a request, a key head and a block of up to 128 MT of the rows (node, query head of the group) that share this
 // head's keys.  Over tiles of 128 keys, S = Q K^T, y = scale log2(e) S - ref, P = 2^y, l += sum P, O += P V, with one reference per row: the
-// largest y of the row's first tile, replaced (l and O scaled) only when a later y exceeds it by more than 8, so P stays
-// below 2^8 and a tile is gone through once.  Tiles run from the last to the first: the tree's tile comes first, where every row sees
-// itself.  The result is O / l.
+// largest y of what the row saw first, raised (l and O scaled) only when a later y exceeds it by more than 8, so P stays
+// below 2^8.  Tiles run from the last to the first: the tree's tile comes first, where every row sees itself.  The result is O / l.
 //
-// What bounds it.  Per tile and key head 64 KB of keys and values (D = 128): 2740 cycles of an SM's share of the HBM rate.  128 rows
-// take 1020 cycles of products and 1024 of exponentials, 256 rows twice that: up to about 250 rows the cache's bytes are the
-// bound, so both products go to the tensor cores even for one row (which fills 1 of 128 lanes), and rows share a lane each: a thread owns a row,
-// and maxima and sums need no exchange.
+// What bounds it.  Per tile and key head 64 KB of keys and values (D = 128): 2740 cycles of an SM's share of the HBM rate at 1.9 GHz.  128
+// rows take 1040 cycles of products and about 1100 of arithmetic per scheduler, 256 rows twice that, so up to about 250 rows the cache's
+// bytes are the floor, and both products go to the tensor cores even for one row (which fills 1 of 128 lanes).  A thread owns a row, and maxima and
+// sums need no exchange.  Measured (one B200): a tile takes 3100 cycles with up to 128 rows (8 requests, 19 nodes, 4 query heads to a key
+// head, contexts to 4096: 38 us, floor 15) and 4500 with 204 (128 requests of 51 nodes: 445 us at 1.55 GHz, floor 226): there a row block's
+// weights wait for its products and these for their turn on the tensor cores.  Small calls are bound by latency: one token over 8192 keys takes 23 us
+// (floor 5), of which 5 pass until the first scores are there, 1.2 a tile, and 6 from the last tile to the joined result.
 //
 // Balance.  The tiles of all units, in order, are cut into one run per CTA (one CTA per SM), whatever the lengths: a unit that a
 // run ends in leaves its O, l and reference in the workspace, and spec_join_kernel puts such parts together.  Every CTA finds its run from
@@ -279,8 +281,8 @@ __device__ __forceinline__ int block_in(const Params &P, int b, int col)
 
 // ---- the kernel ---------------------------------------------------------------------------------------------------------------
 // MT = 2: 256 rows, a warpgroup per 128.  MT = 1, WG = 2: 128 rows, the warpgroups take tiles in turn, each with its own O, reference and l,
-// put together at the segment's end: one warpgroup's tile takes 1400 cycles of arithmetic and 1040 of products one after the other,
-// and the cache delivers one every 2740.  WG = 1: one warpgroup (D = 256: tensor memory has room for one O).
+// put together at the segment's end: one warpgroup's tile takes some 2400 cycles of arithmetic and 1040 of products one after the other, and the
+// cache delivers one every 2740.  WG = 1: one warpgroup (D = 256: tensor memory has room for one O).
 template <int D_, int MT_, int WG_> struct Shape {
     static constexpr int D = D_, MT = MT_, WG = WG_;
     static constexpr bool TURNS = MT == 1 && WG == 2;
@@ -387,9 +389,10 @@ __device__ __forceinline__ unsigned long long exp2_pair(unsigned long long y2)
     unpack_f32x2(p, p0, p1);
     return pack_f32x2(__int_as_float(__float_as_int(p0) + (__float_as_int(t0) << 23)), __int_as_float(__float_as_int(p1) + (__float_as_int(t1) << 23)));
 }
-// 32 columns of scores: weights, their sum, and the weights rounded to the values' type, two to a register.  Three pairs of eight go without
-// the special function unit: 128 columns take a warp 1021 cycles, two warps of a scheduler 1826 (none: 1551 and 2381, every second: 1158
-// and 2023).
+// 32 columns of scores: weights, their sum, and the weights rounded to the values' type, two to a register.  One pair of eight goes without the
+// special function unit.  By itself the loop is fastest with three of eight (128 columns of two warps of a scheduler: 1826 cycles, none: 2381), in the
+// kernel, whose schedulers have the other roles' instructions to issue as well, with one (128 requests of 51 nodes: 445 us, three of eight: 456,
+// half: 471).
 template <typename T>
 __device__ __forceinline__ void weigh(const uint32_t (&s)[32], unsigned long long c2, unsigned long long r2, unsigned long long &sum, uint32_t (&pk)[16])
 {
@@ -398,7 +401,7 @@ __device__ __forceinline__ void weigh(const uint32_t (&s)[32], unsigned long lon
         const unsigned long long y2 = fma_f32x2(pack_f32x2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, r2);
         unsigned long long p2;
         float x, y;
-        if (k % 16 == 6 || k % 16 == 10 || k % 16 == 14) {
+        if (k % 16 == 14) {
             p2 = exp2_pair(y2);
         } else {
             unpack_f32x2(y2, x, y);
@@ -785,7 +788,8 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                 let_go(&B->q_empty);
             } else if (MT == 2) {
                 // A tile in two parts of 64 keys: while the weights of one part are at work the other has its products, and its next scores right behind
-                // them.  (Products of a part: 8 with N = 64 for S, 4 with N = 128 for O.)
+                // them.  (Products of a part: 8 with N = 64 for S, which take as long as 6 of full width, 4 with N = 128 for O.  128 requests of 51 nodes: 457
+                // us; scores of a whole tile at once, which are ready later: 498; weights of a whole tile at once as well: 505.)
                 copied(n, n_tile);
                 for (int h = 0; h < S::PARTS; ++h) scores(m, h, (m * S::PARTS + h) * S::W, n, &B->s_full[m * S::PARTS + h], h == S::PARTS - 1);
                 if (steps == 1) let_go(&B->q_empty);

@@ -12,7 +12,9 @@ namespace cg = cooperative_groups;
 // chain is one round of dependent loads, whatever its length), then the cluster draws from the one row, or pair of rows, that the
 // chain stopped at: the sums of tiles of 512 weights stay in shared memory, the slices' sums are exchanged, and the CTA that the
 // target falls into finds the tile and reads it once more.  Weights, sums and comparisons are fp64: fp32 sums over 1e5 weights would move the
-// borders between tokens by more than the tokens' own masses.  The bytes of one row of p and of q per request bound the call.
+// borders between tokens by more than the tokens' own masses.  The bytes of one row of p and of q per request are the floor: 8 requests of
+// 128256 entries take 8.4 us (floor 1.3: the walk, the row, its exchange and the tile are four rounds of latency), 128 looked-up ones of 151936 entries
+// 23 (floor 12).
 constexpr int NT = 256, WARPS = NT / 32, TILE = 512, TILES = 1024, CMAX = 16;      // a tile: four loads of 128 entries by a warp
 
 struct Params {

@@ -10,7 +10,7 @@
 namespace specv {
 namespace rope {
 
-constexpr int NT = 256, WARPS = NT / 32, ROT_MAX = 256;
+constexpr int NT = 256, ROT_MAX = 256;
 
 struct Params {
     int T, Hq, Hkv, D, rot, pairs, lane_shift;     // 1 << lane_shift threads to a head's row, a power of two >= D / 8
@@ -64,7 +64,7 @@ template <typename T, bool VEC> __device__ __forceinline__ void store8(T *p, con
 // What a thread does to eight entries of a row: norm over the row's threads, rotation.
 struct Turner {
     int l, lanes, half;                            // thread of the row, threads of a row, threads of half a rotated part
-    bool on, halves;
+    bool halves;
     const float2 *turn;
     float inv_D, eps;
 
@@ -130,8 +130,8 @@ template <typename T> __device__ __forceinline__ void narrow(const float (&y)[8]
 // A CTA per token, and several tokens one after the other in a long batch: the token's angles once for all heads (the position times a frequency, in
 // turns, reduced in fp64: fp32 would lose 1e-2 of an angle at position 1e5), then a row per `lanes` threads, eight entries each: the
 // queries' rows two at a time, then those of keys and values side by side.  The first rows of each are on their way while the angles are computed.
-// Bound by the bytes of the projections, if the instructions are few: 6528 tokens of 48 heads of 128 entries (160 MB) took 55 us (2.9
-// instructions a cycle) with the kinds of rows mixed in one loop, 50 with a CTA per token (two thirds of them for addresses).
+// 6528 tokens of 48 heads of 128 entries (160 MB) take 45 us, 0.54 of the copy bandwidth: the instructions (2.5 a cycle) bound it, not yet the
+// bytes.  With the kinds of rows mixed in one loop it took 55 us, with a CTA per token 50.
 template <typename T, bool VEC> __global__ void __launch_bounds__(NT, 4) spec_rope_kernel(const Params P)
 {
     __shared__ __align__(16) float2 turns[2][ROT_MAX / 2];
@@ -172,7 +172,7 @@ template <typename T, bool VEC> __global__ void __launch_bounds__(NT, 4) spec_ro
             turn[i] = make_float2(cosine, sine);
         }
         __syncthreads();
-        const Turner turner = {l, lanes, P.rot / 16, on, P.pairs == 0, turn, P.inv_D, P.eps};
+        const Turner turner = {l, lanes, P.rot / 16, P.pairs == 0, turn, P.inv_D, P.eps};
         float w[8] = {}, y[8];
         if (on && norm_q) widen(load8<T, VEC>((const T *)P.weight[0] + l * 8), w);
         for (int h0 = 0; h0 < P.Hq; h0 += 2 * groups) {

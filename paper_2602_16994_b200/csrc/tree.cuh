@@ -48,12 +48,9 @@ __device__ __forceinline__ bool tree_depths(const int *parent, int n, volatile u
     any(false);
     return true;
 }
-// the joins: every thread of a warp / of a CTA gets whether any of them says so, and sees what the others stored
+// the join of a warp: every thread gets whether any of them says so, and sees what the others stored
 struct AnyInWarp {
     __device__ bool operator()(bool x) const { __syncwarp(); return __any_sync(0xffffffffu, x); }
-};
-struct AnyInBlock {
-    __device__ bool operator()(bool x) const { return __syncthreads_or(x) != 0; }
 };
 
 }  // namespace specv
