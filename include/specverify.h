@@ -344,7 +344,7 @@ int32_t spec_norm_rope_cache(const SpecNormRope *a, void *stream);
  * rows of a request with a bad tree (SPEC_DEV_TOPOLOGY).  What no node sees is not read; what a node does not see does not
  * reach its row, whatever it holds (NaN and infinities too).  Rows of idle requests and of nodes beyond n_nodes[b] stay as they were.
  * D: 64, 128 or 256.  q, caches and out of one type, SPEC_BF16 or SPEC_F16.  Strides in elements, multiples of 8, and bases on 16 bytes;
- * the D entries of a head are contiguous.  lse: optional, log of sum_j exp(scale q.k_j) (natural).
+ * the D entries of a head are contiguous; out overlaps no input.  lse: optional, log of sum_j exp(scale q.k_j) (natural).
  * `ws`: spec_tree_attention_workspace_bytes() bytes (a function of the sizes; contents do not matter).
  */
 typedef struct {

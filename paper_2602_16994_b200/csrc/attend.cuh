@@ -86,12 +86,14 @@ __device__ __forceinline__ int node_of(const Params &P, int row)
 __device__ __forceinline__ Tiles tiles_of(const Params &P, const Request &r, int m, int block_rows)
 {
     const int last = (m + 1) * block_rows >= r.rows ? r.n - 1 : node_of(P, (m + 1) * block_rows - 1);        // the block's last node
+    // (keys behind the table's end have no block: a tile at least, for the rows to come out as those of rows that see nothing)
+    const long long held = min((long long)P.width * P.block, 0x7FFFFFFFll);
     Tiles t;
-    t.end = (int)(((unsigned)r.len + (unsigned)last + KT) / KT);
+    t.end = (int)((min((unsigned)r.len + (unsigned)last + 1, (unsigned)held) + KT - 1) / KT);
     t.sink = t.from = 0;
     if (P.window) {
         t.sink = min(t.end, (int)(((unsigned)min(P.sinks, r.len) + KT - 1) / KT));
-        t.from = max(max(0, r.len - P.window + 1) / KT, t.sink);
+        t.from = max(min(max(0, r.len - P.window + 1) / KT, t.end - 1), t.sink);
     }
     return t;
 }
@@ -1049,7 +1051,8 @@ template <typename T, typename S> __global__ void __launch_bounds__(JOIN_NT, 8) 
         // columns of the table that hold a key that some node sees
         const long long keys = n ? (long long)len + n : 0, since = P.window ? max(0ll, (long long)len - P.window + 1) : 0;
         const long long sinks = min((long long)P.sinks, (long long)len);
-        const int cols = (int)((keys + P.block - 1) / P.block);
+        const int cols = (int)min((keys + P.block - 1) / P.block, (long long)P.width);
+        page = keys > (long long)P.width * P.block;
         for (int col = tid; col < cols; col += JOIN_NT) {
             const long long a = (long long)col * P.block, e = a + P.block;
             if (e > since || a < sinks) page |= block_in(P, b, col) < 0;

@@ -494,6 +494,12 @@ int32_t small(int64_t v, const char *what)
     if (v > 0x7FFFFFFF || v < 0) raise("%s is out of range", what);
     return (int32_t)v;
 }
+int32_t whole(PyObject *o, const char *what)        // an int argument, whole or refused
+{
+    const long long v = integer(o);
+    if (v > 0x7FFFFFFFll || v < -0x7FFFFFFFll - 1) raise("%s is out of range", what);
+    return (int32_t)v;
+}
 // the parents of one tree for all, or of one per request: row length, and the stride between requests
 int64_t tree_of(PyObject *o, const Place &place, int64_t B, int64_t *N, const int32_t **parent)
 {
@@ -547,7 +553,7 @@ PyObject *py_slots(PyObject *, PyObject *const *a, Py_ssize_t n)
         s.topo_seq_stride = tree_of(a[1], place, B, &N, &s.parent);
         const Table table = table_of(a[2], place, B);
         const at::Tensor &ring = ints(a[4], "free_blocks", place);
-        s.B = small(B, "B"); s.N = small(N, "N"); s.block_size = truncated(a[6]); s.table_width = table.width;
+        s.B = small(B, "B"); s.N = small(N, "N"); s.block_size = whole(a[6], "block_size"); s.table_width = table.width;
         s.lengths = int_ptr(lengths); s.block_table = table.ptr; s.table_stride = table.stride;
         s.n_nodes = a[7] == Py_None ? nullptr : int_ptr(ints(a[7], "n_nodes", place, B));
         s.owned = int_ptr(ints(a[3], "owned", place, B));
@@ -596,7 +602,7 @@ PyObject *py_norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n)
         s.positions = int_ptr(ints(a[4], "positions", place, T));
         s.slots = int_ptr(ints(a[5], "slots", place, T));
         s.T = small(T, "T"); s.Hq = small(q.size(1), "Hq"); s.Hkv = small(Hkv, "Hkv"); s.D = small(D, "D");
-        s.rot = small(2 * freq.numel(), "inv_freq"); s.pairs = truncated(a[11]); s.dtype = element_type(type); s.eps = (float)number(a[10]);
+        s.rot = small(2 * freq.numel(), "inv_freq"); s.pairs = whole(a[11], "pairs"); s.dtype = element_type(type); s.eps = (float)number(a[10]);
         s.num_blocks = small(kc.size(0), "num_blocks"); s.block_size = small(kc.size(1), "block_size");
         at::Tensor out;
         if (a[12] == Py_None) {
@@ -639,7 +645,7 @@ PyObject *py_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
         s.B = small(B, "B"); s.N = small(N, "N"); s.Hq = small(Hq, "Hq"); s.Hkv = small(kc.size(2), "Hkv"); s.D = small(D, "D");
         s.dtype = element_type(type);
         s.num_blocks = small(kc.size(0), "num_blocks"); s.block_size = small(kc.size(1), "block_size"); s.table_width = table.width;
-        s.window = truncated(a[8]); s.sinks = truncated(a[9]);
+        s.window = whole(a[8], "window"); s.sinks = whole(a[9], "sinks");
         s.scale = a[7] == Py_None ? (float)(1.0 / std::sqrt((double)(D > 0 ? D : 1))) : (float)number(a[7]);
         s.block_table = table.ptr; s.table_stride = table.stride;
         s.lengths = int_ptr(ints(a[4], "lengths", place, B));
@@ -727,7 +733,7 @@ PyObject *py_chains(PyObject *, PyObject *const *a, Py_ssize_t n)
             s.draft_probs = q.data_ptr();
             if (T > 1) s.draft_stride = q.stride(0);
         }
-        s.B = small(B, "B"); s.V = small(V, "V"); s.max_drafts = truncated(a[6]); s.dtype = element_type(type); s.n_drafts = T;
+        s.B = small(B, "B"); s.V = small(V, "V"); s.max_drafts = whole(a[6], "max_drafts"); s.dtype = element_type(type); s.n_drafts = T;
         s.target_probs = p.data_ptr();
         s.token = int_ptr(token); s.cu_drafts = int_ptr(cu);
         s.u_accept = (const float *)floats(a[4], "u_accept", place, T).data_ptr();

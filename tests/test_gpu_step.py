@@ -253,7 +253,9 @@ TREES = {"token": chain(1), "d2k4": tree(4, 2, 4), "k8": tree(8, 2, 6), "pair": 
 @pytest.mark.parametrize("lengths", [[0], [1], [15, 16, 17], [127, 128, 129, 0], [300, 5, 1000]])
 @pytest.mark.parametrize("shape", ["token", "d2k4", "k8"])
 @pytest.mark.parametrize("Hq,Hkv,D,dtype,block", [(4, 1, 128, torch.bfloat16, 16), (6, 2, 64, torch.float16, 7), (8, 8, 128, torch.float16, 32),
-                                                  (4, 2, 256, torch.bfloat16, 16), (16, 2, 64, torch.bfloat16, 1)])
+                                                  (4, 2, 256, torch.bfloat16, 16), (16, 2, 64, torch.bfloat16, 1),
+                                                  (4, 1, 64, torch.bfloat16, 24), (4, 1, 128, torch.bfloat16, 256),
+                                                  (5, 1, 256, torch.float16, 8)])
 def test_attention(lengths, shape, Hq, Hkv, D, dtype, block):
     check_attention(attention_case(lengths, TREES[shape], Hq, Hkv, D, dtype, block, seed=sum(lengths) + D))
 
@@ -282,6 +284,36 @@ def test_attention_of_ragged_trees_and_idle_requests():
     want = ref.attention(**c)
     assert want["status"].tolist() == [0, 0, 0, 0, 1, 0]
     check_attention(c, want)
+
+
+def test_attention_of_ragged_trees_in_two_blocks_of_rows():
+    """Requests of which the second block of 128 rows, or half of it, has nothing to do, beside ones that fill it; several to a CTA."""
+    g = torch.Generator().manual_seed(4)
+    lengths = torch.randint(0, 300, (40,), generator=g).tolist()
+    nodes = torch.randint(0, 52, (40,), generator=g).tolist()
+    lengths[5] = -1
+    check_attention(attention_case(lengths, tree(8, 2, 6), 32, 8, 128, torch.bfloat16, 16, seed=6, n_nodes=nodes))
+    check_attention(attention_case(lengths, tree(8, 2, 6), 8, 1, 64, torch.float16, 16, seed=7, n_nodes=nodes, window=60, sinks=2))
+
+
+def test_attention_of_nobody():
+    c = attention_case([-1, -5], tree(4, 2, 4), 4, 2, 128, torch.bfloat16, 16)
+    assert check_attention(c).status.tolist() == [0, 0]
+    c = attention_case([9, 0], tree(4, 2, 4), 4, 2, 128, torch.bfloat16, 16, n_nodes=[0, 0])
+    assert check_attention(c).status.tolist() == [0, 0]
+
+
+@pytest.mark.parametrize("window", [0, 50])
+def test_attention_of_lengths_beyond_the_table(window):
+    """Whatever a length says, only the table's blocks are gone through; rows that see some of them are what those give."""
+    c = attention_case([100, 40], tree(4, 2, 4), 4, 2, 128, torch.bfloat16, 16, seed=14, window=window, sinks=3)
+    want = ref.attention(**c)
+    c["lengths"][0] = 2**31 - 1 - 19
+    got = binding.tree_attention(**cuda(c))
+    assert got.status.tolist() == [5, 0]
+    assert bool(got.out[0].isfinite().all())
+    assert torch.equal(got.out[1], binding.tree_attention(**cuda(dict(c, q=c["q"][1:], block_table=c["block_table"][1:], lengths=c["lengths"][1:]))).out[0])
+    assert bool(((got.out[1].cpu().double() - want["out"][1]).abs() <= want["mass"][1] * 2.0**-7).all())
 
 
 def test_attention_of_many_requests():
@@ -651,6 +683,20 @@ def test_commit_strided_cache():
     small = dict(c, cache=c["cache"][:2].contiguous())
     view.copy_(small["cache"])
     check_commit(small, cache=view)
+
+
+def test_arguments_out_of_range_are_refused():
+    d = cuda(attention_case([10], tree(1, 0, 1), 2, 1, 64, torch.bfloat16, 16))
+    for kw in (dict(window=2**32), dict(sinks=2**31), dict(window=-1), dict(scale=-1.0)):
+        with pytest.raises(RuntimeError):
+            binding.tree_attention(**d, **kw)
+    with pytest.raises(TypeError):
+        binding.tree_attention(**d, window=1.5)
+    with pytest.raises(RuntimeError, match="backward"):
+        binding.tree_attention(**dict(d, q=d["q"].requires_grad_()))
+    for name in ("k_cache", "v_cache", "q"):
+        with pytest.raises(RuntimeError):
+            binding.tree_attention(**dict(cuda(attention_case([10], tree(1, 0, 1), 2, 1, 64, torch.bfloat16, 16)), **{name: d[name].detach().half()}))
 
 
 # ---------------------------------------------------------------------------------------------
