@@ -152,7 +152,7 @@ template <typename T, bool VEC> __global__ void __launch_bounds__(NT, 4) spec_ro
     T *cache_first = cache_head(group);
     grid_dependency_wait();
     int t = blockIdx.x, slot = __ldg(P.slots + t), pos = __ldg(P.positions + t);
-    for (int turn_of = 0; t < P.T; turn_of ^= 1) {
+    for (int turn_of = 0; t < P.T;) {
         const int now = t, here = slot, at = pos;
         t += gridDim.x;
         if (t < P.T) { slot = __ldg(P.slots + t); pos = __ldg(P.positions + t); }
@@ -164,7 +164,8 @@ template <typename T, bool VEC> __global__ void __launch_bounds__(NT, 4) spec_ro
         if (on_q0) a = load8<T, VEC>(q);
         if (on_q1) b = load8<T, VEC>(q + q_step);
         if (on_kv) c = load8<T, VEC>(kv_first + (first_key ? k_token : v_token));
-        float2 *turn = turns[turn_of];
+        float2 *turn = turns[turn_of];             // (turned over only here: a token left out has no barrier that parts two uses)
+        turn_of ^= 1;
         for (int i = tid; i < P.rot / 2; i += NT) {
             const double angle = (double)at * (double)__ldg(P.inv_freq + i) * 0.15915494309189533577;      // in turns: / 2 pi
             float sine, cosine;

@@ -185,6 +185,15 @@ def test_norm_rope_skips_padding():
     assert bool((out[[0, 7, 39]] == 3.0).all())
 
 
+@pytest.mark.parametrize("D", [128, 64])
+def test_norm_rope_skips_padding_between_the_tokens_of_a_cta(D):
+    # far more tokens than CTAs, half of them left out at random: a CTA's next token may come right behind the last, or several places on
+    c = rope_case(5000, 6, 2, D, D, torch.bfloat16, seed=6)
+    c["slots"][torch.rand(5000, generator=torch.Generator().manual_seed(7)) < 0.5] = -1
+    for pairs in ("halves", "neighbours"):
+        check_rope(c, pairs)
+
+
 def test_norm_rope_in_place_and_unaligned():
     c = rope_case(21, 6, 2, 64, 64, torch.bfloat16, seed=4)
     wide = torch.zeros(21, 10, 67, dtype=torch.bfloat16, device="cuda")           # rows that start on no 16 bytes
