@@ -88,7 +88,10 @@ bool tensor_map(CUtensorMap *map, const void *base, bool half, const int64_t (&s
     static const EncodeTiled encode = [] {
         void *f = nullptr;
         cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess) { cudaGetLastError(); return (EncodeTiled) nullptr; }
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess) {
+            cudaGetLastError();
+            return (EncodeTiled) nullptr;
+        }
         return found == cudaDriverEntryPointSuccess ? (EncodeTiled)f : nullptr;
     }();
     if (!encode) return false;
@@ -186,7 +189,6 @@ int32_t spec_norm_rope_cache(const SpecNormRope *a, void *stream)
     if (a->D < 8 || a->D > 256 || a->D % 8 || a->rot > a->D || a->rot % 16) return SPEC_ERR_UNSUPPORTED;
     rope::Params p = {};
     p.T = a->T; p.Hq = a->Hq; p.Hkv = a->Hkv; p.D = a->D; p.rot = a->rot; p.pairs = a->pairs;
-    while ((8 << p.lane_shift) < a->D) ++p.lane_shift;
     divisor(a->block_size, &p.block_mul, &p.block_shift);
     p.block = a->block_size; p.n_slots = (long long)a->num_blocks * a->block_size;
     p.x[0] = a->q; p.x[1] = a->k; p.x[2] = a->v;
@@ -206,15 +208,22 @@ int32_t spec_norm_rope_cache(const SpecNormRope *a, void *stream)
         all |= (a->k_cache_stride[j] | a->v_cache_stride[j]) * esz;
     }
     const bool vec = (all & 15) == 0;
-    const auto go = [&](auto kernel) {
+    // sixteen entries to a thread where rows and rotated parts are made of such and lie on 16 bytes: fewer addresses and steps of the norm's sum than
+    // with eight (6528 tokens of 48 heads of 128 entries: 39.4 us, with eight 40.6)
+    const bool wide = vec && a->D % 16 == 0 && a->rot % 32 == 0;
+    while (((wide ? 16 : 8) << p.lane_shift) < a->D) ++p.lane_shift;
+    const auto go = [&](auto kernel, int most) {
         const int rc = prepare(kernel, 0, false);
-        // as many CTAs as have room (four to an SM), each with as many tokens as the others
-        const int most = 148 * 4, each = (a->T + most - 1) / most;
+        // as many CTAs as have room, each with as many tokens as the others
+        const int each = (a->T + most - 1) / most;
         return rc ? rc : launch(kernel, dim3((a->T + each - 1) / each), rope::NT, 0, 0, (cudaStream_t)stream, p);
     };
-    if (a->dtype == SPEC_F32) return vec ? go(rope::spec_rope_kernel<float, true>) : go(rope::spec_rope_kernel<float, false>);
-    if (a->dtype == SPEC_F16) return vec ? go(rope::spec_rope_kernel<__half, true>) : go(rope::spec_rope_kernel<__half, false>);
-    return vec ? go(rope::spec_rope_kernel<__nv_bfloat16, true>) : go(rope::spec_rope_kernel<__nv_bfloat16, false>);
+#define GO(T)                                                                  \
+    (wide  ? go(rope::spec_rope_kernel<T, true, 16>, 148 * rope::CTAS<16>)        \
+     : vec ? go(rope::spec_rope_kernel<T, true, 8>, 148 * rope::CTAS<8>)          \
+           : go(rope::spec_rope_kernel<T, false, 8>, 148 * rope::CTAS<8>))
+    return a->dtype == SPEC_F32 ? GO(float) : a->dtype == SPEC_F16 ? GO(__half) : GO(__nv_bfloat16);
+#undef GO
 }
 
 static int attention_check(const SpecAttention *a)
@@ -228,7 +237,8 @@ static int attention_check(const SpecAttention *a)
     if (!(a->scale >= 0.f && a->scale <= 3.4e38f) || a->window < 0 || a->sinks < 0) return SPEC_ERR_PARAM;
     if (a->D != 64 && a->D != 128 && a->D != 256) return SPEC_ERR_UNSUPPORTED;
     // (tiles are counted in 32 bits)
-    const int64_t blocks = ((int64_t)a->N * (a->Hq / a->Hkv) + 127) / 128, keys = std::min<int64_t>((int64_t)a->table_width * a->block_size, 0x7FFFFFFF) + a->N;
+    const int64_t blocks = ((int64_t)a->N * (a->Hq / a->Hkv) + 127) / 128;
+    const int64_t keys = std::min<int64_t>((int64_t)a->table_width * a->block_size, 0x7FFFFFFF) + a->N;
     if ((double)a->B * a->Hkv * (double)blocks * (double)(keys / attend::KT + 2) > 2.0e9) return SPEC_ERR_UNSUPPORTED;
     int64_t all = 0;
     for (int j = 0; j < 3; ++j) all |= a->q_stride[j] | a->k_cache_stride[j] | a->v_cache_stride[j] | a->out_stride[j];
