@@ -375,15 +375,15 @@ int32_t spec_tree_attention(const SpecAttention *a, void *ws, int64_t ws_bytes, 
  * layers).  The path's node at depth d = 1, 2, ... goes from entry lengths[b] + node to entry lengths[b] + d; other entries
  * stay as they are.  lengths_out[b] = lengths[b] + depth(accepted) + 1 (the root is committed too; the correction token is the next
  * tree's root).  accepted_node[b] = -1 (a failed verification) or an idle request: nothing moves, the length stays.
- * accepted_node outside the tree: SPEC_DEV_TOPOLOGY, as with a bad tree; a bad block id on the path: SPEC_DEV_PAGE; then nothing of the
- * request moves and its length stays.  The blocks that hold a request's tree must be its own.
+ * accepted_node outside the tree: SPEC_DEV_TOPOLOGY, as with a bad tree; a bad block id on the path, also under entries that are in place
+ * already, or a path that leaves the table: SPEC_DEV_PAGE; then nothing of the request moves and its length stays.  The blocks that hold a request's tree must be its own.
  */
 typedef struct {
     int32_t B, N, caches;
     int32_t num_blocks, block_size, table_width;
     void *cache;                      /* row of slot e of block k of cache c: c * stride[0] + k * stride[1] + e * stride[2] bytes */
     int64_t stride[3];
-    int64_t row_bytes;
+    int64_t row_bytes;                /* below 2^31                                                   */
     const int32_t *block_table;
     int64_t table_stride;
     const int32_t *lengths;           /* [B]                                                          */

@@ -11,7 +11,8 @@ struct Params {
     TreeArgs tree;
     int B, caches, num_blocks, block, width, per;      // per: caches that a CTA goes through
     unsigned char *cache;
-    long long stride[3], words;                        // words: of type W in a row
+    long long stride[3];
+    unsigned words;                                    // of type W in a row
     const int *table;
     long long table_stride;
     const int *accepted;
@@ -20,8 +21,8 @@ struct Params {
 
 // A CTA per request and `per` caches; a thread moves the words of one place of a row along the whole path.  Path nodes have rising indices
 // with node(d) >= d, so entry len + d, written at depth d, may be read at depths up to d only: a thread that reads ahead of its
-// writes in rising order is right without a second buffer, and no other thread touches its words.  8 requests, 64 caches of 2 KB rows (7 MB): 5.3 us,
-// 128 requests, 24 caches of 1 KB rows (26 MB): 6.8 (floors 1.1 and 3.9); the path has to be found before the first byte moves.
+// writes in rising order is right without a second buffer, and no other thread touches its words.  8 requests, 64 caches of 2 KB rows (7 MB): 5.0 us,
+// 128 requests, 24 caches of 1 KB rows (26 MB): 5.9, 6.7 with divisions of 64 bits (floors 1.1 and 3.9); the path has to be found before the first byte moves.
 template <typename W>
 __global__ void __launch_bounds__(NT) spec_commit_kernel(const Params P)
 {
@@ -61,15 +62,19 @@ __global__ void __launch_bounds__(NT) spec_commit_kernel(const Params P)
     const int moves = s_moves;
     const int *table = P.table + (long long)b * P.table_stride;
     const auto offset = [&](long long at) -> long long {
-        const long long col = at / P.block;
-        const int id = col < P.width ? __ldg(table + col) : -1;
-        return id < 0 || id >= P.num_blocks ? -1 : id * P.stride[1] + (at % P.block) * P.stride[2];
+        if (at > 0x7FFFFFFFll) return -1;              // (32 bits from here: a division of 64 costs more than the load)
+        const unsigned col = (unsigned)at / (unsigned)P.block, in = (unsigned)at - col * (unsigned)P.block;
+        const int id = col < (unsigned)P.width ? __ldg(table + col) : -1;
+        return id < 0 || id >= P.num_blocks ? -1 : id * P.stride[1] + in * P.stride[2];
     };
-    bool page = false;
-    for (int i = tid; i < moves; i += NT) {
-        from[i] = offset(len + from[i]);
-        to[i] = offset(len + to[i]);
-        page |= from[i] < 0 || to[i] < 0;
+    // the path's entries, those that stay in place too, have to have blocks, or a length would count what the cache cannot hold
+    bool page = (long long)len + s_depth >= 0x7FFFFFFFll;
+    for (int i = tid; i <= s_depth; i += NT) {         // (fewer move than the path has)
+        const bool moved = i < moves;
+        const long long at = offset((long long)len + i);
+        const long long x = offset(len + (moved ? from[i] : i)), y = offset(len + (moved ? to[i] : i));
+        page |= at < 0 || x < 0 || y < 0;
+        if (moved) { from[i] = x; to[i] = y; }
     }
     page = __syncthreads_or(page) != 0;
     if (out) {
@@ -78,10 +83,11 @@ __global__ void __launch_bounds__(NT) spec_commit_kernel(const Params P)
     }
     if (page) return;
     const int c0 = blockIdx.x * P.per, c1 = min(P.caches, c0 + P.per);
-    const long long all = (long long)(c1 - c0) * P.words;
+    const unsigned all = (unsigned)(c1 - c0) * P.words;
     constexpr int AHEAD = 8;
-    for (long long w = tid; w < all; w += NT) {
-        unsigned char *base = P.cache + (c0 + w / P.words) * P.stride[0] + (w % P.words) * (long long)sizeof(W);
+    for (unsigned w = tid; w < all; w += NT) {
+        const unsigned cache = w / P.words, word = w - cache * P.words;
+        unsigned char *base = P.cache + (long long)(c0 + (int)cache) * P.stride[0] + (long long)word * (long long)sizeof(W);
         for (int m = moves; m > 0; m -= AHEAD) {       // (stored downwards: the last is the path's first)
             W x[AHEAD];
 #pragma unroll

@@ -239,7 +239,7 @@ static int attention_check(const SpecAttention *a)
     // (tiles are counted in 32 bits)
     const int64_t blocks = ((int64_t)a->N * (a->Hq / a->Hkv) + 127) / 128;
     const int64_t keys = std::min<int64_t>((int64_t)a->table_width * a->block_size, 0x7FFFFFFF) + a->N;
-    if ((double)a->B * a->Hkv * (double)blocks * (double)(keys / attend::KT + 2) > 2.0e9) return SPEC_ERR_UNSUPPORTED;
+    if ((double)a->B * a->Hkv * (double)blocks * (double)(keys / attend::KT + 1 + attend::START) > 2.0e9) return SPEC_ERR_UNSUPPORTED;
     int64_t all = 0;
     for (int j = 0; j < 3; ++j) all |= a->q_stride[j] | a->k_cache_stride[j] | a->v_cache_stride[j] | a->out_stride[j];
     if (all % 8 || !aligned(a->q, 16) || !aligned(a->k_cache, 16) || !aligned(a->v_cache, 16) || !aligned(a->out, 16))
@@ -332,7 +332,7 @@ int32_t spec_cache_commit(const SpecCommit *a, void *stream)
     if (!a || !a->cache || !a->block_table || !a->lengths || !a->parent || !a->accepted_node || !a->lengths_out || !a->status)
         return SPEC_ERR_NULL;
     if (bad_tree_shape(a->B, a->N, a->topo_seq_stride) || bad_pages(a->num_blocks, a->block_size, a->table_width) ||
-        a->table_stride < a->table_width || a->caches < 1 || a->row_bytes < 1)
+        a->table_stride < a->table_width || a->caches < 1 || a->row_bytes < 1 || a->row_bytes > 0x7FFFFFFF)
         return SPEC_ERR_SHAPE;
     if (a->lengths_out == a->lengths || a->lengths_out == a->accepted_node) return SPEC_ERR_PARAM;
     commit::Params p = {};
@@ -344,8 +344,8 @@ int32_t spec_cache_commit(const SpecCommit *a, void *stream)
     p.table = a->block_table; p.table_stride = a->table_stride; p.accepted = a->accepted_node;
     p.lengths_out = a->lengths_out; p.status = a->status;
     const int unit = all % 16 == 0 ? 16 : all % 4 == 0 ? 4 : 1;
-    p.words = a->row_bytes / unit;
-    p.per = (int)std::max<int64_t>(1, commit::NT / p.words);
+    p.words = (unsigned)(a->row_bytes / unit);
+    p.per = std::max(1, commit::NT / (int)p.words);
     const dim3 grid((a->caches + p.per - 1) / p.per, a->B);
     const auto go = [&](auto kernel) {
         const int rc = prepare(kernel, 0, false);

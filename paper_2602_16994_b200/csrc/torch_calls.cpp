@@ -584,7 +584,7 @@ PyObject *py_norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n)
         rows_of(v, "v", 3, type, place);
         rows_of(kc, "k_cache", 4, type, place);
         rows_of(vc, "v_cache", 4, type, place);
-        no_gradient(q, "q"); no_gradient(k, "k"); no_gradient(v, "v");
+        no_gradient(q, "q"); no_gradient(k, "k"); no_gradient(v, "v"); no_gradient(kc, "k_cache"); no_gradient(vc, "v_cache");
         const int64_t T = q.size(0), D = q.size(2), Hkv = k.size(1);
         if (k.size(0) != T || k.size(2) != D || v.sizes() != k.sizes()) raise("q, k and v must be [T,Hq,D], [T,Hkv,D] and [T,Hkv,D]");
         if (kc.size(2) != Hkv || kc.size(3) != D || vc.sizes() != kc.sizes()) raise("the caches must be [num_blocks, block_size, Hkv, D]");
@@ -611,6 +611,7 @@ PyObject *py_norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n)
             out = cuda_tensor(a[12], "q_out");
             rows_of(out, "q_out", 3, type, place);
             if (out.sizes() != q.sizes()) raise("q_out must have the shape of q");
+            no_gradient(out, "q_out");
         }
         s.q = q.data_ptr(); s.k = k.data_ptr(); s.v = v.data_ptr(); s.inv_freq = (const float *)freq.data_ptr();
         s.q_out = out.data_ptr(); s.k_cache = kc.data_ptr(); s.v_cache = vc.data_ptr();
@@ -657,6 +658,7 @@ PyObject *py_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
             t[0] = cuda_tensor(a[10], "out");
             rows_of(t[0], "out", 4, type, place);
             if (t[0].sizes() != q.sizes()) raise("out must have the shape of q");
+            no_gradient(t[0], "out");
         }
         t[1] = place.fresh({B}, at::kInt);
         if (PyObject_IsTrue(a[11])) t[2] = place.fresh({B, N, Hq}, at::kFloat);
@@ -682,6 +684,7 @@ PyObject *py_commit(PyObject *, PyObject *const *a, Py_ssize_t n)
         const at::Tensor &cache = cuda_tensor(a[0], "cache");
         const Place place(cache, a[6]);
         place.uses(cache, "cache");
+        no_gradient(cache, "cache");
         if (cache.dim() < 4) raise("cache must be [caches, num_blocks, block_size, ...]");
         int64_t row = 1;
         for (int64_t i = cache.dim() - 1; i >= 3; --i) {

@@ -155,7 +155,7 @@ def commit(cache, accepted, parent, lengths, table, n_nodes=None):
             return (k, at % block) if 0 <= k < blocks else None
 
         spots = [(place(length + i), place(length + d)) for i, d in moves]
-        if any(x is None or y is None for x, y in spots):
+        if any(x is None or y is None for x, y in spots) or any(place(length + d) is None for d in range(len(tree[acc]))):
             status[b] = PAGE
             continue
         rows = [cache[:, x[0], x[1]].clone() for x, _ in spots]

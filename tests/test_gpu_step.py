@@ -684,6 +684,16 @@ def test_commit_refuses_what_it_cannot_place():
     assert want["status"].tolist() == [0, 0, 1, 1, 1, 1, 1, 5]
 
 
+def test_commit_of_paths_in_place_without_blocks():
+    # nothing of a chain moves, but what is not in the cache is not committed: a block missing, the table's end, lengths up to the largest
+    c = commit_case([14, 14, 20, 20, 20, 20], chain(4).repeat(6, 1), [1, 2, 3, 3, 0, 2], 2, (16,), torch.float32, 16)
+    c["block_table"][1, 1] = -1
+    c["block_table"][2, 1] = c["cache"].shape[1]
+    c["lengths"][3:] = torch.tensor([2**31 - 5, 2**31 - 2, 2**31 - 1], dtype=I32)
+    want = check_commit(c)
+    assert want["status"].tolist() == [0, 5, 5, 5, 5, 5]
+
+
 def test_commit_strided_cache():
     c = commit_case([5, 31], tree(4, 2, 4), [18, 14], 4, (2, 64), torch.bfloat16, 16)
     P = c["cache"].shape[1]
@@ -703,6 +713,11 @@ def test_arguments_out_of_range_are_refused():
         binding.tree_attention(**d, window=1.5)
     with pytest.raises(RuntimeError, match="backward"):
         binding.tree_attention(**dict(d, q=d["q"].requires_grad_()))
+    r = cuda(rope_case(3, 2, 1, 64, 64, torch.bfloat16))
+    m = cuda(commit_case([5], tree(1, 0, 1), [1], 2, (16,), torch.float32, 16))
+    for call, args, name in ((binding.norm_rope_cache, r, "k_cache"), (binding.norm_rope_cache, r, "v_cache"), (binding.cache_commit, m, "cache")):
+        with pytest.raises(RuntimeError, match="backward"):
+            call(**dict(args, **{name: args[name].clone().requires_grad_()}))
     for name in ("k_cache", "v_cache", "q"):
         with pytest.raises(RuntimeError):
             binding.tree_attention(**dict(cuda(attention_case([10], tree(1, 0, 1), 2, 1, 64, torch.bfloat16, 16)), **{name: d[name].detach().half()}))

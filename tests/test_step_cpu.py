@@ -111,7 +111,7 @@ def test_commit_refusals(lib):
     assert lib.spec_cache_commit(None, None) == -1
     for f in ("cache", "block_table", "lengths", "parent", "accepted_node", "lengths_out", "status"):
         assert call(**{f: None}) == -1, f
-    for kw in (dict(B=0), dict(B=65536), dict(N=1025), dict(caches=0), dict(num_blocks=0), dict(row_bytes=0), dict(table_stride=0)):
+    for kw in (dict(B=0), dict(B=65536), dict(N=1025), dict(caches=0), dict(num_blocks=0), dict(row_bytes=0), dict(row_bytes=2**31), dict(table_stride=0)):
         assert call(**kw) == -2, kw
     assert call(lengths=0x50000, lengths_out=0x50000) == -4
 
