@@ -21,8 +21,9 @@ struct Params {
 
 // A CTA per request and `per` caches; a thread moves the words of one place of a row along the whole path.  Path nodes have rising indices
 // with node(d) >= d, so entry len + d, written at depth d, may be read at depths up to d only: a thread that reads ahead of its
-// writes in rising order is right without a second buffer, and no other thread touches its words.  8 requests, 64 caches of 2 KB rows (7 MB): 5.0 us,
-// 128 requests, 24 caches of 1 KB rows (26 MB): 5.9, 6.7 with divisions of 64 bits (floors 1.1 and 3.9); the path has to be found before the first byte moves.
+// writes in rising order is right without a second buffer, and no other thread touches its words.  8 requests, 64 caches of 2 KB rows
+// (7 MB): 5.0 us; 128 requests, 24 caches of 1 KB rows (26 MB): 5.9, with divisions of 64 bits 6.7 (floors 1.1 and 3.9); the path has to be
+// found before the first byte moves.
 template <typename W>
 __global__ void __launch_bounds__(NT) spec_commit_kernel(const Params P)
 {
