@@ -2,6 +2,8 @@
 #pragma once
 #include <cooperative_groups.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 
 namespace specv {
@@ -13,8 +15,8 @@ namespace cg = cooperative_groups;
 // chain stopped at: the sums of tiles of 512 weights stay in shared memory, the slices' sums are exchanged, and the CTA that the
 // target falls into finds the tile and reads it once more.  Weights, sums and comparisons are fp64: fp32 sums over 1e5 weights would move the
 // borders between tokens by more than the tokens' own masses.  The bytes of one row of p and of q per request are the floor: 8 requests of
-// 128256 entries take 8.4 us (floor 1.3: the walk, the row, its exchange and the tile are four rounds of latency), 128 looked-up ones of 151936 entries
-// 23 (floor 12).
+// 128256 entries take 8.3 us (floor 1.3: the walk, the row, its exchange and the tile are four rounds of latency), 128 looked-up ones of 151936 entries
+// 22.5 (floor 12; 24.4 with q's zeros converted and subtracted too: a conversion to 64 bits costs several of the other instructions).
 constexpr int NT = 256, WARPS = NT / 32, TILE = 512, TILES = 1024, CMAX = 16;      // a tile: four loads of 128 entries by a warp
 
 struct Params {
@@ -47,10 +49,10 @@ template <typename T> struct Rows {
     const T *p, *q;
     int hole;
     bool vec;
-    __device__ __forceinline__ void raw(int t, int end, float4 &a, float4 &b) const
+    template <bool Q> __device__ __forceinline__ void raw(int t, int end, float4 &a, float4 &b) const
     {
         a = entries(p, t, end, vec);
-        b = q ? entries(q, t, end, vec) : make_float4(0.f, 0.f, 0.f, 0.f);
+        b = Q && q ? entries(q, t, end, vec) : make_float4(0.f, 0.f, 0.f, 0.f);
         if (hole >= t && hole < t + 4) {
             if (hole == t) a.x = 0.f;
             if (hole == t + 1) a.y = 0.f;
@@ -59,14 +61,15 @@ template <typename T> struct Rows {
         }
     }
     // (compared in fp32, where p > q means the same; NaN stays)
-    static __device__ __forceinline__ double weight(float p, float q)
+    template <bool Q> static __device__ __forceinline__ double weight(float p, float q)
     {
+        if constexpr (!Q) return (double)(p <= 0.f ? 0.f : p);
         const bool none = p <= q;
         return (double)(none ? 0.f : p) - (double)(none ? 0.f : q);
     }
-    static __device__ __forceinline__ double sum(const float4 &a, const float4 &b)
+    template <bool Q> static __device__ __forceinline__ double sum(const float4 &a, const float4 &b)
     {
-        return (weight(a.x, b.x) + weight(a.y, b.y)) + (weight(a.z, b.z) + weight(a.w, b.w));
+        return (weight<Q>(a.x, b.x) + weight<Q>(a.y, b.y)) + (weight<Q>(a.z, b.z) + weight<Q>(a.w, b.w));
     }
 };
 
@@ -137,16 +140,22 @@ template <typename T> __global__ void __launch_bounds__(NT) spec_chain_kernel(co
         // (the second round: what was left of p is 0 everywhere, the draw is from p)
         for (int round = 0; round < 2; ++round) {
             rows.vec = (((uintptr_t)rows.p | (uintptr_t)rows.q) & (4 * sizeof(T) - 1)) == 0;
-            for (int i = warp; i < tiles; i += WARPS) {
-                const int t = t0 + i * TILE + lane * 4;
-                float4 x[4], y[4];
+            const auto sums = [&](auto with_q) {         // (a loop of its own without q: half of the conversions to 64 bits)
+                constexpr bool Q = decltype(with_q)::value;
+                for (int i = warp; i < tiles; i += WARPS) {
+                    const int t = t0 + i * TILE + lane * 4;
+                    float4 x[4], y[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) rows.raw(t + k * 128, end, x[k], y[k]);
-                double s = (rows.sum(x[0], y[0]) + rows.sum(x[1], y[1])) + (rows.sum(x[2], y[2]) + rows.sum(x[3], y[3]));
+                    for (int k = 0; k < 4; ++k) rows.template raw<Q>(t + k * 128, end, x[k], y[k]);
+                    double s = (rows.template sum<Q>(x[0], y[0]) + rows.template sum<Q>(x[1], y[1])) +
+                               (rows.template sum<Q>(x[2], y[2]) + rows.template sum<Q>(x[3], y[3]));
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                if (lane == 0) tile[i] = s;
-            }
+                    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                    if (lane == 0) tile[i] = s;
+                }
+            };
+            if (rows.q) sums(std::true_type());
+            else sums(std::false_type());
             __syncthreads();
             // a run of tiles per lane (of every warp alike: the slice's sum is needed by all)
             mine = 0.0;
@@ -192,8 +201,9 @@ template <typename T> __global__ void __launch_bounds__(NT) spec_chain_kernel(co
                     for (int k = 0; k < TILE; k += 128) {
                         const int t = t0 + ti * TILE + k + lane * 4;
                         float4 x, y;
-                        rows.raw(t, end, x, y);
-                        const double w[4] = {rows.weight(x.x, y.x), rows.weight(x.y, y.y), rows.weight(x.z, y.z), rows.weight(x.w, y.w)};
+                        rows.template raw<true>(t, end, x, y);
+                        const double w[4] = {rows.template weight<true>(x.x, y.x), rows.template weight<true>(x.y, y.y),
+                                             rows.template weight<true>(x.z, y.z), rows.template weight<true>(x.w, y.w)};
                         const double mine4 = (w[0] + w[1]) + (w[2] + w[3]), sum4 = warp_sum(mine4);
                         const int who = first_above(mine4, rest, tau3);
                         if (who < 0) continue;
