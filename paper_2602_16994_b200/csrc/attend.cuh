@@ -309,7 +309,7 @@ struct Bars {
     uint64_t full[16], empty[16];
     uint64_t q_full, q_empty, s_full[4], p_full[4], pv_done[2], o_empty[2];
     uint32_t tmem;
-    int dead, poison;
+    int dead, poison, bad_tree;                // (bad_tree: of the request that the rows' parents were read for last)
     uint32_t hidden[8][4];                     // keys of a tile on bad blocks, by the tile's number in the CTA's run % 8
     uint32_t plain[8];                         // a byte per warp that copies: whether it stored (part of) the tile by itself
     int found[2], sums[16];
@@ -537,6 +537,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         }
         B->dead = 0;
         B->poison = 0;
+        B->bad_tree = 0;
         mbar_fence_init();
     }
     grid_dependency_wait();
@@ -571,11 +572,13 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             const int r = seg.m * S::ROWS + row, node = node_of(P, min(r, seg.r.rows - 1));
             const bool live = row < seg.rows, warp_live = t * 128 + quad * 32 < seg.rows;
             if (tree_of != seg.b && (tree_of < 0 || P.tree.topo_seq_stride || P.tree.n_nodes)) {
+                if (tid == 0) B->bad_tree = 0;
                 bar_sync(1 + w, 128);
                 const int *from = P.tree.parent + (long long)seg.b * P.tree.topo_seq_stride;
                 for (int i = gt; i < seg.r.n; i += 128) {
                     const int p = __ldg(from + i);
                     parent[i] = p >= 0 && p < i ? (unsigned short)p : (unsigned short)0xFFFF;
+                    if (w == 0 && (i == 0 ? p != -1 : p < 0 || p >= i)) *(volatile int *)&B->bad_tree = 1;
                 }
                 tree_of = seg.b;
                 bar_sync(1 + w, 128);
@@ -1013,10 +1016,11 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         tc::tmem_free(tmem, 512);
         if (lane == 0) {
             P.late[c] = B->dead;
-            // the first of a unit's parts tells what there is to join
+            // The first of a unit's parts tells what there is to join, unless the tree is bad: zeros for its rows come from the request's CTA of the
+            // joining kernel, and nothing else of that kernel may write them.  (The unit is this run's last, so its tree is the one read last.)
             const Segment &seg = hand->seg[0];
             int4 joint = make_int4(0, 0, 0, 0);
-            if (hand->segments && seg.begin == 0 && !seg.whole) {
+            if (hand->segments && seg.begin == 0 && !seg.whole && !B->bad_tree) {
                 // (the unit's end, from what of it lies in this run)
                 const int end = cuts.start(c + 1) + seg.t.count() - seg.end;
                 int last = c + 1;

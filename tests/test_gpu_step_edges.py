@@ -1,0 +1,53 @@
+"""The operators around a verification where two of their threads, calls or results could be at odds: one writer to a row, flags that
+travel with their data, waits that run out, scores and probabilities at the ends of their range, steps that were refused."""
+import math
+
+import pytest
+import torch
+
+from . import step_ref as ref
+from .test_gpu_step import I32, attention_case, chain, check_attention, cuda, tree
+from paper_2602_16994_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------------------------------------
+# tree_attention: rows of a bad tree have one writer
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("shape,Hq,Hkv,D", [((0, 0, 0), 8, 2, 128), ((4, 2, 4), 8, 2, 128), ((8, 2, 6), 32, 8, 128), ((8, 2, 6), 8, 1, 64),
+                                            ((4, 2, 4), 4, 2, 256)])
+@pytest.mark.parametrize("lengths", [[3000], [20000], [2500, 300, 4000, 0]])
+def test_rows_of_a_bad_tree_are_zeros_where_units_are_cut(shape, Hq, Hkv, D, lengths):
+    """Some thousand keys to a unit are cut into runs and joined; the joined rows of a bad tree must not come on top of its zeros."""
+    parent = (tree(*shape) if shape[2] else chain(1)).repeat(len(lengths), 1)
+    c = attention_case(lengths, parent, Hq, Hkv, D, torch.bfloat16, 16, seed=21)
+    bad = [b for b, n in enumerate(lengths) if n >= 2500]
+    for b in bad:
+        c["parent"][b, -1] = parent.shape[1]                      # (of one node: a root with a parent)
+    want = ref.attention(**c)
+    assert [b for b, s in enumerate(want["status"].tolist()) if s == ref.TOPOLOGY] == bad
+    for _ in range(10):
+        got = check_attention(c, want)
+        assert bool((got.out[bad] == 0).all()) and bool((got.lse[bad] == -math.inf).all())
+
+
+def test_a_bad_tree_for_all_requests():
+    c = attention_case([5000, 900, 40], tree(4, 2, 4), 8, 2, 128, torch.bfloat16, 16, seed=22)
+    c["parent"][7] = 7
+    for _ in range(10):
+        got = check_attention(c)
+        assert got.status.tolist() == [1, 1, 1] and bool((got.out == 0).all()) and bool((got.lse == -math.inf).all())
+
+
+def test_a_bad_tree_before_and_behind_good_ones_of_a_run():
+    """Requests of a few tiles, several to a run: what is known of one request's tree is not taken for the next one's."""
+    g = torch.Generator().manual_seed(23)
+    lengths = torch.randint(0, 700, (70,), generator=g).tolist()
+    parent = tree(4, 2, 4).repeat(70, 1)
+    c = attention_case(lengths, parent, 8, 2, 128, torch.bfloat16, 16, seed=24, n_nodes=torch.randint(3, 20, (70,), generator=g).tolist())
+    c["parent"][torch.rand(70, generator=g) < 0.4, 2] = 2
+    want = ref.attention(**c)
+    assert 10 < int((want["status"] == ref.TOPOLOGY).sum()) < 60
+    for _ in range(5):
+        check_attention(c, want)
