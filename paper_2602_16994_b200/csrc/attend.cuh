@@ -296,6 +296,7 @@ template <int D_, int MT_, int WG_> struct Shape {
     static constexpr int SLOTS = D == 64 ? 10 : MT == 2 || D == 256 ? 4 : 5;      // slots in flight
     static constexpr int SOFT = 4 * WG, WARPS = SOFT + WG + 4, NT = WARPS * 32;   // warps: rows, products (one per row warpgroup), copies
     static constexpr int NP = 128;                                                // threads that copy
+    static constexpr int FILLED = NP + 4;                                         // arrivals that fill a slot: theirs, and one more per warp, see filled()
     static constexpr int O = 256;                                                 // column of the first O; S buffers at 0 and 128
     static constexpr int off_slots = ROWS * D * 2;
     static constexpr int off_parent = off_slots + SLOTS * SLOT;                  // one array of parents per row warpgroup
@@ -527,7 +528,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
     if (warp == S::SOFT) tc::tmem_alloc(&B->tmem, 512);
     if (tid == S::NT - 1 && P.box) { tc::prefetch_map(&P.k_map); tc::prefetch_map(&P.v_map); }
     if (tid == 0) {
-        for (int i = 0; i < S::SLOTS; ++i) { mbar_init(&B->full[i], S::NP); mbar_init(&B->empty[i], MT); }
+        for (int i = 0; i < S::SLOTS; ++i) { mbar_init(&B->full[i], S::FILLED); mbar_init(&B->empty[i], MT); }
         mbar_init(&B->q_full, S::NP);
         mbar_init(&B->q_empty, S::WG);
         for (int t = 0; t < 4; ++t) { mbar_init(&B->s_full[t], 1); mbar_init(&B->p_full[t], 4); }
@@ -869,6 +870,9 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         const auto place = [&](uint32_t slot, int row, int chunk) {
             return (slot + chunk / (8 * S::WIDE)) % S::SLOTS * S::SLOT + chunk / 8 % S::WIDE * PANEL + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
         };
+        // The warp's own arrival, by the thread that wrote the tile's `hidden` and `plain`: an arrival that copies make when they are done says nothing
+        // of what their thread stored beside them.
+        const auto filled = [&](uint64_t *bar) { if (lane == 0) mbar_arrive(bar); };
         const auto clean = [&]() {
 #pragma unroll 1
             for (int i = 0; i < CH; ++i) {
@@ -887,7 +891,11 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                 if (bad) { *(uint4 *)at = v; *(volatile int *)&B->poison = 1; }
             }
             tc::publish_shared();
-            for (int p = 0; p < S::STEP; ++p) mbar_arrive(&B->full[(late_slot + p) % S::SLOTS]);
+            for (int p = 0; p < S::STEP; ++p) {
+                uint64_t *bar = &B->full[(late_slot + p) % S::SLOTS];
+                mbar_arrive(bar);
+                filled(bar);
+            }
             late_values = false;
         };
         // a wait for room: values that are held back may be what the room is waiting for
@@ -923,7 +931,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                     for (int p = 0; p < S::STEP; ++p) {
                         uint64_t *bar = &B->full[(n + p) % S::SLOTS];
                         tc::expect_bytes(bar, 32 * 128 * S::WIDE);
-                        tc::arrive_many(bar, 32);
+                        tc::arrive_many(bar, S::FILLED / 4);
                     }
                 }
                 const int boxes = 32 / P.box, g = lane % boxes, p = lane / boxes;
@@ -945,7 +953,11 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                 }
                 hold = values && !x.whole;
                 if (!hold)
-                    for (int p = 0; p < S::STEP; ++p) tc::arrive_with_copies(&B->full[(n + p) % S::SLOTS]);
+                    for (int p = 0; p < S::STEP; ++p) {
+                        uint64_t *bar = &B->full[(n + p) % S::SLOTS];
+                        tc::arrive_with_copies(bar);
+                        filled(bar);
+                    }
             }
             tc::close_copies();
             if (late_values) { tc::wait_copies<1>(); clean(); }

@@ -51,3 +51,26 @@ def test_a_bad_tree_before_and_behind_good_ones_of_a_run():
     assert 10 < int((want["status"] == ref.TOPOLOGY).sum()) < 60
     for _ in range(5):
         check_attention(c, want)
+
+
+# ---------------------------------------------------------------------------------------------
+# tree_attention: what is noted of a tile arrives with it
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("D,heads,parent", [(128, (8, 2), tree(4, 2, 4)), (64, (6, 1), tree(8, 2, 6)), (128, (32, 8), tree(8, 2, 6)),
+                                            (256, (4, 2), chain(1)), (64, (7, 1), chain(1))])
+@pytest.mark.parametrize("block", [16, 24, 7])
+def test_bad_blocks_in_many_tiles(D, heads, parent, block):
+    """Tiles that hold bad blocks between tiles that do not, more of them than the notes of tiles under way have places: the keys that count as seen,
+    and the copies that have to be told to the tensor cores, are those of the tile at hand, every time."""
+    g = torch.Generator().manual_seed(D + block)
+    c = attention_case([2600, 4100, 900], parent, *heads, D, torch.bfloat16, block, seed=D)
+    used = -(-c["lengths"] // block)
+    for b in range(3):
+        hit = (torch.rand(int(used[b]) - 1, generator=g) < 0.05).nonzero().flatten()
+        c["block_table"][b, hit] = torch.where(torch.rand(len(hit), generator=g) < 0.5, -1, 2**31 - 1).int()
+    want = ref.attention(**c)
+    assert want["status"].tolist() == [ref.PAGE] * 3
+    first = check_attention(c, want)
+    for _ in range(10):
+        again = check_attention(c, want)
+        assert torch.equal(first.out, again.out) and torch.equal(first.lse, again.lse)
