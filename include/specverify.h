@@ -343,6 +343,7 @@ int32_t spec_norm_rope_cache(const SpecNormRope *a, void *stream);
  * A row that sees nothing (a block id outside [0, num_blocks) hides its keys and gives SPEC_DEV_PAGE) is 0, its lse -inf; so are all
  * rows of a request with a bad tree (SPEC_DEV_TOPOLOGY).  What no node sees is not read; what a node does not see does not
  * reach its row, whatever it holds (NaN and infinities too).  Rows of idle requests and of nodes beyond n_nodes[b] stay as they were.
+ * SPEC_DEV_TIMEOUT (a wait ran out, in any request's part of the work): the rows of the call's requests are undefined.
  * D: 64, 128 or 256.  q, caches and out of one type, SPEC_BF16 or SPEC_F16.  Strides in elements, multiples of 8, and bases on 16 bytes;
  * the D entries of a head are contiguous; out overlaps no input.  lse: optional, log of sum_j exp(scale q.k_j) (natural).
  * `ws`: spec_tree_attention_workspace_bytes() bytes (a function of the sizes; contents do not matter).
@@ -442,7 +443,8 @@ int64_t spec_kernel_launches(void);
  * is bounded (Section "General rules": a wait that runs out is reported as SPEC_DEV_TIMEOUT, nothing
  * hangs); these two settings let a test watch that happen.  wait_cycles: the limit of every on-device
  * wait in clock cycles (<= 0: the default, about 2 s).  hold_slot: index b * N + node of one node whose
- * Traversal weight the node kernels then never publish, so that the node's own wait runs out
+ * Traversal weight the node kernels then never publish, so that the node's own wait runs out, and whose
+ * sequence's queries the tree attention then never fetches, so that its waits for them do
  * (-1: none).  Synchronous (copies to constant memory of the current device); call it between
  * verification calls, never while one is in flight.
  */

@@ -153,7 +153,7 @@ def _stream_ptr(stream):
 
 def set_test_hooks(wait_cycles: int = 0, hold_slot: int = -1):
     """Test hooks: limit of the on-device waits in clock cycles (0: default) and one Traversal weight slot
-    (index b * N + node) that is left pending (-1: none)."""
+    (index b * N + node) that is left pending, or sequence whose queries the tree attention never fetches (-1: none)."""
     _check(load_library().spec_test_hooks(int(wait_cycles), int(hold_slot)), "spec_test_hooks")
 
 

@@ -322,11 +322,14 @@ __device__ __forceinline__ void wait(Bars *B, uint64_t *bar, uint32_t parity)
 {
     if (mbar_try_wait(bar, parity)) return;
     const long long t0 = clock64();
-    while (!mbar_try_wait(bar, parity)) {
+    do {
         if (*(volatile int *)&B->dead) return;
         if (clock64() - t0 > WAIT_CYCLES) { *(volatile int *)&B->dead = 1; return; }
-    }
+    } while (!mbar_try_wait(bar, parity));
 }
+
+// Whether a wait has run out, one answer for the whole (converged) warp: what follows is done by all of its threads or by none.
+__device__ __forceinline__ bool stopped(Bars *B) { return __any_sync(0xffffffffu, *(volatile int *)&B->dead) != 0; }
 
 __device__ __forceinline__ bool mbar_test(uint64_t *bar, uint32_t parity)
 {
@@ -736,10 +739,11 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             if (*(volatile uint32_t *)&B->plain[i & 7]) tc::publish_shared();
             tc::fence_after();
         };
-        // S of row block t for part h of a tile into columns `to`, from the keys in slots k ..; `bar`: where that is told
+        // (asked by the one thread that issues, behind the choice of it, which takes the whole warp)
         const auto gone = [&] { return *(volatile int *)&B->dead != 0; };
+        // S of row block t for part h of a tile into columns `to`, from the keys in slots k ..; `bar`: where that is told
         const auto scores = [&](int t, int h, int to, uint32_t k, uint64_t *bar, bool release) {
-            if (!gone() && tc::elected()) {
+            if (tc::elected() && !gone()) {
 #pragma unroll
                 for (int p = 0; p < S::STEP; ++p) {
                     const uint32_t slot = (k + p) % S::SLOTS;
@@ -758,7 +762,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         };
         // O number o (+)= P (in columns `from`) V for part h of a tile, from the values in slots k ..
         const auto sums = [&](int o, int h, int from, uint32_t k, bool add, bool release) {
-            if (!gone() && tc::elected()) {
+            if (tc::elected() && !gone()) {
 #pragma unroll
                 for (int p = 0; p < S::STEP; ++p) {
                     const uint32_t slot = (k + p) % S::SLOTS;
@@ -773,7 +777,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             __syncwarp();
         };
         const auto let_go = [&](uint64_t *bar) {
-            if (!gone() && tc::elected()) tc::commit(bar);
+            if (tc::elected() && !gone()) tc::commit(bar);
             __syncwarp();
         };
         // (the slots' order: K0, V0, K1, V1, ...)
@@ -924,7 +928,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                 const uint32_t k = n + p;
                 if (k >= S::SLOTS) room(&B->empty[k % S::SLOTS], (k / S::SLOTS - 1) & 1);
             }
-            if (*(volatile int *)&B->dead) { n += S::STEP; return; }
+            if (stopped(B)) { n += S::STEP; return; }
             bool hold = false;
             if (by_map) {
                 if (lane == 0) {
@@ -967,7 +971,8 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         const auto copy_q = [&](const Segment &s) {
             if (n_seg) room(&B->q_empty, (n_seg - 1) & 1);
             ++n_seg;
-            if (*(volatile int *)&B->dead) return;
+            if (stopped(B)) return;
+            if (c_hold_slot >= 0 && c_hold_slot / P.tree.N == s.b) return;       // (a test may ask for a request's queries to stay away)
             if (P.q_boxes) {
                 // (nodes beyond N come as zeros)
                 if (part == 0 && lane == 0) {

@@ -772,7 +772,7 @@ int32_t spec_test_hooks(int64_t wait_cycles, int32_t hold_slot)
         cudaGetLastError();
         return SPEC_ERR_CUDA;
     }
-    return set_step_wait(wc);
+    return set_step_hooks(wc, hs);
 }
 
 int32_t spec_row_statistics(const SpecIn *in, void *ws, int64_t ws_bytes, void *stream)

@@ -145,9 +145,13 @@ bool aligned(const void *p, int64_t n) { return ((uintptr_t)p & (uintptr_t)(n - 
 
 }  // namespace
 
-int set_step_wait(long long cycles)
+int set_step_hooks(long long cycles, int hold)
 {
-    if (cudaMemcpyToSymbol(c_wait_cycles, &cycles, sizeof(cycles)) != cudaSuccess) { cudaGetLastError(); return SPEC_ERR_CUDA; }
+    if (cudaMemcpyToSymbol(c_wait_cycles, &cycles, sizeof(cycles)) != cudaSuccess ||
+        cudaMemcpyToSymbol(c_hold_slot, &hold, sizeof(hold)) != cudaSuccess) {
+        cudaGetLastError();
+        return SPEC_ERR_CUDA;
+    }
     return SPEC_OK;
 }
 

@@ -11,6 +11,8 @@ from paper_2602_16994_b200 import binding
 
 pytestmark = pytest.mark.gpu
 
+TIMEOUT = 4
+
 
 # ---------------------------------------------------------------------------------------------
 # tree_attention: rows of a bad tree have one writer
@@ -74,3 +76,32 @@ def test_bad_blocks_in_many_tiles(D, heads, parent, block):
     for _ in range(10):
         again = check_attention(c, want)
         assert torch.equal(first.out, again.out) and torch.equal(first.lse, again.lse)
+
+
+# ---------------------------------------------------------------------------------------------
+# tree_attention: a wait that runs out
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("D,heads,parent", [(128, (8, 2), tree(4, 2, 4)), (128, (32, 8), tree(8, 2, 6)), (64, (7, 1), chain(1)),
+                                            (256, (4, 2), tree(4, 2, 4))])
+@pytest.mark.parametrize("block", [16, 7])
+def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right(D, heads, parent, block):
+    """One request's queries are never fetched (the library's test hook) and every wait gives up after 2e6 cycles, about a millisecond: the call
+    comes back with SPEC_DEV_TIMEOUT, and what follows is as if nothing had been."""
+    c = attention_case([2000, 300, -1, 40], parent.repeat(4, 1), *heads, D, torch.bfloat16, block, seed=D)
+    c["parent"][3, -1] = parent.shape[0]
+    want, d = ref.attention(**c), cuda(c)
+    out = torch.full_like(d["q"], 7.0)
+    try:
+        binding.set_test_hooks(wait_cycles=2_000_000, hold_slot=1 * parent.shape[0])
+        t0, t1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        t0.record()
+        got = binding.tree_attention(**d, out=out, want_lse=True)
+        t1.record()
+        torch.cuda.synchronize()
+        assert t0.elapsed_time(t1) < 500.0                        # milliseconds: bounded
+        assert got.status.tolist() == [TIMEOUT, TIMEOUT, 0, ref.TOPOLOGY]
+        assert bool((out[2] == 7.0).all()) and bool((out[3] == 0).all())
+    finally:
+        binding.set_test_hooks(0, -1)
+    for _ in range(3):
+        check_attention(c, want)
