@@ -71,7 +71,7 @@ def test_bad_blocks_in_many_tiles(D, heads, parent, block):
         hit = (torch.rand(int(used[b]) - 1, generator=g) < 0.05).nonzero().flatten()
         c["block_table"][b, hit] = torch.where(torch.rand(len(hit), generator=g) < 0.5, -1, 2**31 - 1).int()
     want = ref.attention(**c)
-    assert want["status"].tolist() == [ref.PAGE] * 3
+    assert want["status"].tolist()[:2] == [ref.PAGE] * 2          # (the short one may have drawn none)
     first = check_attention(c, want)
     for _ in range(10):
         again = check_attention(c, want)
