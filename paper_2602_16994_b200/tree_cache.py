@@ -9,7 +9,8 @@ One step of the loop, for requests whose trees share ``parent`` (Section 2, step
     out = binding.verify_specinfer(...)                   # or another verifier
     cache.commit(out.accepted_node)                       # the accepted paths stay
 
-Nothing synchronises; lengths, tables and free blocks live on the device and are replaced by the calls' results.
+Nothing synchronises; lengths, tables and free blocks live on the device.  ``lengths``, ``owned`` and ``free_range`` are replaced by the
+calls' results: a step captured into a graph is the same step at every replay, unless its results are copied into the tensors that it read.
 """
 from __future__ import annotations
 
@@ -22,7 +23,8 @@ class TreeCache:
     """Caches of ``layers`` layers, a block table of ``width`` columns per request, and a ring of free blocks.
 
     ``storage`` is [2 * layers, num_blocks, block_size, Hkv, D]: keys of layer l at 2 * l, values behind them.  A request whose
-    length is set negative takes no part in the calls; its blocks are the caller's to put back (``release``).
+    length is set negative takes no part in the calls; its blocks are the caller's to put back (``release``).  A row that ``release`` has
+    emptied takes a new request with ``lengths[row] = 0``.
     """
 
     def __init__(self, batch, layers, num_blocks, block_size, Hkv, D, width, dtype=torch.bfloat16, device="cuda"):
@@ -54,8 +56,23 @@ class TreeCache:
                                       self.n_nodes, **kw)
 
     def commit(self, accepted_node, stream=None):
-        """The accepted paths' entries behind the committed tokens, in all layers; new lengths."""
-        done = binding.cache_commit(self.storage, accepted_node, self.parent, self.lengths, self.block_table, self.n_nodes, stream)
+        """The accepted paths' entries behind the committed tokens, in all layers; new lengths.  A request whose ``begin`` was refused
+        (``step.status``) keeps its length: nothing of its tree was written, though its last block may have room for the path."""
+        status = self.step.status
+        if stream is None:
+            accepted = accepted_node.masked_fill(status != 0, -1)
+            done = binding.cache_commit(self.storage, accepted, self.parent, self.lengths, self.block_table, self.n_nodes)
+            done.status = torch.maximum(done.status, status)
+        else:                                            # (the allocator is told of both streams, as the calls tell it)
+            side, current = torch.cuda.ExternalStream(stream.cuda_stream, status.device), torch.cuda.current_stream(status.device)
+            with torch.cuda.stream(side):
+                accepted = accepted_node.masked_fill(status != 0, -1)
+            accepted_node.record_stream(side)
+            done = binding.cache_commit(self.storage, accepted, self.parent, self.lengths, self.block_table, self.n_nodes, stream)
+            with torch.cuda.stream(side):
+                done.status = torch.maximum(done.status, status)
+            status.record_stream(side)
+            done.status.record_stream(current)
         self.lengths = done.lengths
         return done
 

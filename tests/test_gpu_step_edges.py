@@ -8,6 +8,7 @@ import torch
 from . import step_ref as ref
 from .test_gpu_step import I32, attention_case, chain, check_attention, cuda, tree
 from paper_2602_16994_b200 import binding
+from paper_2602_16994_b200.tree_cache import TreeCache
 
 pytestmark = pytest.mark.gpu
 
@@ -105,3 +106,59 @@ def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right(D, heads, p
         binding.set_test_hooks(0, -1)
     for _ in range(3):
         check_attention(c, want)
+
+
+# ---------------------------------------------------------------------------------------------
+# TreeCache: a pool that runs dry
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("side", [False, True])
+def test_a_pool_that_runs_dry_in_mid_loop(side):
+    """Refused steps are not committed, and the steps behind a release are right: entries and attention are those of a program that keeps every
+    request's tokens in a list."""
+    g = torch.Generator().manual_seed(3)
+    B, block, blocks, Hq, Hkv, D = 3, 8, 9, 4, 2, 64
+    parent = tree(3, 0, 3)
+    N, tree_paths = len(parent), ref.paths(parent.tolist())
+    cache = TreeCache(B, 1, blocks, block, Hkv, D, width=8)
+    cache.storage.normal_()
+    kept, refused, parent_d = [[] for _ in range(B)], 0, parent.cuda()
+    stream = torch.cuda.Stream() if side else None
+    torch.cuda.synchronize()
+    for step in range(14):
+        if step == 9:
+            cache.release(2)
+            kept[2] = []
+        if step == 11:
+            cache.lengths[2] = 0                                 # a new request
+        torch.cuda.synchronize()
+        s = cache.begin(parent_d, stream=stream)
+        qkv = torch.randn(B * N, Hq + 2 * Hkv, D, generator=g).to(torch.bfloat16).cuda()
+        torch.cuda.synchronize()
+        q = cache.write(0, qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:], torch.full((D // 2,), 0.01, device="cuda"), stream=stream)
+        out = cache.attend(0, q.view(B, N, Hq, D), stream=stream)
+        torch.cuda.synchronize()
+        lengths, written = cache.lengths.tolist(), {}
+        for b in range(B):
+            if lengths[b] < 0 or s.status[b]:
+                continue
+            k, v = (cache.storage[i].flatten(0, 1)[s.slots[b].long()].cpu() for i in (0, 1))
+            old, written[b] = kept[b], (k, v)
+            c = dict(q=q.view(B, N, Hq, D)[b:b + 1].cpu(), k_cache=torch.stack([x for x, _ in old] + list(k))[None],
+                     v_cache=torch.stack([x for _, x in old] + list(v))[None], parent=parent, block_table=torch.zeros(1, 1, dtype=I32),
+                     lengths=torch.tensor([len(old)], dtype=I32))
+            want = ref.attention(**c)
+            bound = want["mass"] * (2.0**-8 + 2.0**-10) + want["out"].abs() * 2.0**-8
+            assert out.status[b] == 0 and bool(((out.out[b:b + 1].cpu().double() - want["out"]).abs() <= bound).all())
+        node = torch.randint(0, N, (B,), generator=g).int()
+        accepted = node.cuda()
+        torch.cuda.synchronize()
+        done = cache.commit(accepted, stream=stream)
+        torch.cuda.synchronize()
+        for b in range(B):
+            if s.status[b]:
+                refused += 1
+                assert int(done.status[b]) == int(s.status[b]) != 0 and int(done.lengths[b]) == lengths[b]
+            elif lengths[b] >= 0:
+                kept[b] += [(written[b][0][i], written[b][1][i]) for i in tree_paths[int(node[b])]]
+                assert int(done.status[b]) == 0 and int(done.lengths[b]) == len(kept[b])
+    assert refused > 3
