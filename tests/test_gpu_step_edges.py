@@ -6,7 +6,8 @@ import pytest
 import torch
 
 from . import step_ref as ref
-from .test_gpu_step import I32, attention_case, chain, check_attention, cuda, tree
+from .test_gpu_step import (I32, attention_case, chain, chains_case, check_attention, check_chains, commit_case, cuda, rope_case, slots_case,
+                            tree)
 from paper_2602_16994_b200 import binding
 from paper_2602_16994_b200.tree_cache import TreeCache
 
@@ -162,3 +163,33 @@ def test_a_pool_that_runs_dry_in_mid_loop(side):
                 kept[b] += [(written[b][0][i], written[b][1][i]) for i in tree_paths[int(node[b])]]
                 assert int(done.status[b]) == 0 and int(done.lengths[b]) == len(kept[b])
     assert refused > 3
+
+
+# ---------------------------------------------------------------------------------------------
+# tree_attention: exponentials
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("parent,heads", [(chain(1), (1, 1)), (tree(8, 2, 6), (4, 1))])
+def test_every_exponential_is_as_good_as_the_sums(parent, heads):
+    """Requests that each see one weight, 2^-(j / 64), at 16 keys of every place of a run of 16 (others far below), beside two weights of 1: the
+    sum shows how far the weight is off."""
+    B, N, length = 161, parent.shape[-1], 128
+    for place in range(0, 16, 2):
+        c = attention_case([length] * B, parent, *heads, 64, torch.bfloat16, 16, seed=1, scale=math.log(2.0))
+        c["q"].zero_()
+        c["q"][..., 0] = 1.0
+        c["k_cache"].zero_()
+        y = torch.arange(B) / 64.0
+        at = torch.arange(length)
+        for b in range(B):
+            here = (at % 16 == place) | (at % 16 == place + 1)
+            score = torch.where(here, -y[b], -120.0)
+            score[(place + 8) % 16] = 0.0                         # (the reference of this tile, whoever else works on others)
+            c["k_cache"][c["block_table"][b, at // 16].long(), at % 16, 0, 0] = score.to(torch.bfloat16)
+            c["k_cache"][c["block_table"][b, length // 16:(length + N + 15) // 16].long()] = 0.0
+        lse = binding.tree_attention(**cuda(c), want_lse=True).lse[:, 0, 0].cpu().double()
+        scale = float(torch.tensor(math.log(2.0)).float())
+        want = torch.log(2.0 + 16.0 * torch.exp(-y.double() * scale))
+        # eleven sums of one rounding each, 2^-22 for an exponential, the exponent (scale, its product with log2 e, a score of y) and the
+        # logarithm with its product by ln 2 to two roundings
+        bound = 11 * 2.0**-24 + 2.0**-22 + y.double() * 2.0**-23 + want.abs() * 2.0**-23
+        assert bool(((lse - want).abs() <= bound).all()), (place, float(((lse - want).abs() - bound).max()))
