@@ -60,11 +60,11 @@ template <typename T> struct Rows {
             if (hole == t + 3) a.w = 0.f;
         }
     }
-    // (compared in fp32, where p > q means the same; NaN stays)
+    // (the difference's sign is right in fp32, whose small numbers have no gap at 0; NaN stays, and what two infinities leave is NaN too)
     template <bool Q> static __device__ __forceinline__ double weight(float p, float q)
     {
         if constexpr (!Q) return (double)(p <= 0.f ? 0.f : p);
-        const bool none = p <= q;
+        const bool none = p - q <= 0.f;
         return (double)(none ? 0.f : p) - (double)(none ? 0.f : q);
     }
     template <bool Q> static __device__ __forceinline__ double sum(const float4 &a, const float4 &b)

@@ -193,3 +193,28 @@ def test_every_exponential_is_as_good_as_the_sums(parent, heads):
         # logarithm with its product by ln 2 to two roundings
         bound = 11 * 2.0**-24 + 2.0**-22 + y.double() * 2.0**-23 + want.abs() * 2.0**-23
         assert bool(((lse - want).abs() <= bound).all()), (place, float(((lse - want).abs() - bound).max()))
+
+
+# ---------------------------------------------------------------------------------------------
+# verify_probs: infinities that are not at a drafted token
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [7, 1000, 4097, 128256])
+def test_chains_with_infinities_beside_the_drafted_token(dtype, V):
+    inf, nan = math.inf, math.nan
+    c = chains_case([2] * 8, V, dtype, seed=V)
+    c["u_accept"][:] = 1.0 - 2**-24
+    first = torch.arange(8) * 2
+    c["target_probs"][first + torch.arange(8), c["token"][first].long()] *= 0.25        # every first draft is rejected
+    other = (c["token"][first].long() + 3) % V
+    for b, (p, q) in enumerate([(inf, inf), (inf, None), (None, inf), (nan, inf), (None, nan), (inf, nan), (torch.finfo(dtype).max, inf), (-inf, -inf)]):
+        if p is not None:
+            c["target_probs"][3 * b, other[b]] = p
+        if q is not None:
+            c["draft_probs"][2 * b, other[b]] = q
+    want = check_chains(c)
+    assert want["status"].tolist() == [3, 3, 0, 3, 3, 3, 0, 3]
+    lookup = dict(c, draft_probs=None)
+    lookup["target_probs"] = c["target_probs"].clone()
+    lookup["target_probs"][6 * 3, other[6]] = 0.5
+    assert check_chains(lookup)["status"].tolist() == [3, 3, 0, 3, 0, 3, 0, 0]
