@@ -341,7 +341,7 @@ int32_t spec_norm_rope_cache(const SpecNormRope *a, void *stream);
  * N = 1, parent = {-1}: plain decoding; parent[i] = i - 1: a stretch of a prompt.
  * Scores, maxima and sums in fp32; probabilities are rounded to the type of the values for the product with them.
  * A row that sees nothing (a block id outside [0, num_blocks) hides its keys and gives SPEC_DEV_PAGE) is 0, its lse -inf; so are all
- * rows of a request with a bad tree (SPEC_DEV_TOPOLOGY).  What no node sees is not read; what a node does not see does not
+ * rows of a request with a bad tree (SPEC_DEV_TOPOLOGY).  A row whose scores are all -inf is NaN (0 / 0), its lse -inf.  What no node sees is not read; what a node does not see does not
  * reach its row, whatever it holds (NaN and infinities too).  Rows of idle requests and of nodes beyond n_nodes[b] stay as they were.
  * SPEC_DEV_TIMEOUT (a wait ran out, in any request's part of the work): the rows of the call's requests are undefined.
  * D: 64, 128 or 256.  q, caches and out of one type, SPEC_BF16 or SPEC_F16.  Strides in elements, multiples of 8, and bases on 16 bytes;

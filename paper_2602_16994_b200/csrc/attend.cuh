@@ -53,7 +53,7 @@ struct Params {
     int *status;
     int ctas, groups;                          // CTAs with a run each; groups of 32 rows that a block of rows has at most
     float *part;                               // [ctas][2][D / 4][rows][4] unfinished O
-    float2 *ml;                                // [ctas][2][rows] reference and l
+    float2 *ml;                                // [ctas][2][rows] reference and l; reference -inf: none, and l is 1 where keys were seen
     int *late;                                 // [ctas] a wait ran out
     int4 *joint;                               // [ctas] the unit whose first part this is: request, block, head; parts, slot and rows
 };
@@ -522,6 +522,23 @@ __device__ __noinline__ void put_back(const Params &P, const Segment &seg, int n
     }
 }
 
+// Whether a row sees any key of a segment: asked for rows whose weights came to nothing, which are 0 where they see nothing, and no number where all that
+// they see has a score of -inf (0 / 0).
+__device__ __noinline__ bool sees_any(const Params &P, const Segment &seg, int node, int depth, const unsigned short *parent)
+{
+    Walk walk = {node, 0};
+    for (int step = 0; step < seg.steps(); ++step) {
+        const int tile = seg.tile(step);
+        uint32_t words[4];
+        seen_words(P, seg.r, tile, depth, parent, walk, words);
+        for (int j = 0; j < KT; ++j) {
+            const uint32_t word = j < 32 ? words[0] : j < 64 ? words[1] : j < 96 ? words[2] : words[3];
+            if (((word >> (j & 31)) & 1u) && block_in(P, seg.b, column_of(P, tile * KT + j)) >= 0) return true;
+        }
+    }
+    return false;
+}
+
 template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) spec_attend_kernel(const __grid_constant__ Params P)
 {
     constexpr int D = S::D, MT = S::MT;
@@ -671,7 +688,8 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             }
             if (warp_live) {
                 const bool poison = *(volatile int *)&B->poison != 0;
-                const float inv = l == 0.f ? 0.f : 1.f / l;
+                const bool only = live && l == 0.f && sees_any(P, seg, node, depth, parent);         // sees keys, all with a score of -inf
+                const float inv = l == 0.f ? only ? CUDART_NAN_F : 0.f : 1.f / l;
                 const long long slot = (long long)blockIdx.x * 2 + (seg.head ? 0 : 1);
                 const int head = seg.h * P.G + r - node * P.G;
                 T *to = (T *)P.out + seg.b * P.out_stride[0] + node * P.out_stride[1] + head * P.out_stride[2];
@@ -720,7 +738,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                         if (P.lse)
                             P.lse[((long long)seg.b * P.tree.N + node) * P.Hq + head] = l == 0.f ? -CUDART_INF_F : (ref + log2f(l)) * LN2;
                     } else {
-                        P.ml[slot * S::ROWS + row] = make_float2(any ? ref : -CUDART_INF_F, l);
+                        P.ml[slot * S::ROWS + row] = make_float2(any ? ref : -CUDART_INF_F, only ? 1.f : l);
                     }
                 }
                 tc::fence_before();
@@ -1107,6 +1125,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(JOIN_NT, 8) 
     for (int i = tid; i < rows * (D / 4); i += JOIN_NT) {
         const int row = row0 + i % rows, ch = i / rows;
         float ref = -CUDART_INF_F, l = 0.f;
+        bool only = false;                     // (some part saw keys, all with a score of -inf)
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int c0 = j; c0 <= last; c0 += 8) {
             float4 x[8];
@@ -1119,7 +1138,10 @@ template <typename T, typename S> __global__ void __launch_bounds__(JOIN_NT, 8) 
             }
             float top = ref;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) top = fmaxf(top, m[k].x);
+            for (int k = 0; k < 8; ++k) {
+                top = fmaxf(top, m[k].x);
+                only |= m[k].x == -CUDART_INF_F && m[k].y != 0.f;
+            }
             const float f = ref == -CUDART_INF_F ? 0.f : ex2_approx(ref - top);
             ref = top;
             l *= f; o.x *= f; o.y *= f; o.z *= f; o.w *= f;
@@ -1134,7 +1156,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(JOIN_NT, 8) 
             }
         }
         const int q = joint.y * S::ROWS + row, node = node_of(P, q), head = joint.z * P.G + q - node * P.G;
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float inv = l == 0.f ? only ? CUDART_NAN_F : 0.f : 1.f / l;
         T *to = (T *)P.out + b * P.out_stride[0] + node * P.out_stride[1] + head * P.out_stride[2] + ch * 4;
         *(uint2 *)to = make_uint2(Pair<T>::pack(o.x * inv, o.y * inv), Pair<T>::pack(o.z * inv, o.w * inv));
         if (P.lse && ch == 0) P.lse[((long long)b * P.tree.N + node) * P.Hq + head] = l == 0.f ? -CUDART_INF_F : (ref + log2f(l)) * LN2;

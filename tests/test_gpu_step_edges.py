@@ -218,3 +218,68 @@ def test_chains_with_infinities_beside_the_drafted_token(dtype, V):
     lookup["target_probs"] = c["target_probs"].clone()
     lookup["target_probs"][6 * 3, other[6]] = 0.5
     assert check_chains(lookup)["status"].tolist() == [3, 3, 0, 3, 0, 3, 0, 0]
+
+
+# ---------------------------------------------------------------------------------------------
+# tree_attention: scores of -inf
+# ---------------------------------------------------------------------------------------------
+def attended(c, hidden=None):
+    """One request's rows in 64 bits, straight from the definition."""
+    N, Hq, D = c["q"].shape[1:]
+    block, G, length = c["k_cache"].shape[1], Hq // c["k_cache"].shape[2], int(c["lengths"][0])
+    at = torch.arange(length + N)
+    k = c["k_cache"][c["block_table"][0, at // block].long(), at % block].double().repeat_interleave(G, 1)
+    v = c["v_cache"][c["block_table"][0, at // block].long(), at % block].double().repeat_interleave(G, 1)
+    seen = torch.zeros(N, length + N, dtype=torch.bool)
+    seen[:, :length] = True
+    for i, p in enumerate(ref.paths(c["parent"].tolist())):
+        seen[i, [length + x for x in p]] = True
+    score = (c["q"][0].double()[:, :, None] * k.transpose(0, 1)[None]).sum(-1) * D ** -0.5
+    if hidden is not None:
+        seen[:, hidden] = False
+    score = torch.where(seen[:, None], score, -math.inf)
+    return torch.softmax(score, -1), v, torch.logsumexp(score, -1)
+
+
+@pytest.mark.parametrize("length", [0, 40, 300, 3000])
+@pytest.mark.parametrize("parent,heads", [(chain(1), (4, 1)), (tree(4, 2, 4), (4, 2)), (tree(8, 2, 6), (8, 2))])
+def test_scores_of_minus_infinity(length, parent, heads):
+    """A row whose only scores are -inf is 0 / 0, no number; one that has others besides takes no notice of them; the log of the sum is that of 0."""
+    N = parent.shape[-1]
+    c = attention_case([length], parent, *heads, 128, torch.bfloat16, 16, seed=length + N)
+    c["q"] = c["q"].abs() + 0.125
+    c["k_cache"][..., 3] = -math.inf
+    got = binding.tree_attention(**cuda(c), want_lse=True)
+    assert got.status.tolist() == [0] and bool(got.out.isnan().all()) and bool((got.lse == -math.inf).all())
+    # one tree node with a finite key: its own row and those below it are its value
+    node = N // 2
+    c["k_cache"][c["block_table"][0, (length + node) // 16].long(), (length + node) % 16, :, 3] = 1.0
+    got = binding.tree_attention(**cuda(c), want_lse=True)
+    below = torch.tensor([node in p for p in ref.paths(parent.tolist())])
+    v = c["v_cache"][c["block_table"][0, (length + node) // 16].long(), (length + node) % 16].repeat_interleave(heads[0] // heads[1], 0)
+    assert bool((got.out[0, below].cpu() == v).all()) and bool(got.lse[0, below].isfinite().all())
+    assert bool(got.out[0, ~below].isnan().all()) and bool((got.lse[0, ~below] == -math.inf).all())
+    # all keys of the context finite but for one in three: rows are what the others give
+    c["k_cache"][..., 3] = 1.0
+    at = torch.arange(0, length + N, 3)
+    c["k_cache"][c["block_table"][0, at // 16].long(), at % 16, :, 3] = -math.inf
+    got = binding.tree_attention(**cuda(c), want_lse=True)
+    p, v, lse = attended(c, at)
+    some = lse.isfinite()
+    bound = torch.einsum("nhj,jhd->nhd", p, v.abs()) * (2.0**-8 + 2.0**-10) + 2.0**-8 * torch.einsum("nhj,jhd->nhd", p, v).abs()
+    off = (got.out[0].cpu().double() - torch.einsum("nhj,jhd->nhd", p, v)).abs()
+    assert bool((off <= bound)[some].all()) and bool(got.out[0].cpu()[~some].isnan().all())
+    assert bool(((got.lse[0].cpu().double() - lse).abs() <= 2.0**-16 * (1 + lse.abs()))[some].all())
+
+
+def test_scores_of_minus_infinity_beside_bad_blocks_and_windows():
+    """A row that sees nothing is 0; one that sees keys, all at -inf, is no number, also where the rest is hidden or left behind by the window."""
+    parent = tree(4, 2, 4)
+    for window, sinks in ((0, 0), (30, 3), (1, 0)):
+        c = attention_case([700, 700], parent, 8, 2, 128, torch.bfloat16, 16, seed=31, window=window, sinks=sinks)
+        c["q"] = c["q"].abs() + 0.125
+        c["k_cache"][..., 3] = -math.inf
+        c["block_table"][0] = -1                                  # sees nothing
+        c["block_table"][1, :20] = -1                             # sees the rest
+        got = binding.tree_attention(**cuda(c), want_lse=True)
+        assert bool((got.out[0] == 0).all()) and bool(got.out[1].isnan().all()) and bool((got.lse == -math.inf).all())
