@@ -532,6 +532,12 @@ void rows_of(const at::Tensor &t, const char *name, int dims, at::ScalarType typ
 void no_gradient(const at::Tensor &t, const char *name)
 {
     if (t.requires_grad() && c10::GradMode::is_enabled()) raise("%s requires a gradient: the call has no backward pass", name);
+    if (t._fw_grad(0).defined()) raise("%s carries a tangent: the call has no forward-mode derivative", name);
+}
+// A tensor that the call has written: what autograd has kept of it for a backward pass is out of date.
+void written(const at::Tensor &t)
+{
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
 // strides of all but the last dimension; of a dimension of one entry, which nothing steps along: 0
 void strides_of(const at::Tensor &t, int64_t *to)
@@ -564,6 +570,7 @@ PyObject *py_slots(PyObject *, PyObject *const *a, Py_ssize_t n)
         s.slots = int_ptr(t[0]); s.positions = int_ptr(t[1]); s.owned_out = int_ptr(t[3]); s.free_range_out = int_ptr(t[4]);
         s.status = int_ptr(t[5]);
         check(unlocked([&] { return step_lib.slots(&s, place.stream()); }), "spec_cache_slots");
+        written(t[2]);
         return result(slot_outputs_class, t, 6);
     });
 }
@@ -599,6 +606,7 @@ PyObject *py_norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n)
             *weight[i] = w.data_ptr();
         }
         const at::Tensor &freq = floats(a[3], "inv_freq", place);
+        no_gradient(freq, "inv_freq");
         s.positions = int_ptr(ints(a[4], "positions", place, T));
         s.slots = int_ptr(ints(a[5], "slots", place, T));
         s.T = small(T, "T"); s.Hq = small(q.size(1), "Hq"); s.Hkv = small(Hkv, "Hkv"); s.D = small(D, "D");
@@ -618,6 +626,8 @@ PyObject *py_norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n)
         strides_of(q, s.q_stride); strides_of(k, s.k_stride); strides_of(v, s.v_stride); strides_of(out, s.q_out_stride);
         strides_of(kc, s.k_cache_stride); strides_of(vc, s.v_cache_stride);
         if (T) check(unlocked([&] { return step_lib.norm_rope(&s, place.stream()); }), "spec_norm_rope_cache");
+        written(kc); written(vc);
+        if (a[12] != Py_None) written(out);
         return THPVariable_Wrap(out);
     });
 }
@@ -671,6 +681,7 @@ PyObject *py_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
         // graphs, never share it
         const at::Tensor ws = empty({bytes}, at::kByte, place.device());
         check(unlocked([&] { return step_lib.attention(&s, ws.data_ptr(), bytes, place.stream()); }), "spec_tree_attention");
+        if (a[10] != Py_None) written(t[0]);
         return result(attention_outputs_class, t, 3);
     });
 }
@@ -708,6 +719,7 @@ PyObject *py_commit(PyObject *, PyObject *const *a, Py_ssize_t n)
         const at::Tensor t[2] = {made.take({B}), made.take({B})};
         s.lengths_out = int_ptr(t[0]); s.status = int_ptr(t[1]);
         check(unlocked([&] { return step_lib.commit(&s, place.stream()); }), "spec_cache_commit");
+        written(cache);
         return result(commit_outputs_class, t, 2);
     });
 }

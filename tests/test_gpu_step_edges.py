@@ -283,3 +283,55 @@ def test_scores_of_minus_infinity_beside_bad_blocks_and_windows():
         c["block_table"][1, :20] = -1                             # sees the rest
         got = binding.tree_attention(**cuda(c), want_lse=True)
         assert bool((got.out[0] == 0).all()) and bool(got.out[1].isnan().all()) and bool((got.lse == -math.inf).all())
+
+
+# ---------------------------------------------------------------------------------------------
+# what autograd knows of the calls
+# ---------------------------------------------------------------------------------------------
+def small_calls():
+    r = cuda(rope_case(3, 2, 1, 64, 64, torch.bfloat16))
+    a = cuda(attention_case([10], tree(1, 0, 1), 2, 1, 64, torch.bfloat16, 16))
+    m = cuda(commit_case([5], tree(1, 0, 1), [1], 2, (16,), torch.float32, 16))
+    return [(binding.norm_rope_cache, r, ("q", "k", "v", "inv_freq", "q_weight", "k_weight", "k_cache", "v_cache")),
+            (binding.tree_attention, a, ("q", "k_cache", "v_cache")), (binding.cache_commit, m, ("cache",))]
+
+
+def test_tangents_and_gradients_are_not_dropped():
+    for call, args, names in small_calls():
+        for name in names:
+            with pytest.raises(RuntimeError, match="backward"):
+                call(**dict(args, **{name: args[name].clone().requires_grad_()}))
+            with torch.no_grad():
+                call(**dict(args, **{name: args[name].clone().requires_grad_()}))
+            with torch.autograd.forward_ad.dual_level():
+                dual = torch.autograd.forward_ad.make_dual(args[name].clone(), torch.ones_like(args[name]))
+                with pytest.raises(RuntimeError, match="tangent"):
+                    call(**dict(args, **{name: dual}))
+
+
+def test_writes_in_place_are_known_to_autograd():
+    for call, args, _ in small_calls():
+        written = {"norm_rope_cache": ("k_cache", "v_cache", "q_out"), "tree_attention": ("out",), "cache_commit": ("cache",)}[call.__name__]
+        args = dict(args)
+        for name in ("q_out", "out"):
+            if name in written:
+                args[name] = torch.empty_like(args["q"])
+        for name in written:
+            w = torch.ones_like(args[name]).requires_grad_()
+            y = (w * args[name]).sum()                            # keeps what it multiplies by for its backward pass
+            call(**args)
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                y.backward()
+    c = slots_case(2, 3, 8, 1)
+    d = cuda(c)
+    before = d["block_table"]._version
+    binding.cache_slots(**d)
+    assert d["block_table"]._version == before + 1
+
+
+def test_tensors_of_inference_mode_are_taken():
+    for call, args, _ in small_calls():
+        with torch.inference_mode():
+            frozen = {k: v.clone() if isinstance(v, torch.Tensor) else v for k, v in args.items()}
+            call(**frozen)
+        call(**frozen)
