@@ -539,6 +539,12 @@ void written(const at::Tensor &t)
 {
     if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
+// a tensor that the call writes: an expanded one has several threads at the same place
+void apart(const at::Tensor &t, const char *name)
+{
+    for (int64_t i = 0; i < t.dim(); ++i)
+        if (t.size(i) > 1 && t.stride(i) == 0) raise("the entries of %s share memory: it cannot be written", name);
+}
 // strides of all but the last dimension; of a dimension of one entry, which nothing steps along: 0
 void strides_of(const at::Tensor &t, int64_t *to)
 {
@@ -592,6 +598,7 @@ PyObject *py_norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n)
         rows_of(kc, "k_cache", 4, type, place);
         rows_of(vc, "v_cache", 4, type, place);
         no_gradient(q, "q"); no_gradient(k, "k"); no_gradient(v, "v"); no_gradient(kc, "k_cache"); no_gradient(vc, "v_cache");
+        apart(kc, "k_cache"); apart(vc, "v_cache");
         const int64_t T = q.size(0), D = q.size(2), Hkv = k.size(1);
         if (k.size(0) != T || k.size(2) != D || v.sizes() != k.sizes()) raise("q, k and v must be [T,Hq,D], [T,Hkv,D] and [T,Hkv,D]");
         if (kc.size(2) != Hkv || kc.size(3) != D || vc.sizes() != kc.sizes()) raise("the caches must be [num_blocks, block_size, Hkv, D]");
@@ -620,6 +627,7 @@ PyObject *py_norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n)
             rows_of(out, "q_out", 3, type, place);
             if (out.sizes() != q.sizes()) raise("q_out must have the shape of q");
             no_gradient(out, "q_out");
+            apart(out, "q_out");
         }
         s.q = q.data_ptr(); s.k = k.data_ptr(); s.v = v.data_ptr(); s.inv_freq = (const float *)freq.data_ptr();
         s.q_out = out.data_ptr(); s.k_cache = kc.data_ptr(); s.v_cache = vc.data_ptr();
@@ -669,6 +677,7 @@ PyObject *py_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
             rows_of(t[0], "out", 4, type, place);
             if (t[0].sizes() != q.sizes()) raise("out must have the shape of q");
             no_gradient(t[0], "out");
+            apart(t[0], "out");
         }
         t[1] = place.fresh({B}, at::kInt);
         if (PyObject_IsTrue(a[11])) t[2] = place.fresh({B, N, Hq}, at::kFloat);
@@ -696,6 +705,7 @@ PyObject *py_commit(PyObject *, PyObject *const *a, Py_ssize_t n)
         const Place place(cache, a[6]);
         place.uses(cache, "cache");
         no_gradient(cache, "cache");
+        apart(cache, "cache");
         if (cache.dim() < 4) raise("cache must be [caches, num_blocks, block_size, ...]");
         int64_t row = 1;
         for (int64_t i = cache.dim() - 1; i >= 3; --i) {

@@ -335,3 +335,19 @@ def test_tensors_of_inference_mode_are_taken():
             frozen = {k: v.clone() if isinstance(v, torch.Tensor) else v for k, v in args.items()}
             call(**frozen)
         call(**frozen)
+
+
+# ---------------------------------------------------------------------------------------------
+# refusals
+# ---------------------------------------------------------------------------------------------
+def test_written_tensors_whose_entries_share_memory_are_refused():
+    r, a, m = (args for _, args, _ in small_calls())
+    for call, args, names in ((binding.norm_rope_cache, dict(r, q_out=r["q"].clone()), ("k_cache", "v_cache", "q_out")),
+                              (binding.tree_attention, dict(a, out=a["q"].clone()), ("out",)), (binding.cache_commit, m, ("cache",))):
+        call(**args)
+        for name in names:
+            for dim in range(args[name].dim() - 1):
+                if args[name].size(dim) > 1:
+                    with pytest.raises(RuntimeError, match="share memory"):
+                        call(**dict(args, **{name: args[name].narrow(dim, 0, 1).expand_as(args[name])}))
+    call(**dict(m, cache=m["cache"][:1]))
