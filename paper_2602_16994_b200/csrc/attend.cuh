@@ -308,7 +308,8 @@ template <int D_, int MT_, int WG_> struct Shape {
 };
 struct Bars {
     uint64_t full[16], empty[16];
-    uint64_t q_full, q_empty, s_full[4], p_full[4], pv_done[2], o_empty[2];
+    uint64_t q_full, q_empty, s_full[4], p_full[4], o_empty[2];
+    uint64_t pv_done[2][2];                    // per O, even and odd parts: see the rows' wait
     uint32_t tmem;
     int dead, poison, bad_tree;                // (bad_tree: of the request that the rows' parents were read for last)
     uint32_t hidden[8][4];                     // keys of a tile on bad blocks, by the tile's number in the CTA's run % 8
@@ -555,7 +556,8 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         mbar_init(&B->q_empty, S::WG);
         for (int t = 0; t < 4; ++t) { mbar_init(&B->s_full[t], 1); mbar_init(&B->p_full[t], 4); }
         for (int t = 0; t < 2; ++t) {
-            mbar_init(&B->pv_done[t], 1);
+            mbar_init(&B->pv_done[t][0], 1);
+            mbar_init(&B->pv_done[t][1], 1);
             mbar_init(&B->o_empty[t], S::TURNS ? 8 : 4);
         }
         B->dead = 0;
@@ -585,6 +587,11 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         const float c = P.scale * LOG2E;
         uint32_t n_part = 0, n_run = 0, n_seg = 0;     // parts of tiles that this warpgroup has been through, tiles of the run, segments
         int tree_of = -1;
+        // The wait for the product of part n with the values.  Scores run up to two parts ahead of these products, and a barrier's phase tells even numbers
+        // from odd ones only: with one barrier for all parts, waiting for the last but one did not end where the last had already come as well, and
+        // without waiting for it the last could not be told from the one two before.  So even and odd parts have a barrier each, and part n + 2 waits
+        // for this warp.
+        const auto products = [&](uint32_t n) { wait(B, &B->pv_done[w][n & 1], n >> 1 & 1); };
         Segment &seg = hand->seg[0];
         for (; hand->next(P, S::ROWS, 0); ++n_seg) {
             const int steps = seg.steps();
@@ -649,7 +656,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                             }
                             of.l *= f;
                             if (begun && __any_sync(0xffffffffu, f != 1.f)) {
-                                wait(B, &B->pv_done[w], (n_part - 1) & 1);
+                                products(n_part - 1);
                                 tc::fence_after();
                                 scale_sums(o_at, D, f);
                             }
@@ -663,12 +670,8 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                     begun = true;
                 }
             }
-            // the segment's end.  Where scores run ahead of the weights, the last follow all products but the last two, which are waited for one after
-            // the other (the parity of a phase is that of the one two before)
-            if (begun) {
-                if ((S::WG == 1 || S::PARTS == 2) && n_part > 1) wait(B, &B->pv_done[w], n_part & 1);
-                wait(B, &B->pv_done[w], (n_part - 1) & 1);
-            }
+            // the segment's end (products come to their end in order: the last is the last of all)
+            if (begun) products(n_part - 1);
             tc::fence_after();
             float ref = of.ref, l = of.l, f0 = 1.f, f1 = 0.f;
             bool any = of.any;
@@ -780,8 +783,8 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             }
             __syncwarp();
         };
-        // O number o (+)= P (in columns `from`) V for part h of a tile, from the values in slots k ..
-        const auto sums = [&](int o, int h, int from, uint32_t k, bool add, bool release) {
+        // O number o (+)= P (in columns `from`) V for part h of a tile, the part'th of this O's parts, from the values in slots k ..
+        const auto sums = [&](int o, int h, uint32_t part, int from, uint32_t k, bool add, bool release) {
             if (tc::elected() && !gone()) {
 #pragma unroll
                 for (int p = 0; p < S::STEP; ++p) {
@@ -792,7 +795,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                         tc::mma_ts(tmem + S::O + o * D + p * 128, tmem + from + i * 8, vd + i * (2048 >> 4), DO, add || i > 0);
                     if (release) tc::commit(&B->empty[slot]);
                 }
-                tc::commit(&B->pv_done[o]);
+                tc::commit(&B->pv_done[o][part & 1]);
             }
             __syncwarp();
         };
@@ -834,7 +837,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                         wait(B, &B->p_full[buf], n_mine & 1);
                         if (i == 0 && h == 0 && n_o) wait(B, &B->o_empty[m], (n_o - 1) & 1);
                         tc::fence_after();
-                        sums(m, h, buf * S::W, values_of(i), i > 0 || h > 0, last);
+                        sums(m, h, n_mine * S::PARTS + h, buf * S::W, values_of(i), i > 0 || h > 0, last);
                         if (!more) continue;
                         if (h == 0) copied(keys_of(i + 1), n_tile + i + 1);
                         scores(m, h, buf * S::W, keys_of(i + 1), &B->s_full[buf], last);
@@ -854,7 +857,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                     wait(B, &B->p_full[m], n_mine & 1);
                     if (i == first && n_seg) wait(B, &B->o_empty[0], (n_seg - 1) & 1);
                     tc::fence_after();
-                    sums(m, 0, m * 128, values_of(i), i > first, true);
+                    sums(m, 0, n_mine, m * 128, values_of(i), i > first, true);
                 }
             } else {
                 // scores a tile ahead
@@ -873,7 +876,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                     wait(B, &B->p_full[at & 1], (at >> 1) & 1);
                     if (i == 0 && n_seg) wait(B, &B->o_empty[0], (n_seg - 1) & 1);
                     tc::fence_after();
-                    sums(0, 0, (at & 1) * 128, values_of(i), i > 0, true);
+                    sums(0, 0, at, (at & 1) * 128, values_of(i), i > 0, true);
                 }
             }
             n_tile += steps;
