@@ -756,9 +756,15 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         constexpr uint32_t DS = tc::product_desc(Pair<T>::TYPE, S::W, false), DO = tc::product_desc(Pair<T>::TYPE, 64 * S::WIDE, true);
         const uint32_t q_at = smem_u32(base), slots = smem_u32(base + S::off_slots);
         uint32_t n = 0, n_seg = 0, n_tile = 0, n_mine = 0, n_o = 0;    // next slot; segments and tiles of the run; own tiles, own segments
-        // the copies to slots k .., of the run's tile i, are there; what threads stored, seen through the barrier, is put before the tensor cores
+        // the copies to slots k .., of the run's tile i, are there; what threads stored, seen through the barrier, is put before the tensor cores.
+        // In turns a slot's last contents may have been the other warp's: a phase tells even fillings from odd ones only, so that one is first seen let
+        // go of, or its not yet having come would look like the next one's being there.
         const auto copied = [&](uint32_t k, uint32_t i) {
-            for (int p = 0; p < S::STEP; ++p) wait(B, &B->full[(k + p) % S::SLOTS], ((k + p) / S::SLOTS) & 1);
+            for (int p = 0; p < S::STEP; ++p) {
+                const uint32_t slot = (k + p) % S::SLOTS, filling = (k + p) / S::SLOTS;
+                if (S::TURNS && filling > 0) wait(B, &B->empty[slot], (filling - 1) & 1);
+                wait(B, &B->full[slot], filling & 1);
+            }
             if (*(volatile uint32_t *)&B->plain[i & 7]) tc::publish_shared();
             tc::fence_after();
         };
