@@ -997,19 +997,22 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             if (hold) { late_values = true; late_slot = n; }
             n += S::STEP;
         };
+        // (A warp waits only for room that it fills itself: where a unit has one tile, the products let go of its queries as soon as the keys are there,
+        // and a warp that comes to ask after that, and has no part in the next queries, would find a phase that is not told from the one before.)
         const auto copy_q = [&](const Segment &s) {
+            if (P.q_boxes && part != 0) return;
             if (n_seg) room(&B->q_empty, (n_seg - 1) & 1);
             ++n_seg;
             if (stopped(B)) return;
             if (c_hold_slot >= 0 && c_hold_slot / P.tree.N == s.b) return;       // (a test may ask for a request's queries to stay away)
             if (P.q_boxes) {
                 // (nodes beyond N come as zeros)
-                if (part == 0 && lane == 0) {
+                if (lane == 0) {
                     tc::expect_bytes(&B->q_full, S::ROWS * D * 2);
                     tc::arrive_many(&B->q_full, S::NP);
                 }
                 __syncwarp();
-                if (part == 0 && lane < S::PANELS * MT)
+                if (lane < S::PANELS * MT)
                     tc::box_load(q_at + lane * PANEL, &P.q_map, lane / MT * 64, s.h * P.G, node_of(P, s.m * S::ROWS + lane % MT * 128), s.b, &B->q_full);
                 return;
             }

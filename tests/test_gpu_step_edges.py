@@ -356,17 +356,22 @@ def test_written_tensors_whose_entries_share_memory_are_refused():
 # ---------------------------------------------------------------------------------------------
 # tree_attention: many short units, many times
 # ---------------------------------------------------------------------------------------------
-@pytest.mark.parametrize("heads,D,window", [((32, 8), 128, 0), ((8, 1), 64, 60), ((4, 2), 256, 0), ((8, 2), 128, 0)])
-def test_calls_with_many_short_units(heads, D, window):
-    """Warps come to a unit's end at different times, some with nothing to do: whoever comes late finds the products done, or not, and goes on alike."""
+@pytest.mark.parametrize("heads,D,window,shape", [((32, 8), 128, 0, (8, 2, 6)), ((8, 1), 64, 60, (8, 2, 6)), ((4, 2), 256, 0, (8, 2, 6)),
+                                                  ((8, 2), 128, 0, (8, 2, 6)), ((32, 8), 128, 500, None), ((14, 2), 64, 0, None),
+                                                  ((8, 4), 256, 0, None), ((16, 4), 64, 0, (4, 2, 4))])
+def test_calls_with_many_short_units(heads, D, window, shape):
+    """Warps come to a unit's end, and to the next one's beginning, at different times, some with nothing to do: whoever comes late finds the others'
+    work done, or not, and goes on alike."""
     g = torch.Generator().manual_seed(4)
+    parent = tree(*shape) if shape else chain(1)
     lengths = torch.randint(0, 300, (60,), generator=g).tolist()
-    nodes = torch.randint(0, 52, (60,), generator=g).tolist()
-    c = attention_case(lengths, tree(8, 2, 6), *heads, D, torch.bfloat16, 16, seed=6, n_nodes=nodes, window=window, sinks=2)
+    nodes = torch.randint(0, parent.shape[-1] + 1, (60,), generator=g).tolist() if shape else None
+    c = attention_case(lengths, parent, *heads, D, torch.bfloat16, 16, seed=6, n_nodes=nodes, window=window, sinks=2)
     want, d = ref.attention(**c), cuda(c)
     first = check_attention(c, want)
     live = want["live"].cuda()
-    for _ in range(300):
-        again = binding.tree_attention(**d, want_lse=True)
-        assert torch.equal(again.status, first.status)
-        assert torch.equal(again.out[live], first.out[live]) and torch.equal(again.lse[live], first.lse[live])
+    wrong = torch.zeros((), dtype=torch.int32, device="cuda")
+    for _ in range(3000):
+        again = binding.tree_attention(**d)
+        wrong += (again.status != first.status).any() | (again.out[live] != first.out[live]).any()
+    assert int(wrong) == 0
