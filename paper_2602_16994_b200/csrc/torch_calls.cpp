@@ -494,6 +494,12 @@ int32_t small(int64_t v, const char *what)
     if (v > 0x7FFFFFFF || v < 0) raise("%s is out of range", what);
     return (int32_t)v;
 }
+bool truth(PyObject *o)
+{
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw Raised{};
+    return v != 0;
+}
 int32_t whole(PyObject *o, const char *what)        // an int argument, whole or refused
 {
     const long long v = integer(o);
@@ -680,7 +686,7 @@ PyObject *py_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
             apart(t[0], "out");
         }
         t[1] = place.fresh({B}, at::kInt);
-        if (PyObject_IsTrue(a[11])) t[2] = place.fresh({B, N, Hq}, at::kFloat);
+        if (truth(a[11])) t[2] = place.fresh({B, N, Hq}, at::kFloat);
         s.q = q.data_ptr(); s.k_cache = kc.data_ptr(); s.v_cache = vc.data_ptr(); s.out = t[0].data_ptr(); s.status = int_ptr(t[1]);
         s.lse = t[2].defined() ? (float *)t[2].data_ptr() : nullptr;
         strides_of(q, s.q_stride); strides_of(kc, s.k_cache_stride); strides_of(vc, s.v_cache_stride); strides_of(t[0], s.out_stride);

@@ -375,3 +375,9 @@ def test_calls_with_many_short_units(heads, D, window, shape):
         again = binding.tree_attention(**d)
         wrong += (again.status != first.status).any() | (again.out[live] != first.out[live]).any()
     assert int(wrong) == 0
+
+
+def test_a_flag_that_is_no_truth_value_is_refused():
+    d = cuda(attention_case([10], tree(1, 0, 1), 2, 1, 64, torch.bfloat16, 16))
+    with pytest.raises(RuntimeError, match="ambiguous"):
+        binding.tree_attention(**d, want_lse=torch.ones(2))
