@@ -314,7 +314,7 @@ int32_t spec_cache_slots(const SpecSlots *a, void *stream);
  * Queries go to q_out (may be q itself), keys and values (values as they are) to slot slots[token] of the caches.
  * Arithmetic in fp32, angles reduced in fp64, one rounding at the end.  A token whose slot is outside
  * [0, num_blocks * block_size) is padding: nothing of it is read or written.  No two tokens may share a slot.
- * D: a multiple of 8 up to 256; rot: a multiple of 16 up to D.  Strides in elements; the D entries of a head are contiguous.
+ * D: a multiple of 8 up to 256; rot: a multiple of 16 up to D.  T: below 2^31 - 4096.  Strides in elements; the D entries of a head are contiguous.
  */
 typedef struct {
     int32_t T, Hq, Hkv, D, rot, pairs, dtype;   /* tokens; heads; SPEC_F32, SPEC_BF16 or SPEC_F16     */

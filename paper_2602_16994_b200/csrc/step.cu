@@ -185,7 +185,8 @@ int32_t spec_norm_rope_cache(const SpecNormRope *a, void *stream)
 {
     if (!a || !a->q || !a->k || !a->v || (a->rot > 0 && !a->inv_freq) || !a->positions || !a->slots || !a->q_out || !a->k_cache || !a->v_cache)
         return SPEC_ERR_NULL;
-    if (a->T < 1 || a->Hq < 1 || a->Hkv < 1 || a->Hq > 65535 || a->Hkv > 65535 || a->num_blocks < 1 || a->block_size < 1 ||
+    // (a CTA's step from token to token stays below 2^31)
+    if (a->T < 1 || a->T > 0x7FFFFFFF - 4096 || a->Hq < 1 || a->Hkv < 1 || a->Hq > 65535 || a->Hkv > 65535 || a->num_blocks < 1 || a->block_size < 1 ||
         (int64_t)a->num_blocks * a->block_size > 0x7FFFFFFF)
         return SPEC_ERR_SHAPE;
     if (a->dtype != SPEC_F32 && a->dtype != SPEC_BF16 && a->dtype != SPEC_F16) return SPEC_ERR_DTYPE;

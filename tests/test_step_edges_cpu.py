@@ -1,10 +1,12 @@
 """Host-side checks of the operators around a verification: what can be known of them without a device."""
+import ctypes as C
 import os
 import re
 
 import numpy as np
 
 from paper_2602_16994_b200 import build
+from .test_step_cpu import Rope, filled, lib  # noqa: F401
 
 
 def test_the_polynomial_for_exponentials():
@@ -18,3 +20,9 @@ def test_the_polynomial_for_exponentials():
         p = (p.astype(np.float64) * f.astype(np.float64) + np.float64(c)).astype(np.float32)
     assert float(np.abs(p.astype(np.float64) / np.exp2(f.astype(np.float64)) - 1.0).max()) < 2.0e-7
     assert p[f == 0] == 1.0
+
+
+def test_token_counts_up_to_the_end_of_32_bits_are_refused(lib):  # noqa: F811
+    """A CTA goes from token to token in steps of the grid: the step past the last token must not wrap round."""
+    for tokens in (2**31 - 1, 2**31 - 4000):
+        assert lib.spec_norm_rope_cache(C.byref(filled(Rope, D=64, rot=64, T=tokens)), None) == -2
