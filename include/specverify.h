@@ -269,8 +269,9 @@ int32_t spec_verify_host(const SpecIn *in, const SpecOut *out, int32_t algorithm
  * position j lies at entry j % block_size of the block that its row of the block table names in column j / block_size.
  * lengths[b] is the number of committed tokens.  The N nodes of a request's tree lie behind them: node i at entry lengths[b] + i
  * (node 0 is the root: the token emitted last, whose keys and values are not in the cache yet), at POSITION
- * lengths[b] + depth(i).  A request with lengths[b] < 0 takes no part: nothing of it is read but the length.  n_nodes (optional,
- * [B]): the request's tree has n_nodes[b] <= N nodes; what belongs to the others is not read.  Status codes per request as
+ * lengths[b] + depth(i).  A request with lengths[b] < 0 takes no part: nothing of it matters but the length.  n_nodes (optional,
+ * [B]): the request's tree has n_nodes[b] <= N nodes; what belongs to the others reaches no result, whatever it holds (the others'
+ * rows of an array that is there may be read along with the tree's).  Status codes per request as
  * above; a request with n_nodes[b] outside [0,N] counts as one without nodes, with SPEC_DEV_TOPOLOGY.  N is at most
  * SPEC_MAX_NODES here too; a node may have any number of children.
  * ------------------------------------------------------------------------------------------------ */
@@ -341,8 +342,8 @@ int32_t spec_norm_rope_cache(const SpecNormRope *a, void *stream);
  * N = 1, parent = {-1}: plain decoding; parent[i] = i - 1: a stretch of a prompt.
  * Scores, maxima and sums in fp32; probabilities are rounded to the type of the values for the product with them.
  * A row that sees nothing (a block id outside [0, num_blocks) hides its keys and gives SPEC_DEV_PAGE) is 0, its lse -inf; so are all
- * rows of a request with a bad tree (SPEC_DEV_TOPOLOGY).  A row whose scores are all -inf is NaN (0 / 0), its lse -inf.  What no node sees is not read; what a node does not see does not
- * reach its row, whatever it holds (NaN and infinities too).  Rows of idle requests and of nodes beyond n_nodes[b] stay as they were.
+ * rows of a request with a bad tree (SPEC_DEV_TOPOLOGY).  A row whose scores are all -inf is NaN (0 / 0), its lse -inf.  Keys and values that
+ * no node sees are not read; what a node does not see does not reach its row, whatever it holds (NaN and infinities too).  Rows of idle requests and of nodes beyond n_nodes[b] stay as they were.
  * SPEC_DEV_TIMEOUT (a wait ran out, in any request's part of the work): the rows of the call's requests are undefined.
  * D: 64, 128 or 256.  q, caches and out of one type, SPEC_BF16 or SPEC_F16.  Strides in elements, multiples of 8, and bases on 16 bytes;
  * the D entries of a head are contiguous; out overlaps no input.  lse: optional, log of sum_j exp(scale q.k_j) (natural).

@@ -51,7 +51,7 @@ struct Params {
     long long out_stride[3];
     float *lse;
     int *status;
-    int ctas, groups;                          // CTAs with a run each; groups of 32 rows that a block of rows has at most
+    int ctas, groups;                          // CTAs with a run each; groups of JOIN_ROWS rows that a block of rows has at most
     float *part;                               // [ctas][2][D / 4][rows][4] unfinished O
     float2 *ml;                                // [ctas][2][rows] reference and l; reference -inf: none, and l is 1 where keys were seen
     int *late;                                 // [ctas] a wait ran out

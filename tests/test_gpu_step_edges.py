@@ -381,3 +381,41 @@ def test_a_flag_that_is_no_truth_value_is_refused():
     d = cuda(attention_case([10], tree(1, 0, 1), 2, 1, 64, torch.bfloat16, 16))
     with pytest.raises(RuntimeError, match="ambiguous"):
         binding.tree_attention(**d, want_lse=torch.ones(2))
+
+
+# ---------------------------------------------------------------------------------------------
+# tree_attention: what belongs to nodes beyond n_nodes, and lengths beyond the table
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("heads", [(8, 2), (6, 2), (32, 8)])
+@pytest.mark.parametrize("shape", [(4, 2, 4), (8, 2, 6)])
+def test_what_belongs_to_nodes_beyond_a_tree_reaches_no_row(heads, shape):
+    parent = tree(*shape)
+    N = parent.shape[-1]
+    nodes = [1, N, 0, N // 2, 7]
+    c = attention_case([50, 300, 7, 0, 900], parent.repeat(5, 1), *heads, 128, torch.bfloat16, 16, seed=41, n_nodes=nodes)
+    want = ref.attention(**c)
+    for b, n in enumerate(nodes):
+        c["q"][b, n:] = float("nan")
+        c["parent"][b, n:] = 2**31 - 1
+        at = torch.arange(int(c["lengths"][b]) + n, int(c["lengths"][b]) + N)
+        for name in ("k_cache", "v_cache"):
+            c[name][c["block_table"][b, at // 16].long(), at % 16] = float("nan")
+    check_attention(c, want)
+
+
+@pytest.mark.parametrize("window", [0, 50])
+def test_rows_of_lengths_beyond_the_table_are_those_of_its_keys(window):
+    c = attention_case([100], tree(4, 2, 4), 4, 2, 128, torch.bfloat16, 16, seed=14, window=window, sinks=3)
+    held = int((c["block_table"][0] >= 0).sum()) * 16             # (the tree itself lies beyond)
+    c["lengths"][0] = 2**31 - 1 - 19
+    got = binding.tree_attention(**cuda(c), want_lse=True)
+    assert got.status.tolist() == [ref.PAGE]
+    at = torch.arange(3 if window else held)
+    k = c["k_cache"][c["block_table"][0, at // 16].long(), at % 16].double().repeat_interleave(2, 1)
+    v = c["v_cache"][c["block_table"][0, at // 16].long(), at % 16].double().repeat_interleave(2, 1)
+    score = torch.einsum("nhd,jhd->nhj", c["q"][0].double(), k) * 128 ** -0.5
+    p = torch.softmax(score, -1)
+    want = torch.einsum("nhj,jhd->nhd", p, v)
+    bound = torch.einsum("nhj,jhd->nhd", p, v.abs()) * (2.0**-8 + 2.0**-10) + want.abs() * 2.0**-8
+    assert bool(((got.out[0].cpu().double() - want).abs() <= bound).all())
+    assert bool(((got.lse[0].cpu().double() - torch.logsumexp(score, -1)).abs() <= 2.0**-16).all())
