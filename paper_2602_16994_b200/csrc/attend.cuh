@@ -9,9 +9,15 @@
 // rows take 1040 cycles of products and about 1100 of arithmetic per scheduler, 256 rows twice that, so up to about 250 rows the cache's
 // bytes are the floor, and both products go to the tensor cores even for one row (which fills 1 of 128 lanes).  A thread owns a row, and maxima and
 // sums need no exchange.  Measured (one B200): a tile takes 3100 cycles with up to 128 rows (8 requests, 19 nodes, 4 query heads to a key
-// head, contexts to 4096: 38 us, floor 15) and 4500 with 204 (128 requests of 51 nodes: 445 us at 1.55 GHz, floor 226): there a row block's
-// weights wait for its products and these for their turn on the tensor cores.  Small calls are bound by latency: one token over 8192 keys takes 23 us
-// (floor 5), of which 5 pass until the first scores are there, 1.2 a tile, and 6 from the last tile to the joined result.
+// head, contexts to 4096: 38 us, floor 15) and 4500 with 204 (128 requests of 51 nodes: 443 us in a short row of calls, 517 to 524 in a long one, which
+// runs into the power limit at 1.64 GHz; floor 226): there a row block's weights wait for its products and these for their turn on the tensor cores.
+// Small calls are bound by latency: one token over 8192 keys takes 23 us (floor 5), of which 5 pass until the first scores are there, 1.2 a
+// tile, and 6 from the last tile to the joined result.
+//
+// Precision.  Scores, references, sums and O are fp32.  P is rounded to the type of the values: the product takes two operands of one type, and the rest
+// of P as a second operand would cost the products with V again, and their arithmetic.  The rounding is half a step (2^-8 of a weight in bf16,
+// 2^-11 in fp16), by itself for every weight, so a row is off by 2^-8 sum p |v| at most; measured against 64 bits, 0.0021 to 0.0023 of the result's norm
+// where rounding it once leaves 0.0017 (fp16: 0.00029, 0.00021).  l sums the weights before they are rounded.
 //
 // Balance.  The tiles of all units, in order, are cut into one run per CTA (one CTA per SM), whatever the lengths: a unit that a
 // run ends in leaves its O, l and reference in the workspace, and spec_join_kernel puts such parts together.  Every CTA finds its run from
@@ -400,8 +406,8 @@ __device__ __forceinline__ unsigned long long exp2_pair(unsigned long long y2)
 }
 // 32 columns of scores: weights, their sum, and the weights rounded to the values' type, two to a register.  One pair of eight goes without the
 // special function unit.  By itself the loop is fastest with three of eight (128 columns of two warps of a scheduler: 1826 cycles, none: 2381), in the
-// kernel, whose schedulers have the other roles' instructions to issue as well, with one (128 requests of 51 nodes: 445 us, three of eight: 456,
-// half: 471).
+// kernel, whose schedulers have the other roles' instructions to issue as well, with one (128 requests of 51 nodes, short rows of calls: 445 us, three of
+// eight: 456, half: 471).
 template <typename T>
 __device__ __forceinline__ void weigh(const uint32_t (&s)[32], unsigned long long c2, unsigned long long r2, unsigned long long &sum, uint32_t (&pk)[16])
 {
@@ -827,8 +833,8 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                 let_go(&B->q_empty);
             } else if (MT == 2) {
                 // A tile in two parts of 64 keys: while the weights of one part are at work the other has its products, and its next scores right behind
-                // them.  (Products of a part: 8 with N = 64 for S, which take as long as 6 of full width, 4 with N = 128 for O.  128 requests of 51 nodes: 457
-                // us; scores of a whole tile at once, which are ready later: 498; weights of a whole tile at once as well: 505.)
+                // them.  (Products of a part: 8 with N = 64 for S, which take as long as 6 of full width, 4 with N = 128 for O.  128 requests of 51 nodes, when
+                // this was chosen: 457 us; scores of a whole tile at once, which are ready later: 498; weights of a whole tile at once as well: 505.)
                 copied(n, n_tile);
                 for (int h = 0; h < S::PARTS; ++h) scores(m, h, (m * S::PARTS + h) * S::W, n, &B->s_full[m * S::PARTS + h], h == S::PARTS - 1);
                 if (steps == 1) let_go(&B->q_empty);
