@@ -48,7 +48,7 @@ extern "C" {
 #define SPEC_OK 0
 #define SPEC_ERR_NULL (-1)        /* a required pointer is NULL                                  */
 #define SPEC_ERR_SHAPE (-2)       /* B, N, V or a stride is out of range                         */
-#define SPEC_ERR_DTYPE (-3)       /* logits_dtype is neither SPEC_F32 nor SPEC_BF16              */
+#define SPEC_ERR_DTYPE (-3)       /* a dtype that the call does not take                          */
 #define SPEC_ERR_PARAM (-4)       /* temperature <= 0 or not finite, top_p outside (0,1], top_k < 0 */
 #define SPEC_ERR_WORKSPACE (-5)   /* ws NULL, misaligned or too small                            */
 #define SPEC_ERR_UNSUPPORTED (-6) /* vocabulary too large for the on-chip plan of this device    */
@@ -65,7 +65,7 @@ extern "C" {
 
 #define SPEC_F32 0
 #define SPEC_BF16 1
-#define SPEC_F16 2                /* the operators on projections and caches only                */
+#define SPEC_F16 2                /* the operators on projections and caches, and log probabilities */
 
 typedef struct {
     int32_t B, N, V;              /* sequences, nodes per sequence (root included), vocabulary   */
@@ -427,6 +427,76 @@ typedef struct {
     int32_t *status;                  /* [B]                                                          */
 } SpecChains;
 int32_t spec_verify_probs(const SpecChains *a, void *stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Shared prefixes, bounded caches, and what a service answers with.  Caches, tables, lengths and trees as above.
+ * ------------------------------------------------------------------------------------------------ */
+
+/*
+ * Log probabilities of given tokens under rows of logits, with the rows' entropy and their most probable tokens.  Row (b, i) is
+ *   logits[b,i] where parent is NULL;
+ *   the logits of the i-th node of the path to accepted_node[b], the root being the 0th, where parent is given: what a verification's
+ *   out_tokens[b,i] was put out from.  Behind the path, and where accepted_node[b] is -1, there is no row.
+ * With y = z / temperature:  logprob = y_token - log sum exp y;  entropy = -sum p log p, in nats;  top: the `top` largest by (logit, lower index
+ * first), and their log probabilities.  A token of -1 is none: its logprob is 0.  Where there is no row, logprob, entropy and top_logprobs
+ * are 0 and top_tokens -1.
+ * A row with NaN or +inf, or only -inf: SPEC_DEV_NONFINITE, its values NaN and top_tokens -1.  A token outside [-1,V): SPEC_DEV_TOKEN and a
+ * logprob of NaN.  accepted_node outside [-1,N) or a bad parent on its path: SPEC_DEV_TOPOLOGY, as without a row.
+ * Exponentials and sums of up to a few hundred entries in fp32, everything above in fp64.
+ */
+#define SPEC_MAX_TOP 32
+typedef struct {
+    int32_t B, N, V, K, top, dtype;   /* K given tokens a row (with parent: 1); top up to SPEC_MAX_TOP and V; SPEC_F32, SPEC_BF16 or SPEC_F16 */
+    const void *logits;               /* row of (b, i) at b * seq_stride + i * node_stride; its V entries are contiguous */
+    int64_t seq_stride, node_stride;  /* in elements                                                  */
+    const int32_t *parent;            /* optional [N], or [B,N] with topo_seq_stride = N              */
+    int64_t topo_seq_stride;
+    const int32_t *accepted_node;     /* [B], with parent                                             */
+    const int32_t *token;             /* [B,N,K]; may be NULL for K = 0                               */
+    float temperature;                /* in [1e-30, 1e30]                                             */
+    float *logprob;                   /* [B,N,K]                                                      */
+    float *entropy;                   /* [B,N]                                                        */
+    int32_t *top_tokens;              /* [B,N,top]                                                    */
+    float *top_logprobs;              /* [B,N,top]                                                    */
+    int32_t *status;                  /* [B,N]                                                        */
+} SpecLogprobs;
+int32_t spec_token_logprobs(const SpecLogprobs *a, void *stream);
+
+/*
+ * Eviction: a request with more than `budget` committed tokens keeps `budget` entries: its first p = protected[b], its last
+ * min(recent, budget - p), and of those between the ones with the largest weights (NaN below everything; of equal ones the lower entry).
+ * They move together in order, in every cache and in weights; entries from `budget` on keep what they held.  lengths_out[b] = budget.
+ * Blocks behind the shortened request go back to the ring behind the free ones, request by request: owned_out[b] = ceil(budget / block_size).
+ * block_table stays as it is (its columns from owned_out[b] on are no longer the request's); owned and free_range are inputs and stay too.
+ * Requests of at most `budget` tokens stay as they are, blocks included.
+ * protected[b] > budget, or a negative one: SPEC_DEV_TOPOLOGY; a bad block id in the owned columns, or fewer of them than
+ * the tokens need: SPEC_DEV_PAGE; then nothing of the request moves.  A ring without room for a request's blocks (or a free_range
+ * outside it): SPEC_DEV_BLOCKS, the request is shortened but keeps its blocks.  Blocks that hold entries behind protected[b] must be the request's own.
+ * No tree is under way: entries behind the committed tokens are not kept.
+ * `ws`: spec_cache_evict_workspace_bytes() bytes.
+ */
+typedef struct {
+    int32_t B, caches, budget, recent;
+    int32_t num_blocks, block_size, table_width;
+    void *cache;                      /* row of slot e of block k of cache c: c * stride[0] + k * stride[1] + e * stride[2] bytes */
+    int64_t stride[3];
+    int64_t row_bytes;                /* below 2^31                                                   */
+    float *weights;                   /* [num_blocks, block_size]                                     */
+    const int32_t *block_table;
+    int64_t table_stride;
+    const int32_t *lengths;           /* [B]                                                          */
+    const int32_t *owned;             /* [B]                                                          */
+    const int32_t *protected_len;     /* optional [B]                                                 */
+    int32_t *free_blocks;             /* [free_size]; entries behind the free ones are written        */
+    int32_t free_size;
+    const int32_t *free_range;        /* [2]                                                          */
+    int32_t *lengths_out;             /* [B]                                                          */
+    int32_t *owned_out;               /* [B]                                                          */
+    int32_t *free_range_out;          /* [2]                                                          */
+    int32_t *status;                  /* [B]                                                          */
+} SpecEvict;
+int32_t spec_cache_evict_workspace_bytes(const SpecEvict *a, int64_t *bytes);
+int32_t spec_cache_evict(const SpecEvict *a, void *ws, int64_t ws_bytes, void *stream);
 
 /* Launch plan of SpecInfer's walk for a vocabulary size and dtype, of a batch under top-k that fills the
  * device several times over (host-only query, for benchmarks and tests; smaller batches and batches

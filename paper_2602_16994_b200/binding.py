@@ -10,6 +10,8 @@ Device-resident API (inputs already in HBM, nothing is synchronised):
     verify_specinfer / verify_traversal / verify_otlp / tree_probs / sample_bonus / tree_analysis
 Around a verification in a decoding loop with a paged cache (likewise):
     cache_slots / norm_rope_cache / tree_attention / verify_probs / cache_commit
+Bounded caches and answers (likewise):
+    cache_evict / token_logprobs / path_logprobs
 Host API (pinned host buffers in, host results out; copies and one stream sync inside):
     HostVerifier
 """
@@ -32,7 +34,8 @@ EXPORTS = ("spec_workspace_bytes", "spec_tree_probs", "spec_verify_specinfer", "
            "spec_verify_specinfer_static", "spec_kernel_launches", "spec_analysis_workspace_bytes",
            "spec_tree_analysis", "spec_latency_model", "spec_test_hooks", "spec_row_statistics",
            "spec_verify_otlp", "spec_cache_slots", "spec_norm_rope_cache", "spec_tree_attention_workspace_bytes",
-           "spec_tree_attention", "spec_cache_commit", "spec_verify_probs")
+           "spec_tree_attention", "spec_cache_commit", "spec_verify_probs", "spec_token_logprobs",
+           "spec_cache_evict_workspace_bytes", "spec_cache_evict")
 
 
 class SpecIn(C.Structure):
@@ -128,6 +131,7 @@ def _calls():
             raise RuntimeError(f"the native host path is missing: build it with `python -m paper_2602_16994_b200.build` ({e})")
         _torch_calls.init(LIB_PATH, VerifyOutputs, AnalysisOutputs)
         _torch_calls.init_step(LIB_PATH, SlotOutputs, AttentionOutputs, CommitOutputs, ChainOutputs)
+        _torch_calls.init_serve(LIB_PATH, LogprobOutputs, EvictOutputs)
         _native = _torch_calls
     return _native
 
@@ -483,6 +487,51 @@ def verify_probs(target_probs, draft_probs, token, cu_drafts, u_accept, u_bonus,
     in [0, 1); ``max_drafts``: no request has more.
     """
     return _calls().verify_probs(target_probs, draft_probs, token, cu_drafts, u_accept, u_bonus, max_drafts, stream)
+
+
+@dataclass
+class LogprobOutputs:
+    logprob: torch.Tensor                # as tokens, float32
+    entropy: torch.Tensor                # a float32 per row, in nats
+    top_tokens: torch.Tensor | None      # [..., top] int32, the most probable first
+    top_logprobs: torch.Tensor | None    # [..., top] float32
+    status: torch.Tensor                 # an int32 per row
+
+
+def token_logprobs(logits, tokens, temperature=1.0, top=0, stream=None) -> LogprobOutputs:
+    """Log probabilities of ``tokens`` under the rows of ``logits``, the rows' entropy and their ``top`` most probable tokens.
+
+    ``logits`` [R,V] or [B,N,V] (float32, bfloat16 or float16, any strides of the rows), ``tokens`` int32 with an entry per row, or a list
+    of entries per row ([R,K], [B,N,K]); -1: none, its logprob is 0.  ``top`` up to 32, of equal logits the lower token first.
+    """
+    return _calls().logprobs(logits, tokens, None, None, temperature, top, stream)
+
+
+def path_logprobs(logits, accepted_node, out_tokens, parent, temperature=1.0, top=0, stream=None) -> LogprobOutputs:
+    """The same for what a verification put out: ``out_tokens`` [B,N] along the path to ``accepted_node`` [B] (a verifier's outputs), under the
+    rows of ``logits`` [B,N,V] that its nodes have.  Behind a path's end 0, and -1 for the top tokens; only the paths' rows are read.
+    """
+    return _calls().logprobs(logits, out_tokens, accepted_node, parent, temperature, top, stream)
+
+
+@dataclass
+class EvictOutputs:
+    lengths: torch.Tensor        # [B] int32 committed tokens after the eviction
+    owned: torch.Tensor          # [B] int32 columns of the table still in use
+    free_range: torch.Tensor     # [2] int32 the ring with the freed blocks
+    status: torch.Tensor         # [B] int32
+
+
+def cache_evict(cache, weights, lengths, block_table, owned, free_blocks, free_range, budget, recent=0, protected=None,
+                stream=None) -> EvictOutputs:
+    """Requests with more than ``budget`` committed tokens keep ``budget`` entries: the first ``protected[b]``, the last ``recent``, and of
+    those between the ones with the largest ``weights`` ([num_blocks, block_size] float32; of equal ones the lower entry).
+
+    What is kept moves together, in order, in every cache of the stack ``cache`` [caches, num_blocks, block_size, ...] and in
+    ``weights``, in place.  Blocks that are no longer needed go behind the free ones of the ring ``free_blocks`` (in place); ``owned``,
+    ``free_range`` and ``lengths`` stay as they are, the new ones are returned.
+    """
+    return _calls().cache_evict(cache, weights, lengths, block_table, owned, free_blocks, free_range, budget, recent, protected, stream)
 
 
 class HostVerifier:

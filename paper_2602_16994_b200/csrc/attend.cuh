@@ -1091,7 +1091,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
 // The first P.ctas * groups CTAs: (CTA of the attention, JOIN_ROWS rows).  Where that one had the first of a unit's parts, they are put together, in
 // order: out = sum 2^(ref_c - ref) O_c / sum 2^(ref_c - ref) l_c.  The others: a request each, its status (from inputs alone, while the
 // attention still runs) and zeros for a bad tree.
-constexpr int JOIN_NT = 128, JOIN_ROWS = 8, CTAS_MAX = 160;
+constexpr int JOIN_NT = 128, JOIN_ROWS = 8;
 
 template <typename T, typename S> __global__ void __launch_bounds__(JOIN_NT, 8) spec_join_kernel(const __grid_constant__ Params P)
 {

@@ -1,0 +1,120 @@
+// libspecverify: bounded caches and what a service answers with -- host side of their C ABI.
+//
+// Kernels: logprobs.cuh (log probabilities, entropy, most probable tokens), evict.cuh (entries of a cache that are kept).
+// As in specverify.cu, this file validates arguments, chooses the launch shape and enqueues; it never allocates and never synchronises.
+#include "evict.cuh"
+#include "launch.h"
+#include "logprobs.cuh"
+
+namespace specv {
+
+int set_serve_hooks(long long cycles, int hold)
+{
+    if (cudaMemcpyToSymbol(c_wait_cycles, &cycles, sizeof(cycles)) != cudaSuccess ||
+        cudaMemcpyToSymbol(c_hold_slot, &hold, sizeof(hold)) != cudaSuccess) {
+        cudaGetLastError();
+        return SPEC_ERR_CUDA;
+    }
+    return SPEC_OK;
+}
+
+}  // namespace specv
+
+using namespace specv;
+
+extern "C" {
+
+int32_t spec_token_logprobs(const SpecLogprobs *a, void *stream)
+{
+    if (!a || !a->logits || !a->entropy || !a->status || (a->K > 0 && (!a->token || !a->logprob)) ||
+        (a->top > 0 && (!a->top_tokens || !a->top_logprobs)) || (a->parent && !a->accepted_node))
+        return SPEC_ERR_NULL;
+    if (a->B < 1 || a->N < 1 || a->V < 1 || a->K < 0 || a->seq_stride < 0 || a->node_stride < 0 || (int64_t)a->B * a->N > (1 << 26) ||
+        (a->parent && (a->K > 1 || a->N > SPEC_MAX_NODES)) || (a->topo_seq_stride != 0 && a->topo_seq_stride < a->N))
+        return SPEC_ERR_SHAPE;
+    if (a->dtype != SPEC_F32 && a->dtype != SPEC_BF16 && a->dtype != SPEC_F16) return SPEC_ERR_DTYPE;
+    if (!(a->temperature >= 1e-30f && a->temperature <= 1e30f) || a->top < 0 || a->top > SPEC_MAX_TOP || a->top > a->V) return SPEC_ERR_PARAM;
+    if (!aligned(a->logits, a->dtype == SPEC_F32 ? 4 : 2)) return SPEC_ERR_UNSUPPORTED;
+    const int64_t rows = (int64_t)a->B * a->N;
+    // the largest cluster that leaves every CTA a batch of loads and the chip one wave
+    const int batch = logp::NT * logp::BATCH * (a->dtype == SPEC_F32 ? 4 : 8);
+    int C = 1;
+    while (C < logp::CMAX && a->V > C * batch / 2 && rows * 2 * C <= 148 * 2) C *= 2;
+    logp::Params p = {};
+    p.B = a->B; p.N = a->N; p.V = a->V; p.K = a->K; p.top = a->top; p.C = C;
+    p.logits = a->logits; p.seq_stride = a->seq_stride; p.node_stride = a->node_stride;
+    p.parent = a->parent; p.accepted = a->accepted_node; p.topo_seq_stride = a->topo_seq_stride; p.token = a->token;
+    p.T = a->temperature; p.c = 1.4426950408889634f / a->temperature;
+    p.logprob = a->logprob; p.entropy = a->entropy; p.top_logprobs = a->top_logprobs; p.top_tokens = a->top_tokens; p.status = a->status;
+    const auto go = [&](auto kernel) {
+        const int rc = prepare(kernel, 0, true);
+        return rc ? rc : launch(kernel, dim3((unsigned)(rows * C)), logp::NT, 0, C > 1 ? C : 0, (cudaStream_t)stream, p);
+    };
+    return a->dtype == SPEC_F32  ? go(logp::spec_logprobs_kernel<float>)
+           : a->dtype == SPEC_F16 ? go(logp::spec_logprobs_kernel<__half>)
+                                  : go(logp::spec_logprobs_kernel<__nv_bfloat16>);
+}
+
+static int evict_check(const SpecEvict *a)
+{
+    if (!a || !a->cache || !a->weights || !a->block_table || !a->lengths || !a->owned || !a->free_range || !a->lengths_out || !a->owned_out ||
+        !a->free_range_out || !a->status || (a->free_size > 0 && !a->free_blocks))
+        return SPEC_ERR_NULL;
+    if (a->B < 1 || a->B > 65535 || bad_pages(a->num_blocks, a->block_size, a->table_width) || a->table_stride < a->table_width || a->caches < 1 ||
+        a->row_bytes < 1 || a->row_bytes > 0x7FFFFFFF || a->free_size < 0)
+        return SPEC_ERR_SHAPE;
+    if (a->budget < 1 || a->recent < 0 || a->lengths_out == a->lengths || a->owned_out == a->owned || a->owned_out == a->lengths ||
+        a->lengths_out == a->owned || a->free_range_out == a->free_range)
+        return SPEC_ERR_PARAM;
+    return SPEC_OK;
+}
+// (a request keeps no more entries than its row of the table has room for)
+static int64_t most_moves(const SpecEvict *a) { return std::min<int64_t>(a->budget, (int64_t)a->table_width * a->block_size); }
+static int64_t evict_bytes(const SpecEvict *a) { return ((int64_t)a->B * 8 + 255) / 256 * 256 + (int64_t)a->B * most_moves(a) * 8; }
+
+int32_t spec_cache_evict_workspace_bytes(const SpecEvict *a, int64_t *bytes)
+{
+    if (!bytes) return SPEC_ERR_NULL;
+    const int rc = evict_check(a);
+    if (rc) return rc;
+    *bytes = evict_bytes(a);
+    return SPEC_OK;
+}
+
+int32_t spec_cache_evict(const SpecEvict *a, void *ws, int64_t ws_bytes, void *stream)
+{
+    int rc = evict_check(a);
+    if (rc) return rc;
+    if (!ws || !aligned(ws, 256) || ws_bytes < evict_bytes(a)) return SPEC_ERR_WORKSPACE;
+    evict::Params p = {};
+    p.B = a->B; p.caches = a->caches; p.budget = a->budget; p.recent = a->recent;
+    p.num_blocks = a->num_blocks; p.block = a->block_size; p.width = a->table_width; p.free_size = a->free_size;
+    p.cache = (unsigned char *)a->cache; p.weights = a->weights; p.table = a->block_table; p.table_stride = a->table_stride;
+    p.lengths = a->lengths; p.owned = a->owned; p.protect = a->protected_len; p.range = a->free_range; p.ring = a->free_blocks;
+    p.lengths_out = a->lengths_out; p.owned_out = a->owned_out; p.range_out = a->free_range_out; p.status = a->status;
+    p.plan = (int2 *)ws;
+    p.moves = (int2 *)((unsigned char *)ws + ((int64_t)a->B * 8 + 255) / 256 * 256);
+    p.row_moves = most_moves(a);
+    int64_t all = (int64_t)(uintptr_t)a->cache | a->row_bytes;
+    for (int j = 0; j < 3; ++j) { p.stride[j] = a->stride[j]; all |= a->stride[j]; }
+    const int unit = all % 16 == 0 ? 16 : all % 4 == 0 ? 4 : 1;
+    p.total = (unsigned)(a->row_bytes / unit);
+    // slices of 256 bytes, less where a word is less
+    p.words = std::min(p.total, 16u);
+    p.slices = (int)((p.total + p.words - 1) / p.words);
+    if ((int64_t)p.slices * a->caches + 1 > 0x7FFFFFFF) return SPEC_ERR_UNSUPPORTED;
+    const cudaStream_t st = (cudaStream_t)stream;
+    rc = prepare(evict::spec_evict_select_kernel, 0, false);
+    if (!rc) rc = launch(evict::spec_evict_select_kernel, dim3(a->B), evict::NT, 0, 0, st, p);
+    if (rc) return rc;
+    const dim3 grid((unsigned)(p.slices * a->caches + 1), a->B);
+    const auto go = [&](auto kernel) {
+        const int e = prepare(kernel, 0, false);
+        return e ? e : launch(kernel, grid, evict::MOVE_NT, 0, 0, st, p);
+    };
+    return unit == 16  ? go(evict::spec_evict_move_kernel<uint4>)
+           : unit == 4 ? go(evict::spec_evict_move_kernel<uint32_t>)
+                       : go(evict::spec_evict_move_kernel<unsigned char>);
+}
+
+}  // extern "C"

@@ -14,9 +14,11 @@
 #include <c10/cuda/CUDAStream.h>
 #include <dlfcn.h>
 
+#include <algorithm>
 #include <cmath>
 #include <initializer_list>
 #include <optional>
+#include <vector>
 
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -800,6 +802,145 @@ PyObject *py_init_step(PyObject *, PyObject *args)
     Py_RETURN_NONE;
 }
 
+// ---- bounded caches, and what a service answers with ----------------------------------------------------------------------------
+struct ServeLibrary {
+    decltype(&spec_token_logprobs) logprobs;
+    decltype(&spec_cache_evict_workspace_bytes) evict_bytes;
+    decltype(&spec_cache_evict) evict;
+} serve_lib;
+PyObject *logprob_outputs_class, *evict_outputs_class;
+
+// logprobs(logits, tokens, accepted_node, parent, temperature, top, stream): rows as they are where parent is None
+PyObject *py_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!arity(n, 7)) return nullptr;
+    return guarded([&]() -> PyObject * {
+        need((void *)serve_lib.logprobs);
+        const at::Tensor &z = cuda_tensor(a[0], "logits");
+        const Place place(z, a[6]);
+        const auto type = z.scalar_type();
+        if (element_type(type) < 0) raise("logits must be float32, bfloat16 or float16");
+        const bool path = a[3] != Py_None;
+        if (z.dim() != 2 && z.dim() != 3) raise("logits must be [R,V] or [B,N,V]");
+        if (path && z.dim() != 3) raise("logits must be [B,N,V]");
+        rows_of(z, "logits", (int)z.dim(), type, place);
+        no_gradient(z, "logits");
+        const int64_t B = z.size(0), N = z.dim() == 3 ? z.size(1) : 1, V = z.size(-1);
+        const at::Tensor &token = ints(a[1], "tokens", place);
+        SpecLogprobs s = {};
+        std::vector<int64_t> rows(z.sizes().begin(), z.sizes().end() - 1), given = rows, best = rows;
+        const int64_t lead = (int64_t)rows.size();
+        if (token.dim() < lead || token.dim() > lead + 1 || !std::equal(rows.begin(), rows.end(), token.sizes().begin()))
+            raise("tokens must have an entry, or a list of entries, per row of logits");
+        if (path && token.dim() != 2) raise("tokens must be [B,N]");
+        const int64_t K = token.dim() == lead ? 1 : token.size(lead);
+        if (token.dim() > lead) given.push_back(K);
+        s.B = small(B, "B"); s.N = small(N, "N"); s.V = small(V, "V"); s.K = small(K, "K"); s.top = whole(a[5], "top");
+        s.dtype = element_type(type);
+        s.logits = z.data_ptr();
+        s.seq_stride = B > 1 ? z.stride(0) : 0;
+        s.node_stride = N > 1 ? z.stride(1) : 0;
+        s.token = int_ptr(token);
+        s.temperature = (float)number(a[4]);
+        if (path) {
+            int64_t nodes;
+            s.topo_seq_stride = tree_of(a[3], place, B, &nodes, &s.parent);
+            if (nodes != N) raise("logits must be [B,N,V] with the N of parent");
+            s.accepted_node = int_ptr(ints(a[2], "accepted_node", place, B));
+        }
+        best.push_back(s.top < 0 ? 0 : s.top);
+        at::Tensor t[5];
+        t[0] = place.fresh(given, at::kFloat);
+        t[1] = place.fresh(rows, at::kFloat);
+        if (s.top > 0) { t[2] = place.fresh(best, at::kInt); t[3] = place.fresh(best, at::kFloat); }
+        t[4] = place.fresh(rows, at::kInt);
+        s.logprob = (float *)t[0].data_ptr(); s.entropy = (float *)t[1].data_ptr(); s.status = int_ptr(t[4]);
+        if (s.top > 0) { s.top_tokens = int_ptr(t[2]); s.top_logprobs = (float *)t[3].data_ptr(); }
+        if (B * N) check(unlocked([&] { return serve_lib.logprobs(&s, place.stream()); }), "spec_token_logprobs");
+        return result(logprob_outputs_class, t, 5);
+    });
+}
+
+// a stack of caches [caches, num_blocks, block_size, ...] that the call writes: bytes of a row
+int64_t stack_of(const at::Tensor &cache, const Place &place, int64_t (&stride)[3])
+{
+    place.uses(cache, "cache");
+    no_gradient(cache, "cache");
+    apart(cache, "cache");
+    if (cache.dim() < 4) raise("cache must be [caches, num_blocks, block_size, ...]");
+    int64_t row = 1;
+    for (int64_t i = cache.dim() - 1; i >= 3; --i) {
+        if (cache.size(i) > 1 && cache.stride(i) != row) raise("the entries of a slot of cache must be contiguous");
+        row *= cache.size(i);
+    }
+    const int64_t esz = cache.element_size();
+    for (int i = 0; i < 3; ++i) stride[i] = cache.size(i) > 1 ? cache.stride(i) * esz : 0;
+    return row * esz;
+}
+// weights of entries, [num_blocks, block_size]
+float *entry_weights(PyObject *o, const Place &place, int64_t blocks, int64_t block)
+{
+    const at::Tensor &t = cuda_tensor(o, "weights");
+    check_vector(t, "weights", at::kFloat, "torch.float32");
+    if (t.dim() != 2 || t.size(0) != blocks || t.size(1) != block) raise("weights must be [num_blocks, block_size]");
+    no_gradient(t, "weights");
+    place.uses(t, "weights");
+    return (float *)t.data_ptr();
+}
+
+// cache_evict(cache, weights, lengths, block_table, owned, free_blocks, free_range, budget, recent, protected, stream)
+PyObject *py_evict(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!arity(n, 11)) return nullptr;
+    return guarded([&]() -> PyObject * {
+        need((void *)serve_lib.evict);
+        const at::Tensor &cache = cuda_tensor(a[0], "cache");
+        const Place place(cache, a[10]);
+        SpecEvict s = {};
+        s.row_bytes = stack_of(cache, place, s.stride);
+        s.caches = small(cache.size(0), "caches"); s.num_blocks = small(cache.size(1), "num_blocks"); s.block_size = small(cache.size(2), "block_size");
+        s.weights = entry_weights(a[1], place, cache.size(1), cache.size(2));
+        const at::Tensor &lengths = cuda_tensor(a[2], "lengths");
+        const int64_t B = ints(a[2], "lengths", place).numel();
+        const Table table = table_of(a[3], place, B);
+        const at::Tensor &ring = ints(a[5], "free_blocks", place);
+        apart(ring, "free_blocks");
+        s.B = small(B, "B"); s.budget = whole(a[7], "budget"); s.recent = whole(a[8], "recent");
+        s.table_width = table.width; s.block_table = table.ptr; s.table_stride = table.stride;
+        s.cache = cache.data_ptr();
+        s.lengths = int_ptr(lengths); s.owned = int_ptr(ints(a[4], "owned", place, B));
+        s.protected_len = a[9] == Py_None ? nullptr : int_ptr(ints(a[9], "protected", place, B));
+        s.free_blocks = int_ptr(ring); s.free_size = small(ring.numel(), "free_blocks");
+        s.free_range = int_ptr(ints(a[6], "free_range", place, 2));
+        Pieces made(place, {B, B, 2, B});
+        const at::Tensor t[4] = {made.take({B}), made.take({B}), made.take({2}), made.take({B})};
+        s.lengths_out = int_ptr(t[0]); s.owned_out = int_ptr(t[1]); s.free_range_out = int_ptr(t[2]); s.status = int_ptr(t[3]);
+        int64_t bytes = 0;
+        check(serve_lib.evict_bytes(&s, &bytes), "spec_cache_evict_workspace_bytes");
+        const at::Tensor ws = empty({bytes}, at::kByte, place.device());         // (of this call alone)
+        check(unlocked([&] { return serve_lib.evict(&s, ws.data_ptr(), bytes, place.stream()); }), "spec_cache_evict");
+        written(cache); written(THPVariable_Unpack(a[1])); written(ring);
+        return result(evict_outputs_class, t, 4);
+    });
+}
+
+// init_serve(path of libspecverify.so, LogprobOutputs, EvictOutputs): the entry points above
+PyObject *py_init_serve(PyObject *, PyObject *args)
+{
+    const char *path;
+    PyObject *c[2];
+    if (!PyArg_ParseTuple(args, "sOO", &path, &c[0], &c[1])) return nullptr;
+    void *h = dlopen(path, RTLD_NOW | RTLD_LOCAL);
+    if (!h) return PyErr_Format(PyExc_RuntimeError, "%s", dlerror());
+    const auto find = [&](auto &f, const char *name) { f = reinterpret_cast<std::remove_reference_t<decltype(f)>>(dlsym(h, name)); };
+    find(serve_lib.logprobs, "spec_token_logprobs");
+    find(serve_lib.evict_bytes, "spec_cache_evict_workspace_bytes");
+    find(serve_lib.evict, "spec_cache_evict");
+    logprob_outputs_class = Py_NewRef(c[0]);
+    evict_outputs_class = Py_NewRef(c[1]);
+    Py_RETURN_NONE;
+}
+
 PyMethodDef methods[] = {
     {"init", py_init, METH_VARARGS, nullptr},
     {"verify", (PyCFunction)(void *)py_verify, METH_FASTCALL, nullptr},
@@ -813,6 +954,9 @@ PyMethodDef methods[] = {
     {"tree_attention", (PyCFunction)(void *)py_attention, METH_FASTCALL, nullptr},
     {"cache_commit", (PyCFunction)(void *)py_commit, METH_FASTCALL, nullptr},
     {"verify_probs", (PyCFunction)(void *)py_chains, METH_FASTCALL, nullptr},
+    {"init_serve", py_init_serve, METH_VARARGS, nullptr},
+    {"logprobs", (PyCFunction)(void *)py_logprobs, METH_FASTCALL, nullptr},
+    {"cache_evict", (PyCFunction)(void *)py_evict, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_torch_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

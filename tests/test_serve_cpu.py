@@ -1,0 +1,68 @@
+"""Host-side checks of log probabilities and of the calls on a bounded cache: what they refuse, before a device is touched."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2602_16994_b200 import binding
+from .test_step_cpu import F, I, L, P, S3, filled, lib, struct  # noqa: F401
+
+Logprobs = struct("SpecLogprobs", (I, "B N V K top dtype"), (P, "logits"), (L, "seq_stride node_stride"), (P, "parent"), (L, "topo_seq_stride"),
+                  (P, "accepted_node token"), (F, "temperature"), (P, "logprob entropy top_tokens top_logprobs status"))
+Evict = struct("SpecEvict", (I, "B caches budget recent num_blocks block_size table_width"), (P, "cache"), (S3, "stride"), (L, "row_bytes"),
+               (P, "weights block_table"), (L, "table_stride"), (P, "lengths owned protected_len free_blocks"), (I, "free_size"),
+               (P, "free_range lengths_out owned_out free_range_out status"))
+
+
+def test_logprobs_refusals(lib):  # noqa: F811
+    good = dict(V=100, temperature=1.0, parent=None)
+    call = lambda **kw: lib.spec_token_logprobs(C.byref(filled(Logprobs, **dict(good, **kw))), None)  # noqa: E731
+    assert lib.spec_token_logprobs(None, None) == -1
+    for f in ("logits", "token", "logprob", "entropy", "top_tokens", "top_logprobs", "status"):
+        assert call(**{f: None}) == -1, f
+    assert call(parent=0x9000, accepted_node=None) == -1
+    for kw in (dict(B=0), dict(N=0), dict(V=0), dict(K=-1), dict(seq_stride=-1), dict(node_stride=-5), dict(B=1 << 14, N=1 << 14),
+               dict(parent=0x9000, K=2), dict(parent=0x9000, N=1025), dict(parent=0x9000, N=5, topo_seq_stride=4)):
+        assert call(**kw) == -2, kw
+    for dtype in (-1, 3):
+        assert call(dtype=dtype) == -3
+    for kw in (dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=float("nan")), dict(temperature=1e31), dict(top=33), dict(top=-1),
+               dict(V=4, top=5)):
+        assert call(**kw) == -4, kw
+    assert call(logits=0x10001) == -6 and call(logits=0x10002, dtype=0) == -6
+
+
+def test_evict_refusals(lib):  # noqa: F811
+    good = dict(table_stride=1, row_bytes=16)
+    n = L()
+    size = lambda **kw: lib.spec_cache_evict_workspace_bytes(C.byref(filled(Evict, **dict(good, **kw))), C.byref(n))  # noqa: E731
+    assert size() == 0 and n.value >= 8
+    assert lib.spec_cache_evict_workspace_bytes(None, C.byref(n)) == -1
+    assert lib.spec_cache_evict_workspace_bytes(C.byref(filled(Evict, **good)), None) == -1
+    for f in ("cache", "weights", "block_table", "lengths", "owned", "free_blocks", "free_range", "lengths_out", "owned_out", "free_range_out",
+              "status"):
+        assert size(**{f: None}) == -1, f
+    assert size(free_size=0, free_blocks=None) == 0 and size(protected_len=None) == 0
+    for kw in (dict(B=0), dict(B=65536), dict(caches=0), dict(num_blocks=0), dict(block_size=0), dict(table_width=0), dict(row_bytes=0),
+               dict(row_bytes=2**31), dict(table_width=2), dict(free_size=-1), dict(num_blocks=1 << 20, block_size=1 << 12)):
+        assert size(**kw) == -2, kw
+    for kw in (dict(budget=0), dict(budget=-3), dict(recent=-1), dict(lengths=0x50000, lengths_out=0x50000), dict(owned=0x50000, owned_out=0x50000),
+               dict(owned=0x50000, lengths_out=0x50000), dict(lengths=0x50000, owned_out=0x50000), dict(free_range=0x50000, free_range_out=0x50000)):
+        assert size(**kw) == -4, kw
+    # a budget beyond the table costs no more than the table
+    size(budget=2**31 - 1, table_width=4, table_stride=4, block_size=16)
+    assert n.value <= 256 + 64 * 8
+    call = lambda ws, b: lib.spec_cache_evict(C.byref(filled(Evict, **good)), P(ws), L(b), None)  # noqa: E731
+    size()
+    assert call(None, 1 << 30) == -5 and call(0x10010, 1 << 30) == -5 and call(0x10000, n.value - 1) == -5
+
+
+@pytest.mark.parametrize("name,args", [
+    ("token_logprobs", lambda t, i: (t[0, 0], i)),
+    ("path_logprobs", lambda t, i: (t[0], i, i[None], i)),
+    ("cache_evict", lambda t, i: (t, t[0, 0], i, i[None], i, i, i, 1))])
+def test_the_calls_refuse_to_run_without_a_gpu(lib, name, args):  # noqa: F811
+    with pytest.raises(RuntimeError, match="CUDA device"):
+        getattr(binding, name)(*args(torch.zeros(1, 1, 1, 8), torch.zeros(1, dtype=torch.int32)))
+    with pytest.raises(TypeError):
+        getattr(binding, name)(*([None] * len(args(torch.zeros(1, 1, 1, 8), torch.zeros(1, dtype=torch.int32)))))
