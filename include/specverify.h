@@ -463,6 +463,39 @@ typedef struct {
 int32_t spec_token_logprobs(const SpecLogprobs *a, void *stream);
 
 /*
+ * Attention weight that entries of the cache get, added up: for every entry j of a request (committed tokens, then the tree's nodes)
+ *   weights[slot of j] += sum over nodes i that see j, and query heads h, of exp(scale q[b,i,h] . k_j - lse[b,i,h]),
+ * with lse from spec_tree_attention (or spec_prefix_attention) without a window.  Entries below protected[b] (tokens that are never evicted: a shared
+ * prefix, the first few) are left out: neither their keys nor their weights are touched.  fresh != 0: the tree's entries count from 0,
+ * whatever their slots held (the first layer of a step).  A row whose lse is not finite adds nothing, and nothing of its query matters.
+ * Sums in fp32 in a fixed order: the same inputs give the same bits.  A key on a bad block is left out (SPEC_DEV_PAGE); a bad tree leaves
+ * the request's weights as they were (SPEC_DEV_TOPOLOGY).  The blocks behind protected[b] must be the request's own.
+ * What is no number (a score of NaN) adds nothing.  SPEC_DEV_TIMEOUT (a wait ran out): the weights of the requests with this status are undefined.
+ * D: 64, 128 or 256; q and cache SPEC_BF16 or SPEC_F16; strides in elements, multiples of 8, bases on 16 bytes.
+ */
+typedef struct {
+    int32_t B, N, Hq, Hkv, D, dtype;
+    int32_t num_blocks, block_size, table_width;
+    int32_t fresh;
+    float scale;                      /* >= 0, finite                                                 */
+    const void *q;
+    int64_t q_stride[3];              /* request, node, head                                          */
+    const void *k_cache;
+    int64_t k_cache_stride[3];        /* block, slot, head                                            */
+    const float *lse;                 /* [B,N,Hq]                                                     */
+    const int32_t *block_table;
+    int64_t table_stride;
+    const int32_t *lengths;           /* [B]                                                          */
+    const int32_t *n_nodes;           /* optional [B]                                                 */
+    const int32_t *parent;            /* [N], or [B,N] with topo_seq_stride = N                       */
+    int64_t topo_seq_stride;
+    const int32_t *protected_len;     /* optional [B]                                                 */
+    float *weights;                   /* [num_blocks, block_size]                                     */
+    int32_t *status;                  /* [B]                                                          */
+} SpecWeights;
+int32_t spec_cache_weights(const SpecWeights *a, void *stream);
+
+/*
  * Eviction: a request with more than `budget` committed tokens keeps `budget` entries: its first p = protected[b], its last
  * min(recent, budget - p), and of those between the ones with the largest weights (NaN below everything; of equal ones the lower entry).
  * They move together in order, in every cache and in weights; entries from `budget` on keep what they held.  lengths_out[b] = budget.
@@ -515,7 +548,7 @@ int64_t spec_kernel_launches(void);
  * hangs); these two settings let a test watch that happen.  wait_cycles: the limit of every on-device
  * wait in clock cycles (<= 0: the default, about 2 s).  hold_slot: index b * N + node of one node whose
  * Traversal weight the node kernels then never publish, so that the node's own wait runs out, and whose
- * sequence's queries the tree attention then never fetches, so that its waits for them do
+ * sequence's queries the tree attention and spec_cache_weights then never fetch, so that their waits for them do
  * (-1: none).  Synchronous (copies to constant memory of the current device); call it between
  * verification calls, never while one is in flight.
  */

@@ -11,7 +11,7 @@ Device-resident API (inputs already in HBM, nothing is synchronised):
 Around a verification in a decoding loop with a paged cache (likewise):
     cache_slots / norm_rope_cache / tree_attention / verify_probs / cache_commit
 Bounded caches and answers (likewise):
-    cache_evict / token_logprobs / path_logprobs
+    cache_weights / cache_evict / token_logprobs / path_logprobs
 Host API (pinned host buffers in, host results out; copies and one stream sync inside):
     HostVerifier
 """
@@ -35,7 +35,7 @@ EXPORTS = ("spec_workspace_bytes", "spec_tree_probs", "spec_verify_specinfer", "
            "spec_tree_analysis", "spec_latency_model", "spec_test_hooks", "spec_row_statistics",
            "spec_verify_otlp", "spec_cache_slots", "spec_norm_rope_cache", "spec_tree_attention_workspace_bytes",
            "spec_tree_attention", "spec_cache_commit", "spec_verify_probs", "spec_token_logprobs",
-           "spec_cache_evict_workspace_bytes", "spec_cache_evict")
+           "spec_cache_weights", "spec_cache_evict_workspace_bytes", "spec_cache_evict")
 
 
 class SpecIn(C.Structure):
@@ -512,6 +512,17 @@ def path_logprobs(logits, accepted_node, out_tokens, parent, temperature=1.0, to
     rows of ``logits`` [B,N,V] that its nodes have.  Behind a path's end 0, and -1 for the top tokens; only the paths' rows are read.
     """
     return _calls().logprobs(logits, out_tokens, accepted_node, parent, temperature, top, stream)
+
+
+def cache_weights(weights, q, k_cache, lse, block_table, lengths, parent, n_nodes=None, scale=None, protected=None, fresh=False,
+                  stream=None) -> torch.Tensor:
+    """Adds to ``weights`` ([num_blocks, block_size] float32, in place) the attention weight that each entry of the cache gets from the nodes
+    of its request's tree, over all heads: sum exp(scale q . k - lse).  Returns the requests' status.
+
+    ``q``, ``k_cache``, table, lengths and tree as in ``tree_attention``, ``lse`` [B,N,Hq] what that call returned (without a window).
+    Entries below ``protected[b]`` are left out.  ``fresh``: the tree's own entries start from 0 (the first layer of a step).
+    """
+    return _calls().cache_weights(weights, q, k_cache, lse, block_table, lengths, parent, n_nodes, scale, protected, fresh, stream)
 
 
 @dataclass

@@ -11,7 +11,8 @@ SRC = [os.path.join(HERE, "csrc", f) for f in ("specverify.cu", "step.cu", "serv
 DEPS = {"specverify.cu": ("common.cuh", "host.h", "verify.cuh", "rowops.cuh", "cut.cuh", "stream.cuh", "walk.cuh", "nodes.cuh", "trunc.cuh",
                           "analysis.cuh"),
         "step.cu": ("common.cuh", "host.h", "launch.h", "tree.cuh", "tmem.cuh", "slots.cuh", "rope.cuh", "attend.cuh", "chain.cuh", "commit.cuh"),
-        "serve.cu": ("common.cuh", "host.h", "launch.h", "tree.cuh", "cut.cuh", "logprobs.cuh", "evict.cuh")}
+        "serve.cu": ("common.cuh", "host.h", "launch.h", "tree.cuh", "cut.cuh", "tmem.cuh", "attend.cuh", "logprobs.cuh", "weigh.cuh",
+                     "evict.cuh")}
 LIB = os.path.join(HERE, "libspecverify.so")
 HEADERS = [os.path.join(ROOT, "include", "specverify.h")]
 

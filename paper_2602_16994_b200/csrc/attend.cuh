@@ -171,7 +171,7 @@ struct Run {
 };
 // The next segment of a run; false at its end.  (Once in the code: every role of the kernel takes its segments here, and what runs once
 // per segment costs its instructions' fetching.)
-__device__ __noinline__ bool next_segment(const Params &P, int block_rows, Run *run, Segment *s)
+static __device__ __noinline__ bool next_segment(const Params &P, int block_rows, Run *run, Segment *s)
 {
     if (run->left <= 0) return false;
     Place at = run->at;
@@ -459,7 +459,7 @@ struct Row {
     float ref, l;
     bool any;
 };
-__device__ __noinline__ void scale_sums(uint32_t at, int columns, float f)
+static __device__ __noinline__ void scale_sums(uint32_t at, int columns, float f)
 {
     for (int d = 0; d < columns; d += 32) {
         uint32_t o[32];
@@ -531,7 +531,7 @@ __device__ __noinline__ void put_back(const Params &P, const Segment &seg, int n
 
 // Whether a row sees any key of a segment: asked for rows whose weights came to nothing, which are 0 where they see nothing, and no number where all that
 // they see has a score of -inf (0 / 0).
-__device__ __noinline__ bool sees_any(const Params &P, const Segment &seg, int node, int depth, const unsigned short *parent)
+static __device__ __noinline__ bool sees_any(const Params &P, const Segment &seg, int node, int depth, const unsigned short *parent)
 {
     Walk walk = {node, 0};
     for (int step = 0; step < seg.steps(); ++step) {

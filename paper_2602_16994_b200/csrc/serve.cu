@@ -1,10 +1,12 @@
 // libspecverify: bounded caches and what a service answers with -- host side of their C ABI.
 //
-// Kernels: logprobs.cuh (log probabilities, entropy, most probable tokens), evict.cuh (entries of a cache that are kept).
+// Kernels: logprobs.cuh (log probabilities, entropy, most probable tokens), weigh.cuh (attention weight that
+// entries of a cache get), evict.cuh (entries of a cache that are kept).
 // As in specverify.cu, this file validates arguments, chooses the launch shape and enqueues; it never allocates and never synchronises.
 #include "evict.cuh"
 #include "launch.h"
 #include "logprobs.cuh"
+#include "weigh.cuh"
 
 namespace specv {
 
@@ -53,6 +55,50 @@ int32_t spec_token_logprobs(const SpecLogprobs *a, void *stream)
     return a->dtype == SPEC_F32  ? go(logp::spec_logprobs_kernel<float>)
            : a->dtype == SPEC_F16 ? go(logp::spec_logprobs_kernel<__half>)
                                   : go(logp::spec_logprobs_kernel<__nv_bfloat16>);
+}
+
+int32_t spec_cache_weights(const SpecWeights *a, void *stream)
+{
+    if (!a || !a->q || !a->k_cache || !a->lse || !a->block_table || !a->lengths || !a->parent || !a->weights || !a->status) return SPEC_ERR_NULL;
+    if (bad_tree_shape(a->B, a->N, a->topo_seq_stride) || bad_pages(a->num_blocks, a->block_size, a->table_width) ||
+        a->table_stride < a->table_width || a->Hkv < 1 || a->Hq < a->Hkv || a->Hq % a->Hkv || a->Hq > 65535)
+        return SPEC_ERR_SHAPE;
+    if (a->dtype != SPEC_BF16 && a->dtype != SPEC_F16) return SPEC_ERR_DTYPE;
+    if (!(a->scale >= 0.f && a->scale <= 3.4e38f)) return SPEC_ERR_PARAM;
+    if (a->D != 64 && a->D != 128 && a->D != 256) return SPEC_ERR_UNSUPPORTED;
+    // (tiles, and steps of a tile, are counted in 32 bits)
+    const double tiles = (double)std::min<int64_t>((int64_t)a->table_width * a->block_size, 0x7FFFFFFF) / weigh::KT + 2;
+    const double steps = (double)a->Hkv * (((double)a->N * (a->Hq / a->Hkv)) / 64 + 1);
+    if (a->B * tiles > 2.0e9 || a->B * tiles * steps / 148 > 1.0e9) return SPEC_ERR_UNSUPPORTED;
+    int64_t all = 0;
+    for (int j = 0; j < 3; ++j) all |= a->q_stride[j] | a->k_cache_stride[j];
+    if (all % 8 || !aligned(a->q, 16) || !aligned(a->k_cache, 16)) return SPEC_ERR_UNSUPPORTED;
+    weigh::Params p = {};
+    p.tree = tree_args(a->N, a->lengths, a->n_nodes, a->parent, a->topo_seq_stride);
+    p.B = a->B; p.Hq = a->Hq; p.Hkv = a->Hkv; p.G = a->Hq / a->Hkv;
+    p.num_blocks = a->num_blocks; p.block = a->block_size; p.width = a->table_width; p.fresh = a->fresh != 0;
+    divisor(a->block_size, &p.block_mul, &p.block_shift);
+    divisor(p.G, &p.group_mul, &p.group_shift);
+    p.c = a->scale * weigh::LOG2E;
+    p.q = a->q; p.k = a->k_cache; p.lse = a->lse; p.table = a->block_table; p.table_stride = a->table_stride;
+    p.protect = a->protected_len; p.weights = a->weights; p.status = a->status;
+    for (int j = 0; j < 3; ++j) { p.q_stride[j] = a->q_stride[j]; p.k_stride[j] = a->k_cache_stride[j]; }
+    p.ctas = sm_ctas();
+    const bool half = a->dtype == SPEC_F16;
+    p.box = a->block_size % 8 ? 0 : a->block_size % 16 ? 8 : a->block_size % 32 ? 16 : 32;
+    const int64_t sizes[4] = {a->D, a->Hkv, a->block_size, a->num_blocks};
+    if (p.box && !tensor_map(&p.k_map, a->k_cache, half, sizes, {a->k_cache_stride[2], a->k_cache_stride[1], a->k_cache_stride[0]}, {1, p.box, 1}))
+        p.box = 0;
+    const auto go = [&](auto shape, auto kernel) -> int {
+        using S = decltype(shape);
+        const int smem = S::total + 1024, rc = prepare(kernel, smem, false);
+        return rc ? rc : launch(kernel, dim3(p.ctas), weigh::NT, smem, 0, (cudaStream_t)stream, p);
+    };
+#define GO(D)                                                                                                  \
+    (half ? go(weigh::Shape<D>(), weigh::spec_weigh_kernel<__half, weigh::Shape<D>>)                           \
+          : go(weigh::Shape<D>(), weigh::spec_weigh_kernel<__nv_bfloat16, weigh::Shape<D>>))
+    return a->D == 256 ? GO(256) : a->D == 128 ? GO(128) : GO(64);
+#undef GO
 }
 
 static int evict_check(const SpecEvict *a)

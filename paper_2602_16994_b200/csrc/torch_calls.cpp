@@ -805,6 +805,7 @@ PyObject *py_init_step(PyObject *, PyObject *args)
 // ---- bounded caches, and what a service answers with ----------------------------------------------------------------------------
 struct ServeLibrary {
     decltype(&spec_token_logprobs) logprobs;
+    decltype(&spec_cache_weights) weights;
     decltype(&spec_cache_evict_workspace_bytes) evict_bytes;
     decltype(&spec_cache_evict) evict;
 } serve_lib;
@@ -888,6 +889,49 @@ float *entry_weights(PyObject *o, const Place &place, int64_t blocks, int64_t bl
     return (float *)t.data_ptr();
 }
 
+// cache_weights(weights, q, k_cache, lse, block_table, lengths, parent, n_nodes, scale, protected, fresh, stream)
+PyObject *py_weights(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!arity(n, 12)) return nullptr;
+    return guarded([&]() -> PyObject * {
+        need((void *)serve_lib.weights);
+        const at::Tensor &q = cuda_tensor(a[1], "q"), &kc = cuda_tensor(a[2], "k_cache");
+        const Place place(q, a[11]);
+        const auto type = q.scalar_type();
+        if (type != at::kBFloat16 && type != at::kHalf) raise("q must be bfloat16 or float16");
+        rows_of(q, "q", 4, type, place);
+        rows_of(kc, "k_cache", 4, type, place);
+        no_gradient(q, "q"); no_gradient(kc, "k_cache");
+        const int64_t B = q.size(0), Hq = q.size(2), D = q.size(3);
+        if (kc.size(3) != D) raise("the cache must be [num_blocks, block_size, Hkv, D]");
+        SpecWeights s = {};
+        int64_t N;
+        s.topo_seq_stride = tree_of(a[6], place, B, &N, &s.parent);
+        if (N != q.size(1)) raise("q must be [B,N,Hq,D] with the N of parent");
+        const Table table = table_of(a[4], place, B);
+        s.B = small(B, "B"); s.N = small(N, "N"); s.Hq = small(Hq, "Hq"); s.Hkv = small(kc.size(2), "Hkv"); s.D = small(D, "D");
+        s.dtype = element_type(type);
+        s.num_blocks = small(kc.size(0), "num_blocks"); s.block_size = small(kc.size(1), "block_size"); s.table_width = table.width;
+        s.scale = a[8] == Py_None ? (float)(1.0 / std::sqrt((double)(D > 0 ? D : 1))) : (float)number(a[8]);
+        s.fresh = truth(a[10]);
+        s.block_table = table.ptr; s.table_stride = table.stride;
+        s.lengths = int_ptr(ints(a[5], "lengths", place, B));
+        s.n_nodes = a[7] == Py_None ? nullptr : int_ptr(ints(a[7], "n_nodes", place, B));
+        s.protected_len = a[9] == Py_None ? nullptr : int_ptr(ints(a[9], "protected", place, B));
+        const at::Tensor &lse = floats(a[3], "lse", place, B * N * Hq);
+        no_gradient(lse, "lse");
+        s.lse = (const float *)lse.data_ptr();
+        s.weights = entry_weights(a[0], place, kc.size(0), kc.size(1));
+        s.q = q.data_ptr(); s.k_cache = kc.data_ptr();
+        strides_of(q, s.q_stride); strides_of(kc, s.k_cache_stride);
+        const at::Tensor status = place.fresh({B}, at::kInt);
+        s.status = int_ptr(status);
+        check(unlocked([&] { return serve_lib.weights(&s, place.stream()); }), "spec_cache_weights");
+        written(THPVariable_Unpack(a[0]));
+        return THPVariable_Wrap(status);
+    });
+}
+
 // cache_evict(cache, weights, lengths, block_table, owned, free_blocks, free_range, budget, recent, protected, stream)
 PyObject *py_evict(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -934,6 +978,7 @@ PyObject *py_init_serve(PyObject *, PyObject *args)
     if (!h) return PyErr_Format(PyExc_RuntimeError, "%s", dlerror());
     const auto find = [&](auto &f, const char *name) { f = reinterpret_cast<std::remove_reference_t<decltype(f)>>(dlsym(h, name)); };
     find(serve_lib.logprobs, "spec_token_logprobs");
+    find(serve_lib.weights, "spec_cache_weights");
     find(serve_lib.evict_bytes, "spec_cache_evict_workspace_bytes");
     find(serve_lib.evict, "spec_cache_evict");
     logprob_outputs_class = Py_NewRef(c[0]);
@@ -956,6 +1001,7 @@ PyMethodDef methods[] = {
     {"verify_probs", (PyCFunction)(void *)py_chains, METH_FASTCALL, nullptr},
     {"init_serve", py_init_serve, METH_VARARGS, nullptr},
     {"logprobs", (PyCFunction)(void *)py_logprobs, METH_FASTCALL, nullptr},
+    {"cache_weights", (PyCFunction)(void *)py_weights, METH_FASTCALL, nullptr},
     {"cache_evict", (PyCFunction)(void *)py_evict, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_torch_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

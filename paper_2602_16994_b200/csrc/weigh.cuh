@@ -1,0 +1,506 @@
+// Attention weight that entries of a paged cache get (spec_cache_weights).
+//
+// Mathematics.  w_j += sum over rows (node i that sees j, query head) of 2^(c k_j . q_r - lse_r log2 e), c = scale log2 e.  The product is taken with the
+// keys as the tensor cores' rows: S = K Q^T, 128 keys by up to 128 rows of a key head, so a thread owns a key and adds up along its own
+// columns; over the rows, blocks of rows and key heads its sum never leaves its register, and no two CTAs add to the same entry: the order
+// of every sum is fixed.
+//
+// What bounds it.  With few rows the keys' bytes: 256 KB a tile of 128 keys at 8 heads of 128 entries.  With many rows the exponentials.
+//
+// Layout.  Units are tiles of 128 entries of a request, all key heads; the tiles of all requests, in order, are cut into one run per CTA (one CTA per
+// SM).  Two tiles that lie wholly among the committed tokens go together: a block of queries that is on chip serves both.
+// Four warps copy (keys by tensor map where all 32 of a warp's keys are there and blocks are multiples of 8 slots, else 16 bytes at a time), one issues
+// the products, eight take the exponentials: half of the columns each warpgroup.
+//
+// What is not a number adds nothing: the maximum that bounds exponents from below takes NaN for its bound.  So it does not matter what
+// rows without a finite lse, columns beyond the rows, or keys that are not there hold.
+#pragma once
+#include "attend.cuh"
+
+namespace specv {
+namespace weigh {
+
+constexpr int KT = 128, PANEL = 128 * 128;
+constexpr float LOG2E = 1.4426950408889634f;
+
+struct Params {
+    CUtensorMap k_map;                         // the cache as [block][slot][head][entry], boxes of `box` slots by 64 entries
+    int box;                                   // a power of two up to 32 that divides the block; 0: blocks of no multiple of 8 slots
+    TreeArgs tree;
+    int B, Hq, Hkv, G, num_blocks, block, width, fresh;
+    unsigned block_mul, group_mul;             // divisions by block and G, as in the attention
+    int block_shift, group_shift;
+    float c;
+    const void *q, *k;
+    long long q_stride[3], k_stride[3];
+    const float *lse;
+    const int *table;
+    long long table_stride;
+    const int *protect;
+    float *weights;
+    int *status;
+    int ctas;
+};
+
+struct Request {
+    int len, n, from, end;                     // nodes (0: idle or a bad number of them); entries [from, end) count
+    __device__ __forceinline__ int first() const { return from / KT; }
+    __device__ __forceinline__ int tiles() const { return n == 0 || end <= from ? 0 : (end + KT - 1) / KT - from / KT; }
+};
+__device__ __forceinline__ Request request_of(const Params &P, int b)
+{
+    Request r;
+    r.len = __ldg(P.tree.lengths + b);
+    r.n = r.len < 0 ? 0 : max(0, tree_nodes(P.tree, b));
+    // (entries behind the table's end have no block)
+    const long long held = min((long long)P.width * P.block, 0x7FFFFFFFll);
+    r.end = r.len < 0 ? 0 : (int)min((long long)r.len + r.n, held);
+    r.from = P.protect ? max(0, __ldg(P.protect + b)) : 0;
+    return r;
+}
+__device__ __forceinline__ int column_of(const Params &P, int key) { return (int)((__umulhi(P.block_mul, (unsigned)key) + (unsigned)key) >> P.block_shift); }
+__device__ __forceinline__ int node_of(const Params &P, int row) { return (int)((__umulhi(P.group_mul, (unsigned)row) + (unsigned)row) >> P.group_shift); }
+
+// What a CTA has next: a tile of a request, or two; every role counts for itself.
+struct Run {
+    int b, t, left;                            // t: tiles of the request gone by
+    Request r;
+    int tile, count;                           // this step's
+    __device__ __forceinline__ bool next(const Params &P)
+    {
+        if (left <= 0) return false;
+        while (t >= r.tiles()) {
+            if (++b >= P.B) return false;
+            r = request_of(P, b);
+            t = 0;
+        }
+        tile = r.first() + t;
+        count = left >= 2 && t + 1 < r.tiles() && (long long)(tile + 2) * KT <= r.len ? 2 : 1;
+        t += count;
+        left -= count;
+        return true;
+    }
+};
+
+template <int D_> struct Shape {
+    static constexpr int D = D_, PANELS = D / 64, QB = D == 256 ? 64 : 128;       // rows of a block of queries
+    static constexpr int K_SLOT = KT * D * 2, Q_SLOT = QB * D * 2;
+    static constexpr int SK = D == 64 ? 6 : D == 128 ? 3 : 2, SQ = D == 64 ? 4 : D == 128 ? 3 : 2;
+    static constexpr int off_q = SK * K_SLOT, off_mask = off_q + SQ * Q_SLOT;
+    static constexpr int off_ref = off_mask + SPEC_MAX_NODES * 16;                // [SQ][128] -lse log2 e
+    static constexpr int off_node = off_ref + SQ * 128 * 4;                       // [SQ][128] nodes of the columns
+    static constexpr int off_parent = off_node + SQ * 128 * 2;
+    static constexpr int off_part = off_parent + SPEC_MAX_NODES * 2;              // [2][2][128] the other warpgroup's sums
+    static constexpr int off_bar = off_part + 2048;
+    static constexpr int total = off_bar + 512;
+    static_assert(total + 1024 <= 227 * 1024, "shared memory");
+};
+constexpr int SUM_WARPS = 8, PRODUCTS = SUM_WARPS, NT = (SUM_WARPS + 1 + 4) * 32;
+struct Bars {
+    uint64_t k_full[6], k_empty[6], q_full[4], q_empty[4], s_full[4], s_empty[4];
+    uint32_t tmem;
+    int dead, last, found[2], sums[16];        // (last: the last request that this CTA had tiles of)
+};
+static_assert(sizeof(Bars) <= 512, "the area behind the buffers");
+
+__device__ __forceinline__ void wait(Bars *B, uint64_t *bar, uint32_t parity)
+{
+    if (mbar_try_wait(bar, parity)) return;
+    const long long t0 = clock64();
+    do {
+        if (*(volatile int *)&B->dead) return;
+        if (clock64() - t0 > WAIT_CYCLES) { *(volatile int *)&B->dead = 1; return; }
+    } while (!mbar_try_wait(bar, parity));
+}
+// one answer for the whole (converged) warp
+__device__ __forceinline__ bool stopped(Bars *B) { return __any_sync(0xffffffffu, *(volatile int *)&B->dead) != 0; }
+
+// The run of CTA c: all threads.
+__device__ __forceinline__ void find_run(const Params &P, int c, Bars *S, Run *run, int tid)
+{
+    const int lane = tid & 31, warp = tid >> 5;
+    const int per = (P.B + NT - 1) / NT, b0 = min(P.B, tid * per), b1 = min(P.B, b0 + per);
+    int mine = 0;
+    for (int b = b0; b < b1; ++b) mine += request_of(P, b).tiles();
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += t;
+    }
+    if (lane == 31) S->sums[warp] = incl;
+    if (tid == 0) { S->found[0] = P.B; S->found[1] = 0; }
+    __syncthreads();
+    int ahead = incl - mine, all = 0;
+    for (int w = 0; w < NT / 32; ++w) {
+        if (w < warp) ahead += S->sums[w];
+        all += S->sums[w];
+    }
+    const int each = (int)((unsigned)all / (unsigned)P.ctas), more = all - each * P.ctas, start = each * c + min(c, more);
+    if (start >= ahead && start < ahead + mine) {
+        for (int b = b0; b < b1; ++b) {
+            const int t = request_of(P, b).tiles();
+            if (start < ahead + t) { S->found[0] = b; S->found[1] = start - ahead; break; }
+            ahead += t;
+        }
+    }
+    __syncthreads();
+    run->left = each + (c < more);
+    run->b = S->found[0];
+    run->t = S->found[1];
+    if (run->b >= P.B) run->left = 0;
+    else run->r = request_of(P, run->b);
+}
+
+template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_weigh_kernel(const __grid_constant__ Params P)
+{
+    constexpr int D = S::D;
+    unsigned char *base = dyn_smem + (-smem_u32(dyn_smem) & 1023u);
+    Bars *B = (Bars *)(base + S::off_bar);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (warp == PRODUCTS) tc::tmem_alloc(&B->tmem, 512);
+    if (tid == NT - 1 && P.box) tc::prefetch_map(&P.k_map);
+    if (tid == 0) {
+        for (int i = 0; i < S::SK; ++i) { mbar_init(&B->k_full[i], 128); mbar_init(&B->k_empty[i], 1); }
+        for (int i = 0; i < S::SQ; ++i) { mbar_init(&B->q_full[i], 256); mbar_init(&B->q_empty[i], 1 + SUM_WARPS); }
+        for (int i = 0; i < 4; ++i) { mbar_init(&B->s_full[i], 1); mbar_init(&B->s_empty[i], SUM_WARPS); }
+        B->dead = 0;
+        B->last = -1;
+        mbar_fence_init();
+    }
+    grid_dependency_wait();
+    Run run;
+    find_run(P, blockIdx.x, B, &run, tid);
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    const uint32_t tmem = B->tmem;
+    if (warp < SUM_WARPS) {
+        // ---------------------------------------------------------------- sums: a thread owns a key
+        const int w = warp >> 2, quad = warp & 3, mine = quad * 32 + lane;
+        const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
+        unsigned short *parent = (unsigned short *)(base + S::off_parent);
+        uint4 *mask = (uint4 *)(base + S::off_mask);
+        float *part = (float *)(base + S::off_part);
+        // requests' status, from the inputs alone (CTA b mod ctas writes request b's); one whose CTA a wait ran out in is marked at the end
+        for (int b = blockIdx.x; b < P.B; b += P.ctas) {
+            const int len = __ldg(P.tree.lengths + b), nn = tree_nodes(P.tree, b), n = len < 0 ? 0 : max(nn, 0);
+            const int *row = P.tree.parent + (long long)b * P.tree.topo_seq_stride;
+            bool bad = false, page = false;
+            for (int i = tid; i < n; i += 256) {
+                const int p = __ldg(row + i);
+                bad |= i == 0 ? p != -1 : p < 0 || p >= i;
+            }
+            const long long keys = n ? (long long)len + n : 0;
+            const int from = P.protect ? max(0, __ldg(P.protect + b)) : 0;
+            if (n && from < keys) {
+                page = keys > (long long)P.width * P.block;
+                const int last = (int)min((keys + P.block - 1) / P.block, (long long)P.width);
+                for (int col = from / P.block + tid; col < last; col += 256) {
+                    const int id = __ldg(P.table + (long long)b * P.table_stride + col);
+                    page |= id < 0 || id >= P.num_blocks;
+                }
+            }
+            part[tid] = __int_as_float((bad ? 1 : 0) | (page ? 2 : 0));
+            bar_sync(1, 256);
+            if (warp == 0) {
+                int x = 0;
+                for (int i = lane; i < 256; i += 32) x |= __float_as_int(part[i]);
+                bad = __any_sync(0xffffffffu, x & 1) != 0;
+                page = __any_sync(0xffffffffu, x & 2) != 0;
+                if (lane == 0) P.status[b] = len < 0 ? SPEC_DEV_OK : nn < 0 || bad ? SPEC_DEV_TOPOLOGY : page ? SPEC_DEV_PAGE : SPEC_DEV_OK;
+            }
+            bar_sync(1, 256);
+        }
+        const unsigned long long c2 = pack_f32x2(P.c, P.c);
+        uint32_t n_q = 0, n_s = 0, n_step = 0;
+        int tree_of = -1;
+        bool sound = true;
+        for (; run.next(P); ++n_step) {
+            const Request r = run.r;
+            const int rows = r.n * P.G, blocks = (rows + S::QB - 1) / S::QB;
+            // the thread's entry of the tile that it finishes, and what it holds
+            const int entry = (run.tile + (run.count == 2 ? w : 0)) * KT + mine;
+            long long slot = -1;
+            float old = 0.f;
+            if (entry >= r.from && entry < r.end && w < run.count) {
+                const int col = column_of(P, entry), id = __ldg(P.table + (long long)run.b * P.table_stride + col);
+                if (id >= 0 && id < P.num_blocks) {
+                    slot = (long long)id * P.block + (entry - col * P.block);
+                    if (!(P.fresh && entry >= r.len)) old = __ldcg(P.weights + slot);
+                }
+            }
+            if (tree_of != run.b) {
+                bool bad = false;
+                const int *row = P.tree.parent + (long long)run.b * P.tree.topo_seq_stride;
+                bar_sync(1, 256);
+                for (int i = tid; i < r.n; i += 256) {
+                    const int p = __ldg(row + i);
+                    const bool wrong = i == 0 ? p != -1 : p < 0 || p >= i;
+                    parent[i] = wrong || i == 0 ? (unsigned short)0xFFFF : (unsigned short)p;
+                    bad |= wrong;
+                }
+                part[tid] = __int_as_float(bad ? 1 : 0);
+                bar_sync(1, 256);
+                int x = 0;
+                for (int i = lane; i < 256; i += 32) x |= __float_as_int(part[i]);
+                sound = __any_sync(0xffffffffu, x) == 0;
+                tree_of = run.b;
+                bar_sync(1, 256);
+            }
+            const bool masked = (long long)(run.tile + 1) * KT > r.len;            // (then the tile goes by itself)
+            if (masked) {
+                // what each node sees of the tile: itself and its ancestors, by doubling, and all committed tokens
+                const long long a = (long long)run.tile * KT;
+                constexpr int MINE = SPEC_MAX_NODES / 256;
+                int up[MINE];
+                uint4 m[MINE];
+#pragma unroll
+                for (int x = 0; x < MINE; ++x) {
+                    const int i = x * 256 + tid;
+                    m[x] = make_uint4(0, 0, 0, 0);
+                    up[x] = 0xFFFF;
+                    if (i >= r.n) continue;
+                    up[x] = parent[i];
+                    const long long at = (long long)r.len + i - a;
+                    uint32_t bits[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) bits[k] = at >= 32 * k && at < 32 * k + 32 ? 1u << (at & 31) : 0u;
+                    m[x] = make_uint4(bits[0], bits[1], bits[2], bits[3]);
+                    mask[i] = m[x];
+                }
+                unsigned short *above = parent;
+                bar_sync(1, 256);
+                for (int span = 1; span < r.n; span <<= 1) {
+                    uint4 more[MINE];
+                    int further[MINE];
+#pragma unroll
+                    for (int x = 0; x < MINE; ++x) {
+                        more[x] = make_uint4(0, 0, 0, 0);
+                        further[x] = up[x];
+                        if (up[x] != 0xFFFF) { more[x] = mask[up[x]]; further[x] = above[up[x]]; }
+                    }
+                    bar_sync(1, 256);
+#pragma unroll
+                    for (int x = 0; x < MINE; ++x) {
+                        const int i = x * 256 + tid;
+                        if (i >= r.n) continue;
+                        m[x].x |= more[x].x; m[x].y |= more[x].y; m[x].z |= more[x].z; m[x].w |= more[x].w;
+                        up[x] = further[x];
+                        mask[i] = m[x];
+                        above[i] = (unsigned short)up[x];
+                    }
+                    bar_sync(1, 256);
+                }
+                tree_of = -1;                                        // (the parents have been used up)
+                uint32_t all[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) all[k] = attend::bits_of(a + 32 * k, 0, r.len);
+#pragma unroll
+                for (int x = 0; x < MINE; ++x) {
+                    const int i = x * 256 + tid;
+                    if (i < r.n) mask[i] = make_uint4(m[x].x | all[0], m[x].y | all[1], m[x].z | all[2], m[x].w | all[3]);
+                }
+                bar_sync(1, 256);
+            }
+            float acc0 = 0.f, acc1 = 0.f;
+            for (int h = 0; h < P.Hkv; ++h)
+                for (int qb = 0; qb < blocks; ++qb, ++n_q) {
+                    const uint32_t qs = n_q % S::SQ;
+                    const int columns = min(S::QB, rows - qb * S::QB);
+                    wait(B, &B->q_full[qs], n_q / S::SQ & 1);
+                    const float *ref = (const float *)(base + S::off_ref) + qs * 128;
+                    const unsigned short *nodes = (const unsigned short *)(base + S::off_node) + qs * 128;
+                    for (int ti = 0; ti < run.count; ++ti, ++n_s) {
+                        const uint32_t buf = n_s & 3;
+                        wait(B, &B->s_full[buf], n_s >> 2 & 1);
+                        tc::fence_after();
+                        unsigned long long sum = 0ull;
+                        for (int g = w * 32; g < columns; g += 64) {
+                            uint32_t a[32];
+                            tc::tmem_load(lanes + buf * 128 + g, a);
+                            tc::wait_loads(a);
+                            if (masked) {
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) {
+                                    const uint32_t word = ((const uint32_t *)(mask + nodes[g + k]))[quad];
+                                    if (!((word >> lane) & 1u)) a[k] = 0xFF800000u;
+                                }
+                            }
+#pragma unroll
+                            for (int k = 0; k < 32; k += 4) {
+                                const float4 r4 = *(const float4 *)(ref + g + k);
+                                float x, y;
+                                unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(a[k]), __uint_as_float(a[k + 1])), c2, pack_f32x2(r4.x, r4.y)), x, y);
+                                sum = add_f32x2(sum, pack_f32x2(ex2_approx(fmaxf(x, -200.f)), ex2_approx(fmaxf(y, -200.f))));
+                                unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(a[k + 2]), __uint_as_float(a[k + 3])), c2, pack_f32x2(r4.z, r4.w)), x, y);
+                                sum = add_f32x2(sum, pack_f32x2(ex2_approx(fmaxf(x, -200.f)), ex2_approx(fmaxf(y, -200.f))));
+                            }
+                        }
+                        float x, y;
+                        unpack_f32x2(sum, x, y);
+                        if (ti == 0) acc0 += x + y; else acc1 += x + y;
+                        tc::fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&B->s_empty[buf]);
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&B->q_empty[qs]);
+                }
+            // each warpgroup finishes a tile, with what the other has of it
+            float *mail = part + (n_step & 1) * 256;
+            mail[(1 - w) * 128 + mine] = w ? acc0 : acc1;
+            bar_sync(1, 256);
+            const float got = (w ? acc1 : acc0) + mail[w * 128 + mine];
+            if (slot >= 0 && sound && *(volatile int *)&B->dead == 0) __stcg(P.weights + slot, old + got);
+            if (tid == 0) B->last = run.b;
+        }
+    } else if (warp == PRODUCTS) {
+        // ---------------------------------------------------------------- products: one thread issues
+        const uint32_t k_at = smem_u32(base), q_at = smem_u32(base + S::off_q);
+        uint32_t n_k = 0, n_q = 0, n_s = 0;
+        const auto gone = [&] { return *(volatile int *)&B->dead != 0; };
+        while (run.next(P)) {
+            const int rows = run.r.n * P.G, blocks = (rows + S::QB - 1) / S::QB;
+            for (int h = 0; h < P.Hkv; ++h, n_k += run.count)
+                for (int qb = 0; qb < blocks; ++qb, ++n_q) {
+                    const uint32_t qs = n_q % S::SQ;
+                    const int columns = (min(S::QB, rows - qb * S::QB) + 15) / 16 * 16;
+                    const uint32_t desc = tc::product_desc(attend::Pair<T>::TYPE, columns, false);
+                    wait(B, &B->q_full[qs], n_q / S::SQ & 1);
+                    for (int ti = 0; ti < run.count; ++ti, ++n_s) {
+                        const uint32_t ks = (n_k + ti) % S::SK, buf = n_s & 3;
+                        if (qb == 0) wait(B, &B->k_full[ks], (n_k + ti) / S::SK & 1);
+                        if (n_s >= 4) wait(B, &B->s_empty[buf], (n_s / 4 - 1) & 1);
+                        tc::publish_shared();
+                        tc::fence_after();
+                        if (tc::elected() && !gone()) {
+#pragma unroll
+                            for (int p = 0; p < S::PANELS; ++p) {
+                                const uint64_t kd = tc::panel_desc(k_at + ks * S::K_SLOT + p * PANEL);
+                                const uint64_t qd = tc::panel_desc(q_at + qs * S::Q_SLOT + p * S::QB * 128);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) tc::mma_ss(tmem + buf * 128, kd + 2 * i, qd + 2 * i, desc, p > 0 || i > 0);
+                            }
+                            tc::commit(&B->s_full[buf]);
+                            if (ti + 1 == run.count) tc::commit(&B->q_empty[qs]);
+                            if (qb + 1 == blocks) tc::commit(&B->k_empty[ks]);
+                        }
+                        __syncwarp();
+                    }
+                }
+        }
+    } else {
+        // ---------------------------------------------------------------- copies: a warp for 32 keys of every tile and 32 rows of every block of queries
+        const int which = warp - PRODUCTS - 1;
+        constexpr int CH = D / 8;                                     // 16-byte chunks of a row
+        const uint32_t k_at = smem_u32(base), q_at = smem_u32(base + S::off_q);
+        float *refs = (float *)(base + S::off_ref);
+        unsigned short *nodes = (unsigned short *)(base + S::off_node);
+        uint32_t n_k = 0, n_q = 0;
+        while (run.next(P)) {
+            const Request r = run.r;
+            const int rows = r.n * P.G, blocks = (rows + S::QB - 1) / S::QB;
+            int id[2], in[2];
+            bool whole[2];
+#pragma unroll
+            for (int ti = 0; ti < 2; ++ti) {
+                const long long key = (long long)(run.tile + ti) * KT + which * 32 + lane;
+                id[ti] = -1; in[ti] = 0;
+                if (ti < run.count && key >= r.from && key < r.end) {
+                    const int col = column_of(P, (int)key);
+                    in[ti] = (int)key - col * P.block;
+                    id[ti] = __ldg(P.table + (long long)run.b * P.table_stride + col);
+                    if (id[ti] >= P.num_blocks) id[ti] = -1;
+                }
+                whole[ti] = P.box && __all_sync(0xffffffffu, id[ti] >= 0);
+            }
+            // a row's reference, asked for a block ahead of its use
+            const auto reference = [&](int h, int qb) {
+                const int row = qb * S::QB + which * 32 + lane;
+                if (h >= P.Hkv || which * 32 >= S::QB || row >= rows) return -CUDART_INF_F;
+                const int node = node_of(P, row);
+                const float x = __ldg(P.lse + ((long long)run.b * P.tree.N + node) * P.Hq + h * P.G + row - node * P.G);
+                return fabsf(x) < CUDART_INF_F ? -x * LOG2E : -CUDART_INF_F;
+            };
+            float ahead = reference(0, 0);
+            for (int h = 0; h < P.Hkv; ++h) {
+                for (int ti = 0; ti < run.count; ++ti, ++n_k) {
+                    const uint32_t slot = n_k % S::SK;
+                    if (n_k >= S::SK) wait(B, &B->k_empty[slot], (n_k / S::SK - 1) & 1);
+                    __syncwarp();
+                    if (stopped(B)) continue;
+                    const uint32_t to = k_at + slot * S::K_SLOT;
+                    if (whole[ti]) {
+                        if (lane == 0) {
+                            tc::expect_bytes(&B->k_full[slot], 32 * D * 2);
+                            tc::arrive_many(&B->k_full[slot], 32);
+                        }
+                        __syncwarp();
+                        const int boxes = 32 / P.box, g = lane % boxes, p0 = lane / boxes;
+                        const int block = __shfl_sync(0xffffffffu, id[ti], g * P.box), at = __shfl_sync(0xffffffffu, in[ti], g * P.box);
+                        for (int p = p0; p < S::PANELS; p += P.box)
+                            tc::box_load(to + p * PANEL + (which * 32 + g * P.box) * 128, &P.k_map, p * 64, h, at, block, &B->k_full[slot]);
+                    } else {
+                        const unsigned long long from = id[ti] >= 0 ? (unsigned long long)((const T *)P.k + id[ti] * P.k_stride[0] + in[ti] * P.k_stride[1] +
+                                                                                           h * P.k_stride[2])
+                                                                    : (unsigned long long)P.k | 1;           // (odd: zeros)
+#pragma unroll 4
+                        for (int i = 0; i < CH; ++i) {
+                            const int y = i * 32 + lane, row = y / CH, ch = y % CH, at = which * 32 + row;
+                            const unsigned long long f = __shfl_sync(0xffffffffu, from, row);
+                            tc::copy16(to + ch / 8 * PANEL + at * 128 + (((ch & 7) ^ (at & 7)) << 4), (f & ~1ull) + (f & 1 ? 0 : ch * 16), f & 1 ? 0 : 16);
+                        }
+                        tc::arrive_with_copies(&B->k_full[slot]);
+                    }
+                }
+                for (int qb = 0; qb < blocks; ++qb, ++n_q) {
+                    const uint32_t slot = n_q % S::SQ;
+                    const float ref = ahead;
+                    ahead = qb + 1 < blocks ? reference(h, qb + 1) : reference(h + 1, 0);
+                    if (n_q >= S::SQ) wait(B, &B->q_empty[slot], (n_q / S::SQ - 1) & 1);
+                    __syncwarp();
+                    if (stopped(B)) continue;
+                    if (c_hold_slot >= 0 && c_hold_slot / P.tree.N == run.b) continue;       // (a test may ask for a request's queries to stay away)
+                    const int columns = min(S::QB, rows - qb * S::QB);
+                    if (which * 32 < (columns + 15) / 16 * 16) {
+                        const T *q = (const T *)P.q + run.b * P.q_stride[0] + (long long)h * P.G * P.q_stride[2];
+                        const uint32_t to = q_at + slot * S::Q_SLOT;
+                        const int mine = min(qb * S::QB + which * 32 + lane, rows - 1), node = node_of(P, mine);
+                        const unsigned long long from = (unsigned long long)(q + node * P.q_stride[1] + (mine - node * P.G) * P.q_stride[2]);
+#pragma unroll 4
+                        for (int i = 0; i < CH; ++i) {
+                            const int y = i * 32 + lane, row = y / CH, ch = y % CH, at = which * 32 + row;
+                            const unsigned long long f = __shfl_sync(0xffffffffu, from, row);
+                            tc::copy16(to + ch / 8 * (S::QB * 128) + at * 128 + (((ch & 7) ^ (at & 7)) << 4), f + ch * 16, at < columns ? 16 : 0);
+                        }
+                    }
+                    refs[slot * 128 + which * 32 + lane] = ref;
+                    nodes[slot * 128 + which * 32 + lane] = (unsigned short)node_of(P, min(qb * S::QB + which * 32 + lane, rows - 1));
+                    tc::arrive_with_copies(&B->q_full[slot]);
+                    mbar_arrive(&B->q_full[slot]);
+                }
+            }
+        }
+        tc::close_copies();
+        tc::wait_copies<0>();
+    }
+    if (*(volatile int *)&B->dead) {
+        // a wait ran out, and nobody waits any more: copies and products under way, which depend on nothing else, get a millisecond to end
+        const long long t0 = clock64();
+        while (clock64() - t0 < 2000000) __nanosleep(1000);
+    }
+    tc::fence_before();
+    __syncthreads();
+    if (warp == PRODUCTS) {
+        tc::fence_after();
+        tc::tmem_free(tmem, 512);
+        // (behind what the sums' warps of this CTA or another wrote of the request when they began, 2 s ago)
+        if (B->dead)
+            for (int b = B->found[0] + lane; b <= B->last; b += 32)
+                if (__ldg(P.tree.lengths + b) >= 0) P.status[b] = SPEC_DEV_TIMEOUT;
+    }
+}
+
+}  // namespace weigh
+}  // namespace specv

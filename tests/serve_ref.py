@@ -119,3 +119,52 @@ def evict(cache, weights, lengths, table, owned, ring, free_range, budget, recen
         owned_out[b] = stay
     range_out = torch.tensor([begin, count + put] if len(ring) else [0, 0], dtype=torch.int32)
     return dict(cache=cache, weights=weights, free_blocks=ring, lengths=lengths_out, owned=owned_out, free_range=range_out, status=status), kept
+
+
+def weights(w, q, k_cache, lse, table, lengths, parent, n_nodes=None, scale=None, protected=None, fresh=False):
+    """weights after the call, status, and per entry the bound's ingredients: what was added, sum e (|score| + |lse|) and sum e sum_d |q_d k_d| scale."""
+    B, N, Hq, D = q.shape
+    blocks, block, Hkv, _ = k_cache.shape
+    G, scale = Hq // Hkv, D ** -0.5 if scale is None else scale
+    w = w.double().clone()
+    got, size, reach = (torch.zeros_like(w) for _ in range(3))
+    status = torch.zeros(B, dtype=torch.int32)
+    for b in range(B):
+        length, n = int(lengths[b]), N if n_nodes is None else int(n_nodes[b])
+        p = 0 if protected is None else max(0, int(protected[b]))
+        if length < 0:
+            continue
+        row = parent[b] if parent.dim() == 2 else parent
+        seen_by = [path_of(row, i) for i in range(n)] if 0 <= n <= N else None
+        if seen_by is None or any(x is None for x in seen_by):
+            status[b] = TOPOLOGY
+            continue
+        if n == 0:
+            continue
+        sees = torch.zeros(n, length + n, dtype=torch.bool)
+        sees[:, :length] = True
+        for i, nodes in enumerate(seen_by):
+            sees[i, [length + x for x in nodes]] = True
+        j = torch.arange(min(p, length + n), length + n)
+        cols = j // block
+        ids = torch.where(cols < table.shape[1], table[b, cols.clamp(max=table.shape[1] - 1)], -1).long()
+        good = (ids >= 0) & (ids < blocks)
+        if not bool(good.all()):
+            status[b] = PAGE
+        j, ids = j[good], ids[good]
+        k = k_cache[ids, j % block].double().repeat_interleave(G, 1)
+        x = q[b, :n].double()
+        score = torch.einsum("nhd,jhd->nhj", x, k) * scale
+        l = lse[b, :n].double()[:, :, None]
+        y = score - l
+        counts = sees[:, None, j] & l.isfinite() & ~y.isnan()
+        e = torch.where(counts, y.exp(), 0.0)
+        at = (ids, j % block)
+        if fresh:
+            tree = j >= length
+            w[ids[tree], (j % block)[tree]] = 0.0
+        w[at] += e.sum((0, 1))
+        got[at] = e.sum((0, 1))
+        size[at] = torch.where(counts, e * (score.abs() + l.abs()), 0.0).sum((0, 1))
+        reach[at] = torch.where(counts, e * (torch.einsum("nhd,jhd->nhj", x.abs(), k.abs()) * scale), 0.0).sum((0, 1))
+    return dict(weights=w, status=status, got=got, size=size, reach=reach)

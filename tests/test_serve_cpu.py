@@ -13,6 +13,28 @@ Evict = struct("SpecEvict", (I, "B caches budget recent num_blocks block_size ta
                (P, "weights block_table"), (L, "table_stride"), (P, "lengths owned protected_len free_blocks"), (I, "free_size"),
                (P, "free_range lengths_out owned_out free_range_out status"))
 
+Weights = struct("SpecWeights", (I, "B N Hq Hkv D dtype num_blocks block_size table_width fresh"), (F, "scale"), (P, "q"), (S3, "q_stride"),
+                 (P, "k_cache"), (S3, "k_cache_stride"), (P, "lse block_table"), (L, "table_stride"), (P, "lengths n_nodes parent"),
+                 (L, "topo_seq_stride"), (P, "protected_len weights status"))
+
+
+def test_weights_refusals(lib):  # noqa: F811
+    good = dict(B=2, N=19, Hq=8, Hkv=2, D=128, scale=0.1, table_stride=1)
+    call = lambda **kw: lib.spec_cache_weights(C.byref(filled(Weights, **dict(good, **kw))), None)  # noqa: E731
+    assert lib.spec_cache_weights(None, None) == -1
+    for f in ("q", "k_cache", "lse", "block_table", "lengths", "parent", "weights", "status"):
+        assert call(**{f: None}) == -1, f
+    for kw in (dict(B=0), dict(N=0), dict(N=1025), dict(Hkv=0), dict(Hq=7), dict(Hq=1), dict(num_blocks=0), dict(block_size=0),
+               dict(table_width=0), dict(table_width=5, table_stride=4), dict(topo_seq_stride=18), dict(num_blocks=1 << 20, block_size=1 << 12)):
+        assert call(**kw) == -2, kw
+    for dtype in (-1, 0, 3):
+        assert call(dtype=dtype) == -3
+    for kw in (dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=-0.5)):
+        assert call(**kw) == -4, kw
+    for kw in (dict(D=96), dict(D=512), dict(q=0x10008), dict(k_cache=0x10002), dict(q_stride=(1, 8, 8)), dict(k_cache_stride=(8, 8, 12)),
+               dict(B=65535, N=1024, Hq=64, Hkv=64, table_width=1 << 20, table_stride=1 << 20, block_size=1 << 10)):
+        assert call(**kw) == -6, kw
+
 
 def test_logprobs_refusals(lib):  # noqa: F811
     good = dict(V=100, temperature=1.0, parent=None)
@@ -60,6 +82,7 @@ def test_evict_refusals(lib):  # noqa: F811
 @pytest.mark.parametrize("name,args", [
     ("token_logprobs", lambda t, i: (t[0, 0], i)),
     ("path_logprobs", lambda t, i: (t[0], i, i[None], i)),
+    ("cache_weights", lambda t, i: (t[0, 0], t, t, t, i[None], i, i)),
     ("cache_evict", lambda t, i: (t, t[0, 0], i, i[None], i, i, i, 1))])
 def test_the_calls_refuse_to_run_without_a_gpu(lib, name, args):  # noqa: F811
     with pytest.raises(RuntimeError, match="CUDA device"):
