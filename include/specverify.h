@@ -433,6 +433,31 @@ int32_t spec_verify_probs(const SpecChains *a, void *stream);
  * ------------------------------------------------------------------------------------------------ */
 
 /*
+ * spec_tree_attention for requests that share prefixes: a group's prefix is attended to once for all of its members.  Group g has shared_blocks[g] whole
+ * blocks, prefix_table[g][0 ..), and the members members[first[g] .. first[g+1]); group[b] is request b's group (negative: none) and place[b] its
+ * place among that group's members.  A member's committed tokens begin with its prefix: lengths[b] counts it, and the first shared_blocks[g]
+ * columns of its row of block_table are not read.  Every row has the result that spec_tree_attention gives for a row of block_table that begins with
+ * the prefix's blocks, and a lse with it; window and sinks are 0.
+ * A plan that does not fit together (first not rising within [0, n_members], members[first[group[b]] + place[b]] other than b, group[b] >= n_groups,
+ * shared_blocks[g] outside [0, prefix_width]) or a length below the prefix: SPEC_DEV_TOPOLOGY for the requests concerned (a `first` that does not rise:
+ * for all), whose rows are 0.  A bad block of a prefix hides its keys and gives its members SPEC_DEV_PAGE.
+ * `ws`: spec_prefix_attention_workspace_bytes() bytes (a function of the sizes; contents do not matter).
+ */
+typedef struct {
+    SpecAttention attention;          /* window and sinks 0                                           */
+    int32_t n_groups, n_members, prefix_width;      /* n_members at most B                            */
+    const int32_t *group;             /* [B]                                                          */
+    const int32_t *members;           /* [n_members]                                                  */
+    const int32_t *first;             /* [n_groups + 1]                                               */
+    const int32_t *place;             /* [B]                                                          */
+    const int32_t *shared_blocks;     /* [n_groups]                                                   */
+    const int32_t *prefix_table;      /* row g at g * prefix_stride                                   */
+    int64_t prefix_stride;
+} SpecPrefixAttention;
+int32_t spec_prefix_attention_workspace_bytes(const SpecPrefixAttention *a, int64_t *bytes);
+int32_t spec_prefix_attention(const SpecPrefixAttention *a, void *ws, int64_t ws_bytes, void *stream);
+
+/*
  * Log probabilities of given tokens under rows of logits, with the rows' entropy and their most probable tokens.  Row (b, i) is
  *   logits[b,i] where parent is NULL;
  *   the logits of the i-th node of the path to accepted_node[b], the root being the 0th, where parent is given: what a verification's

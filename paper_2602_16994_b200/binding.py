@@ -10,8 +10,8 @@ Device-resident API (inputs already in HBM, nothing is synchronised):
     verify_specinfer / verify_traversal / verify_otlp / tree_probs / sample_bonus / tree_analysis
 Around a verification in a decoding loop with a paged cache (likewise):
     cache_slots / norm_rope_cache / tree_attention / verify_probs / cache_commit
-Bounded caches and answers (likewise):
-    cache_weights / cache_evict / token_logprobs / path_logprobs
+Shared prefixes, bounded caches and answers (likewise):
+    prefix_plan / prefix_attention / cache_weights / cache_evict / token_logprobs / path_logprobs
 Host API (pinned host buffers in, host results out; copies and one stream sync inside):
     HostVerifier
 """
@@ -20,6 +20,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import torch
 
@@ -35,7 +36,7 @@ EXPORTS = ("spec_workspace_bytes", "spec_tree_probs", "spec_verify_specinfer", "
            "spec_tree_analysis", "spec_latency_model", "spec_test_hooks", "spec_row_statistics",
            "spec_verify_otlp", "spec_cache_slots", "spec_norm_rope_cache", "spec_tree_attention_workspace_bytes",
            "spec_tree_attention", "spec_cache_commit", "spec_verify_probs", "spec_token_logprobs",
-           "spec_cache_weights", "spec_cache_evict_workspace_bytes", "spec_cache_evict")
+           "spec_prefix_attention_workspace_bytes", "spec_prefix_attention", "spec_cache_weights", "spec_cache_evict_workspace_bytes", "spec_cache_evict")
 
 
 class SpecIn(C.Structure):
@@ -487,6 +488,44 @@ def verify_probs(target_probs, draft_probs, token, cu_drafts, u_accept, u_bonus,
     in [0, 1); ``max_drafts``: no request has more.
     """
     return _calls().verify_probs(target_probs, draft_probs, token, cu_drafts, u_accept, u_bonus, max_drafts, stream)
+
+
+class PrefixPlan(NamedTuple):
+    """Which requests share which prefix; all int32 on the device."""
+    group: torch.Tensor          # [B] a request's group, negative: none
+    members: torch.Tensor        # the requests in the order of their groups
+    first: torch.Tensor          # [groups + 1] group g has members[first[g]:first[g + 1]]
+    place: torch.Tensor          # [B] a request's place among its group's members
+    blocks: torch.Tensor         # [groups] whole blocks of each group's prefix
+    table: torch.Tensor          # [groups, W] those blocks
+
+
+def prefix_plan(group, blocks, table) -> PrefixPlan:
+    """The plan of ``prefix_attention`` from each request's ``group`` (negative: it shares nothing), and each group's prefix: its first
+    ``blocks[g]`` entries of ``table[g]``.  Made when the requests that share change, kept from step to step and for all layers.
+    """
+    for name, t in (("group", group), ("blocks", blocks), ("table", table)):
+        if t.dtype != torch.int32:
+            raise RuntimeError(f"{name} must be a torch.int32 tensor")
+    if group.dim() != 1 or blocks.dim() != 1 or table.dim() != 2 or table.shape[0] != blocks.numel():
+        raise RuntimeError("group must be [B], blocks [groups] and table [groups,W]")
+    order = torch.sort(group, stable=True)
+    first = torch.searchsorted(order.values, torch.arange(blocks.numel() + 1, dtype=torch.int32, device=group.device)).int()
+    at = torch.arange(group.numel(), dtype=torch.int32, device=group.device)
+    place = torch.empty_like(group).scatter_(0, order.indices, at)
+    if blocks.numel():
+        place = place - first[group.clamp(0, blocks.numel() - 1).long()]
+    return PrefixPlan(group.contiguous(), order.indices.int(), first, place, blocks.contiguous(), table)
+
+
+def prefix_attention(q, k_cache, v_cache, block_table, lengths, parent, plan, n_nodes=None, scale=None, out=None, want_lse=False,
+                     stream=None) -> AttentionOutputs:
+    """``tree_attention`` for requests that share prefixes: what the members of a group share is attended to once for all of them.
+
+    ``plan``: a ``PrefixPlan``.  ``lengths`` counts the prefix, and a member's own blocks begin in column ``plan.blocks[g]`` of its row of
+    ``block_table``; the columns ahead are not read.  No window.
+    """
+    return _calls().prefix_attention(q, k_cache, v_cache, block_table, lengths, parent, n_nodes, plan, scale, out, want_lse, stream)
 
 
 @dataclass

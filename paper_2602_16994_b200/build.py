@@ -7,10 +7,11 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SRC = [os.path.join(HERE, "csrc", f) for f in ("specverify.cu", "step.cu", "serve.cu")]
+SRC = [os.path.join(HERE, "csrc", f) for f in ("specverify.cu", "step.cu", "prefix.cu", "serve.cu")]
 DEPS = {"specverify.cu": ("common.cuh", "host.h", "verify.cuh", "rowops.cuh", "cut.cuh", "stream.cuh", "walk.cuh", "nodes.cuh", "trunc.cuh",
                           "analysis.cuh"),
         "step.cu": ("common.cuh", "host.h", "launch.h", "tree.cuh", "tmem.cuh", "slots.cuh", "rope.cuh", "attend.cuh", "chain.cuh", "commit.cuh"),
+        "prefix.cu": ("common.cuh", "host.h", "launch.h", "tree.cuh", "tmem.cuh", "attend.cuh", "prefix.cuh"),
         "serve.cu": ("common.cuh", "host.h", "launch.h", "tree.cuh", "cut.cuh", "tmem.cuh", "attend.cuh", "logprobs.cuh", "weigh.cuh",
                      "evict.cuh")}
 LIB = os.path.join(HERE, "libspecverify.so")

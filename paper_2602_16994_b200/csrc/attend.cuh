@@ -62,6 +62,16 @@ struct Params {
     float2 *ml;                                // [ctas][2][rows] reference and l; reference -inf: none, and l is 1 where keys were seen
     int *late;                                 // [ctas] a wait ran out
     int4 *joint;                               // [ctas] the unit whose first part this is: request, block, head; parts, slot and rows
+    // shared prefixes (prefix.cuh)
+    int n_groups, n_members, prefix_width;
+    const int *group, *members, *first, *place, *shared, *prefix_table;
+    long long prefix_stride;
+    unsigned nodes_mul;                        // division by N
+    int nodes_shift;
+    float *whole[2];                           // O of units that were not cut, by row: of requests, of prefixes
+    float2 *whole_ml[2];
+    int2 *unit[2];                             // where a unit's parts are: first CTA's slot (-1: in whole), number of them
+    int unit_blocks;                           // blocks of rows of a request
 };
 
 // ---- the schedule -------------------------------------------------------------------------------------------------------------
@@ -76,10 +86,48 @@ struct Tiles {
 };
 struct Request {
     int len, n, rows;                          // (n = 0 for idle requests)
+    int skip;                                  // tokens of its prefix, which other units see to (shared prefixes)
 };
-__device__ __forceinline__ Request request_of(const Params &P, int b)
+// With shared prefixes (SH) the requests' units have those of the groups' prefixes ahead of them: an entry e < n_groups is a prefix, whose rows are those of
+// all of the group's members (no tree, the prefix as its committed tokens), entry n_groups + b request b with what lies behind its prefix.
+template <bool SH> __device__ __forceinline__ int entries(const Params &P) { return SH ? P.n_groups + P.B : P.B; }
+template <bool SH> __device__ __forceinline__ bool is_prefix(const Params &P, int e) { return SH && e < P.n_groups; }
+// a group's members are members[x .. y)
+__device__ __forceinline__ int2 members_of(const Params &P, int g)
+{
+    const int x = min(max(__ldg(P.first + g), 0), P.n_members);
+    return make_int2(x, min(max(__ldg(P.first + g + 1), x), P.n_members));
+}
+__device__ __forceinline__ int prefix_len(const Params &P, int g)
+{
+    return (int)min((long long)min(max(__ldg(P.shared + g), 0), P.prefix_width) * P.block, 0x7FFFFFFFll / P.block * P.block);
+}
+// tokens of a request's prefix
+__device__ __forceinline__ int skip_of(const Params &P, int b)
+{
+    const int g = __ldg(P.group + b);
+    return g < 0 || g >= P.n_groups ? 0 : prefix_len(P, g);
+}
+template <bool SH> __device__ __forceinline__ Request request_of(const Params &P, int b)
 {
     Request r;
+    r.skip = 0;
+    if (SH) {
+        if (b < P.n_groups) {
+            const int2 m = members_of(P, b);
+            r.len = prefix_len(P, b);
+            r.n = 0;
+            r.rows = r.len ? (m.y - m.x) * P.tree.N * P.G : 0;
+            return r;
+        }
+        b -= P.n_groups;
+        r.skip = skip_of(P, b);
+        r.len = __ldg(P.tree.lengths + b);
+        r.n = r.len < r.skip ? 0 : max(0, tree_nodes(P.tree, b));
+        r.len -= r.skip;
+        r.rows = r.n * P.G;
+        return r;
+    }
     r.len = __ldg(P.tree.lengths + b);
     r.n = r.len < 0 ? 0 : max(0, tree_nodes(P.tree, b));
     r.rows = r.n * P.G;
@@ -89,11 +137,12 @@ __device__ __forceinline__ int node_of(const Params &P, int row)
 {
     return (int)((__umulhi(P.group_mul, (unsigned)row) + (unsigned)row) >> P.group_shift);
 }
-__device__ __forceinline__ Tiles tiles_of(const Params &P, const Request &r, int m, int block_rows)
+template <bool SH> __device__ __forceinline__ Tiles tiles_of(const Params &P, const Request &r, int m, int block_rows)
 {
+    if (SH && r.n == 0) return Tiles{0, 0, (int)(((unsigned)r.len + KT - 1) / KT)};                          // a prefix, within its table
     const int last = (m + 1) * block_rows >= r.rows ? r.n - 1 : node_of(P, (m + 1) * block_rows - 1);        // the block's last node
     // (keys behind the table's end have no block: a tile at least, for the rows to come out as those of rows that see nothing)
-    const long long held = min((long long)P.width * P.block, 0x7FFFFFFFll);
+    const long long held = max(min((long long)P.width * P.block, 0x7FFFFFFFll) - r.skip, 1ll);
     Tiles t;
     t.end = (int)((min((unsigned)r.len + (unsigned)last + 1, (unsigned)held) + KT - 1) / KT);
     t.sink = t.from = 0;
@@ -103,11 +152,12 @@ __device__ __forceinline__ Tiles tiles_of(const Params &P, const Request &r, int
     }
     return t;
 }
-__device__ __forceinline__ int tiles_of_request(const Params &P, int b, int block_rows)
+template <bool SH> __device__ __forceinline__ int tiles_of_request(const Params &P, int b, int block_rows)
 {
-    const Request r = request_of(P, b);
+    const Request r = request_of<SH>(P, b);
+    if (is_prefix<SH>(P, b)) return (r.rows + block_rows - 1) / block_rows * (tiles_of<SH>(P, r, 0, block_rows).count() + START) * P.Hkv;
     int s = 0;
-    for (int m = 0; m * block_rows < r.rows; ++m) s += tiles_of(P, r, m, block_rows).count() + START;
+    for (int m = 0; m * block_rows < r.rows; ++m) s += tiles_of<SH>(P, r, m, block_rows).count() + START;
     return s * P.Hkv;
 }
 struct Cuts {                                  // runs of equal length, the first `more` of them longer by one
@@ -121,12 +171,24 @@ struct Place {
     int b, m, h, i;
     __device__ __forceinline__ int tile() const { return max(0, i - START); }
 };
-// All threads of the CTA: the cuts; in found[], the request that the start of run `c` falls into and the length of all ahead of it.
-__device__ __forceinline__ Cuts find_request(const Params &P, int block_rows, int c, int *sums, int *found, int tid, int threads)
+// Whether the groups that this thread looks at lie one behind the other among the members.
+__device__ __forceinline__ bool groups_in_order(const Params &P, int tid, int threads)
 {
-    const int per = (P.B + threads - 1) / threads, b0 = min(P.B, tid * per), b1 = min(P.B, b0 + per);
+    bool good = true;
+    for (int g = tid; g < P.n_groups; g += threads) {
+        const int x = __ldg(P.first + g), y = __ldg(P.first + g + 1);
+        good &= x >= 0 && x <= y && y <= P.n_members;
+    }
+    return good;
+}
+// All threads of the CTA: the cuts; in found[], the request that the start of run `c` falls into and the length of all ahead of it.
+template <bool SH> __device__ __forceinline__ Cuts find_request(const Params &P, int block_rows, int c, int *sums, int *found, int tid, int threads)
+{
+    const int n = entries<SH>(P), per = (n + threads - 1) / threads, b0 = min(n, tid * per), b1 = min(n, b0 + per);
     int mine = 0;
-    for (int b = b0; b < b1; ++b) mine += tiles_of_request(P, b, block_rows);
+    for (int b = b0; b < b1; ++b) mine += tiles_of_request<SH>(P, b, block_rows);
+    // (groups that overlap could add up to more than the launch was checked for: nothing is done then, and the joining kernel says so)
+    if (SH && __syncthreads_or(!groups_in_order(P, tid, threads))) mine = 0;
     const int lane = tid & 31, warp = tid >> 5, warps = threads >> 5;
     int incl = mine;
 #pragma unroll
@@ -145,7 +207,7 @@ __device__ __forceinline__ Cuts find_request(const Params &P, int block_rows, in
     const int target = cuts.start(c);
     if (target >= ahead && target < ahead + mine) {
         for (int b = b0; b < b1; ++b) {
-            const int t = per == 1 ? mine : tiles_of_request(P, b, block_rows);
+            const int t = per == 1 ? mine : tiles_of_request<SH>(P, b, block_rows);
             if (target < ahead + t) { found[0] = b; found[1] = ahead; break; }
             ahead += t;
         }
@@ -171,18 +233,18 @@ struct Run {
 };
 // The next segment of a run; false at its end.  (Once in the code: every role of the kernel takes its segments here, and what runs once
 // per segment costs its instructions' fetching.)
-static __device__ __noinline__ bool next_segment(const Params &P, int block_rows, Run *run, Segment *s)
+template <bool SH> static __device__ __noinline__ bool next_segment(const Params &P, int block_rows, Run *run, Segment *s)
 {
     if (run->left <= 0) return false;
     Place at = run->at;
     Request r;
     for (;;) {
-        if (at.b >= P.B) return false;
-        r = request_of(P, at.b);
+        if (at.b >= entries<SH>(P)) return false;
+        r = request_of<SH>(P, at.b);
         if (at.m * block_rows < r.rows) break;
         ++at.b; at.m = 0;
     }
-    const Tiles t = tiles_of(P, r, at.m, block_rows);
+    const Tiles t = tiles_of<SH>(P, r, at.m, block_rows);
     const int count = t.count(), upto = min(count + START, at.i + run->left), end = max(0, upto - START);
     run->left -= upto - at.i;
     if (end == 0) return false;                // (the run ends before the unit's first tile)
@@ -204,11 +266,11 @@ struct __align__(16) Hand {
     Segment seg[2];
     int more, segments;                        // (segments: how many there were)
     // all lanes of the warp; seg[i] is the next segment
-    __device__ __forceinline__ bool next(const Params &P, int block_rows, int i)
+    template <bool SH> __device__ __forceinline__ bool next(const Params &P, int block_rows, int i)
     {
         __syncwarp();
         if ((threadIdx.x & 31) == 0) {
-            more = next_segment(P, block_rows, &run, &seg[i]);
+            more = next_segment<SH>(P, block_rows, &run, &seg[i]);
             segments += more;
         }
         __syncwarp();
@@ -216,12 +278,17 @@ struct __align__(16) Hand {
     }
 };
 // the place `skip` into request b
-__device__ __forceinline__ Place place_in(const Params &P, int b, int skip, int block_rows)
+template <bool SH> __device__ __forceinline__ Place place_in(const Params &P, int b, int skip, int block_rows)
 {
-    const Request r = request_of(P, b);
+    const Request r = request_of<SH>(P, b);
     Place p = {b, 0, 0, 0};
+    if (is_prefix<SH>(P, b)) {                 // (its blocks of rows are equally long)
+        const int whole = (tiles_of<SH>(P, r, 0, block_rows).count() + START) * P.Hkv;
+        p.m = (int)((unsigned)skip / (unsigned)whole);
+        skip -= p.m * whole;
+    }
     for (; p.m * block_rows < r.rows; ++p.m) {
-        const int length = tiles_of(P, r, p.m, block_rows).count() + START;
+        const int length = tiles_of<SH>(P, r, p.m, block_rows).count() + START;
         if (skip < length * P.Hkv) {
             p.h = (int)((unsigned)skip / (unsigned)length);
             p.i = skip - p.h * length;
@@ -280,19 +347,44 @@ __device__ __forceinline__ int column_of(const Params &P, int key)
 {
     return (int)((__umulhi(P.block_mul, (unsigned)key) + (unsigned)key) >> P.block_shift);
 }
-// the block of a column of a request's row; -1 where there is none in the cache
-__device__ __forceinline__ int block_in(const Params &P, int b, int col)
+// the table's entry of a column, the first being that of the entry's first key; -1 behind the row's end
+template <bool SH> __device__ __forceinline__ int id_in(const Params &P, int b, int skip, int col)
 {
-    const int id = col < P.width ? __ldg(P.table + (long long)b * P.table_stride + col) : -1;
+    if (SH) {
+        if (b < P.n_groups) return col < P.prefix_width ? __ldg(P.prefix_table + (long long)b * P.prefix_stride + col) : -1;
+        b -= P.n_groups;
+        col += skip / P.block;
+    }
+    return col < P.width ? __ldg(P.table + (long long)b * P.table_stride + col) : -1;
+}
+// the block of a column; -1 where there is none in the cache
+template <bool SH> __device__ __forceinline__ int block_in(const Params &P, int b, int skip, int col)
+{
+    const int id = id_in<SH>(P, b, skip, col);
     return id < 0 || id >= P.num_blocks ? -1 : id;
+}
+// A row of a unit (node and head of the group, or member, node and head): whose it is.  b = -1: nobody's (a plan that names no request).
+struct RowOf {
+    int b, node, head;
+};
+template <bool SH> __device__ __forceinline__ RowOf row_of(const Params &P, int e, int h, int r)
+{
+    int node = node_of(P, r);
+    const int head = h * P.G + r - node * P.G;
+    if (!SH) return RowOf{e, node, head};
+    if (e >= P.n_groups) return RowOf{e - P.n_groups, node, head};
+    const int i = (int)((__umulhi(P.nodes_mul, (unsigned)node) + (unsigned)node) >> P.nodes_shift);
+    const int b = __ldg(P.members + min(members_of(P, e).x + i, P.n_members - 1));
+    return RowOf{b < 0 || b >= P.B ? -1 : b, node - i * P.tree.N, head};
 }
 
 // ---- the kernel ---------------------------------------------------------------------------------------------------------------
 // MT = 2: 256 rows, a warpgroup per 128.  MT = 1, WG = 2: 128 rows, the warpgroups take tiles in turn, each with its own O, reference and l,
 // put together at the segment's end: one warpgroup's tile takes some 2400 cycles of arithmetic and 1040 of products one after the other, and the
 // cache delivers one every 2740.  WG = 1: one warpgroup (D = 256: tensor memory has room for one O).
-template <int D_, int MT_, int WG_> struct Shape {
+template <int D_, int MT_, int WG_, bool SH_ = false> struct Shape {
     static constexpr int D = D_, MT = MT_, WG = WG_;
+    static constexpr bool SH = SH_;                                               // prefixes are shared
     static constexpr bool TURNS = MT == 1 && WG == 2;
     static constexpr int PARTS = MT == 2 ? 2 : 1, W = KT / PARTS;                 // a tile's columns in parts: see the products
     static constexpr int PANELS = D / 64;
@@ -323,6 +415,34 @@ struct Bars {
     int found[2], sums[16];
 };
 static_assert(sizeof(Bars) <= 1024, "the area behind the buffers");
+
+// ---- where the parts of units lie (shared prefixes) -----------------------------------------------------------------------------
+// the row of a unit that was not cut, in whole[]
+__device__ __forceinline__ long long whole_row_of(const Params &P, int e, int h, int r)
+{
+    const long long rows = (long long)P.tree.N * P.G;
+    return e < P.n_groups ? ((long long)h * P.n_members + members_of(P, e).x) * rows + r : ((long long)h * P.B + e - P.n_groups) * rows + r;
+}
+// A unit's place in unit[]: of requests their blocks of rows in order; a group's blocks begin where its rows would, and one further for each group ahead, so
+// that no two groups' overlap.
+__device__ __forceinline__ long long unit_of(const Params &P, int e, int m, int h, int block_rows)
+{
+    if (e >= P.n_groups) return ((long long)(e - P.n_groups) * P.unit_blocks + m) * P.Hkv + h;
+    return ((long long)members_of(P, e).x * P.tree.N * P.G / block_rows + e + m) * P.Hkv + h;
+}
+// What the joining kernel is told of a unit, by the CTA that has its first part.
+__device__ __forceinline__ void tell_unit(const Params &P, const Segment &seg, const Cuts &cuts, int c, int block_rows)
+{
+    if (seg.begin != 0) return;
+    int last = c;
+    if (!seg.whole) {                          // (cut: the run's last segment; the unit's end, from what of it lies in this run)
+        const int end = cuts.start(c + 1) + seg.t.count() - seg.end;
+        last = c + 1;
+        while (cuts.start(last + 1) < end) ++last;
+    }
+    P.unit[seg.b < P.n_groups][unit_of(P, seg.b, seg.m, seg.h, block_rows)] =
+        make_int2(seg.whole ? -1 : 2 * c + (seg.head ? 0 : 1), last + 1 - c);
+}
 
 // A bounded wait; once one has run out all others return at once, no copies or products are issued any more, and the kernel comes to its end.
 __device__ __forceinline__ void wait(Bars *B, uint64_t *bar, uint32_t parity)
@@ -506,7 +626,7 @@ template <typename T, int W> __device__ __forceinline__ float tile_weights(uint3
     return x + y;
 }
 // Values that are not finite were taken out of tiles that not all rows see; those that this row sees come back, into columns d .. d + 31.
-template <typename T>
+template <typename T, bool SH>
 __device__ __noinline__ void put_back(const Params &P, const Segment &seg, int node, int depth, const unsigned short *parent, int d, float *o)
 {
     Walk walk = {node, 0};
@@ -518,7 +638,7 @@ __device__ __noinline__ void put_back(const Params &P, const Segment &seg, int n
         for (int j = 0; j < KT; ++j) {
             const uint32_t word = j < 32 ? words[0] : j < 64 ? words[1] : j < 96 ? words[2] : words[3];
             if (!((word >> (j & 31)) & 1u)) continue;
-            const int key = tile * KT + j, col = column_of(P, key), id = block_in(P, seg.b, col);
+            const int key = tile * KT + j, col = column_of(P, key), id = block_in<SH>(P, seg.b, seg.r.skip, col);
             if (id < 0) continue;
             const unsigned short *v = (const unsigned short *)P.v + id * P.v_stride[0] + (key - col * P.block) * P.v_stride[1] + seg.h * P.v_stride[2] + d;
             for (int k = 0; k < 32; ++k) {
@@ -531,7 +651,7 @@ __device__ __noinline__ void put_back(const Params &P, const Segment &seg, int n
 
 // Whether a row sees any key of a segment: asked for rows whose weights came to nothing, which are 0 where they see nothing, and no number where all that
 // they see has a score of -inf (0 / 0).
-static __device__ __noinline__ bool sees_any(const Params &P, const Segment &seg, int node, int depth, const unsigned short *parent)
+template <bool SH> static __device__ __noinline__ bool sees_any(const Params &P, const Segment &seg, int node, int depth, const unsigned short *parent)
 {
     Walk walk = {node, 0};
     for (int step = 0; step < seg.steps(); ++step) {
@@ -540,7 +660,7 @@ static __device__ __noinline__ bool sees_any(const Params &P, const Segment &seg
         seen_words(P, seg.r, tile, depth, parent, walk, words);
         for (int j = 0; j < KT; ++j) {
             const uint32_t word = j < 32 ? words[0] : j < 64 ? words[1] : j < 96 ? words[2] : words[3];
-            if (((word >> (j & 31)) & 1u) && block_in(P, seg.b, column_of(P, tile * KT + j)) >= 0) return true;
+            if (((word >> (j & 31)) & 1u) && block_in<SH>(P, seg.b, seg.r.skip, column_of(P, tile * KT + j)) >= 0) return true;
         }
     }
     return false;
@@ -573,12 +693,12 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
     }
     grid_dependency_wait();
     grid_launch_dependents();                  // (the joining kernel's CTAs may be placed beside this one's; they wait by themselves)
-    const Cuts cuts = find_request(P, S::ROWS, c, B->sums, B->found, tid, S::NT);
+    const Cuts cuts = find_request<S::SH>(P, S::ROWS, c, B->sums, B->found, tid, S::NT);
     if (lane == 0) {
         hand->run.left = cuts.start(c + 1) - cuts.start(c);
         hand->run.first = true;
         hand->segments = 0;
-        if (hand->run.left > 0) hand->run.at = place_in(P, B->found[0], cuts.start(c) - B->found[1], S::ROWS);
+        if (hand->run.left > 0) hand->run.at = place_in<S::SH>(P, B->found[0], cuts.start(c) - B->found[1], S::ROWS);
     }
     tc::fence_before();
     __syncthreads();
@@ -599,18 +719,21 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         // for this warp.
         const auto products = [&](uint32_t n) { wait(B, &B->pv_done[w][n & 1], n >> 1 & 1); };
         Segment &seg = hand->seg[0];
-        for (; hand->next(P, S::ROWS, 0); ++n_seg) {
+        for (; hand->template next<S::SH>(P, S::ROWS, 0); ++n_seg) {
             const int steps = seg.steps();
             if (t * 128 >= seg.rows) {
                 n_run += steps;
                 continue;
             }
-            const int r = seg.m * S::ROWS + row, node = node_of(P, min(r, seg.r.rows - 1));
+            const int r = seg.m * S::ROWS + row;
+            const RowOf of_row = row_of<S::SH>(P, seg.b, seg.h, min(r, seg.r.rows - 1));
+            const bool prefix = is_prefix<S::SH>(P, seg.b);
+            const int node = prefix ? -1 : of_row.node;                        // (no row of a prefix is in a tree)
             const bool live = row < seg.rows, warp_live = t * 128 + quad * 32 < seg.rows;
-            if (tree_of != seg.b && (tree_of < 0 || P.tree.topo_seq_stride || P.tree.n_nodes)) {
+            if (!prefix && tree_of != seg.b && (tree_of < 0 || P.tree.topo_seq_stride || P.tree.n_nodes)) {
                 if (tid == 0) B->bad_tree = 0;
                 bar_sync(1 + w, 128);
-                const int *from = P.tree.parent + (long long)seg.b * P.tree.topo_seq_stride;
+                const int *from = P.tree.parent + (long long)of_row.b * P.tree.topo_seq_stride;
                 for (int i = gt; i < seg.r.n; i += 128) {
                     const int p = __ldg(from + i);
                     parent[i] = p >= 0 && p < i ? (unsigned short)p : (unsigned short)0xFFFF;
@@ -620,7 +743,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                 bar_sync(1 + w, 128);
             }
             int depth = 0;
-            if (P.window)
+            if (!S::SH && P.window)
                 for (unsigned short x = parent[node]; x != 0xFFFF; x = parent[x]) ++depth;
             Walk walk = {node, 0};
             Row of = {0.f, 0.f, false};
@@ -697,12 +820,15 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             }
             if (warp_live) {
                 const bool poison = *(volatile int *)&B->poison != 0;
-                const bool only = live && l == 0.f && sees_any(P, seg, node, depth, parent);         // sees keys, all with a score of -inf
+                const bool only = live && l == 0.f && sees_any<S::SH>(P, seg, node, depth, parent);         // sees keys, all with a score of -inf
                 const float inv = l == 0.f ? only ? CUDART_NAN_F : 0.f : 1.f / l;
                 const long long slot = (long long)blockIdx.x * 2 + (seg.head ? 0 : 1);
-                const int head = seg.h * P.G + r - node * P.G;
-                T *to = (T *)P.out + seg.b * P.out_stride[0] + node * P.out_stride[1] + head * P.out_stride[2];
+                const int head = of_row.head;
+                // (a row that has a prefix elsewhere is put together with it)
+                const bool direct = seg.whole && (!S::SH || (!prefix && seg.r.skip == 0));
+                T *to = (T *)P.out + max(of_row.b, 0) * P.out_stride[0] + of_row.node * P.out_stride[1] + head * P.out_stride[2];
                 float *part = P.part + slot * S::ROWS * D;
+                const long long whole_row = S::SH ? whole_row_of(P, seg.b, seg.h, r) : 0;
                 const int d0 = S::TURNS ? w * (D / 2) : 0, d1 = S::TURNS ? d0 + D / 2 : D;
 #pragma unroll 1
                 for (int d = d0; d < d1; d += 32) {
@@ -721,12 +847,12 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                         float x[32];
 #pragma unroll
                         for (int k = 0; k < 32; ++k) x[k] = __uint_as_float(o[k]);
-                        put_back<T>(P, seg, node, depth, parent, d, x);
+                        put_back<T, S::SH>(P, seg, node, depth, parent, d, x);
 #pragma unroll
                         for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(x[k]);
                     }
                     if (!live) continue;
-                    if (seg.whole) {
+                    if (direct) {
 #pragma unroll
                         for (int k = 0; k < 32; k += 8) {
                             uint4 x;
@@ -736,6 +862,11 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                             x.w = Pair<T>::pack(__uint_as_float(o[k + 6]) * inv, __uint_as_float(o[k + 7]) * inv);
                             *(uint4 *)(to + d + k) = x;
                         }
+                    } else if (S::SH && seg.whole) {
+#pragma unroll
+                        for (int k = 0; k < 32; k += 4)
+                            *(uint4 *)(P.whole[prefix] + ((whole_row >> 5) * (D / 4) + (d + k) / 4) * 128 + (whole_row & 31) * 4) =
+                                make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
                     } else {
 #pragma unroll
                         for (int k = 0; k < 32; k += 4)
@@ -743,9 +874,11 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                     }
                 }
                 if (live && d0 == 0) {
-                    if (seg.whole) {
+                    if (direct) {
                         if (P.lse)
-                            P.lse[((long long)seg.b * P.tree.N + node) * P.Hq + head] = l == 0.f ? -CUDART_INF_F : (ref + log2f(l)) * LN2;
+                            P.lse[((long long)of_row.b * P.tree.N + of_row.node) * P.Hq + head] = l == 0.f ? -CUDART_INF_F : (ref + log2f(l)) * LN2;
+                    } else if (S::SH && seg.whole) {
+                        P.whole_ml[prefix][whole_row] = make_float2(any ? ref : -CUDART_INF_F, only ? 1.f : l);
                     } else {
                         P.ml[slot * S::ROWS + row] = make_float2(any ? ref : -CUDART_INF_F, only ? 1.f : l);
                     }
@@ -818,7 +951,8 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
         // (the slots' order: K0, V0, K1, V1, ...)
         const auto keys_of = [&](int i) { return n + 2 * S::STEP * i; };
         const auto values_of = [&](int i) { return n + 2 * S::STEP * i + S::STEP; };
-        for (; hand->next(P, S::ROWS, 0); ++n_seg) {
+        for (; hand->template next<S::SH>(P, S::ROWS, 0); ++n_seg) {
+            if (S::SH && warp == S::SOFT && lane == 0) tell_unit(P, hand->seg[0], cuts, c, S::ROWS);
             const int steps = hand->seg[0].steps();
             const bool mine = MT == 1 || m * 128 < hand->seg[0].rows;
             wait(B, &B->q_full, n_seg & 1);
@@ -954,7 +1088,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             if (x.seen) {
                 const int col = column_of(P, (int)key);
                 x.in = (int)key - col * P.block;
-                x.id = col < P.width ? __ldg(P.table + (long long)s.b * P.table_stride + col) : -1;
+                x.id = id_in<S::SH>(P, s.b, s.r.skip, col);
             }
             return x;
         };
@@ -1010,7 +1144,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             if (n_seg) room(&B->q_empty, (n_seg - 1) & 1);
             ++n_seg;
             if (stopped(B)) return;
-            if (c_hold_slot >= 0 && c_hold_slot / P.tree.N == s.b) return;       // (a test may ask for a request's queries to stay away)
+            if (c_hold_slot >= 0 && c_hold_slot / P.tree.N == (S::SH ? s.b - P.n_groups : s.b)) return;       // (a test may ask for a request's queries to stay away)
             if (P.q_boxes) {
                 // (nodes beyond N come as zeros)
                 if (lane == 0) {
@@ -1020,6 +1154,28 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                 __syncwarp();
                 if (lane < S::PANELS * MT)
                     tc::box_load(q_at + lane * PANEL, &P.q_map, lane / MT * 64, s.h * P.G, node_of(P, s.m * S::ROWS + lane % MT * 128), s.b, &B->q_full);
+                return;
+            }
+            if (S::SH) {
+                // (rows of several requests: a lane finds a row's place for all)
+#pragma unroll 1
+                for (int x = 0; x < MT; ++x) {
+                    const int first = part * (32 * MT) + x * 32, mine = s.m * S::ROWS + first + lane;
+                    const RowOf at = row_of<S::SH>(P, s.b, s.h, min(mine, s.r.rows - 1));
+                    const bool in = first + lane < s.rows && at.b >= 0;
+                    const unsigned long long a =
+                        in ? (unsigned long long)((const T *)P.q + at.b * P.q_stride[0] + at.node * P.q_stride[1] + at.head * P.q_stride[2])
+                           : (unsigned long long)P.q | 1;                        // (odd: zeros)
+#pragma unroll 4
+                    for (int i = 0; i < CH; ++i) {
+                        const int y = i * 32 + lane, row = first + y / CH, ch = y % CH;
+                        const unsigned long long f = __shfl_sync(0xffffffffu, a, y / CH);
+                        tc::copy16(q_at + ((ch / 8) * MT + row / 128) * PANEL + row % 128 * 128 + (((ch & 7) ^ (row & 7)) << 4),
+                                   (f & ~1ull) + (f & 1 ? 0 : ch * 16), f & 1 ? 0 : 16);
+                    }
+                }
+                tc::arrive_with_copies(&B->q_full);
+                tc::close_copies();
                 return;
             }
             const T *q = (const T *)P.q + s.b * P.q_stride[0] + s.h * P.G * P.q_stride[2];
@@ -1033,7 +1189,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             tc::arrive_with_copies(&B->q_full);
             tc::close_copies();
         };
-        if (hand->next(P, S::ROWS, 0)) {
+        if (hand->template next<S::SH>(P, S::ROWS, 0)) {
             bool more = true;
             int step = 0, in = 0;                                     // in: which of the segments in hand is gone through
             Source ahead = source(hand->seg[0], hand->seg[0].tile(0));
@@ -1042,7 +1198,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
                 const int at = step;
                 const Source here = ahead;
                 const bool last = ++step == now.steps();
-                if (last) { more = hand->next(P, S::ROWS, in ^= 1); step = 0; }
+                if (last) { more = hand->template next<S::SH>(P, S::ROWS, in ^= 1); step = 0; }
                 if (more) ahead = source(hand->seg[in], hand->seg[in].tile(step));
                 const uint32_t bad = __ballot_sync(0xffffffffu, here.seen && (here.id < 0 || here.id >= P.num_blocks));
                 const bool by_map = P.box && here.whole && bad == 0;
@@ -1074,6 +1230,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             // The first of a unit's parts tells what there is to join, unless the tree is bad: zeros for its rows come from the request's CTA of the
             // joining kernel, and nothing else of that kernel may write them.  (The unit is this run's last, so its tree is the one read last.)
             const Segment &seg = hand->seg[0];
+            if (S::SH) return;
             int4 joint = make_int4(0, 0, 0, 0);
             if (hand->segments && seg.begin == 0 && !seg.whole && !B->bad_tree) {
                 // (the unit's end, from what of it lies in this run)
@@ -1114,7 +1271,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(JOIN_NT, 8) 
         page = keys > (long long)P.width * P.block;
         for (int col = tid; col < cols; col += JOIN_NT) {
             const long long a = (long long)col * P.block, e = a + P.block;
-            if (e > since || a < sinks) page |= block_in(P, b, col) < 0;
+            if (e > since || a < sinks) page |= block_in<false>(P, b, 0, col) < 0;
         }
         bad = __syncthreads_or(bad) != 0;
         page = __syncthreads_or(page) != 0;

@@ -9,5 +9,6 @@ __attribute__((visibility("hidden"))) void count_launch();
 // spec_test_hooks for the other sources' kernels (each source has its own copy of the constants), on the current device
 __attribute__((visibility("hidden"))) int set_step_hooks(long long cycles, int hold);
 __attribute__((visibility("hidden"))) int set_serve_hooks(long long cycles, int hold);
+__attribute__((visibility("hidden"))) int set_prefix_hooks(long long cycles, int hold);
 
 }  // namespace specv

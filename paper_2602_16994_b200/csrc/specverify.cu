@@ -772,8 +772,9 @@ int32_t spec_test_hooks(int64_t wait_cycles, int32_t hold_slot)
         cudaGetLastError();
         return SPEC_ERR_CUDA;
     }
-    const int rc = set_step_hooks(wc, hs);
-    return rc ? rc : set_serve_hooks(wc, hs);
+    int rc = set_step_hooks(wc, hs);
+    if (!rc) rc = set_serve_hooks(wc, hs);
+    return rc ? rc : set_prefix_hooks(wc, hs);
 }
 
 int32_t spec_row_statistics(const SpecIn *in, void *ws, int64_t ws_bytes, void *stream)

@@ -648,50 +648,58 @@ PyObject *py_norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// What the calls of attention have alike: q, k_cache, v_cache, block_table, lengths, parent, n_nodes (a[0] .. a[6]), scale, out, want_lse.  The
+// tensors that are made or written: out, status, lse.
+SpecAttention attention_of(PyObject *const *a, PyObject *scale, PyObject *out, PyObject *want_lse, const Place &place, at::Tensor (&t)[3])
+{
+    const at::Tensor &q = cuda_tensor(a[0], "q"), &kc = cuda_tensor(a[1], "k_cache"), &vc = cuda_tensor(a[2], "v_cache");
+    const auto type = q.scalar_type();
+    if (type != at::kBFloat16 && type != at::kHalf) raise("q must be bfloat16 or float16");
+    rows_of(q, "q", 4, type, place);
+    rows_of(kc, "k_cache", 4, type, place);
+    rows_of(vc, "v_cache", 4, type, place);
+    no_gradient(q, "q"); no_gradient(kc, "k_cache"); no_gradient(vc, "v_cache");
+    const int64_t B = q.size(0), Hq = q.size(2), D = q.size(3);
+    if (kc.size(3) != D || vc.sizes() != kc.sizes()) raise("the caches must be [num_blocks, block_size, Hkv, D]");
+    SpecAttention s = {};
+    int64_t N;
+    s.topo_seq_stride = tree_of(a[5], place, B, &N, &s.parent);
+    if (N != q.size(1)) raise("q must be [B,N,Hq,D] with the N of parent");
+    const Table table = table_of(a[3], place, B);
+    s.B = small(B, "B"); s.N = small(N, "N"); s.Hq = small(Hq, "Hq"); s.Hkv = small(kc.size(2), "Hkv"); s.D = small(D, "D");
+    s.dtype = element_type(type);
+    s.num_blocks = small(kc.size(0), "num_blocks"); s.block_size = small(kc.size(1), "block_size"); s.table_width = table.width;
+    s.scale = scale == Py_None ? (float)(1.0 / std::sqrt((double)(D > 0 ? D : 1))) : (float)number(scale);
+    s.block_table = table.ptr; s.table_stride = table.stride;
+    s.lengths = int_ptr(ints(a[4], "lengths", place, B));
+    s.n_nodes = a[6] == Py_None ? nullptr : int_ptr(ints(a[6], "n_nodes", place, B));
+    if (out == Py_None) {
+        t[0] = place.fresh(q.sizes(), type);
+    } else {
+        t[0] = cuda_tensor(out, "out");
+        rows_of(t[0], "out", 4, type, place);
+        if (t[0].sizes() != q.sizes()) raise("out must have the shape of q");
+        no_gradient(t[0], "out");
+        apart(t[0], "out");
+    }
+    t[1] = place.fresh({B}, at::kInt);
+    if (truth(want_lse)) t[2] = place.fresh({B, N, Hq}, at::kFloat);
+    s.q = q.data_ptr(); s.k_cache = kc.data_ptr(); s.v_cache = vc.data_ptr(); s.out = t[0].data_ptr(); s.status = int_ptr(t[1]);
+    s.lse = t[2].defined() ? (float *)t[2].data_ptr() : nullptr;
+    strides_of(q, s.q_stride); strides_of(kc, s.k_cache_stride); strides_of(vc, s.v_cache_stride); strides_of(t[0], s.out_stride);
+    return s;
+}
+
 // tree_attention(q, k_cache, v_cache, block_table, lengths, parent, n_nodes, scale, window, sinks, out, want_lse, stream)
 PyObject *py_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     if (!arity(n, 13)) return nullptr;
     return guarded([&]() -> PyObject * {
         need((void *)step_lib.attention);
-        const at::Tensor &q = cuda_tensor(a[0], "q"), &kc = cuda_tensor(a[1], "k_cache"), &vc = cuda_tensor(a[2], "v_cache");
-        const Place place(q, a[12]);
-        const auto type = q.scalar_type();
-        if (type != at::kBFloat16 && type != at::kHalf) raise("q must be bfloat16 or float16");
-        rows_of(q, "q", 4, type, place);
-        rows_of(kc, "k_cache", 4, type, place);
-        rows_of(vc, "v_cache", 4, type, place);
-        no_gradient(q, "q"); no_gradient(kc, "k_cache"); no_gradient(vc, "v_cache");
-        const int64_t B = q.size(0), Hq = q.size(2), D = q.size(3);
-        if (kc.size(3) != D || vc.sizes() != kc.sizes()) raise("the caches must be [num_blocks, block_size, Hkv, D]");
-        SpecAttention s = {};
-        int64_t N;
-        s.topo_seq_stride = tree_of(a[5], place, B, &N, &s.parent);
-        if (N != q.size(1)) raise("q must be [B,N,Hq,D] with the N of parent");
-        const Table table = table_of(a[3], place, B);
-        s.B = small(B, "B"); s.N = small(N, "N"); s.Hq = small(Hq, "Hq"); s.Hkv = small(kc.size(2), "Hkv"); s.D = small(D, "D");
-        s.dtype = element_type(type);
-        s.num_blocks = small(kc.size(0), "num_blocks"); s.block_size = small(kc.size(1), "block_size"); s.table_width = table.width;
-        s.window = whole(a[8], "window"); s.sinks = whole(a[9], "sinks");
-        s.scale = a[7] == Py_None ? (float)(1.0 / std::sqrt((double)(D > 0 ? D : 1))) : (float)number(a[7]);
-        s.block_table = table.ptr; s.table_stride = table.stride;
-        s.lengths = int_ptr(ints(a[4], "lengths", place, B));
-        s.n_nodes = a[6] == Py_None ? nullptr : int_ptr(ints(a[6], "n_nodes", place, B));
+        const Place place(cuda_tensor(a[0], "q"), a[12]);
         at::Tensor t[3];
-        if (a[10] == Py_None) {
-            t[0] = place.fresh(q.sizes(), type);
-        } else {
-            t[0] = cuda_tensor(a[10], "out");
-            rows_of(t[0], "out", 4, type, place);
-            if (t[0].sizes() != q.sizes()) raise("out must have the shape of q");
-            no_gradient(t[0], "out");
-            apart(t[0], "out");
-        }
-        t[1] = place.fresh({B}, at::kInt);
-        if (truth(a[11])) t[2] = place.fresh({B, N, Hq}, at::kFloat);
-        s.q = q.data_ptr(); s.k_cache = kc.data_ptr(); s.v_cache = vc.data_ptr(); s.out = t[0].data_ptr(); s.status = int_ptr(t[1]);
-        s.lse = t[2].defined() ? (float *)t[2].data_ptr() : nullptr;
-        strides_of(q, s.q_stride); strides_of(kc, s.k_cache_stride); strides_of(vc, s.v_cache_stride); strides_of(t[0], s.out_stride);
+        SpecAttention s = attention_of(a, a[7], a[10], a[11], place, t);
+        s.window = whole(a[8], "window"); s.sinks = whole(a[9], "sinks");
         int64_t bytes = 0;
         check(step_lib.attention_bytes(&s, &bytes), "spec_tree_attention_workspace_bytes");
         // scratch of this call alone (the allocator's blocks lie on 512 bytes): calls on several streams, or captured into several
@@ -802,8 +810,10 @@ PyObject *py_init_step(PyObject *, PyObject *args)
     Py_RETURN_NONE;
 }
 
-// ---- bounded caches, and what a service answers with ----------------------------------------------------------------------------
+// ---- shared prefixes, bounded caches, and what a service answers with ----------------------------------------------------------------------------
 struct ServeLibrary {
+    decltype(&spec_prefix_attention_workspace_bytes) prefix_bytes;
+    decltype(&spec_prefix_attention) prefix;
     decltype(&spec_token_logprobs) logprobs;
     decltype(&spec_cache_weights) weights;
     decltype(&spec_cache_evict_workspace_bytes) evict_bytes;
@@ -968,6 +978,44 @@ PyObject *py_evict(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// prefix_attention(q, k_cache, v_cache, block_table, lengths, parent, n_nodes, plan, scale, out, want_lse, stream); plan: a tuple of group, members,
+// first, place, blocks and table
+PyObject *py_prefix(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (!arity(n, 12)) return nullptr;
+    return guarded([&]() -> PyObject * {
+        need((void *)serve_lib.prefix);
+        const Place place(cuda_tensor(a[0], "q"), a[11]);
+        if (!PyTuple_Check(a[7]) || PyTuple_GET_SIZE(a[7]) != 6) raise("plan must be a PrefixPlan");
+        PyObject *part[6];
+        for (int i = 0; i < 6; ++i) part[i] = PyTuple_GET_ITEM(a[7], i);
+        at::Tensor t[3];
+        SpecPrefixAttention s = {};
+        s.attention = attention_of(a, a[8], a[9], a[10], place, t);
+        const int64_t B = s.attention.B;
+        s.group = int_ptr(ints(part[0], "plan.group", place, B));
+        const at::Tensor &members = ints(part[1], "plan.members", place), &blocks = ints(part[4], "plan.blocks", place);
+        const int64_t groups = blocks.numel();
+        s.members = int_ptr(members);
+        s.first = int_ptr(ints(part[2], "plan.first", place, groups + 1));
+        s.place = int_ptr(ints(part[3], "plan.place", place, B));
+        s.shared_blocks = int_ptr(blocks);
+        const at::Tensor &table = cuda_tensor(part[5], "plan.table");
+        if (table.scalar_type() != at::kInt || table.dim() != 2 || table.size(0) != groups || (table.size(1) > 1 && table.stride(1) != 1))
+            raise("plan.table must be a [groups,W] torch.int32 tensor with contiguous rows");
+        place.uses(table, "plan.table");
+        s.prefix_table = int_ptr(table);
+        s.n_groups = small(groups, "groups"); s.n_members = small(members.numel(), "members"); s.prefix_width = small(table.size(1), "the plan's width");
+        s.prefix_stride = groups > 1 ? table.stride(0) : std::max<int64_t>(table.size(1), 1);
+        int64_t bytes = 0;
+        check(serve_lib.prefix_bytes(&s, &bytes), "spec_prefix_attention_workspace_bytes");
+        const at::Tensor ws = empty({bytes}, at::kByte, place.device());         // (of this call alone)
+        check(unlocked([&] { return serve_lib.prefix(&s, ws.data_ptr(), bytes, place.stream()); }), "spec_prefix_attention");
+        if (a[9] != Py_None) written(t[0]);
+        return result(attention_outputs_class, t, 3);
+    });
+}
+
 // init_serve(path of libspecverify.so, LogprobOutputs, EvictOutputs): the entry points above
 PyObject *py_init_serve(PyObject *, PyObject *args)
 {
@@ -977,6 +1025,8 @@ PyObject *py_init_serve(PyObject *, PyObject *args)
     void *h = dlopen(path, RTLD_NOW | RTLD_LOCAL);
     if (!h) return PyErr_Format(PyExc_RuntimeError, "%s", dlerror());
     const auto find = [&](auto &f, const char *name) { f = reinterpret_cast<std::remove_reference_t<decltype(f)>>(dlsym(h, name)); };
+    find(serve_lib.prefix_bytes, "spec_prefix_attention_workspace_bytes");
+    find(serve_lib.prefix, "spec_prefix_attention");
     find(serve_lib.logprobs, "spec_token_logprobs");
     find(serve_lib.weights, "spec_cache_weights");
     find(serve_lib.evict_bytes, "spec_cache_evict_workspace_bytes");
@@ -1001,6 +1051,7 @@ PyMethodDef methods[] = {
     {"verify_probs", (PyCFunction)(void *)py_chains, METH_FASTCALL, nullptr},
     {"init_serve", py_init_serve, METH_VARARGS, nullptr},
     {"logprobs", (PyCFunction)(void *)py_logprobs, METH_FASTCALL, nullptr},
+    {"prefix_attention", (PyCFunction)(void *)py_prefix, METH_FASTCALL, nullptr},
     {"cache_weights", (PyCFunction)(void *)py_weights, METH_FASTCALL, nullptr},
     {"cache_evict", (PyCFunction)(void *)py_evict, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2602_16994_b200 import binding
-from .test_step_cpu import F, I, L, P, S3, filled, lib, struct  # noqa: F401
+from .test_step_cpu import Attention, F, I, L, P, S3, filled, good_attention, lib, struct  # noqa: F401
 
 Logprobs = struct("SpecLogprobs", (I, "B N V K top dtype"), (P, "logits"), (L, "seq_stride node_stride"), (P, "parent"), (L, "topo_seq_stride"),
                   (P, "accepted_node token"), (F, "temperature"), (P, "logprob entropy top_tokens top_logprobs status"))
@@ -16,6 +16,57 @@ Evict = struct("SpecEvict", (I, "B caches budget recent num_blocks block_size ta
 Weights = struct("SpecWeights", (I, "B N Hq Hkv D dtype num_blocks block_size table_width fresh"), (F, "scale"), (P, "q"), (S3, "q_stride"),
                  (P, "k_cache"), (S3, "k_cache_stride"), (P, "lse block_table"), (L, "table_stride"), (P, "lengths n_nodes parent"),
                  (L, "topo_seq_stride"), (P, "protected_len weights status"))
+
+class Prefix(C.Structure):
+    _fields_ = [("attention", Attention)] + [(f, I) for f in ("n_groups", "n_members", "prefix_width")] + [
+        (f, P) for f in ("group", "members", "first", "place", "shared_blocks", "prefix_table")] + [("prefix_stride", L)]
+
+
+def prefix(**kw):
+    own = {k: kw.pop(k) for k in list(kw) if k in dict(Prefix._fields_)}
+    s = Prefix()
+    s.attention = good_attention(**dict(dict(window=0, sinks=0), **kw))
+    for n, (f, t) in enumerate(Prefix._fields_[1:]):
+        setattr(s, f, own.get(f, 0x900000 + 0x1000 * n if t is P else 1))
+    return s
+
+
+def test_prefix_refusals(lib):  # noqa: F811
+    n = L()
+    size = lambda **kw: lib.spec_prefix_attention_workspace_bytes(C.byref(prefix(**kw)), C.byref(n))  # noqa: E731
+    assert size() == 0 and n.value >= 256
+    assert lib.spec_prefix_attention_workspace_bytes(None, C.byref(n)) == -1
+    assert lib.spec_prefix_attention_workspace_bytes(C.byref(prefix()), None) == -1
+    for f in ("q", "k_cache", "v_cache", "block_table", "lengths", "parent", "out", "status", "group", "members", "first", "place", "shared_blocks",
+              "prefix_table"):
+        assert size(**{f: None}) == -1, f
+    assert size(n_groups=0, members=None, first=None, place=None, shared_blocks=None, prefix_table=None, n_members=0) == 0
+    for kw in (dict(B=0), dict(N=0), dict(N=1025), dict(Hkv=0), dict(Hq=7), dict(num_blocks=0), dict(block_size=0), dict(table_width=0),
+               dict(topo_seq_stride=18), dict(n_groups=-1), dict(n_groups=65536), dict(n_members=-1), dict(n_members=3), dict(n_members=0),
+               dict(prefix_width=0), dict(prefix_width=2)):
+        assert size(**kw) == -2, kw
+    for dtype in (-1, 0, 3):
+        assert size(dtype=dtype) == -3
+    for kw in (dict(scale=float("nan")), dict(scale=-0.5), dict(window=1), dict(sinks=1)):
+        assert size(**kw) == -4, kw
+    for kw in (dict(D=96), dict(q=0x10008), dict(out=0x10004), dict(k_cache_stride=(8, 8, 12)),
+               dict(B=4096, N=1024, Hq=512, n_members=4096), dict(prefix_width=1 << 30, prefix_stride=1 << 30, n_groups=60000, n_members=2, block_size=2)):
+        assert size(**kw) == -6, kw
+    call = lambda ws, b: lib.spec_prefix_attention(C.byref(prefix()), P(ws), L(b), None)  # noqa: E731
+    size()
+    assert call(None, 1 << 30) == -5 and call(0x10010, 1 << 30) == -5 and call(0x10000, n.value - 1) == -5
+
+
+def test_prefix_plan():
+    """Members in the order of groups, places among them, requests of no group in none."""
+    group = torch.tensor([2, 0, -1, 2, 0, 5, 2], dtype=torch.int32)
+    p = binding.prefix_plan(group, torch.tensor([3, 1, 2], dtype=torch.int32), torch.zeros(3, 4, dtype=torch.int32))
+    assert p.members.tolist() == [2, 1, 4, 0, 3, 6, 5] and p.first.tolist() == [1, 3, 3, 6]
+    for b, g in enumerate(group.tolist()):
+        if 0 <= g < 3:
+            assert p.members[p.first[g] + p.place[b]] == b
+    none = binding.prefix_plan(group, torch.zeros(0, dtype=torch.int32), torch.zeros(0, 1, dtype=torch.int32))
+    assert none.first.numel() == 1 and none.place.numel() == 7
 
 
 def test_weights_refusals(lib):  # noqa: F811
@@ -80,6 +131,7 @@ def test_evict_refusals(lib):  # noqa: F811
 
 
 @pytest.mark.parametrize("name,args", [
+    ("prefix_attention", lambda t, i: (t, t, t, i[None], i, i, binding.PrefixPlan(i, i, i, i, i, i[None]))),
     ("token_logprobs", lambda t, i: (t[0, 0], i)),
     ("path_logprobs", lambda t, i: (t[0], i, i[None], i)),
     ("cache_weights", lambda t, i: (t[0, 0], t, t, t, i[None], i, i)),
