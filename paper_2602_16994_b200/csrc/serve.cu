@@ -91,6 +91,11 @@ int32_t spec_cache_weights(const SpecWeights *a, void *stream)
         p.box = 0;
     const auto go = [&](auto shape, auto kernel) -> int {
         using S = decltype(shape);
+        if (S::QB % p.G == 0) {
+            p.q_nodes = std::min(a->N, S::QB / p.G);
+            const int64_t q_sizes[4] = {a->D, a->Hq, a->N, a->B};
+            if (!tensor_map(&p.q_map, a->q, half, q_sizes, {a->q_stride[2], a->q_stride[1], a->q_stride[0]}, {p.G, p.q_nodes, 1})) p.q_nodes = 0;
+        }
         const int smem = S::total + 1024, rc = prepare(kernel, smem, false);
         return rc ? rc : launch(kernel, dim3(p.ctas), weigh::NT, smem, 0, (cudaStream_t)stream, p);
     };

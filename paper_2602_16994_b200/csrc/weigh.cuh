@@ -9,8 +9,8 @@
 //
 // Layout.  Units are tiles of 128 entries of a request, all key heads; the tiles of all requests, in order, are cut into one run per CTA (one CTA per
 // SM).  Two tiles that lie wholly among the committed tokens go together: a block of queries that is on chip serves both.
-// Four warps copy (keys by tensor map where all 32 of a warp's keys are there and blocks are multiples of 8 slots, else 16 bytes at a time), one issues
-// the products, eight take the exponentials: half of the columns each warpgroup.
+// Four warps copy keys (by tensor map where all 32 of a warp's keys are there and blocks are multiples of 8 slots, else 16 bytes at a time), four
+// queries (by tensor map where a block of them is whole nodes), one issues the products, eight take the exponentials: half of the columns each warpgroup.
 //
 // What is not a number adds nothing: the maximum that bounds exponents from below takes NaN for its bound.  So it does not matter what
 // rows without a finite lse, columns beyond the rows, or keys that are not there hold.
@@ -25,6 +25,8 @@ constexpr float LOG2E = 1.4426950408889634f;
 
 struct Params {
     CUtensorMap k_map;                         // the cache as [block][slot][head][entry], boxes of `box` slots by 64 entries
+    CUtensorMap q_map;                         // the queries as [request][node][head][entry], boxes of the rows of `q_nodes` nodes by 64 entries
+    int q_nodes;                               // 0: where a block of queries is no whole number of nodes
     int box;                                   // a power of two up to 32 that divides the block; 0: blocks of no multiple of 8 slots
     TreeArgs tree;
     int B, Hq, Hkv, G, num_blocks, block, width, fresh;
@@ -95,11 +97,12 @@ template <int D_> struct Shape {
     static constexpr int total = off_bar + 512;
     static_assert(total + 1024 <= 227 * 1024, "shared memory");
 };
-constexpr int SUM_WARPS = 8, PRODUCTS = SUM_WARPS, NT = (SUM_WARPS + 1 + 4) * 32;
+constexpr int SUM_WARPS = 8, PRODUCTS = SUM_WARPS, NT = (SUM_WARPS + 1 + 8) * 32;
 struct Bars {
     uint64_t k_full[6], k_empty[6], q_full[4], q_empty[4], s_full[4], s_empty[4];
     uint32_t tmem;
-    int dead, last, found[2], sums[16];        // (last: the last request that this CTA had tiles of)
+    int dead, last, found[2], sums[20];        // (last: the last request that this CTA had tiles of)
+    Request request;                           // the one that the run begins in
 };
 static_assert(sizeof(Bars) <= 512, "the area behind the buffers");
 
@@ -121,7 +124,8 @@ __device__ __forceinline__ void find_run(const Params &P, int c, Bars *S, Run *r
     const int lane = tid & 31, warp = tid >> 5;
     const int per = (P.B + NT - 1) / NT, b0 = min(P.B, tid * per), b1 = min(P.B, b0 + per);
     int mine = 0;
-    for (int b = b0; b < b1; ++b) mine += request_of(P, b).tiles();
+    Request only = {};                         // (at most one request to a thread: it is looked up once)
+    for (int b = b0; b < b1; ++b) { only = request_of(P, b); mine += only.tiles(); }
     int incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -139,8 +143,9 @@ __device__ __forceinline__ void find_run(const Params &P, int c, Bars *S, Run *r
     const int each = (int)((unsigned)all / (unsigned)P.ctas), more = all - each * P.ctas, start = each * c + min(c, more);
     if (start >= ahead && start < ahead + mine) {
         for (int b = b0; b < b1; ++b) {
-            const int t = request_of(P, b).tiles();
-            if (start < ahead + t) { S->found[0] = b; S->found[1] = start - ahead; break; }
+            if (per > 1) only = request_of(P, b);
+            const int t = only.tiles();
+            if (start < ahead + t) { S->found[0] = b; S->found[1] = start - ahead; S->request = only; break; }
             ahead += t;
         }
     }
@@ -148,8 +153,8 @@ __device__ __forceinline__ void find_run(const Params &P, int c, Bars *S, Run *r
     run->left = each + (c < more);
     run->b = S->found[0];
     run->t = S->found[1];
+    run->r = S->request;
     if (run->b >= P.B) run->left = 0;
-    else run->r = request_of(P, run->b);
 }
 
 template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_weigh_kernel(const __grid_constant__ Params P)
@@ -159,7 +164,10 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
     Bars *B = (Bars *)(base + S::off_bar);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (warp == PRODUCTS) tc::tmem_alloc(&B->tmem, 512);
-    if (tid == NT - 1 && P.box) tc::prefetch_map(&P.k_map);
+    if (tid == NT - 1) {
+        if (P.box) tc::prefetch_map(&P.k_map);
+        if (P.q_nodes) tc::prefetch_map(&P.q_map);
+    }
     if (tid == 0) {
         for (int i = 0; i < S::SK; ++i) { mbar_init(&B->k_full[i], 128); mbar_init(&B->k_empty[i], 1); }
         for (int i = 0; i < S::SQ; ++i) { mbar_init(&B->q_full[i], 256); mbar_init(&B->q_empty[i], 1 + SUM_WARPS); }
@@ -182,8 +190,9 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
         unsigned short *parent = (unsigned short *)(base + S::off_parent);
         uint4 *mask = (uint4 *)(base + S::off_mask);
         float *part = (float *)(base + S::off_part);
-        // requests' status, from the inputs alone (CTA b mod ctas writes request b's); one whose CTA a wait ran out in is marked at the end
-        for (int b = blockIdx.x; b < P.B; b += P.ctas) {
+        // requests' status, from the inputs alone, by the last CTAs first: where there are few tiles, these have none; a request whose CTA a
+        // wait ran out in is marked at the end
+        for (int b = P.ctas - 1 - blockIdx.x; b < P.B; b += P.ctas) {
             const int len = __ldg(P.tree.lengths + b), nn = tree_nodes(P.tree, b), n = len < 0 ? 0 : max(nn, 0);
             const int *row = P.tree.parent + (long long)b * P.tree.topo_seq_stride;
             bool bad = false, page = false;
@@ -390,17 +399,14 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
                     }
                 }
         }
-    } else {
-        // ---------------------------------------------------------------- copies: a warp for 32 keys of every tile and 32 rows of every block of queries
+    } else if (warp < PRODUCTS + 5) {
+        // ---------------------------------------------------------------- keys: a warp for 32 of every tile
         const int which = warp - PRODUCTS - 1;
         constexpr int CH = D / 8;                                     // 16-byte chunks of a row
-        const uint32_t k_at = smem_u32(base), q_at = smem_u32(base + S::off_q);
-        float *refs = (float *)(base + S::off_ref);
-        unsigned short *nodes = (unsigned short *)(base + S::off_node);
-        uint32_t n_k = 0, n_q = 0;
+        const uint32_t k_at = smem_u32(base);
+        uint32_t n_k = 0;
         while (run.next(P)) {
             const Request r = run.r;
-            const int rows = r.n * P.G, blocks = (rows + S::QB - 1) / S::QB;
             int id[2], in[2];
             bool whole[2];
 #pragma unroll
@@ -415,16 +421,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
                 }
                 whole[ti] = P.box && __all_sync(0xffffffffu, id[ti] >= 0);
             }
-            // a row's reference, asked for a block ahead of its use
-            const auto reference = [&](int h, int qb) {
-                const int row = qb * S::QB + which * 32 + lane;
-                if (h >= P.Hkv || which * 32 >= S::QB || row >= rows) return -CUDART_INF_F;
-                const int node = node_of(P, row);
-                const float x = __ldg(P.lse + ((long long)run.b * P.tree.N + node) * P.Hq + h * P.G + row - node * P.G);
-                return fabsf(x) < CUDART_INF_F ? -x * LOG2E : -CUDART_INF_F;
-            };
-            float ahead = reference(0, 0);
-            for (int h = 0; h < P.Hkv; ++h) {
+            for (int h = 0; h < P.Hkv; ++h)
                 for (int ti = 0; ti < run.count; ++ti, ++n_k) {
                     const uint32_t slot = n_k % S::SK;
                     if (n_k >= S::SK) wait(B, &B->k_empty[slot], (n_k / S::SK - 1) & 1);
@@ -432,15 +429,22 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
                     if (stopped(B)) continue;
                     const uint32_t to = k_at + slot * S::K_SLOT;
                     if (whole[ti]) {
-                        if (lane == 0) {
+                        // (by one thread, in a loop that the whole warp goes through: boxes from several threads at once go out one by one, far apart)
+                        if (tc::elected()) {
                             tc::expect_bytes(&B->k_full[slot], 32 * D * 2);
                             tc::arrive_many(&B->k_full[slot], 32);
                         }
                         __syncwarp();
-                        const int boxes = 32 / P.box, g = lane % boxes, p0 = lane / boxes;
-                        const int block = __shfl_sync(0xffffffffu, id[ti], g * P.box), at = __shfl_sync(0xffffffffu, in[ti], g * P.box);
-                        for (int p = p0; p < S::PANELS; p += P.box)
-                            tc::box_load(to + p * PANEL + (which * 32 + g * P.box) * 128, &P.k_map, p * 64, h, at, block, &B->k_full[slot]);
+#pragma unroll 1
+                        for (int g = 0; g < 32; g += P.box) {
+                            const int block = __shfl_sync(0xffffffffu, id[ti], g), at = __shfl_sync(0xffffffffu, in[ti], g);
+                            if (tc::elected()) {
+#pragma unroll
+                                for (int p = 0; p < S::PANELS; ++p)
+                                    tc::box_load(to + p * PANEL + (which * 32 + g) * 128, &P.k_map, p * 64, h, at, block, &B->k_full[slot]);
+                            }
+                            __syncwarp();
+                        }
                     } else {
                         const unsigned long long from = id[ti] >= 0 ? (unsigned long long)((const T *)P.k + id[ti] * P.k_stride[0] + in[ti] * P.k_stride[1] +
                                                                                            h * P.k_stride[2])
@@ -454,6 +458,30 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
                         tc::arrive_with_copies(&B->k_full[slot]);
                     }
                 }
+        }
+        tc::close_copies();
+        tc::wait_copies<0>();
+    } else {
+        // ---------------------------------------------------------------- queries: a warp for 32 rows of every block of them
+        const int which = warp - PRODUCTS - 5;
+        constexpr int CH = D / 8;
+        const uint32_t q_at = smem_u32(base + S::off_q);
+        float *refs = (float *)(base + S::off_ref);
+        unsigned short *nodes = (unsigned short *)(base + S::off_node);
+        uint32_t n_q = 0;
+        while (run.next(P)) {
+            const Request r = run.r;
+            const int rows = r.n * P.G, blocks = (rows + S::QB - 1) / S::QB;
+            // a row's reference, asked for a block ahead of its use
+            const auto reference = [&](int h, int qb) {
+                const int row = qb * S::QB + which * 32 + lane;
+                if (h >= P.Hkv || which * 32 >= S::QB || row >= rows) return -CUDART_INF_F;
+                const int node = node_of(P, row);
+                const float x = __ldg(P.lse + ((long long)run.b * P.tree.N + node) * P.Hq + h * P.G + row - node * P.G);
+                return fabsf(x) < CUDART_INF_F ? -x * LOG2E : -CUDART_INF_F;
+            };
+            float ahead = reference(0, 0);
+            for (int h = 0; h < P.Hkv; ++h)
                 for (int qb = 0; qb < blocks; ++qb, ++n_q) {
                     const uint32_t slot = n_q % S::SQ;
                     const float ref = ahead;
@@ -463,7 +491,17 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
                     if (stopped(B)) continue;
                     if (c_hold_slot >= 0 && c_hold_slot / P.tree.N == run.b) continue;       // (a test may ask for a request's queries to stay away)
                     const int columns = min(S::QB, rows - qb * S::QB);
-                    if (which * 32 < (columns + 15) / 16 * 16) {
+                    if (P.q_nodes) {
+                        // (rows behind the tree's come as zeros, those behind the box as they are: columns that nobody counts)
+                        if (which == 0 && tc::elected()) {
+                            tc::expect_bytes(&B->q_full[slot], P.q_nodes * P.G * D * 2);
+#pragma unroll
+                            for (int p = 0; p < S::PANELS; ++p)
+                                tc::box_load(q_at + slot * S::Q_SLOT + p * S::QB * 128, &P.q_map, p * 64, h * P.G, node_of(P, qb * S::QB), run.b,
+                                             &B->q_full[slot]);
+                        }
+                        __syncwarp();
+                    } else if (which * 32 < (columns + 15) / 16 * 16) {
                         const T *q = (const T *)P.q + run.b * P.q_stride[0] + (long long)h * P.G * P.q_stride[2];
                         const uint32_t to = q_at + slot * S::Q_SLOT;
                         const int mine = min(qb * S::QB + which * 32 + lane, rows - 1), node = node_of(P, mine);
@@ -480,7 +518,6 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
                     tc::arrive_with_copies(&B->q_full[slot]);
                     mbar_arrive(&B->q_full[slot]);
                 }
-            }
         }
         tc::close_copies();
         tc::wait_copies<0>();
