@@ -1100,18 +1100,27 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
             if (stopped(B)) { n += S::STEP; return; }
             bool hold = false;
             if (by_map) {
-                if (lane == 0) {
+                // (by one thread, in a loop that the whole warp goes through: from several threads at once they went out one by one all the same, but 290
+                // cycles apart)
+                if (tc::elected()) {
                     for (int p = 0; p < S::STEP; ++p) {
                         uint64_t *bar = &B->full[(n + p) % S::SLOTS];
                         tc::expect_bytes(bar, 32 * 128 * S::WIDE);
                         tc::arrive_many(bar, S::FILLED / 4);
                     }
                 }
-                const int boxes = 32 / P.box, g = lane % boxes, p = lane / boxes;
-                const int id = __shfl_sync(0xffffffffu, x.id, g * P.box), in = __shfl_sync(0xffffffffu, x.in, g * P.box);
-                for (int k = p; k < S::PANELS; k += P.box)
-                    tc::box_load(slots + place(n, part * 32 + g * P.box, k * 8), values ? &P.v_map : &P.k_map, k * 64, x.h, in, id,
-                                 &B->full[(n + k / S::WIDE) % S::SLOTS]);
+                __syncwarp();
+                const CUtensorMap *map = values ? &P.v_map : &P.k_map;
+#pragma unroll 1
+                for (int g = 0; g < 32; g += P.box) {
+                    const int id = __shfl_sync(0xffffffffu, x.id, g), in = __shfl_sync(0xffffffffu, x.in, g);
+                    if (tc::elected()) {
+#pragma unroll
+                        for (int k = 0; k < S::PANELS; ++k)
+                            tc::box_load(slots + place(n, part * 32 + g, k * 8), map, k * 64, x.h, in, id, &B->full[(n + k / S::WIDE) % S::SLOTS]);
+                    }
+                    __syncwarp();
+                }
             } else {
                 const long long *st = values ? P.v_stride : P.k_stride;
                 const T *from = (const T *)(values ? P.v : P.k);
