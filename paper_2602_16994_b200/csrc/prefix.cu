@@ -127,7 +127,7 @@ int32_t spec_prefix_attention(const SpecPrefixAttention *given, void *ws, int64_
     p.late = (int *)(base + L.late);
     const int64_t rows = (int64_t)a->N * p.G;
     p.unit_blocks = (int)((rows + (two ? 255 : 127)) / (two ? 256 : 128));
-    p.groups = (int)((rows * a->Hkv + attend::MERGE_ROWS - 1) / attend::MERGE_ROWS);
+    p.groups = (int)((rows + attend::MERGE_ROWS - 1) / attend::MERGE_ROWS) * a->Hkv;      // CTAs of a request in the joining kernel
     const bool half = a->dtype == SPEC_F16;
     p.box = a->block_size % 8 ? 0 : a->block_size % 16 ? 8 : a->block_size % 32 ? 16 : 32;
     const int64_t sizes[4] = {a->D, a->Hkv, a->block_size, a->num_blocks};

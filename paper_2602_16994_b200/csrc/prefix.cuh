@@ -10,35 +10,41 @@
 namespace specv {
 namespace attend {
 
-constexpr int MERGE_NT = 256, MERGE_ROWS = 16;
+constexpr int MERGE_NT = 128, MERGE_ROWS = 32;
 
-// A CTA per request and MERGE_ROWS of its rows, in the order of key heads, then nodes, then heads of the group; a thread has four entries of a row.
-template <typename T, typename S> __global__ void __launch_bounds__(MERGE_NT, 4) spec_prefix_join_kernel(const __grid_constant__ Params P)
+// A CTA per request, key head and MERGE_ROWS rows of that head (in the order of nodes, then heads of the group); a thread has four entries of a row.  Its
+// rows belong to two units of the request's own and two of the prefix at most.
+template <typename T, typename S> __global__ void __launch_bounds__(MERGE_NT, 8) spec_prefix_join_kernel(const __grid_constant__ Params P)
 {
     constexpr int D = S::D;
-    const int tid = threadIdx.x, each = P.groups, b = blockIdx.x / (unsigned)each, row0 = (blockIdx.x - b * each) * MERGE_ROWS;
+    static_assert(MERGE_ROWS <= S::ROWS, "two units at most");
+    __shared__ int2 s_unit[2][2];
+    const int tid = threadIdx.x, rows = P.tree.N * P.G;
+    const int b = (int)(blockIdx.x / (unsigned)P.groups), in = (int)blockIdx.x - b * P.groups, chunks = P.groups / P.Hkv;
+    const int h = (int)((unsigned)in / (unsigned)chunks), row0 = (in - h * chunks) * MERGE_ROWS;
     grid_launch_dependents();                  // (the next kernel waits for this one by itself, and this one for the attention)
     // ---- what the inputs alone tell, while the attention still runs
-    const int len = __ldg(P.tree.lengths + b), nn = tree_nodes(P.tree, b), n = len < 0 ? 0 : max(nn, 0);
+    const int len = __ldg(P.tree.lengths + b), g_or_none = __ldg(P.group + b), place = __ldg(P.place + b), nn = tree_nodes(P.tree, b);
+    const int n = len < 0 ? 0 : max(nn, 0);
     const int *parent = P.tree.parent + (long long)b * P.tree.topo_seq_stride;
-    bool bad = nn < 0, page = false;
+    bool bad = nn < 0 || g_or_none >= P.n_groups || !groups_in_order(P, tid, MERGE_NT);
     for (int i = tid; i < n; i += MERGE_NT) {
         const int p = __ldg(parent + i);
         bad |= i == 0 ? p != -1 : p < 0 || p >= i;
     }
-    const int g_or_none = __ldg(P.group + b), g = g_or_none < 0 || g_or_none >= P.n_groups ? -1 : g_or_none;
-    const int skip = g < 0 ? 0 : prefix_len(P, g);
+    const int g = g_or_none < 0 || g_or_none >= P.n_groups ? -1 : g_or_none;
+    int skip = 0;
     int2 m = make_int2(0, 0);
-    int place = 0;
-    bad |= g_or_none >= P.n_groups || !groups_in_order(P, tid, MERGE_NT);
     if (g >= 0) {
         const int blocks = __ldg(P.shared + g);
         m = members_of(P, g);
-        place = __ldg(P.place + b);
-        bad |= blocks < 0 || blocks > P.prefix_width || len < skip || place < 0 || place >= m.y - m.x || __ldg(P.members + m.x + place) != b;
+        skip = prefix_len(P, g);
+        bad |= blocks < 0 || blocks > P.prefix_width || len < skip || place < 0 || place >= m.y - m.x;
+        if (!bad) bad = __ldg(P.members + m.x + place) != b;
     }
     bad = __syncthreads_or(len >= 0 && bad) != 0;
-    if (row0 == 0) {
+    bool page = false;
+    if (in == 0) {
         const long long keys = n ? (long long)len + n : 0;
         const int cols = (int)min((keys + P.block - 1) / P.block, (long long)P.width);
         page = keys > (long long)P.width * P.block;
@@ -47,65 +53,66 @@ template <typename T, typename S> __global__ void __launch_bounds__(MERGE_NT, 4)
             for (int col = tid; col < skip / P.block; col += MERGE_NT) page |= block_in<true>(P, g, 0, col) < 0;
         page = __syncthreads_or(page) != 0;
     }
+    const int upto = min(row0 + MERGE_ROWS, n * P.G), q0 = place * rows;          // rows of nodes that there are; the prefix's row of the request's row 0
     grid_dependency_wait();
-    if (row0 == 0) {
+    if (in == 0) {
         bool late = false;
         for (int i = tid; i < P.ctas; i += MERGE_NT) late |= *(volatile int *)(P.late + i) != 0;
         late = __syncthreads_or(late) != 0;
         if (tid == 0)
             P.status[b] = len < 0 ? SPEC_DEV_OK : bad ? SPEC_DEV_TOPOLOGY : late ? SPEC_DEV_TIMEOUT : page ? SPEC_DEV_PAGE : SPEC_DEV_OK;
     }
-    // ---- rows
-    const int rows = P.tree.N * P.G;
-    for (int i = tid; i < MERGE_ROWS * (D / 4); i += MERGE_NT) {
-        const int at = row0 + i % MERGE_ROWS, ch = i / MERGE_ROWS;
-        const int h = at / rows, r = at - h * rows, node = node_of(P, r), head = h * P.G + r - node * P.G;
-        if (h >= P.Hkv || node >= n) continue;
-        T *to = (T *)P.out + b * P.out_stride[0] + node * P.out_stride[1] + head * P.out_stride[2] + ch * 4;
-        float *lse = P.lse && ch == 0 ? P.lse + ((long long)b * P.tree.N + node) * P.Hq + head : nullptr;
-        if (bad) {
-            *(uint2 *)to = make_uint2(0, 0);
-            if (lse) *lse = -CUDART_INF_F;
-            continue;
+    if (row0 >= upto) return;
+    if (bad) {
+        for (int i = tid; i < (upto - row0) * (D / 4); i += MERGE_NT) {
+            const int r = row0 + i / (D / 4), node = node_of(P, r), head = h * P.G + r - node * P.G;
+            *(uint2 *)((T *)P.out + b * P.out_stride[0] + node * P.out_stride[1] + head * P.out_stride[2] + i % (D / 4) * 4) = make_uint2(0, 0);
+            if (P.lse && i % (D / 4) == 0) P.lse[((long long)b * P.tree.N + node) * P.Hq + head] = -CUDART_INF_F;
         }
-        // the row's place in its unit, and the unit's parts: of the request's own, then of the prefix's
-        int row[2], parts[2], first[2];
-        long long whole[2];
-        {
-            const int e = P.n_groups + b, u = r / S::ROWS;
-            const int2 x = __ldcg(&P.unit[0][unit_of(P, e, u, h, S::ROWS)]);
-            first[0] = x.x; parts[0] = min(x.y, P.ctas); row[0] = r - u * S::ROWS;
-            whole[0] = whole_row_of(P, e, h, r);
-            if (x.x < 0 && skip == 0) continue;                     // (not cut, and nothing to put it together with: written already)
-        }
-        parts[1] = first[1] = row[1] = 0;
-        whole[1] = 0;
-        if (skip) {
-            const int q = place * rows + r, u = q / S::ROWS;
-            const int2 x = __ldcg(&P.unit[1][unit_of(P, g, u, h, S::ROWS)]);
-            first[1] = x.x; parts[1] = min(x.y, P.ctas); row[1] = q - u * S::ROWS;
-            whole[1] = whole_row_of(P, g, h, q);
-        }
-        const int all = parts[0] + parts[1];
+        return;
+    }
+    const int first_unit[2] = {row0 / S::ROWS, (q0 + row0) / S::ROWS};
+    if (tid < 4 && (tid < 2 || skip)) {
+        const int w = tid >> 1, u = first_unit[w] + (tid & 1), last = ((w ? q0 : 0) + upto - 1) / S::ROWS;
+        if (u <= last) s_unit[w][tid & 1] = __ldcg(&P.unit[w][unit_of(P, w ? g : P.n_groups + b, u, h, S::ROWS)]);
+    }
+    __syncthreads();
+    const long long whole0 = whole_row_of(P, P.n_groups + b, h, 0), whole1 = skip ? whole_row_of(P, g, h, q0) : 0;
+    const unsigned live = upto - row0;
+#pragma unroll 1
+    for (unsigned i = tid; i < live * (D / 4); i += MERGE_NT) {
+        const int ch = (int)(i / live), r = row0 + (int)(i - ch * live);
+        // the unit's parts: of the request's own, then of the prefix's
+        const int u0 = r / S::ROWS, u1 = (q0 + r) / S::ROWS;
+        const int2 own = s_unit[0][u0 - first_unit[0]], pre = skip ? s_unit[1][u1 - first_unit[1]] : make_int2(0, 0);
+        if (own.x < 0 && skip == 0) continue;                       // (not cut, and nothing to put it together with: written already)
+        const int mine = min(own.y, P.ctas), all = mine + min(pre.y, P.ctas);
+        const auto fetch = [&](int c, float2 &y, float4 &x) {
+            const bool w = c >= mine;
+            const int from = w ? pre.x : own.x, part = w ? c - mine : c;
+            if (from < 0) {
+                const long long at = (w ? whole1 : whole0) + r;
+                y = __ldcg(P.whole_ml[w] + at);
+                x = __ldcg((const float4 *)P.whole[w] + ((at >> 5) * (D / 4) + ch) * 32 + (at & 31));
+            } else {
+                // (its own slot for the first part, the first slot of the CTAs behind)
+                const long long slot = min(part ? (from / 2 + part) * 2 : from, 2 * P.ctas - 1);
+                const int row = w ? q0 + r - u1 * S::ROWS : r - u0 * S::ROWS;
+                y = __ldcg(P.ml + slot * S::ROWS + row);
+                x = __ldcg((const float4 *)P.part + (slot * (D / 4) + ch) * S::ROWS + row);
+            }
+        };
         float ref = -CUDART_INF_F, l = 0.f;
         bool only = false;                     // (some part saw keys, all with a score of -inf)
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        constexpr int AHEAD = 4;
+        constexpr int AHEAD = 6;
         for (int c0 = 0; c0 < all; c0 += AHEAD) {
             float4 x[AHEAD];
             float2 y[AHEAD];
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
-                const int c = min(c0 + k, all - 1), w = c >= parts[0], part = w ? c - parts[0] : c;
-                if (first[w] < 0) {
-                    y[k] = __ldcg(P.whole_ml[w] + whole[w]);
-                    x[k] = __ldcg((const float4 *)P.whole[w] + ((whole[w] >> 5) * (D / 4) + ch) * 32 + (whole[w] & 31));
-                } else {
-                    // (its own slot for the first part, the first slot of the CTAs behind)
-                    const long long slot = min(part ? (first[w] / 2 + part) * 2 : first[w], 2 * P.ctas - 1);
-                    y[k] = __ldcg(P.ml + slot * S::ROWS + row[w]);
-                    x[k] = __ldcg((const float4 *)P.part + (slot * (D / 4) + ch) * S::ROWS + row[w]);
-                }
+                y[k] = make_float2(-CUDART_INF_F, 0.f);
+                if (c0 + k < all) fetch(c0 + k, y[k], x[k]);
             }
             float top = ref;
 #pragma unroll
@@ -119,16 +126,18 @@ template <typename T, typename S> __global__ void __launch_bounds__(MERGE_NT, 4)
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
                 // (a part that saw nothing counts for nothing, whatever the others' reference)
-                const float w = c0 + k >= all || y[k].x == -CUDART_INF_F ? 0.f : ex2_approx(y[k].x - ref);
+                const float w = y[k].x == -CUDART_INF_F ? 0.f : ex2_approx(y[k].x - ref);
                 if (w != 0.f) {
                     l = fmaf(w, y[k].y, l);
                     o.x = fmaf(w, x[k].x, o.x); o.y = fmaf(w, x[k].y, o.y); o.z = fmaf(w, x[k].z, o.z); o.w = fmaf(w, x[k].w, o.w);
                 }
             }
         }
+        const int node = node_of(P, r), head = h * P.G + r - node * P.G;
+        T *to = (T *)P.out + b * P.out_stride[0] + node * P.out_stride[1] + head * P.out_stride[2] + ch * 4;
         const float inv = l == 0.f ? only ? CUDART_NAN_F : 0.f : 1.f / l;
         *(uint2 *)to = make_uint2(Pair<T>::pack(o.x * inv, o.y * inv), Pair<T>::pack(o.z * inv, o.w * inv));
-        if (lse) *lse = l == 0.f ? -CUDART_INF_F : (ref + log2f(l)) * LN2;
+        if (P.lse && ch == 0) P.lse[((long long)b * P.tree.N + node) * P.Hq + head] = l == 0.f ? -CUDART_INF_F : (ref + log2f(l)) * LN2;
     }
 }
 
