@@ -9,8 +9,8 @@
 //
 // Layout.  Units are tiles of 128 entries of a request, all key heads; the tiles of all requests, in order, are cut into one run per CTA (one CTA per
 // SM).  Two tiles that lie wholly among the committed tokens go together: a block of queries that is on chip serves both.
-// Four warps copy keys (by tensor map where all 32 of a warp's keys are there and blocks are multiples of 8 slots, else 16 bytes at a time), four
-// queries (by tensor map where a block of them is whole nodes), one issues the products, eight take the exponentials: half of the columns each warpgroup.
+// Four warps copy keys (by tensor map where all 32 of a warp's keys are there and blocks are multiples of 8 slots, else 16 bytes at a time), two
+// queries (by tensor map where a block of them is whole nodes), two issue the products, eight take the exponentials: half of the columns each warpgroup.
 //
 // What is not a number adds nothing: the maximum that bounds exponents from below takes NaN for its bound.  So it does not matter what
 // rows without a finite lse, columns beyond the rows, or keys that are not there hold.
@@ -97,7 +97,7 @@ template <int D_> struct Shape {
     static constexpr int total = off_bar + 512;
     static_assert(total + 1024 <= 227 * 1024, "shared memory");
 };
-constexpr int SUM_WARPS = 8, PRODUCTS = SUM_WARPS, NT = (SUM_WARPS + 1 + 8) * 32;
+constexpr int SUM_WARPS = 8, PRODUCTS = SUM_WARPS, KEYS = PRODUCTS + 2, QUERIES = KEYS + 4, NT = (QUERIES + 2) * 32;      // the roles' first warps
 struct Bars {
     uint64_t k_full[6], k_empty[6], q_full[4], q_empty[4], s_full[4], s_empty[4];
     uint32_t tmem;
@@ -135,11 +135,15 @@ __device__ __forceinline__ void find_run(const Params &P, int c, Bars *S, Run *r
     if (lane == 31) S->sums[warp] = incl;
     if (tid == 0) { S->found[0] = P.B; S->found[1] = 0; }
     __syncthreads();
-    int ahead = incl - mine, all = 0;
-    for (int w = 0; w < NT / 32; ++w) {
-        if (w < warp) ahead += S->sums[w];
-        all += S->sums[w];
+    static_assert(NT / 32 <= 32, "a lane for a warp's sum");
+    int warps = lane < NT / 32 ? S->sums[lane] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, warps, o);
+        if (lane >= o) warps += t;
     }
+    const int before = __shfl_sync(0xffffffffu, warps, max(warp - 1, 0)), all = __shfl_sync(0xffffffffu, warps, 31);
+    int ahead = incl - mine + (warp ? before : 0);
     const int each = (int)((unsigned)all / (unsigned)P.ctas), more = all - each * P.ctas, start = each * c + min(c, more);
     if (start >= ahead && start < ahead + mine) {
         for (int b = b0; b < b1; ++b) {
@@ -157,6 +161,47 @@ __device__ __forceinline__ void find_run(const Params &P, int c, Bars *S, Run *r
     if (run->b >= P.B) run->left = 0;
 }
 
+// What a key gets of 32 columns of scores (of the first `columns`; more than 16 or not): sum 2^(c s + ref), ref -lse log2 e or -inf.  Three pairs of
+// eight go without the special function unit, which is what the others wait for (16 a cycle on an SM).
+__device__ __forceinline__ float weights_of(uint32_t (&s)[32], unsigned long long c2, const float *ref, int columns, bool masked, const uint4 *mask,
+                                            const unsigned short *nodes, int quad, int lane)
+{
+    if (masked) {
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+            const uint32_t word = ((const uint32_t *)(mask + nodes[k]))[quad];
+            if (!((word >> lane) & 1u)) s[k] = 0xFF800000u;
+        }
+    }
+    unsigned long long sum[2] = {0ull, 0ull};
+    const auto some = [&](int k0) {
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) {
+            const int k = k0 + j;
+            const float4 r4 = *(const float4 *)(ref + k);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const unsigned long long y2 = fma_f32x2(pack_f32x2(__uint_as_float(s[k + 2 * i]), __uint_as_float(s[k + 2 * i + 1])), c2,
+                                                        i ? pack_f32x2(r4.z, r4.w) : pack_f32x2(r4.x, r4.y));
+                float x, y;
+                unpack_f32x2(y2, x, y);
+                const int pair = (j / 2 + i) % 8;
+                if (pair == 2 || pair == 5 || pair == 7) {
+                    // (no more than 2^127: only a lse that is not that of the scores could ask for it)
+                    sum[i] = add_f32x2(sum[i], attend::exp2_pair(pack_f32x2(fminf(fmaxf(x, -127.f), 127.f), fminf(fmaxf(y, -127.f), 127.f))));
+                } else {
+                    sum[i] = add_f32x2(sum[i], pack_f32x2(ex2_approx(fmaxf(x, -200.f)), ex2_approx(fmaxf(y, -200.f))));
+                }
+            }
+        }
+    };
+    some(0);
+    if (columns > 16) some(16);
+    float x, y;
+    unpack_f32x2(add_f32x2(sum[0], sum[1]), x, y);
+    return x + y;
+}
+
 template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_weigh_kernel(const __grid_constant__ Params P)
 {
     constexpr int D = S::D;
@@ -169,8 +214,8 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
         if (P.q_nodes) tc::prefetch_map(&P.q_map);
     }
     if (tid == 0) {
-        for (int i = 0; i < S::SK; ++i) { mbar_init(&B->k_full[i], 128); mbar_init(&B->k_empty[i], 1); }
-        for (int i = 0; i < S::SQ; ++i) { mbar_init(&B->q_full[i], 256); mbar_init(&B->q_empty[i], 1 + SUM_WARPS); }
+        for (int i = 0; i < S::SK; ++i) { mbar_init(&B->k_full[i], 128); mbar_init(&B->k_empty[i], 2); }
+        for (int i = 0; i < S::SQ; ++i) { mbar_init(&B->q_full[i], 128); mbar_init(&B->q_empty[i], 2 + SUM_WARPS); }
         for (int i = 0; i < 4; ++i) { mbar_init(&B->s_full[i], 1); mbar_init(&B->s_empty[i], SUM_WARPS); }
         B->dead = 0;
         B->last = -1;
@@ -324,34 +369,21 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
                         const uint32_t buf = n_s & 3;
                         wait(B, &B->s_full[buf], n_s >> 2 & 1);
                         tc::fence_after();
-                        unsigned long long sum = 0ull;
-                        for (int g = w * 32; g < columns; g += 64) {
-                            uint32_t a[32];
-                            tc::tmem_load(lanes + buf * 128 + g, a);
-                            tc::wait_loads(a);
-                            if (masked) {
-#pragma unroll
-                                for (int k = 0; k < 32; ++k) {
-                                    const uint32_t word = ((const uint32_t *)(mask + nodes[g + k]))[quad];
-                                    if (!((word >> lane) & 1u)) a[k] = 0xFF800000u;
-                                }
-                            }
-#pragma unroll
-                            for (int k = 0; k < 32; k += 4) {
-                                const float4 r4 = *(const float4 *)(ref + g + k);
-                                float x, y;
-                                unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(a[k]), __uint_as_float(a[k + 1])), c2, pack_f32x2(r4.x, r4.y)), x, y);
-                                sum = add_f32x2(sum, pack_f32x2(ex2_approx(fmaxf(x, -200.f)), ex2_approx(fmaxf(y, -200.f))));
-                                unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(a[k + 2]), __uint_as_float(a[k + 3])), c2, pack_f32x2(r4.z, r4.w)), x, y);
-                                sum = add_f32x2(sum, pack_f32x2(ex2_approx(fmaxf(x, -200.f)), ex2_approx(fmaxf(y, -200.f))));
-                            }
-                        }
-                        float x, y;
-                        unpack_f32x2(sum, x, y);
-                        if (ti == 0) acc0 += x + y; else acc1 += x + y;
+                        // the warpgroups take groups of 32 columns in turn, the first of a tile now the one, now the other
+                        const int g = ((w + n_s) & 1) * 32;
+                        const bool one = g < columns, two = g + 64 < columns;
+                        uint32_t x[32], y[32];
+                        if (one) tc::tmem_load(lanes + buf * 128 + g, x);
+                        if (two) tc::tmem_load(lanes + buf * 128 + g + 64, y);
+                        tc::wait_loads(x);
+                        tc::wait_loads(y);
                         tc::fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&B->s_empty[buf]);
+                        float got = 0.f;
+                        if (one) got = weights_of(x, c2, ref + g, columns - g, masked, mask, nodes + g, quad, lane);
+                        if (two) got += weights_of(y, c2, ref + g + 64, columns - g - 64, masked, mask, nodes + g + 64, quad, lane);
+                        if (ti == 0) acc0 += got; else acc1 += got;
                     }
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&B->q_empty[qs]);
@@ -364,22 +396,27 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
             if (slot >= 0 && sound && *(volatile int *)&B->dead == 0) __stcg(P.weights + slot, old + got);
             if (tid == 0) B->last = run.b;
         }
-    } else if (warp == PRODUCTS) {
-        // ---------------------------------------------------------------- products: one thread issues
+    } else if (warp < KEYS) {
+        // ---------------------------------------------------------------- products: two warps in turn, one thread of each issues (a product's 8 instructions,
+        // its barriers and the loop around them take some 900 cycles of a warp).  Each waits for every filling of keys and queries, and has a part in
+        // letting go of it, whether it has a product with it or not: a barrier's phase tells even fillings from odd ones only.
+        const int mine = warp - PRODUCTS;
         const uint32_t k_at = smem_u32(base), q_at = smem_u32(base + S::off_q);
         uint32_t n_k = 0, n_q = 0, n_s = 0;
         const auto gone = [&] { return *(volatile int *)&B->dead != 0; };
         while (run.next(P)) {
             const int rows = run.r.n * P.G, blocks = (rows + S::QB - 1) / S::QB;
-            for (int h = 0; h < P.Hkv; ++h, n_k += run.count)
+            for (int h = 0; h < P.Hkv; ++h, n_k += run.count) {
                 for (int qb = 0; qb < blocks; ++qb, ++n_q) {
                     const uint32_t qs = n_q % S::SQ;
                     const int columns = (min(S::QB, rows - qb * S::QB) + 15) / 16 * 16;
                     const uint32_t desc = tc::product_desc(attend::Pair<T>::TYPE, columns, false);
                     wait(B, &B->q_full[qs], n_q / S::SQ & 1);
+                    if (lane == 0) mbar_arrive(&B->q_empty[qs]);          // (the sums' warps let go of it when its products are done)
                     for (int ti = 0; ti < run.count; ++ti, ++n_s) {
                         const uint32_t ks = (n_k + ti) % S::SK, buf = n_s & 3;
                         if (qb == 0) wait(B, &B->k_full[ks], (n_k + ti) / S::SK & 1);
+                        if ((int)(n_s & 1) != mine) continue;
                         if (n_s >= 4) wait(B, &B->s_empty[buf], (n_s / 4 - 1) & 1);
                         tc::publish_shared();
                         tc::fence_after();
@@ -392,16 +429,19 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
                                 for (int i = 0; i < 4; ++i) tc::mma_ss(tmem + buf * 128, kd + 2 * i, qd + 2 * i, desc, p > 0 || i > 0);
                             }
                             tc::commit(&B->s_full[buf]);
-                            if (ti + 1 == run.count) tc::commit(&B->q_empty[qs]);
-                            if (qb + 1 == blocks) tc::commit(&B->k_empty[ks]);
                         }
                         __syncwarp();
                     }
                 }
+                // (an arrival when this warp's products so far are done; both warps': the keys are free)
+                if (tc::elected() && !gone())
+                    for (int ti = 0; ti < run.count; ++ti) tc::commit(&B->k_empty[(n_k + ti) % S::SK]);
+                __syncwarp();
+            }
         }
-    } else if (warp < PRODUCTS + 5) {
+    } else if (warp < QUERIES) {
         // ---------------------------------------------------------------- keys: a warp for 32 of every tile
-        const int which = warp - PRODUCTS - 1;
+        const int which = warp - KEYS;
         constexpr int CH = D / 8;                                     // 16-byte chunks of a row
         const uint32_t k_at = smem_u32(base);
         uint32_t n_k = 0;
@@ -462,8 +502,8 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
         tc::close_copies();
         tc::wait_copies<0>();
     } else {
-        // ---------------------------------------------------------------- queries: a warp for 32 rows of every block of them
-        const int which = warp - PRODUCTS - 5;
+        // ---------------------------------------------------------------- queries: a warp for 64 rows of every block of them
+        const int which = warp - QUERIES;
         constexpr int CH = D / 8;
         const uint32_t q_at = smem_u32(base + S::off_q);
         float *refs = (float *)(base + S::off_ref);
@@ -472,28 +512,29 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
         while (run.next(P)) {
             const Request r = run.r;
             const int rows = r.n * P.G, blocks = (rows + S::QB - 1) / S::QB;
-            // a row's reference, asked for a block ahead of its use
-            const auto reference = [&](int h, int qb) {
-                const int row = qb * S::QB + which * 32 + lane;
-                if (h >= P.Hkv || which * 32 >= S::QB || row >= rows) return -CUDART_INF_F;
+            // the references of the lane's two rows, asked for a block ahead of their use
+            const auto reference = [&](int h, int qb, int x) {
+                const int in = which * 64 + x * 32 + lane, row = qb * S::QB + in;
+                if (h >= P.Hkv || in >= S::QB || row >= rows) return -CUDART_INF_F;
                 const int node = node_of(P, row);
-                const float x = __ldg(P.lse + ((long long)run.b * P.tree.N + node) * P.Hq + h * P.G + row - node * P.G);
-                return fabsf(x) < CUDART_INF_F ? -x * LOG2E : -CUDART_INF_F;
+                const float l = __ldg(P.lse + ((long long)run.b * P.tree.N + node) * P.Hq + h * P.G + row - node * P.G);
+                return fabsf(l) < CUDART_INF_F ? -l * LOG2E : -CUDART_INF_F;
             };
-            float ahead = reference(0, 0);
+            float ahead[2] = {reference(0, 0, 0), reference(0, 0, 1)};
             for (int h = 0; h < P.Hkv; ++h)
                 for (int qb = 0; qb < blocks; ++qb, ++n_q) {
                     const uint32_t slot = n_q % S::SQ;
-                    const float ref = ahead;
-                    ahead = qb + 1 < blocks ? reference(h, qb + 1) : reference(h + 1, 0);
+                    const float ref[2] = {ahead[0], ahead[1]};
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) ahead[x] = qb + 1 < blocks ? reference(h, qb + 1, x) : reference(h + 1, 0, x);
                     if (n_q >= S::SQ) wait(B, &B->q_empty[slot], (n_q / S::SQ - 1) & 1);
                     __syncwarp();
                     if (stopped(B)) continue;
                     if (c_hold_slot >= 0 && c_hold_slot / P.tree.N == run.b) continue;       // (a test may ask for a request's queries to stay away)
                     const int columns = min(S::QB, rows - qb * S::QB);
-                    if (P.q_nodes) {
+                    if (P.q_nodes && which == 0) {
                         // (rows behind the tree's come as zeros, those behind the box as they are: columns that nobody counts)
-                        if (which == 0 && tc::elected()) {
+                        if (tc::elected()) {
                             tc::expect_bytes(&B->q_full[slot], P.q_nodes * P.G * D * 2);
 #pragma unroll
                             for (int p = 0; p < S::PANELS; ++p)
@@ -501,20 +542,23 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
                                              &B->q_full[slot]);
                         }
                         __syncwarp();
-                    } else if (which * 32 < (columns + 15) / 16 * 16) {
-                        const T *q = (const T *)P.q + run.b * P.q_stride[0] + (long long)h * P.G * P.q_stride[2];
-                        const uint32_t to = q_at + slot * S::Q_SLOT;
-                        const int mine = min(qb * S::QB + which * 32 + lane, rows - 1), node = node_of(P, mine);
-                        const unsigned long long from = (unsigned long long)(q + node * P.q_stride[1] + (mine - node * P.G) * P.q_stride[2]);
-#pragma unroll 4
-                        for (int i = 0; i < CH; ++i) {
-                            const int y = i * 32 + lane, row = y / CH, ch = y % CH, at = which * 32 + row;
-                            const unsigned long long f = __shfl_sync(0xffffffffu, from, row);
-                            tc::copy16(to + ch / 8 * (S::QB * 128) + at * 128 + (((ch & 7) ^ (at & 7)) << 4), f + ch * 16, at < columns ? 16 : 0);
-                        }
                     }
-                    refs[slot * 128 + which * 32 + lane] = ref;
-                    nodes[slot * 128 + which * 32 + lane] = (unsigned short)node_of(P, min(qb * S::QB + which * 32 + lane, rows - 1));
+                    for (int x = 0; x < 2; ++x) {
+                        const int first = which * 64 + x * 32, mine = min(qb * S::QB + first + lane, rows - 1), node = node_of(P, mine);
+                        if (!P.q_nodes && first < (columns + 15) / 16 * 16) {
+                            const T *q = (const T *)P.q + run.b * P.q_stride[0] + (long long)h * P.G * P.q_stride[2];
+                            const uint32_t to = q_at + slot * S::Q_SLOT;
+                            const unsigned long long from = (unsigned long long)(q + node * P.q_stride[1] + (mine - node * P.G) * P.q_stride[2]);
+#pragma unroll 4
+                            for (int i = 0; i < CH; ++i) {
+                                const int y = i * 32 + lane, row = y / CH, ch = y % CH, at = first + row;
+                                const unsigned long long f = __shfl_sync(0xffffffffu, from, row);
+                                tc::copy16(to + ch / 8 * (S::QB * 128) + at * 128 + (((ch & 7) ^ (at & 7)) << 4), f + ch * 16, at < columns ? 16 : 0);
+                            }
+                        }
+                        refs[slot * 128 + first + lane] = ref[x];
+                        nodes[slot * 128 + first + lane] = (unsigned short)node;
+                    }
                     tc::arrive_with_copies(&B->q_full[slot]);
                     mbar_arrive(&B->q_full[slot]);
                 }
