@@ -495,7 +495,8 @@ int32_t spec_token_logprobs(const SpecLogprobs *a, void *stream);
  * whatever their slots held (the first layer of a step).  A row whose lse is not finite adds nothing, and nothing of its query matters.
  * Sums in fp32 in a fixed order: the same inputs give the same bits.  A key on a bad block is left out (SPEC_DEV_PAGE); a bad tree leaves
  * the request's weights as they were (SPEC_DEV_TOPOLOGY).  The blocks behind protected[b] must be the request's own.
- * What is no number (a score of NaN) adds nothing.  SPEC_DEV_TIMEOUT (a wait ran out): the weights of the requests with this status are undefined.
+ * What is no number (a score of NaN) adds nothing.  SPEC_DEV_TIMEOUT (a wait ran out, in any request's part of the work): the weights
+ * of the call's requests are undefined.  `ws`: spec_cache_weights_workspace_bytes() bytes (contents do not matter).
  * D: 64, 128 or 256; q and cache SPEC_BF16 or SPEC_F16; strides in elements, multiples of 8, bases on 16 bytes.
  */
 typedef struct {
@@ -518,7 +519,8 @@ typedef struct {
     float *weights;                   /* [num_blocks, block_size]                                     */
     int32_t *status;                  /* [B]                                                          */
 } SpecWeights;
-int32_t spec_cache_weights(const SpecWeights *a, void *stream);
+int32_t spec_cache_weights_workspace_bytes(const SpecWeights *a, int64_t *bytes);
+int32_t spec_cache_weights(const SpecWeights *a, void *ws, int64_t ws_bytes, void *stream);
 
 /*
  * Eviction: a request with more than `budget` committed tokens keeps `budget` entries: its first p = protected[b], its last

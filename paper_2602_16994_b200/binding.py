@@ -36,7 +36,7 @@ EXPORTS = ("spec_workspace_bytes", "spec_tree_probs", "spec_verify_specinfer", "
            "spec_tree_analysis", "spec_latency_model", "spec_test_hooks", "spec_row_statistics",
            "spec_verify_otlp", "spec_cache_slots", "spec_norm_rope_cache", "spec_tree_attention_workspace_bytes",
            "spec_tree_attention", "spec_cache_commit", "spec_verify_probs", "spec_token_logprobs",
-           "spec_prefix_attention_workspace_bytes", "spec_prefix_attention", "spec_cache_weights", "spec_cache_evict_workspace_bytes", "spec_cache_evict")
+           "spec_prefix_attention_workspace_bytes", "spec_prefix_attention", "spec_cache_weights_workspace_bytes", "spec_cache_weights", "spec_cache_evict_workspace_bytes", "spec_cache_evict")
 
 
 class SpecIn(C.Structure):

@@ -57,7 +57,7 @@ int32_t spec_token_logprobs(const SpecLogprobs *a, void *stream)
                                   : go(logp::spec_logprobs_kernel<__nv_bfloat16>);
 }
 
-int32_t spec_cache_weights(const SpecWeights *a, void *stream)
+static int weights_check(const SpecWeights *a)
 {
     if (!a || !a->q || !a->k_cache || !a->lse || !a->block_table || !a->lengths || !a->parent || !a->weights || !a->status) return SPEC_ERR_NULL;
     if (bad_tree_shape(a->B, a->N, a->topo_seq_stride) || bad_pages(a->num_blocks, a->block_size, a->table_width) ||
@@ -66,13 +66,42 @@ int32_t spec_cache_weights(const SpecWeights *a, void *stream)
     if (a->dtype != SPEC_BF16 && a->dtype != SPEC_F16) return SPEC_ERR_DTYPE;
     if (!(a->scale >= 0.f && a->scale <= 3.4e38f)) return SPEC_ERR_PARAM;
     if (a->D != 64 && a->D != 128 && a->D != 256) return SPEC_ERR_UNSUPPORTED;
-    // (tiles, and steps of a tile, are counted in 32 bits)
-    const double tiles = (double)std::min<int64_t>((int64_t)a->table_width * a->block_size, 0x7FFFFFFF) / weigh::KT + 2;
-    const double steps = (double)a->Hkv * (((double)a->N * (a->Hq / a->Hkv)) / 64 + 1);
+    // (tiles of all heads, and steps of a run, are counted in 32 bits)
+    const double tiles = ((double)std::min<int64_t>((int64_t)a->table_width * a->block_size, 0x7FFFFFFF) / weigh::KT + 2) * a->Hkv;
+    const double steps = ((double)a->N * (a->Hq / a->Hkv)) / 64 + 1;
     if (a->B * tiles > 2.0e9 || a->B * tiles * steps / 148 > 1.0e9) return SPEC_ERR_UNSUPPORTED;
     int64_t all = 0;
     for (int j = 0; j < 3; ++j) all |= a->q_stride[j] | a->k_cache_stride[j];
     if (all % 8 || !aligned(a->q, 16) || !aligned(a->k_cache, 16)) return SPEC_ERR_UNSUPPORTED;
+    return SPEC_OK;
+}
+
+struct WeightsLayout { int64_t part, joint, late, total; };
+static WeightsLayout weights_layout(int ctas)
+{
+    WeightsLayout L = {};
+    L.joint = (int64_t)ctas * 512 * 4;
+    L.late = L.joint + (int64_t)ctas * 16;
+    L.total = L.late + ((int64_t)ctas * 4 + 255) / 256 * 256;
+    return L;
+}
+
+int32_t spec_cache_weights_workspace_bytes(const SpecWeights *a, int64_t *bytes)
+{
+    if (!bytes) return SPEC_ERR_NULL;
+    const int rc = weights_check(a);
+    if (rc) return rc;
+    *bytes = weights_layout(sm_ctas()).total;
+    return SPEC_OK;
+}
+
+int32_t spec_cache_weights(const SpecWeights *a, void *ws, int64_t ws_bytes, void *stream)
+{
+    const int rc = weights_check(a);
+    if (rc) return rc;
+    const int ctas = sm_ctas();
+    const WeightsLayout L = weights_layout(ctas);
+    if (!ws || !aligned(ws, 256) || ws_bytes < L.total) return SPEC_ERR_WORKSPACE;
     weigh::Params p = {};
     p.tree = tree_args(a->N, a->lengths, a->n_nodes, a->parent, a->topo_seq_stride);
     p.B = a->B; p.Hq = a->Hq; p.Hkv = a->Hkv; p.G = a->Hq / a->Hkv;
@@ -83,7 +112,10 @@ int32_t spec_cache_weights(const SpecWeights *a, void *stream)
     p.q = a->q; p.k = a->k_cache; p.lse = a->lse; p.table = a->block_table; p.table_stride = a->table_stride;
     p.protect = a->protected_len; p.weights = a->weights; p.status = a->status;
     for (int j = 0; j < 3; ++j) { p.q_stride[j] = a->q_stride[j]; p.k_stride[j] = a->k_cache_stride[j]; }
-    p.ctas = sm_ctas();
+    p.ctas = ctas;
+    p.part = (float *)((unsigned char *)ws + L.part);
+    p.joint = (int4 *)((unsigned char *)ws + L.joint);
+    p.late = (int *)((unsigned char *)ws + L.late);
     const bool half = a->dtype == SPEC_F16;
     p.box = a->block_size % 8 ? 0 : a->block_size % 16 ? 8 : a->block_size % 32 ? 16 : 32;
     const int64_t sizes[4] = {a->D, a->Hkv, a->block_size, a->num_blocks};
@@ -96,8 +128,12 @@ int32_t spec_cache_weights(const SpecWeights *a, void *stream)
             const int64_t q_sizes[4] = {a->D, a->Hq, a->N, a->B};
             if (!tensor_map(&p.q_map, a->q, half, q_sizes, {a->q_stride[2], a->q_stride[1], a->q_stride[0]}, {p.G, p.q_nodes, 1})) p.q_nodes = 0;
         }
-        const int smem = S::total + 1024, rc = prepare(kernel, smem, false);
-        return rc ? rc : launch(kernel, dim3(p.ctas), weigh::NT, smem, 0, (cudaStream_t)stream, p);
+        const int smem = S::total + 1024;
+        int e = prepare(kernel, smem, false);
+        if (!e) e = prepare(weigh::spec_weigh_join_kernel, 0, false);
+        if (e) return e;
+        e = launch(kernel, dim3(ctas), weigh::NT, smem, 0, (cudaStream_t)stream, p);
+        return e ? e : launch(weigh::spec_weigh_join_kernel, dim3(ctas + a->B), weigh::JOIN_NT, 0, 0, (cudaStream_t)stream, p);
     };
 #define GO(D)                                                                                                  \
     (half ? go(weigh::Shape<D>(), weigh::spec_weigh_kernel<__half, weigh::Shape<D>>)                           \

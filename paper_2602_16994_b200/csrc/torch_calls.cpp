@@ -815,6 +815,7 @@ struct ServeLibrary {
     decltype(&spec_prefix_attention_workspace_bytes) prefix_bytes;
     decltype(&spec_prefix_attention) prefix;
     decltype(&spec_token_logprobs) logprobs;
+    decltype(&spec_cache_weights_workspace_bytes) weights_bytes;
     decltype(&spec_cache_weights) weights;
     decltype(&spec_cache_evict_workspace_bytes) evict_bytes;
     decltype(&spec_cache_evict) evict;
@@ -936,7 +937,10 @@ PyObject *py_weights(PyObject *, PyObject *const *a, Py_ssize_t n)
         strides_of(q, s.q_stride); strides_of(kc, s.k_cache_stride);
         const at::Tensor status = place.fresh({B}, at::kInt);
         s.status = int_ptr(status);
-        check(unlocked([&] { return serve_lib.weights(&s, place.stream()); }), "spec_cache_weights");
+        int64_t bytes = 0;
+        check(serve_lib.weights_bytes(&s, &bytes), "spec_cache_weights_workspace_bytes");
+        const at::Tensor ws = empty({bytes}, at::kByte, place.device());         // (of this call alone)
+        check(unlocked([&] { return serve_lib.weights(&s, ws.data_ptr(), bytes, place.stream()); }), "spec_cache_weights");
         written(THPVariable_Unpack(a[0]));
         return THPVariable_Wrap(status);
     });
@@ -1028,6 +1032,7 @@ PyObject *py_init_serve(PyObject *, PyObject *args)
     find(serve_lib.prefix_bytes, "spec_prefix_attention_workspace_bytes");
     find(serve_lib.prefix, "spec_prefix_attention");
     find(serve_lib.logprobs, "spec_token_logprobs");
+    find(serve_lib.weights_bytes, "spec_cache_weights_workspace_bytes");
     find(serve_lib.weights, "spec_cache_weights");
     find(serve_lib.evict_bytes, "spec_cache_evict_workspace_bytes");
     find(serve_lib.evict, "spec_cache_evict");

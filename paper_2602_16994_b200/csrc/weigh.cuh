@@ -7,8 +7,9 @@
 //
 // What bounds it.  With few rows the keys' bytes: 256 KB a tile of 128 keys at 8 heads of 128 entries.  With many rows the exponentials.
 //
-// Layout.  Units are tiles of 128 entries of a request, all key heads; the tiles of all requests, in order, are cut into one run per CTA (one CTA per
-// SM).  Two tiles that lie wholly among the committed tokens go together: a block of queries that is on chip serves both.
+// Balance.  Two tiles that lie wholly among the committed tokens go together (a block of queries that is on chip serves both), the others by themselves; a
+// unit is such a group and a key head, its length its tiles.  The units of all requests, groups in order, heads within, are cut into one run per CTA (one
+// CTA per SM).  A group whose heads are in several runs leaves their sums in the workspace, and spec_weigh_join_kernel adds them up in order.
 // Four warps copy keys (by tensor map where all 32 of a warp's keys are there and blocks are multiples of 8 slots, else 16 bytes at a time), two
 // queries (by tensor map where a block of them is whole nodes), two issue the products, eight take the exponentials: half of the columns each warpgroup.
 //
@@ -42,12 +43,16 @@ struct Params {
     float *weights;
     int *status;
     int ctas;
+    float *part;                               // [ctas][2][2][128] sums of a run's first and last group, where others have heads of them too
+    int4 *joint;                               // [ctas] the group whose first heads this CTA has: request, tile, tiles; parts and slot
+    int *late;                                 // [ctas] a wait ran out
 };
 
 struct Request {
     int len, n, from, end;                     // nodes (0: idle or a bad number of them); entries [from, end) count
     __device__ __forceinline__ int first() const { return from / KT; }
     __device__ __forceinline__ int tiles() const { return n == 0 || end <= from ? 0 : (end + KT - 1) / KT - from / KT; }
+    __device__ __forceinline__ int pairs() const { return max(0, min(len / KT - from / KT, tiles())) / 2; }
 };
 __device__ __forceinline__ Request request_of(const Params &P, int b)
 {
@@ -63,11 +68,11 @@ __device__ __forceinline__ Request request_of(const Params &P, int b)
 __device__ __forceinline__ int column_of(const Params &P, int key) { return (int)((__umulhi(P.block_mul, (unsigned)key) + (unsigned)key) >> P.block_shift); }
 __device__ __forceinline__ int node_of(const Params &P, int row) { return (int)((__umulhi(P.group_mul, (unsigned)row) + (unsigned)row) >> P.group_shift); }
 
-// What a CTA has next: a tile of a request, or two; every role counts for itself.
+// What a CTA has next: heads of a group; every role counts for itself.
 struct Run {
-    int b, t, left;                            // t: tiles of the request gone by
+    int b, t, h, left, next_at;                // the next unit: request, tiles of it gone by, head; length of the run from there on, and its place
     Request r;
-    int tile, count;                           // this step's
+    int tile, count, h0, h1, at;               // this step's group, and the heads of it, and its place among all units
     __device__ __forceinline__ bool next(const Params &P)
     {
         if (left <= 0) return false;
@@ -77,9 +82,14 @@ struct Run {
             t = 0;
         }
         tile = r.first() + t;
-        count = left >= 2 && t + 1 < r.tiles() && (long long)(tile + 2) * KT <= r.len ? 2 : 1;
-        t += count;
-        left -= count;
+        count = t < 2 * r.pairs() ? 2 : 1;
+        h0 = h;
+        h1 = min(P.Hkv, h0 + (left + count - 1) / count);
+        at = next_at;
+        left -= (h1 - h0) * count;
+        next_at += (h1 - h0) * count;
+        h = h1;
+        if (h == P.Hkv) { h = 0; t += count; }
         return true;
     }
 };
@@ -101,7 +111,7 @@ constexpr int SUM_WARPS = 8, PRODUCTS = SUM_WARPS, KEYS = PRODUCTS + 2, QUERIES 
 struct Bars {
     uint64_t k_full[6], k_empty[6], q_full[4], q_empty[4], s_full[4], s_empty[4];
     uint32_t tmem;
-    int dead, last, found[2], sums[20];        // (last: the last request that this CTA had tiles of)
+    int dead, found[2], sums[20];
     Request request;                           // the one that the run begins in
 };
 static_assert(sizeof(Bars) <= 512, "the area behind the buffers");
@@ -118,14 +128,18 @@ __device__ __forceinline__ void wait(Bars *B, uint64_t *bar, uint32_t parity)
 // one answer for the whole (converged) warp
 __device__ __forceinline__ bool stopped(Bars *B) { return __any_sync(0xffffffffu, *(volatile int *)&B->dead) != 0; }
 
+struct Cuts {                                  // runs of equal length, the first `more` of them longer by one
+    int all, each, more;
+    __device__ __forceinline__ int start(int c) const { return each * c + min(c, more); }
+};
 // The run of CTA c: all threads.
-__device__ __forceinline__ void find_run(const Params &P, int c, Bars *S, Run *run, int tid)
+__device__ __forceinline__ void find_run(const Params &P, int c, Bars *S, Run *run, Cuts *cuts, int tid)
 {
     const int lane = tid & 31, warp = tid >> 5;
     const int per = (P.B + NT - 1) / NT, b0 = min(P.B, tid * per), b1 = min(P.B, b0 + per);
     int mine = 0;
     Request only = {};                         // (at most one request to a thread: it is looked up once)
-    for (int b = b0; b < b1; ++b) { only = request_of(P, b); mine += only.tiles(); }
+    for (int b = b0; b < b1; ++b) { only = request_of(P, b); mine += only.tiles() * P.Hkv; }
     int incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -148,17 +162,30 @@ __device__ __forceinline__ void find_run(const Params &P, int c, Bars *S, Run *r
     if (start >= ahead && start < ahead + mine) {
         for (int b = b0; b < b1; ++b) {
             if (per > 1) only = request_of(P, b);
-            const int t = only.tiles();
+            const int t = only.tiles() * P.Hkv;
             if (start < ahead + t) { S->found[0] = b; S->found[1] = start - ahead; S->request = only; break; }
             ahead += t;
         }
     }
     __syncthreads();
-    run->left = each + (c < more);
     run->b = S->found[0];
-    run->t = S->found[1];
     run->r = S->request;
-    if (run->b >= P.B) run->left = 0;
+    run->left = run->b < P.B ? each + (c < more) : 0;
+    // the place in the request: the first unit that begins there or behind
+    run->next_at = start;
+    int at = S->found[1], pairs = run->b < P.B ? run->r.pairs() * 2 * P.Hkv : 0;
+    if (at < pairs) {
+        const int g = (int)((unsigned)at / (2u * P.Hkv)), in = at - g * 2 * P.Hkv;
+        run->t = 2 * g; run->h = (in + 1) / 2;
+        run->left -= in & 1;
+        run->next_at += in & 1;
+    } else {
+        at -= pairs;
+        const int g = (int)((unsigned)at / (unsigned)P.Hkv);
+        run->t = (run->b < P.B ? 2 * run->r.pairs() : 0) + g; run->h = at - g * P.Hkv;
+    }
+    if (run->h == P.Hkv) { run->h = 0; run->t += 2; }
+    cuts->all = all; cuts->each = each; cuts->more = more;
 }
 
 // What a key gets of 32 columns of scores (of the first `columns`; more than 16 or not): sum 2^(c s + ref), ref -lse log2 e or -inf.  Three pairs of
@@ -218,12 +245,13 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
         for (int i = 0; i < S::SQ; ++i) { mbar_init(&B->q_full[i], 128); mbar_init(&B->q_empty[i], 2 + SUM_WARPS); }
         for (int i = 0; i < 4; ++i) { mbar_init(&B->s_full[i], 1); mbar_init(&B->s_empty[i], SUM_WARPS); }
         B->dead = 0;
-        B->last = -1;
         mbar_fence_init();
     }
     grid_dependency_wait();
     Run run;
-    find_run(P, blockIdx.x, B, &run, tid);
+    Cuts cuts;
+    find_run(P, blockIdx.x, B, &run, &cuts, tid);
+    grid_launch_dependents();                  // (the joining kernel waits by itself)
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
@@ -235,49 +263,20 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
         unsigned short *parent = (unsigned short *)(base + S::off_parent);
         uint4 *mask = (uint4 *)(base + S::off_mask);
         float *part = (float *)(base + S::off_part);
-        // requests' status, from the inputs alone, by the last CTAs first: where there are few tiles, these have none; a request whose CTA a
-        // wait ran out in is marked at the end
-        for (int b = P.ctas - 1 - blockIdx.x; b < P.B; b += P.ctas) {
-            const int len = __ldg(P.tree.lengths + b), nn = tree_nodes(P.tree, b), n = len < 0 ? 0 : max(nn, 0);
-            const int *row = P.tree.parent + (long long)b * P.tree.topo_seq_stride;
-            bool bad = false, page = false;
-            for (int i = tid; i < n; i += 256) {
-                const int p = __ldg(row + i);
-                bad |= i == 0 ? p != -1 : p < 0 || p >= i;
-            }
-            const long long keys = n ? (long long)len + n : 0;
-            const int from = P.protect ? max(0, __ldg(P.protect + b)) : 0;
-            if (n && from < keys) {
-                page = keys > (long long)P.width * P.block;
-                const int last = (int)min((keys + P.block - 1) / P.block, (long long)P.width);
-                for (int col = from / P.block + tid; col < last; col += 256) {
-                    const int id = __ldg(P.table + (long long)b * P.table_stride + col);
-                    page |= id < 0 || id >= P.num_blocks;
-                }
-            }
-            part[tid] = __int_as_float((bad ? 1 : 0) | (page ? 2 : 0));
-            bar_sync(1, 256);
-            if (warp == 0) {
-                int x = 0;
-                for (int i = lane; i < 256; i += 32) x |= __float_as_int(part[i]);
-                bad = __any_sync(0xffffffffu, x & 1) != 0;
-                page = __any_sync(0xffffffffu, x & 2) != 0;
-                if (lane == 0) P.status[b] = len < 0 ? SPEC_DEV_OK : nn < 0 || bad ? SPEC_DEV_TOPOLOGY : page ? SPEC_DEV_PAGE : SPEC_DEV_OK;
-            }
-            bar_sync(1, 256);
-        }
         const unsigned long long c2 = pack_f32x2(P.c, P.c);
         uint32_t n_q = 0, n_s = 0, n_step = 0;
         int tree_of = -1;
         bool sound = true;
+        int4 joint = make_int4(0, 0, 0, 0);
         for (; run.next(P); ++n_step) {
             const Request r = run.r;
+            const bool whole = run.h0 == 0 && run.h1 == P.Hkv;
             const int rows = r.n * P.G, blocks = (rows + S::QB - 1) / S::QB;
             // the thread's entry of the tile that it finishes, and what it holds
             const int entry = (run.tile + (run.count == 2 ? w : 0)) * KT + mine;
             long long slot = -1;
             float old = 0.f;
-            if (entry >= r.from && entry < r.end && w < run.count) {
+            if (whole && entry >= r.from && entry < r.end && w < run.count) {
                 const int col = column_of(P, entry), id = __ldg(P.table + (long long)run.b * P.table_stride + col);
                 if (id >= 0 && id < P.num_blocks) {
                     slot = (long long)id * P.block + (entry - col * P.block);
@@ -358,7 +357,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
                 bar_sync(1, 256);
             }
             float acc0 = 0.f, acc1 = 0.f;
-            for (int h = 0; h < P.Hkv; ++h)
+            for (int h = run.h0; h < run.h1; ++h)
                 for (int qb = 0; qb < blocks; ++qb, ++n_q) {
                     const uint32_t qs = n_q % S::SQ;
                     const int columns = min(S::QB, rows - qb * S::QB);
@@ -370,19 +369,17 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
                         wait(B, &B->s_full[buf], n_s >> 2 & 1);
                         tc::fence_after();
                         // the warpgroups take groups of 32 columns in turn, the first of a tile now the one, now the other
-                        const int g = ((w + n_s) & 1) * 32;
-                        const bool one = g < columns, two = g + 64 < columns;
-                        uint32_t x[32], y[32];
-                        if (one) tc::tmem_load(lanes + buf * 128 + g, x);
-                        if (two) tc::tmem_load(lanes + buf * 128 + g + 64, y);
-                        tc::wait_loads(x);
-                        tc::wait_loads(y);
+                        float got = 0.f;
+#pragma unroll 1
+                        for (int g = ((w + n_s) & 1) * 32; g < columns; g += 64) {
+                            uint32_t x[32];
+                            tc::tmem_load(lanes + buf * 128 + g, x);
+                            tc::wait_loads(x);
+                            got += weights_of(x, c2, ref + g, columns - g, masked, mask, nodes + g, quad, lane);
+                        }
                         tc::fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&B->s_empty[buf]);
-                        float got = 0.f;
-                        if (one) got = weights_of(x, c2, ref + g, columns - g, masked, mask, nodes + g, quad, lane);
-                        if (two) got += weights_of(y, c2, ref + g + 64, columns - g - 64, masked, mask, nodes + g + 64, quad, lane);
                         if (ti == 0) acc0 += got; else acc1 += got;
                     }
                     __syncwarp();
@@ -394,8 +391,22 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
             bar_sync(1, 256);
             const float got = (w ? acc1 : acc0) + mail[w * 128 + mine];
             if (slot >= 0 && sound && *(volatile int *)&B->dead == 0) __stcg(P.weights + slot, old + got);
-            if (tid == 0) B->last = run.b;
+            if (!whole) {
+                const int c = blockIdx.x, place = n_step == 0 ? 0 : 1;
+                __stcg(P.part + ((c * 2 + place) * 2 + w) * 128 + mine, got);
+                if (run.h0 == 0 && sound) {
+                    // the CTA that has a group's first heads tells what there is to join: runs that begin ahead of the group's last unit's end have one
+                    // of its units (or are shorter than that and have none at all)
+                    const int last = run.at + (P.Hkv - 1) * run.count;
+                    int parts = 1;
+                    while (c + parts < P.ctas && cuts.start(c + parts) <= last) ++parts;
+                    joint = make_int4(run.b, run.tile, run.count, parts << 1 | place);
+                }
+            }
         }
+        // (a run without a unit: its part of whatever group is 0)
+        if (n_step == 0) __stcg(P.part + blockIdx.x * 512 + tid, 0.f), __stcg(P.part + blockIdx.x * 512 + 256 + tid, 0.f);
+        if (tid == 0) P.joint[blockIdx.x] = joint;
     } else if (warp < KEYS) {
         // ---------------------------------------------------------------- products: two warps in turn, one thread of each issues (a product's 8 instructions,
         // its barriers and the loop around them take some 900 cycles of a warp).  Each waits for every filling of keys and queries, and has a part in
@@ -406,7 +417,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
         const auto gone = [&] { return *(volatile int *)&B->dead != 0; };
         while (run.next(P)) {
             const int rows = run.r.n * P.G, blocks = (rows + S::QB - 1) / S::QB;
-            for (int h = 0; h < P.Hkv; ++h, n_k += run.count) {
+            for (int h = run.h0; h < run.h1; ++h, n_k += run.count) {
                 for (int qb = 0; qb < blocks; ++qb, ++n_q) {
                     const uint32_t qs = n_q % S::SQ;
                     const int columns = (min(S::QB, rows - qb * S::QB) + 15) / 16 * 16;
@@ -461,7 +472,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
                 }
                 whole[ti] = P.box && __all_sync(0xffffffffu, id[ti] >= 0);
             }
-            for (int h = 0; h < P.Hkv; ++h)
+            for (int h = run.h0; h < run.h1; ++h)
                 for (int ti = 0; ti < run.count; ++ti, ++n_k) {
                     const uint32_t slot = n_k % S::SK;
                     if (n_k >= S::SK) wait(B, &B->k_empty[slot], (n_k / S::SK - 1) & 1);
@@ -515,13 +526,13 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
             // the references of the lane's two rows, asked for a block ahead of their use
             const auto reference = [&](int h, int qb, int x) {
                 const int in = which * 64 + x * 32 + lane, row = qb * S::QB + in;
-                if (h >= P.Hkv || in >= S::QB || row >= rows) return -CUDART_INF_F;
+                if (h >= run.h1 || in >= S::QB || row >= rows) return -CUDART_INF_F;
                 const int node = node_of(P, row);
                 const float l = __ldg(P.lse + ((long long)run.b * P.tree.N + node) * P.Hq + h * P.G + row - node * P.G);
                 return fabsf(l) < CUDART_INF_F ? -l * LOG2E : -CUDART_INF_F;
             };
-            float ahead[2] = {reference(0, 0, 0), reference(0, 0, 1)};
-            for (int h = 0; h < P.Hkv; ++h)
+            float ahead[2] = {reference(run.h0, 0, 0), reference(run.h0, 0, 1)};
+            for (int h = run.h0; h < run.h1; ++h)
                 for (int qb = 0; qb < blocks; ++qb, ++n_q) {
                     const uint32_t slot = n_q % S::SQ;
                     const float ref[2] = {ahead[0], ahead[1]};
@@ -576,11 +587,62 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
     if (warp == PRODUCTS) {
         tc::fence_after();
         tc::tmem_free(tmem, 512);
-        // (behind what the sums' warps of this CTA or another wrote of the request when they began, 2 s ago)
-        if (B->dead)
-            for (int b = B->found[0] + lane; b <= B->last; b += 32)
-                if (__ldg(P.tree.lengths + b) >= 0) P.status[b] = SPEC_DEV_TIMEOUT;
+        if (lane == 0) P.late[blockIdx.x] = B->dead;
     }
+}
+
+// ---- joining ------------------------------------------------------------------------------------------------------------------
+// The first P.ctas CTAs: where that one had a group's first heads and not all of them, the group's sums are added up, in order.  The others: a request
+// each, its status (from inputs alone, while the sums are still made).
+constexpr int JOIN_NT = 256;
+
+__global__ void __launch_bounds__(JOIN_NT) spec_weigh_join_kernel(const __grid_constant__ Params P)
+{
+    const int tid = threadIdx.x;
+    grid_launch_dependents();                  // (the next kernel waits for this one by itself, and this one for the sums)
+    if ((int)blockIdx.x >= P.ctas) {
+        const int b = blockIdx.x - P.ctas;
+        const int len = __ldg(P.tree.lengths + b), nn = tree_nodes(P.tree, b), n = len < 0 ? 0 : max(nn, 0);
+        const int *row = P.tree.parent + (long long)b * P.tree.topo_seq_stride;
+        bool bad = false, page = false, late = false;
+        for (int i = tid; i < n; i += JOIN_NT) {
+            const int p = __ldg(row + i);
+            bad |= i == 0 ? p != -1 : p < 0 || p >= i;
+        }
+        const long long keys = n ? (long long)len + n : 0;
+        const int from = P.protect ? max(0, __ldg(P.protect + b)) : 0;
+        if (n && from < keys) {
+            page = keys > (long long)P.width * P.block;
+            const int last = (int)min((keys + P.block - 1) / P.block, (long long)P.width);
+            for (int col = from / P.block + tid; col < last; col += JOIN_NT) {
+                const int id = __ldg(P.table + (long long)b * P.table_stride + col);
+                page |= id < 0 || id >= P.num_blocks;
+            }
+        }
+        bad = __syncthreads_or(bad) != 0;
+        page = __syncthreads_or(page) != 0;
+        grid_dependency_wait();
+        for (int i = tid; i < P.ctas; i += JOIN_NT) late |= *(volatile int *)(P.late + i) != 0;
+        late = __syncthreads_or(late) != 0;
+        if (tid == 0)
+            P.status[b] = len < 0 ? SPEC_DEV_OK
+                          : nn < 0 || bad ? SPEC_DEV_TOPOLOGY : late ? SPEC_DEV_TIMEOUT : page ? SPEC_DEV_PAGE : SPEC_DEV_OK;
+        return;
+    }
+    grid_dependency_wait();
+    const int4 joint = __ldcg(P.joint + blockIdx.x);
+    const int w = tid >> 7, mine = tid & 127, parts = joint.w >> 1;
+    if (w >= joint.z) return;
+    const Request r = request_of(P, joint.x);
+    const int entry = (joint.y + w) * KT + mine;
+    if (entry < r.from || entry >= r.end) return;
+    const int col = column_of(P, entry), id = __ldg(P.table + (long long)joint.x * P.table_stride + col);
+    float got = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < parts; ++k) got += __ldcg(P.part + (((blockIdx.x + k) * 2 + (k ? 0 : joint.w & 1)) * 2 + w) * 128 + mine);
+    if (id < 0 || id >= P.num_blocks) return;
+    float *to = P.weights + (long long)id * P.block + (entry - col * P.block);
+    __stcg(to, (P.fresh && entry >= r.len ? 0.f : __ldcg(to)) + got);
 }
 
 }  // namespace weigh

@@ -71,8 +71,11 @@ def test_prefix_plan():
 
 def test_weights_refusals(lib):  # noqa: F811
     good = dict(B=2, N=19, Hq=8, Hkv=2, D=128, scale=0.1, table_stride=1)
-    call = lambda **kw: lib.spec_cache_weights(C.byref(filled(Weights, **dict(good, **kw))), None)  # noqa: E731
-    assert lib.spec_cache_weights(None, None) == -1
+    n = L()
+    call = lambda **kw: lib.spec_cache_weights_workspace_bytes(C.byref(filled(Weights, **dict(good, **kw))), C.byref(n))  # noqa: E731
+    assert call() == 0 and n.value >= 256
+    assert lib.spec_cache_weights_workspace_bytes(None, C.byref(n)) == -1
+    assert lib.spec_cache_weights_workspace_bytes(C.byref(filled(Weights, **good)), None) == -1
     for f in ("q", "k_cache", "lse", "block_table", "lengths", "parent", "weights", "status"):
         assert call(**{f: None}) == -1, f
     for kw in (dict(B=0), dict(N=0), dict(N=1025), dict(Hkv=0), dict(Hq=7), dict(Hq=1), dict(num_blocks=0), dict(block_size=0),
@@ -85,6 +88,9 @@ def test_weights_refusals(lib):  # noqa: F811
     for kw in (dict(D=96), dict(D=512), dict(q=0x10008), dict(k_cache=0x10002), dict(q_stride=(1, 8, 8)), dict(k_cache_stride=(8, 8, 12)),
                dict(B=65535, N=1024, Hq=64, Hkv=64, table_width=1 << 20, table_stride=1 << 20, block_size=1 << 10)):
         assert call(**kw) == -6, kw
+    use = lambda ws, b: lib.spec_cache_weights(C.byref(filled(Weights, **good)), P(ws), L(b), None)  # noqa: E731
+    call()
+    assert use(None, 1 << 30) == -5 and use(0x10010, 1 << 30) == -5 and use(0x10000, n.value - 1) == -5
 
 
 def test_logprobs_refusals(lib):  # noqa: F811
