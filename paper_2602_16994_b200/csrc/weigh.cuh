@@ -11,7 +11,8 @@
 // unit is such a group and a key head, its length its tiles.  The units of all requests, groups in order, heads within, are cut into one run per CTA (one
 // CTA per SM).  A group whose heads are in several runs leaves their sums in the workspace, and spec_weigh_join_kernel adds them up in order.
 // Four warps copy keys (by tensor map where all 32 of a warp's keys are there and blocks are multiples of 8 slots, else 16 bytes at a time), two
-// queries (by tensor map where a block of them is whole nodes), two issue the products, eight take the exponentials: half of the columns each warpgroup.
+// queries (by tensor map where a block of them is whole nodes), two issue the products, sixteen take the exponentials, a product a
+// warpgroup in turn (128 columns: 1800 cycles of an SM where all warps had 32 columns each of every product, and its barriers).
 //
 // What is not a number adds nothing: the maximum that bounds exponents from below takes NaN for its bound.  So it does not matter what
 // rows without a finite lse, columns beyond the rows, or keys that are not there hold.
@@ -68,6 +69,10 @@ __device__ __forceinline__ Request request_of(const Params &P, int b)
 __device__ __forceinline__ int column_of(const Params &P, int key) { return (int)((__umulhi(P.block_mul, (unsigned)key) + (unsigned)key) >> P.block_shift); }
 __device__ __forceinline__ int node_of(const Params &P, int row) { return (int)((__umulhi(P.group_mul, (unsigned)row) + (unsigned)row) >> P.group_shift); }
 
+// A unit's length: two tiles that go together take some 1.5 times as long as one (8 requests of 19 nodes: 3500 cycles a head to 2200; stretches of 512 nodes:
+// 49000 to 31000).
+__device__ __forceinline__ int length_of(int count) { return count == 2 ? 3 : 2; }
+__device__ __forceinline__ int length_of(const Request &r) { return 2 * r.tiles() - r.pairs(); }         // of all a request's groups, for a head
 // What a CTA has next: heads of a group; every role counts for itself.
 struct Run {
     int b, t, h, left, next_at;                // the next unit: request, tiles of it gone by, head; length of the run from there on, and its place
@@ -84,32 +89,34 @@ struct Run {
         tile = r.first() + t;
         count = t < 2 * r.pairs() ? 2 : 1;
         h0 = h;
-        h1 = min(P.Hkv, h0 + (left + count - 1) / count);
+        const int each = length_of(count);
+        h1 = min(P.Hkv, h0 + (int)((unsigned)(left + each - 1) / (unsigned)each));
         at = next_at;
-        left -= (h1 - h0) * count;
-        next_at += (h1 - h0) * count;
+        left -= (h1 - h0) * each;
+        next_at += (h1 - h0) * each;
         h = h1;
         if (h == P.Hkv) { h = 0; t += count; }
         return true;
     }
 };
 
+constexpr int SR = 8;                          // blocks of queries whose references are on chip: their products read them, the sums' warps these
 template <int D_> struct Shape {
     static constexpr int D = D_, PANELS = D / 64, QB = D == 256 ? 64 : 128;       // rows of a block of queries
     static constexpr int K_SLOT = KT * D * 2, Q_SLOT = QB * D * 2;
     static constexpr int SK = D == 64 ? 6 : D == 128 ? 3 : 2, SQ = D == 64 ? 4 : D == 128 ? 3 : 2;
     static constexpr int off_q = SK * K_SLOT, off_mask = off_q + SQ * Q_SLOT;
-    static constexpr int off_ref = off_mask + SPEC_MAX_NODES * 16;                // [SQ][128] -lse log2 e
-    static constexpr int off_node = off_ref + SQ * 128 * 4;                       // [SQ][128] nodes of the columns
-    static constexpr int off_parent = off_node + SQ * 128 * 2;
-    static constexpr int off_part = off_parent + SPEC_MAX_NODES * 2;              // [2][2][128] the other warpgroup's sums
-    static constexpr int off_bar = off_part + 2048;
+    static constexpr int off_ref = off_mask + SPEC_MAX_NODES * 16;                // [SR][128] -lse log2 e
+    static constexpr int off_node = off_ref + SR * 128 * 4;                       // [SR][128] nodes of the columns
+    static constexpr int off_parent = off_node + SR * 128 * 2;
+    static constexpr int off_part = off_parent + SPEC_MAX_NODES * 2;              // [2][4][2][128] the warpgroups' sums
+    static constexpr int off_bar = off_part + 8192;
     static constexpr int total = off_bar + 512;
     static_assert(total + 1024 <= 227 * 1024, "shared memory");
 };
-constexpr int SUM_WARPS = 8, PRODUCTS = SUM_WARPS, KEYS = PRODUCTS + 2, QUERIES = KEYS + 4, NT = (QUERIES + 2) * 32;      // the roles' first warps
+constexpr int SUM_WARPS = 16, WG = SUM_WARPS / 4, SUMS = SUM_WARPS * 32, PRODUCTS = SUM_WARPS, KEYS = PRODUCTS + 2, QUERIES = KEYS + 4, NT = (QUERIES + 2) * 32;      // the roles' first warps
 struct Bars {
-    uint64_t k_full[6], k_empty[6], q_full[4], q_empty[4], s_full[4], s_empty[4];
+    uint64_t k_full[6], k_empty[6], q_full[4], q_empty[4], s_full[4], s_empty[4], r_full[SR], r_empty[SR];
     uint32_t tmem;
     int dead, found[2], sums[20];
     Request request;                           // the one that the run begins in
@@ -139,7 +146,7 @@ __device__ __forceinline__ void find_run(const Params &P, int c, Bars *S, Run *r
     const int per = (P.B + NT - 1) / NT, b0 = min(P.B, tid * per), b1 = min(P.B, b0 + per);
     int mine = 0;
     Request only = {};                         // (at most one request to a thread: it is looked up once)
-    for (int b = b0; b < b1; ++b) { only = request_of(P, b); mine += only.tiles() * P.Hkv; }
+    for (int b = b0; b < b1; ++b) { only = request_of(P, b); mine += length_of(only) * P.Hkv; }
     int incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -162,7 +169,7 @@ __device__ __forceinline__ void find_run(const Params &P, int c, Bars *S, Run *r
     if (start >= ahead && start < ahead + mine) {
         for (int b = b0; b < b1; ++b) {
             if (per > 1) only = request_of(P, b);
-            const int t = only.tiles() * P.Hkv;
+            const int t = length_of(only) * P.Hkv;
             if (start < ahead + t) { S->found[0] = b; S->found[1] = start - ahead; S->request = only; break; }
             ahead += t;
         }
@@ -173,60 +180,60 @@ __device__ __forceinline__ void find_run(const Params &P, int c, Bars *S, Run *r
     run->left = run->b < P.B ? each + (c < more) : 0;
     // the place in the request: the first unit that begins there or behind
     run->next_at = start;
-    int at = S->found[1], pairs = run->b < P.B ? run->r.pairs() * 2 * P.Hkv : 0;
-    if (at < pairs) {
-        const int g = (int)((unsigned)at / (2u * P.Hkv)), in = at - g * 2 * P.Hkv;
-        run->t = 2 * g; run->h = (in + 1) / 2;
-        run->left -= in & 1;
-        run->next_at += in & 1;
-    } else {
-        at -= pairs;
-        const int g = (int)((unsigned)at / (unsigned)P.Hkv);
-        run->t = (run->b < P.B ? 2 * run->r.pairs() : 0) + g; run->h = at - g * P.Hkv;
-    }
-    if (run->h == P.Hkv) { run->h = 0; run->t += 2; }
+    int at = S->found[1];
+    const int n_pairs = run->b < P.B ? run->r.pairs() : 0, paired = n_pairs * length_of(2) * P.Hkv, in_pairs = at < paired, each_unit = length_of(in_pairs ? 2 : 1);
+    at -= in_pairs ? 0 : paired;
+    const int units = (int)((unsigned)(at + each_unit - 1) / (unsigned)each_unit), g = (int)((unsigned)units / (unsigned)P.Hkv), past = units * each_unit - at;
+    run->left -= past;
+    run->next_at += past;
+    run->t = in_pairs ? 2 * g : 2 * n_pairs + g;
+    run->h = units - g * P.Hkv;
     cuts->all = all; cuts->each = each; cuts->more = more;
 }
 
-// What a key gets of 32 columns of scores (of the first `columns`; more than 16 or not): sum 2^(c s + ref), ref -lse log2 e or -inf.  Three pairs of
-// eight go without the special function unit, which is what the others wait for (16 a cycle on an SM).
+// What a key gets of 16 columns of scores: sum 2^(c s + ref), ref -lse log2 e or -inf.  BOUND: what is no number adds nothing.
+template <bool BOUND> __device__ __forceinline__ float sixteen(const uint32_t *s, unsigned long long c2, const float *ref)
+{
+    unsigned long long sum[2] = {0ull, 0ull};
+#pragma unroll
+    for (int k = 0; k < 16; k += 4) {
+        const float4 r4 = *(const float4 *)(ref + k);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float x, y;
+            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[k + 2 * i]), __uint_as_float(s[k + 2 * i + 1])), c2,
+                                   i ? pack_f32x2(r4.z, r4.w) : pack_f32x2(r4.x, r4.y)), x, y);
+            sum[i] = add_f32x2(sum[i], BOUND ? pack_f32x2(ex2_approx(fmaxf(x, -200.f)), ex2_approx(fmaxf(y, -200.f))) : pack_f32x2(ex2_approx(x), ex2_approx(y)));
+        }
+    }
+    float x, y;
+    unpack_f32x2(add_f32x2(sum[0], sum[1]), x, y);
+    return x + y;
+}
+// The same of 32 columns, the first `columns` of which are rows' (more than 16 or not).  The exponentials are what the rest waits for (16 a cycle on an SM); the
+// bound that takes NaN out is one instruction more for each, so it is applied where the sum came to NaN only.
 __device__ __forceinline__ float weights_of(uint32_t (&s)[32], unsigned long long c2, const float *ref, int columns, bool masked, const uint4 *mask,
                                             const unsigned short *nodes, int quad, int lane)
 {
     if (masked) {
+        // a lane for a column: what its node sees of the warp's 32 keys.  All of them for most columns of a stretch of a prompt, or none.
+        const uint32_t word = lane < columns ? ((const uint32_t *)(mask + nodes[lane]))[quad] : 0xFFFFFFFFu;
+        if (__all_sync(0xffffffffu, word == 0u || lane >= columns)) return 0.f;
+        if (!__all_sync(0xffffffffu, word == 0xFFFFFFFFu)) {
 #pragma unroll
-        for (int k = 0; k < 32; ++k) {
-            const uint32_t word = ((const uint32_t *)(mask + nodes[k]))[quad];
-            if (!((word >> lane) & 1u)) s[k] = 0xFF800000u;
-        }
-    }
-    unsigned long long sum[2] = {0ull, 0ull};
-    const auto some = [&](int k0) {
-#pragma unroll
-        for (int j = 0; j < 16; j += 4) {
-            const int k = k0 + j;
-            const float4 r4 = *(const float4 *)(ref + k);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const unsigned long long y2 = fma_f32x2(pack_f32x2(__uint_as_float(s[k + 2 * i]), __uint_as_float(s[k + 2 * i + 1])), c2,
-                                                        i ? pack_f32x2(r4.z, r4.w) : pack_f32x2(r4.x, r4.y));
-                float x, y;
-                unpack_f32x2(y2, x, y);
-                const int pair = (j / 2 + i) % 8;
-                if (pair == 2 || pair == 5 || pair == 7) {
-                    // (no more than 2^127: only a lse that is not that of the scores could ask for it)
-                    sum[i] = add_f32x2(sum[i], attend::exp2_pair(pack_f32x2(fminf(fmaxf(x, -127.f), 127.f), fminf(fmaxf(y, -127.f), 127.f))));
-                } else {
-                    sum[i] = add_f32x2(sum[i], pack_f32x2(ex2_approx(fmaxf(x, -200.f)), ex2_approx(fmaxf(y, -200.f))));
-                }
+            for (int k = 0; k < 32; ++k) {
+                const uint32_t w = __shfl_sync(0xffffffffu, word, k);
+                if (!((w >> lane) & 1u)) s[k] = 0xFF800000u;
             }
         }
-    };
-    some(0);
-    if (columns > 16) some(16);
-    float x, y;
-    unpack_f32x2(add_f32x2(sum[0], sum[1]), x, y);
-    return x + y;
+    }
+    float got = sixteen<false>(s, c2, ref);
+    if (columns > 16) got += sixteen<false>(s + 16, c2, ref + 16);
+    if (__any_sync(0xffffffffu, got != got)) {
+        got = sixteen<true>(s, c2, ref);
+        if (columns > 16) got += sixteen<true>(s + 16, c2, ref + 16);
+    }
+    return got;
 }
 
 template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_weigh_kernel(const __grid_constant__ Params P)
@@ -242,8 +249,9 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
     }
     if (tid == 0) {
         for (int i = 0; i < S::SK; ++i) { mbar_init(&B->k_full[i], 128); mbar_init(&B->k_empty[i], 2); }
-        for (int i = 0; i < S::SQ; ++i) { mbar_init(&B->q_full[i], 128); mbar_init(&B->q_empty[i], 2 + SUM_WARPS); }
-        for (int i = 0; i < 4; ++i) { mbar_init(&B->s_full[i], 1); mbar_init(&B->s_empty[i], SUM_WARPS); }
+        for (int i = 0; i < S::SQ; ++i) { mbar_init(&B->q_full[i], 128); mbar_init(&B->q_empty[i], 2); }
+        for (int i = 0; i < SR; ++i) { mbar_init(&B->r_full[i], 64); mbar_init(&B->r_empty[i], 8); }
+        for (int i = 0; i < 4; ++i) { mbar_init(&B->s_full[i], 1); mbar_init(&B->s_empty[i], 4); }
         B->dead = 0;
         mbar_fence_init();
     }
@@ -286,45 +294,57 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
             if (tree_of != run.b) {
                 bool bad = false;
                 const int *row = P.tree.parent + (long long)run.b * P.tree.topo_seq_stride;
-                bar_sync(1, 256);
-                for (int i = tid; i < r.n; i += 256) {
+                bar_sync(1, SUMS);
+                for (int i = tid; i < r.n; i += SUMS) {
                     const int p = __ldg(row + i);
                     const bool wrong = i == 0 ? p != -1 : p < 0 || p >= i;
                     parent[i] = wrong || i == 0 ? (unsigned short)0xFFFF : (unsigned short)p;
                     bad |= wrong;
                 }
                 part[tid] = __int_as_float(bad ? 1 : 0);
-                bar_sync(1, 256);
+                bar_sync(1, SUMS);
                 int x = 0;
-                for (int i = lane; i < 256; i += 32) x |= __float_as_int(part[i]);
+                for (int i = lane; i < SUMS; i += 32) x |= __float_as_int(part[i]);
                 sound = __any_sync(0xffffffffu, x) == 0;
                 tree_of = run.b;
-                bar_sync(1, 256);
+                bar_sync(1, SUMS);
             }
             const bool masked = (long long)(run.tile + 1) * KT > r.len;            // (then the tile goes by itself)
             if (masked) {
                 // what each node sees of the tile: itself and its ancestors, by doubling, and all committed tokens
                 const long long a = (long long)run.tile * KT;
-                constexpr int MINE = SPEC_MAX_NODES / 256;
+                constexpr int MINE = SPEC_MAX_NODES / SUMS;
                 int up[MINE];
                 uint4 m[MINE];
 #pragma unroll
                 for (int x = 0; x < MINE; ++x) {
-                    const int i = x * 256 + tid;
+                    const int i = x * SUMS + tid;
                     m[x] = make_uint4(0, 0, 0, 0);
                     up[x] = 0xFFFF;
                     if (i >= r.n) continue;
-                    up[x] = parent[i];
-                    const long long at = (long long)r.len + i - a;
-                    uint32_t bits[4];
+                    // (32 steps up by itself: all the way in a draft tree)
+                    uint32_t bits[4] = {0u, 0u, 0u, 0u};
+                    int node = i;
+                    for (int step = 0; step <= 32 && node != 0xFFFF; ++step) {
+                        const long long at = (long long)r.len + node - a;
+                        if (at < 0) { node = 0xFFFF; break; }
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) bits[k] = at >= 32 * k && at < 32 * k + 32 ? 1u << (at & 31) : 0u;
+                        for (int k = 0; k < 4; ++k) bits[k] |= at >> 5 == k ? 1u << (at & 31) : 0u;
+                        node = parent[node];
+                    }
+                    up[x] = node;
                     m[x] = make_uint4(bits[0], bits[1], bits[2], bits[3]);
                     mask[i] = m[x];
                 }
                 unsigned short *above = parent;
-                bar_sync(1, 256);
-                for (int span = 1; span < r.n; span <<= 1) {
+                bar_sync(1, SUMS);
+                if (r.n > 33) {
+#pragma unroll
+                    for (int x = 0; x < MINE; ++x)
+                        if (x * SUMS + tid < r.n) above[x * SUMS + tid] = (unsigned short)up[x];
+                    bar_sync(1, SUMS);
+                }
+                for (int span = 33; span < r.n; span <<= 1) {
                     uint4 more[MINE];
                     int further[MINE];
 #pragma unroll
@@ -333,71 +353,76 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
                         further[x] = up[x];
                         if (up[x] != 0xFFFF) { more[x] = mask[up[x]]; further[x] = above[up[x]]; }
                     }
-                    bar_sync(1, 256);
+                    bar_sync(1, SUMS);
 #pragma unroll
                     for (int x = 0; x < MINE; ++x) {
-                        const int i = x * 256 + tid;
+                        const int i = x * SUMS + tid;
                         if (i >= r.n) continue;
                         m[x].x |= more[x].x; m[x].y |= more[x].y; m[x].z |= more[x].z; m[x].w |= more[x].w;
                         up[x] = further[x];
                         mask[i] = m[x];
                         above[i] = (unsigned short)up[x];
                     }
-                    bar_sync(1, 256);
+                    bar_sync(1, SUMS);
                 }
-                tree_of = -1;                                        // (the parents have been used up)
+                if (r.n > 33) tree_of = -1;                          // (the parents have been used up)
                 uint32_t all[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) all[k] = attend::bits_of(a + 32 * k, 0, r.len);
 #pragma unroll
                 for (int x = 0; x < MINE; ++x) {
-                    const int i = x * 256 + tid;
+                    const int i = x * SUMS + tid;
                     if (i < r.n) mask[i] = make_uint4(m[x].x | all[0], m[x].y | all[1], m[x].z | all[2], m[x].w | all[3]);
                 }
-                bar_sync(1, 256);
+                bar_sync(1, SUMS);
             }
             float acc0 = 0.f, acc1 = 0.f;
             for (int h = run.h0; h < run.h1; ++h)
-                for (int qb = 0; qb < blocks; ++qb, ++n_q) {
-                    const uint32_t qs = n_q % S::SQ;
-                    const int columns = min(S::QB, rows - qb * S::QB);
-                    wait(B, &B->q_full[qs], n_q / S::SQ & 1);
-                    const float *ref = (const float *)(base + S::off_ref) + qs * 128;
-                    const unsigned short *nodes = (const unsigned short *)(base + S::off_node) + qs * 128;
+                for (int qb = 0; qb < blocks; ++qb, ++n_q)
                     for (int ti = 0; ti < run.count; ++ti, ++n_s) {
-                        const uint32_t buf = n_s & 3;
-                        wait(B, &B->s_full[buf], n_s >> 2 & 1);
+                        if ((int)(n_s % WG) != w) continue;
+                        const uint32_t rs = n_q % SR;
+                        wait(B, &B->s_full[w], n_s / WG & 1);
                         tc::fence_after();
-                        // the warpgroups take groups of 32 columns in turn, the first of a tile now the one, now the other
+                        // (the references are there, as the product is; a barrier that this warp does not see every filling of is not waited for ahead of that)
+                        wait(B, &B->r_full[rs], n_q / SR & 1);
+                        const float *ref = (const float *)(base + S::off_ref) + rs * 128;
+                        const unsigned short *nodes = (const unsigned short *)(base + S::off_node) + rs * 128;
+                        const int columns = min(S::QB, rows - qb * S::QB);
                         float got = 0.f;
 #pragma unroll 1
-                        for (int g = ((w + n_s) & 1) * 32; g < columns; g += 64) {
+                        for (int g = 0; g < columns; g += 32) {
                             uint32_t x[32];
-                            tc::tmem_load(lanes + buf * 128 + g, x);
+                            tc::tmem_load(lanes + w * 128 + g, x);
                             tc::wait_loads(x);
+                            if (g + 32 >= columns) {                                       // (the next product may come while these are at work)
+                                tc::fence_before();
+                                __syncwarp();
+                                if (lane == 0) mbar_arrive(&B->s_empty[w]);
+                            }
                             got += weights_of(x, c2, ref + g, columns - g, masked, mask, nodes + g, quad, lane);
                         }
-                        tc::fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&B->s_empty[buf]);
                         if (ti == 0) acc0 += got; else acc1 += got;
+                        __syncwarp();
+                        if (lane == 0) tc::arrive_many(&B->r_empty[rs], 3 - run.count);    // (two products to a block of queries: a warp arrives once for each)
                     }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&B->q_empty[qs]);
-                }
-            // each warpgroup finishes a tile, with what the other has of it
-            float *mail = part + (n_step & 1) * 256;
-            mail[(1 - w) * 128 + mine] = w ? acc0 : acc1;
-            bar_sync(1, 256);
-            const float got = (w ? acc1 : acc0) + mail[w * 128 + mine];
+            // the first warpgroups finish a tile each, with what the others have of it
+            float *mail = part + (n_step & 1) * (WG * 256);
+            mail[w * 256 + mine] = acc0;
+            mail[w * 256 + 128 + mine] = acc1;
+            bar_sync(1, SUMS);
+            float got = 0.f;
+            if (w < run.count)
+#pragma unroll
+                for (int k = 0; k < WG; ++k) got += mail[k * 256 + w * 128 + mine];
             if (slot >= 0 && sound && *(volatile int *)&B->dead == 0) __stcg(P.weights + slot, old + got);
             if (!whole) {
                 const int c = blockIdx.x, place = n_step == 0 ? 0 : 1;
-                __stcg(P.part + ((c * 2 + place) * 2 + w) * 128 + mine, got);
+                if (w < 2) __stcg(P.part + ((c * 2 + place) * 2 + w) * 128 + mine, got);
                 if (run.h0 == 0 && sound) {
                     // the CTA that has a group's first heads tells what there is to join: runs that begin ahead of the group's last unit's end have one
                     // of its units (or are shorter than that and have none at all)
-                    const int last = run.at + (P.Hkv - 1) * run.count;
+                    const int last = run.at + (P.Hkv - 1) * length_of(run.count);
                     int parts = 1;
                     while (c + parts < P.ctas && cuts.start(c + parts) <= last) ++parts;
                     joint = make_int4(run.b, run.tile, run.count, parts << 1 | place);
@@ -405,7 +430,8 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
             }
         }
         // (a run without a unit: its part of whatever group is 0)
-        if (n_step == 0) __stcg(P.part + blockIdx.x * 512 + tid, 0.f), __stcg(P.part + blockIdx.x * 512 + 256 + tid, 0.f);
+        if (n_step == 0) __stcg(P.part + blockIdx.x * 512 + tid, 0.f);
+        static_assert(SUMS == 512, "a thread for an entry of the CTA's parts");
         if (tid == 0) P.joint[blockIdx.x] = joint;
     } else if (warp < KEYS) {
         // ---------------------------------------------------------------- products: two warps in turn, one thread of each issues (a product's 8 instructions,
@@ -423,7 +449,8 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
                     const int columns = (min(S::QB, rows - qb * S::QB) + 15) / 16 * 16;
                     const uint32_t desc = tc::product_desc(attend::Pair<T>::TYPE, columns, false);
                     wait(B, &B->q_full[qs], n_q / S::SQ & 1);
-                    if (lane == 0) mbar_arrive(&B->q_empty[qs]);          // (the sums' warps let go of it when its products are done)
+                    const bool has = run.count == 2 || (int)(n_s & 1) == mine;
+                    if (!has && lane == 0) mbar_arrive(&B->q_empty[qs]);
                     for (int ti = 0; ti < run.count; ++ti, ++n_s) {
                         const uint32_t ks = (n_k + ti) % S::SK, buf = n_s & 3;
                         if (qb == 0) wait(B, &B->k_full[ks], (n_k + ti) / S::SK & 1);
@@ -440,6 +467,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
                                 for (int i = 0; i < 4; ++i) tc::mma_ss(tmem + buf * 128, kd + 2 * i, qd + 2 * i, desc, p > 0 || i > 0);
                             }
                             tc::commit(&B->s_full[buf]);
+                            tc::commit(&B->q_empty[qs]);
                         }
                         __syncwarp();
                     }
@@ -538,10 +566,21 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
                     const float ref[2] = {ahead[0], ahead[1]};
 #pragma unroll
                     for (int x = 0; x < 2; ++x) ahead[x] = qb + 1 < blocks ? reference(h, qb + 1, x) : reference(h + 1, 0, x);
-                    if (n_q >= S::SQ) wait(B, &B->q_empty[slot], (n_q / S::SQ - 1) & 1);
+                    const uint32_t rs = n_q % SR;
+                    if (n_q >= SR) wait(B, &B->r_empty[rs], (n_q / SR - 1) & 1);
                     __syncwarp();
                     if (stopped(B)) continue;
                     if (c_hold_slot >= 0 && c_hold_slot / P.tree.N == run.b) continue;       // (a test may ask for a request's queries to stay away)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int in = which * 64 + x * 32 + lane;
+                        refs[rs * 128 + in] = ref[x];
+                        nodes[rs * 128 + in] = (unsigned short)node_of(P, min(qb * S::QB + in, rows - 1));
+                    }
+                    mbar_arrive(&B->r_full[rs]);
+                    if (n_q >= S::SQ) wait(B, &B->q_empty[slot], (n_q / S::SQ - 1) & 1);
+                    __syncwarp();
+                    if (stopped(B)) continue;
                     const int columns = min(S::QB, rows - qb * S::QB);
                     if (P.q_nodes && which == 0) {
                         // (rows behind the tree's come as zeros, those behind the box as they are: columns that nobody counts)
@@ -554,9 +593,9 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
                         }
                         __syncwarp();
                     }
-                    for (int x = 0; x < 2; ++x) {
+                    for (int x = 0; x < 2 && !P.q_nodes; ++x) {
                         const int first = which * 64 + x * 32, mine = min(qb * S::QB + first + lane, rows - 1), node = node_of(P, mine);
-                        if (!P.q_nodes && first < (columns + 15) / 16 * 16) {
+                        if (first < (columns + 15) / 16 * 16) {
                             const T *q = (const T *)P.q + run.b * P.q_stride[0] + (long long)h * P.G * P.q_stride[2];
                             const uint32_t to = q_at + slot * S::Q_SLOT;
                             const unsigned long long from = (unsigned long long)(q + node * P.q_stride[1] + (mine - node * P.G) * P.q_stride[2]);
@@ -567,8 +606,6 @@ template <typename T, typename S> __global__ void __launch_bounds__(NT, 1) spec_
                                 tc::copy16(to + ch / 8 * (S::QB * 128) + at * 128 + (((ch & 7) ^ (at & 7)) << 4), f + ch * 16, at < columns ? 16 : 0);
                             }
                         }
-                        refs[slot * 128 + first + lane] = ref[x];
-                        nodes[slot * 128 + first + lane] = (unsigned short)node;
                     }
                     tc::arrive_with_copies(&B->q_full[slot]);
                     mbar_arrive(&B->q_full[slot]);
