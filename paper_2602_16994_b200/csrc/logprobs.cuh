@@ -21,15 +21,16 @@ namespace specv {
 namespace logp {
 
 constexpr int NT = 256, WARPS = NT / 32, BATCH = 4, SEGS = 4, ROOM = 512, CMAX = 16;
+constexpr int STAGES = 3, RING = STAGES * BATCH * NT * 16;             // a thread's batches on their way, in shared memory (no barrier: it reads its own)
 constexpr float LOW = -3.0e38f;                        // stands for -inf where 0 times it has to be 0
 
 struct Params {
-    int B, N, V, K, top, C;
+    int B, N, V, K, top, C, step;                      // step: places on a path that are gone through at once
     const void *logits;
     long long seq_stride, node_stride;
     const int *parent, *accepted, *token;
     long long topo_seq_stride;
-    float c, T;                                        // log2(e) / T, T
+    float c, T, room;                                  // log2(e) / T, T, 8 / c
     float *logprob, *entropy, *top_logprobs;
     int *top_tokens, *status;
 };
@@ -101,11 +102,9 @@ template <> struct Chunk<__half> {
     }
 };
 
-__device__ __forceinline__ uint4 load_once(const uint4 *p)
+__device__ __forceinline__ void copy_chunk(uint32_t to, const uint4 *from)
 {
-    uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 
 // a candidate, larger is better: the logit's order, then the lower index
@@ -125,12 +124,13 @@ struct Shared {
     Sums sums;
     unsigned long long best[SPEC_MAX_TOP];             // 0: none
     unsigned long long found[ROOM + SPEC_MAX_TOP > CMAX * SPEC_MAX_TOP ? ROOM + SPEC_MAX_TOP : CMAX * SPEC_MAX_TOP];
-    float maxima[NT];
+    __align__(16) float maxima[NT];
     float stretch[SEGS][NT];
     unsigned short units[SEGS * NT];
     double warp_S[WARPS], warp_U[WARPS];
     float warp_m[WARPS];
-    int count, n_units, row, why;
+    int count, n_units, depth, why;
+    unsigned short path[SPEC_MAX_NODES];
     float bound;
     int warp_count[WARPS];
 };
@@ -147,6 +147,7 @@ __device__ __forceinline__ void order(Shared *S, int n, int top, int tid)
     for (int i = tid; i < n; i += NT) {
         const unsigned long long x = S->found[i];
         int before = 0;
+#pragma unroll 8
         for (int j = 0; j < n; ++j) before += S->found[j] > x;
         if (before < top && x) S->best[before] = x;
     }
@@ -160,42 +161,45 @@ template <typename T> __global__ void __launch_bounds__(NT, 3) spec_logprobs_ker
     __shared__ Shared sh;
     Shared *S = &sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, C = P.C;
-    const int rank = C > 1 ? (int)cluster_ctarank() : 0, out = (int)(blockIdx.x / (unsigned)C), b = out / P.N, i = out - b * P.N;
+    const int rank = C > 1 ? (int)cluster_ctarank() : 0, row_of_grid = (int)(blockIdx.x / (unsigned)C);
+    // (along paths the roots' rows come first, then those below: the rows that there are ahead of those that there are not)
+    const int b = P.parent ? row_of_grid % P.B : row_of_grid / P.N, i0 = P.parent ? row_of_grid / P.B : row_of_grid - b * P.N;
     grid_dependency_wait();
-    // ---- which row
-    int node = i, why = SPEC_DEV_OK;
     if (P.parent) {
+        // the path: the parents on chip (they may be as many as fit the ring), then one thread goes up
+        int *up = (int *)dyn_smem;
+        const int *parent = P.parent + (long long)b * P.topo_seq_stride;
+        for (int x = tid; x < P.N; x += NT) up[x] = __ldg(parent + x);
+        const int acc = __ldg(P.accepted + b);
+        __syncthreads();
         if (tid == 0) {
-            const int *parent = P.parent + (long long)b * P.topo_seq_stride;
-            const int acc = __ldg(P.accepted + b);
             int depth = 0, at = acc, bad = acc < -1 || acc >= P.N;
             if (!bad) {
                 for (; at > 0; ++depth) {
-                    const int up = __ldg(parent + at);
-                    if (up < 0 || up >= at) { bad = 1; break; }
-                    at = up;
+                    const int above = up[at];
+                    if (above < 0 || above >= at) { bad = 1; break; }
+                    at = above;
                 }
-                bad |= acc >= 0 && __ldg(parent) != -1;
+                bad |= acc >= 0 && up[0] != -1;
             }
-            int row = -1;
-            if (!bad && acc >= 0 && i <= depth) {
-                row = acc;
-                for (int d = depth; d > i; --d) row = __ldg(parent + row);
-            }
-            S->row = row;
+            S->depth = bad ? -1 : acc < 0 ? -1 : depth;
             S->why = bad ? SPEC_DEV_TOPOLOGY : SPEC_DEV_OK;
+            if (!bad && acc >= 0)
+                for (int d = depth, node = acc; d >= 0; --d, node = up[node]) S->path[d] = (unsigned short)node;
         }
         __syncthreads();
-        node = S->row;
-        why = S->why;
     }
+    for (int i = i0; i < P.N; i += P.step) {
+    const int out = b * P.N + i;
+    const int node = !P.parent ? i : i <= S->depth ? S->path[i] : -1, why = P.parent ? S->why : SPEC_DEV_OK;
+    __syncthreads();                                   // (what the row before left in shared memory has been read)
     if (node < 0) {                                    // (all CTAs of the cluster alike)
         if (rank == 0) {
             for (int k = tid; k < P.K; k += NT) P.logprob[(long long)out * P.K + k] = 0.f;
             for (int k = tid; k < P.top; k += NT) { P.top_tokens[(long long)out * P.top + k] = -1; P.top_logprobs[(long long)out * P.top + k] = 0.f; }
             if (tid == 0) { P.entropy[out] = 0.f; P.status[out] = why; }
         }
-        return;
+        continue;
     }
     const T *row = (const T *)P.logits + (long long)b * P.seq_stride + (long long)node * P.node_stride;
     // ---- the row in 16-byte chunks, a few entries ahead of them and behind
@@ -207,56 +211,89 @@ template <typename T> __global__ void __launch_bounds__(NT, 3) spec_logprobs_ker
     // the ends go to the first CTA: entry -1: none
     const int edge = rank || tid >= head + tail ? -1 : tid < head ? tid : P.V - tail + tid - head;
 
-    float m = -CUDART_INF_F, ref = 0.f, run = -CUDART_INF_F;
+    // The thread's largest logit m, its reference (behind m by 8 powers of two at most, so that it rarely moves: `over` is where it has to), and the sums about
+    // it.
+    float m = -CUDART_INF_F, ref = 0.f, over = -CUDART_INF_F, run = -CUDART_INF_F;
     bool bad = false;
     unsigned long long s2 = 0ull, u2 = 0ull;
     const unsigned long long c2 = pack_f32x2(P.c, P.c);
-    const auto raise = [&](float to) {                 // a larger maximum: the sums about it
-        const float d = ref - to, f = m == -CUDART_INF_F ? 0.f : ex2_approx(d * P.c);
+    const auto raise = [&](float to) {
+        const float d = ref - to, f = over == -CUDART_INF_F ? 0.f : ex2_approx(d * P.c);
         const unsigned long long f2 = pack_f32x2(f, f), d2 = pack_f32x2(f == 0.f ? 0.f : d, f == 0.f ? 0.f : d);
         u2 = fma_f32x2(fma_f32x2(s2, d2, u2), f2, 0ull);
         s2 = fma_f32x2(s2, f2, 0ull);
-        m = ref = to;
+        ref = to;
+        over = to + P.room;
     };
-    const auto add2 = [&](float x, float y, unsigned long long r2) {
-        const unsigned long long d = add_f32x2(pack_f32x2(x, y), r2);
-        unpack_f32x2(d, x, y);
-        const unsigned long long d2 = pack_f32x2(fmaxf(x, LOW), fmaxf(y, LOW)), y2 = fma_f32x2(d2, c2, 0ull);
+    // (a masked logit: 0 times -inf where its distance is not bounded)
+    const auto add2 = [&](float x, float y, unsigned long long r2, bool bound) {
+        unsigned long long d2 = add_f32x2(pack_f32x2(x, y), r2);
+        if (bound) {
+            unpack_f32x2(d2, x, y);
+            d2 = pack_f32x2(fmaxf(x, LOW), fmaxf(y, LOW));
+        }
+        const unsigned long long y2 = fma_f32x2(d2, c2, 0ull);
         unpack_f32x2(y2, x, y);
         const unsigned long long e2 = pack_f32x2(ex2_approx(x), ex2_approx(y));
         s2 = add_f32x2(s2, e2);
         u2 = fma_f32x2(e2, d2, u2);
     };
     const uint4 none = make_uint4(X::MASKED, X::MASKED, X::MASKED, X::MASKED);
-    uint4 next[BATCH];
+    uint4 *ring = (uint4 *)dyn_smem;
     const auto fetch = [&](int batch) {
+        if ((batch + 1) * (BATCH * NT) <= n) {
 #pragma unroll
-        for (int j = 0; j < BATCH; ++j) {
-            const int k = (batch * BATCH + j) * NT + tid;
-            next[j] = k < n ? load_once(body + k) : none;
+            for (int j = 0; j < BATCH; ++j)
+                copy_chunk(smem_u32(ring + ((batch % STAGES) * BATCH + j) * NT + tid), body + (batch * BATCH + j) * NT + tid);
+        } else if (batch < batches) {
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) {
+                const int k = (batch * BATCH + j) * NT + tid;
+                uint4 *to = ring + ((batch % STAGES) * BATCH + j) * NT + tid;
+                if (k < n) copy_chunk(smem_u32(to), body + k);
+                else *to = none;
+            }
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    if (batches) fetch(0);
+#pragma unroll
+    for (int g = 0; g < STAGES - 1; ++g) fetch(g);
     for (int g = 0, left = each, seg = 0; g < batches; ++g) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
         uint4 w[BATCH];
 #pragma unroll
-        for (int j = 0; j < BATCH; ++j) w[j] = next[j];
-        if (g + 1 < batches) fetch(g + 1);
+        for (int j = 0; j < BATCH; ++j) w[j] = ring[((g % STAGES) * BATCH + j) * NT + tid];
         uint32_t t = X::MASKED;
 #pragma unroll
         for (int j = 0; j < BATCH; ++j) t = X::top2(t, X::top2(X::top2(w[j].x, w[j].y), X::top2(w[j].z, w[j].w)));
         const float top = X::last(t);
         run = fmaxf(run, top);
+        m = fmaxf(m, top);
         bad |= !(top < CUDART_INF_F);
-        if (top > m) raise(top);
-        const unsigned long long r2 = pack_f32x2(-ref, -ref);
+        if (top > over) raise(top);
+        const unsigned long long r2 = pack_f32x2(-ref, -ref), s_before = s2, u_before = u2;
 #pragma unroll
         for (int j = 0; j < BATCH; ++j) {
             float x[E];
             X::open(w[j], x);
 #pragma unroll
-            for (int e = 0; e < E; e += 2) add2(x[e], x[e + 1], r2);
+            for (int e = 0; e < E; e += 2) add2(x[e], x[e + 1], r2, false);
         }
+        float ux, uy;
+        unpack_f32x2(u2, ux, uy);
+        if (__any_sync(0xffffffffu, !(fabsf(ux + uy) < CUDART_INF_F))) {
+            // masked logits among them: once more, bounded
+            s2 = s_before; u2 = u_before;
+#pragma unroll 1
+            for (int j = 0; j < BATCH; ++j) {
+                float x[E];
+                const uint4 v = ring[((g % STAGES) * BATCH + j) * NT + tid];
+                X::open(v, x);
+#pragma unroll
+                for (int e = 0; e < E; e += 2) add2(x[e], x[e + 1], r2, true);
+            }
+        }
+        fetch(g + STAGES - 1);
         if (--left == 0) { S->stretch[seg++][tid] = run; run = -CUDART_INF_F; left = each; }
         if (g + 1 == batches && left != each) S->stretch[seg][tid] = run;
     }
@@ -264,8 +301,9 @@ template <typename T> __global__ void __launch_bounds__(NT, 3) spec_logprobs_ker
     if (edge >= 0) {
         edge_x = X::one(row[edge]);
         bad |= !(edge_x < CUDART_INF_F);
-        if (edge_x > m) raise(edge_x);
-        add2(edge_x, -CUDART_INF_F, pack_f32x2(-ref, -ref));
+        m = fmaxf(m, edge_x);
+        if (edge_x > over) raise(edge_x);
+        add2(edge_x, -CUDART_INF_F, pack_f32x2(-ref, -ref), true);
     }
     // ---- the CTA's sums
     {
@@ -275,8 +313,8 @@ template <typename T> __global__ void __launch_bounds__(NT, 3) spec_logprobs_ker
         float x, y, p, q;
         unpack_f32x2(s2, x, y);
         unpack_f32x2(u2, p, q);
-        const double d = m == -CUDART_INF_F ? 0.0 : (double)m - (double)top;
-        const float f = m == -CUDART_INF_F ? 0.f : ex2_approx((m - top) * P.c);
+        const double d = m == -CUDART_INF_F ? 0.0 : (double)ref - (double)top;
+        const float f = m == -CUDART_INF_F ? 0.f : ex2_approx((ref - top) * P.c);
         double s = (double)x + (double)y, u = (double)p + (double)q;
         u = f == 0.f ? 0.0 : (u + s * d) * (double)f;
         s *= (double)f;
@@ -289,28 +327,43 @@ template <typename T> __global__ void __launch_bounds__(NT, 3) spec_logprobs_ker
         if (tid < SPEC_MAX_TOP) S->best[tid] = 0ull;
         __syncthreads();
     }
-    const auto join = [&](Sums &a, float m1, double S1, double U1) {
-        if (m1 == -CUDART_INF_F) return;
-        const float top = fmaxf(a.m, m1);
-        const double fa = a.m == -CUDART_INF_F ? 0.0 : (double)ex2_approx((a.m - top) * P.c), fb = (double)ex2_approx((m1 - top) * P.c);
+    // a warp puts the sums of its lanes together (a lane without any: m = -inf)
+    const auto join = [&](float m1, double S1, double U1, bool wrong) {
+        float top = m1;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const double f = m1 == -CUDART_INF_F ? 0.0 : (double)ex2_approx((m1 - top) * P.c);
         // (0 times a distance that is infinite, of parts that are nothing)
-        a.U = (fa == 0.0 ? 0.0 : (a.U + a.S * ((double)a.m - (double)top)) * fa) + (fb == 0.0 ? 0.0 : (U1 + S1 * ((double)m1 - (double)top)) * fb);
-        a.S = a.S * fa + S1 * fb;
+        Sums a;
+        a.U = warp_sum(f == 0.0 ? 0.0 : (U1 + S1 * ((double)m1 - (double)top)) * f);
+        a.S = warp_sum(f == 0.0 ? 0.0 : S1 * f);
         a.m = top;
+        a.bad = __any_sync(0xffffffffu, wrong);
+        return a;
     };
-    if (tid == 0) {
-        Sums a = {0.0, 0.0, -CUDART_INF_F, bad};
-        for (int w = 0; w < WARPS; ++w) join(a, S->warp_m[w], S->warp_S[w], S->warp_U[w]);
-        S->sums = a;
+    if (warp == 0) {
+        const bool has = lane < WARPS;
+        const Sums a = join(has ? S->warp_m[lane] : -CUDART_INF_F, has ? S->warp_S[lane] : 0.0, has ? S->warp_U[lane] : 0.0, bad);
+        if (lane == 0) S->sums = a;
     }
     // ---- the CTA's most probable tokens
     if (P.top && !bad) {                               // (the same for all threads of the CTA)
-        int before = 0;
-        for (int j = 0; j < NT; ++j) {
-            const float x = S->maxima[j];
-            before += x > m || (x == m && j < tid);
+        // One warp looks for the bound, by the upper 16 bits of an order-preserving image of the maxima: the largest that `top` maxima reach.
+        if (warp == WARPS - 1) {
+            uint32_t key[NT / 32], found = 0u;
+#pragma unroll
+            for (int j = 0; j < NT / 32; ++j) key[j] = cut::key_of(S->maxima[j * 32 + lane]) >> 16;
+#pragma unroll 1
+            for (uint32_t bit = 0x8000u; bit; bit >>= 1) {
+                int reach = 0;
+#pragma unroll
+                for (int j = 0; j < NT / 32; ++j) reach += __popc(__ballot_sync(0xffffffffu, key[j] >= (found | bit)));
+                if (reach >= P.top) found |= bit;
+            }
+            // (what has the image of -inf, or of a number below all others, bounds nothing)
+            const float x = cut::value_of(found << 16);
+            if (lane == 0) S->bound = found > 0x007Fu && x == x ? x : -CUDART_INF_F;
         }
-        if (before == P.top - 1) S->bound = m;
         __syncthreads();
         const float bound = S->bound;
         const auto put = [&](float x, int index) {
@@ -425,21 +478,19 @@ template <typename T> __global__ void __launch_bounds__(NT, 3) spec_logprobs_ker
         if (rank == 0) {
             for (int k = tid; k < C * P.top; k += NT) S->found[k] = of_rank(S->best, k / P.top)[k % P.top];
             __syncthreads();                           // (its own list is read before it is written again)
-            if (tid == 0) {
-                Sums a = S->sums;
-                for (int r = 1; r < C; ++r) {
-                    const Sums o = *of_rank(&S->sums, r);
-                    join(a, o.m, o.S, o.U);
-                    a.bad |= o.bad;
-                }
-                S->sums = a;
+            if (warp == 0) {
+                const bool has = lane < C;
+                const Sums o = *of_rank(&S->sums, has ? lane : 0);
+                const Sums a = join(has ? o.m : -CUDART_INF_F, o.S, o.U, has && o.bad);
+                __syncwarp();
+                if (lane == 0) S->sums = a;
             }
             if (tid < SPEC_MAX_TOP) S->best[tid] = 0ull;
             __syncthreads();
             if (P.top) order(S, C * P.top, P.top, tid);
         }
-        cluster_sync_all();                            // (no CTA leaves while the first one reads it)
-        if (rank) return;
+        cluster_sync_all();                            // (no CTA goes on while the first one reads it)
+        if (rank) continue;
     }
     // ---- results
     const Sums a = S->sums;
@@ -463,6 +514,7 @@ template <typename T> __global__ void __launch_bounds__(NT, 3) spec_logprobs_ker
     if (tid == 0) {
         P.entropy[out] = wrong ? CUDART_NAN_F : (float)(log_S - a.U / (a.S * T_d));
         P.status[out] = wrong ? SPEC_DEV_NONFINITE : no_token ? SPEC_DEV_TOKEN : SPEC_DEV_OK;
+    }
     }
 }
 

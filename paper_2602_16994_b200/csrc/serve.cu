@@ -38,19 +38,23 @@ int32_t spec_token_logprobs(const SpecLogprobs *a, void *stream)
     if (!(a->temperature >= 1e-30f && a->temperature <= 1e30f) || a->top < 0 || a->top > SPEC_MAX_TOP || a->top > a->V) return SPEC_ERR_PARAM;
     if (!aligned(a->logits, a->dtype == SPEC_F32 ? 4 : 2)) return SPEC_ERR_UNSUPPORTED;
     const int64_t rows = (int64_t)a->B * a->N;
-    // the largest cluster that leaves every CTA a batch of loads and the chip one wave
+    // the largest cluster that leaves every CTA half a batch of loads and the chip one wave of two CTAs per SM; of the rows along paths some four a sequence
+    // are there
     const int batch = logp::NT * logp::BATCH * (a->dtype == SPEC_F32 ? 4 : 8);
+    const int64_t there = a->parent ? std::min<int64_t>(rows, (int64_t)a->B * 4) : rows;
     int C = 1;
-    while (C < logp::CMAX && a->V > C * batch / 2 && rows * 2 * C <= 148 * 2) C *= 2;
+    while (C < logp::CMAX && a->V > C * batch / 2 && there * 2 * C <= 148 * 2) C *= 2;
     logp::Params p = {};
     p.B = a->B; p.N = a->N; p.V = a->V; p.K = a->K; p.top = a->top; p.C = C;
     p.logits = a->logits; p.seq_stride = a->seq_stride; p.node_stride = a->node_stride;
     p.parent = a->parent; p.accepted = a->accepted_node; p.topo_seq_stride = a->topo_seq_stride; p.token = a->token;
-    p.T = a->temperature; p.c = 1.4426950408889634f / a->temperature;
+    p.T = a->temperature; p.c = 1.4426950408889634f / a->temperature; p.room = 8.f / p.c;
+    // (along paths eight places at once: most end before)
+    p.step = a->parent ? std::min(a->N, 8) : a->N;
     p.logprob = a->logprob; p.entropy = a->entropy; p.top_logprobs = a->top_logprobs; p.top_tokens = a->top_tokens; p.status = a->status;
     const auto go = [&](auto kernel) {
-        const int rc = prepare(kernel, 0, true);
-        return rc ? rc : launch(kernel, dim3((unsigned)(rows * C)), logp::NT, 0, C > 1 ? C : 0, (cudaStream_t)stream, p);
+        const int rc = prepare(kernel, std::max(logp::RING, 48 * 1024 + 1), true);          // (beside the static part)
+        return rc ? rc : launch(kernel, dim3((unsigned)((a->parent ? (int64_t)a->B * p.step : rows) * C)), logp::NT, logp::RING, C > 1 ? C : 0, (cudaStream_t)stream, p);
     };
     return a->dtype == SPEC_F32  ? go(logp::spec_logprobs_kernel<float>)
            : a->dtype == SPEC_F16 ? go(logp::spec_logprobs_kernel<__half>)
