@@ -1,8 +1,8 @@
 // Eviction from a paged cache: the entries of a request that are kept, and their way together (spec_cache_evict).
 //
-// Selection.  Of the M entries between the first p and the last r, the m with the largest weights: the m-th largest is found by its bits (an
-// order-preserving integer image of the weight, four passes of 256 counters), then one walk over the entries in order decides what stays (all above
-// it, and the first of those equal to it) and where it goes.
+// Selection (spec_evict_select_kernel).  Of the M entries between the first p and the last r, the m with the largest weights: the m-th largest is found by its bits (an
+// order-preserving integer image of the weight, four passes of 256 counters), then one walk over the entries in order decides what stays (all above it, and the
+// first of those equal to it) and where it goes.  The request's row of the table and its weights are on chip for all that, up to COLS and KEYS of them.
 //
 // Moves.  The i-th kept entry goes to entry i, in every cache.  It comes from an entry at or behind i, so a CTA that takes kept entries in order, so
 // many at a time, reads all of a batch before it writes any of it, and may read the next batch before: what lies ahead of the last source is
@@ -33,43 +33,39 @@ struct Params {
 };
 
 // ---- selection ----------------------------------------------------------------------------------------------------------------
-constexpr int NT = 1024, WARPS = NT / 32;
+constexpr int NT = 1024, WARPS = NT / 32, COLS = 4096, KEYS = 46 * 1024;         // 16 and 184 KB
 
-__device__ __forceinline__ long long slot_of(const Params &P, const int *table, int entry)       // (entry < the owned columns' end)
-{
-    const unsigned col = (unsigned)entry / (unsigned)P.block;
-    return (long long)__ldg(table + col) * P.block + (entry - (int)col * P.block);
-}
 __device__ __forceinline__ uint32_t weight_key(float w) { return w == w ? cut::key_of(w) : 0u; }
 
-// Exclusive sums of two counts over the CTA, and their totals.
-__device__ __forceinline__ void scan2(int a, int b, int2 *part, int &a_ahead, int &b_ahead, int &a_all, int &b_all)
+// Exclusive sums over the CTA of two counts of at most 1 a thread, and their totals.  part: of this call or of the one before last.
+__device__ __forceinline__ void scan2(bool a, bool b, int *part, int &a_ahead, int &b_ahead, int &a_all, int &b_all)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int x = a, y = b;
+    const unsigned below = (1u << lane) - 1u, all_a = __ballot_sync(0xffffffffu, a), all_b = __ballot_sync(0xffffffffu, b);
+    if (lane == 0) part[warp] = __popc(all_a) | __popc(all_b) << 16;
+    __syncthreads();
+    static_assert(WARPS == 32, "a lane for a warp");
+    int sum = part[lane];
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int s = __shfl_up_sync(0xffffffffu, x, o), t = __shfl_up_sync(0xffffffffu, y, o);
-        if (lane >= o) { x += s; y += t; }
+        const int t = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += t;
     }
-    if (lane == 31) part[warp] = make_int2(x, y);
-    __syncthreads();
-    a_ahead = x - a; b_ahead = y - b; a_all = b_all = 0;
-    for (int w = 0; w < WARPS; ++w) {
-        const int2 p = part[w];
-        if (w < warp) { a_ahead += p.x; b_ahead += p.y; }
-        a_all += p.x; b_all += p.y;
-    }
-    __syncthreads();
+    const int before = warp ? __shfl_sync(0xffffffffu, sum, warp - 1) : 0, total = __shfl_sync(0xffffffffu, sum, 31);
+    a_ahead = (before & 0xFFFF) + __popc(all_a & below); b_ahead = (before >> 16) + __popc(all_b & below);
+    a_all = total & 0xFFFF; b_all = total >> 16;
 }
 
 __global__ void __launch_bounds__(NT) spec_evict_select_kernel(const __grid_constant__ Params P)
 {
-    __shared__ int2 part[WARPS];
+    __shared__ int part[2][WARPS];
     __shared__ int count[256];
     __shared__ int s_digit, s_above, s_first;
     const int tid = threadIdx.x, lane = tid & 31, b = blockIdx.x;
+    int *cols = (int *)dyn_smem;
+    float *held = (float *)(cols + COLS);              // the weight of entry p + i
     grid_dependency_wait();
+    grid_launch_dependents();                          // (the moving kernel waits by itself)
     const int len = __ldg(P.lengths + b), own = __ldg(P.owned + b), budget = P.budget;
     const int p = P.protect ? __ldg(P.protect + b) : 0;
     const int *table = P.table + (long long)b * P.table_stride;
@@ -81,6 +77,7 @@ __global__ void __launch_bounds__(NT) spec_evict_select_kernel(const __grid_cons
             for (int col = tid; col < own; col += NT) {
                 const int id = __ldg(table + col);
                 page |= id < 0 || id >= P.num_blocks;
+                if (col < COLS) cols[col] = id;
             }
     }
     page = __syncthreads_or(page) != 0;
@@ -94,6 +91,24 @@ __global__ void __launch_bounds__(NT) spec_evict_select_kernel(const __grid_cons
         return;
     }
     const int r = min(P.recent, budget - p), end = len - r, m = budget - p - r;      // chosen: m of the entries [p, end)
+    const auto slot_of = [&](int entry) {              // (entry < the owned columns' end)
+        const unsigned col = (unsigned)entry / (unsigned)P.block;
+        return (long long)(col < COLS ? cols[col] : __ldg(table + col)) * P.block + (entry - (int)col * P.block);
+    };
+    for (int j0 = p; j0 < min(len, p + KEYS); j0 += 8 * NT) {
+        float w[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const int j = j0 + x * NT + tid;
+            w[x] = j < min(len, p + KEYS) ? __ldcg(P.weights + slot_of(j)) : 0.f;
+        }
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const int j = j0 + x * NT + tid;
+            if (j < min(len, p + KEYS)) held[j - p] = w[x];
+        }
+    }
+    const auto weight_of = [&](int j) { return j - p < KEYS ? held[j - p] : __ldcg(P.weights + slot_of(j)); };
     // the m-th largest key by its digits; `above`: entries with a larger one
     uint32_t key = 0u;
     int above = 0;
@@ -101,9 +116,18 @@ __global__ void __launch_bounds__(NT) spec_evict_select_kernel(const __grid_cons
         for (int shift = 24; shift >= 0; shift -= 8) {
             if (tid < 256) count[tid] = 0;
             __syncthreads();
-            for (int j = p + tid; j < end; j += NT) {
-                const uint32_t k = weight_key(__ldcg(P.weights + slot_of(P, table, j)));
-                if (shift == 24 || (k >> (shift + 8)) == key >> (shift + 8)) atomicAdd(&count[k >> shift & 255u], 1);
+            // (whole warps go round, so that lanes with the same digit add up ahead of the counter: most weights share a few exponents)
+            for (int j0 = p; j0 < end; j0 += NT) {
+                const int j = j0 + tid;
+                const uint32_t k = j < end ? weight_key(weight_of(j)) : 0u;
+                const bool in = j < end && (shift == 24 || (k >> (shift + 8)) == key >> (shift + 8));
+                const unsigned digit = in ? k >> shift & 255u : 256u;
+                if (shift == 24) {
+                    const unsigned same = __match_any_sync(0xffffffffu, digit);
+                    if (in && lane == __ffs(same) - 1) atomicAdd(&count[digit], __popc(same));
+                } else if (in) {
+                    atomicAdd(&count[digit], 1);
+                }
             }
             __syncthreads();
             if (tid < 32) {                            // the digit in which the count from above reaches m
@@ -141,8 +165,8 @@ __global__ void __launch_bounds__(NT) spec_evict_select_kernel(const __grid_cons
         long long slot = 0;
         float w = 0.f;
         if (j < len) {
-            slot = slot_of(P, table, j);
-            w = __ldcg(P.weights + slot);
+            slot = slot_of(j);
+            w = weight_of(j);
             if (j >= end) larger = true;
             else if (m > 0) {
                 const uint32_t k = weight_key(w);
@@ -151,13 +175,13 @@ __global__ void __launch_bounds__(NT) spec_evict_select_kernel(const __grid_cons
             }
         }
         int a_ahead, e_ahead, a_all, e_all;
-        scan2(larger, equal, part, a_ahead, e_ahead, a_all, e_all);
+        scan2(larger, equal, part[(j0 - p) / NT & 1], a_ahead, e_ahead, a_all, e_all);
         // of the equal ones ahead in this batch, those that still count
         const int room = max(0, equals - same);
         const bool stays = larger || (equal && e_ahead < room);
         const int to = kept + a_ahead + min(e_ahead, room);
         if (stays) {
-            const long long goal = slot_of(P, table, to);
+            const long long goal = slot_of(to);
             moves[to] = make_int2((int)slot, (int)goal);
             if (to != j) {
                 atomicMin(&s_first, to);
@@ -176,7 +200,7 @@ __global__ void __launch_bounds__(NT) spec_evict_select_kernel(const __grid_cons
 }
 
 // ---- moves --------------------------------------------------------------------------------------------------------------------
-constexpr int MOVE_NT = 256, DEPTH = 4;
+constexpr int MOVE_NT = 256;
 
 // The last CTA: freed blocks behind the free ones of the ring, request by request.
 __device__ void refill(const Params &P)
@@ -235,7 +259,8 @@ __device__ void refill(const Params &P)
     }
 }
 
-template <typename W> __global__ void __launch_bounds__(MOVE_NT) spec_evict_move_kernel(const __grid_constant__ Params P)
+// DEPTH: rows of a thread on their way at once: 4 where there are many CTAs (six of them fit an SM), 16 where there are few.
+template <typename W, int DEPTH> __global__ void __launch_bounds__(MOVE_NT) spec_evict_move_kernel(const __grid_constant__ Params P)
 {
     grid_dependency_wait();
     if (blockIdx.x == gridDim.x - 1) {
@@ -254,7 +279,7 @@ template <typename W> __global__ void __launch_bounds__(MOVE_NT) spec_evict_move
     };
     W x[DEPTH];
     int2 way[DEPTH];
-    const auto fetch = [&](int i0) {
+    for (int i0 = first; i0 < budget; i0 += per * DEPTH) {
 #pragma unroll
         for (int k = 0; k < DEPTH; ++k) {
             const int i = i0 + k * per + lane;
@@ -263,10 +288,7 @@ template <typename W> __global__ void __launch_bounds__(MOVE_NT) spec_evict_move
 #pragma unroll
         for (int k = 0; k < DEPTH; ++k)
             if (way[k].x >= 0) x[k] = *(const W *)(base + offset(way[k].x));
-    };
-    for (int i0 = first; i0 < budget; i0 += per * DEPTH) {
-        fetch(i0);
-        __syncthreads();
+        __syncthreads();                               // (all of the batch have their rows)
 #pragma unroll
         for (int k = 0; k < DEPTH; ++k)
             if (way[k].x >= 0) *(W *)(base + offset(way[k].y)) = x[k];

@@ -190,22 +190,26 @@ int32_t spec_cache_evict(const SpecEvict *a, void *ws, int64_t ws_bytes, void *s
     for (int j = 0; j < 3; ++j) { p.stride[j] = a->stride[j]; all |= a->stride[j]; }
     const int unit = all % 16 == 0 ? 16 : all % 4 == 0 ? 4 : 1;
     p.total = (unsigned)(a->row_bytes / unit);
-    // slices of 256 bytes, less where a word is less
+    // Slices of a row: 256 bytes, or fewer, down to 32, where that leaves fewer CTAs than two to an SM (a CTA goes through the kept entries in order).
     p.words = std::min(p.total, 16u);
+    while (p.words > 2 && (int64_t)((p.total + p.words - 1) / p.words) * a->caches * a->B < 148 * 2) p.words /= 2;
     p.slices = (int)((p.total + p.words - 1) / p.words);
     if ((int64_t)p.slices * a->caches + 1 > 0x7FFFFFFF) return SPEC_ERR_UNSUPPORTED;
     const cudaStream_t st = (cudaStream_t)stream;
-    rc = prepare(evict::spec_evict_select_kernel, 0, false);
-    if (!rc) rc = launch(evict::spec_evict_select_kernel, dim3(a->B), evict::NT, 0, 0, st, p);
+    // (a row of the table, and weights of as many entries as a request can have)
+    const int smem = (evict::COLS + (int)std::min<int64_t>(evict::KEYS, (int64_t)a->table_width * a->block_size)) * 4;
+    rc = prepare(evict::spec_evict_select_kernel, (evict::COLS + evict::KEYS) * 4, false);
+    if (!rc) rc = launch(evict::spec_evict_select_kernel, dim3(a->B), evict::NT, smem, 0, st, p);
     if (rc) return rc;
     const dim3 grid((unsigned)(p.slices * a->caches + 1), a->B);
     const auto go = [&](auto kernel) {
         const int e = prepare(kernel, 0, false);
         return e ? e : launch(kernel, grid, evict::MOVE_NT, 0, 0, st, p);
     };
-    return unit == 16  ? go(evict::spec_evict_move_kernel<uint4>)
-           : unit == 4 ? go(evict::spec_evict_move_kernel<uint32_t>)
-                       : go(evict::spec_evict_move_kernel<unsigned char>);
+    const bool few = (int64_t)p.slices * a->caches * a->B < 148 * 4;
+    return unit == 16  ? few ? go(evict::spec_evict_move_kernel<uint4, 16>) : go(evict::spec_evict_move_kernel<uint4, 4>)
+           : unit == 4 ? go(evict::spec_evict_move_kernel<uint32_t, 4>)
+                       : go(evict::spec_evict_move_kernel<unsigned char, 4>);
 }
 
 }  // extern "C"
