@@ -198,11 +198,14 @@ template <bool SH> __device__ __forceinline__ Cuts find_request(const Params &P,
     }
     if (lane == 31) sums[warp] = incl;
     __syncthreads();
-    int ahead = incl - mine, all = 0;
-    for (int w = 0; w < warps; ++w) {
-        if (w < warp) ahead += sums[w];
-        all += sums[w];
+    int upto = lane < warps ? sums[lane] : 0;                      // (at most 32 warps)
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += t;
     }
+    const int before = __shfl_sync(0xffffffffu, upto, max(warp - 1, 0)), all = __shfl_sync(0xffffffffu, upto, 31);
+    int ahead = incl - mine + (warp ? before : 0);
     const Cuts cuts(all, P.ctas);
     const int target = cuts.start(c);
     if (target >= ahead && target < ahead + mine) {
