@@ -127,7 +127,7 @@ struct Shared {
     __align__(16) float maxima[NT];
     float stretch[SEGS][NT];
     unsigned short units[SEGS * NT];
-    double warp_S[WARPS], warp_U[WARPS];
+    double warp_S[WARPS], warp_U[WARPS], log_S;
     float warp_m[WARPS];
     int count, n_units, depth, why;
     unsigned short path[SPEC_MAX_NODES];
@@ -202,6 +202,9 @@ template <typename T> __global__ void __launch_bounds__(NT, 3) spec_logprobs_ker
         continue;
     }
     const T *row = (const T *)P.logits + (long long)b * P.seq_stride + (long long)node * P.node_stride;
+    // (the first given tokens and their logits, asked for ahead of the row)
+    const int my_token = rank == 0 && tid < P.K ? __ldg(P.token + (long long)out * P.K + tid) : -1;
+    const float my_logit = my_token >= 0 && my_token < P.V ? X::one(row[my_token]) : 0.f;
     // ---- the row in 16-byte chunks, a few entries ahead of them and behind
     const int head = min(P.V, (int)((16u - (unsigned)((uintptr_t)row & 15u)) & 15u) / (int)sizeof(T));
     const int chunks = (P.V - head) / E, tail = P.V - head - chunks * E;
@@ -376,17 +379,30 @@ template <typename T> __global__ void __launch_bounds__(NT, 3) spec_logprobs_ker
                 if (wanted(S->stretch[s][tid])) S->units[atomicAdd(&S->n_units, 1)] = (unsigned short)(s * NT + tid);
             if (edge >= 0 && wanted(edge_x)) put(edge_x, edge);
             __syncthreads();
-            for (int u = warp; u < S->n_units; u += WARPS) {
-                const int s = S->units[u] / NT, who = S->units[u] % NT;
-                for (int q = lane; q < each * BATCH; q += 32) {
-                    const int k = (s * each * BATCH + q) * NT + who;
-                    if (k >= n) continue;
-                    const uint4 w = __ldg(body + k);
-                    float x[E];
-                    X::open(w, x);
+            // (four stretches of a warp on their way at once)
+            for (int u0 = warp; u0 < S->n_units; u0 += 4 * WARPS) {
+                for (int q0 = 0; q0 < each * BATCH; q0 += 32) {
+                    uint4 w[4];
+                    int at[4];
 #pragma unroll
-                    for (int e = 0; e < E; ++e)
-                        if (wanted(x[e])) put(x[e], head + (k0 + k) * E + e);
+                    for (int v = 0; v < 4; ++v) {
+                        const int u = u0 + v * WARPS, q = q0 + lane;
+                        at[v] = -1;
+                        w[v] = none;
+                        if (u < S->n_units && q < each * BATCH) {
+                            const int k = (S->units[u] / NT * each * BATCH + q) * NT + S->units[u] % NT;
+                            if (k < n) { at[v] = k; w[v] = __ldg(body + k); }
+                        }
+                    }
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        if (at[v] < 0) continue;
+                        float x[E];
+                        X::open(w[v], x);
+#pragma unroll
+                        for (int e = 0; e < E; ++e)
+                            if (wanted(x[e])) put(x[e], head + (k0 + at[v]) * E + e);
+                    }
                 }
             }
             __syncthreads();
@@ -495,14 +511,16 @@ template <typename T> __global__ void __launch_bounds__(NT, 3) spec_logprobs_ker
     // ---- results
     const Sums a = S->sums;
     const bool wrong = a.bad || a.m == -CUDART_INF_F;
-    const double log_S = wrong ? 0.0 : log(a.S), T_d = (double)P.T;
+    if (tid == 0) S->log_S = wrong ? 0.0 : log(a.S);
+    __syncthreads();
+    const double log_S = S->log_S, T_d = (double)P.T;
     const auto value = [&](float z) { return wrong ? CUDART_NAN_F : (float)(((double)z - (double)a.m) / T_d - log_S); };
     bool no_token = false;
     for (int k = tid; k < P.K; k += NT) {
-        const int token = __ldg(P.token + (long long)out * P.K + k);
+        const int token = k < NT ? my_token : __ldg(P.token + (long long)out * P.K + k);
         float v = 0.f;
         if (token < -1 || token >= P.V) { v = CUDART_NAN_F; no_token = true; }
-        else if (token >= 0) v = value(X::one(row[token]));
+        else if (token >= 0) v = value(k < NT ? my_logit : X::one(row[token]));
         P.logprob[(long long)out * P.K + k] = v;
     }
     for (int k = tid; k < P.top; k += NT) {
