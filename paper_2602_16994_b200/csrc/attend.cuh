@@ -72,6 +72,7 @@ struct Params {
     float2 *whole_ml[2];
     int2 *unit[2];                             // where a unit's parts are: first CTA's slot (-1: in whole), number of them
     int unit_blocks;                           // blocks of rows of a request
+    int merge_rows;                            // rows of a CTA of the joining kernel
 };
 
 // ---- the schedule -------------------------------------------------------------------------------------------------------------

@@ -50,7 +50,7 @@ static int prefix_check(const SpecPrefixAttention *p)
     const double prefix = (double)std::min<int64_t>((int64_t)p->prefix_width * a.block_size, 0x7FFFFFFF);
     const double tiles = a.B * (double)a.Hkv * std::ceil(rows / block) * (keys / attend::KT + 1 + attend::START) +
                          (p->n_groups ? a.Hkv * (p->n_members * rows / block + p->n_groups) * (prefix / attend::KT + 1 + attend::START) : 0.0);
-    if (tiles > 2.0e9 || a.B * rows > 1.0e9) return SPEC_ERR_UNSUPPORTED;
+    if (tiles > 2.0e9 || a.B * rows > 1.0e9 || a.B * (double)a.Hkv * std::ceil(rows / attend::MERGE_ROWS) > 2.0e9) return SPEC_ERR_UNSUPPORTED;
     int64_t all = 0;
     for (int j = 0; j < 3; ++j) all |= a.q_stride[j] | a.k_cache_stride[j] | a.v_cache_stride[j] | a.out_stride[j];
     if (all % 8 || !aligned(a.q, 16) || !aligned(a.k_cache, 16) || !aligned(a.v_cache, 16) || !aligned(a.out, 16)) return SPEC_ERR_UNSUPPORTED;
@@ -127,7 +127,10 @@ int32_t spec_prefix_attention(const SpecPrefixAttention *given, void *ws, int64_
     p.late = (int *)(base + L.late);
     const int64_t rows = (int64_t)a->N * p.G;
     p.unit_blocks = (int)((rows + (two ? 255 : 127)) / (two ? 256 : 128));
-    p.groups = (int)((rows + attend::MERGE_ROWS - 1) / attend::MERGE_ROWS) * a->Hkv;      // CTAs of a request in the joining kernel
+    p.merge_rows = attend::MERGE_ROWS;
+    const auto merging = [&] { return (rows + p.merge_rows - 1) / p.merge_rows * a->Hkv; };         // CTAs of a request in the joining kernel
+    while (p.merge_rows * (a->D / 4) > attend::MERGE_NT && merging() * a->B < 148 * 4) p.merge_rows /= 2;
+    p.groups = (int)merging();
     const bool half = a->dtype == SPEC_F16;
     p.box = a->block_size % 8 ? 0 : a->block_size % 16 ? 8 : a->block_size % 32 ? 16 : 32;
     const int64_t sizes[4] = {a->D, a->Hkv, a->block_size, a->num_blocks};

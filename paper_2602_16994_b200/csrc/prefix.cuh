@@ -12,8 +12,9 @@ namespace attend {
 
 constexpr int MERGE_NT = 128, MERGE_ROWS = 32;
 
-// A CTA per request, key head and MERGE_ROWS rows of that head (in the order of nodes, then heads of the group); a thread has four entries of a row.  Its
-// rows belong to two units of the request's own and two of the prefix at most.
+// A CTA per request, key head and up to MERGE_ROWS rows of that head (in the order of nodes, then heads of the group); a thread has four entries of a row.  Its
+// rows belong to two units of the request's own and two of the prefix at most.  Where that makes few CTAs they have fewer rows, down to one for a thread: a row
+// of a unit that is cut into many parts takes a load's latency for every six of them (3 requests of 18 nodes, D = 256: 89 us with 32 rows).
 template <typename T, typename S> __global__ void __launch_bounds__(MERGE_NT, 8) spec_prefix_join_kernel(const __grid_constant__ Params P)
 {
     constexpr int D = S::D;
@@ -21,10 +22,10 @@ template <typename T, typename S> __global__ void __launch_bounds__(MERGE_NT, 8)
     __shared__ int2 s_unit[2][2];
     const int tid = threadIdx.x, rows = P.tree.N * P.G;
     const int b = (int)(blockIdx.x / (unsigned)P.groups), in = (int)blockIdx.x - b * P.groups, chunks = P.groups / P.Hkv;
-    const int h = (int)((unsigned)in / (unsigned)chunks), row0 = (in - h * chunks) * MERGE_ROWS;
+    const int h = (int)((unsigned)in / (unsigned)chunks), row0 = (in - h * chunks) * P.merge_rows;
     grid_launch_dependents();                  // (the next kernel waits for this one by itself, and this one for the attention)
     // ---- what the inputs alone tell, while the attention still runs
-    const int len = __ldg(P.tree.lengths + b), g_or_none = __ldg(P.group + b), place = __ldg(P.place + b), nn = tree_nodes(P.tree, b);
+    const int len = __ldg(P.tree.lengths + b), g_or_none = __ldg(P.group + b), place = P.n_groups ? __ldg(P.place + b) : 0, nn = tree_nodes(P.tree, b);
     const int n = len < 0 ? 0 : max(nn, 0);
     const int *parent = P.tree.parent + (long long)b * P.tree.topo_seq_stride;
     bool bad = nn < 0 || g_or_none >= P.n_groups || !groups_in_order(P, tid, MERGE_NT);
@@ -53,7 +54,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(MERGE_NT, 8)
             for (int col = tid; col < skip / P.block; col += MERGE_NT) page |= block_in<true>(P, g, 0, col) < 0;
         page = __syncthreads_or(page) != 0;
     }
-    const int upto = min(row0 + MERGE_ROWS, n * P.G), q0 = place * rows;          // rows of nodes that there are; the prefix's row of the request's row 0
+    const int upto = min(row0 + P.merge_rows, n * P.G), q0 = place * rows;          // rows of nodes that there are; the prefix's row of the request's row 0
     grid_dependency_wait();
     if (in == 0) {
         bool late = false;

@@ -73,7 +73,7 @@ static int weights_check(const SpecWeights *a)
     // (tiles of all heads, and steps of a run, are counted in 32 bits)
     const double tiles = ((double)std::min<int64_t>((int64_t)a->table_width * a->block_size, 0x7FFFFFFF) / weigh::KT + 2) * a->Hkv;
     const double steps = ((double)a->N * (a->Hq / a->Hkv)) / 64 + 1;
-    if (a->B * tiles > 2.0e9 || a->B * tiles * steps / 148 > 1.0e9) return SPEC_ERR_UNSUPPORTED;
+    if (a->B * tiles > 1.0e9 || a->B * tiles * steps / 148 > 1.0e9) return SPEC_ERR_UNSUPPORTED;          // (a tile's length is 2)
     int64_t all = 0;
     for (int j = 0; j < 3; ++j) all |= a->q_stride[j] | a->k_cache_stride[j];
     if (all % 8 || !aligned(a->q, 16) || !aligned(a->k_cache, 16)) return SPEC_ERR_UNSUPPORTED;
