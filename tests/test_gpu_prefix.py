@@ -32,7 +32,8 @@ def prefix_case(group, blocks, own, parent, Hq, Hkv, D, dtype=torch.bfloat16, bl
     skip = torch.tensor([blocks[x] if 0 <= x < len(blocks) else 0 for x in group.tolist()], dtype=I32)
     rows = torch.full((B, int(skip.max()) + table.shape[1]), -1, dtype=I32)
     for b in range(B):
-        rows[b, :skip[b]] = prefix[group[b], :skip[b]]
+        if skip[b]:
+            rows[b, :skip[b]] = prefix[group[b], :skip[b]]
         rows[b, skip[b]:skip[b] + table.shape[1]] = table[b]
     lengths = torch.where(own >= 0, own + skip * block, own)
     normal = lambda *s: torch.randn(*s, generator=g).to(dtype)  # noqa: E731

@@ -1,0 +1,152 @@
+"""Shared prefixes, weights, eviction and log probabilities at the ends of their ranges: offsets beyond 32 bits, the most nodes, heads, tokens and
+requests, temperatures at their limits, two calls at once."""
+import math
+
+import pytest
+import torch
+
+from . import serve_ref, step_ref as ref
+from .test_gpu_prefix import check as check_prefix, prefix_case
+from .test_gpu_serve import check_logprobs, evict_case, rows
+from .test_gpu_step import chain, cuda, random_tree, tree
+from .test_gpu_weights import case as weights_case, check as check_weights
+from paper_2602_16994_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+I32 = torch.int32
+
+
+def far(cache, blocks):
+    """The same blocks at the end of a cache of `blocks` (on the device), and what is added to their numbers."""
+    big = torch.zeros(blocks, *cache.shape[1:], dtype=cache.dtype, device="cuda")
+    shift = blocks - cache.shape[0]
+    big[shift:] = cache.cuda()
+    return big, shift
+
+
+def shifted(table, shift):
+    return torch.where(table >= 0, table + shift, table)
+
+
+def test_offsets_beyond_32_bits_in_prefixes_and_weights():
+    blocks = 2**31 // (16 * 2 * 128) + 2000                       # entries of a cache: above 2^31
+    case = prefix_case([0, 0, 1], [9, 2], [100, 3, 50], tree(4, 2, 4), 8, 2, 128, seed=1)
+    c, (group, shared, table), skip = case
+    want = ref.attention(**c)
+    k, shift = far(c["k_cache"], blocks)
+    v, _ = far(c["v_cache"], blocks)
+    assert k.numel() > 2**31
+    plan = binding.prefix_plan(group.cuda(), shared.cuda(), shifted(table, shift).cuda())
+    check_prefix(case, want, hide=False, k_cache=k, v_cache=v, block_table=shifted(c["block_table"], shift).cuda(), plan=plan)
+    del v
+    w = weights_case([300, 40], tree(4, 2, 4), 8, 2, 128, 16, seed=2)
+    want = serve_ref.weights(w["weights"], w["q"], w["k_cache"], w["lse"], w["table"], w["lengths"], w["parent"])
+    k.zero_()
+    k[blocks - w["k_cache"].shape[0]:] = w["k_cache"].cuda()
+    shift = blocks - w["k_cache"].shape[0]
+    got = torch.zeros(blocks, 16, device="cuda")
+    got[shift:] = w["weights"].cuda()
+    d = cuda(w)
+    binding.cache_weights(got, d["q"], k, d["lse"], shifted(w["table"], shift).cuda(), d["lengths"], d["parent"])
+    assert bool((got[:shift] == 0).all())
+    assert float((got[shift:].cpu().double() - want["weights"]).abs().max()) < 1e-4
+
+
+def test_offsets_beyond_32_bits_in_an_eviction():
+    c = evict_case(3, 300, 16, 2, (8, 128), seed=3)
+    blocks = 2**31 // (16 * 8 * 128) + 3000
+    want, _ = serve_ref.evict(c["cache"], c["weights"], c["lengths"], c["block_table"], c["owned"], c["free_blocks"], c["free_range"], 100, 20)
+    n = c["cache"].shape[1]
+    shift = blocks - n
+    big = torch.zeros(2, blocks, 16, 8, 128, dtype=torch.bfloat16, device="cuda")
+    big[:, shift:] = c["cache"].cuda()
+    w = torch.zeros(blocks, 16, device="cuda")
+    w[shift:] = c["weights"].cuda()
+    d = cuda(c)
+    got = binding.cache_evict(big, w, d["lengths"], shifted(c["block_table"], shift).cuda(), d["owned"], d["free_blocks"], d["free_range"], 100, recent=20)
+    assert torch.equal(big[:, shift:].cpu(), want["cache"]) and not bool(big[:, :shift].any())
+    assert torch.equal(w[shift:].cpu(), want["weights"]) and torch.equal(got.lengths.cpu(), want["lengths"])
+
+
+def test_offsets_beyond_32_bits_in_logits():
+    R, V = 17000, 131072
+    z = torch.zeros(R, V, dtype=torch.bfloat16, device="cuda")
+    some, t = rows(3, V, 1, torch.bfloat16, 4)
+    at = torch.tensor([0, 9000, R - 1])
+    z[at.cuda()] = some.cuda()
+    tokens = torch.zeros(R, 1, dtype=I32)
+    tokens[at] = t
+    got = binding.token_logprobs(z, tokens.cuda(), top=4)
+    want = serve_ref.logprobs(some, t, 1.0, 4)
+    assert torch.equal(got.top_tokens[at.cuda()].cpu(), want["top_tokens"])
+    assert float((got.logprob[at.cuda()].cpu() - want["logprob"]).abs().max()) < 1e-4
+    flat = got.logprob[1:9000]                                   # rows of one value: log V each, and the first tokens
+    assert float((flat + math.log(V)).abs().max()) < 1e-4 and got.top_tokens[5].tolist() == [0, 1, 2, 3]
+
+
+def test_prefixes_without_groups_and_with_empty_ones():
+    case = prefix_case([-1, -2, -1], [], [100, 0, 50], tree(4, 2, 4), 8, 2, 128, seed=5)
+    none = binding.prefix_plan(case[1][0].cuda(), torch.zeros(0, dtype=I32, device="cuda"), torch.zeros(0, 1, dtype=I32, device="cuda"))
+    check_prefix(case, plan=none)
+    check_prefix(prefix_case([1, 1, -1], [4, 0, 7], [100, 0, 50], tree(4, 2, 4), 8, 2, 128, seed=6))
+
+
+def test_the_most_nodes_and_heads():
+    g = torch.Generator().manual_seed(7)
+    check_prefix(prefix_case([0, 0], [3], [5, 60], random_tree(1024, g), 2, 1, 64, seed=7))
+    check_prefix(prefix_case([0, 0, 0], [3], [5, 60, 200], chain(3), 128, 1, 64, seed=8))
+    check_weights(weights_case([5, 300], random_tree(1024, g), 2, 1, 64, 16, seed=9))
+    check_weights(weights_case([5, 300], chain(1024), 1, 1, 64, 16, seed=10, fresh=True))
+    check_weights(weights_case([5, 300, 40], chain(3), 200, 1, 64, 16, seed=11))
+    check_weights(weights_case([64, 300], random_tree(33, g), 6, 3, 128, 16, seed=12))
+    check_weights(weights_case([64, 300], random_tree(34, g), 6, 3, 128, 16, seed=13))
+
+
+@pytest.mark.parametrize("temperature", [1e-30, 1e30])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_temperatures_at_their_limits(temperature, dtype):
+    z, t = rows(2, 3000, 2, dtype, 14)
+    z[0, ::2] = -math.inf
+    z[1, 5] = torch.finfo(dtype).min
+    t[:, 0] = z.argmax(-1).int()
+    check_logprobs(z, t, temperature, 5)
+
+
+def test_many_given_tokens():
+    check_logprobs(*rows(2, 9000, 700, torch.bfloat16, 15), top=2)
+
+
+def test_masks_that_come_late_in_a_row():
+    """Masked stretches ahead of, between and behind the others, of sizes around a batch of loads."""
+    for R in (1, 300):
+        for first in (1, 8191, 8192, 8193, 20000):
+            z, t = rows(R, 40000, 1, torch.bfloat16, 16)
+            z[:, :first] = -math.inf
+            z[:, 30000:39000] = -math.inf
+            t[:] = 39999
+            check_logprobs(z, t, 1.0, 3)
+
+
+def test_two_calls_at_once():
+    """The same calls on two streams at the same time, each with tensors of its own to write."""
+    w = cuda(weights_case([900, 40, 333], tree(4, 2, 4), 8, 2, 128, 16, seed=17))
+    c = evict_case(4, 2000, 16, 3, (2, 64), seed=18)
+    p = prefix_case([0, 1, 0, -1], [40, 7], [100, 60, 30, 200], tree(4, 2, 4), 8, 2, 128, seed=19)
+    plan, d = binding.prefix_plan(*(x.cuda() for x in p[1])), cuda(p[0])
+    streams, out = [torch.cuda.Stream() for _ in range(3)], []
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for s in streams:
+            e = cuda(c)
+            weights = w["weights"].clone()
+            s.wait_stream(torch.cuda.current_stream())
+            status = binding.cache_weights(weights, w["q"], w["k_cache"], w["lse"], w["table"], w["lengths"], w["parent"], stream=s)
+            a = binding.prefix_attention(d["q"], d["k_cache"], d["v_cache"], d["block_table"], d["lengths"], d["parent"], plan, stream=s)
+            cut = binding.cache_evict(e["cache"], e["weights"], e["lengths"], e["block_table"], e["owned"], e["free_blocks"], e["free_range"], 300,
+                                      recent=7, stream=s)
+            out.append((weights, status, a.out, a.status, e["cache"], e["weights"], cut.lengths, cut.free_range, e["free_blocks"]))
+    torch.cuda.synchronize()
+    for x in out[1:]:
+        for a, b in zip(x, out[0]):
+            assert torch.equal(a, b)
