@@ -129,7 +129,7 @@ int32_t spec_prefix_attention(const SpecPrefixAttention *given, void *ws, int64_
     p.unit_blocks = (int)((rows + (two ? 255 : 127)) / (two ? 256 : 128));
     p.merge_rows = attend::MERGE_ROWS;
     const auto merging = [&] { return (rows + p.merge_rows - 1) / p.merge_rows * a->Hkv; };         // CTAs of a request in the joining kernel
-    while (p.merge_rows * (a->D / 4) > attend::MERGE_NT && merging() * a->B < 148 * 4) p.merge_rows /= 2;
+    while (p.merge_rows * (a->D / 8) > attend::MERGE_NT && merging() * a->B < 148 * 4) p.merge_rows /= 2;
     p.groups = (int)merging();
     const bool half = a->dtype == SPEC_F16;
     p.box = a->block_size % 8 ? 0 : a->block_size % 16 ? 8 : a->block_size % 32 ? 16 : 32;

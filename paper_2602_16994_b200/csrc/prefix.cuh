@@ -12,9 +12,9 @@ namespace attend {
 
 constexpr int MERGE_NT = 128, MERGE_ROWS = 32;
 
-// A CTA per request, key head and up to MERGE_ROWS rows of that head (in the order of nodes, then heads of the group); a thread has four entries of a row.  Its
+// A CTA per request, key head and up to MERGE_ROWS rows of that head (in the order of nodes, then heads of the group); a thread has eight entries of a row.  Its
 // rows belong to two units of the request's own and two of the prefix at most.  Where that makes few CTAs they have fewer rows, down to one for a thread: a row
-// of a unit that is cut into many parts takes a load's latency for every six of them (3 requests of 18 nodes, D = 256: 89 us with 32 rows).
+// of a unit that is cut into many parts takes a load's latency for every three of them (3 requests of 18 nodes, D = 256: 89 us with 32 rows).
 template <typename T, typename S> __global__ void __launch_bounds__(MERGE_NT, 8) spec_prefix_join_kernel(const __grid_constant__ Params P)
 {
     constexpr int D = S::D;
@@ -65,10 +65,10 @@ template <typename T, typename S> __global__ void __launch_bounds__(MERGE_NT, 8)
     }
     if (row0 >= upto) return;
     if (bad) {
-        for (int i = tid; i < (upto - row0) * (D / 4); i += MERGE_NT) {
-            const int r = row0 + i / (D / 4), node = node_of(P, r), head = h * P.G + r - node * P.G;
-            *(uint2 *)((T *)P.out + b * P.out_stride[0] + node * P.out_stride[1] + head * P.out_stride[2] + i % (D / 4) * 4) = make_uint2(0, 0);
-            if (P.lse && i % (D / 4) == 0) P.lse[((long long)b * P.tree.N + node) * P.Hq + head] = -CUDART_INF_F;
+        for (int i = tid; i < (upto - row0) * (D / 8); i += MERGE_NT) {
+            const int r = row0 + i / (D / 8), node = node_of(P, r), head = h * P.G + r - node * P.G;
+            *(uint4 *)((T *)P.out + b * P.out_stride[0] + node * P.out_stride[1] + head * P.out_stride[2] + i % (D / 8) * 8) = make_uint4(0, 0, 0, 0);
+            if (P.lse && i % (D / 8) == 0) P.lse[((long long)b * P.tree.N + node) * P.Hq + head] = -CUDART_INF_F;
         }
         return;
     }
@@ -81,34 +81,42 @@ template <typename T, typename S> __global__ void __launch_bounds__(MERGE_NT, 8)
     const long long whole0 = whole_row_of(P, P.n_groups + b, h, 0), whole1 = skip ? whole_row_of(P, g, h, q0) : 0;
     const unsigned live = upto - row0;
 #pragma unroll 1
-    for (unsigned i = tid; i < live * (D / 4); i += MERGE_NT) {
+    for (unsigned i = tid; i < live * (D / 8); i += MERGE_NT) {
         const int ch = (int)(i / live), r = row0 + (int)(i - ch * live);
         // the unit's parts: of the request's own, then of the prefix's
         const int u0 = r / S::ROWS, u1 = (q0 + r) / S::ROWS;
         const int2 own = s_unit[0][u0 - first_unit[0]], pre = skip ? s_unit[1][u1 - first_unit[1]] : make_int2(0, 0);
         if (own.x < 0 && skip == 0) continue;                       // (not cut, and nothing to put it together with: written already)
         const int mine = min(own.y, P.ctas), all = mine + min(pre.y, P.ctas);
-        const auto fetch = [&](int c, float2 &y, float4 &x) {
+        struct Eight { float4 a, b; };
+        const auto fetch = [&](int c, float2 &y, Eight &x) {
             const bool w = c >= mine;
             const int from = w ? pre.x : own.x, part = w ? c - mine : c;
+            const float4 *at;
+            long long step;
             if (from < 0) {
-                const long long at = (w ? whole1 : whole0) + r;
-                y = __ldcg(P.whole_ml[w] + at);
-                x = __ldcg((const float4 *)P.whole[w] + ((at >> 5) * (D / 4) + ch) * 32 + (at & 31));
+                const long long row = (w ? whole1 : whole0) + r;
+                y = __ldcg(P.whole_ml[w] + row);
+                at = (const float4 *)P.whole[w] + ((row >> 5) * (D / 4) + 2 * ch) * 32 + (row & 31);
+                step = 32;
             } else {
                 // (its own slot for the first part, the first slot of the CTAs behind)
                 const long long slot = min(part ? (from / 2 + part) * 2 : from, 2 * P.ctas - 1);
                 const int row = w ? q0 + r - u1 * S::ROWS : r - u0 * S::ROWS;
                 y = __ldcg(P.ml + slot * S::ROWS + row);
-                x = __ldcg((const float4 *)P.part + (slot * (D / 4) + ch) * S::ROWS + row);
+                at = (const float4 *)P.part + (slot * (D / 4) + 2 * ch) * S::ROWS + row;
+                step = S::ROWS;
             }
+            x.a = __ldcg(at);
+            x.b = __ldcg(at + step);
         };
         float ref = -CUDART_INF_F, l = 0.f;
         bool only = false;                     // (some part saw keys, all with a score of -inf)
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        constexpr int AHEAD = 6;
+        float o[8] = {};
+        constexpr int AHEAD = 3;
+#pragma unroll 1
         for (int c0 = 0; c0 < all; c0 += AHEAD) {
-            float4 x[AHEAD];
+            Eight x[AHEAD];
             float2 y[AHEAD];
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
@@ -123,21 +131,25 @@ template <typename T, typename S> __global__ void __launch_bounds__(MERGE_NT, 8)
             }
             const float f = ref == -CUDART_INF_F ? 0.f : ex2_approx(ref - top);
             ref = top;
-            l *= f; o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < 8; ++d) o[d] *= f;
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
                 // (a part that saw nothing counts for nothing, whatever the others' reference)
                 const float w = y[k].x == -CUDART_INF_F ? 0.f : ex2_approx(y[k].x - ref);
                 if (w != 0.f) {
                     l = fmaf(w, y[k].y, l);
-                    o.x = fmaf(w, x[k].x, o.x); o.y = fmaf(w, x[k].y, o.y); o.z = fmaf(w, x[k].z, o.z); o.w = fmaf(w, x[k].w, o.w);
+                    o[0] = fmaf(w, x[k].a.x, o[0]); o[1] = fmaf(w, x[k].a.y, o[1]); o[2] = fmaf(w, x[k].a.z, o[2]); o[3] = fmaf(w, x[k].a.w, o[3]);
+                    o[4] = fmaf(w, x[k].b.x, o[4]); o[5] = fmaf(w, x[k].b.y, o[5]); o[6] = fmaf(w, x[k].b.z, o[6]); o[7] = fmaf(w, x[k].b.w, o[7]);
                 }
             }
         }
         const int node = node_of(P, r), head = h * P.G + r - node * P.G;
-        T *to = (T *)P.out + b * P.out_stride[0] + node * P.out_stride[1] + head * P.out_stride[2] + ch * 4;
+        T *to = (T *)P.out + b * P.out_stride[0] + node * P.out_stride[1] + head * P.out_stride[2] + ch * 8;
         const float inv = l == 0.f ? only ? CUDART_NAN_F : 0.f : 1.f / l;
-        *(uint2 *)to = make_uint2(Pair<T>::pack(o.x * inv, o.y * inv), Pair<T>::pack(o.z * inv, o.w * inv));
+        *(uint4 *)to = make_uint4(Pair<T>::pack(o[0] * inv, o[1] * inv), Pair<T>::pack(o[2] * inv, o[3] * inv), Pair<T>::pack(o[4] * inv, o[5] * inv),
+                                  Pair<T>::pack(o[6] * inv, o[7] * inv));
         if (P.lse && ch == 0) P.lse[((long long)b * P.tree.N + node) * P.Hq + head] = l == 0.f ? -CUDART_INF_F : (ref + log2f(l)) * LN2;
     }
 }
