@@ -23,12 +23,13 @@ int set_prefix_hooks(long long cycles, int hold)
 
 using namespace specv;
 
-// Two blocks of 128 rows share the loads of a tile where a prefix has, on average, more rows than one block, or a request has.
+// Two blocks of 128 rows share the loads of a tile where a prefix has, on average, more rows than they, or a request more than one of them (8192 shared keys; one
+// and two blocks: 228 rows 41 and 43 us, 256 rows a prefix of 32 members 265 and 279, 456 rows 64 and 51, 4864 rows 381 and 254).
 static bool two_blocks(const SpecPrefixAttention *p)
 {
     const SpecAttention &a = p->attention;
     const int64_t rows = (int64_t)a.N * (a.Hq / a.Hkv);
-    return a.D <= 128 && (rows > 128 || (p->n_groups > 0 && (int64_t)p->n_members * rows > (int64_t)p->n_groups * 128));
+    return a.D <= 128 && (rows > 128 || (p->n_groups > 0 && (int64_t)p->n_members * rows > (int64_t)p->n_groups * 256));
 }
 static int prefix_check(const SpecPrefixAttention *p)
 {
