@@ -20,7 +20,7 @@
 namespace specv {
 namespace logp {
 
-constexpr int NT = 256, WARPS = NT / 32, BATCH = 4, SEGS = 4, ROOM = 512, CMAX = 16;
+constexpr int NT = 256, WARPS = NT / 32, BATCH = 4, SEGS = 4, ROOM = 512, CMAX = 8;
 constexpr int STAGES = 3, RING = STAGES * BATCH * NT * 16;             // a thread's batches on their way, in shared memory (no barrier: it reads its own)
 constexpr float LOW = -3.0e38f;                        // stands for -inf where 0 times it has to be 0
 

@@ -38,22 +38,24 @@ int32_t spec_token_logprobs(const SpecLogprobs *a, void *stream)
     if (!(a->temperature >= 1e-30f && a->temperature <= 1e30f) || a->top < 0 || a->top > SPEC_MAX_TOP || a->top > a->V) return SPEC_ERR_PARAM;
     if (!aligned(a->logits, a->dtype == SPEC_F32 ? 4 : 2)) return SPEC_ERR_UNSUPPORTED;
     const int64_t rows = (int64_t)a->B * a->N;
-    // the largest cluster that leaves every CTA half a batch of loads and the chip one wave of two CTAs per SM; of the rows along paths some four a sequence
-    // are there
+    // The largest cluster that leaves every CTA two batches of loads (none for a row of four batches, whose last exchange costs more than it saves) and the chip one
+    // CTA an SM, two thirds of that in clusters of eight, which leave SMs of a GPC over; of the rows along paths some four a sequence are there.  Measured
+    // (bf16, top 20, us) with 1, 2, 4, 8, 16 CTAs a row: 1 row of 32000 entries 9.5, 10.3, 10.1, 10.9, 15; of 128256 15.0, 13.4, 11.8, 11.5, 15;
+    // 16 rows of 151936 16.5, 14.6, 12.7, 13.8, 22; 64 of them 16.8, 15.0, 15.2, 28, 64.
     const int batch = logp::NT * logp::BATCH * (a->dtype == SPEC_F32 ? 4 : 8);
     const int64_t there = a->parent ? std::min<int64_t>(rows, (int64_t)a->B * 4) : rows;
     int C = 1;
-    while (C < logp::CMAX && a->V > C * batch / 2 && there * 2 * C <= 148 * 2) C *= 2;
+    while (C < logp::CMAX && a->V > std::max(4, 2 * C) * batch && there * 2 * C <= (C == 4 ? 98 : 148)) C *= 2;
     logp::Params p = {};
     p.B = a->B; p.N = a->N; p.V = a->V; p.K = a->K; p.top = a->top; p.C = C;
     p.logits = a->logits; p.seq_stride = a->seq_stride; p.node_stride = a->node_stride;
     p.parent = a->parent; p.accepted = a->accepted_node; p.topo_seq_stride = a->topo_seq_stride; p.token = a->token;
     p.T = a->temperature; p.c = 1.4426950408889634f / a->temperature; p.room = 8.f / p.c;
-    // (along paths eight places at once: most end before)
-    p.step = a->parent ? std::min(a->N, 8) : a->N;
+    // (along paths 32 places at once: most end before, and a CTA without one ends at once; 8 sequences: 13.4 us for all 19 places, 13.9 for 8 at once, 21 for 4)
+    p.step = a->parent ? std::min(a->N, 32) : a->N;
     p.logprob = a->logprob; p.entropy = a->entropy; p.top_logprobs = a->top_logprobs; p.top_tokens = a->top_tokens; p.status = a->status;
     const auto go = [&](auto kernel) {
-        const int rc = prepare(kernel, std::max(logp::RING, 48 * 1024 + 1), true);          // (beside the static part)
+        const int rc = prepare(kernel, std::max(logp::RING, 48 * 1024 + 1), false);          // (beside the static part)
         return rc ? rc : launch(kernel, dim3((unsigned)((a->parent ? (int64_t)a->B * p.step : rows) * C)), logp::NT, logp::RING, C > 1 ? C : 0, (cudaStream_t)stream, p);
     };
     return a->dtype == SPEC_F32  ? go(logp::spec_logprobs_kernel<float>)
