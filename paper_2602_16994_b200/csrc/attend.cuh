@@ -9,9 +9,9 @@
 // rows take 1040 cycles of products and about 1100 of arithmetic per scheduler, 256 rows twice that, so up to about 250 rows the cache's
 // bytes are the floor, and both products go to the tensor cores even for one row (which fills 1 of 128 lanes).  A thread owns a row, and maxima and
 // sums need no exchange.  Measured (one B200): a tile takes 3100 cycles with up to 128 rows (8 requests, 19 nodes, 4 query heads to a key
-// head, contexts to 4096: 38 us, floor 15) and 4500 with 204 (128 requests of 51 nodes: 443 us in a short row of calls, 517 to 524 in a long one, which
+// head, contexts to 4096: 37 us, floor 15) and 4500 with 204 (128 requests of 51 nodes: 427 to 435 us in a short row of calls, 517 to 524 in a long one, which
 // runs into the power limit at 1.64 GHz; floor 226): there a row block's weights wait for its products and these for their turn on the tensor cores.
-// Small calls are bound by latency: one token over 8192 keys takes 23 us (floor 5), of which 5 pass until the first scores are there, 1.2 a
+// Small calls are bound by latency: one token over 8192 keys takes 22 us (floor 5), of which 5 pass until the first scores are there, 1.2 a
 // tile, and 6 from the last tile to the joined result.
 //
 // Precision.  Scores, references, sums and O are fp32.  P is rounded to the type of the values: the product takes two operands of one type, and the rest

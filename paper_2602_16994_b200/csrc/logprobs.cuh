@@ -9,7 +9,9 @@
 // maximum reaches the bound, about n of 1024, and the candidates of a CTA are put in order by counting.  Ties beyond the candidates' room
 // (rows under a mask, where the bound is -inf) are filled up in index order.
 //
-// What bounds it.  One read of the rows.
+// What bounds it.  One read of the rows: 2048 rows of 151936 bf16 entries in 130 us, 0.74 of the copy bandwidth (without the most probable 107 us, 0.90; with them
+// the exponentials, the maxima and the search share the issue slots: 59 % of them).  Few rows: latency, of one launch, one row and the exchange in the cluster
+// (1 row 9 to 12 us).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -133,6 +133,7 @@ int32_t spec_prefix_attention(const SpecPrefixAttention *given, void *ws, int64_
     while (p.merge_rows * (a->D / 8) > attend::MERGE_NT && merging() * a->B < 148 * 4) p.merge_rows /= 2;
     p.groups = (int)merging();
     const bool half = a->dtype == SPEC_F16;
+    // (boxes: 254 us for 64 requests of 19 nodes; by 16-byte copies 270)
     p.box = a->block_size % 8 ? 0 : a->block_size % 16 ? 8 : a->block_size % 32 ? 16 : 32;
     const int64_t sizes[4] = {a->D, a->Hkv, a->block_size, a->num_blocks};
     const auto cache_map = [&](CUtensorMap *map, const void *cache, const int64_t *s) {

@@ -5,13 +5,16 @@
 // columns; over the rows, blocks of rows and key heads its sum never leaves its register, and no two CTAs add to the same entry: the order
 // of every sum is fixed.
 //
-// What bounds it.  With few rows the keys' bytes: 256 KB a tile of 128 keys at 8 heads of 128 entries.  With many rows the exponentials.
+// What bounds it.  With many rows the exponentials: 16 a cycle and SM, of which this reaches two thirds (2 stretches of 512 nodes, 32 heads to 8, behind up to 16384 tokens: 180 us; 96
+// of exponentials alone, 64 of products).  Taking one to three of eight by a polynomial instead made that 1 to 5 % longer.  With few rows latency: the keys'
+// bytes of 8 requests of 19 nodes over 1500 to 4096 keys would take 7.5 us, the call takes 25, of one token over 4096 keys 1.3 and 12: a CTA knows its run
+// after 2.7 us and has its first sums after 6, then a tile and head take 1300 to 2200 cycles.
 //
 // Balance.  Two tiles that lie wholly among the committed tokens go together (a block of queries that is on chip serves both), the others by themselves; a
 // unit is such a group and a key head, its length its tiles.  The units of all requests, groups in order, heads within, are cut into one run per CTA (one
 // CTA per SM).  A group whose heads are in several runs leaves their sums in the workspace, and spec_weigh_join_kernel adds them up in order.
 // Four warps copy keys (by tensor map where all 32 of a warp's keys are there and blocks are multiples of 8 slots, else 16 bytes at a time), two
-// queries (by tensor map where a block of them is whole nodes), two issue the products, sixteen take the exponentials, a product a
+// queries (by tensor map where a block of them is whole nodes: 179 us for the stretches of 512 nodes, 292 by 16-byte copies; keys 25.0 and 25.2 for 8 requests), two issue the products, sixteen take the exponentials, a product a
 // warpgroup in turn (128 columns: 1800 cycles of an SM where all warps had 32 columns each of every product, and its barriers).
 //
 // What is not a number adds nothing: the maximum that bounds exponents from below takes NaN for its bound.  So it does not matter what
