@@ -7,7 +7,7 @@ import torch
 
 from . import serve_ref, step_ref as ref
 from .test_gpu_prefix import check as check_prefix, prefix_case
-from .test_gpu_serve import check_logprobs, evict_case, rows
+from .test_gpu_serve import check_logprobs, check_path, evict_case, rows
 from .test_gpu_step import chain, cuda, random_tree, tree
 from .test_gpu_weights import case as weights_case, check as check_weights
 from paper_2602_16994_b200 import binding
@@ -150,3 +150,31 @@ def test_two_calls_at_once():
     for x in out[1:]:
         for a, b in zip(x, out[0]):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("N,V", [(33, 500), (70, 70001), (1024, 300)])
+@pytest.mark.parametrize("B", [1, 3])
+def test_paths_of_many_nodes(B, N, V):
+    """Chains longer than the places that are gone through at once, accepted to their ends or not; rows by one CTA and by several."""
+    g = torch.Generator().manual_seed(N + B)
+    z = (3 * torch.randn(B, N, V, generator=g)).bfloat16()
+    parent = torch.arange(-1, N - 1, dtype=I32)
+    accepted = torch.tensor([N - 1, 32, 31][:B], dtype=I32)
+    check_path(z, accepted, torch.randint(0, V, (B, N), generator=g).int(), parent, 0.9, 2)
+
+
+@pytest.mark.parametrize("V", [16385, 32768, 32769, 65537, 131073, 262151])
+@pytest.mark.parametrize("R", [1, 12, 13, 37, 75])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rows_by_any_number_of_ctas(R, V, dtype):
+    """Sizes on both sides of where a row goes to one CTA more."""
+    z, t = rows(R, V, 1, dtype, R + V)
+    z[R // 2, : V // 2] = -math.inf
+    check_logprobs(z, t, 1.0, 32)
+
+
+@pytest.mark.parametrize("groups", [[0] * 3, [0] * 4, [0] * 6 + [1] * 2, [0, 1, 1, 2, 2, 2, 2, 2, 2]])
+def test_prefix_rows_around_two_blocks(groups):
+    """Averages of rows of a prefix below, at and above two blocks, groups of unequal sizes among them."""
+    n = max(groups) + 1
+    check_prefix(prefix_case(groups, [20, 9, 30][:n], [50 + 37 * i for i in range(len(groups))], tree(4, 2, 4), 8, 2, 128, seed=len(groups)))
