@@ -860,7 +860,7 @@ PyObject *py_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n)
             if (nodes != N) raise("logits must be [B,N,V] with the N of parent");
             s.accepted_node = int_ptr(ints(a[2], "accepted_node", place, B));
         }
-        best.push_back(s.top < 0 ? 0 : s.top);
+        best.push_back(std::clamp(s.top, 0, SPEC_MAX_TOP));        // (more is refused below)
         at::Tensor t[5];
         t[0] = place.fresh(given, at::kFloat);
         t[1] = place.fresh(rows, at::kFloat);

@@ -10,8 +10,8 @@ One step of the loop, for requests whose trees share ``parent`` (Section 2, step
     cache.commit(out.accepted_node)                       # the accepted paths stay
     cache.evict(budget, recent)                           # (with ``weigh``) longer requests keep their heaviest entries
 
-Requests that begin with the same tokens hold them once (``share``), and attend to them together.  Nothing synchronises; lengths, tables and free blocks live on the device.  ``lengths``, ``owned`` and ``free_range`` are replaced by the
-calls' results: a step captured into a graph is the same step at every replay, unless its results are copied into the tensors that it read.
+Requests that begin with the same tokens hold them once (``share``), and attend to them together.  Nothing in a step synchronises; lengths, tables and free
+blocks live on the device.  ``lengths``, ``owned`` and ``free_range`` are replaced by the calls' results: a step captured into a graph is the same step at every replay, unless its results are copied into the tensors that it read.
 """
 from __future__ import annotations
 
@@ -30,7 +30,7 @@ class TreeCache:
     emptied takes a new request with ``lengths[row] = 0``.
 
     ``weigh``: the attention weight that entries get is added up in ``weights``, over all layers that ``attend`` sees, for ``evict``.  ``protected`` [B]:
-    tokens at a request's beginning that are neither weighed nor evicted.  After an eviction a request's positions run on: its tokens are
+    tokens at a request's beginning that are neither weighed nor evicted; 0 again after ``release``.  After an eviction a request's positions run on: its tokens are
     ``dropped`` more than its entries.
     """
 
@@ -135,7 +135,7 @@ class TreeCache:
         done = binding.cache_evict(self.storage, self.weights, self.lengths, self.block_table, self.owned, self.free_blocks, self.free_range, budget,
                                    recent, self.protected, stream)
         current = torch.cuda.current_stream(done.lengths.device) if stream is not None else None
-        with self._on(stream, self.lengths):
+        with self._on(stream, self.lengths, *([] if self.dropped is None else [self.dropped])):
             fewer = torch.where(self.lengths >= 0, self.lengths - done.lengths, 0)
             self.dropped = fewer if self.dropped is None else self.dropped + fewer
         if current is not None:
@@ -145,8 +145,8 @@ class TreeCache:
 
     def share(self, request, rows):
         """Empty ``rows`` begin with the tokens of ``request`` so far, as many as fill whole blocks, which all of them then hold together: what they attend
-        to there is read once.  Returns the number of tokens; the ones behind are the rows' own to write again.  For the rare beginning of a
-        request: reads tables on the host.
+        to there is read once.  Returns the number of tokens; the ones behind are the rows' own to write again.  Between two steps; for the
+        rare beginning of a request: reads tables on the host.
         """
         rows = [int(x) for x in rows]
         n = int(self.lengths[request]) // self.block_size

@@ -10,7 +10,7 @@ from .test_gpu_prefix import check as check_prefix, prefix_case
 from .test_gpu_serve import check_logprobs, check_path, evict_case, rows
 from .test_gpu_step import chain, cuda, random_tree, tree
 from .test_gpu_weights import case as weights_case, check as check_weights
-from paper_2602_16994_b200 import binding
+from paper_2602_16994_b200 import binding, tree_cache
 
 pytestmark = pytest.mark.gpu
 
@@ -178,3 +178,34 @@ def test_prefix_rows_around_two_blocks(groups):
     """Averages of rows of a prefix below, at and above two blocks, groups of unequal sizes among them."""
     n = max(groups) + 1
     check_prefix(prefix_case(groups, [20, 9, 30][:n], [50 + 37 * i for i in range(len(groups))], tree(4, 2, 4), 8, 2, 128, seed=len(groups)))
+
+
+def test_more_alternatives_than_there_may_be_take_no_memory():
+    z, t = rows(1, 100, 1, torch.float32, 21)
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.max_memory_allocated()
+    with pytest.raises(RuntimeError):
+        binding.token_logprobs(z.cuda(), t.cuda(), top=2**31 - 1)
+    assert torch.cuda.max_memory_allocated() < before + 2**20
+
+
+def test_an_eviction_on_a_stream_tells_the_allocator_of_what_it_reads(monkeypatch):
+    """``dropped`` of an earlier eviction, which another stream may have made, is read on the stream of the next one and let go of."""
+    cache = tree_cache.TreeCache(2, 1, 16, 4, 1, 64, width=8, weigh=True)
+    cache.block_table.copy_(torch.arange(16, dtype=I32).view(2, 8))
+    cache.lengths, cache.owned = torch.full((2,), 30, dtype=I32, device="cuda"), torch.full((2,), 8, dtype=I32, device="cuda")
+    cache.free_range = torch.tensor([0, 0], dtype=I32, device="cuda")
+    cache.evict(20)
+    before, told, real = cache.dropped, [], cache._on
+
+    def on(stream, *used):
+        told.extend(used)
+        return real(stream, *used)
+
+    monkeypatch.setattr(cache, "_on", on)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    cache.evict(10, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert any(x is before for x in told)
+    assert cache.dropped.tolist() == [20, 20] and cache.lengths.tolist() == [10, 10] and cache.free_range.tolist() == [0, 10]
