@@ -46,6 +46,7 @@ class TreeCache:
         self.weights = torch.zeros((num_blocks, block_size), dtype=torch.float32, device=device) if weigh else None
         self.protected = torch.zeros(batch, **i32)
         self.dropped = None                              # [B] evicted tokens, once there have been any
+        self.weighed = None                              # [B] lengths of the requests whose trees add weight
         self.fresh = True                                # (no layer of the step has been attended to)
         self.prefixes = {}                               # groups that share a prefix: its blocks and the members, on the host
         self.plan = None
@@ -57,10 +58,17 @@ class TreeCache:
                                         self.block_size, n_nodes, stream)
         self.owned, self.free_range = self.step.owned, self.step.free_range
         self.fresh = True
+        if self.weights is not None:                     # (a refused tree has no entries of its own, and its nodes weigh nothing)
+            with self._on(stream, self.lengths):
+                self.weighed = torch.where(self.step.status != 0, -1, self.lengths)
         if self.dropped is not None:                     # (a node without a position keeps its -1)
             with self._on(stream, self.dropped):
                 at = self.step.positions
                 self.step.positions = torch.where(at < 0, at, at + self.dropped[:, None])
+        if stream is not None:                           # (they may be read on the current stream too)
+            for t in (self.weighed, self.step.positions):
+                if t is not None:
+                    t.record_stream(torch.cuda.current_stream(t.device))
         return self.step
 
     @contextlib.contextmanager
@@ -88,7 +96,7 @@ class TreeCache:
             raise RuntimeError("entries are not weighed under a window")
         wanted = kw.get("want_lse", False)
         got = self._attend(layer, q, dict(kw, want_lse=True))
-        self.weigh_status = binding.cache_weights(self.weights, q, self.storage[2 * layer], got.lse, self.block_table, self.lengths, self.parent,
+        self.weigh_status = binding.cache_weights(self.weights, q, self.storage[2 * layer], got.lse, self.block_table, self.weighed, self.parent,
                                                   self.n_nodes, scale=kw.get("scale"), protected=self.protected, fresh=self.fresh,
                                                   stream=kw.get("stream"))
         self.fresh = False

@@ -209,3 +209,25 @@ def test_an_eviction_on_a_stream_tells_the_allocator_of_what_it_reads(monkeypatc
     torch.cuda.current_stream().wait_stream(side)
     assert any(x is before for x in told)
     assert cache.dropped.tolist() == [20, 20] and cache.lengths.tolist() == [10, 10] and cache.free_range.tolist() == [0, 10]
+
+
+def test_a_refused_tree_adds_no_weight():
+    """Two requests, blocks for one of them: the other's entries keep the weights that they had, and its lengths."""
+    g = torch.Generator().manual_seed(23)
+    cache = tree_cache.TreeCache(2, 1, 9, 16, 2, 64, width=5, weigh=True)
+    cache.storage.copy_(torch.randn(cache.storage.shape, generator=g))
+    cache.weights.copy_(torch.rand(cache.weights.shape, generator=g))
+    cache.block_table[:, :4] = torch.arange(8, dtype=I32).view(2, 4)
+    cache.lengths, cache.owned = torch.full((2,), 64, dtype=I32, device="cuda"), torch.full((2,), 4, dtype=I32, device="cuda")
+    cache.free_range = torch.tensor([8, 1], dtype=I32, device="cuda")
+    before = cache.weights.cpu()
+    parent = torch.arange(-1, 2, dtype=I32).cuda()
+    done = cache.begin(parent)
+    refused = (done.status != 0).nonzero().flatten().tolist()
+    assert refused == [1]
+    q = torch.randn(2, 3, 4, 64, generator=g).bfloat16().cuda()
+    cache.attend(0, q)
+    after = cache.weights.cpu()
+    assert torch.equal(after[4:8], before[4:8]) and bool((after[:4] > before[:4]).all())
+    added = after[:4].double() - before[:4].double()
+    assert float(added.sum() + after[8, :3].double().sum()) == pytest.approx(12, rel=1e-3)          # (three nodes of four heads)
