@@ -121,7 +121,8 @@ constexpr int SUM_WARPS = 16, WG = SUM_WARPS / 4, SUMS = SUM_WARPS * 32, PRODUCT
 struct Bars {
     uint64_t k_full[6], k_empty[6], q_full[4], q_empty[4], s_full[4], s_empty[4], r_full[SR], r_empty[SR];
     uint32_t tmem;
-    int dead, found[2], sums[20];
+    int dead, found[2];
+    int sums[NT / 32];                         // an entry for every warp of the CTA
     Request request;                           // the one that the run begins in
 };
 static_assert(sizeof(Bars) <= 512, "the area behind the buffers");
@@ -142,7 +143,8 @@ struct Cuts {                                  // runs of equal length, the firs
     int all, each, more;
     __device__ __forceinline__ int start(int c) const { return each * c + min(c, more); }
 };
-// The run of CTA c: all threads.
+// The run of CTA c: all threads.  Between the two barriers every warp reads all of `sums`, and the one thread that finds the run's start writes `found` and
+// `request`, which no other reads there: sums has an entry for every warp and ends ahead of both, so nothing that is written is read before the second barrier.
 __device__ __forceinline__ void find_run(const Params &P, int c, Bars *S, Run *run, Cuts *cuts, int tid)
 {
     const int lane = tid & 31, warp = tid >> 5;
@@ -159,7 +161,7 @@ __device__ __forceinline__ void find_run(const Params &P, int c, Bars *S, Run *r
     if (lane == 31) S->sums[warp] = incl;
     if (tid == 0) { S->found[0] = P.B; S->found[1] = 0; }
     __syncthreads();
-    static_assert(NT / 32 <= 32, "a lane for a warp's sum");
+    static_assert(sizeof(S->sums) / sizeof(int) == NT / 32 && NT / 32 <= 32, "an entry of sums, and a lane, for every warp");
     int warps = lane < NT / 32 ? S->sums[lane] : 0;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from . import serve_ref as ref, step_ref
-from .test_gpu_step import chain, pages, random_tree, tree
+from .test_gpu_step import chain, cuda, pages, random_tree, tree
 from paper_2602_16994_b200 import binding
 
 pytestmark = pytest.mark.gpu
@@ -75,6 +75,25 @@ def test_weights_over_many_requests():
     g = torch.Generator().manual_seed(2)
     check(case(torch.randint(0, 400, (333,), generator=g), tree(2, 0, 2), 2, 1, 64, 16, seed=2))
     check(case([5000, 3, 2000], tree(2, 0, 2), 2, 2, 64, 16, seed=3, protected=torch.tensor([129, 0, 1900], dtype=I32)))
+
+
+@pytest.mark.parametrize("requests", [641, 700, 768, 769, 1600])
+def test_weights_of_as_many_requests_as_a_cta_has_threads_and_more(requests):
+    """One request to a thread, in all of its warps, and several."""
+    g = torch.Generator().manual_seed(requests)
+    lengths = torch.randint(0, 150, (requests,), generator=g)
+    lengths[::7], lengths[-1] = -1, 300
+    check(case(lengths, tree(2, 0, 1), 2, 1, 64, 16, seed=requests))
+
+
+def test_weights_are_the_same_bits_in_many_calls():
+    c = cuda(case([900, 40, 333, 2000, 7], tree(4, 2, 4), 8, 2, 128, 16, seed=14))
+    want = None
+    for _ in range(200):
+        w = c["weights"].clone()
+        status = binding.cache_weights(w, c["q"], c["k_cache"], c["lse"], c["table"], c["lengths"], c["parent"])
+        want = w if want is None else want
+        assert torch.equal(w, want) and not bool(status.any())
 
 
 def test_weights_beside_what_is_no_number():
