@@ -16,6 +16,7 @@ blocks live on the device.  ``lengths``, ``owned`` and ``free_range`` are replac
 from __future__ import annotations
 
 import contextlib
+import operator
 
 import torch
 
@@ -151,12 +152,19 @@ class TreeCache:
         self.lengths, self.owned, self.free_range = done.lengths, done.owned, done.free_range
         return done
 
+    def _row(self, x):
+        """A request's row as its number from 0 on, by which groups know their members: of a negative one (from the end) or a tensor too."""
+        x, batch = operator.index(x), self.lengths.numel()
+        if not -batch <= x < batch:
+            raise IndexError(f"there is no row {x} among {batch}")
+        return x % batch
+
     def share(self, request, rows):
         """Empty ``rows`` begin with the tokens of ``request`` so far, as many as fill whole blocks, which all of them then hold together: what they attend
         to there is read once.  Returns the number of tokens; the ones behind are the rows' own to write again.  Between two steps; for the
         rare beginning of a request: reads tables on the host.
         """
-        rows = [int(x) for x in rows]
+        request, rows = self._row(request), [self._row(x) for x in rows]
         n = int(self.lengths[request]) // self.block_size
         if any(request in members for _, members in self.prefixes.values()) or (self.dropped is not None and int(self.dropped[request])):
             raise RuntimeError("a request that shares a prefix already, or has been cut, is not shared again")
@@ -172,7 +180,7 @@ class TreeCache:
         for x in rows + [request]:
             protected[x] = protected[x].clamp(min=n * self.block_size)
         self.lengths, self.owned, self.protected = lengths, owned, protected
-        self.prefixes[max(self.prefixes, default=-1) + 1] = (blocks, {int(request), *rows})
+        self.prefixes[max(self.prefixes, default=-1) + 1] = (blocks, {request, *rows})
         self._plan()
         return n * self.block_size
 
@@ -192,7 +200,8 @@ class TreeCache:
     def release(self, request):
         """Puts the blocks of a request that has ended back behind the free ones; those of a shared prefix when its last member ends.  For the rare end of a
         request: reads its row on the host."""
-        request, n, (first, count), size = int(request), int(self.owned[request]), self.free_range.tolist(), self.free_blocks.numel()
+        request = self._row(request)
+        n, (first, count), size = int(self.owned[request]), self.free_range.tolist(), self.free_blocks.numel()
         keep = 0
         for g, (blocks, members) in list(self.prefixes.items()):
             if request in members:

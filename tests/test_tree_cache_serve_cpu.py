@@ -118,6 +118,52 @@ def test_a_prefix_is_shared_and_comes_back_with_its_last_member(calls):
     assert sorted(free.tolist()) == list(range(12)) and cache.protected.tolist() == [0, 0, 0, 0] and cache.dropped.tolist() == [0, 0, 0, 0]
 
 
+def holdings(cache):
+    """Blocks that are free, in the ring's order, and those that requests hold."""
+    first, count = cache.free_range.tolist()
+    free = cache.free_blocks[(first + torch.arange(count)) % cache.free_blocks.numel()].tolist()
+    return free, {x for b in range(cache.owned.numel()) for x in cache.block_table[b, :int(cache.owned[b])].tolist()}
+
+
+def shared_by_four(weigh=True):
+    cache = tree_cache.TreeCache(4, 1, 12, 4, 1, 1, width=6, dtype=torch.float32, device="cpu", weigh=weigh)
+    cache.lengths = torch.tensor([0, -1, -1, -1], dtype=I32)
+    step(cache, torch.arange(-1, 9, dtype=I32), 0.0, [9, -1, -1, -1])
+    return cache
+
+
+@pytest.mark.parametrize("shared,ended", [([-1], [3, 0]), ([-1], [-1, 0]), ([3], [-1, -4]), ([3], [-4, 3]), ([torch.tensor(-1), 1], [1, 0, 3]),
+                                          (torch.tensor([1, 3]), [torch.tensor(-3), 0, torch.tensor(3)])])
+def test_rows_are_the_same_by_any_name(calls, shared, ended):
+    """Rows from the end, and rows in tensors: no block that a request still holds comes back, and none twice."""
+    cache = shared_by_four()
+    assert cache.share(torch.tensor(0), shared) == 8
+    for x in ended:
+        cache.release(x)
+        free, held = holdings(cache)
+        assert len(set(free)) == len(free) and not held & set(free) and len(free) + len(held) == 12
+    assert cache.plan is None and cache.prefixes == {} and cache.protected.tolist() == [0, 0, 0, 0]
+
+
+def test_a_member_is_not_shared_again_by_another_name(calls):
+    cache = shared_by_four()
+    assert cache.share(-4, [1]) == 8
+    for request in (0, -4, torch.tensor(0), torch.tensor(-4), 1, -3):
+        with pytest.raises(RuntimeError, match="already"):
+            cache.share(request, [2])
+    other = shared_by_four()
+    for rows in ([0], [-4], [torch.tensor(0)], [1, -3], [torch.tensor(1), 1]):
+        with pytest.raises(RuntimeError, match="empty"):
+            other.share(0, rows)
+    for request, rows in ((4, [1]), (-5, [1]), (0, [4]), (0, [1, -5])):
+        with pytest.raises(IndexError):
+            other.share(request, rows)
+    for request in (4, -5):
+        with pytest.raises(IndexError):
+            other.release(request)
+    assert other.prefixes == {} and other.share(0, []) == 8
+
+
 def test_without_weights_nothing_is_evicted(calls):
     cache = tree_cache.TreeCache(1, 1, 2, 4, 1, 1, width=2, dtype=torch.float32, device="cpu")
     with pytest.raises(RuntimeError, match="weigh"):
