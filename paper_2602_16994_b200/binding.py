@@ -550,6 +550,8 @@ def path_logprobs(logits, accepted_node, out_tokens, parent, temperature=1.0, to
     """The same for what a verification put out: ``out_tokens`` [B,N] along the path to ``accepted_node`` [B] (a verifier's outputs), under the
     rows of ``logits`` [B,N,V] that its nodes have.  Behind a path's end 0, and -1 for the top tokens; only the paths' rows are read.
     """
+    if accepted_node is None or parent is None:         # (without a tree the call would take every row for itself)
+        raise TypeError("accepted_node and parent must be tensors")
     return _calls().logprobs(logits, out_tokens, accepted_node, parent, temperature, top, stream)
 
 

@@ -147,3 +147,10 @@ def test_the_calls_refuse_to_run_without_a_gpu(lib, name, args):  # noqa: F811
         getattr(binding, name)(*args(torch.zeros(1, 1, 1, 8), torch.zeros(1, dtype=torch.int32)))
     with pytest.raises(TypeError):
         getattr(binding, name)(*([None] * len(args(torch.zeros(1, 1, 1, 8), torch.zeros(1, dtype=torch.int32)))))
+
+
+def test_paths_without_a_tree_are_refused():
+    t, i = torch.zeros(1, 2, 8), torch.zeros(1, 2, dtype=torch.int32)
+    for accepted, parent in ((i[0, :1], None), (None, i[0]), (None, None)):
+        with pytest.raises(TypeError, match="must be tensors"):
+            binding.path_logprobs(t, accepted, i, parent)
