@@ -530,7 +530,7 @@ int32_t spec_cache_weights(const SpecWeights *a, void *ws, int64_t ws_bytes, voi
  * block_table stays as it is (its columns from owned_out[b] on are no longer the request's); owned and free_range are inputs and stay too.
  * Requests of at most `budget` tokens stay as they are, blocks included.
  * protected[b] > budget, or a negative one: SPEC_DEV_TOPOLOGY; a bad block id in the owned columns, or fewer of them than
- * the tokens need: SPEC_DEV_PAGE; then nothing of the request moves.  A ring without room for a request's blocks (or a free_range
+ * the tokens need, or more tokens than the cache has slots or than 2^31 - 65537: SPEC_DEV_PAGE; then nothing of the request moves.  A ring without room for a request's blocks (or a free_range
  * outside it): SPEC_DEV_BLOCKS, the request is shortened but keeps its blocks.  Blocks that hold entries behind protected[b] must be the request's own.
  * No tree is under way: entries behind the committed tokens are not kept.
  * `ws`: spec_cache_evict_workspace_bytes() bytes.

@@ -37,6 +37,8 @@ struct Params {
 
 // ---- selection ----------------------------------------------------------------------------------------------------------------
 constexpr int NT = 1024, WARPS = NT / 32, COLS = 4096, KEYS = 46 * 1024;         // 16 and 184 KB
+constexpr int MOST = 0x7FFFFFFF - 65536;               // tokens of a request that is cut: KEYS, and a batch of the moves, may be added to an index
+static_assert(KEYS + 8 * NT <= 65536, "an index and what is added to it");
 
 __device__ __forceinline__ uint32_t weight_key(float w) { return w == w ? cut::key_of(w) : 0u; }
 
@@ -75,7 +77,8 @@ __global__ void __launch_bounds__(NT) spec_evict_select_kernel(const __grid_cons
     const bool idle = len <= budget;                   // (negative lengths too)
     bool page = false;
     if (!idle) {
-        page = own < 0 || own > P.width || (len - 1) / P.block >= own;
+        // (no more tokens than the cache has slots, nor so many that an index into them and a batch would pass 32 bits)
+        page = own < 0 || own > P.width || (len - 1) / P.block >= own || len > min((long long)P.num_blocks * P.block, (long long)MOST);
         if (!page)
             for (int col = tid; col < own; col += NT) {
                 const int id = __ldg(table + col);
@@ -197,7 +200,7 @@ __global__ void __launch_bounds__(NT) spec_evict_select_kernel(const __grid_cons
     __syncthreads();
     if (tid == 0) {
         P.lengths_out[b] = budget;
-        P.plan[b] = make_int2(s_first, own - (budget + P.block - 1) / P.block);
+        P.plan[b] = make_int2(s_first, own - ((budget - 1) / P.block + 1));
         P.status[b] = SPEC_DEV_OK;
     }
 }

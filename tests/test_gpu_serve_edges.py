@@ -69,6 +69,41 @@ def test_offsets_beyond_32_bits_in_an_eviction():
     assert torch.equal(w[shift:].cpu(), want["weights"]) and torch.equal(got.lengths.cpu(), want["lengths"])
 
 
+def test_an_eviction_of_lengths_at_the_end_of_32_bits():
+    """A length that the table's columns have room for and the cache has not: nothing moves.  (Blocks that the table names again and again.)"""
+    block, width = 2**20, 2048
+    g = torch.Generator().manual_seed(24)
+    cache, weights = torch.randint(0, 256, (1, 1, block, 1), generator=g).byte().cuda(), torch.rand(1, block, generator=g).cuda()
+    before, w = cache.clone(), weights.clone()
+    lengths = torch.tensor([2**31 - 1, 2**31 - 65537, block + 1, -2**31], dtype=I32, device="cuda")
+    table, owned = torch.zeros(4, width, dtype=I32, device="cuda"), torch.full((4,), width, dtype=I32, device="cuda")
+    ring, free = torch.full((9,), -1, dtype=I32, device="cuda"), torch.tensor([0, 0], dtype=I32, device="cuda")
+    for budget in (100, 2**20):
+        got = binding.cache_evict(cache, weights, lengths, table, owned, ring, free, budget)
+        assert got.status.tolist() == [5, 5, 5, 0] and torch.equal(got.lengths, lengths) and torch.equal(got.owned, owned)
+        assert torch.equal(cache, before) and torch.equal(weights, w) and got.free_range.tolist() == [0, 0]
+
+
+def test_an_eviction_in_one_block_of_almost_all_slots():
+    """A budget and a block that 32 bits do not hold together: the same as in a block of just the request's size."""
+    n, budget, most = 70100, 70000, 2**31 - 65600
+    g = torch.Generator().manual_seed(25)
+    rows, w = torch.randint(0, 256, (n,), generator=g).byte(), torch.rand(n, generator=g)
+    got = []
+    for block in (n, most):
+        cache, weights = torch.zeros(1, 1, block, 1, dtype=torch.uint8, device="cuda"), torch.zeros(1, block, device="cuda")
+        cache[0, 0, :n, 0], weights[0, :n] = rows.cuda(), w.cuda()
+        one = torch.zeros(1, dtype=I32, device="cuda")
+        done = binding.cache_evict(cache, weights, one + n, one[None], one + 1, torch.full((3,), -1, dtype=I32, device="cuda"),
+                                   torch.zeros(2, dtype=I32, device="cuda"), budget, recent=9)
+        assert done.status.tolist() == [0] and done.lengths.tolist() == [budget] and done.owned.tolist() == [1] and done.free_range.tolist() == [0, 0]
+        got.append((cache[0, 0, :n, 0].cpu(), weights[0, :n].cpu()))
+        del cache, weights
+    keep = sorted(torch.sort(w[:n - 9], descending=True, stable=True).indices[:budget - 9].tolist()) + list(range(n - 9, n))
+    assert torch.equal(got[0][0][:budget], rows[keep]) and torch.equal(got[0][1][:budget], w[keep])
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
 def test_offsets_beyond_32_bits_in_logits():
     R, V = 17000, 131072
     z = torch.zeros(R, V, dtype=torch.bfloat16, device="cuda")
