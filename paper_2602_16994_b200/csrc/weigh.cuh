@@ -55,7 +55,7 @@ struct Params {
 struct Request {
     int len, n, from, end;                     // nodes (0: idle or a bad number of them); entries [from, end) count
     __device__ __forceinline__ int first() const { return from / KT; }
-    __device__ __forceinline__ int tiles() const { return n == 0 || end <= from ? 0 : (end + KT - 1) / KT - from / KT; }
+    __device__ __forceinline__ int tiles() const { return n == 0 || end <= from ? 0 : (int)(((unsigned)end + KT - 1) / KT) - from / KT; }
     __device__ __forceinline__ int pairs() const { return max(0, min(len / KT - from / KT, tiles())) / 2; }
 };
 __device__ __forceinline__ Request request_of(const Params &P, int b)

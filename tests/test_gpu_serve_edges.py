@@ -69,6 +69,29 @@ def test_offsets_beyond_32_bits_in_an_eviction():
     assert torch.equal(w[shift:].cpu(), want["weights"]) and torch.equal(got.lengths.cpu(), want["lengths"])
 
 
+def test_weights_of_lengths_at_the_end_of_32_bits():
+    """Tables with room for 2^31 entries, few of whose columns name a block: those get their weight, and the requests beside them theirs."""
+    block, width, D = 2**16, 2**15, 64
+    g = torch.Generator().manual_seed(26)
+    k = torch.randn(4, block, 1, D, generator=g).bfloat16()
+    q = torch.randn(3, 1, 1, D, generator=g).bfloat16()
+    table = torch.full((3, width), -1, dtype=I32)
+    table[0, 0], table[0, width - 1], table[1, 5], table[2, 0] = 0, 1, 2, 3
+    lengths, lse = torch.tensor([2**31 - 1, 2**31 - 60, 1000], dtype=I32), torch.tensor([1.0, 2.0, 3.0]).view(3, 1, 1)
+    w = torch.zeros(4, block, device="cuda")
+    status = binding.cache_weights(w, q.cuda(), k.cuda(), lse.cuda(), table.cuda(), lengths.cuda(), torch.tensor([-1], dtype=I32).cuda())
+    assert status.tolist() == [5, 5, 0]
+    for b, (owner, upto) in enumerate(((0, block), (0, block - 1), (1, block), (2, 1001))):
+        # (the table ends where 2^31 entries do: its last entry, 2^31 - 1, lies behind the last that counts)
+        score = (k[b, :, 0].double() @ q[owner, 0, 0].double()) / 8
+        want = (score - float(lse[owner])).exp()
+        want[upto:] = 0.0
+        # an exponential is off by 2^-22, its argument by three roundings and by a product of 64 entries summed in fp32
+        reach = (k[b, :, 0].double().abs() @ q[owner, 0, 0].double().abs()) / 8
+        bound = want * ((score.abs() + 3) * 3 * 2.0**-24 + reach * 5 * 2.0**-22 + 2.0**-21)
+        assert bool(((w[b].cpu().double() - want).abs() <= bound).all()), b
+
+
 def test_an_eviction_of_lengths_at_the_end_of_32_bits():
     """A length that the table's columns have room for and the cache has not: nothing moves.  (Blocks that the table names again and again.)"""
     block, width = 2**20, 2048
