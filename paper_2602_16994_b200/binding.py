@@ -500,9 +500,13 @@ class PrefixPlan(NamedTuple):
     table: torch.Tensor          # [groups, W] those blocks
 
 
-def prefix_plan(group, blocks, table) -> PrefixPlan:
+def prefix_plan(group, blocks, table, sharing=None) -> PrefixPlan:
     """The plan of ``prefix_attention`` from each request's ``group`` (negative: it shares nothing), and each group's prefix: its first
     ``blocks[g]`` entries of ``table[g]``.  Made when the requests that share change, kept from step to step and for all layers.
+
+    ``sharing``: how many requests have a group, for a caller that knows it (it is not read from the device).  The members are then those alone;
+    without it all requests are listed, the form of the kernel is chosen as if all of them shared, and scratch is taken for all.  Another number is a
+    plan that does not fit, as ``prefix_attention``'s status tells.
     """
     for name, t in (("group", group), ("blocks", blocks), ("table", table)):
         if t.dtype != torch.int32:
@@ -515,7 +519,13 @@ def prefix_plan(group, blocks, table) -> PrefixPlan:
     place = torch.empty_like(group).scatter_(0, order.indices, at)
     if blocks.numel():
         place = place - first[group.clamp(0, blocks.numel() - 1).long()]
-    return PrefixPlan(group.contiguous(), order.indices.int(), first, place, blocks.contiguous(), table)
+    members = order.indices.int()
+    if sharing is not None:                              # (requests of no group come first)
+        ahead = group.numel() - int(sharing)
+        if not 0 <= ahead <= group.numel():
+            raise RuntimeError("sharing must be a number of requests of group")
+        members, first = members[max(0, min(ahead, group.numel() - 1)):].contiguous(), first - ahead
+    return PrefixPlan(group.contiguous(), members, first, place, blocks.contiguous(), table)
 
 
 def prefix_attention(q, k_cache, v_cache, block_table, lengths, parent, plan, n_nodes=None, scale=None, out=None, want_lse=False,

@@ -24,7 +24,9 @@ int set_prefix_hooks(long long cycles, int hold)
 using namespace specv;
 
 // Two blocks of 128 rows share the loads of a tile where a prefix has, on average, more rows than they, or a request more than one of them (8192 shared keys; one
-// and two blocks: 228 rows 41 and 43 us, 256 rows a prefix of 32 members 265 and 279, 456 rows 64 and 51, 4864 rows 381 and 254).
+// and two blocks: 228 rows 41 and 43 us, 256 rows a prefix of 32 members 265 and 279, 456 rows 64 and 51, 4864 rows 381 and 254).  The rows are those of the
+// members that the plan lists; a plan that lists requests without a group too is taken for one of longer prefixes (128 tokens, two of which share 8192 keys:
+// 253 us, 243 with the two alone).
 static bool two_blocks(const SpecPrefixAttention *p)
 {
     const SpecAttention &a = p->attention;

@@ -195,7 +195,8 @@ class TreeCache:
         for g, (blocks, members) in enumerate(self.prefixes.values()):
             group[sorted(members)] = g
             table[g, :blocks.numel()] = blocks
-        self.plan = binding.prefix_plan(group, torch.tensor([b.numel() for b, _ in self.prefixes.values()], **i32), table)
+        self.plan = binding.prefix_plan(group, torch.tensor([b.numel() for b, _ in self.prefixes.values()], **i32), table,
+                                        sum(len(m) for _, m in self.prefixes.values()))
 
     def release(self, request):
         """Puts the blocks of a request that has ended back behind the free ones; those of a shared prefix when its last member ends.  For the rare end of a

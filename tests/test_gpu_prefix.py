@@ -253,3 +253,17 @@ def test_prefix_attention_refusals():
             call(**bad)
     with pytest.raises(RuntimeError):
         binding.prefix_plan(plan.group.long(), plan.blocks, plan.table)
+
+
+@pytest.mark.parametrize("groups", [[-1] * 126 + [0, 0], [0, -1, 1, -1, 0, 1, -1], [-1, -1, 0], [0, 1, 1, 0]])
+def test_prefix_attention_of_plans_that_list_those_that_share(groups):
+    """The members alone in the plan, few of many requests or all; scratch for them alone; a plan told a wrong number fits nobody."""
+    case = prefix_case(groups, [9, 20][:max(groups) + 1], [(29 * i) % 200 for i in range(len(groups))], chain(1), 16, 4, 128, seed=len(groups))
+    parts, sharing = [x.cuda() for x in case[1]], sum(g >= 0 for g in groups)
+    plan = binding.prefix_plan(*parts, sharing)
+    assert plan.members.numel() == sharing
+    check(case, plan=plan)
+    if sharing < len(groups):
+        w = {k: v.clone() for k, v in ref.attention(**case[0]).items()}
+        w["out"][:], w["lse"][:], w["status"][:] = 0, -math.inf, 1
+        check(case, w, plan=binding.prefix_plan(*parts, sharing - 1))

@@ -69,6 +69,23 @@ def test_prefix_plan():
     assert none.first.numel() == 1 and none.place.numel() == 7
 
 
+def test_prefix_plan_of_those_that_share():
+    """Told how many requests have a group, the plan lists no others."""
+    table = torch.zeros(3, 4, dtype=torch.int32)
+    for groups in ([2, 0, -1, 2, 0, -7, 2], [-1, -1, 1], [0, 0], [-1, 0, 5], [-1, -1]):
+        group, sharing = torch.tensor(groups, dtype=torch.int32), sum(g >= 0 for g in groups)
+        p = binding.prefix_plan(group, torch.tensor([3, 1, 2], dtype=torch.int32), table, sharing)
+        assert p.members.numel() == max(1, sharing) and p.first.dtype == torch.int32
+        first = p.first.tolist()
+        assert 0 <= first[0] and first == sorted(first) and first[-1] <= p.members.numel()
+        for b, g in enumerate(groups):
+            if 0 <= g < 3:
+                assert p.members[first[g] + p.place[b]] == b and first[g] + int(p.place[b]) < first[g + 1]
+    for wrong in (-1, 4):
+        with pytest.raises(RuntimeError, match="sharing"):
+            binding.prefix_plan(torch.tensor([0, -1, 0], dtype=torch.int32), torch.tensor([3, 1, 2], dtype=torch.int32), table, wrong)
+
+
 def test_weights_refusals(lib):  # noqa: F811
     good = dict(B=2, N=19, Hq=8, Hkv=2, D=128, scale=0.1, table_stride=1)
     n = L()

@@ -145,6 +145,14 @@ def test_rows_are_the_same_by_any_name(calls, shared, ended):
     assert cache.plan is None and cache.prefixes == {} and cache.protected.tolist() == [0, 0, 0, 0]
 
 
+def test_a_plan_lists_those_that_share_alone(calls):
+    cache = shared_by_four()
+    cache.share(0, [3])
+    assert cache.plan.members.tolist() == [0, 3] and cache.plan.first.tolist() == [0, 2]
+    cache.release(0)
+    assert cache.plan.members.tolist() == [3] and cache.plan.first.tolist() == [0, 1] and int(cache.plan.place[3]) == 0
+
+
 def test_a_member_is_not_shared_again_by_another_name(calls):
     cache = shared_by_four()
     assert cache.share(-4, [1]) == 8
