@@ -120,6 +120,40 @@ def test_logprobs_of_rows_made_for_the_search(V, order, dtype):
     check_logprobs(torch.stack([z, z.roll(3)]).repeat(200, 1).to(dtype), torch.zeros(400, 1, dtype=I32), 1.0, 20)
 
 
+@pytest.mark.parametrize("value,dtype", [(0.1, torch.float32), (-0.1, torch.float32), (-1.0, torch.bfloat16), (-2.5, torch.float16), (1.0009765625, torch.float16)])
+@pytest.mark.parametrize("R,V", [(1, 128256), (300, 9001)])
+def test_logprobs_of_rows_of_one_value(value, dtype, R, V):
+    """More entries at the search's bound than there is room for, which the bound's bits do or do not name: the lowest indices, all of the same probability."""
+    z, t = torch.full((R, V), value, dtype=dtype), torch.full((R, 1), V - 1, dtype=I32)
+    z[-1, V // 2] += 0.5
+    check_logprobs(z, t, 1.0, 20)
+
+
+def entropy_case(near, D):
+    """A logit alone in a thread's first batch, one `near` above it in a later batch of the same thread, all others far below."""
+    batch = 4 * 256 * (128 // torch.finfo(D).bits)               # entries of a batch of all threads; its first chunk is the first thread's
+    z = torch.full((2, 4 * batch), -1000.0)                      # (a row of four batches goes to one CTA)
+    z[0, 0], z[0, 2 * batch] = 3.0, 3.0 + near
+    z[1, 0], z[1, 2 * batch], z[1, 3 * batch] = 3.0 + near, 3.0, 3.0 + near
+    return z.to(D)
+
+
+@pytest.mark.parametrize("near", [0.125, 2.0, 4.0, 5.5, 6.0, 20.0])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_logprobs_of_little_entropy(near, dtype):
+    """The sums are taken about a logit below the largest, by up to 8 powers of two, and moved at the end: the entropy is off by what that costs, about 8 ln 2
+    times a rounding for each of the two terms, and never below 0; no log probability lies above it."""
+    z = entropy_case(near, dtype)
+    got = binding.token_logprobs(z.cuda(), z.argmax(-1).int().cuda(), top=2)
+    want = ref.logprobs(z, z.argmax(-1).int()[:, None], 1.0, 2)
+    # S and U are off by 2^-22 (an exponential, and one that moves them) and 2^-24 a term (three, added up twice); U's terms are up to 8 ln 2 of S, log S and
+    # U / S each bring that to the entropy
+    off = (got.entropy.cpu().double() - want["entropy"]).abs()
+    assert bool((off <= (1 + 8 * math.log(2)) * 2 * (2 * 2.0**-22 + 6 * 2.0**-24)).all()), off.tolist()
+    assert bool((got.entropy >= 0).all()) and bool((got.logprob <= 0).all()) and bool((got.top_logprobs <= 0).all())
+    check_rows(got, want, z.shape[1], 1.0, 2)
+
+
 def test_logprobs_of_bad_rows_and_tokens():
     z, t = rows(9, 5000, 3, torch.float32, 8)
     z[0, 17], z[1, 4999], z[2, 0] = math.nan, INF, -INF
@@ -234,6 +268,30 @@ def check_evict(c, budget, recent=0):
 @pytest.mark.parametrize("ties", [False, True])
 def test_evict(B, L, block, caches, row, budget, recent, ties):
     check_evict(evict_case(B, L, block, caches, row, seed=B + L, ties=ties), budget, recent)
+
+
+@pytest.mark.parametrize("block,L,budget,recent,protected", [(8, 60000, 30000, 100, None), (1, 5000, 4990, 0, [4500, 10]), (4, 52000, 51990, 3, [0, 4000]),
+                                                             (16, 66000, 500, 0, [20, 0])])
+@pytest.mark.parametrize("ties", [False, True])
+def test_evict_beyond_what_is_on_chip(block, L, budget, recent, protected, ties):
+    """Rows of the table of more than 4096 columns, requests of more than 47104 entries behind the protected ones: what lies beyond is read from memory, the
+    weights while those of earlier entries are written."""
+    c = evict_case(2, L, block, 2, (4,), seed=L, ties=ties, protected=None if protected is None else torch.tensor(protected, dtype=I32))
+    c["lengths"][1] = L - 1                                      # (the second as long: its blocks behind those of the first)
+    c["owned"][1] = (L - 1 + block - 1) // block
+    total = int(c["owned"].sum()) + 3
+    ids = torch.randperm(total, generator=torch.Generator().manual_seed(L)).int()
+    c["block_table"] = torch.full((2, int(c["owned"].max()) + 1), -1, dtype=I32)
+    c["block_table"][0, :c["owned"][0]] = ids[:int(c["owned"][0])]
+    c["block_table"][1, :c["owned"][1]] = ids[int(c["owned"][0]):-3]
+    g = torch.Generator().manual_seed(L + 1)
+    c["cache"] = torch.randn(2, total, block, 4, generator=g).bfloat16()
+    c["weights"] = torch.rand(total, block, generator=g)
+    if ties:
+        c["weights"] = (c["weights"] * 4).floor()
+    c["free_blocks"], c["free_range"] = torch.full((total,), -7, dtype=I32), torch.tensor([total - 2, 3], dtype=I32)
+    want = check_evict(c, budget, recent)
+    assert want["status"].tolist() == [0, 0]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.uint8])
