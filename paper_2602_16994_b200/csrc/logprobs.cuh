@@ -1,8 +1,11 @@
 // Log probabilities of given tokens, entropy and the most probable tokens of rows of logits (spec_token_logprobs).
 //
 // Mathematics.  With m the largest logit and d = z - m: S = sum e^(d / T), U = sum e^(d / T) d; log p(t) = d_t / T - log S,
-// H = log S - U / (S T): both terms of H are at least 0, nothing cancels.  A thread has its own running maximum in place of m and scales its sums
-// when that rises; threads, then CTAs of a cluster, put theirs together.
+// H = log S - U / (S T): both terms of H are at least 0.  A thread takes a reference of its own in place of m, which may lie up to 8 powers of two below its
+// largest logit, and moves its sums when that rises further; threads, then CTAs of a cluster, put theirs together about the largest of all.  Terms of U about
+// a lower reference are positive, and moving it takes them away again: what that leaves is an error of H of up to about 8 ln 2 = 5.5 times that of an
+// exponential (2^-22), whatever H is.  A reference that far below stands for a logit with a probability of at least 2^-8 beside the largest, so H is then above
+// 0.02 and stays positive; where the reference is the largest logit itself, no term is positive.
 //
 // The most probable tokens.  A thread's maximum is that of its logits.  The n-th largest of a CTA's 256 maxima bounds the n-th largest logit from below, since
 // n logits are at least that: after the one pass over the row only the stretches of a thread's logits are read again (from L2) whose
