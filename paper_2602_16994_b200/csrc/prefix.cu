@@ -23,15 +23,17 @@ int set_prefix_hooks(long long cycles, int hold)
 
 using namespace specv;
 
-// Two blocks of 128 rows share the loads of a tile where a prefix has, on average, more rows than they, or a request more than one of them (8192 shared keys; one
-// and two blocks: 228 rows 41 and 43 us, 256 rows a prefix of 32 members 265 and 279, 456 rows 64 and 51, 4864 rows 381 and 254).  The rows are those of the
-// members that the plan lists; a plan that lists requests without a group too is taken for one of longer prefixes (128 tokens, two of which share 8192 keys:
-// 253 us, 243 with the two alone).
+// Two blocks of 128 rows share the loads of a tile where a prefix has, on average, more rows than one block, or a request has.  Long rows of calls, us with one and two
+// blocks, 32 heads to 8 (D = 128): tokens of 2 groups over 16384 shared keys, up to 512 behind them, 128 rows a prefix 90 and 95, 160 rows 134 and 112, 256 rows 161
+// and 148; 8 groups of two trees of 19 nodes over 8192 (152 rows) 154 and 102, of three (228) 164 and 112.  Where what lies behind the prefix is most of the work the
+// second block costs more than it saves, since requests have few rows: 33 tokens, 8192 shared and up to 4096 behind 106 and 113, 160 tokens in 4 groups, 4096 and 4096,
+// 424 and 458; lengths are not known here.  The rows are those of the members that the plan lists; a plan that lists requests without a group too is taken for one
+// of longer prefixes (128 tokens, two of which share 8192 keys: 253, 243 with the two alone).
 static bool two_blocks(const SpecPrefixAttention *p)
 {
     const SpecAttention &a = p->attention;
     const int64_t rows = (int64_t)a.N * (a.Hq / a.Hkv);
-    return a.D <= 128 && (rows > 128 || (p->n_groups > 0 && (int64_t)p->n_members * rows > (int64_t)p->n_groups * 256));
+    return a.D <= 128 && (rows > 128 || (p->n_groups > 0 && (int64_t)p->n_members * rows > (int64_t)p->n_groups * 128));
 }
 static int prefix_check(const SpecPrefixAttention *p)
 {

@@ -57,6 +57,19 @@ def test_prefix_refusals(lib):  # noqa: F811
     assert call(None, 1 << 30) == -5 and call(0x10010, 1 << 30) == -5 and call(0x10000, n.value - 1) == -5
 
 
+def test_prefix_rows_take_two_blocks_beyond_one(lib):  # noqa: F811
+    """The form of the kernel goes by the rows that a prefix has on average: scratch for the CTAs' parts tells which it is."""
+    def bytes_of(members, groups, N=1, D=128):
+        n, s = L(), prefix(B=512, N=N, Hq=8, Hkv=2, D=D, n_members=members, n_groups=groups, topo_seq_stride=0)
+        assert lib.spec_prefix_attention_workspace_bytes(C.byref(s), C.byref(n)) == 0
+        each = 512 + members                                     # (rows that are not cut, and records of units, for every request and member)
+        return n.value - each * 8 * N * (D * 4 + 8)
+    block = 148 * 2 * 128 * (128 * 4 + 8)
+    for members, groups, N, blocks in ((32, 1, 1, 1), (33, 1, 1, 2), (64, 1, 1, 2), (128, 4, 1, 1), (129, 4, 1, 2), (1, 1, 19, 1), (2, 1, 19, 2), (16, 8, 19, 2),
+                                       (2, 2, 19, 1), (1, 1, 33, 2)):
+        assert abs(bytes_of(members, groups, N) - blocks * block) < block // 2, (members, groups, N)
+
+
 def test_prefix_plan():
     """Members in the order of groups, places among them, requests of no group in none."""
     group = torch.tensor([2, 0, -1, 2, 0, 5, 2], dtype=torch.int32)
