@@ -134,7 +134,7 @@ int32_t spec_prefix_attention(const SpecPrefixAttention *given, void *ws, int64_
     p.unit_blocks = (int)((rows + (two ? 255 : 127)) / (two ? 256 : 128));
     p.merge_rows = attend::MERGE_ROWS;
     const auto merging = [&] { return (rows + p.merge_rows - 1) / p.merge_rows * a->Hkv; };         // CTAs of a request in the joining kernel
-    while (p.merge_rows * (a->D / 8) > attend::MERGE_NT && merging() * a->B < 148 * 4) p.merge_rows /= 2;
+    while (p.merge_rows * (a->D / 8) > attend::MERGE_NT && merging() * a->B < ctas * 4) p.merge_rows /= 2;
     p.groups = (int)merging();
     const bool half = a->dtype == SPEC_F16;
     // (boxes: 254 us for 64 requests of 19 nodes; by 16-byte copies 270)

@@ -45,7 +45,7 @@ int32_t spec_token_logprobs(const SpecLogprobs *a, void *stream)
     const int batch = logp::NT * logp::BATCH * (a->dtype == SPEC_F32 ? 4 : 8);
     const int64_t there = a->parent ? std::min<int64_t>(rows, (int64_t)a->B * 4) : rows;
     int C = 1;
-    while (C < logp::CMAX && a->V > std::max(4, 2 * C) * batch && there * 2 * C <= (C == 4 ? 98 : 148)) C *= 2;
+    while (C < logp::CMAX && a->V > std::max(4, 2 * C) * batch && there * 2 * C <= (C == 4 ? sm_ctas() * 2 / 3 : sm_ctas())) C *= 2;
     logp::Params p = {};
     p.B = a->B; p.N = a->N; p.V = a->V; p.K = a->K; p.top = a->top; p.C = C;
     p.logits = a->logits; p.seq_stride = a->seq_stride; p.node_stride = a->node_stride;
@@ -75,7 +75,7 @@ static int weights_check(const SpecWeights *a)
     // (tiles of all heads, and steps of a run, are counted in 32 bits)
     const double tiles = ((double)std::min<int64_t>((int64_t)a->table_width * a->block_size, 0x7FFFFFFF) / weigh::KT + 2) * a->Hkv;
     const double steps = ((double)a->N * (a->Hq / a->Hkv)) / 64 + 1;
-    if (a->B * tiles > 1.0e9 || a->B * tiles * steps / 148 > 1.0e9) return SPEC_ERR_UNSUPPORTED;          // (a tile's length is 2)
+    if (a->B * tiles > 1.0e9 || a->B * tiles * steps / sm_ctas() > 1.0e9) return SPEC_ERR_UNSUPPORTED;          // (a tile's length is 2)
     int64_t all = 0;
     for (int j = 0; j < 3; ++j) all |= a->q_stride[j] | a->k_cache_stride[j];
     if (all % 8 || !aligned(a->q, 16) || !aligned(a->k_cache, 16)) return SPEC_ERR_UNSUPPORTED;
@@ -195,7 +195,7 @@ int32_t spec_cache_evict(const SpecEvict *a, void *ws, int64_t ws_bytes, void *s
     // Slices of a row: 256 bytes, or fewer, down to 32, where that leaves fewer CTAs than two to an SM (a CTA goes through the kept entries in order): one request of
     // 13738 entries 75 us with 32 bytes, 256 with 256; 16 requests 614 and 359.
     p.words = std::min(p.total, 16u);
-    while (p.words > 2 && (int64_t)((p.total + p.words - 1) / p.words) * a->caches * a->B < 148 * 2) p.words /= 2;
+    while (p.words > 2 && (int64_t)((p.total + p.words - 1) / p.words) * a->caches * a->B < sm_ctas() * 2) p.words /= 2;
     p.slices = (int)((p.total + p.words - 1) / p.words);
     if ((int64_t)p.slices * a->caches + 1 > 0x7FFFFFFF) return SPEC_ERR_UNSUPPORTED;
     const cudaStream_t st = (cudaStream_t)stream;
@@ -209,7 +209,7 @@ int32_t spec_cache_evict(const SpecEvict *a, void *ws, int64_t ws_bytes, void *s
         const int e = prepare(kernel, 0, false);
         return e ? e : launch(kernel, grid, evict::MOVE_NT, 0, 0, st, p);
     };
-    const bool few = (int64_t)p.slices * a->caches * a->B < 148 * 4;
+    const bool few = (int64_t)p.slices * a->caches * a->B < sm_ctas() * 4;
     return unit == 16  ? few ? go(evict::spec_evict_move_kernel<uint4, 16>) : go(evict::spec_evict_move_kernel<uint4, 4>)
            : unit == 4 ? go(evict::spec_evict_move_kernel<uint32_t, 4>)
                        : go(evict::spec_evict_move_kernel<unsigned char, 4>);
