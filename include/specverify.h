@@ -441,7 +441,8 @@ int32_t spec_verify_probs(const SpecChains *a, void *stream);
  * A plan that does not fit together (first not rising within [0, n_members], members[first[group[b]] + place[b]] other than b, group[b] >= n_groups,
  * shared_blocks[g] outside [0, prefix_width]) or a length below the prefix: SPEC_DEV_TOPOLOGY for the requests concerned (a `first` that does not rise:
  * for all), whose rows are 0.  A bad block of a prefix hides its keys and gives its members SPEC_DEV_PAGE.
- * `ws`: spec_prefix_attention_workspace_bytes() bytes (a function of the sizes; contents do not matter).
+ * `ws`: spec_prefix_attention_workspace_bytes() bytes (a function of the sizes; contents do not matter).  With groups about 4 (B + n_members) N Hq D of them, for rows
+ * whose two parts are put together at the end: up to four times the output.
  */
 typedef struct {
     SpecAttention attention;          /* window and sinks 0                                           */
@@ -535,6 +536,8 @@ int32_t spec_cache_weights(const SpecWeights *a, void *ws, int64_t ws_bytes, voi
  * the tokens need, or more tokens than the cache has slots or than 2^31 - 65537: SPEC_DEV_PAGE; then nothing of the request moves.  A ring without room for a request's blocks (or a free_range
  * outside it): SPEC_DEV_BLOCKS, the request is shortened but keeps its blocks.  Blocks that hold entries behind protected[b] must be the request's own.
  * No tree is under way: entries behind the committed tokens are not kept.
+ * What lies behind the first entry that goes moves, in all caches, however few go: 16 requests of 4096 entries and 1, 4 or 16 more, 16 caches of 1 KB a row, take
+ * 290, 420 and 490 us, of 8192 entries 500.  A loop that cuts now and then, to a budget so much lower, moves them less often.
  * `ws`: spec_cache_evict_workspace_bytes() bytes.
  */
 typedef struct {

@@ -16,8 +16,8 @@
 // bits do not tell apart (normal rows of 50257 fp32 entries about 60000: 64 of them 266 us, about 0 16; 512 of 151936 about 1000: 2750, about 0 88), and ties of
 // negative entries in any type, whose bits the bound's lower edge does not name (2048 rows of -1 in bf16: 6450 us).
 //
-// What bounds it.  One read of the rows: 2048 rows of 151936 bf16 entries in 130 us, 0.74 of the copy bandwidth (without the most probable 107 us, 0.90; with them
-// the exponentials, the maxima and the search share the issue slots: 59 % of them).  Few rows: latency, of one launch, one row and the exchange in the cluster
+// What bounds it.  One read of the rows: 2048 rows of 151936 bf16 entries in 135 us, 0.71 of the copy bandwidth (140 in a long row of calls; without the most
+// probable 107 us, 0.90; with them the exponentials, the maxima and the search share the issue slots: 59 % of them).  Few rows: latency, of one launch, one row and the exchange in the cluster
 // (1 row 9 to 12 us).
 #pragma once
 #include <cuda_bf16.h>

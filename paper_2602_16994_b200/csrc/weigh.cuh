@@ -5,8 +5,9 @@
 // columns; over the rows, blocks of rows and key heads its sum never leaves its register, and no two CTAs add to the same entry: the order
 // of every sum is fixed.
 //
-// What bounds it.  With many rows the exponentials: 16 a cycle and SM, of which this reaches two thirds (2 stretches of 512 nodes, 32 heads to 8, behind up to 16384 tokens: 180 us; 96
-// of exponentials alone, 64 of products).  Taking one to three of eight by a polynomial instead made that 1 to 5 % longer.  With few rows latency: the keys'
+// What bounds it.  With many rows the exponentials: 16 a cycle and SM, of which this reaches 0.52 (2 stretches of 512 nodes, 32 heads to 8, behind up to 16384 tokens: 184 us; 96
+// of exponentials alone, 64 of products): a warp loads 32 columns, waits for them and takes their exponentials, and four such warps to a scheduler do not cover the
+// loads.  Taking one to three of eight by a polynomial instead made that 1 to 5 % longer.  With few rows latency: the keys'
 // bytes of 8 requests of 19 nodes over 1500 to 4096 keys would take 7.5 us, the call takes 25, of one token over 4096 keys 1.3 and 12: a CTA knows its run
 // after 2.7 us and has its first sums after 6, then a tile and head take 1300 to 2200 cycles.
 //

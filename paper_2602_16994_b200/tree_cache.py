@@ -32,7 +32,8 @@ class TreeCache:
 
     ``weigh``: the attention weight that entries get is added up in ``weights``, over all layers that ``attend`` sees, for ``evict``.  ``protected`` [B]:
     tokens at a request's beginning that are neither weighed nor evicted; 0 again after ``release``.  After an eviction a request's positions run on: its tokens are
-    ``dropped`` more than its entries.
+    ``dropped`` more than its entries.  All nodes of a step's tree add weight, ahead of the verification: those of branches that it rejects, most of a wide tree's, as
+    those of the path that stays.
     """
 
     def __init__(self, batch, layers, num_blocks, block_size, Hkv, D, width, dtype=torch.bfloat16, device="cuda", weigh=False):
@@ -138,7 +139,11 @@ class TreeCache:
         return done
 
     def evict(self, budget, recent=0, stream=None):
-        """``binding.cache_evict`` of all layers, between two steps: requests of more than ``budget`` tokens keep that many."""
+        """``binding.cache_evict`` of all layers, between two steps: requests of more than ``budget`` tokens keep that many.
+
+        What lies behind the first entry that goes moves, in all layers, however few go: calls every so many steps, to a budget so much lower, cost less
+        than one a step (16 requests of 4096 tokens, 16 caches of 1 KB a token: 290 us for 1 token too many, 490 for 16, 500 for 4096).
+        """
         if self.weights is None:
             raise RuntimeError("evict needs a cache made with weigh=True")
         done = binding.cache_evict(self.storage, self.weights, self.lengths, self.block_table, self.owned, self.free_blocks, self.free_range, budget,
@@ -163,6 +168,9 @@ class TreeCache:
         """Empty ``rows`` begin with the tokens of ``request`` so far, as many as fill whole blocks, which all of them then hold together: what they attend
         to there is read once.  Returns the number of tokens; the ones behind are the rows' own to write again.  Between two steps; for the
         rare beginning of a request: reads tables on the host.
+
+        A group keeps the members that it began with until they end: no rows join it later, and its last member is protected as it was.  Requests that come
+        later share with one that is in no group, which has the prompt written for itself once more.
         """
         request, rows = self._row(request), [self._row(x) for x in rows]
         n = int(self.lengths[request]) // self.block_size
