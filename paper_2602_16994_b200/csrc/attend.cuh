@@ -697,6 +697,7 @@ template <typename T, typename S> __global__ void __launch_bounds__(S::NT, 1) sp
     }
     grid_dependency_wait();
     grid_launch_dependents();                  // (the joining kernel's CTAs may be placed beside this one's; they wait by themselves)
+    static_assert(S::NT / 32 <= (int)(sizeof(B->sums) / sizeof(int)), "an entry of sums for every warp");
     const Cuts cuts = find_request<S::SH>(P, S::ROWS, c, B->sums, B->found, tid, S::NT);
     if (lane == 0) {
         hand->run.left = cuts.start(c + 1) - cuts.start(c);
